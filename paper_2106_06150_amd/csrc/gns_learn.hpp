@@ -1,0 +1,150 @@
+// What the kernels of training and answering share: rows of either type, the row count, launches (gfx950, wave64).
+#pragma once
+#include "../../include/gns_learn.h"
+#include "gns_internal.h"
+#include "gns_device.hpp"
+
+namespace gns {
+
+struct Bf16 { uint16_t bits; };
+
+// A row count that the host knows or the device holds (rows is then the worst case).
+struct RowCount {
+    int32_t rows;
+    const int32_t* rows_dev;
+    __device__ __forceinline__ int32_t get() const { return rows_dev ? (*rows_dev < rows ? *rows_dev : rows) : rows; }
+};
+
+struct ConstRows {
+    const void* data;
+    int64_t stride;
+    int32_t width;
+};
+
+struct MutRows {
+    void* data;
+    int64_t stride;
+    int32_t width;
+};
+
+template <typename T> __device__ __forceinline__ float to_float(T v);
+template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_float<Bf16>(Bf16 v) { return __uint_as_float((uint32_t) v.bits << 16); }
+
+// Rounded to nearest, ties to even; a NaN stays one.
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ Bf16 from_float<Bf16>(float v)
+{
+    return Bf16{__builtin_bit_cast(uint16_t, (__bf16) v)};
+}
+
+template <typename T>
+__device__ __forceinline__ float load_at(const ConstRows& x, int64_t r, int64_t c)
+{
+    return to_float<T>(reinterpret_cast<const T*>(x.data)[r * x.stride + c]);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_at(const MutRows& x, int64_t r, int64_t c, float v)
+{
+    reinterpret_cast<T*>(x.data)[r * x.stride + c] = from_float<T>(v);
+}
+
+constexpr uint32_t kInfBits = 0x7F800000u;
+__device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+__device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7FC00000u); }
+
+// max(0, v) that keeps a NaN
+__device__ __forceinline__ float relu_of(float v) { return v < 0.f ? 0.f : v; }
+
+struct QuantizeArgs {
+    ConstRows x1, x2;             // x2.width 0: one input
+    int8_t* q;
+    float* scale;
+    int64_t stride;               // of q
+    RowCount count;
+};
+
+struct DenseInt8Args {
+    const int8_t* q;
+    const float* scale;
+    const int8_t* wq;
+    const float* w_scale;
+    const float* bias;
+    MutRows out;
+    int64_t stride;               // of q and wq
+    int32_t k, relu;
+    RowCount count;
+};
+
+struct CheckpointArgs {
+    ConstRows x;                  // save
+    MutRows out;                  // load
+    int8_t* q;
+    uint8_t* exponents;
+    uint32_t* positive;
+    int32_t width, groups;
+    RowCount count;
+};
+
+struct PackedRows {
+    const int8_t* q;
+    const uint8_t* exponents;
+    int32_t width, groups;
+};
+
+struct BackwardArgs {
+    ConstRows d_out;
+    const uint32_t* positive;
+    PackedRows x1, x2;
+    const float* w;
+    float* dw;
+    float* db;
+    MutRows dx;
+    int32_t hdim;
+    RowCount count;
+    float* partial;               // workspace
+};
+
+struct LogProbsArgs {
+    ConstRows logits;
+    const int32_t* labels;
+    float* logp;
+    float* entropy;
+    float* stats;
+    int32_t* top_index;
+    float* top_logp;
+    int32_t top;
+    RowCount count;
+    void* workspace;
+};
+
+struct LogProbsBackwardArgs {
+    ConstRows logits;
+    const int32_t* labels;
+    const float* stats;
+    const float* entropy;
+    const float* g_logp;
+    const float* g_entropy;
+    MutRows d_logits;
+    RowCount count;
+};
+
+// gns_int8.hip
+hipError_t launch_quantize(const gns_ctx* c, const QuantizeArgs& a, int32_t type, hipStream_t s);
+hipError_t launch_dense_int8(const gns_ctx* c, const DenseInt8Args& a, int32_t out_type, hipStream_t s);
+hipError_t launch_sage_dense_int8(const gns_ctx* c, const QuantizeArgs& x, const DenseInt8Args& a, int32_t type, int32_t out_type,
+                                  hipStream_t s);
+// gns_checkpoint.hip
+hipError_t launch_checkpoint_save(const gns_ctx* c, const CheckpointArgs& a, int32_t type, hipStream_t s);
+hipError_t launch_checkpoint_load(const gns_ctx* c, const CheckpointArgs& a, int32_t type, hipStream_t s);
+// gns_backward.hip
+size_t backward_workspace(const gns_ctx* c, int32_t k, int32_t hdim, int32_t rows);
+hipError_t launch_backward(const gns_ctx* c, const BackwardArgs& a, int32_t type, hipStream_t s);
+// gns_log_probs.hip
+size_t log_probs_workspace(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows);
+hipError_t launch_log_probs(const gns_ctx* c, const LogProbsArgs& a, int32_t type, hipStream_t s);
+hipError_t launch_log_probs_backward(const gns_ctx* c, const LogProbsBackwardArgs& a, int32_t type, int32_t out_type, hipStream_t s);
+
+}  // namespace gns

@@ -1,0 +1,769 @@
+"""The operators of include/gns_learn.h on the GPU against plain implementations in 64 bits, through the C ABI.
+
+Error bounds follow from the arithmetic: u = 2^-24 is one rounding to fp32.  A sum of n products in fp32, in any order, is off by
+at most n roundings of the sum of magnitudes; n * 2u leaves room for products split into terms and for matrix cores that cut
+where they add.  A result stored in bf16 is off by 2^-9 of itself besides.
+"""
+import math
+import zlib
+
+import numpy as np
+import pytest
+import torch
+
+from conftest import random_symmetric_csr
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    from paper_2106_06150_amd import binding as B
+    from paper_2106_06150_amd import learn, synth
+    from gpu_harness import GpuGns
+
+U = 2.0 ** -24
+FP32, BF16 = torch.float32, torch.bfloat16
+TYPES = pytest.mark.parametrize("dtype", [FP32, BF16], ids=["fp32", "bf16"])
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    dev = torch.device("cuda:0")
+    graph = B.make_graph(torch.tensor([0, 1, 2], dtype=torch.int32, device=dev), torch.tensor([1, 0], dtype=torch.int32, device=dev))
+    config = B.make_config([1], [B.GNS_UNIFORM], 0, 1)
+    workspace = B.alloc_workspace(graph, config, dev)
+    c = B.gns_create(graph, config, workspace)
+    yield c
+    torch.cuda.synchronize()
+    B.gns_destroy(c)
+
+
+def layout(t, how):
+    """The 2-D tensor on the GPU with its rows adjacent, further apart, or off the 16-byte marks."""
+    t = t.cuda()
+    if how == "packed":
+        return t.contiguous()
+    rows, width = t.shape
+    pad, first = (16, 0) if how == "strided" else (3, 1)
+    wide = torch.full((rows, width + pad + first), float("nan"), dtype=t.dtype, device="cuda")
+    view = wide[:, first:first + width]
+    view.copy_(t)
+    return view
+
+
+LAYOUTS = ("packed", "strided", "odd")
+
+
+def gen(*key):
+    return torch.Generator().manual_seed(zlib.crc32(repr(key).encode()))
+
+
+def within(got, want, bound):
+    got, want, bound = (np.asarray(v, dtype=np.float64) for v in (got, want, bound))
+    bound = np.broadcast_to(bound, want.shape)
+    odd = ~np.isfinite(want)
+    assert np.array_equal(got[odd], want[odd], equal_nan=True)
+    off = np.abs(got[~odd] - want[~odd])
+    assert np.all(off <= bound[~odd]), (float(np.max(off / np.maximum(bound[~odd], 1e-300))), int(np.argmax(off)))
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+# ---- 8-bit rows and their product -------------------------------------------------------------------------------
+def ref_quantize(x):
+    """q and scale of rows, each operation in fp32 as the definition says."""
+    x = x.float().numpy()
+    with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
+        amax = np.abs(x).max(1).astype(np.float32)
+        bad, none = ~np.isfinite(amax), amax < np.float32(2.0 ** -120)
+        inv = np.where(bad | none, np.float32(0), np.float32(127) / amax).astype(np.float32)
+        q = np.where((bad | none)[:, None], 0, np.rint((x * inv[:, None]).astype(np.float32)))
+        scale = np.where(bad, np.float32(np.nan), np.where(none, np.float32(0), amax / np.float32(127)))
+    return q.astype(np.int64), scale.astype(np.float32)
+
+
+def special_rows(x):
+    """Rows of zeros, of tiny values, with an infinity, a NaN, the type's largest value."""
+    for i, v in enumerate((0.0, 1e-37, math.inf, math.nan, torch.finfo(x.dtype).max)):
+        if x.shape[0] > i + 1:
+            if i < 2:
+                x[i + 1] = v
+            else:
+                x[i + 1, x.shape[1] // 2] = v
+    return x
+
+
+@TYPES
+@pytest.mark.parametrize("how", LAYOUTS)
+@pytest.mark.parametrize("rows,f1,f2", [(1, 1, 0), (3, 5, 0), (9, 63, 1), (9, 64, 64), (33, 65, 31), (130, 100, 28), (7, 4096, 0),
+                                        (6, 1000, 3001), (300, 128, 128), (2, 20000, 0)])
+def test_quantize_rows(ctx, rows, f1, f2, how, dtype):
+    x = special_rows((torch.randn(rows, f1 + f2, generator=gen(rows, f1, f2)) * 3).to(dtype))
+    k = f1 + f2
+    q = torch.full((rows, learn.int8_stride(k)), 77, dtype=torch.int8, device="cuda")
+    scale = torch.full((rows,), -1.0, device="cuda")
+    learn.gns_quantize_rows(ctx, layout(x[:, :f1], how), layout(x[:, f1:], how) if f2 else None, q, scale, rows)
+    want_q, want_scale = ref_quantize(x)
+    assert np.array_equal(q[:, :k].cpu().numpy(), want_q)
+    assert not q[:, k:].any()
+    assert np.array_equal(scale.cpu().numpy(), want_scale, equal_nan=True)
+
+
+def check_int8(out, q, scale, w, w_scale, bias, relu):
+    """out against 64 bits: three products, one sum, one rounding to its type."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        y = (q @ w.T).astype(np.float64) * scale.astype(np.float64)[:, None] * w_scale.astype(np.float64)
+        b = np.zeros(w.shape[0]) if bias is None else f64(bias)
+        size = np.abs(y) + np.abs(b)
+        y = y + b
+        y = np.where(np.abs(y) > float(torch.finfo(out.dtype).max), np.sign(y) * np.inf, y)      # what the type does not hold
+        if relu:
+            y = np.where(y < 0, 0.0, y)
+    bound = 4 * U * size
+    if out.dtype == BF16:
+        bound = bound + 2.0 ** -8 * np.abs(y)
+    within(f64(out), y, bound + 2.0 ** -133)
+
+
+@TYPES
+@pytest.mark.parametrize("rows,k,n", [(1, 1, 1), (1, 64, 7), (1, 4096, 515), (2, 1000, 33), (5, 257, 64), (16, 512, 129), (17, 96, 96),
+                                      (64, 2048, 40), (65, 65, 65), (130, 300, 47), (257, 128, 256), (1000, 256, 172), (300, 1024, 1027)])
+def test_int8_product(ctx, rows, k, n, dtype):
+    g = gen(rows, k, n)
+    q = torch.randint(-127, 128, (rows, learn.int8_stride(k)), generator=g, dtype=torch.int8)
+    w = torch.randint(-127, 128, (n, learn.int8_stride(k)), generator=g, dtype=torch.int8)       # padding of any content
+    q[:, k:] = 0
+    q[0] = torch.where(torch.arange(q.shape[1]) < k, 127, 0)                                     # the largest sums
+    w[0, :k] = -127
+    scale, w_scale = torch.rand(rows, generator=g) * 0.05, torch.rand(n, generator=g) * 0.01
+    bias = torch.randn(n, generator=g) if n % 2 else None
+    relu = rows % 2 == 0
+    for how in LAYOUTS:
+        out = layout(torch.full((rows, n), 9.0, dtype=dtype), how)
+        learn.gns_dense_int8(ctx, q.cuda(), scale.cuda(), k, w.cuda(), w_scale.cuda(), None if bias is None else bias.cuda(), relu, out, rows)
+        check_int8(out, q[:, :k].numpy().astype(np.int64), scale.numpy(), w[:, :k].numpy().astype(np.int64), w_scale.numpy(), bias, relu)
+
+
+@TYPES
+@pytest.mark.parametrize("rows,f1,f2,n", [(1, 3, 0, 5), (1, 4096, 0, 300), (1, 100, 28, 47), (4, 700, 0, 130), (7, 256, 256, 48), (8, 64, 0, 1),
+                                          (16, 1024, 1, 64), (33, 129, 0, 65), (200, 128, 128, 256), (700, 300, 212, 100)])
+@pytest.mark.parametrize("how", LAYOUTS)
+def test_update_step_in_int8(ctx, rows, f1, f2, n, how, dtype):
+    g = gen(rows, f1, f2, n)
+    k = f1 + f2
+    x = special_rows((torch.randn(rows, k, generator=g) * 2).to(dtype))
+    w = torch.randint(-127, 128, (n, learn.int8_stride(k)), generator=g, dtype=torch.int8)
+    w_scale, bias = torch.rand(n, generator=g) * 0.01, torch.randn(n, generator=g)
+    out = layout(torch.zeros(rows, n, dtype=dtype), how)
+    space = learn.alloc_workspace(learn.gns_sage_dense_int8_workspace_bytes(ctx, k, rows))
+    learn.gns_sage_dense_int8(ctx, layout(x[:, :f1], how), layout(x[:, f1:], how) if f2 else None, w.cuda(), w_scale.cuda(),
+                              bias.cuda(), True, out, rows, space)
+    q, scale = ref_quantize(x)
+    check_int8(out, q, scale, w[:, :k].numpy().astype(np.int64), w_scale.numpy(), bias, True)
+
+
+# ---- checkpoints --------------------------------------------------------------------------------------------------
+def ref_checkpoint(x):
+    """(values in 64 bits with NaN for spoilt groups, exponent bytes, positive words) from the definition."""
+    x = x.double().numpy()
+    rows, dim = x.shape
+    groups = (dim + 31) // 32
+    padded = np.zeros((rows, groups * 32))
+    padded[:, :dim] = x
+    g = padded.reshape(rows, groups, 32)
+    positive = ((g > 0) << np.arange(32)).sum(2).astype(np.uint32)
+    with np.errstate(invalid="ignore"):
+        a = np.abs(g).max(2)
+        bad, none = ~np.isfinite(a), a < 2.0 ** -100
+        safe = np.where(bad | none, 1.0, a)
+        e = np.floor(np.log2(safe)).astype(int) - 8
+        for _ in range(4):
+            e = e + (safe >= 127.5 * np.exp2(e))
+        e = np.minimum(e, 121)
+        q = np.clip(np.rint(g / np.exp2(e)[:, :, None]), -127, 127)
+        values = np.where(none[:, :, None], 0.0, q * np.exp2(e)[:, :, None])
+        values[bad] = np.nan
+    byte = np.where(bad, 255, np.where(none, 0, e + 127)).astype(np.uint8)
+    return values.reshape(rows, groups * 32)[:, :dim], byte, positive
+
+
+def save(ctx, x, how="packed"):
+    rows, dim = x.shape
+    groups = learn.checkpoint_groups(dim)
+    q = torch.full((rows, groups * 32), 55, dtype=torch.int8, device="cuda")
+    e = torch.full((rows, groups), 7, dtype=torch.uint8, device="cuda")
+    positive = torch.zeros((rows, groups), dtype=torch.int32, device="cuda")
+    learn.gns_checkpoint_save(ctx, layout(x, how), q, e, positive, rows)
+    return q, e, positive
+
+
+@TYPES
+@pytest.mark.parametrize("how", LAYOUTS)
+@pytest.mark.parametrize("rows,dim", [(1, 1), (3, 31), (5, 32), (7, 33), (64, 100), (33, 128), (2, 4096), (3, 8191), (700, 65), (129, 256)])
+def test_checkpoint_is_the_definition_to_the_bit(ctx, rows, dim, how, dtype):
+    g = gen(rows, dim)
+    x = torch.randn(rows, dim, generator=g) * torch.exp2(torch.randint(-20, 20, (rows, dim), generator=g).float())
+    x = x.to(dtype)
+    x[0, 0] = 0.0
+    if rows > 2:                                          # groups of zeros, of the smallest that counts, of what is below
+        x[1] = 0.0
+        x[2, :32] = torch.linspace(-1, 1, min(32, dim)) * 2.0 ** -100
+        x[2, 32:64] = 2.0 ** -101
+    if rows > 6:
+        x[3, 0], x[4, dim - 1], x[5, 0] = math.inf, math.nan, torch.finfo(dtype).max
+        x[6, :2] = torch.tensor([127.0, 0.5])             # a step of one, and a tie
+    if rows > 32:
+        x[7, 0], x[8, 0] = 127.5, 127.25                  # the next power of two, and the last of this one
+    values, byte, words = ref_checkpoint(x)
+    q, e, positive = save(ctx, x, how)
+    assert np.array_equal(e.cpu().numpy(), byte)
+    assert np.array_equal(positive.cpu().numpy().view(np.uint32), words)
+    assert not q[:, dim:].any()
+    for out_type in (FP32, BF16):
+        for out_how in LAYOUTS:
+            out = layout(torch.zeros(rows, dim, dtype=out_type), out_how)
+            learn.gns_checkpoint_load(ctx, q, e, out, rows)
+            assert np.array_equal(f64(out), values, equal_nan=True)
+    bare = torch.empty_like(q), torch.empty_like(e)
+    learn.gns_checkpoint_save(ctx, layout(x, how), *bare, None, rows)
+    assert torch.equal(bare[0], q) and torch.equal(bare[1], e)
+
+
+def test_checkpoint_is_at_most_half_a_step_off(ctx):
+    x = torch.randn(500, 64, generator=gen("step"))
+    q, e, _ = save(ctx, x)
+    out = torch.empty(500, 64, device="cuda")
+    learn.gns_checkpoint_load(ctx, q, e, out, 500)
+    step = np.exp2(e.cpu().numpy().astype(float) - 127).repeat(32, 1)
+    assert np.all(np.abs(f64(out) - f64(x)) <= step / 2)
+    assert np.all(step <= np.abs(f64(x)).reshape(500, 2, 32).max(2).repeat(32, 1) / 63.75)
+
+
+# ---- backward pass ------------------------------------------------------------------------------------------------
+def backward_case(ctx, rows, f1, f2, hdim, dtype, relu, how):
+    g = gen(rows, f1, f2, hdim, relu)
+    parts = [save(ctx, torch.randn(rows, f, generator=g) * torch.exp(torch.randn(1, f, generator=g))) if f else None for f in (f1, f2)]
+    x = np.zeros((rows, 0))
+    for p, f in zip(parts, (f1, f2)):
+        if f:
+            scale = np.exp2(p[1].cpu().numpy().astype(float) - 127).repeat(32, 1)
+            x = np.concatenate([x, (p[0].cpu().numpy() * scale)[:, :f]], 1)
+    d_out = (torch.randn(rows, hdim, generator=g) * 1e-2 * torch.exp(torch.randn(rows, 1, generator=g))).to(dtype)
+    mask = torch.rand(rows, hdim, generator=g) < 0.5
+    w = torch.randn(f1 + f2, hdim, generator=g) / math.sqrt(f1 + f2)
+    positive = None
+    dz = f64(d_out)
+    if relu:
+        words = np.zeros((rows, learn.checkpoint_groups(hdim) * 32), dtype=np.int64)
+        words[:, :hdim] = mask.numpy()
+        words = (words.reshape(rows, -1, 32) << np.arange(32)).sum(2).astype(np.uint32).view(np.int32)
+        positive = torch.from_numpy(words).cuda()
+        dz = np.where(mask.numpy(), dz, 0.0)
+        spoilt = torch.rand(rows, hdim, generator=g) < 0.02       # what a masked place holds does not matter
+        d_out[~mask & spoilt] = math.nan
+        d_out[~mask & ~spoilt & (torch.rand(rows, hdim, generator=g) < 0.02)] = math.inf
+    return parts, x, layout(d_out, how), positive, dz, w
+
+
+def run_backward(ctx, parts, f1, f2, d_out, positive, w, want_dx=True, want_dw=True, rows=None, how="packed"):
+    rows, hdim = d_out.shape[0] if rows is None else rows, d_out.shape[1]
+    dw = torch.full((f1 + f2, hdim), 3.0, device="cuda") if want_dw else None
+    db = torch.full((hdim,), 3.0, device="cuda") if want_dw else None
+    dx = layout(torch.full((d_out.shape[0], f1 + f2), 3.0, dtype=d_out.dtype), how) if want_dx else None
+    space = learn.alloc_workspace(learn.gns_sage_dense_backward_workspace_bytes(ctx, f1, f2, hdim, rows))
+    one, two = (p if p is None else p[:2] for p in parts)
+    learn.gns_sage_dense_backward(ctx, d_out, positive, one, f1, two, f2, w.cuda(), dw, db, dx, rows, space)
+    return dw, db, dx
+
+
+def check_backward(dw, db, dx, x, dz, w, dtype):
+    rows, hdim = dz.shape
+    if dw is not None:
+        within(f64(dw), x.T @ dz, (rows + 8) * 2 * U * (np.abs(x).T @ np.abs(dz)))
+        within(f64(db), dz.sum(0), (rows + 8) * 2 * U * np.abs(dz).sum(0))
+    if dx is not None:
+        want, size = dz @ f64(w).T, np.abs(dz) @ np.abs(f64(w)).T
+        bound = (hdim + 8) * 2 * U * size
+        if dtype == BF16:
+            bound = bound + 2.0 ** -16 * size + 2.0 ** -8 * np.abs(want)
+        within(f64(dx), want, bound + 2.0 ** -126)
+
+
+BACKWARD_SHAPES = [(1, 1, 0, 1), (2, 3, 2, 5), (31, 32, 0, 32), (33, 33, 31, 65), (64, 64, 64, 64), (100, 47, 0, 172), (129, 128, 128, 130),
+                   (300, 100, 28, 47), (1000, 20, 300, 256), (513, 257, 0, 385), (2500, 128, 128, 256), (70, 1030, 0, 516)]
+
+
+@TYPES
+@pytest.mark.parametrize("relu", [False, True], ids=["identity", "relu"])
+@pytest.mark.parametrize("rows,f1,f2,hdim", BACKWARD_SHAPES)
+def test_backward(ctx, rows, f1, f2, hdim, relu, dtype):
+    for how in LAYOUTS:
+        parts, x, d_out, positive, dz, w = backward_case(ctx, rows, f1, f2, hdim, dtype, relu, how)
+        check_backward(*run_backward(ctx, parts, f1, f2, d_out, positive, w, how=how), x, dz, w, dtype)
+
+
+@TYPES
+@pytest.mark.parametrize("rows,f1,f2,hdim", [(20000, 128, 128, 256), (3000, 1024, 0, 1024), (9001, 300, 0, 47), (40000, 64, 36, 40), (600, 2000, 97, 1500)])
+def test_backward_of_many_rows_or_wide_layers(ctx, rows, f1, f2, hdim, dtype):
+    parts, x, d_out, positive, dz, w = backward_case(ctx, rows, f1, f2, hdim, dtype, True, "packed")
+    check_backward(*run_backward(ctx, parts, f1, f2, d_out, positive, w), x, dz, w, dtype)
+
+
+@TYPES
+def test_backward_alone_and_in_parts(ctx, dtype):
+    rows, f1, f2, hdim = 500, 96, 40, 72
+    parts, x, d_out, positive, dz, w = backward_case(ctx, rows, f1, f2, hdim, dtype, True, "packed")
+    whole = run_backward(ctx, parts, f1, f2, d_out, positive, w)
+    again = run_backward(ctx, parts, f1, f2, d_out, positive, w)
+    assert all(torch.equal(a, b) for a, b in zip(whole, again))
+    weights, _, none = run_backward(ctx, parts, f1, f2, d_out, positive, w, want_dx=False)
+    assert none is None and torch.equal(weights, whole[0])
+    _, _, dx = run_backward(ctx, (None, None), f1, f2, d_out, positive, w, want_dw=False)
+    assert torch.equal(dx, whole[2])
+
+
+@TYPES
+def test_backward_of_no_rows(ctx, dtype):
+    parts, _, d_out, positive, _, w = backward_case(ctx, 4, 40, 8, 24, dtype, True, "packed")
+    dw, db, dx = run_backward(ctx, parts, 40, 8, d_out, positive, w, rows=0)
+    assert not dw.any() and not db.any() and bool((dx == 3.0).all())
+
+
+def test_backward_against_differences(ctx):
+    """dw and dx of sum(c * relu([x1 | x2] w + b)) against central differences of that function in 64 bits."""
+    rows, f1, f2, hdim = 40, 9, 24, 17
+    parts, x, c, _, _, w = backward_case(ctx, rows, f1, f2, hdim, FP32, False, "packed")
+    bias = torch.randn(hdim, generator=gen("bias"))
+    z = torch.from_numpy(x) @ w.double() + bias.double()
+    positive = save(ctx, torch.clamp(z, min=0.0).float())[2]
+    dw, db, dx = run_backward(ctx, parts, f1, f2, c, positive, w)
+
+    def loss(x_, w_, b_):
+        return float((np.maximum(x_ @ w_ + b_, 0.0) * f64(c)).sum())
+
+    rng, eps = np.random.default_rng(3), 1e-6
+    for got, which in ((dw, 1), (db, 2), (dx, 0)):
+        for _ in range(20):
+            at = tuple(int(rng.integers(0, s)) for s in got.shape)
+            ends = []
+            for sign in (1, -1):
+                args = [x.copy(), f64(w).copy(), f64(bias).copy()]
+                args[which][at] += sign * eps
+                ends.append(loss(*args))
+            # a kink within eps of a value is as good as never met; the difference itself is good to 1e-16 / eps of the loss
+            assert abs(float(got[at]) - (ends[0] - ends[1]) / (2 * eps)) < 1e-5
+
+
+# ---- log probabilities --------------------------------------------------------------------------------------------
+def ref_log_probs(z, labels, top):
+    z = z.double().numpy()
+    rows, classes = z.shape
+    with np.errstate(invalid="ignore", divide="ignore"):
+        bad = np.isnan(z).any(1) | (z == np.inf).any(1)
+        none = ~bad & (z == -np.inf).all(1)
+        m = np.where(bad, np.nan, z.max(1))
+        d = z - np.where(none, 0.0, m)[:, None]
+        p = np.exp(d)
+        s = p.sum(1)
+        log_s = np.where(none, 0.0, np.log(np.where(none, 1.0, s)))
+        weighted = np.where(p > 0, p * np.where(p > 0, d, 0.0), 0.0).sum(1)
+        entropy = np.where(none, 0.0, log_s - weighted / np.where(none, 1.0, s))
+        entropy[bad] = np.nan
+        log_p = d - log_s[:, None]
+        log_p[none] = -np.inf
+        log_p[bad] = np.nan
+        log_p[log_p < -float(torch.finfo(FP32).max)] = -np.inf       # what fp32 does not hold
+    logp = np.array([np.nan if bad[r] or labels[r] >= classes else 0.0 if labels[r] < 0 else log_p[r, labels[r]] for r in range(rows)])
+    index = np.full((rows, top), -1, dtype=np.int64)
+    value = np.full((rows, top), -np.inf)
+    value[bad] = np.nan
+    for r in range(rows):
+        if bad[r]:
+            continue
+        best = [j for j in np.argsort(-z[r], kind="stable")[:top] if z[r, j] > -np.inf]
+        index[r, :len(best)] = best
+        value[r, :len(best)] = log_p[r, best]
+    chain = min(classes, 64 + classes / 64) + 16                # sequential additions of a lane, and what joins the lanes
+    log_tol = U * 2 * (chain + 2 * np.abs(np.nan_to_num(log_s)))
+    tol = dict(logp=log_tol, entropy=U * 2 * chain * (1 + np.abs(np.nan_to_num(entropy)) + np.abs(np.nan_to_num(log_s))),
+               value=lambda v: log_tol[:, None] + 4 * U * np.abs(np.nan_to_num(v, neginf=0.0)))
+    return logp, entropy, m, log_s, index, value, tol
+
+
+def logits_case(rows, classes, dtype):
+    g = gen(rows, classes, str(dtype))
+    z = torch.randn(rows, classes, generator=g) * 3 + 5 * torch.randn(rows, 1, generator=g)
+    z = z.to(dtype)
+    labels = torch.randint(0, classes, (rows,), generator=g, dtype=torch.int32)
+    lowest = torch.finfo(dtype).min
+    fills = [lambda r: r.fill_(-math.inf),                                          # nothing left
+             lambda r: r.fill_(lowest),                                             # all at the lowest value: uniform
+             lambda r: r[: max(1, classes // 2)].fill_(lowest),
+             lambda r: r.masked_fill_(torch.rand(classes, generator=g) < 0.7, -math.inf),
+             lambda r: r.fill_(0.25),                                               # ties
+             lambda r: r.copy_(torch.where(torch.arange(classes) % 2 == 0, 0.0, -0.0)),
+             lambda r: r[classes - 1].fill_(math.nan),
+             lambda r: r[0].fill_(math.inf),
+             lambda r: r.copy_(torch.sort(r).values),
+             lambda r: (r.fill_(-math.inf), r[classes // 2].fill_(1000.0)),         # a single class
+             lambda r: r.add_(3000.0),
+             lambda r: (r.fill_(torch.finfo(dtype).min), r[classes // 3].fill_(torch.finfo(dtype).max))]
+    for i, fill in enumerate(fills):
+        if rows > i + 1:
+            fill(z[i + 1])
+    if rows > 20:
+        labels[15], labels[16], labels[17] = -1, classes, -7
+    return z, labels
+
+
+def run_log_probs(ctx, z, labels, top, rows=None):
+    rows = z.shape[0] if rows is None else rows
+    n = z.shape[0]
+    out = dict(logp=torch.full((n,), 9.0, device="cuda"), entropy=torch.full((n,), 9.0, device="cuda"),
+               stats=torch.full((n, 2), 9.0, device="cuda"),
+               index=torch.full((n, top), 99, dtype=torch.int32, device="cuda") if top else None,
+               value=torch.full((n, top), 9.0, device="cuda") if top else None)
+    space = learn.alloc_workspace(learn.gns_log_probs_workspace_bytes(ctx, z.shape[1], top, rows))
+    learn.gns_log_probs(ctx, z, labels.cuda(), out["logp"], out["entropy"], out["stats"], out["index"], out["value"], rows, space)
+    return out
+
+
+LOG_PROBS_SHAPES = [(1, 1, 1), (3, 2, 5), (30, 3, 2), (70, 47, 5), (33, 64, 32), (40, 65, 1), (130, 172, 20), (25, 255, 32), (26, 1000, 10),
+                    (25, 1025, 32), (24, 4097, 20), (3, 16384, 7), (24, 20011, 32), (2, 100003, 20), (1, 131072, 32)]
+
+
+@TYPES
+@pytest.mark.parametrize("rows,classes,top", LOG_PROBS_SHAPES)
+def test_log_probs(ctx, rows, classes, top, dtype):
+    z, labels = logits_case(rows, classes, dtype)
+    logp, entropy, m, log_s, index, value, tol = ref_log_probs(z, labels.numpy(), top)
+    for how in LAYOUTS:
+        out = run_log_probs(ctx, layout(z, how), labels, top)
+        within(f64(out["logp"]), logp, tol["value"](logp[:, None])[:, 0])
+        within(f64(out["entropy"]), entropy, tol["entropy"])
+        within(f64(out["stats"][:, 0]), m, 0.0)
+        within(f64(out["stats"][:, 1]), np.where(np.isnan(m), np.nan, log_s), tol["logp"])
+        assert np.array_equal(out["index"].cpu().numpy(), index)
+        within(f64(out["value"]), value, tol["value"](value))
+
+
+@TYPES
+def test_log_probs_of_single_outputs(ctx, dtype):
+    z, labels = logits_case(40, 300, dtype)
+    full = run_log_probs(ctx, z.cuda(), labels, 8)
+    for want in (("logp",), ("entropy",), ("stats",), ("index", "value")):
+        some = {k: torch.empty_like(full[k]) if k in want else None for k in full}
+        top = 8 if "index" in want else 0
+        space = learn.alloc_workspace(learn.gns_log_probs_workspace_bytes(ctx, 300, top, 40))
+        learn.gns_log_probs(ctx, z.cuda(), labels.cuda() if "logp" in want else None, some["logp"], some["entropy"], some["stats"],
+                            some["index"], some["value"], 40, space)
+        for k in want:
+            assert np.array_equal(f64(some[k]), f64(full[k]), equal_nan=True), k
+
+
+@TYPES
+@pytest.mark.parametrize("entropy_term", [False, True])
+@pytest.mark.parametrize("rows,classes", [(1, 1), (3, 2), (70, 47), (130, 172), (26, 1000), (25, 4097), (3, 100003), (400, 33)])
+def test_log_probs_gradient(ctx, rows, classes, entropy_term, dtype):
+    z, labels = logits_case(rows, classes, dtype)
+    g = gen("grad", rows, classes)
+    g_logp, g_entropy = torch.randn(rows, generator=g), torch.randn(rows, generator=g)
+    _, entropy, m, log_s, _, _, _ = ref_log_probs(z, labels.numpy(), 0)
+    with np.errstate(invalid="ignore"):
+        stats = np.stack([m, np.where(np.isnan(m), np.nan, log_s)], 1).astype(np.float32)
+        held = entropy.astype(np.float32)
+        # from the statistics that the call is given; each factor of a term is good to a few roundings
+        log_p = (z.double().numpy() - stats[:, :1].astype(np.float64)) - stats[:, 1:]
+        p = np.exp(log_p)
+        label = labels.numpy()
+        gl = np.where(label < 0, 0.0, np.where(label >= classes, np.nan, f64(g_logp)))[:, None]
+        one = np.arange(classes)[None, :] == label[:, None]
+        want = gl * (one - p)
+        size = np.abs(gl) * (one + p * (8 + np.abs(np.where(p > 0, log_p, 0.0))))
+        if entropy_term:
+            inner = np.where(p > 0, log_p + held[:, None].astype(np.float64), 0.0)
+            want = want - f64(g_entropy)[:, None] * p * inner
+            size = size + np.abs(f64(g_entropy))[:, None] * p * (8 + np.abs(np.where(p > 0, log_p, 0.0))) * (1 + np.abs(np.where(p > 0, log_p, 0.0)) + np.abs(held[:, None]))
+        none = m == -np.inf
+        want[none] = 0.0
+        size[none] = 0.0
+    for out_type in (FP32, BF16):
+        for how in LAYOUTS:
+            out = layout(torch.full((rows, classes), 9.0, dtype=out_type), how)
+            learn.gns_log_probs_backward(ctx, layout(z, how), labels.cuda(), torch.from_numpy(stats).cuda(),
+                                         torch.from_numpy(held).cuda() if entropy_term else None, g_logp.cuda(),
+                                         g_entropy.cuda() if entropy_term else None, out, rows)
+            bound = 4 * U * size + (2.0 ** -8 * np.abs(want) if out_type == BF16 else 0.0)
+            within(f64(out), want, bound + 2.0 ** -126)
+    own = z.cuda()
+    out = torch.empty_like(own)
+    args = (labels.cuda(), torch.from_numpy(stats).cuda(), torch.from_numpy(held).cuda(), g_logp.cuda(), g_entropy.cuda())
+    learn.gns_log_probs_backward(ctx, own, *args, out, rows)
+    learn.gns_log_probs_backward(ctx, own, *args, own, rows)                        # in place
+    assert np.array_equal(f64(own), f64(out), equal_nan=True)
+
+
+def test_log_probs_gradient_against_differences(ctx):
+    rows, classes, eps = 12, 37, 1e-5
+    z = torch.randn(rows, classes, generator=gen("differences")) * 2
+    labels = torch.randint(0, classes, (rows,), generator=gen("labels"), dtype=torch.int32)
+    g_logp, g_entropy = torch.randn(rows, generator=gen("a")), torch.randn(rows, generator=gen("b"))
+    out = run_log_probs(ctx, z.cuda(), labels, 0)
+    grad = torch.empty(rows, classes, device="cuda")
+    learn.gns_log_probs_backward(ctx, z.cuda(), labels.cuda(), out["stats"], out["entropy"], g_logp.cuda(), g_entropy.cuda(), grad, rows)
+
+    def loss(v):
+        log_p = v - np.log(np.exp(v).sum(1, keepdims=True))
+        p = np.exp(log_p)
+        return float((f64(g_logp) * log_p[np.arange(rows), labels.numpy()] - f64(g_entropy) * (p * log_p).sum(1)).sum())
+
+    rng = np.random.default_rng(1)
+    for _ in range(60):
+        at = int(rng.integers(0, rows)), int(rng.integers(0, classes))
+        up, down = f64(z).copy(), f64(z).copy()
+        up[at] += eps
+        down[at] -= eps
+        # the difference is good to eps^2 and 1e-15 / eps, the gradient to some roundings of terms of about 10
+        assert abs(float(grad[at]) - (loss(up) - loss(down)) / (2 * eps)) < 2e-6 + 1e-5 * abs(float(grad[at]))
+
+
+# ---- what all calls share -----------------------------------------------------------------------------------------
+def test_calls_of_no_rows_write_nothing(ctx):
+    x = torch.randn(3, 40, device="cuda")
+    q = torch.full((3, 64), 5, dtype=torch.int8, device="cuda")
+    scale, e = torch.full((3,), 5.0, device="cuda"), torch.full((3, 2), 5, dtype=torch.uint8, device="cuda")
+    learn.gns_quantize_rows(ctx, x, None, q, scale, 0)
+    learn.gns_checkpoint_save(ctx, x, q, e, None, 0)
+    out = torch.full((3, 40), 5.0, device="cuda")
+    learn.gns_checkpoint_load(ctx, q, e, out, 0)
+    learn.gns_dense_int8(ctx, q, scale, 40, torch.zeros(40, 64, dtype=torch.int8, device="cuda"), torch.ones(40, device="cuda"), None, False, out, 0)
+    learn.gns_sage_dense_int8(ctx, x, None, torch.zeros(40, 64, dtype=torch.int8, device="cuda"), torch.ones(40, device="cuda"), None, False, out, 0, None)
+    learn.gns_log_probs(ctx, x, None, None, scale, None, None, None, 0)
+    learn.gns_log_probs_backward(ctx, x, None, out, scale, None, scale, out, 0)
+    torch.cuda.synchronize()
+    assert all(bool((t == 5).all()) for t in (q, scale, e, out))
+
+
+def test_refusals(ctx):
+    lib = B.lib
+    x = torch.randn(4, 64, device="cuda")
+    q = torch.zeros(4, 64, dtype=torch.int8, device="cuda")
+    e = torch.zeros(4, 2, dtype=torch.uint8, device="cuda")
+    f = torch.zeros(64 * 64, device="cuda")
+    labels = torch.zeros(4, dtype=torch.int32, device="cuda")
+    space = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    s, p = torch.cuda.current_stream().cuda_stream, x.data_ptr()
+    qp, ep, fp, lp, wp, size = q.data_ptr(), e.data_ptr(), f.data_ptr(), labels.data_ptr(), space.data_ptr(), space.numel()
+
+    def rows(data=p, stride=64, width=64, type=0):
+        return learn.gns_rows(data, stride, width, type)
+
+    def refused(status, name, *args):
+        assert getattr(lib, name)(ctx, *args) == status, (name, args)
+        assert lib.gns_last_error(ctx)
+
+    bad_rows = [None, rows(data=None), rows(stride=63), rows(width=0), rows(width=-1), rows(type=2), rows(type=-1), rows(data=p + 2),
+                rows(data=p + 1, type=1), rows(stride=1 << 40, width=learn.GNS_MAX_WIDTH + 1)]
+    einval, small = B.GNS_EINVAL, B.GNS_ECAPACITY
+    for r in bad_rows:
+        refused(einval, "gns_quantize_rows", r, None, qp, fp, 4, s)
+        refused(einval, "gns_dense_int8", qp, fp, 64, qp, fp, None, 0, r, 4, s)
+        refused(einval, "gns_sage_dense_int8", r, None, qp, fp, None, 0, rows(), 4, wp, size, s)
+        refused(einval, "gns_sage_dense_int8", rows(), None, qp, fp, None, 0, r, 4, wp, size, s)
+        refused(einval, "gns_checkpoint_save", r, qp, ep, None, 4, s)
+        refused(einval, "gns_checkpoint_load", qp, ep, r, 4, s)
+        refused(einval, "gns_sage_dense_backward", r, None, qp, ep, 64, None, None, 0, fp, fp, None, None, 4, wp, size, s)
+        refused(einval, "gns_log_probs", r, lp, fp, None, None, 0, None, None, 4, None, 0, s)
+        refused(einval, "gns_log_probs_backward", r, lp, fp, None, fp, None, rows(), 4, s)
+        refused(einval, "gns_log_probs_backward", rows(), lp, fp, None, fp, None, r, 4, s)
+    for n in (-2, -9):                                                              # layers that the context does not have
+        refused(einval, "gns_quantize_rows", rows(), None, qp, fp, n, s)
+        refused(einval, "gns_dense_int8", qp, fp, 64, qp, fp, None, 0, rows(), n, s)
+        refused(einval, "gns_checkpoint_save", rows(), qp, ep, None, n, s)
+        refused(einval, "gns_checkpoint_load", qp, ep, rows(), n, s)
+        refused(einval, "gns_sage_dense_backward", rows(), None, qp, ep, 64, None, None, 0, fp, fp, None, None, n, wp, size, s)
+        refused(einval, "gns_log_probs", rows(), lp, fp, None, None, 0, None, None, n, None, 0, s)
+        refused(einval, "gns_log_probs_backward", rows(), lp, fp, None, fp, None, rows(), n, s)
+    refused(einval, "gns_quantize_rows", rows(), rows(type=1), qp, fp, 4, s)        # two types
+    refused(einval, "gns_quantize_rows", rows(width=learn.GNS_INT8_MAX_K, stride=1 << 20), rows(), qp, fp, 4, s)
+    for q_, f_ in ((None, fp), (qp, None), (qp + 8, fp), (qp, fp + 2)):
+        refused(einval, "gns_quantize_rows", rows(), None, q_, f_, 4, s)
+        refused(einval, "gns_dense_int8", q_, f_, 64, qp, fp, None, 0, rows(), 4, s)
+        refused(einval, "gns_dense_int8", qp, fp, 64, q_, f_, None, 0, rows(), 4, s)
+        refused(einval, "gns_sage_dense_int8", rows(), None, q_, f_, None, 0, rows(), 4, wp, size, s)
+    for k in (0, -1, learn.GNS_INT8_MAX_K + 1):
+        refused(einval, "gns_dense_int8", qp, fp, k, qp, fp, None, 0, rows(), 4, s)
+    refused(einval, "gns_dense_int8", qp, fp, 64, qp, fp, fp + 1, 0, rows(), 4, s)
+    refused(einval, "gns_sage_dense_int8", rows(), None, qp, fp, None, 0, rows(), 4, None, size, s)
+    refused(einval, "gns_sage_dense_int8", rows(), None, qp, fp, None, 0, rows(), 4, wp + 16, size, s)
+    refused(small, "gns_sage_dense_int8", rows(), None, qp, fp, None, 0, rows(), 4, wp, 256, s)
+    for q_, e_ in ((None, ep), (qp, None), (qp + 4, ep)):
+        refused(einval, "gns_checkpoint_save", rows(), q_, e_, None, 4, s)
+        refused(einval, "gns_checkpoint_load", q_, e_, rows(), 4, s)
+        refused(einval, "gns_sage_dense_backward", rows(), None, q_, e_, 64, None, None, 0, fp, fp, None, None, 4, wp, size, s)
+        refused(einval, "gns_sage_dense_backward", rows(), None, qp, ep, 32, q_, e_, 32, fp, fp, None, None, 4, wp, size, s)
+    refused(einval, "gns_checkpoint_save", rows(), qp, ep, lp + 2, 4, s)
+
+    def backward(status, f1=64, f2=0, w=fp, dw=fp, db=None, dx=None, space_=wp, size_=size, positive=None):
+        refused(status, "gns_sage_dense_backward", rows(), positive, qp, ep, f1, None, None, f2, w, dw, db, dx, 4, space_, size_, s)
+
+    backward(einval, f1=0)
+    backward(einval, f2=-1)
+    backward(einval, f1=learn.GNS_MAX_WIDTH, f2=1)
+    backward(einval, dw=None)                                                       # nothing is wanted
+    backward(einval, dw=fp + 1)
+    backward(einval, db=fp + 1)
+    backward(einval, positive=lp + 1)
+    backward(einval, w=None, dx=rows())
+    backward(einval, dx=rows(type=1))
+    backward(einval, dx=rows(width=32))
+    backward(einval, space_=None)
+    backward(einval, space_=wp + 128)
+    backward(small, size_=0)
+    for args in ((None, fp, None, None, 0, None, None), (lp, None, None, None, 0, None, None), (None, None, None, None, 0, None, None),
+                 (lp, fp, None, None, 33, fp, fp), (lp, fp, None, None, -1, fp, fp), (lp, fp, None, None, 2, None, fp),
+                 (lp, fp, None, None, 2, fp, None), (lp, fp, None, None, 0, fp, fp), (lp, fp, None, fp + 4, 0, None, None),
+                 (lp, fp + 1, None, None, 0, None, None)):
+        refused(einval, "gns_log_probs", rows(), *args, 4, wp, size, s)
+    for args in ((lp, None, None, fp, None), (lp, fp, None, None, None), (None, fp, None, fp, None), (lp, fp, fp, fp, None),
+                 (None, fp, None, None, None), (lp, fp + 4, None, fp, None)):
+        refused(einval, "gns_log_probs_backward", rows(), *args, rows(), 4, s)
+    refused(einval, "gns_log_probs_backward", rows(), lp, fp, None, fp, None, rows(width=63), 4, s)
+    refused(einval, "gns_log_probs_backward", rows(), lp, fp, None, fp, None, rows(stride=128), 4, s)      # over the logits, another stride
+    assert learn.gns_sage_dense_int8_workspace_bytes(ctx, 0, 4) == 0
+    assert learn.gns_sage_dense_int8_workspace_bytes(ctx, 64, -5) == 0
+    assert learn.gns_log_probs_workspace_bytes(ctx, 64, 33, 4) == 0
+    assert learn.gns_sage_dense_backward_workspace_bytes(ctx, 64, 0, 0, 4) == 0
+    torch.cuda.synchronize()
+
+
+def test_captured_calls_replay_with_the_same_results(ctx):
+    """A captured sequence of all calls gives the eager results on every replay, with eager work in between."""
+    rows, f, hdim, classes = 200, 72, 64, 50000
+    g = gen("graph")
+    x = torch.randn(rows, f, generator=g).cuda()
+    w = torch.randn(f, hdim, generator=g).cuda()
+    q, e, _ = save(ctx, x.cpu())
+    positive = torch.randint(-2 ** 31, 2 ** 31 - 1, (rows, 2), generator=g, dtype=torch.int32).cuda()
+    d_out = torch.randn(rows, hdim, generator=g).cuda()
+    z = torch.randn(20, classes, generator=g).cuda()
+    labels = torch.randint(0, classes, (20,), generator=g, dtype=torch.int32).cuda()
+    wq, w_scale = torch.empty(hdim, learn.int8_stride(f), dtype=torch.int8, device="cuda"), torch.empty(hdim, device="cuda")
+    learn.gns_quantize_rows(ctx, w.t().contiguous(), None, wq, w_scale, hdim)
+    outs = [torch.zeros(rows, hdim, device="cuda"), torch.zeros(rows, f, device="cuda"), torch.zeros(f, hdim, device="cuda"), torch.zeros(hdim, device="cuda"),
+            torch.zeros(rows, f, device="cuda"), torch.zeros(20, device="cuda"), torch.zeros(20, device="cuda"), torch.zeros(20, 2, device="cuda"),
+            torch.zeros(20, 9, dtype=torch.int32, device="cuda"), torch.zeros(20, 9, device="cuda"), torch.zeros(20, classes, device="cuda")]
+    spaces = [learn.alloc_workspace(n) for n in (learn.gns_sage_dense_int8_workspace_bytes(ctx, f, rows),
+                                                 learn.gns_sage_dense_backward_workspace_bytes(ctx, f, 0, hdim, rows),
+                                                 learn.gns_log_probs_workspace_bytes(ctx, classes, 9, 20))]
+
+    def calls():
+        learn.gns_sage_dense_int8(ctx, x, None, wq, w_scale, None, True, outs[0], rows, spaces[0])
+        learn.gns_checkpoint_save(ctx, x, q, e, None, rows)
+        learn.gns_checkpoint_load(ctx, q, e, outs[1], rows)
+        learn.gns_sage_dense_backward(ctx, d_out, positive, (q, e), f, None, 0, w, outs[2], outs[3], outs[4], rows, spaces[1])
+        learn.gns_log_probs(ctx, z, labels, outs[5], outs[6], outs[7], outs[8], outs[9], 20, spaces[2])
+        learn.gns_log_probs_backward(ctx, z, labels, outs[7], outs[6], outs[5], outs[6], outs[10], 20)
+
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for turn in range(4):
+        d_out.mul_(1.5)
+        z.add_(0.25 * turn)
+        calls()
+        torch.cuda.synchronize()
+        eager = [t.clone() for t in outs]
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, outs)), turn
+
+
+def test_calls_on_another_stream(ctx):
+    z, labels = logits_case(50, 3001, FP32)
+    want = run_log_probs(ctx, z.cuda(), labels, 6)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    z_dev, labels_dev = z.cuda(), labels.cuda()
+    out = {k: torch.zeros_like(v) for k, v in want.items()}
+    space = learn.alloc_workspace(learn.gns_log_probs_workspace_bytes(ctx, 3001, 6, 50))
+    torch.cuda.synchronize()
+    learn.gns_log_probs(ctx, z_dev, labels_dev, out["logp"], out["entropy"], out["stats"], out["index"], out["value"], 50, space, stream=stream)
+    stream.synchronize()
+    for k in want:
+        assert np.array_equal(f64(out[k]), f64(want[k]), equal_nan=True), k
+
+
+def test_stage_timer_counts_the_calls(ctx):
+    x = torch.randn(64, 64, device="cuda")
+    e, entropy = torch.empty(64, 2, dtype=torch.uint8, device="cuda"), torch.empty(64, device="cuda")
+    q = torch.empty(64, 64, dtype=torch.int8, device="cuda")
+    B.gns_profile_begin(ctx, 1 << learn.GNS_STAGE_CHECKPOINT | 1 << learn.GNS_STAGE_LOG_PROBS, 16)
+    learn.gns_checkpoint_save(ctx, x, q, e, None, 64)
+    learn.gns_checkpoint_load(ctx, q, e, x, 64)
+    learn.gns_log_probs(ctx, x, None, None, entropy, None, None, None, 64)
+    assert B.gns_profile_collect(ctx, learn.GNS_STAGE_CHECKPOINT)[1] == 2
+    assert B.gns_profile_collect(ctx, learn.GNS_STAGE_LOG_PROBS)[1] == 1
+    B.gns_profile_begin(ctx, 0, 0)
+
+
+@TYPES
+def test_rows_counted_on_the_device(dtype):
+    """num_rows as a layer's placeholder: results of as many rows as the layer has, nothing behind them."""
+    indptr, indices = random_symmetric_csr(3000, 10, np.random.default_rng(5))
+    gns = GpuGns(torch.from_numpy(indptr), torch.from_numpy(indices), None, fanouts=(6, 4), policies=(0, 0), cache_size=0, max_seeds=100)
+    try:
+        c, layer = gns.ctx, 1
+        seeds = synth.uniform_seed_batch(3000, 60, 9).cuda()
+        B.gns_sample_blocks(c, 3, seeds, gns.blocks.array)
+        count, cap = gns.blocks.array[layer].num_dst, gns.blocks.array[layer].cap_dst
+        assert 60 < count < cap
+        place = -1 - layer
+        g = gen("device")
+        x = torch.randn(cap, 100, generator=g).to(dtype).cuda()
+        d_out = torch.randn(cap, 72, generator=g).to(dtype).cuda()
+        w = torch.randn(100, 72, generator=g).cuda()
+        labels = torch.randint(0, 100, (cap,), generator=g, dtype=torch.int32).cuda()
+        wq, w_scale = torch.empty(72, 128, dtype=torch.int8, device="cuda"), torch.empty(72, device="cuda")
+        learn.gns_quantize_rows(c, w.t().contiguous(), None, wq, w_scale, 72)
+
+        def everything(rows):
+            new = lambda *shape, t=FP32: torch.full(shape, 42, dtype=t, device="cuda")
+            q8, scale, out8, out8b = new(cap, 128, t=torch.int8), new(cap), new(cap, 72, t=dtype), new(cap, 72, t=dtype)
+            learn.gns_quantize_rows(c, x, None, q8, scale, rows)
+            learn.gns_dense_int8(c, q8, scale, 100, wq, w_scale, None, True, out8, rows)
+            learn.gns_sage_dense_int8(c, x, None, wq, w_scale, None, True, out8b, rows,
+                                      learn.alloc_workspace(learn.gns_sage_dense_int8_workspace_bytes(c, 100, rows)))
+            q, e, positive, back = new(cap, 128, t=torch.int8), new(cap, 4, t=torch.uint8), new(cap, 4, t=torch.int32), new(cap, 100, t=dtype)
+            learn.gns_checkpoint_save(c, x, q, e, positive, rows)
+            learn.gns_checkpoint_load(c, q, e, back, rows)
+            dw, db, dx = new(100, 72), new(72), new(cap, 100, t=dtype)
+            learn.gns_sage_dense_backward(c, d_out, None, (q, e), 100, None, 0, w, dw, db, dx, rows,
+                                          learn.alloc_workspace(learn.gns_sage_dense_backward_workspace_bytes(c, 100, 0, 72, rows)))
+            logp, entropy, stats, index, value, grad = new(cap), new(cap), new(cap, 2), new(cap, 3, t=torch.int32), new(cap, 3), new(cap, 100, t=dtype)
+            learn.gns_log_probs(c, x, labels, logp, entropy, stats, index, value, rows,
+                                learn.alloc_workspace(learn.gns_log_probs_workspace_bytes(c, 100, 3, rows)))
+            learn.gns_log_probs_backward(c, x, labels, stats, entropy, entropy, logp, grad, rows)
+            torch.cuda.synchronize()
+            return [q8, scale, out8, out8b, q, e, positive, back, dx, logp, entropy, stats, index, value, grad], [dw, db]
+
+        by_row, sums = everything(place)
+        want_rows, want_sums = everything(count)
+        for i, (a, b) in enumerate(zip(by_row, want_rows)):
+            if i in (2, 3, 8):                # products: the kernel goes by the rows the layer can have
+                tol = 2.0 ** -7 if dtype == BF16 else 1e-5
+                within(f64(a[:count]), f64(b[:count]), tol * (f64(b[:count].abs()) + f64(b[:count].abs().max())))
+            elif i in (9, 10, 11, 13, 14):
+                within(f64(a[:count]), f64(b[:count]), (2.0 ** -7 if dtype == BF16 else 1e-5) * (1 + np.abs(f64(b[:count]))))
+            else:
+                assert torch.equal(a[:count], b[:count]), i
+            assert bool((a[count:] == 42).all()), i
+        for a, b in zip(sums, want_sums):
+            within(f64(a), f64(b), 1e-5 * (np.abs(f64(b)) + float(b.abs().max())))
+    finally:
+        gns.close()
