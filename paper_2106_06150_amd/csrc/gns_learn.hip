@@ -290,8 +290,8 @@ gns_status gns_log_probs_backward(gns_ctx* ctx, const gns_rows* logits, const in
     GNS_REQUIRE(d_logits->data != logits->data || (d_logits->stride == logits->stride && d_logits->type == logits->type),
                 "d_logits may only be the logits' own rows");
     GNS_REQUIRE(stats_dev && !misaligned(stats_dev, 8), "stats are null or not 8-byte aligned");
-    GNS_REQUIRE(!labels_dev == !g_logp_dev, "labels and g_logp go together");
-    GNS_REQUIRE(!entropy_dev == !g_entropy_dev, "entropy and g_entropy go together");
+    GNS_REQUIRE(!g_logp_dev || labels_dev, "g_logp needs the labels");
+    GNS_REQUIRE(!g_entropy_dev || entropy_dev, "g_entropy needs the entropy");
     GNS_REQUIRE(g_logp_dev || g_entropy_dev, "no gradient is given");
     GNS_REQUIRE(!misaligned(labels_dev, 4) && !misaligned(g_logp_dev, 4) && !misaligned(entropy_dev, 4) && !misaligned(g_entropy_dev, 4),
                 "labels and gradients must be aligned");
@@ -299,7 +299,9 @@ gns_status gns_log_probs_backward(gns_ctx* ctx, const gns_rows* logits, const in
     GNS_REQUIRE(row_count(ctx, num_rows, &a.count), "bad device-count placeholder");
     if (a.count.rows == 0) return GNS_OK;
     a.logits = as_const(logits);
-    a.labels = labels_dev; a.stats = stats_dev; a.entropy = entropy_dev; a.g_logp = g_logp_dev; a.g_entropy = g_entropy_dev;
+    a.labels = g_logp_dev ? labels_dev : nullptr;
+    a.entropy = g_entropy_dev ? entropy_dev : nullptr;
+    a.stats = stats_dev; a.g_logp = g_logp_dev; a.g_entropy = g_entropy_dev;
     a.d_logits = as_mut(d_logits);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     StageTimer t(ctx, GNS_STAGE_LOG_PROBS, s);

@@ -1,127 +1,608 @@
 // Log probabilities of given classes, entropy and best classes of rows of logits, and the gradient of the first two.
+//
+// With m the largest logit, S = sum e^(z - m) and T = sum e^(z - m) (z - m):  log p_y = (z_y - m) - log S and the entropy is
+// log S - T / S.  A row is read once: maximum, S and T are kept together, and what was summed so far is rescaled when the
+// maximum grows (with d = m_old - m_new: S <- e^d S, T <- e^d (T + d S)).  All of it, and exp itself, is bound by the bytes of
+// the logits; the arithmetic (ten instructions a value, four of them the exponential's cycles) is just short enough for bf16.
 #include "gns_learn.hpp"
 
 namespace gns {
 
-// A value's place in the order of all values: larger floats have larger keys, and of equal ones (0 and -0 too) the lower index.
-__device__ __forceinline__ uint64_t order_key(float z, int32_t index)
-{
-    const uint32_t b = __float_as_uint(z + 0.f);
-    return (uint64_t) (b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t) ~index;
-}
+constexpr float kLog2E = 1.44269504f;
+constexpr float kFar = -1000.f;               // e^kFar is zero in fp32
 
-template <typename V, typename Op>
-__device__ __forceinline__ V block_reduce(V v, V* smem, Op op)
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+
+// A value's place in the order of all values: larger floats have larger keys, and of equal ones (0 and -0 too) the lower index.
+struct Best {
+    float z;
+    int32_t index;
+};
+__device__ __forceinline__ bool before(const Best& a, const Best& b) { return a.z > b.z || (a.z == b.z && a.index < b.index); }
+
+template <int kCtrl>
+__device__ __forceinline__ float dpp_float(float v)
 {
-    for (int off = 32; off; off >>= 1) v = op(v, __shfl_xor(v, off));
-    __syncthreads();
-    if (lane_id() == 0) smem[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = smem[0];
-    for (int w = 1; w < kBlock / kWave; ++w) v = op(v, smem[w]);
+    return __uint_as_float((uint32_t) __builtin_amdgcn_update_dpp(0, (int) __float_as_uint(v), kCtrl, 0xf, 0xf, true));
+}
+template <int kCtrl>
+__device__ __forceinline__ int32_t dpp_int(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, kCtrl, 0xf, 0xf, true); }
+
+// Reduction over groups of L consecutive lanes; every lane gets the result.  Up to 16 lanes it stays in the registers.
+template <int L, typename Op>
+__device__ __forceinline__ float reduce_float(float v, Op op)
+{
+    if (L > 1) v = op(v, dpp_float<0xB1>(v));      // lanes 1 0 3 2
+    if (L > 2) v = op(v, dpp_float<0x4E>(v));      // lanes 2 3 0 1
+    if (L > 4) v = op(v, dpp_float<0x141>(v));     // mirrored in halves of a row of 16
+    if (L > 8) v = op(v, dpp_float<0x140>(v));     // mirrored in the row
+    if (L > 16) v = op(v, __shfl_xor(v, 16));
+    if (L > 32) v = op(v, __shfl_xor(v, 32));
+    return v;
+}
+template <int L>
+__device__ __forceinline__ float sum_of(float v) { return reduce_float<L>(v, [](float a, float b) { return a + b; }); }
+template <int L>
+__device__ __forceinline__ float max_of(float v) { return reduce_float<L>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int L>
+__device__ __forceinline__ int32_t min_of(int32_t v)
+{
+    if (L > 1) v = min(v, dpp_int<0xB1>(v));
+    if (L > 2) v = min(v, dpp_int<0x4E>(v));
+    if (L > 4) v = min(v, dpp_int<0x141>(v));
+    if (L > 8) v = min(v, dpp_int<0x140>(v));
+    if (L > 16) v = min(v, __shfl_xor(v, 16));
+    if (L > 32) v = min(v, __shfl_xor(v, 32));
     return v;
 }
 
-// A block per row; a pass for the maximum, one for the sums and one per best class.
+// Running maximum and sums.  A NaN or +infinity among the values makes S NaN.
+struct Softmax {
+    float m, S, T;
+};
+
+// The values' maximum becomes (at least) `most`.
+__device__ __forceinline__ void raise(Softmax& s, float most)
+{
+    const float d = fmaxf(s.m - most, kFar);        // from -infinity: nothing was summed yet
+    if (most > s.m) {
+        const float f = exp_of(d);
+        s.T = f * fmaf(d, s.S, s.T);
+        s.S *= f;
+        s.m = most;
+    }
+}
+
+// Adds N values none of which is above s.m.  Masked ones (-infinity) make T NaN, and it is summed once more with their share
+// left out: a test per value would cost all rows what only masked ones need.
+template <int N>
+__device__ __forceinline__ void add_values(Softmax& s, const float (&z)[N])
+{
+    const float m = s.m == -__builtin_inff() ? 0.f : s.m, T0 = s.T;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float d = z[i] - m, p = exp_of(d);
+        s.S += p;
+        s.T = fmaf(p, d, s.T);
+    }
+    if (__builtin_expect(s.T != s.T, 0)) {
+        s.T = T0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float d = z[i] - m;
+            s.T = fmaf(exp_of(d), fmaxf(d, kFar), s.T);
+        }
+    }
+}
+
+// The sums of a group of L lanes; every lane gets them.
+template <int L>
+__device__ __forceinline__ void join_lanes(Softmax& s)
+{
+    const float most = max_of<L>(s.m), d = fmaxf(s.m - most, kFar), f = exp_of(d);
+    s.T = sum_of<L>(f * fmaf(d, s.S, s.T));
+    s.S = sum_of<L>(f * s.S);
+    s.m = most;
+}
+
+struct RowResult {
+    float m, log_sum, entropy;
+    bool bad, none;
+};
+__device__ __forceinline__ RowResult result_of(const Softmax& s)
+{
+    RowResult o;
+    o.bad = s.S != s.S;
+    o.none = !o.bad && s.m == -__builtin_inff();
+    o.m = o.bad ? quiet_nan() : s.m;
+    o.log_sum = o.none ? 0.f : logf(s.S);
+    o.entropy = o.none ? 0.f : o.log_sum - s.T / s.S;
+    return o;
+}
+// log p of a class with logit z
+__device__ __forceinline__ float log_p_of(const RowResult& o, float z) { return o.none ? -__builtin_inff() : (z - o.m) - o.log_sum; }
+
 template <typename T>
-__global__ void __launch_bounds__(kBlock) k_log_probs(LogProbsArgs a)
+__device__ __forceinline__ void write_row(const LogProbsArgs& a, int64_t r, const RowResult& o, int32_t label, float z_label)
 {
-    __shared__ float s_f[kBlock / kWave];
-    __shared__ unsigned long long s_key[kBlock / kWave];
+    if (a.logp) a.logp[r] = o.bad || label >= a.logits.width ? quiet_nan() : label < 0 ? 0.f : log_p_of(o, z_label);
+    if (a.entropy) a.entropy[r] = o.entropy;
+    if (a.stats) *reinterpret_cast<float2*>(a.stats + 2 * r) = make_float2(o.m, o.log_sum);
+}
+
+template <typename T>
+__device__ __forceinline__ float label_logit(const LogProbsArgs& a, int64_t r, int32_t* label)
+{
+    *label = a.labels ? a.labels[r] : -1;
+    return *label >= 0 && *label < a.logits.width ? load_at<T>(a.logits, r, *label) : 0.f;
+}
+
+// Rows of up to L * E classes: L lanes a row, E values a lane in registers, 64 / L rows a wave.  The best classes come one
+// after the other: each lane has its own best at hand, the lane that wins looks for its next.
+// 85,000 rows of 172 classes, fp32, five best: see launch_log_probs.
+template <typename T, int L, int E>
+__global__ void __launch_bounds__(kBlock) k_log_probs_short(LogProbsArgs a)
+{
+    constexpr float kNone = -__builtin_inff();
     const int32_t rows = a.count.get(), C = a.logits.width;
-    auto add = [](float x, float y) { return x + y; };
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        float m = -__builtin_inff(), bad = 0.f;
-        for (int32_t j = (int32_t) threadIdx.x; j < C; j += kBlock) {
-            const float z = load_at<T>(a.logits, r, j);
-            if (!(z < __builtin_inff())) bad = 1.f;
-            m = fmaxf(m, z);
+    const int64_t step = (int64_t) gridDim.x * (kBlock / L);
+    // the lanes of a wave make as many turns, as the exchange between them asks for
+    for (int64_t r0 = ((int64_t) blockIdx.x * kBlock + (threadIdx.x & ~(kWave - 1))) / L; r0 < rows; r0 += step) {
+        const int lane = opaque_lane_id(), l = lane & (L - 1);
+        const int64_t row = r0 + lane / L, r = row < rows ? row : rows - 1;
+        float z[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int32_t c = e * L + l;
+            z[e] = c < C ? load_at<T>(a.logits, r, c) : kNone;
         }
-        m = block_reduce(m, s_f, [](float x, float y) { return fmaxf(x, y); });
-        bad = block_reduce(bad, s_f, add);
-        const bool none = m == -__builtin_inff();
-        float sum = 0.f, weighted = 0.f;
-        for (int32_t j = (int32_t) threadIdx.x; !none && bad == 0.f && j < C; j += kBlock) {
-            const float d = load_at<T>(a.logits, r, j) - m, p = expf(d);
-            sum += p;
-            if (p > 0.f) weighted = fmaf(p, d, weighted);
-        }
-        sum = block_reduce(sum, s_f, add);
-        weighted = block_reduce(weighted, s_f, add);
-        const float nan = quiet_nan();
-        const float log_sum = bad != 0.f ? nan : none ? 0.f : logf(sum);
-        if (threadIdx.x == 0) {
-            if (a.logp) {
-                const int32_t y = a.labels[r];
-                float v = y < 0 ? 0.f : y >= C ? nan : none ? -__builtin_inff() : load_at<T>(a.logits, r, y) - m - log_sum;
-                a.logp[r] = bad != 0.f ? nan : v;
-            }
-            if (a.entropy) a.entropy[r] = bad != 0.f ? nan : none ? 0.f : log_sum - weighted / sum;
-            if (a.stats) { a.stats[2 * r] = bad != 0.f ? nan : m; a.stats[2 * r + 1] = log_sum; }
-        }
-        unsigned long long last = ~0ull;
+        int32_t label;
+        const float z_label = label_logit<T>(a, r, &label);
+        Softmax s = {kNone, 0.f, 0.f};
+        float mine = kNone;                       // (the larger of a NaN and a number is the number)
+#pragma unroll
+        for (int e = 0; e < E; ++e) mine = fmaxf(mine, z[e]);
+        s.m = max_of<L>(mine);
+        add_values(s, z);
+        s.S = sum_of<L>(s.S);
+        s.T = sum_of<L>(s.T);
+        const RowResult o = result_of(s);
+        if (l == 0 && row < rows) write_row<T>(a, r, o, label, z_label);
         for (int32_t i = 0; i < a.top; ++i) {
-            unsigned long long best = 0;
-            for (int32_t j = (int32_t) threadIdx.x; bad == 0.f && j < C; j += kBlock) {
-                const float z = load_at<T>(a.logits, r, j);
-                const unsigned long long key = order_key(z, j);
-                if (z > -__builtin_inff() && key < last && key > best) best = key;
+            int32_t slot = 0;
+#pragma unroll
+            for (int e = E - 1; e >= 0; --e) slot = z[e] == mine ? e : slot;
+            const float best = max_of<L>(mine);
+            const int32_t index = min_of<L>(mine == best ? slot * L + l : INT32_MAX);
+            if (l == 0 && row < rows) {
+                const bool gone = o.bad || best == kNone;
+                a.top_index[r * a.top + i] = gone ? -1 : index;
+                a.top_logp[r * a.top + i] = o.bad ? quiet_nan() : gone ? kNone : log_p_of(o, best);
             }
-            best = block_reduce(best, s_key, [](unsigned long long x, unsigned long long y) { return x > y ? x : y; });
-            if (threadIdx.x == 0) {
-                const int32_t j = best ? (int32_t) ~(uint32_t) best : -1;
-                a.top_index[r * a.top + i] = j;
-                a.top_logp[r * a.top + i] = bad != 0.f ? nan : j < 0 ? -__builtin_inff() : load_at<T>(a.logits, r, j) - m - log_sum;
+            const int32_t drop = index == slot * L + l ? slot : -1;
+            mine = kNone;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                z[e] = e == drop ? kNone : z[e];
+                mine = fmaxf(mine, z[e]);
             }
-            last = best;
         }
     }
 }
 
-template <typename T, typename O>
-__global__ void __launch_bounds__(kBlock) k_log_probs_backward(LogProbsBackwardArgs a)
+// The best classes a wave has seen, one a lane, in order.  What does not come before `last` is not among the row's best:
+// the last one that counts, or a bound from elsewhere.
+struct WaveList {
+    Best mine, last;
+};
+
+__device__ __forceinline__ Best lane_best(const Best& b, int lane)
 {
-    const int32_t rows = a.count.get(), C = a.logits.width;
+    return Best{__uint_as_float((uint32_t) __builtin_amdgcn_readlane((int) __float_as_uint(b.z), lane)), __builtin_amdgcn_readlane(b.index, lane)};
+}
+
+__device__ __forceinline__ void insert(WaveList& list, const Best& b, int32_t top)
+{
+    const int lane = opaque_lane_id(), at = __popcll(__ballot(before(list.mine, b)));
+    Best up;                                                   // of the lane below
+    up.z = __uint_as_float((uint32_t) __builtin_amdgcn_update_dpp(0, (int) __float_as_uint(list.mine.z), 0x138, 0xf, 0xf, true));
+    up.index = __builtin_amdgcn_update_dpp(0, list.mine.index, 0x138, 0xf, 0xf, true);
+    list.mine = lane < at ? list.mine : lane == at ? b : up;
+    const Best bound = lane_best(list.mine, top - 1);          // none while the list is short
+    if (before(bound, list.last)) list.last = bound;
+}
+
+// Takes up N values a lane; index_of(i) is the class of the lane's i-th.  -infinity is none.  Nearly all values are
+// passed over by one comparison of the lane's largest; equal values are told apart by their classes, so a row of one
+// value costs no insertions after the first.
+template <int N, typename Index>
+__device__ __forceinline__ void take_up(WaveList& list, const float (&z)[N], float largest, int32_t top, Index&& index_of)
+{
+    if (!__ballot(largest >= list.last.z && largest > -__builtin_inff())) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int32_t index = index_of(i);
+        uint64_t hits = __ballot(z[i] > -__builtin_inff() && before(Best{z[i], index}, list.last));
+        for (; hits; hits &= hits - 1) {
+            const Best b = lane_best(Best{z[i], index}, __builtin_ctzll(hits));
+            if (before(b, list.last)) insert(list, b, top);
+        }
+    }
+}
+
+// A bound that at least `top` of the wave's values reach: the top-th of the lanes' largest.
+__device__ __forceinline__ float lanes_bound(float largest, int32_t top)
+{
+    const int lane = opaque_lane_id();
+    int32_t rank = 0;
+    for (int i = 0; i < kWave; ++i) {
+        const float other = __uint_as_float((uint32_t) __builtin_amdgcn_readlane((int) __float_as_uint(largest), i));
+        rank += other > largest || (other == largest && i < lane) ? 1 : 0;
+    }
+    return __uint_as_float((uint32_t) __builtin_amdgcn_readlane((int) __float_as_uint(largest), __builtin_ctzll(__ballot(rank == top - 1))));
+}
+
+template <typename T> constexpr int kVec = 16 / (int) sizeof(T);
+
+// Sixteen values of a lane: 16 / kVec<T> pieces of 16 bytes, pieces kWave * kVec<T> values apart.
+constexpr int kLaneValues = 16;
+constexpr int kWaveTile = kLaneValues * kWave;
+
+template <typename T> struct alignas(16) Piece { T v[kVec<T>]; };
+
+// What a part of a row leaves for the join.
+struct PartSums {
+    float m, S, T, unused;
+};
+
+struct LongArgs {
+    LogProbsArgs a;
+    int32_t parts;                // of a row
+    int32_t tiles;                // of a part
+    PartSums* sums;               // [rows x parts], if parts > 1
+    Best* best;                   // [rows x parts x top]
+};
+
+// Rows of any length: a wave per row, or per part of a row where there are few.  Pieces of 16 bytes are read at 16-byte
+// marks whatever the row's own alignment; the few values in front of the first mark and behind the last are read singly.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) k_log_probs_long(LongArgs g)
+{
+    constexpr float kNone = -__builtin_inff();
+    constexpr int V = kVec<T>, kPieces = kLaneValues / V;
+    const LogProbsArgs& a = g.a;
+    const int32_t rows = a.count.get(), C = a.logits.width, top = a.top;
+    const int64_t work = (int64_t) rows * g.parts;
+    for (int64_t w = (int64_t) blockIdx.x * (kBlock / kWave) + __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)); w < work;
+         w += (int64_t) gridDim.x * (kBlock / kWave)) {
+        const int lane = opaque_lane_id();
+        const int64_t r = w / g.parts;
+        const int32_t part = (int32_t) (w - r * g.parts);
+        const T* row = reinterpret_cast<const T*>(a.logits.data) + r * a.logits.stride;
+        const int32_t off = (int32_t) (reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
+        const int32_t head = min((V - off) % V, C), body = (C - head) / V;         // pieces
+        const Piece<T>* pieces = reinterpret_cast<const Piece<T>*>(row + head);
+        const int32_t p0 = (int32_t) min((int64_t) part * g.tiles * (kPieces * kWave), (int64_t) body);
+        const int32_t p1 = (int32_t) min((int64_t) (part + 1) * g.tiles * (kPieces * kWave), (int64_t) body);
+        int32_t label = -1;
+        float z_label = 0.f;
+        if (g.parts == 1) z_label = label_logit<T>(a, r, &label);
+        Softmax s = {kNone, 0.f, 0.f};
+        WaveList list = {{kNone, INT32_MAX}, {kNone, INT32_MAX}};
+        bool first = true;
+        if (part == 0) {                          // the single values: lanes 0 .. head - 1 and from 32 on
+            const int32_t behind = C - head - body * V;
+            float z[1] = {kNone};
+            const int32_t c = lane < 32 ? lane : head + body * V + lane - 32;
+            if (lane < 32 ? lane < head : lane - 32 < behind) z[0] = to_float(row[c]);
+            raise(s, z[0]);
+            add_values(s, z);
+            if (top) take_up(list, z, z[0], top, [&](int) { return c; });
+        }
+        // pieces of the next tile are on their way while this one's are worked on; those past the part repeat its last one and
+        // count as nothing
+        Piece<T> x[kPieces];
+        auto fetch = [&](int32_t p) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int32_t at = p + j * kWave + lane;
+                x[j] = pieces[at < p1 ? at : p1 - 1];
+            }
+        };
+        if (p0 < p1) fetch(p0);
+        for (int32_t p = p0; p < p1; p += kPieces * kWave) {
+            float z[kLaneValues];
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) z[j * V + v] = p + j * kWave + lane < p1 ? to_float(x[j].v[v]) : kNone;
+            if (p + kPieces * kWave < p1) fetch(p + kPieces * kWave);
+            float largest = kNone;
+#pragma unroll
+            for (int i = 0; i < kLaneValues; ++i) largest = fmaxf(largest, z[i]);
+            raise(s, largest);
+            add_values(s, z);
+            if (top) {
+                if (first) {
+                    const float bound = lanes_bound(largest, top);
+                    if (bound > list.last.z) list.last = Best{bound, INT32_MAX};
+                    first = false;
+                }
+                take_up(list, z, largest, top, [&](int i) { return head + (p + i / V * kWave + lane) * V + i % V; });
+            }
+        }
+        join_lanes<kWave>(s);
+        if (g.parts > 1) {
+            if (lane == 0) g.sums[w] = PartSums{s.m, s.S, s.T, 0.f};
+            if (lane < top) g.best[w * top + lane] = list.mine;
+            continue;
+        }
+        const RowResult o = result_of(s);
+        if (lane == 0) write_row<T>(a, r, o, label, z_label);
+        if (lane < top) {
+            const bool gone = o.bad || list.mine.z == kNone;
+            a.top_index[r * top + lane] = gone ? -1 : list.mine.index;
+            a.top_logp[r * top + lane] = o.bad ? quiet_nan() : gone ? kNone : log_p_of(o, list.mine.z);
+        }
+    }
+}
+
+// A wave per row: its parts' sums and best classes.
+template <typename T>
+__global__ void __launch_bounds__(kWave) k_log_probs_join(LongArgs g)
+{
+    constexpr float kNone = -__builtin_inff();
+    const LogProbsArgs& a = g.a;
+    const int32_t rows = a.count.get(), top = a.top;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const float m = a.stats[2 * r], log_sum = a.stats[2 * r + 1];
-        const int32_t y = a.labels ? a.labels[r] : -1;
-        const float g = y < 0 ? 0.f : y >= C ? quiet_nan() : a.g_logp[r];
-        const float h = a.g_entropy ? a.g_entropy[r] : 0.f, entropy = a.entropy ? a.entropy[r] : 0.f;
-        const bool none = m == -__builtin_inff();
-        for (int32_t j = (int32_t) threadIdx.x; j < C; j += kBlock) {
-            const float log_p = (load_at<T>(a.logits, r, j) - m) - log_sum, p = none ? 0.f : expf(log_p);
-            float v = -g * p;
-            if (p > 0.f) v -= h * p * (log_p + entropy);
-            if (j == y && !none) v += g;
-            store_at<O>(a.d_logits, r, j, none ? 0.f : p == p ? v : quiet_nan());
+        const int lane = opaque_lane_id();
+        int32_t label;
+        const float z_label = label_logit<T>(a, r, &label);
+        Softmax s = {kNone, 0.f, 0.f};
+        for (int32_t p = lane; p < g.parts; p += kWave) {
+            const PartSums q = g.sums[r * g.parts + p];
+            raise(s, q.m);
+            const float d = fmaxf(q.m - s.m, kFar), f = exp_of(d);
+            s.T += f * fmaf(d, q.S, q.T);
+            s.S += f * q.S;
+        }
+        join_lanes<kWave>(s);
+        const RowResult o = result_of(s);
+        if (lane == 0) write_row<T>(a, r, o, label, z_label);
+        if (!top) continue;
+        WaveList list = {{kNone, INT32_MAX}, {kNone, INT32_MAX}};
+        const Best* from = g.best + r * g.parts * top;
+        const int32_t n = g.parts * top;
+        for (int32_t i0 = 0; i0 < n; i0 += kWave * 8) {
+            float z[8];
+            int32_t index[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int32_t i = i0 + j * kWave + lane;
+                const Best b = i < n ? from[i] : Best{kNone, INT32_MAX};
+                z[j] = b.z;
+                index[j] = b.index;
+            }
+            float largest = kNone;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) largest = fmaxf(largest, z[j]);
+            if (i0 == 0) {
+                const float bound = lanes_bound(largest, top);
+                if (bound > kNone) list.last = Best{bound, INT32_MAX};
+            }
+            take_up(list, z, largest, top, [&](int j) { return index[j]; });
+        }
+        if (lane < top) {
+            const bool gone = o.bad || list.mine.z == kNone;
+            a.top_index[r * top + lane] = gone ? -1 : list.mine.index;
+            a.top_logp[r * top + lane] = o.bad ? quiet_nan() : gone ? kNone : log_p_of(o, list.mine.z);
         }
     }
 }
 
-static unsigned row_grid(const gns_ctx* c, int32_t rows)
+// What a row's gradient is made of: p_j (slope (log p_j) + base), and `at` more for the label's class.
+struct RowGradient {
+    float m, log_sum, base, slope, at;
+    int32_t label;
+};
+__device__ __forceinline__ RowGradient row_gradient(const LogProbsBackwardArgs& a, int64_t r)
 {
-    const int64_t most = (int64_t) c->num_cus * 64;
-    return (unsigned) (rows < most ? rows : most);
+    const float2 stats = *reinterpret_cast<const float2*>(a.stats + 2 * r);
+    RowGradient o;
+    o.label = a.labels ? a.labels[r] : -1;
+    o.m = stats.x;
+    o.log_sum = stats.y;
+    o.at = o.label < 0 ? 0.f : o.label >= a.logits.width ? quiet_nan() : a.g_logp[r];
+    o.slope = a.g_entropy ? -a.g_entropy[r] : 0.f;
+    o.base = -o.at + (a.g_entropy ? o.slope * a.entropy[r] : 0.f);
+    if (stats.x == -__builtin_inff()) o.m = o.base = o.slope = o.at = 0.f;      // no class left: every p is zero
+    if (stats.x != stats.x) o.base = quiet_nan();                               // where a masked class has p = 0 too
+    return o;
+}
+template <bool kEntropy>
+__device__ __forceinline__ float gradient_of(const RowGradient& o, float z)
+{
+    const float log_p = (z - o.m) - o.log_sum, p = exp_of(log_p);
+    return p * (kEntropy ? fmaf(o.slope, fmaxf(log_p, kFar), o.base) : o.base);
 }
 
-size_t log_probs_workspace(const gns_ctx*, int32_t, int32_t, int32_t) { return 0; }
+// L lanes a row (of short rows several a wave), a value at a time; `chunk` columns of a long row.
+template <typename T, typename O, bool kEntropy, int L>
+__global__ void __launch_bounds__(kBlock) k_log_probs_backward(LogProbsBackwardArgs a, int32_t chunk)
+{
+    const int32_t rows = a.count.get(), C = a.logits.width, l = lane_id() & (L - 1);
+    const int32_t chunks = (C + chunk - 1) / chunk;
+    const int64_t work = (int64_t) rows * chunks;
+    for (int64_t w = ((int64_t) blockIdx.x * kBlock + threadIdx.x) / L; w < work; w += (int64_t) gridDim.x * (kBlock / L)) {
+        const int64_t r = chunks == 1 ? w : w / chunks;
+        const int32_t c0 = (int32_t) (w - r * chunks) * chunk, c1 = min(c0 + chunk, C);
+        const RowGradient o = row_gradient(a, r);
+        const T* in = reinterpret_cast<const T*>(a.logits.data) + r * a.logits.stride;
+        O* out = reinterpret_cast<O*>(a.d_logits.data) + r * a.d_logits.stride;
+        constexpr int kTurn = 4;                  // values on their way together
+        for (int32_t c = c0 + l; c < c1; c += kTurn * L) {
+            float z[kTurn];
+#pragma unroll
+            for (int i = 0; i < kTurn; ++i) z[i] = to_float(in[min(c + i * L, c1 - 1)]);
+#pragma unroll
+            for (int i = 0; i < kTurn; ++i) {
+                const float v = gradient_of<kEntropy>(o, z[i]) + (c + i * L == o.label ? o.at : 0.f);
+                if (c + i * L < c1) out[c + i * L] = from_float<O>(v);
+            }
+        }
+    }
+}
+
+// Long rows whose logits and gradients lie alike against the 16-byte marks: pieces of 16 bytes at the marks, single values
+// in front of and behind them.  A wave has `tiles` tiles of a row.
+template <typename T, bool kEntropy>
+__global__ void __launch_bounds__(kBlock) k_log_probs_backward_long(LogProbsBackwardArgs a, int32_t parts, int32_t tiles)
+{
+    constexpr int V = kVec<T>, kPieces = kLaneValues / V;
+    const int32_t rows = a.count.get(), C = a.logits.width, lane = lane_id();
+    const int64_t work = (int64_t) rows * parts;
+    for (int64_t w = (int64_t) blockIdx.x * (kBlock / kWave) + __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)); w < work;
+         w += (int64_t) gridDim.x * (kBlock / kWave)) {
+        const int64_t r = w / parts;
+        const int32_t part = (int32_t) (w - r * parts);
+        const T* in = reinterpret_cast<const T*>(a.logits.data) + r * a.logits.stride;
+        T* out = reinterpret_cast<T*>(a.d_logits.data) + r * a.d_logits.stride;
+        const int32_t off = (int32_t) (reinterpret_cast<uintptr_t>(in) % 16 / sizeof(T));
+        const int32_t head = min((V - off) % V, C), body = (C - head) / V;
+        const int32_t p0 = (int32_t) min((int64_t) part * tiles * (kPieces * kWave), (int64_t) body);
+        const int32_t p1 = (int32_t) min((int64_t) (part + 1) * tiles * (kPieces * kWave), (int64_t) body);
+        const Piece<T>* from = reinterpret_cast<const Piece<T>*>(in + head);
+        Piece<T>* to = reinterpret_cast<Piece<T>*>(out + head);
+        const RowGradient o = row_gradient(a, r);
+        auto value = [&](float z, int32_t c) { return from_float<T>(gradient_of<kEntropy>(o, z) + (c == o.label ? o.at : 0.f)); };
+        if (part == 0) {
+            const int32_t behind = C - head - body * V, c = lane < 32 ? lane : head + body * V + lane - 32;
+            if (lane < 32 ? lane < head : lane - 32 < behind) out[c] = value(to_float(in[c]), c);
+        }
+        for (int32_t p = p0 + lane; p < p1; p += kPieces * kWave) {
+            Piece<T> x[kPieces];
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) x[j] = from[min(p + j * kWave, p1 - 1)];
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int32_t c = head + (p + j * kWave) * V;
+                const bool here = o.label >= c && o.label < c + V;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    float y = gradient_of<kEntropy>(o, to_float(x[j].v[v]));
+                    if (here && c + v == o.label) y += o.at;
+                    x[j].v[v] = from_float<T>(y);
+                }
+                if (p + j * kWave < p1) to[p + j * kWave] = x[j];
+            }
+        }
+    }
+}
+
+static unsigned grid_of(const gns_ctx* c, int64_t blocks, int per_cu)
+{
+    const int64_t most = (int64_t) c->num_cus * per_cu;
+    return (unsigned) (blocks < most ? blocks : most);
+}
+
+constexpr int32_t kShortClasses = 256;
+
+// Parts of a row: enough for eight waves on every SIMD, of at least two tiles.
+static void split_rows(const gns_ctx* c, int32_t classes, int32_t rows, int32_t* parts, int32_t* tiles)
+{
+    const int32_t all = (int32_t) (((int64_t) classes + kWaveTile - 1) / kWaveTile);
+    const int64_t waves = (int64_t) c->num_cus * 4 * 8;
+    int64_t p = 1;
+    if ((int64_t) rows * 2 <= waves) p = waves / rows;
+    if (p > all / 2) p = all / 2;
+    if (p < 1) p = 1;
+    *tiles = (int32_t) ((all + p - 1) / p);
+    *parts = (all + *tiles - 1) / *tiles;
+}
+
+static size_t sums_bytes(int64_t rows, int32_t parts) { return ((size_t) rows * (size_t) parts * sizeof(PartSums) + 255) / 256 * 256; }
+
+size_t log_probs_workspace(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows)
+{
+    if (classes <= kShortClasses) return 0;
+    int32_t parts, tiles;
+    split_rows(c, classes, rows, &parts, &tiles);
+    return parts == 1 ? 0 : sums_bytes(rows, parts) + (size_t) rows * (size_t) parts * (size_t) top * sizeof(Best);
+}
+
+template <typename T, int L, int E>
+static hipError_t launch_short(const gns_ctx* c, const LogProbsArgs& a, hipStream_t s)
+{
+    const int64_t per_block = kBlock / L;
+    hipLaunchKernelGGL((k_log_probs_short<T, L, E>), dim3(grid_of(c, (a.count.rows + per_block - 1) / per_block, 32)), dim3(kBlock), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_typed(const gns_ctx* c, const LogProbsArgs& a, hipStream_t s)
+{
+    const int32_t C = a.logits.width;
+    if (C <= 16) return launch_short<T, 4, 4>(c, a, s);
+    if (C <= 64) return launch_short<T, 8, 8>(c, a, s);
+    if (C <= 128) return launch_short<T, 16, 8>(c, a, s);
+    if (C <= 192) return launch_short<T, 16, 12>(c, a, s);
+    if (C <= kShortClasses) return launch_short<T, 16, 16>(c, a, s);
+    LongArgs g = {};
+    g.a = a;
+    split_rows(c, C, a.count.rows, &g.parts, &g.tiles);
+    if (g.parts > 1) {
+        g.sums = static_cast<PartSums*>(a.workspace);
+        g.best = reinterpret_cast<Best*>(static_cast<char*>(a.workspace) + sums_bytes(a.count.rows, g.parts));
+    }
+    const int64_t blocks = ((int64_t) a.count.rows * g.parts + kBlock / kWave - 1) / (kBlock / kWave);
+    hipLaunchKernelGGL(k_log_probs_long<T>, dim3(grid_of(c, blocks, 32)), dim3(kBlock), 0, s, g);
+    if (g.parts > 1) hipLaunchKernelGGL(k_log_probs_join<T>, dim3(grid_of(c, a.count.rows, 32)), dim3(kWave), 0, s, g);
+    return hipGetLastError();
+}
 
 hipError_t launch_log_probs(const gns_ctx* c, const LogProbsArgs& a, int32_t type, hipStream_t s)
 {
-    const dim3 grid(row_grid(c, a.count.rows));
-    if (type == GNS_FP32) hipLaunchKernelGGL(k_log_probs<float>, grid, dim3(kBlock), 0, s, a);
-    else                  hipLaunchKernelGGL(k_log_probs<Bf16>, grid, dim3(kBlock), 0, s, a);
+    return type == GNS_FP32 ? launch_typed<float>(c, a, s) : launch_typed<Bf16>(c, a, s);
+}
+
+template <typename T, typename O, bool kEntropy>
+static hipError_t launch_backward_typed(const gns_ctx* c, const LogProbsBackwardArgs& a, hipStream_t s)
+{
+    const int32_t C = a.logits.width;
+    const int64_t rows = a.count.rows;
+    auto lies = [](const void* p, int64_t stride, size_t size) {      // of all rows against the 16-byte marks: their stride and first
+        return (uint32_t) (reinterpret_cast<uintptr_t>(p) % 16 + (uint64_t) stride * size % 16 * 16);
+    };
+    if constexpr (sizeof(T) == sizeof(O)) {
+        if (C > kShortClasses && lies(a.logits.data, a.logits.stride, sizeof(T)) == lies(a.d_logits.data, a.d_logits.stride, sizeof(T))) {
+            constexpr int32_t kTiles = 4;
+            const int32_t parts = (int32_t) (((int64_t) C + kTiles * kWaveTile - 1) / (kTiles * kWaveTile));
+            hipLaunchKernelGGL((k_log_probs_backward_long<T, kEntropy>), dim3(grid_of(c, (rows * parts + 3) / 4, 64)), dim3(kBlock), 0, s, a, parts, kTiles);
+            return hipGetLastError();
+        }
+    }
+    if (C <= 16) {
+        hipLaunchKernelGGL((k_log_probs_backward<T, O, kEntropy, 4>), dim3(grid_of(c, (rows + 63) / 64, 64)), dim3(kBlock), 0, s, a, C);
+    } else if (C <= kShortClasses) {
+        hipLaunchKernelGGL((k_log_probs_backward<T, O, kEntropy, 16>), dim3(grid_of(c, (rows + 15) / 16, 64)), dim3(kBlock), 0, s, a, C);
+    } else {
+        constexpr int32_t kChunk = 4096;
+        const int64_t work = rows * ((C + kChunk - 1) / kChunk);
+        hipLaunchKernelGGL((k_log_probs_backward<T, O, kEntropy, kWave>), dim3(grid_of(c, (work + 3) / 4, 64)), dim3(kBlock), 0, s, a, kChunk);
+    }
     return hipGetLastError();
 }
 
 hipError_t launch_log_probs_backward(const gns_ctx* c, const LogProbsBackwardArgs& a, int32_t type, int32_t out_type, hipStream_t s)
 {
-    const dim3 grid(row_grid(c, a.count.rows));
-    if (type == GNS_FP32 && out_type == GNS_FP32) hipLaunchKernelGGL((k_log_probs_backward<float, float>), grid, dim3(kBlock), 0, s, a);
-    else if (type == GNS_FP32)                    hipLaunchKernelGGL((k_log_probs_backward<float, Bf16>), grid, dim3(kBlock), 0, s, a);
-    else if (out_type == GNS_FP32)                hipLaunchKernelGGL((k_log_probs_backward<Bf16, float>), grid, dim3(kBlock), 0, s, a);
-    else                                          hipLaunchKernelGGL((k_log_probs_backward<Bf16, Bf16>), grid, dim3(kBlock), 0, s, a);
-    return hipGetLastError();
+    const bool entropy = a.g_entropy != nullptr;
+    if (type == GNS_FP32 && out_type == GNS_FP32)
+        return entropy ? launch_backward_typed<float, float, true>(c, a, s) : launch_backward_typed<float, float, false>(c, a, s);
+    if (type == GNS_FP32)
+        return entropy ? launch_backward_typed<float, Bf16, true>(c, a, s) : launch_backward_typed<float, Bf16, false>(c, a, s);
+    if (out_type == GNS_FP32)
+        return entropy ? launch_backward_typed<Bf16, float, true>(c, a, s) : launch_backward_typed<Bf16, float, false>(c, a, s);
+    return entropy ? launch_backward_typed<Bf16, Bf16, true>(c, a, s) : launch_backward_typed<Bf16, Bf16, false>(c, a, s);
 }
 
 }  // namespace gns

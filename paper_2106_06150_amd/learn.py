@@ -172,7 +172,7 @@ def gns_log_probs(ctx, logits, labels, logp, entropy, stats, top_index, top_logp
 
 
 def gns_log_probs_backward(ctx, logits, labels, stats, entropy, g_logp, g_entropy, d_logits, num_rows, stream=None):
-    """labels with g_logp, entropy with g_entropy may be None; d_logits may be logits itself."""
+    """g_logp (which needs labels) or g_entropy (which needs entropy) may be None; d_logits may be logits itself."""
     rows = max(num_rows, 0)
     _check(lib.gns_log_probs_backward(ctx, _rows(logits, num_rows), _flat(labels, torch.int32, rows),
                                       _flat(stats, torch.float32, 2 * rows), _flat(entropy, torch.float32, rows),

@@ -626,8 +626,8 @@ def test_refusals(ctx):
                  (lp, fp, None, None, 2, fp, None), (lp, fp, None, None, 0, fp, fp), (lp, fp, None, fp + 4, 0, None, None),
                  (lp, fp + 1, None, None, 0, None, None)):
         refused(einval, "gns_log_probs", rows(), *args, 4, wp, size, s)
-    for args in ((lp, None, None, fp, None), (lp, fp, None, None, None), (None, fp, None, fp, None), (lp, fp, fp, fp, None),
-                 (None, fp, None, None, None), (lp, fp + 4, None, fp, None)):
+    for args in ((lp, None, None, fp, None), (lp, fp, None, None, None), (None, fp, None, fp, None), (lp, fp, None, fp, fp),
+                 (None, fp, fp, None, None), (lp, fp + 4, None, fp, None)):
         refused(einval, "gns_log_probs_backward", rows(), *args, rows(), 4, s)
     refused(einval, "gns_log_probs_backward", rows(), lp, fp, None, fp, None, rows(width=63), 4, s)
     refused(einval, "gns_log_probs_backward", rows(), lp, fp, None, fp, None, rows(stride=128), 4, s)      # over the logits, another stride
