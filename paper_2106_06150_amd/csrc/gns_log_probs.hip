@@ -14,11 +14,19 @@ constexpr float kFar = -1000.f;               // e^kFar is zero in fp32
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
 
 // A value's place in the order of all values: larger floats have larger keys, and of equal ones (0 and -0 too) the lower index.
-struct Best {
-    float z;
-    int32_t index;
-};
-__device__ __forceinline__ bool before(const Best& a, const Best& b) { return a.z > b.z || (a.z == b.z && a.index < b.index); }
+typedef unsigned long long Key;
+constexpr Key kNoKey = 0x007FFFFFFFFFFFFFull;     // above every class of -infinity, below every other
+__device__ __forceinline__ Key key_of(float z, int32_t index)
+{
+    const uint32_t b = __float_as_uint(z + 0.f), flip = (uint32_t) ((int32_t) b >> 31) | 0x80000000u;
+    return (Key) (b ^ flip) << 32 | (uint32_t) ~index;
+}
+__device__ __forceinline__ float value_of(Key k)
+{
+    const uint32_t b = (uint32_t) (k >> 32);
+    return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
+}
+__device__ __forceinline__ int32_t index_of(Key k) { return (int32_t) ~(uint32_t) k; }
 
 template <int kCtrl>
 __device__ __forceinline__ float dpp_float(float v)
@@ -190,56 +198,60 @@ __global__ void __launch_bounds__(kBlock) k_log_probs_short(LogProbsArgs a)
     }
 }
 
-// The best classes a wave has seen, one a lane, in order.  What does not come before `last` is not among the row's best:
-// the last one that counts, or a bound from elsewhere.
+// The best classes a wave has seen, one a lane, in order (kNoKey: none).  What is not above `last` is not among the row's
+// best; `last_z` is its value.
 struct WaveList {
-    Best mine, last;
+    Key mine, last;
+    float last_z;
 };
+__device__ __forceinline__ WaveList empty_list() { return WaveList{kNoKey, kNoKey, -__builtin_inff()}; }
 
-__device__ __forceinline__ Best lane_best(const Best& b, int lane)
+__device__ __forceinline__ Key read_lane(Key k, int lane)
 {
-    return Best{__uint_as_float((uint32_t) __builtin_amdgcn_readlane((int) __float_as_uint(b.z), lane)), __builtin_amdgcn_readlane(b.index, lane)};
+    return (Key) (uint32_t) __builtin_amdgcn_readlane((int) (uint32_t) (k >> 32), lane) << 32 |
+           (uint32_t) __builtin_amdgcn_readlane((int) (uint32_t) k, lane);
 }
 
-__device__ __forceinline__ void insert(WaveList& list, const Best& b, int32_t top)
+__device__ __forceinline__ void insert(WaveList& list, Key k)
 {
-    const int lane = opaque_lane_id(), at = __popcll(__ballot(before(list.mine, b)));
-    Best up;                                                   // of the lane below
-    up.z = __uint_as_float((uint32_t) __builtin_amdgcn_update_dpp(0, (int) __float_as_uint(list.mine.z), 0x138, 0xf, 0xf, true));
-    up.index = __builtin_amdgcn_update_dpp(0, list.mine.index, 0x138, 0xf, 0xf, true);
-    list.mine = lane < at ? list.mine : lane == at ? b : up;
-    const Best bound = lane_best(list.mine, top - 1);          // none while the list is short
-    if (before(bound, list.last)) list.last = bound;
+    const int lane = opaque_lane_id(), at = __popcll(__ballot(list.mine > k));
+    const uint32_t hi = (uint32_t) __builtin_amdgcn_update_dpp(0, (int) (uint32_t) (list.mine >> 32), 0x138, 0xf, 0xf, true);
+    const uint32_t lo = (uint32_t) __builtin_amdgcn_update_dpp(0, (int) (uint32_t) list.mine, 0x138, 0xf, 0xf, true);
+    const Key below = (Key) hi << 32 | lo;                     // of the lane below
+    list.mine = lane < at ? list.mine : lane == at ? k : below;
 }
 
-// Takes up N values a lane; index_of(i) is the class of the lane's i-th.  -infinity is none.  Nearly all values are
-// passed over by one comparison of the lane's largest; equal values are told apart by their classes, so a row of one
-// value costs no insertions after the first.
-template <int N, typename Index>
-__device__ __forceinline__ void take_up(WaveList& list, const float (&z)[N], float largest, int32_t top, Index&& index_of)
+// Takes up N values a lane; class_of(i) is the class of the lane's i-th.  Nearly all values are passed over by one comparison
+// of the lane's largest; equal values are told apart by their classes, so a row of one value costs no insertions after
+// the first.
+template <int N, typename Class>
+__device__ __forceinline__ void take_up(WaveList& list, const float (&z)[N], float largest, int32_t top, Class&& class_of)
 {
-    if (!__ballot(largest >= list.last.z && largest > -__builtin_inff())) return;
+    if (!__ballot(largest >= list.last_z)) return;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int32_t index = index_of(i);
-        uint64_t hits = __ballot(z[i] > -__builtin_inff() && before(Best{z[i], index}, list.last));
-        for (; hits; hits &= hits - 1) {
-            const Best b = lane_best(Best{z[i], index}, __builtin_ctzll(hits));
-            if (before(b, list.last)) insert(list, b, top);
-        }
+        const Key k = key_of(z[i], class_of(i));
+        uint64_t hits = __ballot(k > list.last);
+        if (!hits) continue;
+        for (; hits; hits &= hits - 1) insert(list, read_lane(k, __builtin_ctzll(hits)));
+        const Key bound = read_lane(list.mine, top - 1);       // none while the list is short
+        if (bound > list.last) list.last = bound;
     }
+    list.last_z = value_of(list.last);
 }
 
-// A bound that at least `top` of the wave's values reach: the top-th of the lanes' largest.
-__device__ __forceinline__ float lanes_bound(float largest, int32_t top)
+// A bound that at least `top` of the wave's values reach, by way of the lanes' largest: the top-th of those.
+__device__ __forceinline__ void bound_by_lanes(WaveList& list, float largest, int32_t top)
 {
-    const int lane = opaque_lane_id();
-    int32_t rank = 0;
-    for (int i = 0; i < kWave; ++i) {
-        const float other = __uint_as_float((uint32_t) __builtin_amdgcn_readlane((int) __float_as_uint(largest), i));
-        rank += other > largest || (other == largest && i < lane) ? 1 : 0;
+    int32_t above = 0;
+    for (int i = 0; i < kWave; ++i)
+        above += __uint_as_float((uint32_t) __builtin_amdgcn_readlane((int) __float_as_uint(largest), i)) > largest ? 1 : 0;
+    const float bound = -max_of<kWave>(above < top ? -largest : -__builtin_inff());
+    const Key k = key_of(bound, INT32_MAX);                    // every class of that value is above it
+    if (k > list.last) {
+        list.last = k;
+        list.last_z = bound;
     }
-    return __uint_as_float((uint32_t) __builtin_amdgcn_readlane((int) __float_as_uint(largest), __builtin_ctzll(__ballot(rank == top - 1))));
 }
 
 template <typename T> constexpr int kVec = 16 / (int) sizeof(T);
@@ -260,7 +272,7 @@ struct LongArgs {
     int32_t parts;                // of a row
     int32_t tiles;                // of a part
     PartSums* sums;               // [rows x parts], if parts > 1
-    Best* best;                   // [rows x parts x top]
+    Key* best;                    // [rows x parts x top]
 };
 
 // Rows of any length: a wave per row, or per part of a row where there are few.  Pieces of 16 bytes are read at 16-byte
@@ -288,7 +300,7 @@ __global__ void __launch_bounds__(kBlock) k_log_probs_long(LongArgs g)
         float z_label = 0.f;
         if (g.parts == 1) z_label = label_logit<T>(a, r, &label);
         Softmax s = {kNone, 0.f, 0.f};
-        WaveList list = {{kNone, INT32_MAX}, {kNone, INT32_MAX}};
+        WaveList list = empty_list();
         bool first = true;
         if (part == 0) {                          // the single values: lanes 0 .. head - 1 and from 32 on
             const int32_t behind = C - head - body * V;
@@ -323,11 +335,8 @@ __global__ void __launch_bounds__(kBlock) k_log_probs_long(LongArgs g)
             raise(s, largest);
             add_values(s, z);
             if (top) {
-                if (first) {
-                    const float bound = lanes_bound(largest, top);
-                    if (bound > list.last.z) list.last = Best{bound, INT32_MAX};
-                    first = false;
-                }
+                if (first) bound_by_lanes(list, largest, top);
+                first = false;
                 take_up(list, z, largest, top, [&](int i) { return head + (p + i / V * kWave + lane) * V + i % V; });
             }
         }
@@ -340,9 +349,9 @@ __global__ void __launch_bounds__(kBlock) k_log_probs_long(LongArgs g)
         const RowResult o = result_of(s);
         if (lane == 0) write_row<T>(a, r, o, label, z_label);
         if (lane < top) {
-            const bool gone = o.bad || list.mine.z == kNone;
-            a.top_index[r * top + lane] = gone ? -1 : list.mine.index;
-            a.top_logp[r * top + lane] = o.bad ? quiet_nan() : gone ? kNone : log_p_of(o, list.mine.z);
+            const bool gone = o.bad || list.mine == kNoKey;
+            a.top_index[r * top + lane] = gone ? -1 : index_of(list.mine);
+            a.top_logp[r * top + lane] = o.bad ? quiet_nan() : gone ? kNone : log_p_of(o, value_of(list.mine));
         }
     }
 }
@@ -370,32 +379,29 @@ __global__ void __launch_bounds__(kWave) k_log_probs_join(LongArgs g)
         const RowResult o = result_of(s);
         if (lane == 0) write_row<T>(a, r, o, label, z_label);
         if (!top) continue;
-        WaveList list = {{kNone, INT32_MAX}, {kNone, INT32_MAX}};
-        const Best* from = g.best + r * g.parts * top;
+        WaveList list = empty_list();
+        const Key* from = g.best + r * g.parts * top;
         const int32_t n = g.parts * top;
-        for (int32_t i0 = 0; i0 < n; i0 += kWave * 8) {
-            float z[8];
-            int32_t index[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int32_t i = i0 + j * kWave + lane;
-                const Best b = i < n ? from[i] : Best{kNone, INT32_MAX};
-                z[j] = b.z;
-                index[j] = b.index;
-            }
+        constexpr int kTurn = 16;
+        for (int32_t i0 = 0; i0 < n; i0 += kWave * kTurn) {
+            float z[kTurn];
+            int32_t index[kTurn];
             float largest = kNone;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) largest = fmaxf(largest, z[j]);
-            if (i0 == 0) {
-                const float bound = lanes_bound(largest, top);
-                if (bound > kNone) list.last = Best{bound, INT32_MAX};
+            for (int j = 0; j < kTurn; ++j) {
+                const int32_t i = i0 + j * kWave + lane;
+                const Key k = i < n ? from[i] : kNoKey;
+                z[j] = value_of(k);
+                index[j] = index_of(k);
+                largest = fmaxf(largest, z[j]);
             }
+            if (i0 == 0) bound_by_lanes(list, largest, top);
             take_up(list, z, largest, top, [&](int j) { return index[j]; });
         }
         if (lane < top) {
-            const bool gone = o.bad || list.mine.z == kNone;
-            a.top_index[r * top + lane] = gone ? -1 : list.mine.index;
-            a.top_logp[r * top + lane] = o.bad ? quiet_nan() : gone ? kNone : log_p_of(o, list.mine.z);
+            const bool gone = o.bad || list.mine == kNoKey;
+            a.top_index[r * top + lane] = gone ? -1 : index_of(list.mine);
+            a.top_logp[r * top + lane] = o.bad ? quiet_nan() : gone ? kNone : log_p_of(o, value_of(list.mine));
         }
     }
 }
@@ -527,7 +533,7 @@ size_t log_probs_workspace(const gns_ctx* c, int32_t classes, int32_t top, int32
     if (classes <= kShortClasses) return 0;
     int32_t parts, tiles;
     split_rows(c, classes, rows, &parts, &tiles);
-    return parts == 1 ? 0 : sums_bytes(rows, parts) + (size_t) rows * (size_t) parts * (size_t) top * sizeof(Best);
+    return parts == 1 ? 0 : sums_bytes(rows, parts) + (size_t) rows * (size_t) parts * (size_t) top * sizeof(Key);
 }
 
 template <typename T, int L, int E>
@@ -552,7 +558,7 @@ static hipError_t launch_typed(const gns_ctx* c, const LogProbsArgs& a, hipStrea
     split_rows(c, C, a.count.rows, &g.parts, &g.tiles);
     if (g.parts > 1) {
         g.sums = static_cast<PartSums*>(a.workspace);
-        g.best = reinterpret_cast<Best*>(static_cast<char*>(a.workspace) + sums_bytes(a.count.rows, g.parts));
+        g.best = reinterpret_cast<Key*>(static_cast<char*>(a.workspace) + sums_bytes(a.count.rows, g.parts));
     }
     const int64_t blocks = ((int64_t) a.count.rows * g.parts + kBlock / kWave - 1) / (kBlock / kWave);
     hipLaunchKernelGGL(k_log_probs_long<T>, dim3(grid_of(c, blocks, 32)), dim3(kBlock), 0, s, g);
