@@ -1,9 +1,11 @@
-// Activation checkpoints in 8 bits: 32 columns share a power of two.
+// Activation checkpoints in 8 bits: 32 columns share a power of two 2^e, the smallest with which the largest magnitude a of
+// the group rounds to 127 steps or fewer, a < 127.5 * 2^e.  With a power of two the quantisation is exact arithmetic, and a
+// value q * 2^e is a bf16 value, which the matrix cores take as it is.  Bound by the bytes.
 #include "gns_learn.hpp"
 
 namespace gns {
 
-// Exponent byte of a group whose largest magnitude has these bits: e + 127 for the smallest e with a < 127.5 * 2^e.
+// Exponent byte (e + 127) of a group whose largest magnitude has these bits.
 __device__ __forceinline__ uint32_t group_exponent(uint32_t most)
 {
     const uint32_t biased = most >> 23;                       // E + 127
@@ -16,47 +18,93 @@ __device__ __forceinline__ uint32_t group_exponent(uint32_t most)
 // 2^e; 0 for byte 0, infinity for byte 255
 __device__ __forceinline__ float group_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-__device__ __forceinline__ int32_t group_step(float x, uint32_t byte)
+// 2^-e; 0 where a group has no values
+__device__ __forceinline__ float group_inverse(uint32_t byte) { return byte == 0 || byte == 255 ? 0.f : __uint_as_float((254u - byte) << 23); }
+
+__device__ __forceinline__ uint32_t step_of(float x, float inverse)
 {
-    if (byte == 0 || byte == 255) return 0;
-    const float t = rintf(x * __uint_as_float((254u - byte) << 23));
-    return (int32_t) fminf(fmaxf(t, -127.f), 127.f);
+    const float t = fminf(fmaxf(rintf(x * inverse), -127.f), 127.f);
+    return (uint32_t) (int32_t) t & 255u;
 }
 
-// 32 lanes per group, a value each.
-template <typename T>
+// Four lanes a group, eight consecutive values each (two pieces of 16 bytes of fp32, one of bf16), sixteen groups a wave.
+// kAligned: every row begins at a 16-byte mark, so a lane's values are pieces; else, and where a row ends inside, they are
+// read singly.
+template <typename T, bool kAligned>
 __global__ void __launch_bounds__(kBlock) k_checkpoint_save(CheckpointArgs a)
 {
     const int64_t total = (int64_t) a.count.get() * a.groups;
-    const int lane = lane_id(), l32 = lane & 31;
-    const int64_t step = (int64_t) gridDim.x * (kBlock / 32);
-    // both halves of a wave make as many turns, as the exchange between lanes asks for
-    for (int64_t g0 = (int64_t) blockIdx.x * (kBlock / 32) + (threadIdx.x >> 6) * 2; g0 < total; g0 += step) {
-        const int64_t g = g0 + (lane >> 5), gc = g < total ? g : total - 1;
-        const int64_t r = gc / a.groups;
-        const int32_t col = (int32_t) (gc - r * a.groups) * 32 + l32;
-        const float x = col < a.width ? load_at<T>(a.x, r, col) : 0.f;
-        uint32_t most = magnitude_bits(x);
-        for (int off = 16; off; off >>= 1) most = max(most, (uint32_t) __shfl_xor((int) most, off));
-        const uint64_t up = __ballot(x > 0.f);
+    const int64_t step = (int64_t) gridDim.x * (kBlock / 4);
+    // the lanes of a wave make as many turns, as the exchange between them asks for
+    for (int64_t g0 = ((int64_t) blockIdx.x * kBlock + (threadIdx.x & ~(kWave - 1))) / 4; g0 < total; g0 += step) {
+        const int lane = opaque_lane_id();
+        const int64_t g = g0 + lane / 4, gc = g < total ? g : total - 1;
+        const int64_t r = total <= 0xFFFFFFFFll ? (int64_t) ((uint32_t) gc / (uint32_t) a.groups) : gc / a.groups;
+        const int32_t col = (int32_t) (gc - r * a.groups) * 32 + (lane & 3) * 8;
+        const T* row = reinterpret_cast<const T*>(a.x.data) + r * a.x.stride;
+        float x[8];
+        if (kAligned && col + 8 <= a.width) {
+            struct alignas(16) Eight { T v[8]; };
+            const Eight v = *reinterpret_cast<const Eight*>(row + col);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = to_float(v.v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = col + i < a.width ? to_float(row[col + i]) : 0.f;
+        }
+        uint32_t most = 0, up = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            most = max(most, magnitude_bits(x[i]));
+            up |= x[i] > 0.f ? 1u << i : 0u;
+        }
+        up <<= (lane & 3) * 8;
+        most = max(most, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) most, 0xB1, 0xf, 0xf, true));       // lanes 1 0 3 2
+        up |= (uint32_t) __builtin_amdgcn_update_dpp(0, (int) up, 0xB1, 0xf, 0xf, true);
+        most = max(most, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) most, 0x4E, 0xf, 0xf, true));       // lanes 2 3 0 1
+        up |= (uint32_t) __builtin_amdgcn_update_dpp(0, (int) up, 0x4E, 0xf, 0xf, true);
         if (g >= total) continue;
         const uint32_t byte = group_exponent(most);
-        a.q[g * 32 + l32] = (int8_t) group_step(x, byte);
-        if (l32 == 0) {
+        const float inverse = group_inverse(byte);
+        uint2 q = make_uint2(0, 0);
+        if (inverse != 0.f) {                                 // (a spoilt group's values times zero are no numbers)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                q.x |= step_of(x[i], inverse) << (8 * i);
+                q.y |= step_of(x[4 + i], inverse) << (8 * i);
+            }
+        }
+        *reinterpret_cast<uint2*>(a.q + g * 32 + (lane & 3) * 8) = q;
+        if ((lane & 3) == 0) {
             a.exponents[g] = (uint8_t) byte;
-            if (a.positive) a.positive[g] = (uint32_t) (up >> (lane & 32));
+            if (a.positive) a.positive[g] = up;
         }
     }
 }
 
-template <typename T>
+// Four lanes a group, eight values each.
+template <typename T, bool kAligned>
 __global__ void __launch_bounds__(kBlock) k_checkpoint_load(CheckpointArgs a)
 {
-    const int64_t total = (int64_t) a.count.get() * a.groups * 32;
+    const int64_t total = (int64_t) a.count.get() * a.groups * 4;
     for (int64_t i = (int64_t) blockIdx.x * kBlock + threadIdx.x; i < total; i += (int64_t) gridDim.x * kBlock) {
-        const int64_t g = i >> 5, r = g / a.groups;
-        const int32_t col = (int32_t) (g - r * a.groups) * 32 + (int32_t) (i & 31);
-        if (col < a.width) store_at<T>(a.out, r, col, (float) a.q[i] * group_scale(a.exponents[g]));
+        const int64_t g = i >> 2;
+        const int64_t r = total <= 0xFFFFFFFFll ? (int64_t) ((uint32_t) g / (uint32_t) a.groups) : g / a.groups;
+        const int32_t col = (int32_t) (g - r * a.groups) * 32 + (int32_t) (i & 3) * 8;
+        if (col >= a.width) continue;
+        const uint2 q = *reinterpret_cast<const uint2*>(a.q + i * 8);
+        const float scale = group_scale(a.exponents[g]);
+        T* row = reinterpret_cast<T*>(a.out.data) + r * a.out.stride;
+        struct alignas(16) Eight { T v[8]; } v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v.v[j] = from_float<T>((float) (int8_t) ((j < 4 ? q.x : q.y) >> (8 * (j & 3))) * scale);
+        if (kAligned && col + 8 <= a.width) {
+            *reinterpret_cast<Eight*>(row + col) = v;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (col + j < a.width) row[col + j] = v.v[j];
+        }
     }
 }
 
@@ -66,20 +114,39 @@ static unsigned grid_of(const gns_ctx* c, int64_t blocks)
     return (unsigned) (blocks < most ? blocks : most);
 }
 
+// Whether every row begins at a 16-byte mark
+template <typename T>
+static bool at_marks(const void* data, int64_t stride)
+{
+    return reinterpret_cast<uintptr_t>(data) % 16 == 0 && (uint64_t) stride * sizeof(T) % 16 == 0;
+}
+
+template <typename T>
+static hipError_t launch_save(const gns_ctx* c, const CheckpointArgs& a, hipStream_t s)
+{
+    const dim3 grid(grid_of(c, ((int64_t) a.count.rows * a.groups + kBlock / 4 - 1) / (kBlock / 4)));
+    if (at_marks<T>(a.x.data, a.x.stride)) hipLaunchKernelGGL((k_checkpoint_save<T, true>), grid, dim3(kBlock), 0, s, a);
+    else                                   hipLaunchKernelGGL((k_checkpoint_save<T, false>), grid, dim3(kBlock), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_load(const gns_ctx* c, const CheckpointArgs& a, hipStream_t s)
+{
+    const dim3 grid(grid_of(c, ((int64_t) a.count.rows * a.groups + kBlock / 4 - 1) / (kBlock / 4)));
+    if (at_marks<T>(a.out.data, a.out.stride)) hipLaunchKernelGGL((k_checkpoint_load<T, true>), grid, dim3(kBlock), 0, s, a);
+    else                                       hipLaunchKernelGGL((k_checkpoint_load<T, false>), grid, dim3(kBlock), 0, s, a);
+    return hipGetLastError();
+}
+
 hipError_t launch_checkpoint_save(const gns_ctx* c, const CheckpointArgs& a, int32_t type, hipStream_t s)
 {
-    const dim3 grid(grid_of(c, ((int64_t) a.count.rows * a.groups + kBlock / 32 - 1) / (kBlock / 32)));
-    if (type == GNS_FP32) hipLaunchKernelGGL(k_checkpoint_save<float>, grid, dim3(kBlock), 0, s, a);
-    else                  hipLaunchKernelGGL(k_checkpoint_save<Bf16>, grid, dim3(kBlock), 0, s, a);
-    return hipGetLastError();
+    return type == GNS_FP32 ? launch_save<float>(c, a, s) : launch_save<Bf16>(c, a, s);
 }
 
 hipError_t launch_checkpoint_load(const gns_ctx* c, const CheckpointArgs& a, int32_t type, hipStream_t s)
 {
-    const dim3 grid(grid_of(c, ((int64_t) a.count.rows * a.groups * 32 + kBlock - 1) / kBlock));
-    if (type == GNS_FP32) hipLaunchKernelGGL(k_checkpoint_load<float>, grid, dim3(kBlock), 0, s, a);
-    else                  hipLaunchKernelGGL(k_checkpoint_load<Bf16>, grid, dim3(kBlock), 0, s, a);
-    return hipGetLastError();
+    return type == GNS_FP32 ? launch_load<float>(c, a, s) : launch_load<Bf16>(c, a, s);
 }
 
 }  // namespace gns
