@@ -3,85 +3,482 @@
 
 namespace gns {
 
-// One wave per row, two passes over it: the largest magnitude, then the values.
+// In this order only results that are too large overflow.
+__device__ __forceinline__ float output_of(int sum, float w_scale, float scale, float bias, int32_t relu)
+{
+    const float y = (float) sum * w_scale * scale + bias;
+    return relu ? relu_of(y) : y;
+}
+
+// Tile (m, n) of a block.  Blocks go to the eight XCDs in turn; each XCD's L2 gets a run of consecutive tiles, and those go
+// down eight rows of tiles before they go on to the next column, so that what runs together shares rows and weights.
+__device__ __forceinline__ void tile_of(int32_t block, int32_t m_tiles, int32_t n_tiles, int32_t* tm, int32_t* tn)
+{
+    const int32_t all = m_tiles * n_tiles, each = all / kXcds, more = all % kXcds;
+    const int32_t xcd = block % kXcds, turn = block / kXcds;
+    const int32_t t = xcd * each + (xcd < more ? xcd : more) + turn;
+    constexpr int32_t kBand = 8;
+    const int32_t band = t / (kBand * n_tiles), in = t - band * kBand * n_tiles;
+    const int32_t height = m_tiles - band * kBand < kBand ? m_tiles - band * kBand : kBand;
+    *tm = band * kBand + in % height;
+    *tn = in / height;
+}
+
+// Pieces of V consecutive columns of a row [x1 | x2]: 16 bytes of either type.
+template <typename T> constexpr int kPiece = 16 / (int) sizeof(T);
+
+// kAligned: both inputs' rows begin at 16-byte marks and f1 is a multiple of the piece, so a piece inside a row is one read;
+// else its values are read singly.  Columns past the last are zero.
+template <typename T, bool kAligned>
+__device__ __forceinline__ void load_piece(const QuantizeArgs& a, int64_t r, int32_t c, float (&x)[kPiece<T>])
+{
+    constexpr int V = kPiece<T>;
+    const int32_t f1 = a.x1.width, k = f1 + a.x2.width;
+    if (kAligned && c + V <= k) {
+        struct alignas(16) Piece { T v[V]; };
+        const T* from = c < f1 ? reinterpret_cast<const T*>(a.x1.data) + r * a.x1.stride + c
+                               : reinterpret_cast<const T*>(a.x2.data) + r * a.x2.stride + (c - f1);
+        const Piece p = *reinterpret_cast<const Piece*>(from);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = to_float(p.v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            x[i] = c + i < f1 ? load_at<T>(a.x1, r, c + i) : c + i < k ? load_at<T>(a.x2, r, c + i - f1) : 0.f;
+    }
+}
+
+struct RowScale {
+    float scale, inverse;         // inverse 0: the row has no values
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t most)
+{
+    const float amax = __uint_as_float(most);
+    if (most >= kInfBits) return RowScale{quiet_nan(), 0.f};
+    if (amax < 0x1p-120f) return RowScale{0.f, 0.f};
+    return RowScale{amax / 127.f, 127.f / amax};
+}
+
+template <int V>
+__device__ __forceinline__ uint32_t largest_of(const float (&x)[V], uint32_t most)
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) most = max(most, magnitude_bits(x[i]));
+    return most;
+}
+
+// Four values as bytes of a word; |x * inverse| is at most 127 and a bit, which rounds to 127.
+__device__ __forceinline__ uint32_t pack4(const float* x, float inverse)
+{
+    if (inverse == 0.f) return 0;                             // (an infinity times zero is no number)
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= ((uint32_t) (int32_t) rintf(x[i] * inverse) & 255u) << (8 * i);
+    return w;
+}
+
 template <typename T>
+__device__ __forceinline__ void store_piece(int8_t* to, const float (&x)[kPiece<T>], float inverse)
+{
+    if (kPiece<T> == 4) *reinterpret_cast<uint32_t*>(to) = pack4(x, inverse);
+    else                *reinterpret_cast<uint2*>(to) = make_uint2(pack4(x, inverse), pack4(x + 4, inverse));
+}
+
+template <int L>
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
+{
+    if (L > 1) v = max(v, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) v, 0xB1, 0xf, 0xf, true));       // lanes 1 0 3 2
+    if (L > 2) v = max(v, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) v, 0x4E, 0xf, 0xf, true));       // lanes 2 3 0 1
+    if (L > 4) v = max(v, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) v, 0x141, 0xf, 0xf, true));      // mirrored in 8
+    if (L > 8) v = max(v, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) v, 0x140, 0xf, 0xf, true));      // mirrored in 16
+    if (L > 16) v = max(v, (uint32_t) __shfl_xor((int) v, 16));
+    if (L > 32) v = max(v, (uint32_t) __shfl_xor((int) v, 32));
+    return v;
+}
+
+// Rows of up to L * P pieces: L lanes a row, P pieces a lane in registers; the row is read once.
+template <typename T, bool kAligned, int L, int P>
 __global__ void __launch_bounds__(kBlock) k_quantize_rows(QuantizeArgs a)
 {
-    const int32_t rows = a.count.get(), lane = lane_id();
-    const int32_t f1 = a.x1.width, k = f1 + a.x2.width;
-    for (int64_t r = (int64_t) blockIdx.x * (kBlock / kWave) + (threadIdx.x >> 6); r < rows; r += (int64_t) gridDim.x * (kBlock / kWave)) {
+    constexpr int V = kPiece<T>;
+    const int32_t rows = a.count.get();
+    const int64_t step = (int64_t) gridDim.x * (kBlock / L);
+    // the lanes of a wave make as many turns, as the exchange between them asks for
+    for (int64_t r0 = ((int64_t) blockIdx.x * kBlock + (threadIdx.x & ~(kWave - 1))) / L; r0 < rows; r0 += step) {
+        const int lane = opaque_lane_id(), l = lane & (L - 1);
+        const int64_t row = r0 + lane / L, r = row < rows ? row : rows - 1;
+        float x[P][V];
         uint32_t most = 0;
-        auto at = [&](int32_t c) { return c < f1 ? load_at<T>(a.x1, r, c) : load_at<T>(a.x2, r, c - f1); };
-        for (int32_t c = lane; c < k; c += kWave) most = max(most, magnitude_bits(at(c)));
-        for (int off = 32; off; off >>= 1) most = max(most, (uint32_t) __shfl_xor((int) most, off));
-        const float amax = __uint_as_float(most);
-        const bool none = most >= kInfBits || amax < 0x1p-120f;
-        const float inv = none ? 0.f : 127.f / amax;
-        for (int32_t c = lane; c < (int32_t) a.stride; c += kWave)
-            a.q[r * a.stride + c] = c < k && !none ? (int8_t) (int) rintf(at(c) * inv) : (int8_t) 0;
-        if (lane == 0) a.scale[r] = most >= kInfBits ? quiet_nan() : none ? 0.f : amax / 127.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) load_piece<T, kAligned>(a, r, (p * L + l) * V, x[p]);
+#pragma unroll
+        for (int p = 0; p < P; ++p) most = largest_of(x[p], most);
+        const RowScale s = row_scale(largest_of_lanes<L>(most));
+        if (row >= rows) continue;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if ((p * L + l) * V < (int32_t) a.stride) store_piece<T>(a.q + r * a.stride + (p * L + l) * V, x[p], s.inverse);
+        if (l == 0) a.scale[r] = s.scale;
     }
 }
 
-// 64 x 64 outputs a block, 4 x 4 a thread, four products of bytes at a time.
-template <typename T>
-__global__ void __launch_bounds__(kBlock) k_dense_int8(DenseInt8Args a)
+// Longer rows: a block per row, which reads it twice (the second time near by).
+constexpr int kLongBlock = 1024;
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kLongBlock) k_quantize_long(QuantizeArgs a)
 {
-    __shared__ int s_q[16][65], s_w[16][65];
+    constexpr int V = kPiece<T>;
+    __shared__ uint32_t s_most[kLongBlock / kWave];
+    const int32_t rows = a.count.get(), k = a.x1.width + a.x2.width;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        uint32_t most = 0;
+        for (int32_t c = (int32_t) threadIdx.x * V; c < k; c += kLongBlock * V) {
+            float x[V];
+            load_piece<T, kAligned>(a, r, c, x);
+            most = largest_of(x, most);
+        }
+        most = largest_of_lanes<kWave>(most);
+        __syncthreads();
+        if (opaque_lane_id() == 0) s_most[threadIdx.x >> 6] = most;
+        __syncthreads();
+        for (int w = 0; w < kLongBlock / kWave; ++w) most = max(most, s_most[w]);
+        const RowScale s = row_scale(most);
+        for (int32_t c = (int32_t) threadIdx.x * V; c < (int32_t) a.stride; c += kLongBlock * V) {
+            float x[V];
+            load_piece<T, kAligned>(a, r, c, x);
+            store_piece<T>(a.q + r * a.stride + c, x, s.inverse);
+        }
+        if (threadIdx.x == 0) a.scale[r] = s.scale;
+    }
+}
+
+typedef int int4v __attribute__((ext_vector_type(4)));
+typedef int int16v __attribute__((ext_vector_type(16)));
+
+constexpr int kStepBytes = 64;                // k of a stage
+
+// Waits for this wave's LDS accesses and for the block's other waves; reads from memory stay on their way.
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+__device__ __forceinline__ int row_turn(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
+
+// k_int8_tiles: BM x BN outputs a block, WM x WN a wave, products of 32 x 32 x 32 bytes.  A stage of 64 k of the rows and weights
+// is read two stages before it is written to LDS, and written two before it is multiplied; one barrier a stage.  So
+// nothing that the products wait for is less than a stage old: the last fragments of a stage are read while its first are
+// multiplied, the first of the next one while its last are.  Chunk c of 16 bytes of row r lies at c ^ row_turn(r) of the
+// row, so that reads of the same chunk of eight or sixteen rows spread over all banks.
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(DenseInt8Args a, int32_t m_tiles, int32_t n_tiles)
+{
+    constexpr int kWaves = (BM / WM) * (BN / WN), kLoads = (BM + BN) / 16 / kWaves;     // of 16 rows, by a wave and stage
+    constexpr int MI = WM / 32, NI = WN / 32, kStage = (BM + BN) * 4;
+    static_assert((BM + BN) / 16 % kWaves == 0 && BM / 16 % kLoads == 0, "a wave loads whole pieces of one side");
+    __shared__ int4v s_stage[3 * kStage];
     const int32_t rows = a.count.get(), n = a.out.width;
-    const int64_t r0 = (int64_t) blockIdx.x * 64;
-    const int32_t n0 = (int32_t) blockIdx.y * 64;
-    if (r0 >= rows) return;
-    const int tx = (int) threadIdx.x % 16, ty = (int) threadIdx.x / 16;
-    int acc[4][4] = {};
-    for (int32_t k0 = 0; k0 < (int32_t) a.stride; k0 += 64) {
-        for (int i = (int) threadIdx.x; i < 16 * 64; i += kBlock) {
-            const int row = i / 16, word = i % 16;
-            s_q[word][row] = r0 + row < rows ? *reinterpret_cast<const int*>(a.q + (r0 + row) * a.stride + k0 + word * 4) : 0;
-            s_w[word][row] = n0 + row < n ? *reinterpret_cast<const int*>(a.wq + (int64_t) (n0 + row) * a.stride + k0 + word * 4) : 0;
-        }
-        __syncthreads();
-        for (int w = 0; w < 16; ++w)
-            for (int i = 0; i < 4; ++i)
-                for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_sdot4(s_q[w][ty + 16 * i], s_w[w][tx + 16 * j], acc[i][j], false);
-        __syncthreads();
+    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
+    int32_t tm, tn;
+    tile_of((int32_t) blockIdx.x, m_tiles, n_tiles, &tm, &tn);
+    const int64_t m0 = (int64_t) tm * BM;
+    const int32_t n0 = tn * BN;
+    if (m0 >= rows) return;
+    const int32_t steps = (int32_t) (a.stride / kStepBytes);
+    // this wave's pieces: 16 rows each, of the rows' side or the weights'; those past the end repeat the last
+    const bool weights = wave * kLoads * 16 >= BM;
+    const int32_t first = wave * kLoads * 16 - (weights ? BM : 0);
+    const int64_t last = weights ? n - 1 - n0 : rows - 1 - m0;
+    const int8_t* base = weights ? a.wq + (int64_t) n0 * a.stride : a.q + m0 * a.stride;
+    const int32_t turned = (lane & 3) ^ row_turn(lane >> 2);
+    uint32_t from[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int32_t row = first + i * 16 + (lane >> 2), at = (int32_t) (row < last ? row : last);
+        from[i] = (uint32_t) at * (uint32_t) a.stride + (uint32_t) (lane & 3) * 16;
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int64_t r = r0 + ty + 16 * i;
-            const int32_t c = n0 + tx + 16 * j;
-            if (r >= rows || c >= n) continue;
-            float y = (float) acc[i][j] * a.w_scale[c] * a.scale[r];       // in this order only results that are too large overflow
-            if (a.bias) y += a.bias[c];
-            store_at<T>(a.out, r, c, a.relu ? relu_of(y) : y);
+    int4v* put_at = s_stage + (wave * kLoads * 16 + (lane >> 2)) * 4 + turned;
+    int4v read[2][kLoads];
+    const int8_t* next;                                       // of the step that is read
+    auto seek = [&](int32_t step) { next = base + (int64_t) (step < steps ? step : steps - 1) * kStepBytes; };   // past the last: the last again
+    auto fetch = [&](int set, int i) { read[set][i] = *reinterpret_cast<const int4v*>(next + from[i]); };
+    auto put = [&](int set, int stage, int i) { put_at[stage * kStage + i * 64] = read[set][i]; };
+    auto fetch_all = [&](int set, int32_t step) {
+        seek(step);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) fetch(set, i);
+        __builtin_amdgcn_sched_barrier(0);                    // in this order, or the first waits of the loop are for all reads
+    };
+    auto put_all = [&](int set, int stage) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) put(set, stage, i);
+    };
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+    const int l32 = lane & 31, kh = lane >> 5, bank = row_turn(l32);
+    int16v acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
+    int4v f[2][MI + NI];                                      // fragments of the rows, then of the weights
+    const int4v* x_at = s_stage + (wm + l32) * 4;
+    const int4v* w_at = s_stage + (BM + wn + l32) * 4;
+    auto get = [&](int h, int stage, int i) {
+        const int chunk = (2 * h + kh) ^ bank;
+        f[h][i] = i < MI ? x_at[stage * kStage + i * 128 + chunk] : w_at[stage * kStage + (i - MI) * 128 + chunk];
+    };
+    // the products of one half of a stage, and between them, one after the other, what else there is to do
+    auto multiply = [&](int h, auto&& other, int others) {
+        constexpr int kProducts = MI * NI;
+#pragma unroll
+        for (int m = 0; m < kProducts; ++m) {
+            acc[m / NI][m % NI] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[h][m / NI], f[h][MI + m % NI], acc[m / NI][m % NI], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int o = others * m / kProducts; o < others * (m + 1) / kProducts; ++o) other(o);
+            __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    int s0 = 0, s1 = 1, s2 = 2;                               // stages of this step, the next and the one after
+    fetch_all(0, 0);
+    fetch_all(1, 1);
+    put_all(0, 0);
+    fetch_all(0, 2);
+    put_all(1, 1);
+    fetch_all(1, 3);
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < MI + NI; ++i) get(0, 0, i);
+    // stage `step` is multiplied; what was read for step + 2 goes to LDS, what is read now is for step + 4
+    auto turn = [&](int set, int32_t step) {
+        seek(step + 4);
+        multiply(0, [&](int o) { if (o < MI + NI) get(1, s0, o); else put(set, s2, o - (MI + NI)); }, MI + NI + kLoads);
+        multiply(1, [&](int o) { if (o < MI + NI) get(0, s1, o); else fetch(set, o - (MI + NI)); }, MI + NI + kLoads);
+        const int t = s0;
+        s0 = s1; s1 = s2; s2 = t;
+        lds_barrier();
+    };
+    int32_t step = 0;
+    for (; step + 2 <= steps; step += 2) {
+        turn(0, step);
+        turn(1, step + 1);
+    }
+    if (step < steps) turn(0, step);
+    const bool whole = m0 + BM <= rows && n0 + BN <= n;
+    // (from a lane id the compiler cannot see through: what it would work out of this in front of the loop costs registers)
+    const int e_lane = opaque_lane_id(), e32 = e_lane & 31;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int64_t r0 = m0 + wm + i * 32 + 4 * (e_lane >> 5);
+        float scale[16];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int64_t r = r0 + 8 * (v >> 2) + (v & 3);
+            scale[v] = a.scale[r < rows ? r : rows - 1];
+        }
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int32_t c = n0 + wn + j * 32 + e32, cc = c < n ? c : n - 1;
+            const float w_scale = a.w_scale[cc], bias = a.bias ? a.bias[cc] : 0.f;
+            T* out = reinterpret_cast<T*>(a.out.data) + r0 * a.out.stride + c;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const T y = from_float<T>(output_of(acc[i][j][v], w_scale, scale[v], bias, a.relu));
+                if (whole || (r0 + 8 * (v >> 2) + (v & 3) < rows && c < n)) out[(8 * (v >> 2) + (v & 3)) * a.out.stride] = y;
+            }
+        }
+    }
 }
 
-static unsigned wave_rows_grid(const gns_ctx* c, int64_t rows)
+// k_int8_few: for rows by the ten, where the weights' bytes are all there is to do.  A block has 16 output channels and
+// all rows (16 a tile, up to MT tiles), its eight waves an eighth of k each, products of 16 x 16 x 64 bytes; their sums meet in
+// LDS.  kFused: the block quantises the rows itself into LDS (every block does, which costs less than a launch in front), while
+// its first weights are on their way.
+constexpr int kFewBlock = 512, kFewWaves = kFewBlock / kWave, kFewColumns = 16;
+constexpr int kFewDepth = 8;                  // reads of weights in flight
+constexpr size_t kFewLds = 64 * 1024;         // of quantised rows
+
+__host__ __device__ constexpr int64_t few_stride(int64_t stride) { return stride + 16; }        // of rows in LDS, off the banks' period
+
+template <typename T, typename X, bool kFused, bool kAligned, int MT>
+__global__ void __launch_bounds__(kFewBlock) k_int8_few(DenseInt8Args a, QuantizeArgs x)
 {
-    const int64_t blocks = (rows + kBlock / kWave - 1) / (kBlock / kWave), most = (int64_t) c->num_cus * 64;
+    constexpr int V = kPiece<X>;
+    extern __shared__ int4v s_rows[];                         // kFused: the rows in 8 bits
+    __shared__ int s_sum[kFewWaves][MT][4][kWave];
+    __shared__ uint32_t s_most[16];
+    const int32_t rows = a.count.get(), n = a.out.width, steps = (int32_t) (a.stride / 64);
+    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
+    const int l16 = lane & 15, kg = lane >> 4;
+    const int32_t n0 = (int32_t) blockIdx.x * kFewColumns, column = n0 + l16 < n ? n0 + l16 : n - 1;
+    const int32_t s0 = (int32_t) ((int64_t) steps * wave / kFewWaves), s1 = (int32_t) ((int64_t) steps * (wave + 1) / kFewWaves);
+    const int8_t* w = a.wq + (int64_t) column * a.stride + kg * 16;
+    int4v read[kFewDepth];
+    auto fetch = [&](int32_t from) {                          // steps past the last repeat it
+#pragma unroll
+        for (int d = 0; d < kFewDepth; ++d) read[d] = *reinterpret_cast<const int4v*>(w + (int64_t) (from + d < s1 ? from + d : s1 - 1) * 64);
+    };
+    if (s0 < s1) fetch(s0);
+    if (rows <= 0) return;
+    const int64_t pitch = few_stride(a.stride);
+    int8_t* const s_q = reinterpret_cast<int8_t*>(s_rows);
+    if (kFused) {
+        if (threadIdx.x < 16) s_most[threadIdx.x] = 0;
+        __syncthreads();
+        for (int32_t r = 0; r < rows; ++r) {
+            uint32_t most = 0;
+            for (int32_t c = (int32_t) threadIdx.x * V; c < a.k; c += kFewBlock * V) {
+                float v[V];
+                load_piece<X, kAligned>(x, r, c, v);
+                most = largest_of(v, most);
+            }
+            most = largest_of_lanes<kWave>(most);
+            if (lane == 0) atomicMax(&s_most[r], most);
+        }
+        __syncthreads();
+        for (int32_t r = 0; r < rows; ++r) {
+            const RowScale s = row_scale(s_most[r]);
+            for (int32_t c = (int32_t) threadIdx.x * V; c < (int32_t) a.stride; c += kFewBlock * V) {
+                float v[V];
+                load_piece<X, kAligned>(x, r, c, v);
+                store_piece<X>(s_q + r * pitch + c, v, s.inverse);
+            }
+        }
+        __syncthreads();
+    }
+    const int8_t* q[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int32_t r = t * 16 + l16 < rows ? t * 16 + l16 : rows - 1;
+        q[t] = (kFused ? s_q + r * pitch : a.q + (int64_t) r * a.stride) + kg * 16;
+    }
+    int4v acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = int4v{0, 0, 0, 0};
+    for (int32_t s = s0; s < s1; s += kFewDepth) {
+        int4v now[kFewDepth];
+#pragma unroll
+        for (int d = 0; d < kFewDepth; ++d) now[d] = read[d];
+        if (s + kFewDepth < s1) fetch(s + kFewDepth);
+#pragma unroll
+        for (int d = 0; d < kFewDepth; ++d) {
+            if (s + d >= s1) break;                           // wave-uniform
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const int4v v = *reinterpret_cast<const int4v*>(q[t] + (int64_t) (s + d) * 64);
+                acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v, now[d], acc[t], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s_sum[wave][t][v][lane] = acc[t][v];
+    __syncthreads();
+    // element v of lane l is row 4 * (l / 16) + v, column l % 16
+    for (int i = (int) threadIdx.x; i < MT * 4 * kWave; i += kFewBlock) {
+        const int t = i / (4 * kWave), v = i / kWave % 4, l = i % kWave;
+        const int32_t r = t * 16 + 4 * (l >> 4) + v, c = n0 + (l & 15);
+        if (r >= rows || c >= n) continue;
+        int sum = 0;
+#pragma unroll
+        for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][t][v][l];
+        const float scale = kFused ? row_scale(s_most[r & 15]).scale : a.scale[r];
+        store_at<T>(a.out, r, c, output_of(sum, a.w_scale[c], scale, a.bias ? a.bias[c] : 0.f, a.relu));
+    }
+}
+
+static unsigned grid_of(const gns_ctx* c, int64_t blocks, int per_cu)
+{
+    const int64_t most = (int64_t) c->num_cus * per_cu;
     return (unsigned) (blocks < most ? blocks : most);
+}
+
+// Whether pieces of these rows are single reads
+template <typename T>
+static bool whole_pieces(const QuantizeArgs& a)
+{
+    auto marks = [](const ConstRows& x) { return reinterpret_cast<uintptr_t>(x.data) % 16 == 0 && (uint64_t) x.stride * sizeof(T) % 16 == 0; };
+    return marks(a.x1) && (a.x2.width == 0 || (marks(a.x2) && a.x1.width % kPiece<T> == 0));
+}
+
+template <typename T, bool kAligned>
+static hipError_t launch_quantize_typed(const gns_ctx* c, const QuantizeArgs& a, hipStream_t s)
+{
+    const int64_t rows = a.count.rows, pieces = a.stride / kPiece<T>;
+    const dim3 short_grid(grid_of(c, (rows + 15) / 16, 32)), wave_grid(grid_of(c, (rows + 3) / 4, 32));
+    if (pieces <= 32)        hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 16, 2>), short_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 64)   hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 16, 4>), short_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 256)  hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 64, 4>), wave_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 512)  hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 64, 8>), wave_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 1024 && sizeof(T) == 4) hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 64, 16>), wave_grid, dim3(kBlock), 0, s, a);
+    else                     hipLaunchKernelGGL((k_quantize_long<T, kAligned>), dim3(grid_of(c, rows, 8)), dim3(kLongBlock), 0, s, a);
+    return hipGetLastError();
 }
 
 hipError_t launch_quantize(const gns_ctx* c, const QuantizeArgs& a, int32_t type, hipStream_t s)
 {
-    const dim3 grid(wave_rows_grid(c, a.count.rows));
-    if (type == GNS_FP32) hipLaunchKernelGGL(k_quantize_rows<float>, grid, dim3(kBlock), 0, s, a);
-    else                  hipLaunchKernelGGL(k_quantize_rows<Bf16>, grid, dim3(kBlock), 0, s, a);
+    if (type == GNS_FP32) return whole_pieces<float>(a) ? launch_quantize_typed<float, true>(c, a, s) : launch_quantize_typed<float, false>(c, a, s);
+    return whole_pieces<Bf16>(a) ? launch_quantize_typed<Bf16, true>(c, a, s) : launch_quantize_typed<Bf16, false>(c, a, s);
+}
+
+template <typename T, int BM, int BN, int WM, int WN>
+static hipError_t launch_tiles(const DenseInt8Args& a, hipStream_t s)
+{
+    const int64_t m_tiles = ((int64_t) a.count.rows + BM - 1) / BM, n_tiles = (a.out.width + BN - 1) / BN;
+    if (m_tiles * n_tiles > (1 << 22)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((k_int8_tiles<T, BM, BN, WM, WN>), dim3((unsigned) (m_tiles * n_tiles)), dim3((BM / WM) * (BN / WN) * kWave), 0, s, a,
+                       (int32_t) m_tiles, (int32_t) n_tiles);
     return hipGetLastError();
 }
 
-hipError_t launch_dense_int8(const gns_ctx*, const DenseInt8Args& a, int32_t out_type, hipStream_t s)
+constexpr int32_t kFewRows = 64;
+
+template <typename T>
+static hipError_t launch_typed(const gns_ctx* c, const DenseInt8Args& a, hipStream_t s)
 {
-    const dim3 grid((unsigned) ((a.count.rows + 63) / 64), (unsigned) ((a.out.width + 63) / 64));
-    if (out_type == GNS_FP32) hipLaunchKernelGGL(k_dense_int8<float>, grid, dim3(kBlock), 0, s, a);
-    else                      hipLaunchKernelGGL(k_dense_int8<Bf16>, grid, dim3(kBlock), 0, s, a);
-    return hipGetLastError();
+    if (a.count.rows <= kFewRows) {
+        const dim3 grid((unsigned) ((a.out.width + kFewColumns - 1) / kFewColumns));
+        if (a.count.rows <= 16)      hipLaunchKernelGGL((k_int8_few<T, float, false, false, 1>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
+        else if (a.count.rows <= 32) hipLaunchKernelGGL((k_int8_few<T, float, false, false, 2>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
+        else                         hipLaunchKernelGGL((k_int8_few<T, float, false, false, 4>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
+        return hipGetLastError();
+    }
+    auto tiles = [&](int64_t bm, int64_t bn) { return (a.count.rows + bm - 1) / bm * ((a.out.width + bn - 1) / bn); };
+    if (tiles(256, 256) >= c->num_cus && a.k >= 1024) return launch_tiles<T, 256, 256, 128, 64>(a, s);
+    if (tiles(128, 128) >= c->num_cus) return launch_tiles<T, 128, 128, 64, 64>(a, s);
+    return launch_tiles<T, 64, 64, 32, 32>(a, s);
+}
+
+hipError_t launch_dense_int8(const gns_ctx* c, const DenseInt8Args& a, int32_t out_type, hipStream_t s)
+{
+    return out_type == GNS_FP32 ? launch_typed<float>(c, a, s) : launch_typed<Bf16>(c, a, s);
+}
+
+template <typename T, typename X>
+static void launch_few_fused(const QuantizeArgs& x, const DenseInt8Args& a, size_t lds, hipStream_t s)
+{
+    const dim3 grid((unsigned) ((a.out.width + kFewColumns - 1) / kFewColumns));
+    if (whole_pieces<X>(x)) hipLaunchKernelGGL((k_int8_few<T, X, true, true, 1>), grid, dim3(kFewBlock), lds, s, a, x);
+    else                    hipLaunchKernelGGL((k_int8_few<T, X, true, false, 1>), grid, dim3(kFewBlock), lds, s, a, x);
 }
 
 hipError_t launch_sage_dense_int8(const gns_ctx* c, const QuantizeArgs& x, const DenseInt8Args& a, int32_t type, int32_t out_type,
                                   hipStream_t s)
 {
+    const int64_t lds = a.count.rows * few_stride(a.stride);
+    if (a.count.rows <= 16 && lds <= (int64_t) kFewLds) {
+        if (type == GNS_FP32 && out_type == GNS_FP32) launch_few_fused<float, float>(x, a, (size_t) lds, s);
+        else if (type == GNS_FP32)                    launch_few_fused<Bf16, float>(x, a, (size_t) lds, s);
+        else if (out_type == GNS_FP32)                launch_few_fused<float, Bf16>(x, a, (size_t) lds, s);
+        else                                          launch_few_fused<Bf16, Bf16>(x, a, (size_t) lds, s);
+        return hipGetLastError();
+    }
     const hipError_t e = launch_quantize(c, x, type, s);
     return e != hipSuccess ? e : launch_dense_int8(c, a, out_type, s);
 }
