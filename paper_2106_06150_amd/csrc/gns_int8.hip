@@ -328,25 +328,30 @@ __global__ void __launch_bounds__(kFewBlock) k_int8_few(DenseInt8Args a, Quantiz
     const int64_t pitch = few_stride(a.stride);
     int8_t* const s_q = reinterpret_cast<int8_t*>(s_rows);
     if (kFused) {
+        // all rows at once, a team of 32 to 512 threads each; the second reading finds them near by
+        const int32_t team = kFewBlock >> (rows > 1 ? 32 - __builtin_clz((uint32_t) rows - 1) : 0);
+        const int32_t r = (int32_t) threadIdx.x / team, c0 = (int32_t) threadIdx.x % team * V;
         if (threadIdx.x < 16) s_most[threadIdx.x] = 0;
         __syncthreads();
-        for (int32_t r = 0; r < rows; ++r) {
-            uint32_t most = 0;
-            for (int32_t c = (int32_t) threadIdx.x * V; c < a.k; c += kFewBlock * V) {
+        uint32_t most = 0;
+        if (r < rows) {
+#pragma unroll 4
+            for (int32_t c = c0; c < a.k; c += team * V) {
                 float v[V];
                 load_piece<X, kAligned>(x, r, c, v);
                 most = largest_of(v, most);
             }
-            most = largest_of_lanes<kWave>(most);
-            if (lane == 0) atomicMax(&s_most[r], most);
         }
+        most = largest_of_lanes<32>(most);
+        if ((lane & 31) == 0 && r < rows) atomicMax(&s_most[r], most);
         __syncthreads();
-        for (int32_t r = 0; r < rows; ++r) {
-            const RowScale s = row_scale(s_most[r]);
-            for (int32_t c = (int32_t) threadIdx.x * V; c < (int32_t) a.stride; c += kFewBlock * V) {
+        if (r < rows) {
+            const float inverse = row_scale(s_most[r]).inverse;
+#pragma unroll 4
+            for (int32_t c = c0; c < (int32_t) a.stride; c += team * V) {
                 float v[V];
                 load_piece<X, kAligned>(x, r, c, v);
-                store_piece<X>(s_q + r * pitch + c, v, s.inverse);
+                store_piece<X>(s_q + r * pitch + c, v, inverse);
             }
         }
         __syncthreads();
@@ -390,6 +395,119 @@ __global__ void __launch_bounds__(kFewBlock) k_int8_few(DenseInt8Args a, Quantiz
         for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][t][v][l];
         const float scale = kFused ? row_scale(s_most[r & 15]).scale : a.scale[r];
         store_at<T>(a.out, r, c, output_of(sum, a.w_scale[c], scale, a.bias ? a.bias[c] : 0.f, a.relu));
+    }
+}
+
+// k_int8_rows: many rows against weights that fit LDS: rows come in, are quantised and multiplied, and leave, without a
+// trip through memory in 8 bits (85,000 rows, 256 x 256, fp32: 17 us for the quantisation and 44 for the product otherwise).
+// A block per CU holds all weights; its waves walk tiles of 16 rows: a row is read by L lanes, P pieces each, quantised, turned
+// through a piece of LDS of the wave's own and multiplied, 16 x 16 x 64 bytes, with the weights as the left factor, so that a
+// lane gets four consecutive outputs of a row.  Bound by the rows' bytes, in and out.
+constexpr int64_t rows_lds(int64_t stride, int32_t n, int waves)
+{
+    return (few_stride(stride) * ((n + 15) / 16 * 16 + waves * 16)) + (int64_t) (n + 15) / 16 * 16 * 8;
+}
+
+template <typename T> struct alignas(16) Piece { T v[kPiece<T>]; };
+
+template <typename T, int L, int P, int kWaves>
+__global__ void __launch_bounds__(kWaves * kWave) k_int8_rows(DenseInt8Args a, QuantizeArgs x)
+{
+    constexpr int V = kPiece<T>, kTurns = 16 * L / kWave;      // of a wave over a tile's rows
+    constexpr int kGroups = 4;                                 // of 16 output columns, multiplied together
+    extern __shared__ int4v s_rows[];
+    const int32_t rows = a.count.get(), n = a.out.width, n16 = (n + 15) / 16 * 16, steps = (int32_t) (a.stride / 64);
+    const int32_t pitch = (int32_t) few_stride(a.stride), f1 = x.x1.width, k = a.k;
+    int8_t* const s_w = reinterpret_cast<int8_t*>(s_rows);
+    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6));
+    int8_t* const s_q = s_w + n16 * pitch + wave * 16 * pitch;
+    float* const s_scale = reinterpret_cast<float*>(s_w + (n16 + kWaves * 16) * pitch);
+    float* const s_bias = s_scale + n16;
+    const int32_t chunks = (int32_t) (a.stride / 16);
+    for (int32_t i = (int32_t) threadIdx.x; i < n16 * chunks; i += kWaves * kWave) {
+        const int32_t row = i / chunks, chunk = i - row * chunks;
+        *reinterpret_cast<int4v*>(s_w + row * pitch + chunk * 16) =
+            *reinterpret_cast<const int4v*>(a.wq + (int64_t) (row < n ? row : n - 1) * a.stride + chunk * 16);
+    }
+    for (int32_t i = (int32_t) threadIdx.x; i < n16; i += kWaves * kWave) {
+        s_scale[i] = a.w_scale[i < n ? i : n - 1];
+        s_bias[i] = a.bias ? a.bias[i < n ? i : n - 1] : 0.f;
+    }
+    __syncthreads();
+    const int32_t tiles = (rows + 15) / 16;
+    const bool stores = n % 4 == 0 && reinterpret_cast<uintptr_t>(a.out.data) % 16 == 0 && (uint64_t) a.out.stride * sizeof(T) % 16 == 0;
+    // the blocks' first waves take the first tiles: a remainder spreads over all CUs
+    for (int32_t tile = wave * (int32_t) gridDim.x + (int32_t) blockIdx.x; tile < tiles; tile += (int32_t) gridDim.x * kWaves) {
+        const int lane = opaque_lane_id(), l = lane & (L - 1), l16 = lane & 15, kg = lane >> 4;
+        const int64_t r0 = (int64_t) tile * 16;
+        Piece<T> v[kTurns][P];
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int64_t row = r0 + t * (kWave / L) + lane / L, r = row < rows ? row : rows - 1;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int32_t c = (p * L + l) * V, cc = c < k ? c : 0;        // lanes past the last column read the first
+                v[t][p] = *reinterpret_cast<const Piece<T>*>(cc < f1 ? reinterpret_cast<const T*>(x.x1.data) + r * x.x1.stride + cc
+                                                                     : reinterpret_cast<const T*>(x.x2.data) + r * x.x2.stride + (cc - f1));
+            }
+        }
+        float scale = 0.f;                                    // of row l16
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            uint32_t most = 0;
+            float f[P][V];
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[p][i] = (p * L + l) * V < k ? to_float(v[t][p].v[i]) : 0.f;
+                most = largest_of(f[p], most);
+            }
+            const RowScale s = row_scale(largest_of_lanes<L>(most));
+            const int32_t row = t * (kWave / L) + lane / L;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                if ((p * L + l) * V < (int32_t) a.stride) store_piece<T>(s_q + row * pitch + (p * L + l) * V, f[p], s.inverse);
+            const float other = __shfl(s.scale, l16 % (kWave / L) * L);
+            if (l16 / (kWave / L) == t) scale = other;
+        }
+        __builtin_amdgcn_wave_barrier();
+        const int8_t* q = s_q + l16 * pitch + kg * 16;
+        T* out = reinterpret_cast<T*>(a.out.data) + (r0 + l16) * a.out.stride;
+        for (int32_t c0 = 0; c0 < n16; c0 += 16 * kGroups) {
+            const int8_t* w[kGroups];
+            int4v acc[kGroups];
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {               // groups past the last repeat it
+                w[g] = s_w + ((c0 + g * 16 < n16 ? c0 + g * 16 : n16 - 16) + l16) * pitch + kg * 16;
+                acc[g] = int4v{0, 0, 0, 0};
+            }
+            for (int32_t s = 0; s < steps; ++s) {
+                const int4v right = *reinterpret_cast<const int4v*>(q + s * 64);
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+                    acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const int4v*>(w[g] + s * 64), right, acc[g], 0, 0, 0);
+            }
+            // element i of lane l is output column 4 * (l / 16) + i of row l % 16
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int32_t c = c0 + g * 16 + 4 * kg;
+                if (c0 + g * 16 >= n16 || r0 + l16 >= rows) continue;
+                const float4 ws = *reinterpret_cast<const float4*>(s_scale + c), b = *reinterpret_cast<const float4*>(s_bias + c);
+                struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
+                y.v[0] = from_float<T>(output_of(acc[g][0], ws.x, scale, b.x, a.relu));
+                y.v[1] = from_float<T>(output_of(acc[g][1], ws.y, scale, b.y, a.relu));
+                y.v[2] = from_float<T>(output_of(acc[g][2], ws.z, scale, b.z, a.relu));
+                y.v[3] = from_float<T>(output_of(acc[g][3], ws.w, scale, b.w, a.relu));
+                if (stores) {
+                    if (c < n) *reinterpret_cast<Four*>(out + c) = y;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (c + i < n) out[c + i] = y.v[i];
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -460,6 +578,38 @@ hipError_t launch_dense_int8(const gns_ctx* c, const DenseInt8Args& a, int32_t o
     return out_type == GNS_FP32 ? launch_typed<float>(c, a, s) : launch_typed<Bf16>(c, a, s);
 }
 
+// Rows and weights of k_int8_rows: rows of whole pieces, as many as a tile's registers hold, and weights that leave room in LDS
+template <typename T>
+static bool rows_fit(const gns_ctx* c, const QuantizeArgs& x, const DenseInt8Args& a)
+{
+    return a.count.rows >= c->num_cus * 32 && a.stride <= 512 && a.k % kPiece<T> == 0 && whole_pieces<T>(x) &&
+           rows_lds(a.stride, a.out.width, 8) <= (int64_t) c->lds_bitmap_limit;
+}
+
+template <typename T, int L, int P>
+static void launch_rows_of(const gns_ctx* c, const QuantizeArgs& x, const DenseInt8Args& a, hipStream_t s)
+{
+    const int64_t lds16 = rows_lds(a.stride, a.out.width, 16), lds8 = rows_lds(a.stride, a.out.width, 8);
+    if (P == 1 && lds16 <= (int64_t) c->lds_bitmap_limit) {
+        const dim3 grid((unsigned) (c->num_cus * (lds16 <= 80 * 1024 ? 2 : 1)));
+        hipLaunchKernelGGL((k_int8_rows<T, L, P, P == 1 ? 16 : 8>), grid, dim3(16 * kWave), (size_t) lds16, s, a, x);
+    } else {
+        const dim3 grid((unsigned) (c->num_cus * (lds8 <= 80 * 1024 ? 2 : 1)));
+        hipLaunchKernelGGL((k_int8_rows<T, L, P, 8>), grid, dim3(8 * kWave), (size_t) lds8, s, a, x);
+    }
+}
+
+template <typename T>
+static hipError_t launch_rows(const gns_ctx* c, const QuantizeArgs& x, const DenseInt8Args& a, hipStream_t s)
+{
+    constexpr int V = kPiece<T>;
+    if (a.stride <= 16 * V)      launch_rows_of<T, 16, 1>(c, x, a, s);
+    else if (a.stride <= 32 * V) launch_rows_of<T, 32, 1>(c, x, a, s);
+    else if (a.stride <= 64 * V) launch_rows_of<T, 64, 1>(c, x, a, s);
+    else if constexpr (V == 4)   launch_rows_of<T, 64, 2>(c, x, a, s);
+    return hipGetLastError();
+}
+
 template <typename T, typename X>
 static void launch_few_fused(const QuantizeArgs& x, const DenseInt8Args& a, size_t lds, hipStream_t s)
 {
@@ -479,6 +629,8 @@ hipError_t launch_sage_dense_int8(const gns_ctx* c, const QuantizeArgs& x, const
         else                                          launch_few_fused<Bf16, Bf16>(x, a, (size_t) lds, s);
         return hipGetLastError();
     }
+    if (type == GNS_FP32 && out_type == GNS_FP32 && rows_fit<float>(c, x, a)) return launch_rows<float>(c, x, a, s);
+    if (type == GNS_BF16 && out_type == GNS_BF16 && rows_fit<Bf16>(c, x, a)) return launch_rows<Bf16>(c, x, a, s);
     const hipError_t e = launch_quantize(c, x, type, s);
     return e != hipSuccess ? e : launch_dense_int8(c, a, out_type, s);
 }

@@ -147,7 +147,8 @@ def test_int8_product(ctx, rows, k, n, dtype):
 
 @TYPES
 @pytest.mark.parametrize("rows,f1,f2,n", [(1, 3, 0, 5), (1, 4096, 0, 300), (1, 100, 28, 47), (4, 700, 0, 130), (7, 256, 256, 48), (8, 64, 0, 1),
-                                          (16, 1024, 1, 64), (33, 129, 0, 65), (200, 128, 128, 256), (700, 300, 212, 100)])
+                                          (16, 1024, 1, 64), (33, 129, 0, 65), (200, 128, 128, 256), (700, 300, 212, 100),
+                                          (9000, 32, 28, 47), (8200, 100, 28, 48), (8300, 128, 128, 100), (8195, 256, 200, 36), (8192, 512, 0, 40)])
 @pytest.mark.parametrize("how", LAYOUTS)
 def test_update_step_in_int8(ctx, rows, f1, f2, n, how, dtype):
     g = gen(rows, f1, f2, n)
