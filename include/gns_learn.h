@@ -86,7 +86,7 @@ gns_status gns_checkpoint_load(gns_ctx* ctx, const int8_t* q_dev, const uint8_t*
  *   dz = d_out where bit n of the row's `positive` words (of the output, as gns_checkpoint_save writes them) is set, zero
  *        elsewhere, whatever d_out holds there; positive_dev NULL: dz = d_out
  *   dw[k, n] = sum_r x[r, k] * dz[r, n]     fp32[(f1 + f2) x hdim]
- *   db[n]    = sum_r dz[r, n]               fp32[hdim], or NULL
+ *   db[n]    = sum_r dz[r, n]               fp32[hdim], or NULL; comes with dw only
  *   dx[r, k] = sum_n dz[r, n] * w[k, n]     rows of f1 + f2 columns, in d_out's type, or NULL; w fp32[(f1 + f2) x hdim]
  * hdim = d_out->width.  dw may be NULL (then neither checkpoint is read).  Products have fp32's precision (fp32 values are
  * split into bf16 terms; w into two where dx is bf16), sums are fp32; an infinity in dz or w makes what it enters

@@ -10,20 +10,6 @@ __device__ __forceinline__ float output_of(int sum, float w_scale, float scale, 
     return relu ? relu_of(y) : y;
 }
 
-// Tile (m, n) of a block.  Blocks go to the eight XCDs in turn; each XCD's L2 gets a run of consecutive tiles, and those go
-// down eight rows of tiles before they go on to the next column, so that what runs together shares rows and weights.
-__device__ __forceinline__ void tile_of(int32_t block, int32_t m_tiles, int32_t n_tiles, int32_t* tm, int32_t* tn)
-{
-    const int32_t all = m_tiles * n_tiles, each = all / kXcds, more = all % kXcds;
-    const int32_t xcd = block % kXcds, turn = block / kXcds;
-    const int32_t t = xcd * each + (xcd < more ? xcd : more) + turn;
-    constexpr int32_t kBand = 8;
-    const int32_t band = t / (kBand * n_tiles), in = t - band * kBand * n_tiles;
-    const int32_t height = m_tiles - band * kBand < kBand ? m_tiles - band * kBand : kBand;
-    *tm = band * kBand + in % height;
-    *tn = in / height;
-}
-
 // Pieces of V consecutive columns of a row [x1 | x2]: 16 bytes of either type.
 template <typename T> constexpr int kPiece = 16 / (int) sizeof(T);
 
@@ -157,16 +143,6 @@ typedef int int16v __attribute__((ext_vector_type(16)));
 
 constexpr int kStepBytes = 64;                // k of a stage
 
-// Waits for this wave's LDS accesses and for the block's other waves; reads from memory stay on their way.
-__device__ __forceinline__ void lds_barrier()
-{
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
-__device__ __forceinline__ int row_turn(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
-
 // k_int8_tiles: BM x BN outputs a block, WM x WN a wave, products of 32 x 32 x 32 bytes.  A stage of 64 k of the rows and weights
 // is read two stages before it is written to LDS, and written two before it is multiplied; one barrier a stage.  So
 // nothing that the products wait for is less than a stage old: the last fragments of a stage are read while its first are
@@ -182,7 +158,7 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(De
     const int32_t rows = a.count.get(), n = a.out.width;
     const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
     int32_t tm, tn;
-    tile_of((int32_t) blockIdx.x, m_tiles, n_tiles, &tm, &tn);
+    tile_of(xcd_run((int32_t) blockIdx.x, m_tiles * n_tiles), m_tiles, n_tiles, &tm, &tn);
     const int64_t m0 = (int64_t) tm * BM;
     const int32_t n0 = tn * BN;
     if (m0 >= rows) return;

@@ -197,7 +197,7 @@ size_t gns_sage_dense_backward_workspace_bytes(const gns_ctx* ctx, int32_t f1, i
 {
     if (!ctx || f1 < 1 || f2 < 0 || hdim < 1 || (int64_t) f1 + f2 > GNS_MAX_WIDTH || hdim > GNS_MAX_WIDTH) return 0;
     const int32_t rows = worst_rows(ctx, num_rows);
-    return rows < 0 ? 0 : align256(backward_workspace(ctx, f1 + f2, hdim, rows));
+    return rows < 0 ? 0 : align256(backward_workspace(ctx, f1, f2, hdim, rows));
 }
 
 gns_status gns_sage_dense_backward(gns_ctx* ctx, const gns_rows* d_out, const uint32_t* positive_dev,
@@ -209,7 +209,8 @@ gns_status gns_sage_dense_backward(gns_ctx* ctx, const gns_rows* d_out, const ui
     if (!ctx) return GNS_EINVAL;
     GNS_REQUIRE_ROWS(d_out);
     GNS_REQUIRE(f1 >= 1 && f2 >= 0 && (int64_t) f1 + f2 <= GNS_MAX_WIDTH, "f1 or f2 out of range");
-    GNS_REQUIRE(dw_dev || db_dev || dx, "no gradient is wanted");
+    GNS_REQUIRE(dw_dev || dx, "no gradient is wanted");
+    GNS_REQUIRE(dw_dev || !db_dev, "db comes with dw only");
     GNS_REQUIRE(!misaligned(positive_dev, 4) && !misaligned(db_dev, 4), "positive and db must be aligned");
     if (dw_dev) {
         GNS_REQUIRE(q1_dev && exponents1_dev && (!f2 || (q2_dev && exponents2_dev)), "null checkpoint");
@@ -234,7 +235,7 @@ gns_status gns_sage_dense_backward(gns_ctx* ctx, const gns_rows* d_out, const ui
     a.x2 = PackedRows{q2_dev, exponents2_dev, f2, (int32_t) (((int64_t) f2 + 31) / 32)};
     a.w = w_dev; a.dw = dw_dev; a.db = db_dev;
     a.hdim = d_out->width;
-    a.partial = static_cast<float*>(workspace);
+    a.workspace = workspace;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     StageTimer t(ctx, GNS_STAGE_BACKWARD, s);
     const hipError_t e = launch_backward(ctx, a, d_out->type, s);

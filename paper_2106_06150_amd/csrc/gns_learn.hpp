@@ -58,6 +58,34 @@ __device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7FC00000
 // max(0, v) that keeps a NaN
 __device__ __forceinline__ float relu_of(float v) { return v < 0.f ? 0.f : v; }
 
+// Waits for this wave's LDS accesses and for the block's other waves; reads from memory stay on their way.
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Rows of a tile lie in LDS 64 bytes each, four chunks of 16: chunk c of row r at c ^ row_turn(r), so that reads of the same chunk
+// of eight or sixteen rows spread over all banks.
+__device__ __forceinline__ int row_turn(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
+
+// Tile (m, n) of a block.  Blocks go to the eight XCDs in turn; each XCD's L2 gets a run of consecutive tiles, and those go
+// down eight rows of tiles before they go on to the next column, so that what runs together shares rows and weights.
+__device__ __forceinline__ int32_t xcd_run(int32_t block, int32_t all)
+{
+    const int32_t each = all / kXcds, more = all % kXcds, xcd = block % kXcds;
+    return xcd * each + (xcd < more ? xcd : more) + block / kXcds;
+}
+__device__ __forceinline__ void tile_of(int32_t t, int32_t m_tiles, int32_t n_tiles, int32_t* tm, int32_t* tn)
+{
+    constexpr int32_t kBand = 8;
+    const int32_t band = t / (kBand * n_tiles), in = t - band * kBand * n_tiles;
+    const int32_t height = m_tiles - band * kBand < kBand ? m_tiles - band * kBand : kBand;
+    *tm = band * kBand + in % height;
+    *tn = in / height;
+}
+
 struct QuantizeArgs {
     ConstRows x1, x2;             // x2.width 0: one input
     int8_t* q;
@@ -104,7 +132,7 @@ struct BackwardArgs {
     MutRows dx;
     int32_t hdim;
     RowCount count;
-    float* partial;               // workspace
+    void* workspace;
 };
 
 struct LogProbsArgs {
@@ -140,7 +168,7 @@ hipError_t launch_sage_dense_int8(const gns_ctx* c, const QuantizeArgs& x, const
 hipError_t launch_checkpoint_save(const gns_ctx* c, const CheckpointArgs& a, int32_t type, hipStream_t s);
 hipError_t launch_checkpoint_load(const gns_ctx* c, const CheckpointArgs& a, int32_t type, hipStream_t s);
 // gns_backward.hip
-size_t backward_workspace(const gns_ctx* c, int32_t k, int32_t hdim, int32_t rows);
+size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows);
 hipError_t launch_backward(const gns_ctx* c, const BackwardArgs& a, int32_t type, hipStream_t s);
 // gns_log_probs.hip
 size_t log_probs_workspace(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows);

@@ -613,6 +613,7 @@ def test_refusals(ctx):
     backward(einval, f2=-1)
     backward(einval, f1=learn.GNS_MAX_WIDTH, f2=1)
     backward(einval, dw=None)                                                       # nothing is wanted
+    backward(einval, dw=None, db=fp, dx=rows())
     backward(einval, dw=fp + 1)
     backward(einval, db=fp + 1)
     backward(einval, positive=lp + 1)
