@@ -15,16 +15,25 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 __device__ __forceinline__ uint32_t lower_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 
-// Two values' three terms as packed pairs: each term is what is left, cut to its upper half.
-__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&t)[3])
+// The leading bf16 terms of eight values, packed, which are taken off the values.
+__device__ __forceinline__ uint4 take_terms(uint32_t (&v)[8])
 {
+    uint32_t t[4];
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
-        const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
-        t[q] = upper_halves(ua, ub);
-        a -= __uint_as_float(ua & 0xFFFF0000u);
-        b -= __uint_as_float(ub & 0xFFFF0000u);
-    }
+    for (int p = 0; p < 4; ++p) t[p] = upper_halves(v[2 * p], v[2 * p + 1]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) - __uint_as_float(v[i] & 0xFFFF0000u));
+    return make_uint4(t[0], t[1], t[2], t[3]);
+}
+
+// All bits set if bit i of w is, else none.
+__device__ __forceinline__ uint32_t spread_bit(uint32_t w, int i) { return (uint32_t) __builtin_amdgcn_sbfe((int) w, (uint32_t) i, 1); }
+
+// Lane kLane of each row of sixteen lanes, for all of the row (kBanks: for those of its quarters that have a bit; others keep `old`)
+template <int kLane, int kBanks = 0xf>
+__device__ __forceinline__ uint32_t row_broadcast(uint32_t old, uint32_t v)
+{
+    return (uint32_t) __builtin_amdgcn_update_dpp((int) old, (int) v, 0x150 + kLane, 0xf, kBanks, false);
 }
 
 // The products of terms: which term of the left factor meets which of the right, the smallest first.
@@ -59,12 +68,6 @@ struct Tile {
         bank = row_turn(l32);
         a_at = lds + (wave / (BN / WN) * WM + l32) * 4;
         b_at = lds + (BM * NA + wave % (BN / WN) * WN + l32) * 4;
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
     }
     // where a chunk of eight k of a row of the left or right factor goes
     static __device__ __forceinline__ int place_a(int plane, int row, int chunk) { return (plane * BM + row) * 4 + (chunk ^ row_turn(row)); }
@@ -91,15 +94,16 @@ struct Tile {
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    // Source: seek(set, step), then fetch(set, i), i < kFetches; put(set, stage, i), i < kPuts.  Steps past the last are read
-    // and never multiplied.
-    template <typename Source>
-    __device__ __forceinline__ void run(Source& source, int32_t steps)
+    // `tiles` tiles of `steps` steps each (a multiple of Source::kSets), one after the other without a pause; finish(tile) takes
+    // each one's outputs.  Source: seek(set), which goes on to the next step, then fetch(set, i), i < kFetches; put(set, stage, i),
+    // i < kPuts.  Steps past the last are read and never multiplied.
+    template <typename Source, typename Finish>
+    __device__ __forceinline__ void run(Source& source, int32_t steps, int32_t tiles, Finish&& finish)
     {
-        if (steps <= 0) return;
+        constexpr int kSets = Source::kSets;
         int s0 = 0, s1 = 1, s2 = 2;                           // stages of this step, the next and the one after
-        auto fetch_all = [&](int set, int32_t step) {
-            source.seek(set, step);
+        auto fetch_all = [&](int set) {
+            source.seek(set);
 #pragma unroll
             for (int i = 0; i < Source::kFetches; ++i) source.fetch(set, i);
             __builtin_amdgcn_sched_barrier(0);                // in this order, or the first waits of the loop are for all reads
@@ -108,29 +112,39 @@ struct Tile {
 #pragma unroll
             for (int i = 0; i < Source::kPuts; ++i) source.put(set, stage, i);
         };
-        fetch_all(0, 0);
-        fetch_all(1, 1);
-        put_all(0, 0);
-        fetch_all(0, 2);
-        put_all(1, 1);
-        fetch_all(1, 3);
-        lds_barrier();
-#pragma unroll
-        for (int i = 0; i < kFragments; ++i) get(0, 0, i);
-        auto turn = [&](int set, int32_t step) {
+        // a stage is multiplied; what was read for the step after the next goes to LDS, what is read now is for kSets further on
+        auto turn = [&](int set) {
             multiply(0, kFragments + Source::kPuts, [&](int o) { if (o < kFragments) get(1, s0, o); else source.put(set, s2, o - kFragments); });
-            source.seek(set, step + 4);
+            source.seek(set);
             multiply(1, kFragments + Source::kFetches, [&](int o) { if (o < kFragments) get(0, s1, o); else source.fetch(set, o - kFragments); });
             const int t = s0;
             s0 = s1; s1 = s2; s2 = t;
             lds_barrier();
         };
-        int32_t step = 0;
-        for (; step + 2 <= steps; step += 2) {
-            turn(0, step);
-            turn(1, step + 1);
+        if (steps > 0) {
+            fetch_all(0);
+            fetch_all(1);
+            put_all(0, 0);
+            put_all(1, 1);
+#pragma unroll
+            for (int i = 0; i < kSets; ++i) fetch_all(i);
+            lds_barrier();
+#pragma unroll
+            for (int i = 0; i < kFragments; ++i) get(0, 0, i);
         }
-        if (step < steps) turn(0, step);
+        for (int32_t tile = 0; tile < tiles; ++tile) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+            for (int32_t step = 0; step < steps; step += kSets) {
+#pragma unroll
+                for (int i = 0; i < kSets; ++i) turn(i);
+            }
+            finish(tile);
+        }
     }
     // visit(row of LDS of the left factor, of the right one, value) for the lane's outputs; adjacent lanes have adjacent rows
     // of the right factor
@@ -190,30 +204,33 @@ struct WeightsSource {
     static constexpr int kQuads = Tiles::kM / 4, kQuadsWave = kQuads < kWave ? kQuads : kWave;       // of columns, of X
     static constexpr int kLanes = kFloat ? Tiles::kN : Tiles::kN / 2;                               // that read a row of dz
     static constexpr int kReads = kFloat || kPairs ? 8 : 16;
-    static constexpr int kFetches = 4 + 1 + (kMask ? 1 : 0) + kReads, kPuts = 4 + 4;
+    static constexpr int kSets = 2, kFetches = 1 + (kMask ? 1 : 0) + 4 + kReads, kPuts = 1 + 4 + 2 + (kFloat ? 3 : 2);
     static_assert(kQuads * 8 == kThreads && kLanes * 4 == kThreads, "each thread has its share of a stage");
 
-    const BackwardArgs& a;
-    Tiles& tile;
-    int64_t r0, r1;                           // rows of the split
+    uint4* const lds;
+    const int64_t row_bytes;                  // of d_out
+    int64_t rest;                             // rows there are from the next step's first on
+    bool begun;
     int quad, rows4;                          // this thread's columns of X, and its four rows of a stage
     int column, chunk;                        // its first column of dz, and its eight rows
-    const int8_t* q;                          // its columns, row 0
-    const uint8_t* e;                         // the exponent this lane reads, row 0
-    const T* z;                               // its column, row 0
-    const uint32_t* m;                        // the word of the mask this lane reads, row 0
-    int64_t q_stride, e_stride, m_stride, r;
-    int e_row, m_row, to_second;
-    bool sums;                                // whether db is wanted of this block
-    uint32_t x[2][4], ex[2], d[2][kReads], words[2];
-    int32_t left[2];                          // rows of the split from the step's first on
-    uint32_t t[3][4];
-    float sum[2];
+    // of the step that is read, its first row:
+    const int8_t* q;                          // this thread's columns of X
+    const uint8_t* e;                         // the exponent this lane reads
+    const uint32_t* m;                        // the word of the mask this lane reads
+    const char* d_out;
+    uint32_t q_stride, e_stride, m_stride;
+    uint32_t z, second;                       // bytes from a row's first to this lane's column of dz, and to the next one
+    int e_row, m_row;
+    int last;                                 // row that there is
+    int32_t left[kSets];                      // rows there are from the step's first on
+    uint32_t x[kSets][4], ex[kSets], d[kSets][kReads], words[kSets];
+    float scale[4], sum[2];
 
-    __device__ __forceinline__ WeightsSource(const BackwardArgs& args, Tiles& tiles, int64_t first, int64_t end, int32_t c0, int32_t n0)
-        : a(args), tile(tiles), r0(first), r1(end)
+    __device__ __forceinline__ WeightsSource(const BackwardArgs& a, uint4* stages, int64_t first, int64_t end, int32_t c0, int32_t n0)
+        : lds(stages), row_bytes(a.d_out.stride * (int64_t) sizeof(T)), rest(end - first), begun(false)
     {
         const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
+        const int row16 = lane >> 4, i8 = lane & 7;
         const int32_t p1 = a.x1.groups * 32, all = p1 + a.x2.groups * 32, hdim = a.hdim;
         // columns past the last read the last ones again; they are not stored
         auto part_of = [&](int32_t c, int32_t* in) -> const PackedRows& { *in = c < p1 ? c : c - p1; return c < p1 ? a.x1 : a.x2; };
@@ -221,109 +238,112 @@ struct WeightsSource {
         rows4 = (kQuads == kWave ? wave : (int) threadIdx.x / kQuads) * 4;
         int32_t in;
         const PackedRows& part = part_of(min(c0 + quad * 4, all - 4), &in);
-        q = part.q + in;
-        q_stride = (int64_t) part.groups * 32;
-        constexpr int kGroups = kQuadsWave / 8;                // of the wave's columns; the first 32 lanes read a byte each
-        e_row = wave * (kWave / kQuads) * 4 + (lane & 31) / kGroups;
-        const PackedRows& part_e = part_of(min(c0 + ((lane & 31) % kGroups) * 32, all - 32), &in);
-        e = part_e.exponents + in / 32;
-        e_stride = part_e.groups;
+        q_stride = (uint32_t) part.groups * 32;
+        q = part.q + first * q_stride + in;
+        // Eight lanes share a group's exponents; a row of sixteen lanes has two groups, of which its first eight lanes read the
+        // exponents: of the first group's four rows, of the second's.
+        const int group = quad_group(row16) + (i8 >> 2);
+        e_row = (kQuadsWave == kWave ? wave * 4 : wave * 8 + (row16 >> 1) * 4) + (i8 & 3);
+        const PackedRows& part_e = part_of(min(c0 + group * 32, all - 32), &in);
+        e_stride = (uint32_t) part_e.groups;
+        e = part_e.exponents + first * e_stride + in / 32;
         const int lanes0 = wave * kWave % kLanes;              // the wave's first column of dz (of bf16: first pair)
         chunk = wave * kWave / kLanes;
         column = kFloat ? lanes0 + lane : 2 * (lanes0 + lane);
-        const int32_t n = min(n0 + column, kFloat ? hdim - 1 : kPairs ? hdim - 2 : hdim - 1);
-        z = reinterpret_cast<const T*>(a.d_out.data) + n;
-        to_second = min(n + 1, hdim - 1) - n;
-        m_stride = (hdim + 31) / 32;
-        constexpr int kWords = kFloat ? 2 : 4;                 // of the wave's columns; the first 16 or 32 lanes read one each
-        m_row = chunk * 8 + (lane & (8 * kWords - 1)) / kWords;
-        m = kMask ? a.positive + min((n0 + (kFloat ? lanes0 : 2 * lanes0)) / 32 + lane % kWords, (int32_t) m_stride - 1) : nullptr;
-        sums = false;
+        const int32_t n = min(n0 + column, !kFloat && kPairs ? hdim - 2 : hdim - 1);
+        d_out = static_cast<const char*>(a.d_out.data) + first * row_bytes;
+        z = (uint32_t) n * (uint32_t) sizeof(T);
+        second = n + 1 < hdim ? (uint32_t) sizeof(T) : 0u;
+        // a row of sixteen lanes has columns of one word; its first eight lanes read that of eight rows
+        m_stride = (uint32_t) (hdim + 31) / 32;
+        m_row = chunk * 8 + i8;
+        if constexpr (kMask) {
+            const int32_t word = kFloat ? (n0 + lanes0) / 32 + (row16 >> 1) : (n0 + 2 * lanes0) / 32 + row16;
+            m = a.positive + first * m_stride + min(word, (int32_t) m_stride - 1);
+        }
         sum[0] = sum[1] = 0.f;
     }
-    __device__ __forceinline__ void seek(int set, int32_t step)
+    static __device__ __forceinline__ int quad_group(int row16) { return kQuadsWave == kWave ? 2 * row16 : 2 * (row16 & 1); }
+    __device__ __forceinline__ void seek(int set)
     {
-        r = r0 + (int64_t) step * kStageK;
-        const int64_t rest = r1 - r;
+        // steps past the last read the last one's first row, which counts as nothing
+        const uint32_t on = begun && rest > 0 ? kStageK : 0;
+        begun = true;
+        q += (uint64_t) on * q_stride;
+        e += (uint64_t) on * e_stride;
+        if constexpr (kMask) m += (uint64_t) on * m_stride;
+        d_out += on * row_bytes;
         left[set] = (int32_t) (rest < kStageK ? rest : kStageK);
+        last = max(left[set], 1) - 1;
+        rest -= kStageK;
     }
-    // Rows past the split's last are read as the last; they count as nothing.
-    __device__ __forceinline__ int64_t row_at(int i) const { return r + i < r1 ? r + i : r1 - 1; }
     __device__ __forceinline__ void fetch(int set, int i)
     {
-        if (i < 4) {
-            x[set][i] = *reinterpret_cast<const uint32_t*>(q + row_at(rows4 + i) * q_stride);
-        } else if (i == 4) {
-            ex[set] = e[row_at(e_row) * e_stride];
-        } else if (i < 5 + kReads) {
-            const int j = i - 5;
-            const T* from = z + row_at(chunk * 8 + j % 8) * a.d_out.stride;
-            if constexpr (kFloat)      d[set][j] = *reinterpret_cast<const uint32_t*>(from);
-            else if constexpr (kPairs) d[set][j] = *reinterpret_cast<const uint32_t*>(from);
-            else                       d[set][j] = from[j < 8 ? 0 : to_second].bits;
+        if (i == 0) {
+            ex[set] = e[(uint64_t) (uint32_t) min(e_row, last) * e_stride];
+        } else if (kMask && i == 1) {
+            words[set] = m[(uint64_t) (uint32_t) min(m_row, last) * m_stride];
+        } else if (i < (kMask ? 6 : 5)) {
+            const int j = i - (kMask ? 2 : 1);
+            x[set][j] = *reinterpret_cast<const uint32_t*>(q + (uint64_t) (uint32_t) min(rows4 + j, last) * q_stride);
         } else {
-            words[set] = m[row_at(m_row) * m_stride];
+            const int j = i - (kMask ? 6 : 5);
+            const char* row = d_out + min(chunk * 8 + j % 8, last) * row_bytes;                   // wave-uniform
+            if constexpr (kFloat || kPairs) d[set][j] = *reinterpret_cast<const uint32_t*>(row + z);
+            else                            d[set][j] = *reinterpret_cast<const uint16_t*>(row + (j < 8 ? z : z + second));
         }
     }
     __device__ __forceinline__ void put(int set, int stage, int i)
     {
-        if (i < 4) put_x(set, stage, i);
-        else       put_z(set, stage, i - 4);
+        if (i == 0) {
+            const uint32_t own = e_row < left[set] ? ex[set] << 23 : 0u;
+            scale[0] = __uint_as_float(row_broadcast<4, 0xc>(row_broadcast<0>(0u, own), own));
+            scale[1] = __uint_as_float(row_broadcast<5, 0xc>(row_broadcast<1>(0u, own), own));
+            scale[2] = __uint_as_float(row_broadcast<6, 0xc>(row_broadcast<2>(0u, own), own));
+            scale[3] = __uint_as_float(row_broadcast<7, 0xc>(row_broadcast<3>(0u, own), own));
+        } else if (i < 5) {
+            const int j = i - 1;                              // column j of the four
+            uint32_t v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = __float_as_uint((float) (int8_t) (x[set][k] >> (8 * j)) * scale[k]);
+            uint2* to = reinterpret_cast<uint2*>(lds + stage * Tiles::kStage + Tiles::place_a(0, quad_row(quad * 4 + j), rows4 >> 3));
+            to[(rows4 >> 2) & 1] = make_uint2(upper_halves(v[0], v[1]), upper_halves(v[2], v[3]));
+        } else if (i == 5) {
+            const uint32_t own = kMask && m_row < left[set] ? words[set] : 0u;
+            keep_positive<0>(set, own); keep_positive<1>(set, own); keep_positive<2>(set, own); keep_positive<3>(set, own);
+        } else if (i == 6) {
+            const uint32_t own = kMask && m_row < left[set] ? words[set] : 0u;
+            keep_positive<4>(set, own); keep_positive<5>(set, own); keep_positive<6>(set, own); keep_positive<7>(set, own);
+        } else if constexpr (kFloat) {
+            uint32_t (&v)[8] = d[set];
+            lds[stage * Tiles::kStage + Tiles::place_b(i - 7, column, chunk)] = take_terms(v);
+        } else {
+            const int k = i - 7;
+            uint32_t t[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) t[p] = k == 0 ? lower_halves(d[set][2 * p], d[set][2 * p + 1]) : upper_halves(d[set][2 * p], d[set][2 * p + 1]);
+            lds[stage * Tiles::kStage + Tiles::place_b(0, pair_row(column + k), chunk)] = make_uint4(t[0], t[1], t[2], t[3]);
+        }
     }
-    __device__ __forceinline__ void put_x(int set, int stage, int j)          // column j of the four
+    // What the mask leaves of row kRow of the eight, and the sums.  (A row past the last has no exponents, so its products are zero.)
+    template <int kRow>
+    __device__ __forceinline__ void keep_positive(int set, uint32_t own)
     {
         const int lane = (int) threadIdx.x & 63;
-        constexpr int kGroups = kQuadsWave / 8;
-        uint32_t v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t byte = (uint32_t) __shfl((int) ex[set], (lane / kQuadsWave * 4 + i) * kGroups + lane % kQuadsWave / 8);
-            const float scale = __uint_as_float(rows4 + i < left[set] ? byte << 23 : 0u);
-            v[i] = __float_as_uint((float) (int8_t) (x[set][i] >> (8 * j)) * scale);
+        uint32_t v = d[set][kRow];
+        if constexpr (!kFloat && !kPairs) v |= d[set][kRow + kReads - 8] << 16;
+        if constexpr (kMask) {
+            const uint32_t w = row_broadcast<kRow>(0u, own);
+            if constexpr (kFloat) v &= spread_bit(w, lane & 31);
+            else                  v &= (spread_bit(w, 2 * (lane & 15)) & 0xFFFFu) | (spread_bit(w, 2 * (lane & 15) + 1) & 0xFFFF0000u);
         }
-        uint2* to = reinterpret_cast<uint2*>(tile.lds + stage * Tiles::kStage + Tiles::place_a(0, quad_row(quad * 4 + j), rows4 >> 3));
-        to[(rows4 >> 2) & 1] = make_uint2(upper_halves(v[0], v[1]), upper_halves(v[2], v[3]));
-    }
-    __device__ __forceinline__ void put_z(int set, int stage, int p)          // rows 2 p and 2 p + 1 of the eight
-    {
-        const int lane = (int) threadIdx.x & 63;
-        uint32_t v[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int i = 2 * p + h;
-            if constexpr (kFloat) {
-                bool keep = chunk * 8 + i < left[set];
-                if (kMask) keep = keep && ((uint32_t) __shfl((int) words[set], i * 2 + (lane >> 5)) >> (lane & 31) & 1u);
-                v[h] = keep ? d[set][i] : 0u;
-            } else {
-                v[h] = kPairs ? d[set][i] : d[set][i] | d[set][i + kReads - 8] << 16;
-                uint32_t keep = chunk * 8 + i < left[set] ? 3u : 0u;
-                if (kMask) keep &= (uint32_t) __shfl((int) words[set], i * 4 + (lane >> 4)) >> (2 * (lane & 15));
-                v[h] &= (keep & 1u ? 0xFFFFu : 0u) | (keep & 2u ? 0xFFFF0000u : 0u);
-            }
-        }
+        d[set][kRow] = v;
+        const uint32_t in = kMask || chunk * 8 + kRow < left[set] ? v : 0u;
         if constexpr (kFloat) {
-            if (sums) sum[0] += __uint_as_float(v[0]) + __uint_as_float(v[1]);
-            uint32_t pair[3];
-            split_pair(__uint_as_float(v[0]), __uint_as_float(v[1]), pair);
-#pragma unroll
-            for (int k = 0; k < 3; ++k) t[k][p] = pair[k];
+            sum[0] += __uint_as_float(in);
         } else {
-            t[0][p] = lower_halves(v[0], v[1]);
-            t[1][p] = upper_halves(v[0], v[1]);
-            if (sums) {
-                sum[0] += __uint_as_float(v[0] << 16) + __uint_as_float(v[1] << 16);
-                sum[1] += __uint_as_float(v[0] & 0xFFFF0000u) + __uint_as_float(v[1] & 0xFFFF0000u);
-            }
-        }
-        if (p < 3) return;
-        uint4* to = tile.lds + stage * Tiles::kStage;
-        if constexpr (kFloat) {
-#pragma unroll
-            for (int k = 0; k < 3; ++k) to[Tiles::place_b(k, column, chunk)] = make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) to[Tiles::place_b(0, pair_row(column + k), chunk)] = make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]);
+            sum[0] += __uint_as_float(in << 16);
+            sum[1] += __uint_as_float(in & 0xFFFF0000u);
         }
     }
 };
@@ -340,57 +360,106 @@ __global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
     int32_t tm, tn;
     tile_of(t - split * all, g.m_tiles, g.n_tiles, &tm, &tn);
     const int32_t c0 = tm * Tiles::kM, n0 = tn * Tiles::kN;
-    const int64_t each = ((rows + g.splits - 1) / g.splits + kStageK - 1) / kStageK * kStageK;
+    constexpr int kRound = kStageK * Source::kSets;
+    const int64_t each = ((rows + g.splits - 1) / g.splits + kRound - 1) / kRound * kRound;
     const int64_t first = split * each < rows ? split * each : rows, end = first + each < rows ? first + each : rows;
     Tiles tile(s_stage);
-    Source source(a, tile, first, end, c0, n0);
-    source.sums = g.db && tm == 0;
-    tile.run(source, (int32_t) ((end - first + kStageK - 1) / kStageK));
-    if (g.db && tm == 0) {                                    // eight rows a thread and stage, four chunks of them
-        float* s_sum = reinterpret_cast<float*>(s_stage);     // [4][Tiles::kN]
-        __syncthreads();
-        s_sum[source.chunk * Tiles::kN + source.column] = source.sum[0];
-        if (sizeof(T) == 2) s_sum[source.chunk * Tiles::kN + source.column + 1] = source.sum[1];
-        __syncthreads();
-        const int n = (int) threadIdx.x;
-        if (n < Tiles::kN && n0 + n < a.hdim)
-            g.db[(int64_t) split * a.hdim + n0 + n] = (s_sum[n] + s_sum[Tiles::kN + n]) + (s_sum[2 * Tiles::kN + n] + s_sum[3 * Tiles::kN + n]);
-    }
+    Source source(a, s_stage, first, end, c0, n0);
     float* dw = g.dw + (int64_t) split * (a.x1.width + a.x2.width) * a.hdim;
-    tile.each([&](int m, int n, float v) {
-        const int32_t k = weight_row(a, c0 + quad_column(m)), c = n0 + (sizeof(T) == 4 ? n : pair_column(n));
-        if (k >= 0 && c < a.hdim) dw[(int64_t) k * a.hdim + c] = v;
+    tile.run(source, (int32_t) ((end - first + kRound - 1) / kRound) * Source::kSets, 1, [&](int32_t) {
+        tile.each([&](int m, int n, float v) {
+            const int32_t k = weight_row(a, c0 + quad_column(m)), c = n0 + (sizeof(T) == 4 ? n : pair_column(n));
+            if (k >= 0 && c < a.hdim) dw[(int64_t) k * a.hdim + c] = v;
+        });
     });
+    if (!g.db || tm != 0) return;
+    float* s_sum = reinterpret_cast<float*>(s_stage);         // [4][Tiles::kN]: of the four threads that read a column
+    __syncthreads();
+    s_sum[source.chunk * Tiles::kN + source.column] = source.sum[0];
+    if (sizeof(T) == 2) s_sum[source.chunk * Tiles::kN + source.column + 1] = source.sum[1];
+    __syncthreads();
+    const int n = (int) threadIdx.x;
+    if (n < Tiles::kN && n0 + n < a.hdim)
+        g.db[(int64_t) split * a.hdim + n0 + n] = (s_sum[n] + s_sum[Tiles::kN + n]) + (s_sum[2 * Tiles::kN + n] + s_sum[3 * Tiles::kN + n]);
 }
 
-// Sums of the splits, in their order.
-__global__ void __launch_bounds__(kBlock) k_join_splits(const float* parts, int32_t splits, int64_t n, float* out)
+// Between the two products: the splits' sums, and W in bf16 terms for dx: [plane][f1 + f2][hdim rounded up to kStageK], zeros
+// behind hdim.  Items of four values; a sum's splits are shared by sixteen threads, since there may be few sums of many splits.
+struct BetweenArgs {
+    const float *dw_parts, *db_parts, *w;     // null: nothing to join; null: no db; null: no dx
+    float *dw, *db;
+    uint16_t* terms;
+    int64_t k;
+    int32_t hdim, pitch, splits, planes;
+    int32_t join_blocks;                      // the grid's first; the others cut W
+};
+
+constexpr int kJoinItems = 16, kJoinThreads = kBlock / kJoinItems;
+
+// Values i .. i + 3 of n; marks: they are one read.
+__device__ __forceinline__ float4 load_four(const float* p, int64_t i, int64_t n, bool marks)
 {
-    for (int64_t i = (int64_t) blockIdx.x * kBlock + threadIdx.x; i < n; i += (int64_t) gridDim.x * kBlock) {
-        float v = 0.f;
+    if (marks && i + 4 <= n) return *reinterpret_cast<const float4*>(p + i);
+    return make_float4(i < n ? p[i] : 0.f, i + 1 < n ? p[i + 1] : 0.f, i + 2 < n ? p[i + 2] : 0.f, i + 3 < n ? p[i + 3] : 0.f);
+}
+
+__global__ void __launch_bounds__(kBlock) k_backward_between(BetweenArgs a)
+{
+    __shared__ float4 s_part[kJoinThreads][kJoinItems];
+    if ((int32_t) blockIdx.x < a.join_blocks) {
+        const int64_t n = a.k * a.hdim, joins = (n + 3) / 4, all = joins + (a.db_parts ? (a.hdim + 3) / 4 : 0);
+        const int item = (int) threadIdx.x % kJoinItems, part = (int) threadIdx.x / kJoinItems;
+        for (int64_t i0 = (int64_t) blockIdx.x * kJoinItems; i0 < all; i0 += (int64_t) a.join_blocks * kJoinItems) {
+            const bool bias = i0 + item >= joins;
+            const float* parts = bias ? a.db_parts : a.dw_parts;
+            const int64_t i = 4 * (bias ? i0 + item - joins : i0 + item), count = bias ? a.hdim : n;
+            const bool marks = count % 4 == 0;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i0 + item < all) {
 #pragma unroll 8
-        for (int32_t s = 0; s < splits; ++s) v += parts[s * n + i];
-        out[i] = v;
+                for (int32_t s = part; s < a.splits; s += kJoinThreads) {
+                    const float4 p = load_four(parts + s * count, i, count, marks);
+                    v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+                }
+            }
+            __syncthreads();
+            s_part[part][item] = v;
+            __syncthreads();
+            if (part == 0 && i0 + item < all) {
+#pragma unroll
+                for (int p = 1; p < kJoinThreads; ++p) {
+                    const float4 w = s_part[p][item];
+                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                }
+                float* out = (bias ? a.db : a.dw) + i;
+                out[0] = v.x;
+                if (i + 1 < count) out[1] = v.y;
+                if (i + 2 < count) out[2] = v.z;
+                if (i + 3 < count) out[3] = v.w;
+            }
+        }
+        return;
     }
-}
-
-// ---- dx -----------------------------------------------------------------------------------------------------------
-// W in bf16 terms: [plane][f1 + f2][hdim rounded up to kStageK], zeros behind hdim.
-__global__ void __launch_bounds__(kBlock) k_split_weights(const float* w, int64_t rows, int32_t hdim, int32_t pitch, int planes, uint16_t* out)
-{
-    const int64_t n = rows * pitch;
-    for (int64_t i = (int64_t) blockIdx.x * kBlock + threadIdx.x; i < n; i += (int64_t) gridDim.x * kBlock) {
-        const int64_t r = i / pitch;
-        const int32_t c = (int32_t) (i - r * pitch);
-        float v = c < hdim ? w[r * hdim + c] : 0.f;
-        for (int p = 0; p < planes; ++p) {
-            const uint32_t u = __float_as_uint(v);
-            out[p * n + i] = (uint16_t) (u >> 16);
-            v -= __uint_as_float(u & 0xFFFF0000u);
+    const int64_t fours = a.pitch / 4, terms = a.k * fours;
+    const int32_t block = (int32_t) blockIdx.x - a.join_blocks, blocks = (int32_t) gridDim.x - a.join_blocks;
+    const bool marks = a.hdim % 4 == 0 && reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
+    for (int64_t t = (int64_t) block * kBlock + threadIdx.x; t < terms; t += (int64_t) blocks * kBlock) {
+        const int64_t row = t / fours, c = (t - row * fours) * 4;
+        const float4 four = load_four(a.w + row * a.hdim, c, a.hdim, marks);
+        float v[4] = {four.x, four.y, four.z, four.w};
+        for (int p = 0; p < a.planes; ++p) {
+            uint32_t u[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                u[j] = __float_as_uint(v[j]);
+                v[j] -= __uint_as_float(u[j] & 0xFFFF0000u);
+            }
+            *reinterpret_cast<uint2*>(a.terms + (p * a.k + row) * a.pitch + c) = make_uint2(upper_halves(u[0], u[1]), upper_halves(u[2], u[3]));
         }
     }
 }
 
+// ---- dx -----------------------------------------------------------------------------------------------------------
 struct InputArgs {
     BackwardArgs a;
     int32_t m_tiles, n_tiles, pitch;
@@ -404,99 +473,121 @@ template <> struct InputTile<Bf16, 512> { typedef Tile<256, 128, 64, 64, 1, 2> T
 template <> struct InputTile<Bf16, 256> { typedef Tile<128, 128, 64, 64, 1, 2> Type; };
 
 // A thread reads eight columns of a row of dz (of two rows of bf16), and as many of W's planes.  kWhole: rows of dz begin at
-// 16-byte marks and hdim is a multiple of eight, so eight columns are one or two reads; else they are read singly.
+// 16-byte marks and hdim is a multiple of eight, so eight columns are one or two reads; else they are read singly.  A block goes
+// through tiles, `stride` apart.
 template <typename T, int kThreads, bool kMask, bool kWhole>
 struct InputSource {
     typedef typename InputTile<T, kThreads>::Type Tiles;
     static constexpr bool kFloat = sizeof(T) == 4;
     static constexpr int kPlanes = kFloat ? 3 : 2, kStep = kThreads / 4;                            // rows the threads cover at once
     static constexpr int kRowsA = Tiles::kM / kStep, kRowsB = Tiles::kN / kStep, kWords = kFloat ? 8 : 4;
-    static constexpr int kFetches = kRowsA * (1 + (kMask ? 1 : 0)) + kRowsB * kPlanes;
-    static constexpr int kPuts = kRowsA * 4 + kRowsB * kPlanes;
+    static constexpr int kSets = kFloat ? 2 : 4, kFetches = kRowsA * (1 + (kMask ? 1 : 0)) + kRowsB * kPlanes;
+    static constexpr int kPutsA = kFloat ? 4 : 2, kPuts = kRowsA * kPutsA + kRowsB * kPlanes;
 
-    const BackwardArgs& a;
-    Tiles& tile;
+    const InputArgs& g;
+    uint4* const lds;
+    const int64_t rows, K;
+    const int32_t stride, columns;            // columns: hdim rounded up to whole turns of kSets steps
+    int32_t t, n0;                            // tile and first column of the next step
     int row, chunk;
-    int32_t n, pitch, words_each;
-    const T* z[kRowsA];
+    const char* z[kRowsA];                    // of the step that is read: this thread's columns
     const uint32_t* m[kRowsA];
     const uint16_t* w[kRowsB];
-    int64_t plane;
-    uint32_t d[2][kRowsA][kWords], words[2][kRowsA];
-    uint4 planes[2][kRowsB][kPlanes];
-    int32_t at[2];                            // the step's first column for this thread
-    uint32_t t[3][4];
+    int32_t inside;                           // of the eight columns
+    uint32_t d[kSets][kRowsA][kWords], words[kSets][kRowsA], keep[kSets];
+    uint4 planes[kSets][kRowsB][kPlanes];
 
-    __device__ __forceinline__ InputSource(const InputArgs& g, Tiles& tiles, int64_t r0, int64_t rows, int32_t k0) : a(g.a), tile(tiles), pitch(g.pitch)
+    __device__ __forceinline__ InputSource(const InputArgs& args, uint4* stages, int64_t rows_, int32_t first, int32_t stride_)
+        : g(args), lds(stages), rows(rows_), K(args.a.x1.width + args.a.x2.width), stride(stride_),
+          columns((args.a.hdim + kStageK * kSets - 1) / (kStageK * kSets) * (kStageK * kSets)), t(first), n0(0)
     {
         row = (int) threadIdx.x >> 2;
         chunk = (int) threadIdx.x & 3;
-        words_each = (a.hdim + 31) / 32;
-        const int64_t K = a.x1.width + a.x2.width;
-        plane = K * pitch;
+        begin_tile();
+    }
+    __device__ __forceinline__ void begin_tile()
+    {
+        const BackwardArgs& a = g.a;
+        const int32_t all = g.m_tiles * g.n_tiles;
+        int32_t tm, tn;
+        tile_of(t < all ? t : all - 1, g.m_tiles, g.n_tiles, &tm, &tn);
 #pragma unroll
         for (int i = 0; i < kRowsA; ++i) {                    // rows past the last are read as the last; they are not stored
-            const int64_t r = min(r0 + row + i * kStep, rows - 1);
-            z[i] = reinterpret_cast<const T*>(a.d_out.data) + r * a.d_out.stride;
-            if constexpr (kMask) m[i] = a.positive + r * words_each;
+            const int64_t r = min((int64_t) tm * Tiles::kM + row + i * kStep, rows - 1);
+            z[i] = static_cast<const char*>(a.d_out.data) + r * a.d_out.stride * (int64_t) sizeof(T);
+            if constexpr (kMask) m[i] = a.positive + r * ((a.hdim + 31) / 32);
         }
 #pragma unroll
-        for (int i = 0; i < kRowsB; ++i) w[i] = g.w + min((int64_t) k0 + row + i * kStep, K - 1) * pitch;
+        for (int i = 0; i < kRowsB; ++i) w[i] = g.w + min((int64_t) tn * Tiles::kN + row + i * kStep, K - 1) * g.pitch + chunk * 8;
     }
-    __device__ __forceinline__ void seek(int set, int32_t step)
+    __device__ __forceinline__ void seek(int set)
     {
-        n = step * kStageK + chunk * 8;
-        at[set] = n;
+        if (n0 >= columns) {
+            n0 = 0;
+            t += stride;
+            begin_tile();
+        }
+        inside = g.a.hdim - n0 - chunk * 8;
+        keep[set] = inside >= 8 ? 0xFFu : inside > 0 ? (1u << inside) - 1u : 0u;
+        n0 += kStageK;
     }
     __device__ __forceinline__ void fetch(int set, int i)
     {
+        const int32_t n = n0 - kStageK + chunk * 8, hdim = g.a.hdim;
         if (i < kRowsA) {
             if constexpr (kWhole) {
-                const T* from = z[i] + min(n, a.hdim - 8);
+                const uint4* from = reinterpret_cast<const uint4*>(z[i] + (int64_t) min(n, hdim - 8) * (int64_t) sizeof(T));
 #pragma unroll
                 for (int j = 0; j < kWords / 4; ++j) {
-                    const uint4 v = reinterpret_cast<const uint4*>(from)[j];
+                    const uint4 v = from[j];
                     d[set][i][4 * j] = v.x; d[set][i][4 * j + 1] = v.y; d[set][i][4 * j + 2] = v.z; d[set][i][4 * j + 3] = v.w;
                 }
             } else if constexpr (kFloat) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[set][i][j] = reinterpret_cast<const uint32_t*>(z[i])[min(n + j, a.hdim - 1)];
+                for (int j = 0; j < 8; ++j) d[set][i][j] = reinterpret_cast<const uint32_t*>(z[i])[min(n + j, hdim - 1)];
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    d[set][i][j] = z[i][min(n + 2 * j, a.hdim - 1)].bits | (uint32_t) z[i][min(n + 2 * j + 1, a.hdim - 1)].bits << 16;
+                for (int j = 0; j < 4; ++j) {
+                    const uint16_t* from = reinterpret_cast<const uint16_t*>(z[i]);
+                    d[set][i][j] = from[min(n + 2 * j, hdim - 1)] | (uint32_t) from[min(n + 2 * j + 1, hdim - 1)] << 16;
+                }
             }
         } else if (i < kRowsA + kRowsB * kPlanes) {
             const int b = (i - kRowsA) / kPlanes, p = (i - kRowsA) % kPlanes;
-            planes[set][b][p] = *reinterpret_cast<const uint4*>(w[b] + p * plane + min(n, pitch - 8));
+            planes[set][b][p] = *reinterpret_cast<const uint4*>(w[b] + p * K * g.pitch + min(n0, g.pitch) - kStageK);
         } else {
             const int b = i - kRowsA - kRowsB * kPlanes;
-            words[set][b] = m[b][min(n >> 5, words_each - 1)];
+            words[set][b] = m[b][(min(n0, g.pitch) - kStageK) >> 5];
         }
     }
     __device__ __forceinline__ void put(int set, int stage, int i)
     {
-        uint4* to = tile.lds + stage * Tiles::kStage;
-        if (i >= kRowsA * 4) {
-            const int b = (i - kRowsA * 4) / kPlanes, p = (i - kRowsA * 4) % kPlanes;
+        uint4* to = lds + stage * Tiles::kStage;
+        if (i >= kRowsA * kPutsA) {
+            const int b = (i - kRowsA * kPutsA) / kPlanes, p = (i - kRowsA * kPutsA) % kPlanes;
             to[Tiles::place_b(p, row + b * kStep, chunk)] = planes[set][b][p];
             return;
         }
-        const int b = i / 4, p = i % 4;                       // columns 2 p and 2 p + 1 of the eight
-        const int32_t c = at[set] + 2 * p;
-        uint32_t keep = (c < a.hdim ? 1u : 0u) | (c + 1 < a.hdim ? 2u : 0u);
-        if (kMask) keep &= words[set][b] >> (chunk * 8 + 2 * p);
-        if constexpr (kFloat) {
-            uint32_t pair[3];
-            split_pair(__uint_as_float(keep & 1u ? d[set][b][2 * p] : 0u), __uint_as_float(keep & 2u ? d[set][b][2 * p + 1] : 0u), pair);
+        const int b = i / kPutsA, u = i % kPutsA;
+        if (u == 0) {                                         // what the mask and the last column leave
+            uint32_t k8 = keep[set];
+            if constexpr (kMask) k8 &= words[set][b] >> (chunk * 8);
+            if constexpr (!kMask && kWhole) {
+                const uint32_t all = k8 ? ~0u : 0u;
 #pragma unroll
-            for (int k = 0; k < 3; ++k) t[k][p] = pair[k];
+                for (int j = 0; j < kWords; ++j) d[set][b][j] &= all;
+            } else if constexpr (kFloat) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[set][b][j] &= spread_bit(k8, j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[set][b][j] &= (spread_bit(k8, 2 * j) & 0xFFFFu) | (spread_bit(k8, 2 * j + 1) & 0xFFFF0000u);
+            }
+        } else if constexpr (kFloat) {
+            to[Tiles::place_a(u - 1, row + b * kStep, chunk)] = take_terms(d[set][b]);
         } else {
-            t[0][p] = d[set][b][p] & ((keep & 1u ? 0xFFFFu : 0u) | (keep & 2u ? 0xFFFF0000u : 0u));
+            to[Tiles::place_a(0, row + b * kStep, chunk)] = make_uint4(d[set][b][0], d[set][b][1], d[set][b][2], d[set][b][3]);
         }
-        if (p < 3) return;
-#pragma unroll
-        for (int k = 0; k < (kFloat ? 3 : 1); ++k) to[Tiles::place_a(k, row + b * kStep, chunk)] = make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]);
     }
 };
 
@@ -508,17 +599,25 @@ __global__ void __launch_bounds__(kThreads) k_backward_input(InputArgs g)
     __shared__ uint4 s_stage[3 * Tiles::kStage];
     const BackwardArgs& a = g.a;
     const int64_t rows = a.count.get();
-    int32_t tm, tn;
-    tile_of(xcd_run((int32_t) blockIdx.x, g.m_tiles * g.n_tiles), g.m_tiles, g.n_tiles, &tm, &tn);
-    const int64_t r0 = (int64_t) tm * Tiles::kM;
-    const int32_t k0 = tn * Tiles::kN, K = a.x1.width + a.x2.width;
-    if (r0 >= rows) return;
+    if (rows <= 0) return;
+    // a block's tiles: of those that have rows, every gridDim.x-th of its XCD's
+    const int32_t all = (int32_t) ((rows + Tiles::kM - 1) / Tiles::kM) * g.n_tiles, first = xcd_run((int32_t) blockIdx.x, (int32_t) gridDim.x);
+    const int32_t tiles = first < all ? (all - first + (int32_t) gridDim.x - 1) / (int32_t) gridDim.x : 0;
+    if (tiles == 0) return;
+    InputArgs here = g;
+    here.m_tiles = all / g.n_tiles;
     Tiles tile(s_stage);
-    Source source(g, tile, r0, rows, k0);
-    tile.run(source, g.pitch / kStageK);
+    Source source(here, s_stage, rows, first, (int32_t) gridDim.x);
+    const int32_t K = a.x1.width + a.x2.width;
     T* out = reinterpret_cast<T*>(a.dx.data);
-    tile.each([&](int m, int n, float v) {
-        if (r0 + m < rows && k0 + n < K) out[(r0 + m) * a.dx.stride + k0 + n] = from_float<T>(v);
+    tile.run(source, source.columns / kStageK, tiles, [&](int32_t i) {
+        int32_t tm, tn;
+        tile_of(first + i * (int32_t) gridDim.x, here.m_tiles, g.n_tiles, &tm, &tn);
+        const int64_t r0 = (int64_t) tm * Tiles::kM;
+        const int32_t k0 = tn * Tiles::kN;
+        tile.each([&](int m, int n, float v) {
+            if (r0 + m < rows && k0 + n < K) out[(r0 + m) * a.dx.stride + k0 + n] = from_float<T>(v);
+        });
     });
 }
 
@@ -591,13 +690,14 @@ static hipError_t launch_weights(const WeightsArgs& g, hipStream_t s)
 }
 
 template <typename T, int kThreads>
-static hipError_t launch_input(InputArgs g, hipStream_t s)
+static hipError_t launch_input(const gns_ctx* c, InputArgs g, hipStream_t s)
 {
     typedef typename InputTile<T, kThreads>::Type Tiles;
     g.m_tiles = (int32_t) (((int64_t) g.a.count.rows + Tiles::kM - 1) / Tiles::kM);
     g.n_tiles = (g.a.x1.width + g.a.x2.width + Tiles::kN - 1) / Tiles::kN;
-    if (too_many((int64_t) g.m_tiles * g.n_tiles, kThreads)) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned) (g.m_tiles * g.n_tiles)), block(kThreads);
+    const int64_t tiles = (int64_t) g.m_tiles * g.n_tiles, most = (int64_t) c->num_cus * (kThreads == 512 ? 1 : 2);
+    if (tiles >= (int64_t) 1 << 30) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned) (tiles < most ? tiles : most)), block(kThreads);
     const bool whole = g.a.hdim % 8 == 0 && reinterpret_cast<uintptr_t>(g.a.d_out.data) % 16 == 0 && (uint64_t) g.a.d_out.stride * sizeof(T) % 16 == 0;
     if (g.a.positive && whole)  hipLaunchKernelGGL((k_backward_input<T, kThreads, true, true>), grid, block, 0, s, g);
     else if (g.a.positive)      hipLaunchKernelGGL((k_backward_input<T, kThreads, true, false>), grid, block, 0, s, g);
@@ -613,32 +713,34 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     const int32_t K = a.x1.width + a.x2.width;
     const int64_t pitch = ((int64_t) a.hdim + kStageK - 1) / kStageK * kStageK;
     char* at = static_cast<char*>(a.workspace);
+    const bool dx = a.dx.data && a.count.rows;
+    BetweenArgs b = {};
+    b.k = K; b.hdim = a.hdim; b.pitch = (int32_t) pitch; b.planes = kFloat ? 3 : 2;
     if (a.dw) {
         const WeightsPlan p = plan_weights(c, a.x1.width, a.x2.width, a.hdim, a.count.rows, kFloat, kFloat || reads_pairs(a.d_out));
         WeightsArgs g = {a, p.m_tiles, p.n_tiles, p.splits, a.dw, a.db};
         if (p.splits > 1) {
-            g.dw = reinterpret_cast<float*>(at);
+            b.dw_parts = g.dw = reinterpret_cast<float*>(at);
             at += align256((size_t) p.splits * (size_t) K * (size_t) a.hdim * 4);
-            g.db = a.db ? reinterpret_cast<float*>(at) : nullptr;
+            if (a.db) b.db_parts = g.db = reinterpret_cast<float*>(at);
             at += align256((size_t) p.splits * (size_t) a.hdim * 4);
+            b.dw = a.dw; b.db = a.db; b.splits = p.splits;
         }
         const hipError_t e = p.wide ? launch_weights<T, 512>(g, s) : launch_weights<T, 256>(g, s);
         if (e != hipSuccess) return e;
-        if (p.splits > 1) {
-            const int64_t n = (int64_t) K * a.hdim;
-            hipLaunchKernelGGL(k_join_splits, dim3(grid_of(c, n)), dim3(kBlock), 0, s, g.dw, p.splits, n, a.dw);
-            if (a.db) hipLaunchKernelGGL(k_join_splits, dim3(grid_of(c, a.hdim)), dim3(kBlock), 0, s, g.db, p.splits, (int64_t) a.hdim, a.db);
-        }
     }
-    if (a.dx.data && a.count.rows) {
-        InputArgs g = {a, 0, 0, (int32_t) pitch, reinterpret_cast<const uint16_t*>(at)};
-        hipLaunchKernelGGL(k_split_weights, dim3(grid_of(c, K * pitch)), dim3(kBlock), 0, s, a.w, (int64_t) K, a.hdim, (int32_t) pitch, kFloat ? 3 : 2,
-                           reinterpret_cast<uint16_t*>(at));
-        typedef typename InputTile<T, 512>::Type Wide;
-        const int64_t tiles = ((int64_t) a.count.rows + Wide::kM - 1) / Wide::kM * ((K + Wide::kN - 1) / Wide::kN);
-        return tiles >= c->num_cus ? launch_input<T, 512>(g, s) : launch_input<T, 256>(g, s);
+    if (dx) {
+        b.w = a.w;
+        b.terms = reinterpret_cast<uint16_t*>(at);
     }
-    return hipGetLastError();
+    b.join_blocks = b.dw_parts ? (int32_t) grid_of(c, ((int64_t) K * a.hdim + a.hdim + 6) / 4 * kJoinThreads) : 0;
+    const int32_t term_blocks = dx ? (int32_t) grid_of(c, K * (pitch / 4)) : 0;
+    if (b.join_blocks + term_blocks) hipLaunchKernelGGL(k_backward_between, dim3((unsigned) (b.join_blocks + term_blocks)), dim3(kBlock), 0, s, b);
+    if (!dx) return hipGetLastError();
+    InputArgs g = {a, 0, 0, (int32_t) pitch, b.terms};
+    typedef typename InputTile<T, 512>::Type Wide;
+    const int64_t tiles = ((int64_t) a.count.rows + Wide::kM - 1) / Wide::kM * ((K + Wide::kN - 1) / Wide::kN);
+    return tiles >= c->num_cus ? launch_input<T, 512>(c, g, s) : launch_input<T, 256>(c, g, s);
 }
 
 hipError_t launch_backward(const gns_ctx* c, const BackwardArgs& a, int32_t type, hipStream_t s)
