@@ -10,20 +10,21 @@ namespace gns {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef uint32_t Chunk __attribute__((ext_vector_type(4)));        // eight values of bf16 (a struct of four words would not stay in registers)
 
 // Upper halves of two words, a's in the lower half.
 __device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 __device__ __forceinline__ uint32_t lower_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 
 // The leading bf16 terms of eight values, packed, which are taken off the values.
-__device__ __forceinline__ uint4 take_terms(uint32_t (&v)[8])
+__device__ __forceinline__ Chunk take_terms(uint32_t (&v)[8])
 {
     uint32_t t[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p) t[p] = upper_halves(v[2 * p], v[2 * p + 1]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) - __uint_as_float(v[i] & 0xFFFF0000u));
-    return make_uint4(t[0], t[1], t[2], t[3]);
+    return Chunk{t[0], t[1], t[2], t[3]};
 }
 
 // All bits set if bit i of w is, else none.
@@ -55,13 +56,13 @@ struct Tile {
     static constexpr int kStage = (BM * NA + BN * NB) * 4, kFragments = MI * NA + NI * NB;
     typedef Pairs<NA, NB> P;
 
-    uint4* lds;                               // [3 * kStage]
-    const uint4 *a_at, *b_at;
+    Chunk* lds;                               // [3 * kStage]
+    const Chunk *a_at, *b_at;
     int kh, bank;
-    uint4 f[2][kFragments];
+    Chunk f[2][kFragments];
     floatx16 acc[MI][NI];
 
-    __device__ __forceinline__ explicit Tile(uint4* s) : lds(s)
+    __device__ __forceinline__ explicit Tile(Chunk* s) : lds(s)
     {
         const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63, l32 = lane & 31;
         kh = lane >> 5;
@@ -207,7 +208,7 @@ struct WeightsSource {
     static constexpr int kSets = 2, kFetches = 1 + (kMask ? 1 : 0) + 4 + kReads, kPuts = 1 + 4 + 2 + (kFloat ? 3 : 2);
     static_assert(kQuads * 8 == kThreads && kLanes * 4 == kThreads, "each thread has its share of a stage");
 
-    uint4* const lds;
+    Chunk* const lds;
     const int64_t row_bytes;                  // of d_out
     int64_t rest;                             // rows there are from the next step's first on
     bool begun;
@@ -226,7 +227,7 @@ struct WeightsSource {
     uint32_t x[kSets][4], ex[kSets], d[kSets][kReads], words[kSets];
     float scale[4], sum[2];
 
-    __device__ __forceinline__ WeightsSource(const BackwardArgs& a, uint4* stages, int64_t first, int64_t end, int32_t c0, int32_t n0)
+    __device__ __forceinline__ WeightsSource(const BackwardArgs& a, Chunk* stages, int64_t first, int64_t end, int32_t c0, int32_t n0)
         : lds(stages), row_bytes(a.d_out.stride * (int64_t) sizeof(T)), rest(end - first), begun(false)
     {
         const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
@@ -322,7 +323,7 @@ struct WeightsSource {
             uint32_t t[4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) t[p] = k == 0 ? lower_halves(d[set][2 * p], d[set][2 * p + 1]) : upper_halves(d[set][2 * p], d[set][2 * p + 1]);
-            lds[stage * Tiles::kStage + Tiles::place_b(0, pair_row(column + k), chunk)] = make_uint4(t[0], t[1], t[2], t[3]);
+            lds[stage * Tiles::kStage + Tiles::place_b(0, pair_row(column + k), chunk)] = Chunk{t[0], t[1], t[2], t[3]};
         }
     }
     // What the mask leaves of row kRow of the eight, and the sums.  (A row past the last has no exponents, so its products are zero.)
@@ -353,7 +354,7 @@ __global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
 {
     typedef WeightsSource<T, kThreads, kMask, kPairs> Source;
     typedef typename Source::Tiles Tiles;
-    __shared__ uint4 s_stage[3 * Tiles::kStage];
+    __shared__ Chunk s_stage[3 * Tiles::kStage];
     const BackwardArgs& a = g.a;
     const int64_t rows = a.count.get();
     const int32_t all = g.m_tiles * g.n_tiles, t = xcd_run((int32_t) blockIdx.x, all * g.splits), split = t / all;
@@ -485,9 +486,9 @@ struct InputSource {
     static constexpr int kPutsA = kFloat ? 4 : 2, kPuts = kRowsA * kPutsA + kRowsB * kPlanes;
 
     const InputArgs& g;
-    uint4* const lds;
+    Chunk* const lds;
     const int64_t rows, K;
-    const int32_t stride, columns;            // columns: hdim rounded up to whole turns of kSets steps
+    const int32_t m_tiles, stride, columns;            // columns: hdim rounded up to whole turns of kSets steps
     int32_t t, n0;                            // tile and first column of the next step
     int row, chunk;
     const char* z[kRowsA];                    // of the step that is read: this thread's columns
@@ -495,10 +496,10 @@ struct InputSource {
     const uint16_t* w[kRowsB];
     int32_t inside;                           // of the eight columns
     uint32_t d[kSets][kRowsA][kWords], words[kSets][kRowsA], keep[kSets];
-    uint4 planes[kSets][kRowsB][kPlanes];
+    Chunk planes[kSets][kRowsB][kPlanes];
 
-    __device__ __forceinline__ InputSource(const InputArgs& args, uint4* stages, int64_t rows_, int32_t first, int32_t stride_)
-        : g(args), lds(stages), rows(rows_), K(args.a.x1.width + args.a.x2.width), stride(stride_),
+    __device__ __forceinline__ InputSource(const InputArgs& args, Chunk* stages, int64_t rows_, int32_t tiles_, int32_t first, int32_t stride_)
+        : g(args), lds(stages), rows(rows_), K(args.a.x1.width + args.a.x2.width), m_tiles(tiles_), stride(stride_),
           columns((args.a.hdim + kStageK * kSets - 1) / (kStageK * kSets) * (kStageK * kSets)), t(first), n0(0)
     {
         row = (int) threadIdx.x >> 2;
@@ -508,9 +509,9 @@ struct InputSource {
     __device__ __forceinline__ void begin_tile()
     {
         const BackwardArgs& a = g.a;
-        const int32_t all = g.m_tiles * g.n_tiles;
+        const int32_t all = m_tiles * g.n_tiles;
         int32_t tm, tn;
-        tile_of(t < all ? t : all - 1, g.m_tiles, g.n_tiles, &tm, &tn);
+        tile_of(t < all ? t : all - 1, m_tiles, g.n_tiles, &tm, &tn);
 #pragma unroll
         for (int i = 0; i < kRowsA; ++i) {                    // rows past the last are read as the last; they are not stored
             const int64_t r = min((int64_t) tm * Tiles::kM + row + i * kStep, rows - 1);
@@ -536,10 +537,10 @@ struct InputSource {
         const int32_t n = n0 - kStageK + chunk * 8, hdim = g.a.hdim;
         if (i < kRowsA) {
             if constexpr (kWhole) {
-                const uint4* from = reinterpret_cast<const uint4*>(z[i] + (int64_t) min(n, hdim - 8) * (int64_t) sizeof(T));
+                const Chunk* from = reinterpret_cast<const Chunk*>(z[i] + (int64_t) min(n, hdim - 8) * (int64_t) sizeof(T));
 #pragma unroll
                 for (int j = 0; j < kWords / 4; ++j) {
-                    const uint4 v = from[j];
+                    const Chunk v = from[j];
                     d[set][i][4 * j] = v.x; d[set][i][4 * j + 1] = v.y; d[set][i][4 * j + 2] = v.z; d[set][i][4 * j + 3] = v.w;
                 }
             } else if constexpr (kFloat) {
@@ -554,7 +555,7 @@ struct InputSource {
             }
         } else if (i < kRowsA + kRowsB * kPlanes) {
             const int b = (i - kRowsA) / kPlanes, p = (i - kRowsA) % kPlanes;
-            planes[set][b][p] = *reinterpret_cast<const uint4*>(w[b] + p * K * g.pitch + min(n0, g.pitch) - kStageK);
+            planes[set][b][p] = *reinterpret_cast<const Chunk*>(w[b] + p * K * g.pitch + min(n0, g.pitch) - kStageK);
         } else {
             const int b = i - kRowsA - kRowsB * kPlanes;
             words[set][b] = m[b][(min(n0, g.pitch) - kStageK) >> 5];
@@ -562,7 +563,7 @@ struct InputSource {
     }
     __device__ __forceinline__ void put(int set, int stage, int i)
     {
-        uint4* to = lds + stage * Tiles::kStage;
+        Chunk* to = lds + stage * Tiles::kStage;
         if (i >= kRowsA * kPutsA) {
             const int b = (i - kRowsA * kPutsA) / kPlanes, p = (i - kRowsA * kPutsA) % kPlanes;
             to[Tiles::place_b(p, row + b * kStep, chunk)] = planes[set][b][p];
@@ -586,7 +587,7 @@ struct InputSource {
         } else if constexpr (kFloat) {
             to[Tiles::place_a(u - 1, row + b * kStep, chunk)] = take_terms(d[set][b]);
         } else {
-            to[Tiles::place_a(0, row + b * kStep, chunk)] = make_uint4(d[set][b][0], d[set][b][1], d[set][b][2], d[set][b][3]);
+            to[Tiles::place_a(0, row + b * kStep, chunk)] = Chunk{d[set][b][0], d[set][b][1], d[set][b][2], d[set][b][3]};
         }
     }
 };
@@ -596,23 +597,21 @@ __global__ void __launch_bounds__(kThreads) k_backward_input(InputArgs g)
 {
     typedef InputSource<T, kThreads, kMask, kWhole> Source;
     typedef typename Source::Tiles Tiles;
-    __shared__ uint4 s_stage[3 * Tiles::kStage];
+    __shared__ Chunk s_stage[3 * Tiles::kStage];
     const BackwardArgs& a = g.a;
     const int64_t rows = a.count.get();
     if (rows <= 0) return;
     // a block's tiles: of those that have rows, every gridDim.x-th of its XCD's
-    const int32_t all = (int32_t) ((rows + Tiles::kM - 1) / Tiles::kM) * g.n_tiles, first = xcd_run((int32_t) blockIdx.x, (int32_t) gridDim.x);
+    const int32_t m_tiles = (int32_t) ((rows + Tiles::kM - 1) / Tiles::kM), all = m_tiles * g.n_tiles, first = xcd_run((int32_t) blockIdx.x, (int32_t) gridDim.x);
     const int32_t tiles = first < all ? (all - first + (int32_t) gridDim.x - 1) / (int32_t) gridDim.x : 0;
     if (tiles == 0) return;
-    InputArgs here = g;
-    here.m_tiles = all / g.n_tiles;
     Tiles tile(s_stage);
-    Source source(here, s_stage, rows, first, (int32_t) gridDim.x);
+    Source source(g, s_stage, rows, m_tiles, first, (int32_t) gridDim.x);
     const int32_t K = a.x1.width + a.x2.width;
     T* out = reinterpret_cast<T*>(a.dx.data);
     tile.run(source, source.columns / kStageK, tiles, [&](int32_t i) {
         int32_t tm, tn;
-        tile_of(first + i * (int32_t) gridDim.x, here.m_tiles, g.n_tiles, &tm, &tn);
+        tile_of(first + i * (int32_t) gridDim.x, m_tiles, g.n_tiles, &tm, &tn);
         const int64_t r0 = (int64_t) tm * Tiles::kM;
         const int32_t k0 = tn * Tiles::kN;
         tile.each([&](int m, int n, float v) {
