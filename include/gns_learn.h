@@ -27,7 +27,7 @@ extern "C" {
 #endif
 
 enum { GNS_FP32 = 0, GNS_BF16 = 1 };
-#define GNS_MAX_WIDTH (1 << 24)
+#define GNS_MAX_WIDTH (1 << 22)
 
 /* Rows of a matrix on the device: element (r, c) is data[r * stride + c], 0 <= c < width <= GNS_MAX_WIDTH.  stride >= width, in elements;
  * data aligned to the element.  Any width, stride and alignment is taken; rows that begin at multiples of 16 bytes are

@@ -147,20 +147,17 @@ struct Tile {
             finish(tile);
         }
     }
-    // visit(row of LDS of the left factor, of the right one, value) for the lane's outputs; adjacent lanes have adjacent rows
-    // of the right factor
-    template <typename Visit>
-    __device__ __forceinline__ void each(Visit&& visit)
+    // Output acc[i][j][v] of a lane is that of row first_row + row_step(i, v) of the left factor in LDS and of row first_column
+    // + 32 j of the right one.
+    static __device__ __forceinline__ int first_row(int lane)
     {
-        const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = opaque_lane_id();
-        const int m0 = wave / (BN / WN) * WM + 4 * (lane >> 5), n0 = wave % (BN / WN) * WN + (lane & 31);
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-#pragma unroll
-                for (int j = 0; j < NI; ++j) visit(m0 + i * 32 + 8 * (v >> 2) + (v & 3), n0 + j * 32, acc[i][j][v]);
+        return __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)) / (BN / WN) * WM + 4 * (lane >> 5);
     }
+    static __device__ __forceinline__ int first_column(int lane)
+    {
+        return __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)) % (BN / WN) * WN + (lane & 31);
+    }
+    static constexpr int row_step(int i, int v) { return i * 32 + 8 * (v >> 2) + (v & 3); }
 };
 
 // ---- dw and db ----------------------------------------------------------------------------------------------------
@@ -368,10 +365,20 @@ __global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
     Source source(a, s_stage, first, end, c0, n0);
     float* dw = g.dw + (int64_t) split * (a.x1.width + a.x2.width) * a.hdim;
     tile.run(source, (int32_t) ((end - first + kRound - 1) / kRound) * Source::kSets, 1, [&](int32_t) {
-        tile.each([&](int m, int n, float v) {
-            const int32_t k = weight_row(a, c0 + quad_column(m)), c = n0 + (sizeof(T) == 4 ? n : pair_column(n));
-            if (k >= 0 && c < a.hdim) dw[(int64_t) k * a.hdim + c] = v;
-        });
+        const int lane = opaque_lane_id(), m0 = Tiles::first_row(lane), n = Tiles::first_column(lane);
+#pragma unroll
+        for (int i = 0; i < Tiles::MI; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int32_t k = weight_row(a, c0 + quad_column(m0 + Tiles::row_step(i, v)));
+                if (k < 0) continue;
+                float* row = dw + (int64_t) k * a.hdim + n0;
+#pragma unroll
+                for (int j = 0; j < Tiles::NI; ++j) {
+                    const int32_t c = sizeof(T) == 4 ? n + 32 * j : pair_column(n + 32 * j);
+                    if (n0 + c < a.hdim) row[c] = tile.acc[i][j][v];
+                }
+            }
     });
     if (!g.db || tm != 0) return;
     float* s_sum = reinterpret_cast<float*>(s_stage);         // [4][Tiles::kN]: of the four threads that read a column
@@ -474,8 +481,8 @@ template <> struct InputTile<Bf16, 512> { typedef Tile<256, 128, 64, 64, 1, 2> T
 template <> struct InputTile<Bf16, 256> { typedef Tile<128, 128, 64, 64, 1, 2> Type; };
 
 // A thread reads eight columns of a row of dz (of two rows of bf16), and as many of W's planes.  kWhole: rows of dz begin at
-// 16-byte marks and hdim is a multiple of eight, so eight columns are one or two reads; else they are read singly.  A block goes
-// through tiles, `stride` apart.
+// 16-byte marks and hdim is a multiple of eight, so eight columns are one or two reads; else they are read singly.  Columns
+// past the last are read as the last ones: W's planes are zero there.  A block goes through tiles, `stride` apart.
 template <typename T, int kThreads, bool kMask, bool kWhole>
 struct InputSource {
     typedef typename InputTile<T, kThreads>::Type Tiles;
@@ -483,18 +490,20 @@ struct InputSource {
     static constexpr int kPlanes = kFloat ? 3 : 2, kStep = kThreads / 4;                            // rows the threads cover at once
     static constexpr int kRowsA = Tiles::kM / kStep, kRowsB = Tiles::kN / kStep, kWords = kFloat ? 8 : 4;
     static constexpr int kSets = kFloat ? 2 : 4, kFetches = kRowsA * (1 + (kMask ? 1 : 0)) + kRowsB * kPlanes;
-    static constexpr int kPutsA = kFloat ? 4 : 2, kPuts = kRowsA * kPutsA + kRowsB * kPlanes;
+    static constexpr int kPutsA = (kMask ? 1 : 0) + (kFloat ? 3 : 1), kPuts = kRowsA * kPutsA + kRowsB * kPlanes;
 
     const InputArgs& g;
     Chunk* const lds;
     const int64_t rows, K;
-    const int32_t m_tiles, stride, columns;            // columns: hdim rounded up to whole turns of kSets steps
+    const int32_t m_tiles, stride, columns;   // columns: hdim rounded up to whole turns of kSets steps
     int32_t t, n0;                            // tile and first column of the next step
     int row, chunk;
-    const char* z[kRowsA];                    // of the step that is read: this thread's columns
-    const uint32_t* m[kRowsA];
-    const uint16_t* w[kRowsB];
-    int32_t inside;                           // of the eight columns
+    const char* z[kRowsA];                    // this thread's rows of dz
+    const uint32_t* m[kRowsA];                // and of the mask
+    const char* w;                            // the tile's first row of W's planes
+    uint32_t w_at[kRowsB];                    // from there to this thread's rows and columns
+    int32_t n, word;                          // of the step that is read: this thread's first column, its word of the mask
+    int64_t w_step;                           // and bytes from a plane's row to its columns
     uint32_t d[kSets][kRowsA][kWords], words[kSets][kRowsA], keep[kSets];
     Chunk planes[kSets][kRowsB][kPlanes];
 
@@ -518,8 +527,10 @@ struct InputSource {
             z[i] = static_cast<const char*>(a.d_out.data) + r * a.d_out.stride * (int64_t) sizeof(T);
             if constexpr (kMask) m[i] = a.positive + r * ((a.hdim + 31) / 32);
         }
+        const int64_t k0 = (int64_t) tn * Tiles::kN;
+        w = reinterpret_cast<const char*>(g.w + k0 * g.pitch);
 #pragma unroll
-        for (int i = 0; i < kRowsB; ++i) w[i] = g.w + min((int64_t) tn * Tiles::kN + row + i * kStep, K - 1) * g.pitch + chunk * 8;
+        for (int i = 0; i < kRowsB; ++i) w_at[i] = (uint32_t) min((int64_t) row + i * kStep, K - 1 - k0) * (uint32_t) g.pitch * 2u + (uint32_t) chunk * 16u;
     }
     __device__ __forceinline__ void seek(int set)
     {
@@ -528,20 +539,30 @@ struct InputSource {
             t += stride;
             begin_tile();
         }
-        inside = g.a.hdim - n0 - chunk * 8;
-        keep[set] = inside >= 8 ? 0xFFu : inside > 0 ? (1u << inside) - 1u : 0u;
+        const int32_t hdim = g.a.hdim, at = n0 < g.pitch ? n0 : g.pitch - kStageK;       // steps that only fill a turn read the last again
+        n = n0 + chunk * 8;
+        if constexpr (kWhole) n = min(n, hdim - 8);
+        if constexpr (kMask) {
+            const int32_t inside = hdim - n0 - chunk * 8;     // of the eight columns
+            keep[set] = inside >= 8 ? 0xFFu : inside > 0 ? (1u << inside) - 1u : 0u;
+        } else {
+            keep[set] = n0 < g.pitch ? 1u : 0u;               // wave-uniform
+        }
+        word = at >> 5;
+        w_step = (int64_t) at * 2;
         n0 += kStageK;
     }
     __device__ __forceinline__ void fetch(int set, int i)
     {
-        const int32_t n = n0 - kStageK + chunk * 8, hdim = g.a.hdim;
+        const int32_t hdim = g.a.hdim;
         if (i < kRowsA) {
             if constexpr (kWhole) {
-                const Chunk* from = reinterpret_cast<const Chunk*>(z[i] + (int64_t) min(n, hdim - 8) * (int64_t) sizeof(T));
+                const Chunk* from = reinterpret_cast<const Chunk*>(z[i] + (uint64_t) ((uint32_t) n * (uint32_t) sizeof(T)));
 #pragma unroll
                 for (int j = 0; j < kWords / 4; ++j) {
                     const Chunk v = from[j];
-                    d[set][i][4 * j] = v.x; d[set][i][4 * j + 1] = v.y; d[set][i][4 * j + 2] = v.z; d[set][i][4 * j + 3] = v.w;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) d[set][i][4 * j + k] = v[k];
                 }
             } else if constexpr (kFloat) {
 #pragma unroll
@@ -555,10 +576,10 @@ struct InputSource {
             }
         } else if (i < kRowsA + kRowsB * kPlanes) {
             const int b = (i - kRowsA) / kPlanes, p = (i - kRowsA) % kPlanes;
-            planes[set][b][p] = *reinterpret_cast<const Chunk*>(w[b] + p * K * g.pitch + min(n0, g.pitch) - kStageK);
+            planes[set][b][p] = *reinterpret_cast<const Chunk*>(w + (w_step + p * K * g.pitch * 2) + w_at[b]);
         } else {
             const int b = i - kRowsA - kRowsB * kPlanes;
-            words[set][b] = m[b][(min(n0, g.pitch) - kStageK) >> 5];
+            words[set][b] = m[b][word];
         }
     }
     __device__ __forceinline__ void put(int set, int stage, int i)
@@ -566,18 +587,15 @@ struct InputSource {
         Chunk* to = lds + stage * Tiles::kStage;
         if (i >= kRowsA * kPutsA) {
             const int b = (i - kRowsA * kPutsA) / kPlanes, p = (i - kRowsA * kPutsA) % kPlanes;
-            to[Tiles::place_b(p, row + b * kStep, chunk)] = planes[set][b][p];
+            Chunk v = planes[set][b][p];
+            if (!kMask && kSets > 1) v = keep[set] ? v : Chunk{0, 0, 0, 0};
+            to[Tiles::place_b(p, row + b * kStep, chunk)] = v;
             return;
         }
-        const int b = i / kPutsA, u = i % kPutsA;
-        if (u == 0) {                                         // what the mask and the last column leave
-            uint32_t k8 = keep[set];
-            if constexpr (kMask) k8 &= words[set][b] >> (chunk * 8);
-            if constexpr (!kMask && kWhole) {
-                const uint32_t all = k8 ? ~0u : 0u;
-#pragma unroll
-                for (int j = 0; j < kWords; ++j) d[set][b][j] &= all;
-            } else if constexpr (kFloat) {
+        const int b = i / kPutsA, u = i % kPutsA - (kMask ? 1 : 0);
+        if (u < 0) {                                          // what the mask leaves
+            const uint32_t k8 = keep[set] & words[set][b] >> (chunk * 8);
+            if constexpr (kFloat) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[set][b][j] &= spread_bit(k8, j);
             } else {
@@ -585,7 +603,7 @@ struct InputSource {
                 for (int j = 0; j < 4; ++j) d[set][b][j] &= (spread_bit(k8, 2 * j) & 0xFFFFu) | (spread_bit(k8, 2 * j + 1) & 0xFFFF0000u);
             }
         } else if constexpr (kFloat) {
-            to[Tiles::place_a(u - 1, row + b * kStep, chunk)] = take_terms(d[set][b]);
+            to[Tiles::place_a(u, row + b * kStep, chunk)] = take_terms(d[set][b]);
         } else {
             to[Tiles::place_a(0, row + b * kStep, chunk)] = Chunk{d[set][b][0], d[set][b][1], d[set][b][2], d[set][b][3]};
         }
@@ -614,9 +632,18 @@ __global__ void __launch_bounds__(kThreads) k_backward_input(InputArgs g)
         tile_of(first + i * (int32_t) gridDim.x, m_tiles, g.n_tiles, &tm, &tn);
         const int64_t r0 = (int64_t) tm * Tiles::kM;
         const int32_t k0 = tn * Tiles::kN;
-        tile.each([&](int m, int n, float v) {
-            if (r0 + m < rows && k0 + n < K) out[(r0 + m) * a.dx.stride + k0 + n] = from_float<T>(v);
-        });
+        const int lane = opaque_lane_id(), m0 = Tiles::first_row(lane), n = Tiles::first_column(lane);
+        const bool whole = r0 + Tiles::kM <= rows && k0 + Tiles::kN <= K;
+        T* first = out + (r0 + m0) * a.dx.stride + k0 + n;
+#pragma unroll
+        for (int i = 0; i < Tiles::MI; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                T* row = first + Tiles::row_step(i, v) * a.dx.stride;
+#pragma unroll
+                for (int j = 0; j < Tiles::NI; ++j)
+                    if (whole || (r0 + m0 + Tiles::row_step(i, v) < rows && k0 + n + 32 * j < K)) row[32 * j] = from_float<T>(tile.acc[i][j][v]);
+            }
     });
 }
 
@@ -739,7 +766,7 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     InputArgs g = {a, 0, 0, (int32_t) pitch, b.terms};
     typedef typename InputTile<T, 512>::Type Wide;
     const int64_t tiles = ((int64_t) a.count.rows + Wide::kM - 1) / Wide::kM * ((K + Wide::kN - 1) / Wide::kN);
-    return tiles >= c->num_cus ? launch_input<T, 512>(c, g, s) : launch_input<T, 256>(c, g, s);
+    return tiles >= c->num_cus && K > Wide::kN / 2 ? launch_input<T, 512>(c, g, s) : launch_input<T, 256>(c, g, s);
 }
 
 hipError_t launch_backward(const gns_ctx* c, const BackwardArgs& a, int32_t type, hipStream_t s)
