@@ -28,9 +28,10 @@ extern "C" {
 
 enum { GNS_FP32 = 0, GNS_BF16 = 1 };
 #define GNS_MAX_WIDTH (1 << 22)
+#define GNS_MAX_STRIDE (1 << 24)
 
-/* Rows of a matrix on the device: element (r, c) is data[r * stride + c], 0 <= c < width <= GNS_MAX_WIDTH.  stride >= width, in elements;
- * data aligned to the element.  Any width, stride and alignment is taken; rows that begin at multiples of 16 bytes are
+/* Rows of a matrix on the device: element (r, c) is data[r * stride + c], 0 <= c < width <= GNS_MAX_WIDTH.  width <= stride <=
+ * GNS_MAX_STRIDE, in elements; data aligned to the element.  Any width, stride and alignment is taken; rows that begin at multiples of 16 bytes are
  * read and written faster. */
 typedef struct {
     void* data;

@@ -169,7 +169,7 @@ struct WeightsArgs {
     BackwardArgs a;
     int32_t m_tiles, n_tiles, splits;
     float* dw;                                // [splits x (f1 + f2) x hdim]: the caller's if there is one split
-    float* db;                                // [splits x hdim], or null
+    float* db;                                // [splits x m_tiles x hdim]: the caller's if that is one; or null
 };
 
 // Packed columns of X are those of x1's groups, then those of x2's.  Row of dw, or -1 where a group is padded.
@@ -202,30 +202,33 @@ struct WeightsSource {
     static constexpr int kQuads = Tiles::kM / 4, kQuadsWave = kQuads < kWave ? kQuads : kWave;       // of columns, of X
     static constexpr int kLanes = kFloat ? Tiles::kN : Tiles::kN / 2;                               // that read a row of dz
     static constexpr int kReads = kFloat || kPairs ? 8 : 16;
-    static constexpr int kSets = 2, kFetches = 1 + (kMask ? 1 : 0) + 4 + kReads, kPuts = 1 + 4 + 2 + (kFloat ? 3 : 2);
+    static constexpr int kSets = 2, kFetches = 1 + (kMask ? 1 : 0) + 4 + kReads, kPuts = 1 + 4 + 2 + 1 + (kFloat ? 3 : 2);
     static_assert(kQuads * 8 == kThreads && kLanes * 4 == kThreads, "each thread has its share of a stage");
 
     Chunk* const lds;
-    const int64_t row_bytes;                  // of d_out
+    const uint32_t row_bytes;                 // of d_out
+    const int32_t m_tiles, tm;                // this block adds up db over every m_tiles-th step
     int64_t rest;                             // rows there are from the next step's first on
+    int32_t until_sum;
     bool begun;
     int quad, rows4;                          // this thread's columns of X, and its four rows of a stage
     int column, chunk;                        // its first column of dz, and its eight rows
-    // of the step that is read, its first row:
-    const int8_t* q;                          // this thread's columns of X
+    // of the step that is read:
+    const char* z[8];                         // the wave's eight rows of dz
+    uint32_t z_at, second;                    // bytes from there to this lane's column, and to the next one
+    const int8_t* q[4];                       // this thread's columns of X
     const uint8_t* e;                         // the exponent this lane reads
     const uint32_t* m;                        // the word of the mask this lane reads
-    const char* d_out;
     uint32_t q_stride, e_stride, m_stride;
-    uint32_t z, second;                       // bytes from a row's first to this lane's column of dz, and to the next one
     int e_row, m_row;
-    int last;                                 // row that there is
     int32_t left[kSets];                      // rows there are from the step's first on
+    bool sums[kSets];
     uint32_t x[kSets][4], ex[kSets], d[kSets][kReads], words[kSets];
     float scale[4], sum[2];
 
-    __device__ __forceinline__ WeightsSource(const BackwardArgs& a, Chunk* stages, int64_t first, int64_t end, int32_t c0, int32_t n0)
-        : lds(stages), row_bytes(a.d_out.stride * (int64_t) sizeof(T)), rest(end - first), begun(false)
+    __device__ __forceinline__ WeightsSource(const BackwardArgs& a, Chunk* stages, int64_t first, int64_t end, int32_t c0, int32_t n0, int32_t m_tiles_, int32_t tm_, bool bias)
+        : lds(stages), row_bytes((uint32_t) a.d_out.stride * (uint32_t) sizeof(T)), m_tiles(bias ? m_tiles_ : INT32_MAX), tm(tm_), rest(end - first),
+          until_sum(bias ? tm_ : INT32_MAX), begun(false)
     {
         const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
         const int row16 = lane >> 4, i8 = lane & 7;
@@ -237,58 +240,74 @@ struct WeightsSource {
         int32_t in;
         const PackedRows& part = part_of(min(c0 + quad * 4, all - 4), &in);
         q_stride = (uint32_t) part.groups * 32;
-        q = part.q + first * q_stride + in;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = part.q + (first + rows4 + j) * (int64_t) q_stride + in;
         // Eight lanes share a group's exponents; a row of sixteen lanes has two groups, of which its first eight lanes read the
         // exponents: of the first group's four rows, of the second's.
         const int group = quad_group(row16) + (i8 >> 2);
         e_row = (kQuadsWave == kWave ? wave * 4 : wave * 8 + (row16 >> 1) * 4) + (i8 & 3);
         const PackedRows& part_e = part_of(min(c0 + group * 32, all - 32), &in);
         e_stride = (uint32_t) part_e.groups;
-        e = part_e.exponents + first * e_stride + in / 32;
+        e = part_e.exponents + (first + e_row) * (int64_t) e_stride + in / 32;
         const int lanes0 = wave * kWave % kLanes;              // the wave's first column of dz (of bf16: first pair)
         chunk = wave * kWave / kLanes;
         column = kFloat ? lanes0 + lane : 2 * (lanes0 + lane);
         const int32_t n = min(n0 + column, !kFloat && kPairs ? hdim - 2 : hdim - 1);
-        d_out = static_cast<const char*>(a.d_out.data) + first * row_bytes;
-        z = (uint32_t) n * (uint32_t) sizeof(T);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = static_cast<const char*>(a.d_out.data) + (first + chunk * 8 + j) * (int64_t) row_bytes;
+        z_at = (uint32_t) n * (uint32_t) sizeof(T);
         second = n + 1 < hdim ? (uint32_t) sizeof(T) : 0u;
         // a row of sixteen lanes has columns of one word; its first eight lanes read that of eight rows
         m_stride = (uint32_t) (hdim + 31) / 32;
         m_row = chunk * 8 + i8;
         if constexpr (kMask) {
             const int32_t word = kFloat ? (n0 + lanes0) / 32 + (row16 >> 1) : (n0 + 2 * lanes0) / 32 + row16;
-            m = a.positive + first * m_stride + min(word, (int32_t) m_stride - 1);
+            m = a.positive + (first + m_row) * (int64_t) m_stride + min(word, (int32_t) m_stride - 1);
         }
         sum[0] = sum[1] = 0.f;
     }
     static __device__ __forceinline__ int quad_group(int row16) { return kQuadsWave == kWave ? 2 * row16 : 2 * (row16 & 1); }
     __device__ __forceinline__ void seek(int set)
     {
-        // steps past the last read the last one's first row, which counts as nothing
-        const uint32_t on = begun && rest > 0 ? kStageK : 0;
+        // steps past the last read the last one again, which counts as nothing
+        if (begun && rest > 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] += (uint64_t) q_stride * kStageK;
+            e += e_stride * kStageK;
+            if constexpr (kMask) m += m_stride * kStageK;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] += (uint64_t) row_bytes * kStageK;
+        }
         begun = true;
-        q += (uint64_t) on * q_stride;
-        e += (uint64_t) on * e_stride;
-        if constexpr (kMask) m += (uint64_t) on * m_stride;
-        d_out += on * row_bytes;
+        // rows past the last of the last step are read as that one
+        if (rest > 0 && rest < kStageK) {
+            const int last = (int) rest - 1;
+            auto back = [&](int row) { return max(row - last, 0); };
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] -= (uint64_t) (uint32_t) back(rows4 + j) * q_stride;
+            e -= (uint64_t) (uint32_t) back(e_row) * e_stride;
+            if constexpr (kMask) m -= (uint64_t) (uint32_t) back(m_row) * m_stride;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] -= (uint64_t) (uint32_t) back(chunk * 8 + j) * row_bytes;
+        }
         left[set] = (int32_t) (rest < kStageK ? rest : kStageK);
-        last = max(left[set], 1) - 1;
         rest -= kStageK;
+        sums[set] = until_sum == 0;
+        until_sum = until_sum == 0 ? m_tiles - 1 : until_sum - 1;
     }
     __device__ __forceinline__ void fetch(int set, int i)
     {
         if (i == 0) {
-            ex[set] = e[(uint64_t) (uint32_t) min(e_row, last) * e_stride];
+            ex[set] = *e;
         } else if (kMask && i == 1) {
-            words[set] = m[(uint64_t) (uint32_t) min(m_row, last) * m_stride];
+            words[set] = *m;
         } else if (i < (kMask ? 6 : 5)) {
             const int j = i - (kMask ? 2 : 1);
-            x[set][j] = *reinterpret_cast<const uint32_t*>(q + (uint64_t) (uint32_t) min(rows4 + j, last) * q_stride);
+            x[set][j] = *reinterpret_cast<const uint32_t*>(q[j]);
         } else {
             const int j = i - (kMask ? 6 : 5);
-            const char* row = d_out + min(chunk * 8 + j % 8, last) * row_bytes;                   // wave-uniform
-            if constexpr (kFloat || kPairs) d[set][j] = *reinterpret_cast<const uint32_t*>(row + z);
-            else                            d[set][j] = *reinterpret_cast<const uint16_t*>(row + (j < 8 ? z : z + second));
+            if constexpr (kFloat || kPairs) d[set][j] = *reinterpret_cast<const uint32_t*>(z[j] + z_at);
+            else                            d[set][j] = *reinterpret_cast<const uint16_t*>(z[j % 8] + (j < 8 ? z_at : z_at + second));
         }
     }
     __device__ __forceinline__ void put(int set, int stage, int i)
@@ -312,18 +331,20 @@ struct WeightsSource {
         } else if (i == 6) {
             const uint32_t own = kMask && m_row < left[set] ? words[set] : 0u;
             keep_positive<4>(set, own); keep_positive<5>(set, own); keep_positive<6>(set, own); keep_positive<7>(set, own);
+        } else if (i == 7) {
+            if (sums[set]) add_up(set);
         } else if constexpr (kFloat) {
             uint32_t (&v)[8] = d[set];
-            lds[stage * Tiles::kStage + Tiles::place_b(i - 7, column, chunk)] = take_terms(v);
+            lds[stage * Tiles::kStage + Tiles::place_b(i - 8, column, chunk)] = take_terms(v);
         } else {
-            const int k = i - 7;
+            const int k = i - 8;
             uint32_t t[4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) t[p] = k == 0 ? lower_halves(d[set][2 * p], d[set][2 * p + 1]) : upper_halves(d[set][2 * p], d[set][2 * p + 1]);
             lds[stage * Tiles::kStage + Tiles::place_b(0, pair_row(column + k), chunk)] = Chunk{t[0], t[1], t[2], t[3]};
         }
     }
-    // What the mask leaves of row kRow of the eight, and the sums.  (A row past the last has no exponents, so its products are zero.)
+    // What the mask leaves of row kRow of the eight.  (A row past the last has no exponents, so its products are zero.)
     template <int kRow>
     __device__ __forceinline__ void keep_positive(int set, uint32_t own)
     {
@@ -336,12 +357,18 @@ struct WeightsSource {
             else                  v &= (spread_bit(w, 2 * (lane & 15)) & 0xFFFFu) | (spread_bit(w, 2 * (lane & 15) + 1) & 0xFFFF0000u);
         }
         d[set][kRow] = v;
-        const uint32_t in = kMask || chunk * 8 + kRow < left[set] ? v : 0u;
-        if constexpr (kFloat) {
-            sum[0] += __uint_as_float(in);
-        } else {
-            sum[0] += __uint_as_float(in << 16);
-            sum[1] += __uint_as_float(in & 0xFFFF0000u);
+    }
+    __device__ __forceinline__ void add_up(int set)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t v = chunk * 8 + i < left[set] ? d[set][i] : 0u;
+            if constexpr (kFloat) {
+                sum[0] += __uint_as_float(v);
+            } else {
+                sum[0] += __uint_as_float(v << 16);
+                sum[1] += __uint_as_float(v & 0xFFFF0000u);
+            }
         }
     }
 };
@@ -362,7 +389,7 @@ __global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
     const int64_t each = ((rows + g.splits - 1) / g.splits + kRound - 1) / kRound * kRound;
     const int64_t first = split * each < rows ? split * each : rows, end = first + each < rows ? first + each : rows;
     Tiles tile(s_stage);
-    Source source(a, s_stage, first, end, c0, n0);
+    Source source(a, s_stage, first, end, c0, n0, g.m_tiles, tm, g.db != nullptr);
     float* dw = g.dw + (int64_t) split * (a.x1.width + a.x2.width) * a.hdim;
     tile.run(source, (int32_t) ((end - first + kRound - 1) / kRound) * Source::kSets, 1, [&](int32_t) {
         const int lane = opaque_lane_id(), m0 = Tiles::first_row(lane), n = Tiles::first_column(lane);
@@ -380,7 +407,7 @@ __global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
                 }
             }
     });
-    if (!g.db || tm != 0) return;
+    if (!g.db) return;
     float* s_sum = reinterpret_cast<float*>(s_stage);         // [4][Tiles::kN]: of the four threads that read a column
     __syncthreads();
     s_sum[source.chunk * Tiles::kN + source.column] = source.sum[0];
@@ -388,17 +415,17 @@ __global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
     __syncthreads();
     const int n = (int) threadIdx.x;
     if (n < Tiles::kN && n0 + n < a.hdim)
-        g.db[(int64_t) split * a.hdim + n0 + n] = (s_sum[n] + s_sum[Tiles::kN + n]) + (s_sum[2 * Tiles::kN + n] + s_sum[3 * Tiles::kN + n]);
+        g.db[((int64_t) split * g.m_tiles + tm) * a.hdim + n0 + n] = (s_sum[n] + s_sum[Tiles::kN + n]) + (s_sum[2 * Tiles::kN + n] + s_sum[3 * Tiles::kN + n]);
 }
 
 // Between the two products: the splits' sums, and W in bf16 terms for dx: [plane][f1 + f2][hdim rounded up to kStageK], zeros
 // behind hdim.  Items of four values; a sum's splits are shared by sixteen threads, since there may be few sums of many splits.
 struct BetweenArgs {
-    const float *dw_parts, *db_parts, *w;     // null: nothing to join; null: no db; null: no dx
+    const float *dw_parts, *db_parts, *w;     // null: nothing to join; likewise; no dx
     float *dw, *db;
     uint16_t* terms;
     int64_t k;
-    int32_t hdim, pitch, splits, planes;
+    int32_t hdim, pitch, dw_splits, db_splits, planes;
     int32_t join_blocks;                      // the grid's first; the others cut W
 };
 
@@ -415,17 +442,18 @@ __global__ void __launch_bounds__(kBlock) k_backward_between(BetweenArgs a)
 {
     __shared__ float4 s_part[kJoinThreads][kJoinItems];
     if ((int32_t) blockIdx.x < a.join_blocks) {
-        const int64_t n = a.k * a.hdim, joins = (n + 3) / 4, all = joins + (a.db_parts ? (a.hdim + 3) / 4 : 0);
+        const int64_t n = a.k * a.hdim, joins = a.dw_parts ? (n + 3) / 4 : 0, all = joins + (a.db_parts ? (a.hdim + 3) / 4 : 0);
         const int item = (int) threadIdx.x % kJoinItems, part = (int) threadIdx.x / kJoinItems;
         for (int64_t i0 = (int64_t) blockIdx.x * kJoinItems; i0 < all; i0 += (int64_t) a.join_blocks * kJoinItems) {
             const bool bias = i0 + item >= joins;
             const float* parts = bias ? a.db_parts : a.dw_parts;
             const int64_t i = 4 * (bias ? i0 + item - joins : i0 + item), count = bias ? a.hdim : n;
             const bool marks = count % 4 == 0;
+            const int32_t splits = bias ? a.db_splits : a.dw_splits;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             if (i0 + item < all) {
 #pragma unroll 8
-                for (int32_t s = part; s < a.splits; s += kJoinThreads) {
+                for (int32_t s = part; s < splits; s += kJoinThreads) {
                     const float4 p = load_four(parts + s * count, i, count, marks);
                     v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
                 }
@@ -689,7 +717,7 @@ size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim
     size_t parts = 0;
     for (int i = 0; i < 3; ++i) {                              // of either type, and of bf16 columns read singly
         const WeightsPlan p = plan_weights(c, f1, f2, hdim, rows, i == 0, i < 2);
-        const size_t need = p.splits > 1 ? align256((size_t) p.splits * k * (size_t) hdim * 4) + align256((size_t) p.splits * (size_t) hdim * 4) : 0;
+        const size_t need = (p.splits > 1 ? align256((size_t) p.splits * k * (size_t) hdim * 4) : 0) + align256((size_t) p.splits * (size_t) p.m_tiles * (size_t) hdim * 4);
         if (need > parts) parts = need;
     }
     return parts + align256(3 * k * pitch * 2);
@@ -745,12 +773,16 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     if (a.dw) {
         const WeightsPlan p = plan_weights(c, a.x1.width, a.x2.width, a.hdim, a.count.rows, kFloat, kFloat || reads_pairs(a.d_out));
         WeightsArgs g = {a, p.m_tiles, p.n_tiles, p.splits, a.dw, a.db};
+        b.dw = a.dw; b.db = a.db;
+        b.dw_splits = p.splits;
+        b.db_splits = p.splits * p.m_tiles;
         if (p.splits > 1) {
             b.dw_parts = g.dw = reinterpret_cast<float*>(at);
             at += align256((size_t) p.splits * (size_t) K * (size_t) a.hdim * 4);
-            if (a.db) b.db_parts = g.db = reinterpret_cast<float*>(at);
-            at += align256((size_t) p.splits * (size_t) a.hdim * 4);
-            b.dw = a.dw; b.db = a.db; b.splits = p.splits;
+        }
+        if (a.db && b.db_splits > 1) {
+            b.db_parts = g.db = reinterpret_cast<float*>(at);
+            at += align256((size_t) b.db_splits * (size_t) a.hdim * 4);
         }
         const hipError_t e = p.wide ? launch_weights<T, 512>(g, s) : launch_weights<T, 256>(g, s);
         if (e != hipSuccess) return e;
@@ -759,7 +791,8 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
         b.w = a.w;
         b.terms = reinterpret_cast<uint16_t*>(at);
     }
-    b.join_blocks = b.dw_parts ? (int32_t) grid_of(c, ((int64_t) K * a.hdim + a.hdim + 6) / 4 * kJoinThreads) : 0;
+    const int64_t joins = (b.dw_parts ? ((int64_t) K * a.hdim + 3) / 4 : 0) + (b.db_parts ? (a.hdim + 3) / 4 : 0);
+    b.join_blocks = joins ? (int32_t) grid_of(c, joins * kJoinThreads) : 0;
     const int32_t term_blocks = dx ? (int32_t) grid_of(c, K * (pitch / 4)) : 0;
     if (b.join_blocks + term_blocks) hipLaunchKernelGGL(k_backward_between, dim3((unsigned) (b.join_blocks + term_blocks)), dim3(kBlock), 0, s, b);
     if (!dx) return hipGetLastError();

@@ -32,7 +32,7 @@ const char* rows_fault(const gns_rows* x)
     if (!x || !x->data) return "null rows";
     if (x->type != GNS_FP32 && x->type != GNS_BF16) return "rows are of no known type";
     if (x->width < 1 || x->width > GNS_MAX_WIDTH) return "width of rows out of range";
-    if (x->stride < x->width) return "stride of rows is below their width";
+    if (x->stride < x->width || x->stride > GNS_MAX_STRIDE) return "stride of rows out of range";
     if (reinterpret_cast<uintptr_t>(x->data) % (x->type == GNS_FP32 ? 4 : 2)) return "rows are not aligned to their element";
     return nullptr;
 }

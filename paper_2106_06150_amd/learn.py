@@ -12,7 +12,7 @@ import torch
 from .binding import _check, _stream_ptr, lib
 
 GNS_FP32, GNS_BF16 = 0, 1
-GNS_MAX_WIDTH = 1 << 22
+GNS_MAX_WIDTH, GNS_MAX_STRIDE = 1 << 22, 1 << 24
 GNS_INT8_MAX_K = 131072
 GNS_MAX_TOP = 32
 GNS_STAGE_INT8, GNS_STAGE_CHECKPOINT, GNS_STAGE_BACKWARD, GNS_STAGE_LOG_PROBS = 22, 23, 24, 25

@@ -565,7 +565,8 @@ def test_refusals(ctx):
         assert lib.gns_last_error(ctx)
 
     bad_rows = [None, rows(data=None), rows(stride=63), rows(width=0), rows(width=-1), rows(type=2), rows(type=-1), rows(data=p + 2),
-                rows(data=p + 1, type=1), rows(stride=1 << 40, width=learn.GNS_MAX_WIDTH + 1)]
+                rows(data=p + 1, type=1), rows(stride=learn.GNS_MAX_STRIDE, width=learn.GNS_MAX_WIDTH + 1),
+                rows(stride=learn.GNS_MAX_STRIDE + 1), rows(stride=-64)]
     einval, small = B.GNS_EINVAL, B.GNS_ECAPACITY
     for r in bad_rows:
         refused(einval, "gns_quantize_rows", r, None, qp, fp, 4, s)
