@@ -168,8 +168,9 @@ struct Tile {
 struct WeightsArgs {
     BackwardArgs a;
     int32_t m_tiles, n_tiles, splits;
+    int32_t db_shares;                        // of the m_tiles blocks that read the same rows, how many add up db: all or one
     float* dw;                                // [splits x (f1 + f2) x hdim]: the caller's if there is one split
-    float* db;                                // [splits x m_tiles x hdim]: the caller's if that is one; or null
+    float* db;                                // [splits x db_shares x hdim]: the caller's if that is one; or null
 };
 
 // Packed columns of X are those of x1's groups, then those of x2's.  Row of dw, or -1 where a group is padded.
@@ -207,7 +208,7 @@ struct WeightsSource {
 
     Chunk* const lds;
     const uint32_t row_bytes;                 // of d_out
-    const int32_t m_tiles, tm;                // this block adds up db over every m_tiles-th step
+    const int32_t db_shares;                  // this block adds up db over every so many steps
     int64_t rest;                             // rows there are from the next step's first on
     int32_t until_sum;
     bool begun;
@@ -226,9 +227,9 @@ struct WeightsSource {
     uint32_t x[kSets][4], ex[kSets], d[kSets][kReads], words[kSets];
     float scale[4], sum[2];
 
-    __device__ __forceinline__ WeightsSource(const BackwardArgs& a, Chunk* stages, int64_t first, int64_t end, int32_t c0, int32_t n0, int32_t m_tiles_, int32_t tm_, bool bias)
-        : lds(stages), row_bytes((uint32_t) a.d_out.stride * (uint32_t) sizeof(T)), m_tiles(bias ? m_tiles_ : INT32_MAX), tm(tm_), rest(end - first),
-          until_sum(bias ? tm_ : INT32_MAX), begun(false)
+    __device__ __forceinline__ WeightsSource(const BackwardArgs& a, Chunk* stages, int64_t first, int64_t end, int32_t c0, int32_t n0, int32_t shares, int32_t share)
+        : lds(stages), row_bytes((uint32_t) a.d_out.stride * (uint32_t) sizeof(T)), db_shares(shares), rest(end - first),
+          until_sum(share < shares ? share : INT32_MAX), begun(false)
     {
         const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
         const int row16 = lane >> 4, i8 = lane & 7;
@@ -293,7 +294,7 @@ struct WeightsSource {
         left[set] = (int32_t) (rest < kStageK ? rest : kStageK);
         rest -= kStageK;
         sums[set] = until_sum == 0;
-        until_sum = until_sum == 0 ? m_tiles - 1 : until_sum - 1;
+        until_sum = until_sum == 0 ? db_shares - 1 : until_sum - 1;
     }
     __device__ __forceinline__ void fetch(int set, int i)
     {
@@ -374,7 +375,7 @@ struct WeightsSource {
 };
 
 template <typename T, int kThreads, bool kMask, bool kPairs>
-__global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
+__global__ void __launch_bounds__(kThreads, 2) k_backward_weights(WeightsArgs g)
 {
     typedef WeightsSource<T, kThreads, kMask, kPairs> Source;
     typedef typename Source::Tiles Tiles;
@@ -389,7 +390,7 @@ __global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
     const int64_t each = ((rows + g.splits - 1) / g.splits + kRound - 1) / kRound * kRound;
     const int64_t first = split * each < rows ? split * each : rows, end = first + each < rows ? first + each : rows;
     Tiles tile(s_stage);
-    Source source(a, s_stage, first, end, c0, n0, g.m_tiles, tm, g.db != nullptr);
+    Source source(a, s_stage, first, end, c0, n0, g.db ? g.db_shares : 0, tm);
     float* dw = g.dw + (int64_t) split * (a.x1.width + a.x2.width) * a.hdim;
     tile.run(source, (int32_t) ((end - first + kRound - 1) / kRound) * Source::kSets, 1, [&](int32_t) {
         const int lane = opaque_lane_id(), m0 = Tiles::first_row(lane), n = Tiles::first_column(lane);
@@ -407,7 +408,7 @@ __global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
                 }
             }
     });
-    if (!g.db) return;
+    if (!g.db || tm >= g.db_shares) return;
     float* s_sum = reinterpret_cast<float*>(s_stage);         // [4][Tiles::kN]: of the four threads that read a column
     __syncthreads();
     s_sum[source.chunk * Tiles::kN + source.column] = source.sum[0];
@@ -415,7 +416,7 @@ __global__ void __launch_bounds__(kThreads) k_backward_weights(WeightsArgs g)
     __syncthreads();
     const int n = (int) threadIdx.x;
     if (n < Tiles::kN && n0 + n < a.hdim)
-        g.db[((int64_t) split * g.m_tiles + tm) * a.hdim + n0 + n] = (s_sum[n] + s_sum[Tiles::kN + n]) + (s_sum[2 * Tiles::kN + n] + s_sum[3 * Tiles::kN + n]);
+        g.db[((int64_t) split * g.db_shares + tm) * a.hdim + n0 + n] = (s_sum[n] + s_sum[Tiles::kN + n]) + (s_sum[2 * Tiles::kN + n] + s_sum[3 * Tiles::kN + n]);
 }
 
 // Between the two products: the splits' sums, and W in bf16 terms for dx: [plane][f1 + f2][hdim rounded up to kStageK], zeros
@@ -499,7 +500,7 @@ __global__ void __launch_bounds__(kBlock) k_backward_between(BetweenArgs a)
 struct InputArgs {
     BackwardArgs a;
     int32_t m_tiles, n_tiles, pitch;
-    const uint16_t* w;                        // k_split_weights' planes
+    const uint16_t* w;                        // planes of k_backward_between
 };
 
 template <typename T, int kThreads> struct InputTile;
@@ -511,13 +512,16 @@ template <> struct InputTile<Bf16, 256> { typedef Tile<128, 128, 64, 64, 1, 2> T
 // A thread reads eight columns of a row of dz (of two rows of bf16), and as many of W's planes.  kWhole: rows of dz begin at
 // 16-byte marks and hdim is a multiple of eight, so eight columns are one or two reads; else they are read singly.  Columns
 // past the last are read as the last ones: W's planes are zero there.  A block goes through tiles, `stride` apart.
-template <typename T, int kThreads, bool kMask, bool kWhole>
+// kPlain: W is read as it is and cut here, by every block that needs it, which where there is no more than a block or two per
+// CU costs less than a launch and a trip through memory in front.
+template <typename T, int kThreads, bool kMask, bool kWhole, bool kPlain>
 struct InputSource {
     typedef typename InputTile<T, kThreads>::Type Tiles;
     static constexpr bool kFloat = sizeof(T) == 4;
     static constexpr int kPlanes = kFloat ? 3 : 2, kStep = kThreads / 4;                            // rows the threads cover at once
     static constexpr int kRowsA = Tiles::kM / kStep, kRowsB = Tiles::kN / kStep, kWords = kFloat ? 8 : 4;
-    static constexpr int kSets = kFloat ? 2 : 4, kFetches = kRowsA * (1 + (kMask ? 1 : 0)) + kRowsB * kPlanes;
+    static constexpr int kSets = (kFloat ? kPlain : kThreads == 512) ? 4 : 2, kReadsB = kPlain ? 1 : kPlanes;
+    static constexpr int kFetches = kRowsA * (1 + (kMask ? 1 : 0)) + kRowsB * kReadsB;
     static constexpr int kPutsA = (kMask ? 1 : 0) + (kFloat ? 3 : 1), kPuts = kRowsA * kPutsA + kRowsB * kPlanes;
 
     const InputArgs& g;
@@ -528,12 +532,13 @@ struct InputSource {
     int row, chunk;
     const char* z[kRowsA];                    // this thread's rows of dz
     const uint32_t* m[kRowsA];                // and of the mask
-    const char* w;                            // the tile's first row of W's planes
+    const char* w;                            // the tile's first row of W or its planes
     uint32_t w_at[kRowsB];                    // from there to this thread's rows and columns
     int32_t n, word;                          // of the step that is read: this thread's first column, its word of the mask
     int64_t w_step;                           // and bytes from a plane's row to its columns
     uint32_t d[kSets][kRowsA][kWords], words[kSets][kRowsA], keep[kSets];
-    Chunk planes[kSets][kRowsB][kPlanes];
+    Chunk planes[kSets][kRowsB][kPlain ? 1 : kPlanes];
+    uint32_t plain[kSets][kRowsB][kPlain ? 8 : 1];
 
     __device__ __forceinline__ InputSource(const InputArgs& args, Chunk* stages, int64_t rows_, int32_t tiles_, int32_t first, int32_t stride_)
         : g(args), lds(stages), rows(rows_), K(args.a.x1.width + args.a.x2.width), m_tiles(tiles_), stride(stride_),
@@ -556,9 +561,13 @@ struct InputSource {
             if constexpr (kMask) m[i] = a.positive + r * ((a.hdim + 31) / 32);
         }
         const int64_t k0 = (int64_t) tn * Tiles::kN;
-        w = reinterpret_cast<const char*>(g.w + k0 * g.pitch);
+        if constexpr (kPlain) w = reinterpret_cast<const char*>(a.w + k0 * a.hdim);
+        else                  w = reinterpret_cast<const char*>(g.w + k0 * g.pitch);
 #pragma unroll
-        for (int i = 0; i < kRowsB; ++i) w_at[i] = (uint32_t) min((int64_t) row + i * kStep, K - 1 - k0) * (uint32_t) g.pitch * 2u + (uint32_t) chunk * 16u;
+        for (int i = 0; i < kRowsB; ++i) {
+            const uint32_t k = (uint32_t) min((int64_t) row + i * kStep, K - 1 - k0);
+            w_at[i] = kPlain ? k * (uint32_t) a.hdim * 4u : k * (uint32_t) g.pitch * 2u + (uint32_t) chunk * 16u;
+        }
     }
     __device__ __forceinline__ void seek(int set)
     {
@@ -570,7 +579,7 @@ struct InputSource {
         const int32_t hdim = g.a.hdim, at = n0 < g.pitch ? n0 : g.pitch - kStageK;       // steps that only fill a turn read the last again
         n = n0 + chunk * 8;
         if constexpr (kWhole) n = min(n, hdim - 8);
-        if constexpr (kMask) {
+        if constexpr (kMask || kPlain) {
             const int32_t inside = hdim - n0 - chunk * 8;     // of the eight columns
             keep[set] = inside >= 8 ? 0xFFu : inside > 0 ? (1u << inside) - 1u : 0u;
         } else {
@@ -602,11 +611,25 @@ struct InputSource {
                     d[set][i][j] = from[min(n + 2 * j, hdim - 1)] | (uint32_t) from[min(n + 2 * j + 1, hdim - 1)] << 16;
                 }
             }
-        } else if (i < kRowsA + kRowsB * kPlanes) {
+        } else if (kPlain && i < kRowsA + kRowsB) {
+            const int b = i - kRowsA;
+            const float* from = reinterpret_cast<const float*>(w + w_at[b]);
+            if constexpr (kWhole) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const Chunk v = *reinterpret_cast<const Chunk*>(from + n + 4 * j);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) plain[set][b][4 * j + k] = v[k];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) plain[set][b][j] = __float_as_uint(from[min(n + j, hdim - 1)]);
+            }
+        } else if (i < kRowsA + kRowsB * kReadsB) {
             const int b = (i - kRowsA) / kPlanes, p = (i - kRowsA) % kPlanes;
             planes[set][b][p] = *reinterpret_cast<const Chunk*>(w + (w_step + p * K * g.pitch * 2) + w_at[b]);
         } else {
-            const int b = i - kRowsA - kRowsB * kPlanes;
+            const int b = i - kRowsA - kRowsB * kReadsB;
             words[set][b] = m[b][word];
         }
     }
@@ -615,9 +638,18 @@ struct InputSource {
         Chunk* to = lds + stage * Tiles::kStage;
         if (i >= kRowsA * kPutsA) {
             const int b = (i - kRowsA * kPutsA) / kPlanes, p = (i - kRowsA * kPutsA) % kPlanes;
-            Chunk v = planes[set][b][p];
-            if (!kMask && kSets > 1) v = keep[set] ? v : Chunk{0, 0, 0, 0};
-            to[Tiles::place_b(p, row + b * kStep, chunk)] = v;
+            if constexpr (kPlain) {
+                uint32_t (&v)[8] = plain[set][b];
+                if (p == 0) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] &= kWhole ? (keep[set] ? ~0u : 0u) : spread_bit(keep[set], j);
+                }
+                to[Tiles::place_b(p, row + b * kStep, chunk)] = take_terms(v);
+            } else {
+                Chunk v = planes[set][b][p];
+                if (!kMask) v = keep[set] ? v : Chunk{0, 0, 0, 0};
+                to[Tiles::place_b(p, row + b * kStep, chunk)] = v;
+            }
             return;
         }
         const int b = i / kPutsA, u = i % kPutsA - (kMask ? 1 : 0);
@@ -638,10 +670,10 @@ struct InputSource {
     }
 };
 
-template <typename T, int kThreads, bool kMask, bool kWhole>
-__global__ void __launch_bounds__(kThreads) k_backward_input(InputArgs g)
+template <typename T, int kThreads, bool kMask, bool kWhole, bool kPlain>
+__global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
 {
-    typedef InputSource<T, kThreads, kMask, kWhole> Source;
+    typedef InputSource<T, kThreads, kMask, kWhole, kPlain> Source;
     typedef typename Source::Tiles Tiles;
     __shared__ Chunk s_stage[3 * Tiles::kStage];
     const BackwardArgs& a = g.a;
@@ -693,22 +725,30 @@ static bool reads_pairs(const ConstRows& d_out)
 // How a call's weights' gradient is shared out.
 struct WeightsPlan {
     bool wide;                                // blocks of 512 threads
-    int32_t m_tiles, n_tiles, splits;
+    int32_t m_tiles, n_tiles, splits, db_shares;
 };
 
 static WeightsPlan plan_weights(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int64_t rows, bool fp32, bool wide)
 {
-    WeightsPlan p;
     const int32_t columns = ((f1 + 31) / 32 + (f2 + 31) / 32) * 32, n512 = fp32 ? 128 : 256;
-    p.wide = wide && columns > 128 && hdim > n512 / 2;
-    const int32_t bm = p.wide ? 256 : 128, bn = p.wide ? n512 : n512 / 2;
-    p.m_tiles = (columns + bm - 1) / bm;
-    p.n_tiles = (hdim + bn - 1) / bn;
-    const int64_t blocks = (int64_t) c->num_cus * (p.wide ? 1 : 2), most = (rows + 127) / 128;
-    int64_t s = blocks / ((int64_t) p.m_tiles * p.n_tiles);
-    if (s > most) s = most;
-    p.splits = s < 1 ? 1 : (int32_t) s;
-    return p;
+    const int64_t most = (rows + 127) / 128;                  // splits of four steps at least
+    auto plan = [&](bool is_wide) {
+        WeightsPlan p;
+        p.wide = is_wide;
+        const int32_t bm = is_wide ? 256 : 128, bn = is_wide ? n512 : n512 / 2;
+        p.m_tiles = (columns + bm - 1) / bm;
+        p.n_tiles = (hdim + bn - 1) / bn;
+        int64_t s = (int64_t) c->num_cus * (is_wide ? 1 : 2) / ((int64_t) p.m_tiles * p.n_tiles);
+        if (s > most) s = most;
+        p.splits = s < 1 ? 1 : (int32_t) s;
+        // a few steps more of one block in m_tiles cost less than the launch that joins the shares
+        p.db_shares = p.splits == 1 && rows <= 512 ? 1 : p.m_tiles;
+        return p;
+    };
+    // Wide blocks where layers fill them and they fill half the chip at least
+    const WeightsPlan p = plan(true);
+    if (wide && columns > 128 && hdim > n512 / 2 && (int64_t) p.m_tiles * p.n_tiles * p.splits >= c->num_cus / 2) return p;
+    return plan(false);
 }
 
 size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows)
@@ -717,7 +757,7 @@ size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim
     size_t parts = 0;
     for (int i = 0; i < 3; ++i) {                              // of either type, and of bf16 columns read singly
         const WeightsPlan p = plan_weights(c, f1, f2, hdim, rows, i == 0, i < 2);
-        const size_t need = (p.splits > 1 ? align256((size_t) p.splits * k * (size_t) hdim * 4) : 0) + align256((size_t) p.splits * (size_t) p.m_tiles * (size_t) hdim * 4);
+        const size_t need = (p.splits > 1 ? align256((size_t) p.splits * k * (size_t) hdim * 4) : 0) + align256((size_t) p.splits * (size_t) p.db_shares * (size_t) hdim * 4);
         if (need > parts) parts = need;
     }
     return parts + align256(3 * k * pitch * 2);
@@ -743,20 +783,28 @@ static hipError_t launch_weights(const WeightsArgs& g, hipStream_t s)
     return hipGetLastError();
 }
 
+// Tiles of dx in blocks of so many threads
 template <typename T, int kThreads>
-static hipError_t launch_input(const gns_ctx* c, InputArgs g, hipStream_t s)
+static int64_t input_tiles(const BackwardArgs& a, int32_t* m_tiles, int32_t* n_tiles)
 {
     typedef typename InputTile<T, kThreads>::Type Tiles;
-    g.m_tiles = (int32_t) (((int64_t) g.a.count.rows + Tiles::kM - 1) / Tiles::kM);
-    g.n_tiles = (g.a.x1.width + g.a.x2.width + Tiles::kN - 1) / Tiles::kN;
-    const int64_t tiles = (int64_t) g.m_tiles * g.n_tiles, most = (int64_t) c->num_cus * (kThreads == 512 ? 1 : 2);
+    *m_tiles = (int32_t) (((int64_t) a.count.rows + Tiles::kM - 1) / Tiles::kM);
+    *n_tiles = (a.x1.width + a.x2.width + Tiles::kN - 1) / Tiles::kN;
+    return (int64_t) *m_tiles * *n_tiles;
+}
+
+template <typename T, int kThreads, bool kPlain>
+static hipError_t launch_input(const gns_ctx* c, InputArgs g, hipStream_t s)
+{
+    const int64_t tiles = input_tiles<T, kThreads>(g.a, &g.m_tiles, &g.n_tiles), most = (int64_t) c->num_cus * (kThreads == 512 ? 1 : 2);
     if (tiles >= (int64_t) 1 << 30) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned) (tiles < most ? tiles : most)), block(kThreads);
-    const bool whole = g.a.hdim % 8 == 0 && reinterpret_cast<uintptr_t>(g.a.d_out.data) % 16 == 0 && (uint64_t) g.a.d_out.stride * sizeof(T) % 16 == 0;
-    if (g.a.positive && whole)  hipLaunchKernelGGL((k_backward_input<T, kThreads, true, true>), grid, block, 0, s, g);
-    else if (g.a.positive)      hipLaunchKernelGGL((k_backward_input<T, kThreads, true, false>), grid, block, 0, s, g);
-    else if (whole)             hipLaunchKernelGGL((k_backward_input<T, kThreads, false, true>), grid, block, 0, s, g);
-    else                        hipLaunchKernelGGL((k_backward_input<T, kThreads, false, false>), grid, block, 0, s, g);
+    const bool whole = g.a.hdim % 8 == 0 && reinterpret_cast<uintptr_t>(g.a.d_out.data) % 16 == 0 && (uint64_t) g.a.d_out.stride * sizeof(T) % 16 == 0 &&
+                       (!kPlain || reinterpret_cast<uintptr_t>(g.a.w) % 16 == 0);
+    if (g.a.positive && whole)  hipLaunchKernelGGL((k_backward_input<T, kThreads, true, true, kPlain>), grid, block, 0, s, g);
+    else if (g.a.positive)      hipLaunchKernelGGL((k_backward_input<T, kThreads, true, false, kPlain>), grid, block, 0, s, g);
+    else if (whole)             hipLaunchKernelGGL((k_backward_input<T, kThreads, false, true, kPlain>), grid, block, 0, s, g);
+    else                        hipLaunchKernelGGL((k_backward_input<T, kThreads, false, false, kPlain>), grid, block, 0, s, g);
     return hipGetLastError();
 }
 
@@ -772,10 +820,10 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     b.k = K; b.hdim = a.hdim; b.pitch = (int32_t) pitch; b.planes = kFloat ? 3 : 2;
     if (a.dw) {
         const WeightsPlan p = plan_weights(c, a.x1.width, a.x2.width, a.hdim, a.count.rows, kFloat, kFloat || reads_pairs(a.d_out));
-        WeightsArgs g = {a, p.m_tiles, p.n_tiles, p.splits, a.dw, a.db};
+        WeightsArgs g = {a, p.m_tiles, p.n_tiles, p.splits, p.db_shares, a.dw, a.db};
         b.dw = a.dw; b.db = a.db;
         b.dw_splits = p.splits;
-        b.db_splits = p.splits * p.m_tiles;
+        b.db_splits = p.splits * p.db_shares;
         if (p.splits > 1) {
             b.dw_parts = g.dw = reinterpret_cast<float*>(at);
             at += align256((size_t) p.splits * (size_t) K * (size_t) a.hdim * 4);
@@ -787,19 +835,23 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
         const hipError_t e = p.wide ? launch_weights<T, 512>(g, s) : launch_weights<T, 256>(g, s);
         if (e != hipSuccess) return e;
     }
-    if (dx) {
+    // Blocks of 512 threads where they fill the chip and layers are not too narrow for them; else of 256, and with no more than
+    // those that run together W is read as it is.
+    typedef typename InputTile<T, 512>::Type Wide;
+    int32_t m_tiles, n_tiles;
+    const bool wide = input_tiles<T, 512>(a, &m_tiles, &n_tiles) >= c->num_cus && K > Wide::kN / 2;
+    const bool plain = !wide && input_tiles<T, 256>(a, &m_tiles, &n_tiles) <= c->num_cus;
+    if (dx && !plain) {
         b.w = a.w;
         b.terms = reinterpret_cast<uint16_t*>(at);
     }
     const int64_t joins = (b.dw_parts ? ((int64_t) K * a.hdim + 3) / 4 : 0) + (b.db_parts ? (a.hdim + 3) / 4 : 0);
     b.join_blocks = joins ? (int32_t) grid_of(c, joins * kJoinThreads) : 0;
-    const int32_t term_blocks = dx ? (int32_t) grid_of(c, K * (pitch / 4)) : 0;
+    const int32_t term_blocks = b.w ? (int32_t) grid_of(c, K * (pitch / 4)) : 0;
     if (b.join_blocks + term_blocks) hipLaunchKernelGGL(k_backward_between, dim3((unsigned) (b.join_blocks + term_blocks)), dim3(kBlock), 0, s, b);
     if (!dx) return hipGetLastError();
     InputArgs g = {a, 0, 0, (int32_t) pitch, b.terms};
-    typedef typename InputTile<T, 512>::Type Wide;
-    const int64_t tiles = ((int64_t) a.count.rows + Wide::kM - 1) / Wide::kM * ((K + Wide::kN - 1) / Wide::kN);
-    return tiles >= c->num_cus && K > Wide::kN / 2 ? launch_input<T, 512>(c, g, s) : launch_input<T, 256>(c, g, s);
+    return wide ? launch_input<T, 512, false>(c, g, s) : plain ? launch_input<T, 256, true>(c, g, s) : launch_input<T, 256, false>(c, g, s);
 }
 
 hipError_t launch_backward(const gns_ctx* c, const BackwardArgs& a, int32_t type, hipStream_t s)
