@@ -47,7 +47,7 @@ typedef struct {
 #define GNS_INT8_MAX_K 131072 /* 127 * 127 * k stays below 2^31 */
 
 /* Quantises rows [x1 | x2] (x2 may be NULL; both of one type) of together k <= GNS_INT8_MAX_K columns: a = max |x[r, :]|,
- * scale[r] = a / 127, q[r, c] = x[r, c] * (127 / a) rounded to nearest, ties to even, each operation in fp32.  A row whose a is
+ * scale[r] = a / 127, q[r, c] = x[r, c] * (127 * (1 / a)) rounded to nearest, ties to even, each operation in fp32.  A row whose a is
  * below 2^-120 gets scale 0 and zeros; one with an infinity or NaN gets scale NaN and zeros.  Also the way to quantise
  * weights, given as hdim rows of k (one scale per output channel). */
 gns_status gns_quantize_rows(gns_ctx* ctx, const gns_rows* x1, const gns_rows* x2, int8_t* q_dev, float* scale_dev,

@@ -42,7 +42,7 @@ __device__ __forceinline__ RowScale row_scale(uint32_t most)
     const float amax = __uint_as_float(most);
     if (most >= kInfBits) return RowScale{quiet_nan(), 0.f};
     if (amax < 0x1p-120f) return RowScale{0.f, 0.f};
-    return RowScale{amax / 127.f, 127.f / amax};
+    return RowScale{amax / 127.f, 127.f * (1.f / amax)};
 }
 
 template <int V>
@@ -412,21 +412,28 @@ __global__ void __launch_bounds__(kWaves * kWave) k_int8_rows(DenseInt8Args a, Q
     __syncthreads();
     const int32_t tiles = (rows + 15) / 16;
     const bool stores = n % 4 == 0 && reinterpret_cast<uintptr_t>(a.out.data) % 16 == 0 && (uint64_t) a.out.stride * sizeof(T) % 16 == 0;
-    // the blocks' first waves take the first tiles: a remainder spreads over all CUs
-    for (int32_t tile = wave * (int32_t) gridDim.x + (int32_t) blockIdx.x; tile < tiles; tile += (int32_t) gridDim.x * kWaves) {
-        const int lane = opaque_lane_id(), l = lane & (L - 1), l16 = lane & 15, kg = lane >> 4;
-        const int64_t r0 = (int64_t) tile * 16;
-        Piece<T> v[kTurns][P];
+    // A tile's rows are read when the one before has been quantised, and come while that one is multiplied and stored.  Rows past
+    // the last are read as the last, lanes past the last column read the first.
+    Piece<T> v[kTurns][P];
+    auto fetch = [&](int32_t tile) {
+        const int lane = opaque_lane_id(), l = lane & (L - 1);
 #pragma unroll
         for (int t = 0; t < kTurns; ++t) {
-            const int64_t row = r0 + t * (kWave / L) + lane / L, r = row < rows ? row : rows - 1;
+            const int64_t row = (int64_t) tile * 16 + t * (kWave / L) + lane / L, r = row < rows ? row : rows - 1;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const int32_t c = (p * L + l) * V, cc = c < k ? c : 0;        // lanes past the last column read the first
+                const int32_t c = (p * L + l) * V, cc = c < k ? c : 0;
                 v[t][p] = *reinterpret_cast<const Piece<T>*>(cc < f1 ? reinterpret_cast<const T*>(x.x1.data) + r * x.x1.stride + cc
                                                                      : reinterpret_cast<const T*>(x.x2.data) + r * x.x2.stride + (cc - f1));
             }
         }
+    };
+    // the blocks' first waves take the first tiles: a remainder spreads over all CUs
+    int32_t tile = wave * (int32_t) gridDim.x + (int32_t) blockIdx.x;
+    if (tile < tiles) fetch(tile);
+    for (; tile < tiles; tile += (int32_t) gridDim.x * kWaves) {
+        const int lane = opaque_lane_id(), l = lane & (L - 1), l16 = lane & 15, kg = lane >> 4;
+        const int64_t r0 = (int64_t) tile * 16;
         float scale = 0.f;                                    // of row l16
 #pragma unroll
         for (int t = 0; t < kTurns; ++t) {
@@ -447,6 +454,7 @@ __global__ void __launch_bounds__(kWaves * kWave) k_int8_rows(DenseInt8Args a, Q
             if (l16 / (kWave / L) == t) scale = other;
         }
         __builtin_amdgcn_wave_barrier();
+        if (tile + (int32_t) gridDim.x * kWaves < tiles) fetch(tile + (int32_t) gridDim.x * kWaves);
         const int8_t* q = s_q + l16 * pitch + kg * 16;
         T* out = reinterpret_cast<T*>(a.out.data) + (r0 + l16) * a.out.stride;
         for (int32_t c0 = 0; c0 < n16; c0 += 16 * kGroups) {

@@ -77,7 +77,7 @@ def ref_quantize(x):
     with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
         amax = np.abs(x).max(1).astype(np.float32)
         bad, none = ~np.isfinite(amax), amax < np.float32(2.0 ** -120)
-        inv = np.where(bad | none, np.float32(0), np.float32(127) / amax).astype(np.float32)
+        inv = np.where(bad | none, np.float32(0), np.float32(127) * (np.float32(1) / amax)).astype(np.float32)
         q = np.where((bad | none)[:, None], 0, np.rint((x * inv[:, None]).astype(np.float32)))
         scale = np.where(bad, np.float32(np.nan), np.where(none, np.float32(0), amax / np.float32(127)))
     return q.astype(np.int64), scale.astype(np.float32)
