@@ -356,15 +356,32 @@ __global__ void __launch_bounds__(kBlock) k_log_probs_long(LongArgs g)
     }
 }
 
-// A wave per row: its parts' sums and best classes.
+// A wave per row: its parts' sums and best classes, which are on their way first.
+constexpr int kJoinKeys = 16;                 // of a lane
 template <typename T>
 __global__ void __launch_bounds__(kWave) k_log_probs_join(LongArgs g)
 {
     constexpr float kNone = -__builtin_inff();
     const LogProbsArgs& a = g.a;
-    const int32_t rows = a.count.get(), top = a.top;
+    const int32_t rows = a.count.get(), top = a.top, n = g.parts * top;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const int lane = opaque_lane_id();
+        const Key* from = g.best + r * n;
+        float z[kJoinKeys];
+        int32_t index[kJoinKeys];
+        float largest;
+        auto fetch = [&](int32_t i0) {
+            largest = kNone;
+#pragma unroll
+            for (int j = 0; j < kJoinKeys; ++j) {
+                const int32_t i = i0 + j * kWave + lane;
+                const Key k = i < n ? from[i] : kNoKey;
+                z[j] = value_of(k);
+                index[j] = index_of(k);
+                largest = fmaxf(largest, z[j]);
+            }
+        };
+        if (top) fetch(0);
         int32_t label;
         const float z_label = label_logit<T>(a, r, &label);
         Softmax s = {kNone, 0.f, 0.f};
@@ -380,23 +397,12 @@ __global__ void __launch_bounds__(kWave) k_log_probs_join(LongArgs g)
         if (lane == 0) write_row<T>(a, r, o, label, z_label);
         if (!top) continue;
         WaveList list = empty_list();
-        const Key* from = g.best + r * g.parts * top;
-        const int32_t n = g.parts * top;
-        constexpr int kTurn = 16;
-        for (int32_t i0 = 0; i0 < n; i0 += kWave * kTurn) {
-            float z[kTurn];
-            int32_t index[kTurn];
-            float largest = kNone;
-#pragma unroll
-            for (int j = 0; j < kTurn; ++j) {
-                const int32_t i = i0 + j * kWave + lane;
-                const Key k = i < n ? from[i] : kNoKey;
-                z[j] = value_of(k);
-                index[j] = index_of(k);
-                largest = fmaxf(largest, z[j]);
-            }
-            if (i0 == 0) bound_by_lanes(list, largest, top);
+        bound_by_lanes(list, largest, top);
+        for (int32_t i0 = 0;;) {
             take_up(list, z, largest, top, [&](int j) { return index[j]; });
+            i0 += kWave * kJoinKeys;
+            if (i0 >= n) break;
+            fetch(i0);
         }
         if (lane < top) {
             const bool gone = o.bad || list.mine == kNoKey;
@@ -513,14 +519,15 @@ static unsigned grid_of(const gns_ctx* c, int64_t blocks, int per_cu)
 
 constexpr int32_t kShortClasses = 256;
 
-// Parts of a row: enough for eight waves on every SIMD, of at least two tiles.
-static void split_rows(const gns_ctx* c, int32_t classes, int32_t rows, int32_t* parts, int32_t* tiles)
+// Parts of a row: enough for eight waves on every SIMD, of at least two tiles, and no more best classes than the join reads at once.
+static void split_rows(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows, int32_t* parts, int32_t* tiles)
 {
     const int32_t all = (int32_t) (((int64_t) classes + kWaveTile - 1) / kWaveTile);
     const int64_t waves = (int64_t) c->num_cus * 4 * 8;
     int64_t p = 1;
     if ((int64_t) rows * 2 <= waves) p = waves / rows;
     if (p > all / 2) p = all / 2;
+    if (top && p > kJoinKeys * kWave / top) p = kJoinKeys * kWave / top;
     if (p < 1) p = 1;
     *tiles = (int32_t) ((all + p - 1) / p);
     *parts = (all + *tiles - 1) / *tiles;
@@ -532,7 +539,7 @@ size_t log_probs_workspace(const gns_ctx* c, int32_t classes, int32_t top, int32
 {
     if (classes <= kShortClasses) return 0;
     int32_t parts, tiles;
-    split_rows(c, classes, rows, &parts, &tiles);
+    split_rows(c, classes, top, rows, &parts, &tiles);
     return parts == 1 ? 0 : sums_bytes(rows, parts) + (size_t) rows * (size_t) parts * (size_t) top * sizeof(Key);
 }
 
@@ -555,7 +562,7 @@ static hipError_t launch_typed(const gns_ctx* c, const LogProbsArgs& a, hipStrea
     if (C <= kShortClasses) return launch_short<T, 16, 16>(c, a, s);
     LongArgs g = {};
     g.a = a;
-    split_rows(c, C, a.count.rows, &g.parts, &g.tiles);
+    split_rows(c, C, a.top, a.count.rows, &g.parts, &g.tiles);
     if (g.parts > 1) {
         g.sums = static_cast<PartSums*>(a.workspace);
         g.best = reinterpret_cast<Key*>(static_cast<char*>(a.workspace) + sums_bytes(a.count.rows, g.parts));
