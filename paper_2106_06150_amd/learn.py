@@ -61,22 +61,24 @@ def checkpoint_groups(width):
     return (width + CHECKPOINT_GROUP - 1) // CHECKPOINT_GROUP
 
 
+_TYPES = {torch.float32: GNS_FP32, torch.bfloat16: GNS_BF16}
+
+
 def _rows(t, num_rows):
     """gns_rows of a 2-D tensor, or None of None."""
     if t is None:
         return None
-    assert t.is_cuda and t.dim() == 2 and t.dtype in (torch.float32, torch.bfloat16)
     count, width = t.shape
-    assert count >= num_rows and (width == 1 or t.stride(1) == 1)
-    return gns_rows(t.data_ptr(), t.stride(0) if count > 1 else max(width, t.stride(0)), width,
-                    GNS_FP32 if t.dtype == torch.float32 else GNS_BF16)
+    stride, step = t.stride()
+    assert t.is_cuda and count >= num_rows and (step == 1 or width == 1)
+    return gns_rows(t.data_ptr(), stride if count > 1 else max(width, stride), width, _TYPES[t.dtype])
 
 
 def _flat(t, dtype, count):
     """Address of a contiguous tensor of at least `count` elements, or None of None."""
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.numel() >= count
+    assert t.is_cuda and t.dtype is dtype and t.numel() >= count and t.is_contiguous()
     return t.data_ptr()
 
 
