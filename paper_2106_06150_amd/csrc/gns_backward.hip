@@ -707,6 +707,130 @@ __global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
     });
 }
 
+// k_backward_few: dx of rows by the ten, where W's bytes are all there is to do.  A block has 16 columns of dx (rows of W) and all
+// rows, 16 a tile; its eight waves an eighth of hdim each, 16 x 16 x 32 products; their sums meet in LDS.  W is cut into terms
+// on the way, as dz is.
+constexpr int kFewBlock = 512, kFewWaves = kFewBlock / kWave, kFewColumns = 16;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+template <typename T, int MT, bool kMask, bool kWhole>
+__global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
+{
+    constexpr bool kFloat = sizeof(T) == 4;
+    constexpr int kTermsA = kFloat ? 3 : 1, kTermsB = kFloat ? 3 : 2, kSets = MT == 1 ? 4 : 2;
+    typedef Pairs<kTermsA, kTermsB> P;
+    __shared__ float s_sum[kFewWaves][MT][4][kWave];
+    const int32_t rows = a.count.get(), K = a.x1.width + a.x2.width, hdim = a.hdim, steps = (hdim + 31) / 32;
+    if (rows <= 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
+    const int l16 = lane & 15, kg = lane >> 4;
+    const int32_t k0 = (int32_t) blockIdx.x * kFewColumns;
+    const int32_t s0 = (int32_t) ((int64_t) steps * wave / kFewWaves), s1 = (int32_t) ((int64_t) steps * (wave + 1) / kFewWaves);
+    const float* w = a.w + (int64_t) min(k0 + l16, K - 1) * hdim;
+    const T* z[MT];
+    const uint32_t* m[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {                            // rows past the last are read as the last; they are not stored
+        const int64_t r = min(t * 16 + l16, rows - 1);
+        z[t] = reinterpret_cast<const T*>(a.d_out.data) + r * a.d_out.stride;
+        if constexpr (kMask) m[t] = a.positive + r * steps;
+    }
+    uint32_t wv[kSets][8], zv[kSets][MT][kFloat ? 8 : 4], words[kSets][MT];
+    auto fetch = [&](int set, int32_t step) {                 // steps past the wave's last read that one again
+        step = min(step, s1 - 1);
+        const int32_t n = step * 32 + kg * 8;
+        if constexpr (kWhole) {
+            const int32_t at = min(n, hdim - 8);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const Chunk v = *reinterpret_cast<const Chunk*>(w + at + 4 * j);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) wv[set][4 * j + k] = v[k];
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int j = 0; j < (kFloat ? 2 : 1); ++j) {
+                    const Chunk v = *reinterpret_cast<const Chunk*>(z[t] + at + 4 * j);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) zv[set][t][4 * j + k] = v[k];
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) wv[set][j] = __float_as_uint(w[min(n + j, hdim - 1)]);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                if constexpr (kFloat) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) zv[set][t][j] = __float_as_uint(z[t][min(n + j, hdim - 1)]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) zv[set][t][j] = z[t][min(n + 2 * j, hdim - 1)].bits | (uint32_t) z[t][min(n + 2 * j + 1, hdim - 1)].bits << 16;
+                }
+            }
+        }
+        if constexpr (kMask) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t) words[set][t] = m[t][step];
+        }
+    };
+    floatx4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](int set, int32_t step) {
+        const int32_t inside = hdim - step * 32 - kg * 8;     // of the eight columns
+        const uint32_t keep = inside >= 8 ? 0xFFu : inside > 0 ? (1u << inside) - 1u : 0u;
+        Chunk wt[kTermsB];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) wv[set][j] &= spread_bit(keep, j);
+#pragma unroll
+        for (int k = 0; k < kTermsB; ++k) wt[k] = take_terms(wv[set]);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const uint32_t k8 = kMask ? keep & words[set][t] >> (kg * 8) : keep;
+            Chunk zt[kTermsA];
+            if constexpr (kFloat) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) zv[set][t][j] &= spread_bit(k8, j);
+#pragma unroll
+                for (int k = 0; k < kTermsA; ++k) zt[k] = take_terms(zv[set][t]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) zt[0][j] = zv[set][t][j] & ((spread_bit(k8, 2 * j) & 0xFFFFu) | (spread_bit(k8, 2 * j + 1) & 0xFFFF0000u));
+            }
+#pragma unroll
+            for (int p = 0; p < P::kCount; ++p)
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, zt[P::kA[p]]), __builtin_bit_cast(bf16x8, wt[P::kB[p]]), acc[t], 0, 0, 0);
+        }
+    };
+    if (s0 < s1) {
+#pragma unroll
+        for (int d = 0; d < kSets; ++d) fetch(d, s0 + d);
+        for (int32_t s = s0; s < s1; s += kSets) {
+#pragma unroll
+            for (int d = 0; d < kSets; ++d) {
+                if (s + d < s1) multiply(d, s + d);           // wave-uniform
+                fetch(d, s + d + kSets);
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s_sum[wave][t][v][lane] = acc[t][v];
+    __syncthreads();
+    // element v of lane l is row 4 * (l / 16) + v, column l % 16
+    for (int i = (int) threadIdx.x; i < MT * 4 * kWave; i += kFewBlock) {
+        const int t = i / (4 * kWave), v = i / kWave % 4, l = i % kWave;
+        const int32_t r = t * 16 + 4 * (l >> 4) + v, k = k0 + (l & 15);
+        if (r >= rows || k >= K) continue;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][t][v][l];
+        store_at<T>(a.dx, r, k, sum);
+    }
+}
+
 // ---- launches -----------------------------------------------------------------------------------------------------
 static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -808,6 +932,21 @@ static hipError_t launch_input(const gns_ctx* c, InputArgs g, hipStream_t s)
     return hipGetLastError();
 }
 
+constexpr int32_t kFewRows = 64;
+
+template <typename T, int MT>
+static hipError_t launch_few(const BackwardArgs& a, hipStream_t s)
+{
+    const dim3 grid((unsigned) ((a.x1.width + a.x2.width + kFewColumns - 1) / kFewColumns)), block(kFewBlock);
+    const bool whole = a.hdim % 8 == 0 && reinterpret_cast<uintptr_t>(a.d_out.data) % 16 == 0 && (uint64_t) a.d_out.stride * sizeof(T) % 16 == 0 &&
+                       reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
+    if (a.positive && whole) hipLaunchKernelGGL((k_backward_few<T, MT, true, true>), grid, block, 0, s, a);
+    else if (a.positive)     hipLaunchKernelGGL((k_backward_few<T, MT, true, false>), grid, block, 0, s, a);
+    else if (whole)          hipLaunchKernelGGL((k_backward_few<T, MT, false, true>), grid, block, 0, s, a);
+    else                     hipLaunchKernelGGL((k_backward_few<T, MT, false, false>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
 template <typename T>
 static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStream_t s)
 {
@@ -840,8 +979,8 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     typedef typename InputTile<T, 512>::Type Wide;
     int32_t m_tiles, n_tiles;
     const bool wide = input_tiles<T, 512>(a, &m_tiles, &n_tiles) >= c->num_cus && K > Wide::kN / 2;
-    const bool plain = !wide && input_tiles<T, 256>(a, &m_tiles, &n_tiles) <= c->num_cus;
-    if (dx && !plain) {
+    const bool plain = !wide && input_tiles<T, 256>(a, &m_tiles, &n_tiles) <= c->num_cus, few = a.count.rows <= kFewRows;
+    if (dx && !plain && !few) {
         b.w = a.w;
         b.terms = reinterpret_cast<uint16_t*>(at);
     }
@@ -850,6 +989,7 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     const int32_t term_blocks = b.w ? (int32_t) grid_of(c, K * (pitch / 4)) : 0;
     if (b.join_blocks + term_blocks) hipLaunchKernelGGL(k_backward_between, dim3((unsigned) (b.join_blocks + term_blocks)), dim3(kBlock), 0, s, b);
     if (!dx) return hipGetLastError();
+    if (few) return a.count.rows <= 16 ? launch_few<T, 1>(a, s) : launch_few<T, 4>(a, s);
     InputArgs g = {a, 0, 0, (int32_t) pitch, b.terms};
     return wide ? launch_input<T, 512, false>(c, g, s) : plain ? launch_input<T, 256, true>(c, g, s) : launch_input<T, 256, false>(c, g, s);
 }
