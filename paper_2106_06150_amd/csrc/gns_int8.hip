@@ -12,6 +12,7 @@ __device__ __forceinline__ float output_of(int sum, float w_scale, float scale, 
 
 // Pieces of V consecutive columns of a row [x1 | x2]: 16 bytes of either type.
 template <typename T> constexpr int kPiece = 16 / (int) sizeof(T);
+template <typename T> struct alignas(16) Piece { T v[kPiece<T>]; };
 
 // kAligned: both inputs' rows begin at 16-byte marks and f1 is a multiple of the piece, so a piece inside a row is one read;
 // else its values are read singly.  Columns past the last are zero.
@@ -21,10 +22,9 @@ __device__ __forceinline__ void load_piece(const QuantizeArgs& a, int64_t r, int
     constexpr int V = kPiece<T>;
     const int32_t f1 = a.x1.width, k = f1 + a.x2.width;
     if (kAligned && c + V <= k) {
-        struct alignas(16) Piece { T v[V]; };
         const T* from = c < f1 ? reinterpret_cast<const T*>(a.x1.data) + r * a.x1.stride + c
                                : reinterpret_cast<const T*>(a.x2.data) + r * a.x2.stride + (c - f1);
-        const Piece p = *reinterpret_cast<const Piece*>(from);
+        const Piece<T> p = *reinterpret_cast<const Piece<T>*>(from);
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] = to_float(p.v[i]);
     } else {
@@ -155,6 +155,7 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(De
     constexpr int MI = WM / 32, NI = WN / 32, kStage = (BM + BN) * 4;
     static_assert((BM + BN) / 16 % kWaves == 0 && BM / 16 % kLoads == 0, "a wave loads whole pieces of one side");
     __shared__ int4v s_stage[3 * kStage];
+    __shared__ float s_scale[BM], s_w_scale[BN], s_bias[BN];
     const int32_t rows = a.count.get(), n = a.out.width;
     const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
     int32_t tm, tn;
@@ -163,6 +164,12 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(De
     const int32_t n0 = tn * BN;
     if (m0 >= rows) return;
     const int32_t steps = (int32_t) (a.stride / kStepBytes);
+    for (int i = (int) threadIdx.x; i < BM; i += kWaves * kWave) s_scale[i] = a.scale[m0 + i < rows ? m0 + i : rows - 1];
+    for (int i = (int) threadIdx.x; i < BN; i += kWaves * kWave) {
+        const int32_t c = n0 + i < n ? n0 + i : n - 1;
+        s_w_scale[i] = a.w_scale[c];
+        s_bias[i] = a.bias ? a.bias[c] : 0.f;
+    }
     // this wave's pieces: 16 rows each, of the rows' side or the weights'; those past the end repeat the last
     const bool weights = wave * kLoads * 16 >= BM;
     const int32_t first = wave * kLoads * 16 - (weights ? BM : 0);
@@ -212,7 +219,7 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(De
         constexpr int kProducts = MI * NI;
 #pragma unroll
         for (int m = 0; m < kProducts; ++m) {
-            acc[m / NI][m % NI] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[h][m / NI], f[h][MI + m % NI], acc[m / NI][m % NI], 0, 0, 0);
+            acc[m / NI][m % NI] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[h][MI + m % NI], f[h][m / NI], acc[m / NI][m % NI], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int o = others * m / kProducts; o < others * (m + 1) / kProducts; ++o) other(o);
@@ -244,30 +251,46 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(De
         turn(1, step + 1);
     }
     if (step < steps) turn(0, step);
-    const bool whole = m0 + BM <= rows && n0 + BN <= n;
+    // Each strip of 32 rows goes through a piece of LDS of the wave's own, so that rows leave in pieces of 16 bytes.
     // (from a lane id the compiler cannot see through: what it would work out of this in front of the loop costs registers)
-    const int e_lane = opaque_lane_id(), e32 = e_lane & 31;
+    constexpr int V = 16 / (int) sizeof(T), kLanes = WN / V, kPitch = WN * (int) sizeof(T) + 16;
+    static_assert(kWaves * 32 * kPitch <= 3 * kStage * 16, "the strips lie in the stages' place");
+    const int e_lane = opaque_lane_id(), e32 = e_lane & 31, four = 4 * (e_lane >> 5);
+    char* const strip = reinterpret_cast<char*>(s_stage) + wave * (32 * kPitch);
+    const int32_t c = n0 + wn + e_lane % kLanes * V;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-        const int64_t r0 = m0 + wm + i * 32 + 4 * (e_lane >> 5);
-        float scale[16];
+        const float scale = s_scale[wm + i * 32 + e32];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int64_t r = r0 + 8 * (v >> 2) + (v & 3);
-            scale[v] = a.scale[r < rows ? r : rows - 1];
-        }
+        for (int j = 0; j < NI; ++j)
 #pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            const int32_t c = n0 + wn + j * 32 + e32, cc = c < n ? c : n - 1;
-            const float w_scale = a.w_scale[cc], bias = a.bias ? a.bias[cc] : 0.f;
-            T* out = reinterpret_cast<T*>(a.out.data) + r0 * a.out.stride + c;
-            __builtin_amdgcn_sched_barrier(0);
+            for (int q = 0; q < 4; ++q) {                     // elements 4 q .. 4 q + 3: four columns of row e32
+                const int at = j * 32 + 8 * q + four;
+                const float4 ws = *reinterpret_cast<const float4*>(s_w_scale + wn + at), b = *reinterpret_cast<const float4*>(s_bias + wn + at);
+                struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
+                y.v[0] = from_float<T>(output_of(acc[i][j][4 * q], ws.x, scale, b.x, a.relu));
+                y.v[1] = from_float<T>(output_of(acc[i][j][4 * q + 1], ws.y, scale, b.y, a.relu));
+                y.v[2] = from_float<T>(output_of(acc[i][j][4 * q + 2], ws.z, scale, b.z, a.relu));
+                y.v[3] = from_float<T>(output_of(acc[i][j][4 * q + 3], ws.w, scale, b.w, a.relu));
+                *reinterpret_cast<Four*>(strip + e32 * kPitch + at * (int) sizeof(T)) = y;
+            }
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const T y = from_float<T>(output_of(acc[i][j][v], w_scale, scale[v], bias, a.relu));
-                if (whole || (r0 + 8 * (v >> 2) + (v & 3) < rows && c < n)) out[(8 * (v >> 2) + (v & 3)) * a.out.stride] = y;
+        for (int t = 0; t < 32 * kLanes / kWave; ++t) {
+            const int row = t * (kWave / kLanes) + e_lane / kLanes;
+            const Piece<T> y = *reinterpret_cast<const Piece<T>*>(strip + row * kPitch + e_lane % kLanes * 16);
+            const int64_t r = m0 + wm + i * 32 + row;
+            if (r >= rows) continue;
+            T* out = reinterpret_cast<T*>(a.out.data) + r * a.out.stride + c;
+            if (c + V <= n) {
+                __builtin_memcpy(out, &y, 16);                // whatever the row's alignment
+            } else {
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (c + k < n) out[k] = y.v[k];
             }
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -383,8 +406,6 @@ constexpr int64_t rows_lds(int64_t stride, int32_t n, int waves)
 {
     return (few_stride(stride) * ((n + 15) / 16 * 16 + waves * 16)) + (int64_t) (n + 15) / 16 * 16 * 8;
 }
-
-template <typename T> struct alignas(16) Piece { T v[kPiece<T>]; };
 
 template <typename T, int L, int P, int kWaves>
 __global__ void __launch_bounds__(kWaves * kWave) k_int8_rows(DenseInt8Args a, QuantizeArgs x)
