@@ -419,18 +419,28 @@ __global__ void __launch_bounds__(kThreads, 2) k_backward_weights(WeightsArgs g)
         g.db[((int64_t) split * g.db_shares + tm) * a.hdim + n0 + n] = (s_sum[n] + s_sum[Tiles::kN + n]) + (s_sum[2 * Tiles::kN + n] + s_sum[3 * Tiles::kN + n]);
 }
 
-// Between the two products: the splits' sums, and W in bf16 terms for dx: [plane][f1 + f2][hdim rounded up to kStageK], zeros
-// behind hdim.  Items of four values; a sum's splits are shared by sixteen threads, since there may be few sums of many splits.
-struct BetweenArgs {
-    const float *dw_parts, *db_parts, *w;     // null: nothing to join; likewise; no dx
-    float *dw, *db;
-    uint16_t* terms;
-    int64_t k;
-    int32_t hdim, pitch, dw_splits, db_splits, planes;
-    int32_t join_blocks;                      // the grid's first; the others cut W
+// ---- sums and terms -------------------------------------------------------------------------------------------------
+// Sums over splits, four at a time; `threads` of a block share one, since there may be few sums of many splits.
+struct JoinArgs {
+    const float* parts;                       // [splits x count]
+    float* out;
+    int64_t count;
+    int32_t splits, threads, blocks;          // blocks 0: nothing to join
 };
 
-constexpr int kJoinItems = 16, kJoinThreads = kBlock / kJoinItems;
+// One launch for what is left to do beside the products: db and dw from their splits, dx from its splits, and W in bf16
+// terms for dx: [plane][f1 + f2][hdim rounded up to kStageK], zeros behind hdim.  Each has so many of the grid's blocks.
+struct BetweenArgs {
+    JoinArgs db, dw;
+    const float* dx_parts;                    // [dx_splits x rows x (f1 + f2)]
+    MutRows dx;
+    RowCount count;
+    int32_t dx_type, dx_splits, dx_blocks;
+    const float* w;
+    uint16_t* terms;
+    int64_t k;
+    int32_t hdim, pitch, planes, term_blocks;
+};
 
 // Values i .. i + 3 of n; marks: they are one read.
 __device__ __forceinline__ float4 load_four(const float* p, int64_t i, int64_t n, bool marks)
@@ -439,48 +449,63 @@ __device__ __forceinline__ float4 load_four(const float* p, int64_t i, int64_t n
     return make_float4(i < n ? p[i] : 0.f, i + 1 < n ? p[i + 1] : 0.f, i + 2 < n ? p[i + 2] : 0.f, i + 3 < n ? p[i + 3] : 0.f);
 }
 
+__device__ __forceinline__ void join_sums(const JoinArgs& a, int32_t block, float4* s_part)
+{
+    const int items = kBlock / a.threads, item = (int) threadIdx.x % items, part = (int) threadIdx.x / items;
+    const int64_t fours = (a.count + 3) / 4;
+    const bool marks = a.count % 4 == 0;
+    for (int64_t i0 = (int64_t) block * items; i0 < fours; i0 += (int64_t) a.blocks * items) {
+        const int64_t i = 4 * (i0 + item);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < a.count) {
+#pragma unroll 8
+            for (int32_t s = part; s < a.splits; s += a.threads) {
+                const float4 p = load_four(a.parts + s * a.count, i, a.count, marks);
+                v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+            }
+        }
+        for (int w = a.threads / 2; w > 0; w /= 2) {
+            __syncthreads();
+            if (part >= w && part < 2 * w) s_part[(part - w) * items + item] = v;
+            __syncthreads();
+            if (part < w) {
+                const float4 p = s_part[part * items + item];
+                v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+            }
+        }
+        if (part == 0 && i < a.count) {
+            a.out[i] = v.x;
+            if (i + 1 < a.count) a.out[i + 1] = v.y;
+            if (i + 2 < a.count) a.out[i + 2] = v.z;
+            if (i + 3 < a.count) a.out[i + 3] = v.w;
+        }
+    }
+}
+
 __global__ void __launch_bounds__(kBlock) k_backward_between(BetweenArgs a)
 {
-    __shared__ float4 s_part[kJoinThreads][kJoinItems];
-    if ((int32_t) blockIdx.x < a.join_blocks) {
-        const int64_t n = a.k * a.hdim, joins = a.dw_parts ? (n + 3) / 4 : 0, all = joins + (a.db_parts ? (a.hdim + 3) / 4 : 0);
-        const int item = (int) threadIdx.x % kJoinItems, part = (int) threadIdx.x / kJoinItems;
-        for (int64_t i0 = (int64_t) blockIdx.x * kJoinItems; i0 < all; i0 += (int64_t) a.join_blocks * kJoinItems) {
-            const bool bias = i0 + item >= joins;
-            const float* parts = bias ? a.db_parts : a.dw_parts;
-            const int64_t i = 4 * (bias ? i0 + item - joins : i0 + item), count = bias ? a.hdim : n;
-            const bool marks = count % 4 == 0;
-            const int32_t splits = bias ? a.db_splits : a.dw_splits;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (i0 + item < all) {
-#pragma unroll 8
-                for (int32_t s = part; s < splits; s += kJoinThreads) {
-                    const float4 p = load_four(parts + s * count, i, count, marks);
-                    v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
-                }
-            }
-            __syncthreads();
-            s_part[part][item] = v;
-            __syncthreads();
-            if (part == 0 && i0 + item < all) {
-#pragma unroll
-                for (int p = 1; p < kJoinThreads; ++p) {
-                    const float4 w = s_part[p][item];
-                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-                }
-                float* out = (bias ? a.db : a.dw) + i;
-                out[0] = v.x;
-                if (i + 1 < count) out[1] = v.y;
-                if (i + 2 < count) out[2] = v.z;
-                if (i + 3 < count) out[3] = v.w;
-            }
+    __shared__ float4 s_part[kBlock / 2];
+    int32_t block = (int32_t) blockIdx.x;
+    if (block < a.db.blocks) return join_sums(a.db, block, s_part);
+    block -= a.db.blocks;
+    if (block < a.dw.blocks) return join_sums(a.dw, block, s_part);
+    block -= a.dw.blocks;
+    if (block < a.dx_blocks) {
+        const uint32_t K = (uint32_t) a.k, all = (uint32_t) max(a.count.get(), 0) * K, each = (uint32_t) a.count.rows * K;
+        for (uint32_t i = (uint32_t) block * kBlock + threadIdx.x; i < all; i += (uint32_t) a.dx_blocks * kBlock) {
+            float v = 0.f;
+#pragma unroll 4
+            for (int32_t s = 0; s < a.dx_splits; ++s) v += a.dx_parts[(uint64_t) s * each + i];
+            const uint32_t r = i / K;
+            if (a.dx_type == GNS_FP32) store_at<float>(a.dx, r, (int32_t) (i - r * K), v);
+            else                       store_at<Bf16>(a.dx, r, (int32_t) (i - r * K), v);
         }
         return;
     }
+    block -= a.dx_blocks;
     const int64_t fours = a.pitch / 4, terms = a.k * fours;
-    const int32_t block = (int32_t) blockIdx.x - a.join_blocks, blocks = (int32_t) gridDim.x - a.join_blocks;
     const bool marks = a.hdim % 4 == 0 && reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
-    for (int64_t t = (int64_t) block * kBlock + threadIdx.x; t < terms; t += (int64_t) blocks * kBlock) {
+    for (int64_t t = (int64_t) block * kBlock + threadIdx.x; t < terms; t += (int64_t) a.term_blocks * kBlock) {
         const int64_t row = t / fours, c = (t - row * fours) * 4;
         const float4 four = load_four(a.w + row * a.hdim, c, a.hdim, marks);
         float v[4] = {four.x, four.y, four.z, four.w};
@@ -500,8 +525,32 @@ __global__ void __launch_bounds__(kBlock) k_backward_between(BetweenArgs a)
 struct InputArgs {
     BackwardArgs a;
     int32_t m_tiles, n_tiles, pitch;
+    int32_t splits;                           // of hdim
     const uint16_t* w;                        // planes of k_backward_between
+    float* parts;                             // [splits x rows x (f1 + f2)], if there are splits
 };
+
+// Eight values from wherever they begin: the reads need no marks.
+template <int N>
+__device__ __forceinline__ void load_words(const void* from, uint32_t (&to)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N / 4; ++j) {
+        Chunk v;
+        __builtin_memcpy(&v, static_cast<const char*>(from) + 16 * j, 16);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) to[4 * j + k] = v[k];
+    }
+}
+
+// The columns of a step that count, for a thread that reads eight of them from column n on, but none past the last: where a row
+// ends inside, it reads the row's last eight, and of those the last `inside` count.
+__device__ __forceinline__ uint32_t columns_kept(int32_t inside)
+{
+    return inside >= 8 ? 0xFFu : inside > 0 ? 0xFFu << (8 - inside) & 0xFFu : 0u;
+}
+// and those that are left of them by a mask's bits from column n on
+__device__ __forceinline__ uint32_t columns_left(uint32_t kept, uint32_t bits) { return kept & bits << ((__ffs((int) kept) - 1) & 31); }
 
 template <typename T, int kThreads> struct InputTile;
 template <> struct InputTile<float, 512> { typedef Tile<128, 128, 64, 32, 3, 3> Type; };
@@ -509,9 +558,10 @@ template <> struct InputTile<float, 256> { typedef Tile<64, 64, 32, 32, 3, 3> Ty
 template <> struct InputTile<Bf16, 512> { typedef Tile<256, 128, 64, 64, 1, 2> Type; };
 template <> struct InputTile<Bf16, 256> { typedef Tile<128, 128, 64, 64, 1, 2> Type; };
 
-// A thread reads eight columns of a row of dz (of two rows of bf16), and as many of W's planes.  kWhole: rows of dz begin at
-// 16-byte marks and hdim is a multiple of eight, so eight columns are one or two reads; else they are read singly.  Columns
-// past the last are read as the last ones: W's planes are zero there.  A block goes through tiles, `stride` apart.
+// A thread reads eight columns of a row of dz (of two rows of bf16), and as many of W's planes.  kWhole: hdim is a multiple of
+// eight.  Chunks past the last are read as the last: W's planes are zero there.  Else a row's last chunk is its last eight
+// columns, for dz as for W, and those that the chunk before has are left out of dz.  hdim is eight at least.
+// A block goes through tiles, `stride` apart, or has a split of one tile's hdim.
 // kPlain: W is read as it is and cut here, by every block that needs it, which where there is no more than a block or two per
 // CU costs less than a launch and a trip through memory in front.
 template <typename T, int kThreads, bool kMask, bool kWhole, bool kPlain>
@@ -521,13 +571,14 @@ struct InputSource {
     static constexpr int kPlanes = kFloat ? 3 : 2, kStep = kThreads / 4;                            // rows the threads cover at once
     static constexpr int kRowsA = Tiles::kM / kStep, kRowsB = Tiles::kN / kStep, kWords = kFloat ? 8 : 4;
     static constexpr int kSets = (kFloat ? kPlain : kThreads == 512) ? 4 : 2, kReadsB = kPlain ? 1 : kPlanes;
+    static constexpr bool kKeeps = kMask || !kWhole;          // dz has columns left out
     static constexpr int kFetches = kRowsA * (1 + (kMask ? 1 : 0)) + kRowsB * kReadsB;
-    static constexpr int kPutsA = (kMask ? 1 : 0) + (kFloat ? 3 : 1), kPuts = kRowsA * kPutsA + kRowsB * kPlanes;
+    static constexpr int kPutsA = (kKeeps ? 1 : 0) + (kFloat ? 3 : 1), kPuts = kRowsA * kPutsA + kRowsB * kPlanes;
 
     const InputArgs& g;
     Chunk* const lds;
     const int64_t rows, K;
-    const int32_t m_tiles, stride, columns;   // columns: hdim rounded up to whole turns of kSets steps
+    const int32_t m_tiles, stride, begin, end;          // begin, end: of the columns, in whole turns of kSets steps
     int32_t t, n0;                            // tile and first column of the next step
     int row, chunk;
     const char* z[kRowsA];                    // this thread's rows of dz
@@ -540,9 +591,14 @@ struct InputSource {
     Chunk planes[kSets][kRowsB][kPlain ? 1 : kPlanes];
     uint32_t plain[kSets][kRowsB][kPlain ? 8 : 1];
 
-    __device__ __forceinline__ InputSource(const InputArgs& args, Chunk* stages, int64_t rows_, int32_t tiles_, int32_t first, int32_t stride_)
+    static constexpr int kTurn = kStageK * kSets;
+    static __device__ __forceinline__ int32_t turns_before(int32_t hdim, int32_t split, int32_t splits)
+    {
+        return (int32_t) ((int64_t) ((hdim + kTurn - 1) / kTurn) * split / splits);
+    }
+    __device__ __forceinline__ InputSource(const InputArgs& args, Chunk* stages, int64_t rows_, int32_t tiles_, int32_t first, int32_t stride_, int32_t split)
         : g(args), lds(stages), rows(rows_), K(args.a.x1.width + args.a.x2.width), m_tiles(tiles_), stride(stride_),
-          columns((args.a.hdim + kStageK * kSets - 1) / (kStageK * kSets) * (kStageK * kSets)), t(first), n0(0)
+          begin(turns_before(args.a.hdim, split, args.splits) * kTurn), end(turns_before(args.a.hdim, split + 1, args.splits) * kTurn), t(first), n0(begin)
     {
         row = (int) threadIdx.x >> 2;
         chunk = (int) threadIdx.x & 3;
@@ -566,68 +622,34 @@ struct InputSource {
 #pragma unroll
         for (int i = 0; i < kRowsB; ++i) {
             const uint32_t k = (uint32_t) min((int64_t) row + i * kStep, K - 1 - k0);
-            w_at[i] = kPlain ? k * (uint32_t) a.hdim * 4u : k * (uint32_t) g.pitch * 2u + (uint32_t) chunk * 16u;
+            w_at[i] = kPlain ? k * (uint32_t) a.hdim * 4u : k * (uint32_t) g.pitch * 2u + (kWhole ? (uint32_t) chunk * 16u : 0u);
         }
     }
     __device__ __forceinline__ void seek(int set)
     {
-        if (n0 >= columns) {
-            n0 = 0;
+        if (n0 >= end) {
+            n0 = begin;
             t += stride;
             begin_tile();
         }
         const int32_t hdim = g.a.hdim, at = n0 < g.pitch ? n0 : g.pitch - kStageK;       // steps that only fill a turn read the last again
         n = n0 + chunk * 8;
-        if constexpr (kWhole) n = min(n, hdim - 8);
-        if constexpr (kMask || kPlain) {
-            const int32_t inside = hdim - n0 - chunk * 8;     // of the eight columns
-            keep[set] = inside >= 8 ? 0xFFu : inside > 0 ? (1u << inside) - 1u : 0u;
-        } else {
-            keep[set] = n0 < g.pitch ? 1u : 0u;               // wave-uniform
-        }
+        if constexpr (kKeeps || kPlain) keep[set] = columns_kept(hdim - n);
+        else                            keep[set] = n0 < g.pitch ? 1u : 0u;               // wave-uniform
+        n = min(n, hdim - 8);
         word = at >> 5;
-        w_step = (int64_t) at * 2;
+        w_step = kWhole ? (int64_t) at * 2 : 0;
         n0 += kStageK;
     }
     __device__ __forceinline__ void fetch(int set, int i)
     {
-        const int32_t hdim = g.a.hdim;
         if (i < kRowsA) {
-            if constexpr (kWhole) {
-                const Chunk* from = reinterpret_cast<const Chunk*>(z[i] + (uint64_t) ((uint32_t) n * (uint32_t) sizeof(T)));
-#pragma unroll
-                for (int j = 0; j < kWords / 4; ++j) {
-                    const Chunk v = from[j];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) d[set][i][4 * j + k] = v[k];
-                }
-            } else if constexpr (kFloat) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[set][i][j] = reinterpret_cast<const uint32_t*>(z[i])[min(n + j, hdim - 1)];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint16_t* from = reinterpret_cast<const uint16_t*>(z[i]);
-                    d[set][i][j] = from[min(n + 2 * j, hdim - 1)] | (uint32_t) from[min(n + 2 * j + 1, hdim - 1)] << 16;
-                }
-            }
+            load_words(z[i] + (uint64_t) ((uint32_t) n * (uint32_t) sizeof(T)), d[set][i]);
         } else if (kPlain && i < kRowsA + kRowsB) {
-            const int b = i - kRowsA;
-            const float* from = reinterpret_cast<const float*>(w + w_at[b]);
-            if constexpr (kWhole) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const Chunk v = *reinterpret_cast<const Chunk*>(from + n + 4 * j);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) plain[set][b][4 * j + k] = v[k];
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) plain[set][b][j] = __float_as_uint(from[min(n + j, hdim - 1)]);
-            }
+            if constexpr (kPlain) load_words(w + ((uint64_t) w_at[i - kRowsA] + (uint32_t) n * 4u), plain[set][i - kRowsA]);
         } else if (i < kRowsA + kRowsB * kReadsB) {
             const int b = (i - kRowsA) / kPlanes, p = (i - kRowsA) % kPlanes;
-            planes[set][b][p] = *reinterpret_cast<const Chunk*>(w + (w_step + p * K * g.pitch * 2) + w_at[b]);
+            __builtin_memcpy(&planes[set][b][p], __builtin_assume_aligned(w + (w_step + p * K * g.pitch * 2) + (w_at[b] + (kWhole ? 0u : (uint32_t) n * 2u)), kWhole ? 16 : 2), 16);
         } else {
             const int b = i - kRowsA - kRowsB * kReadsB;
             words[set][b] = m[b][word];
@@ -640,21 +662,21 @@ struct InputSource {
             const int b = (i - kRowsA * kPutsA) / kPlanes, p = (i - kRowsA * kPutsA) % kPlanes;
             if constexpr (kPlain) {
                 uint32_t (&v)[8] = plain[set][b];
-                if (p == 0) {
+                if (p == 0 && !kKeeps) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] &= kWhole ? (keep[set] ? ~0u : 0u) : spread_bit(keep[set], j);
+                    for (int j = 0; j < 8; ++j) v[j] &= keep[set] ? ~0u : 0u;
                 }
                 to[Tiles::place_b(p, row + b * kStep, chunk)] = take_terms(v);
             } else {
                 Chunk v = planes[set][b][p];
-                if (!kMask) v = keep[set] ? v : Chunk{0, 0, 0, 0};
+                if (!kKeeps) v = keep[set] ? v : Chunk{0, 0, 0, 0};
                 to[Tiles::place_b(p, row + b * kStep, chunk)] = v;
             }
             return;
         }
-        const int b = i / kPutsA, u = i % kPutsA - (kMask ? 1 : 0);
-        if (u < 0) {                                          // what the mask leaves
-            const uint32_t k8 = keep[set] & words[set][b] >> (chunk * 8);
+        const int b = i / kPutsA, u = i % kPutsA - (kKeeps ? 1 : 0);
+        if (u < 0) {                                          // what is left of the columns
+            const uint32_t k8 = kMask ? columns_left(keep[set], words[set][b] >> (chunk * 8)) : keep[set];
             if constexpr (kFloat) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[set][b][j] &= spread_bit(k8, j);
@@ -679,21 +701,34 @@ __global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
     const BackwardArgs& a = g.a;
     const int64_t rows = a.count.get();
     if (rows <= 0) return;
-    // a block's tiles: of those that have rows, every gridDim.x-th of its XCD's
-    const int32_t m_tiles = (int32_t) ((rows + Tiles::kM - 1) / Tiles::kM), all = m_tiles * g.n_tiles, first = xcd_run((int32_t) blockIdx.x, (int32_t) gridDim.x);
-    const int32_t tiles = first < all ? (all - first + (int32_t) gridDim.x - 1) / (int32_t) gridDim.x : 0;
+    // a block's tiles: of those that have rows, every `stride`-th of its XCD's; where hdim is split, a split of one
+    const int32_t blocks = (int32_t) gridDim.x, stride = kPlain ? blocks / g.splits : blocks, at = xcd_run((int32_t) blockIdx.x, blocks);
+    const int32_t split = kPlain ? at / stride : 0, first = kPlain ? at - split * stride : at;
+    const int32_t m_tiles = (int32_t) ((rows + Tiles::kM - 1) / Tiles::kM), all = m_tiles * g.n_tiles;
+    const int32_t tiles = first < all ? (all - first + stride - 1) / stride : 0;
     if (tiles == 0) return;
     Tiles tile(s_stage);
-    Source source(g, s_stage, rows, m_tiles, first, (int32_t) gridDim.x);
+    Source source(g, s_stage, rows, m_tiles, first, stride, split);
     const int32_t K = a.x1.width + a.x2.width;
     T* out = reinterpret_cast<T*>(a.dx.data);
-    tile.run(source, source.columns / kStageK, tiles, [&](int32_t i) {
+    tile.run(source, (source.end - source.begin) / kStageK, tiles, [&](int32_t i) {
         int32_t tm, tn;
-        tile_of(first + i * (int32_t) gridDim.x, m_tiles, g.n_tiles, &tm, &tn);
+        tile_of(first + i * stride, m_tiles, g.n_tiles, &tm, &tn);
         const int64_t r0 = (int64_t) tm * Tiles::kM;
         const int32_t k0 = tn * Tiles::kN;
         const int lane = opaque_lane_id(), m0 = Tiles::first_row(lane), n = Tiles::first_column(lane);
         const bool whole = r0 + Tiles::kM <= rows && k0 + Tiles::kN <= K;
+        if (kPlain && g.parts) {
+            float* part = g.parts + ((int64_t) split * a.count.rows + r0 + m0) * K + k0 + n;
+#pragma unroll
+            for (int i = 0; i < Tiles::MI; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+#pragma unroll
+                    for (int j = 0; j < Tiles::NI; ++j)
+                        if (whole || (r0 + m0 + Tiles::row_step(i, v) < rows && k0 + n + 32 * j < K)) part[(int64_t) Tiles::row_step(i, v) * K + 32 * j] = tile.acc[i][j][v];
+            return;
+        }
         T* first = out + (r0 + m0) * a.dx.stride + k0 + n;
 #pragma unroll
         for (int i = 0; i < Tiles::MI; ++i)
@@ -713,7 +748,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
 constexpr int kFewBlock = 512, kFewWaves = kFewBlock / kWave, kFewColumns = 16;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-template <typename T, int MT, bool kMask, bool kWhole>
+template <typename T, int MT, bool kMask>
 __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
 {
     constexpr bool kFloat = sizeof(T) == 4;
@@ -738,37 +773,10 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
     uint32_t wv[kSets][8], zv[kSets][MT][kFloat ? 8 : 4], words[kSets][MT];
     auto fetch = [&](int set, int32_t step) {                 // steps past the wave's last read that one again
         step = min(step, s1 - 1);
-        const int32_t n = step * 32 + kg * 8;
-        if constexpr (kWhole) {
-            const int32_t at = min(n, hdim - 8);
+        const int32_t n = min(step * 32 + kg * 8, hdim - 8);
+        load_words(w + n, wv[set]);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const Chunk v = *reinterpret_cast<const Chunk*>(w + at + 4 * j);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) wv[set][4 * j + k] = v[k];
-            }
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int j = 0; j < (kFloat ? 2 : 1); ++j) {
-                    const Chunk v = *reinterpret_cast<const Chunk*>(z[t] + at + 4 * j);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) zv[set][t][4 * j + k] = v[k];
-                }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) wv[set][j] = __float_as_uint(w[min(n + j, hdim - 1)]);
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                if constexpr (kFloat) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) zv[set][t][j] = __float_as_uint(z[t][min(n + j, hdim - 1)]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) zv[set][t][j] = z[t][min(n + 2 * j, hdim - 1)].bits | (uint32_t) z[t][min(n + 2 * j + 1, hdim - 1)].bits << 16;
-                }
-            }
-        }
+        for (int t = 0; t < MT; ++t) load_words(z[t] + n, zv[set][t]);
         if constexpr (kMask) {
 #pragma unroll
             for (int t = 0; t < MT; ++t) words[set][t] = m[t][step];
@@ -778,8 +786,7 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
     auto multiply = [&](int set, int32_t step) {
-        const int32_t inside = hdim - step * 32 - kg * 8;     // of the eight columns
-        const uint32_t keep = inside >= 8 ? 0xFFu : inside > 0 ? (1u << inside) - 1u : 0u;
+        const uint32_t keep = columns_kept(hdim - step * 32 - kg * 8);
         Chunk wt[kTermsB];
 #pragma unroll
         for (int j = 0; j < 8; ++j) wv[set][j] &= spread_bit(keep, j);
@@ -787,7 +794,7 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
         for (int k = 0; k < kTermsB; ++k) wt[k] = take_terms(wv[set]);
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            const uint32_t k8 = kMask ? keep & words[set][t] >> (kg * 8) : keep;
+            const uint32_t k8 = kMask ? columns_left(keep, words[set][t] >> (kg * 8)) : keep;
             Chunk zt[kTermsA];
             if constexpr (kFloat) {
 #pragma unroll
@@ -828,6 +835,52 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
 #pragma unroll
         for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][t][v][l];
         store_at<T>(a.dx, r, k, sum);
+    }
+}
+
+// k_backward_narrow: dx of fewer than eight columns of dz, by as many multiplications each, in fp32.  A lane has four columns of
+// dx, whose rows of W stay in registers, and rows one after the other; 2^lanes_log2 lanes have a row.  Bound by the bytes of dx.
+constexpr int kNarrow = 8, kNarrowRows = 16;  // rows of a lane
+template <typename T, bool kMask>
+__global__ void __launch_bounds__(kBlock) k_backward_narrow(BackwardArgs a, int32_t lanes_log2)
+{
+    const int32_t rows = a.count.get(), K = a.x1.width + a.x2.width, hdim = a.hdim;
+    const int32_t per_wave = kWave >> lanes_log2, each = per_wave * kNarrowRows, lane = lane_id(), chunks = (K + (4 << lanes_log2) - 1) / (4 << lanes_log2);
+    const int64_t work = ((int64_t) rows + each - 1) / each * chunks;
+    for (int64_t i = (int64_t) blockIdx.x * (kBlock / kWave) + __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)); i < work;
+         i += (int64_t) gridDim.x * (kBlock / kWave)) {
+        const int64_t group = i / chunks, r0 = group * each + (lane >> lanes_log2);
+        const int32_t k = ((int32_t) (i - group * chunks) << lanes_log2) * 4 + (lane & ((1 << lanes_log2) - 1)) * 4;
+        float w[4][kNarrow - 1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int n = 0; n < kNarrow - 1; ++n) w[j][n] = n < hdim ? a.w[(int64_t) min(k + j, K - 1) * hdim + n] : 0.f;
+#pragma unroll 4
+        for (int t = 0; t < kNarrowRows; ++t) {
+            const int64_t row = r0 + t * per_wave, r = row < rows ? row : rows - 1;
+            const uint32_t keep = kMask ? a.positive[r] : ~0u;
+            float z[kNarrow - 1];
+#pragma unroll
+            for (int n = 0; n < kNarrow - 1; ++n) z[n] = load_at<T>(a.d_out, r, n < hdim ? n : 0);
+            struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float sum = 0.f;
+#pragma unroll
+                for (int n = 0; n < kNarrow - 1; ++n) sum = n < hdim && (keep >> n & 1u) ? fmaf(z[n], w[j][n], sum) : sum;
+                y.v[j] = from_float<T>(sum);
+            }
+            if (row >= rows || k >= K) continue;
+            T* out = reinterpret_cast<T*>(a.dx.data) + r * a.dx.stride + k;
+            if (k + 4 <= K) {
+                __builtin_memcpy(out, &y, sizeof(y));         // whatever the row's alignment
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (k + j < K) out[j] = y.v[j];
+            }
+        }
     }
 }
 
@@ -875,18 +928,6 @@ static WeightsPlan plan_weights(const gns_ctx* c, int32_t f1, int32_t f2, int32_
     return plan(false);
 }
 
-size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows)
-{
-    const size_t k = (size_t) f1 + (size_t) f2, pitch = ((size_t) hdim + kStageK - 1) / kStageK * kStageK;
-    size_t parts = 0;
-    for (int i = 0; i < 3; ++i) {                              // of either type, and of bf16 columns read singly
-        const WeightsPlan p = plan_weights(c, f1, f2, hdim, rows, i == 0, i < 2);
-        const size_t need = (p.splits > 1 ? align256((size_t) p.splits * k * (size_t) hdim * 4) : 0) + align256((size_t) p.splits * (size_t) p.db_shares * (size_t) hdim * 4);
-        if (need > parts) parts = need;
-    }
-    return parts + align256(3 * k * pitch * 2);
-}
-
 // A grid's blocks times their threads stay below 2^32.
 static bool too_many(int64_t blocks, int threads) { return blocks * threads >= (int64_t) 1 << 32; }
 
@@ -917,14 +958,23 @@ static int64_t input_tiles(const BackwardArgs& a, int32_t* m_tiles, int32_t* n_t
     return (int64_t) *m_tiles * *n_tiles;
 }
 
+// Splits of hdim for dx where its tiles are few: those that fill the chip, of four turns at least, and one more launch joins them
+// (or the one that joins dw's splits anyway).  fp32, 1104 rows of 128 x 2048: 15 us, 37 unsplit.
+template <typename T>
+static int32_t input_splits(const gns_ctx* c, int64_t tiles, int32_t hdim)
+{
+    constexpr int32_t kLeast = 4 * kStageK * (sizeof(T) == 4 ? 4 : 2);
+    const int64_t s = min((int64_t) c->num_cus / max(tiles, (int64_t) 1), (int64_t) hdim / kLeast);
+    return s < 2 ? 1 : (int32_t) s;
+}
+
 template <typename T, int kThreads, bool kPlain>
 static hipError_t launch_input(const gns_ctx* c, InputArgs g, hipStream_t s)
 {
     const int64_t tiles = input_tiles<T, kThreads>(g.a, &g.m_tiles, &g.n_tiles), most = (int64_t) c->num_cus * (kThreads == 512 ? 1 : 2);
     if (tiles >= (int64_t) 1 << 30) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned) (tiles < most ? tiles : most)), block(kThreads);
-    const bool whole = g.a.hdim % 8 == 0 && reinterpret_cast<uintptr_t>(g.a.d_out.data) % 16 == 0 && (uint64_t) g.a.d_out.stride * sizeof(T) % 16 == 0 &&
-                       (!kPlain || reinterpret_cast<uintptr_t>(g.a.w) % 16 == 0);
+    const dim3 grid((unsigned) (kPlain ? tiles * g.splits : tiles < most ? tiles : most)), block(kThreads);
+    const bool whole = g.a.hdim % 8 == 0;
     if (g.a.positive && whole)  hipLaunchKernelGGL((k_backward_input<T, kThreads, true, true, kPlain>), grid, block, 0, s, g);
     else if (g.a.positive)      hipLaunchKernelGGL((k_backward_input<T, kThreads, true, false, kPlain>), grid, block, 0, s, g);
     else if (whole)             hipLaunchKernelGGL((k_backward_input<T, kThreads, false, true, kPlain>), grid, block, 0, s, g);
@@ -938,13 +988,66 @@ template <typename T, int MT>
 static hipError_t launch_few(const BackwardArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned) ((a.x1.width + a.x2.width + kFewColumns - 1) / kFewColumns)), block(kFewBlock);
-    const bool whole = a.hdim % 8 == 0 && reinterpret_cast<uintptr_t>(a.d_out.data) % 16 == 0 && (uint64_t) a.d_out.stride * sizeof(T) % 16 == 0 &&
-                       reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
-    if (a.positive && whole) hipLaunchKernelGGL((k_backward_few<T, MT, true, true>), grid, block, 0, s, a);
-    else if (a.positive)     hipLaunchKernelGGL((k_backward_few<T, MT, true, false>), grid, block, 0, s, a);
-    else if (whole)          hipLaunchKernelGGL((k_backward_few<T, MT, false, true>), grid, block, 0, s, a);
-    else                     hipLaunchKernelGGL((k_backward_few<T, MT, false, false>), grid, block, 0, s, a);
+    if (a.positive) hipLaunchKernelGGL((k_backward_few<T, MT, true>), grid, block, 0, s, a);
+    else            hipLaunchKernelGGL((k_backward_few<T, MT, false>), grid, block, 0, s, a);
     return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_narrow(const gns_ctx* c, const BackwardArgs& a, hipStream_t s)
+{
+    const int32_t K = a.x1.width + a.x2.width;
+    int32_t lanes_log2 = 0;
+    while (lanes_log2 < 6 && (4 << lanes_log2) < K) ++lanes_log2;
+    const int64_t each = (int64_t) (kWave >> lanes_log2) * kNarrowRows, chunks = (K + (4 << lanes_log2) - 1) / (4 << lanes_log2);
+    const dim3 grid(grid_of(c, ((int64_t) a.count.rows + each - 1) / each * chunks * kWave)), block(kBlock);
+    if (a.positive) hipLaunchKernelGGL((k_backward_narrow<T, true>), grid, block, 0, s, a, lanes_log2);
+    else            hipLaunchKernelGGL((k_backward_narrow<T, false>), grid, block, 0, s, a, lanes_log2);
+    return hipGetLastError();
+}
+
+// How a call's dx is made.
+enum class Way { kNarrow, kFew, kPlain, kCut, kWide };
+struct InputPlan {
+    Way way;
+    int32_t splits;
+};
+// Blocks of 512 threads where they fill half the chip and layers are not too narrow for them (fp32, dw too, 2400 rows of 1000 x 1000:
+// 78 us, 99 with 256 threads; 600 rows of 4096 x 4096: 237 and 338; with less than half 1400 rows: no difference, bf16 3000: 81
+// and 73).  Else of 256, and with no more of them than CUs W is read as it is.
+template <typename T>
+static InputPlan plan_input(const gns_ctx* c, const BackwardArgs& a)
+{
+    typedef typename InputTile<T, 512>::Type Wide;
+    int32_t m_tiles, n_tiles;
+    if (a.hdim < kNarrow) return {Way::kNarrow, 1};
+    if (a.count.rows <= kFewRows) return {Way::kFew, 1};
+    if (input_tiles<T, 512>(a, &m_tiles, &n_tiles) * 2 >= c->num_cus && a.x1.width + a.x2.width > Wide::kN / 2) return {Way::kWide, 1};
+    const int64_t tiles = input_tiles<T, 256>(a, &m_tiles, &n_tiles);
+    return tiles <= c->num_cus ? InputPlan{Way::kPlain, input_splits<T>(c, tiles, a.hdim)} : InputPlan{Way::kCut, 1};
+}
+
+size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows)
+{
+    const size_t k = (size_t) f1 + (size_t) f2, pitch = ((size_t) hdim + kStageK - 1) / kStageK * kStageK;
+    size_t parts = 0;
+    for (int i = 0; i < 3; ++i) {                              // of either type, and of bf16 columns read singly
+        const WeightsPlan p = plan_weights(c, f1, f2, hdim, rows, i == 0, i < 2);
+        const size_t need = (p.splits > 1 ? align256((size_t) p.splits * k * (size_t) hdim * 4) : 0) + align256((size_t) p.splits * (size_t) p.db_shares * (size_t) hdim * 4);
+        if (need > parts) parts = need;
+    }
+    BackwardArgs a = {};
+    a.x1.width = f1; a.x2.width = f2; a.hdim = hdim; a.count.rows = rows;
+    const int32_t splits = max(plan_input<float>(c, a).splits, plan_input<Bf16>(c, a).splits);
+    return parts + max(align256(3 * k * pitch * 2), splits > 1 ? align256((size_t) splits * (size_t) rows * k * 4) : 0);
+}
+
+// Threads that share a sum: all sums' first reads should be on their way at once.
+static JoinArgs join_of(const gns_ctx* c, const float* parts, float* out, int64_t count, int32_t splits)
+{
+    const int64_t fours = (count + 3) / 4;
+    const int32_t threads = splits <= 8 ? 1 : fours * 16 > (int64_t) c->num_cus * kBlock ? 16 : 64;
+    return {parts, out, count, splits, threads, (int32_t) grid_of(c, fours * threads)};
 }
 
 template <typename T>
@@ -954,44 +1057,52 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     const int32_t K = a.x1.width + a.x2.width;
     const int64_t pitch = ((int64_t) a.hdim + kStageK - 1) / kStageK * kStageK;
     char* at = static_cast<char*>(a.workspace);
-    const bool dx = a.dx.data && a.count.rows;
     BetweenArgs b = {};
-    b.k = K; b.hdim = a.hdim; b.pitch = (int32_t) pitch; b.planes = kFloat ? 3 : 2;
+    b.k = K;
     if (a.dw) {
         const WeightsPlan p = plan_weights(c, a.x1.width, a.x2.width, a.hdim, a.count.rows, kFloat, kFloat || reads_pairs(a.d_out));
         WeightsArgs g = {a, p.m_tiles, p.n_tiles, p.splits, p.db_shares, a.dw, a.db};
-        b.dw = a.dw; b.db = a.db;
-        b.dw_splits = p.splits;
-        b.db_splits = p.splits * p.db_shares;
         if (p.splits > 1) {
-            b.dw_parts = g.dw = reinterpret_cast<float*>(at);
+            g.dw = reinterpret_cast<float*>(at);
             at += align256((size_t) p.splits * (size_t) K * (size_t) a.hdim * 4);
+            b.dw = join_of(c, g.dw, a.dw, (int64_t) K * a.hdim, p.splits);
         }
-        if (a.db && b.db_splits > 1) {
-            b.db_parts = g.db = reinterpret_cast<float*>(at);
-            at += align256((size_t) b.db_splits * (size_t) a.hdim * 4);
+        if (a.db && p.splits * p.db_shares > 1) {
+            g.db = reinterpret_cast<float*>(at);
+            at += align256((size_t) p.splits * (size_t) p.db_shares * (size_t) a.hdim * 4);
+            b.db = join_of(c, g.db, a.db, a.hdim, p.splits * p.db_shares);
         }
         const hipError_t e = p.wide ? launch_weights<T, 512>(g, s) : launch_weights<T, 256>(g, s);
         if (e != hipSuccess) return e;
     }
-    // Blocks of 512 threads where they fill the chip and layers are not too narrow for them; else of 256, and with no more than
-    // those that run together W is read as it is.
-    typedef typename InputTile<T, 512>::Type Wide;
-    int32_t m_tiles, n_tiles;
-    const bool wide = input_tiles<T, 512>(a, &m_tiles, &n_tiles) >= c->num_cus && K > Wide::kN / 2;
-    const bool plain = !wide && input_tiles<T, 256>(a, &m_tiles, &n_tiles) <= c->num_cus, few = a.count.rows <= kFewRows;
-    if (dx && !plain && !few) {
+    const bool dx = a.dx.data && a.count.rows;
+    const InputPlan p = dx ? plan_input<T>(c, a) : InputPlan{Way::kFew, 1};
+    if (dx && (p.way == Way::kCut || p.way == Way::kWide)) {
         b.w = a.w;
         b.terms = reinterpret_cast<uint16_t*>(at);
+        b.hdim = a.hdim; b.pitch = (int32_t) pitch; b.planes = kFloat ? 3 : 2;
+        b.term_blocks = (int32_t) grid_of(c, K * (pitch / 4));
     }
-    const int64_t joins = (b.dw_parts ? ((int64_t) K * a.hdim + 3) / 4 : 0) + (b.db_parts ? (a.hdim + 3) / 4 : 0);
-    b.join_blocks = joins ? (int32_t) grid_of(c, joins * kJoinThreads) : 0;
-    const int32_t term_blocks = b.w ? (int32_t) grid_of(c, K * (pitch / 4)) : 0;
-    if (b.join_blocks + term_blocks) hipLaunchKernelGGL(k_backward_between, dim3((unsigned) (b.join_blocks + term_blocks)), dim3(kBlock), 0, s, b);
-    if (!dx) return hipGetLastError();
-    if (few) return a.count.rows <= 16 ? launch_few<T, 1>(a, s) : launch_few<T, 4>(a, s);
-    InputArgs g = {a, 0, 0, (int32_t) pitch, b.terms};
-    return wide ? launch_input<T, 512, false>(c, g, s) : plain ? launch_input<T, 256, true>(c, g, s) : launch_input<T, 256, false>(c, g, s);
+    InputArgs g = {a, 0, 0, (int32_t) pitch, p.splits, b.terms, nullptr};
+    if (p.splits > 1) {
+        b.dx_parts = g.parts = reinterpret_cast<float*>(at);
+        b.dx = a.dx; b.count = a.count;
+        b.dx_type = kFloat ? GNS_FP32 : GNS_BF16;
+        b.dx_splits = p.splits;
+        b.dx_blocks = (int32_t) grid_of(c, (int64_t) a.count.rows * K);
+        const hipError_t e = launch_input<T, 256, true>(c, g, s);             // in front of the sums
+        if (e != hipSuccess) return e;
+    }
+    const int32_t blocks = b.db.blocks + b.dw.blocks + b.dx_blocks + b.term_blocks;
+    if (blocks) hipLaunchKernelGGL(k_backward_between, dim3((unsigned) blocks), dim3(kBlock), 0, s, b);
+    if (!dx || p.splits > 1) return hipGetLastError();
+    switch (p.way) {
+    case Way::kNarrow: return launch_narrow<T>(c, a, s);
+    case Way::kFew:    return a.count.rows <= 16 ? launch_few<T, 1>(a, s) : launch_few<T, 4>(a, s);
+    case Way::kPlain:  return launch_input<T, 256, true>(c, g, s);
+    case Way::kCut:    return launch_input<T, 256, false>(c, g, s);
+    default:           return launch_input<T, 512, false>(c, g, s);
+    }
 }
 
 hipError_t launch_backward(const gns_ctx* c, const BackwardArgs& a, int32_t type, hipStream_t s)
