@@ -10,7 +10,6 @@ namespace gns {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef uint32_t Chunk __attribute__((ext_vector_type(4)));        // eight values of bf16 (a struct of four words would not stay in registers)
 
 // Upper halves of two words, a's in the lower half.
 __device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
@@ -530,19 +529,6 @@ struct InputArgs {
     float* parts;                             // [splits x rows x (f1 + f2)], if there are splits
 };
 
-// Eight values from wherever they begin: the reads need no marks.
-template <int N>
-__device__ __forceinline__ void load_words(const void* from, uint32_t (&to)[N])
-{
-#pragma unroll
-    for (int j = 0; j < N / 4; ++j) {
-        Chunk v;
-        __builtin_memcpy(&v, static_cast<const char*>(from) + 16 * j, 16);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) to[4 * j + k] = v[k];
-    }
-}
-
 // The columns of a step that count, for a thread that reads eight of them from column n on, but none past the last: where a row
 // ends inside, it reads the row's last eight, and of those the last `inside` count.
 __device__ __forceinline__ uint32_t columns_kept(int32_t inside)
@@ -874,7 +860,9 @@ __global__ void __launch_bounds__(kBlock) k_backward_narrow(BackwardArgs a, int3
             if (row >= rows || k >= K) continue;
             T* out = reinterpret_cast<T*>(a.dx.data) + r * a.dx.stride + k;
             if (k + 4 <= K) {
-                __builtin_memcpy(out, &y, sizeof(y));         // whatever the row's alignment
+                typedef uint32_t Word __attribute__((ext_vector_type(sizeof(T))));
+                const Word v = __builtin_bit_cast(Word, y);
+                __builtin_memcpy(out, &v, sizeof(v));         // whatever the row's alignment
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)

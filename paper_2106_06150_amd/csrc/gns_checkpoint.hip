@@ -28,9 +28,8 @@ __device__ __forceinline__ uint32_t step_of(float x, float inverse)
 }
 
 // Four lanes a group, eight consecutive values each (two pieces of 16 bytes of fp32, one of bf16), sixteen groups a wave.
-// kAligned: every row begins at a 16-byte mark, so a lane's values are pieces; else, and where a row ends inside, they are
-// read singly.
-template <typename T, bool kAligned>
+// A lane's values are pieces whatever the row's alignment; where a row ends inside, they are read singly.
+template <typename T>
 __global__ void __launch_bounds__(kBlock) k_checkpoint_save(CheckpointArgs a)
 {
     const int64_t total = (int64_t) a.count.get() * a.groups;
@@ -43,11 +42,11 @@ __global__ void __launch_bounds__(kBlock) k_checkpoint_save(CheckpointArgs a)
         const int32_t col = (int32_t) (gc - r * a.groups) * 32 + (lane & 3) * 8;
         const T* row = reinterpret_cast<const T*>(a.x.data) + r * a.x.stride;
         float x[8];
-        if (kAligned && col + 8 <= a.width) {
-            struct alignas(16) Eight { T v[8]; };
-            const Eight v = *reinterpret_cast<const Eight*>(row + col);
+        if (col + 8 <= a.width) {
+            uint32_t words[2 * sizeof(T)];
+            load_words(row + col, words);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = to_float(v.v[i]);
+            for (int i = 0; i < 8; ++i) x[i] = value_of_words<T>(words, i);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = col + i < a.width ? to_float(row[col + i]) : 0.f;
@@ -83,7 +82,7 @@ __global__ void __launch_bounds__(kBlock) k_checkpoint_save(CheckpointArgs a)
 }
 
 // Four lanes a group, eight values each.
-template <typename T, bool kAligned>
+template <typename T>
 __global__ void __launch_bounds__(kBlock) k_checkpoint_load(CheckpointArgs a)
 {
     const int64_t total = (int64_t) a.count.get() * a.groups * 4;
@@ -95,15 +94,21 @@ __global__ void __launch_bounds__(kBlock) k_checkpoint_load(CheckpointArgs a)
         const uint2 q = *reinterpret_cast<const uint2*>(a.q + i * 8);
         const float scale = group_scale(a.exponents[g]);
         T* row = reinterpret_cast<T*>(a.out.data) + r * a.out.stride;
-        struct alignas(16) Eight { T v[8]; } v;
+        T v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.v[j] = from_float<T>((float) (int8_t) ((j < 4 ? q.x : q.y) >> (8 * (j & 3))) * scale);
-        if (kAligned && col + 8 <= a.width) {
-            *reinterpret_cast<Eight*>(row + col) = v;
+        for (int j = 0; j < 8; ++j) v[j] = from_float<T>((float) (int8_t) ((j < 4 ? q.x : q.y) >> (8 * (j & 3))) * scale);
+        if (col + 8 <= a.width) {
+            uint32_t words[2 * sizeof(T)];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (sizeof(T) == 4) words[j] = __float_as_uint(v[j]);
+                else if (j % 2 == 1)          words[j / 2] = v[j - 1].bits | (uint32_t) v[j].bits << 16;
+            }
+            store_words(row + col, words);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (col + j < a.width) row[col + j] = v.v[j];
+                if (col + j < a.width) row[col + j] = v[j];
         }
     }
 }
@@ -114,19 +119,11 @@ static unsigned grid_of(const gns_ctx* c, int64_t blocks)
     return (unsigned) (blocks < most ? blocks : most);
 }
 
-// Whether every row begins at a 16-byte mark
-template <typename T>
-static bool at_marks(const void* data, int64_t stride)
-{
-    return reinterpret_cast<uintptr_t>(data) % 16 == 0 && (uint64_t) stride * sizeof(T) % 16 == 0;
-}
-
 template <typename T>
 static hipError_t launch_save(const gns_ctx* c, const CheckpointArgs& a, hipStream_t s)
 {
     const dim3 grid(grid_of(c, ((int64_t) a.count.rows * a.groups + kBlock / 4 - 1) / (kBlock / 4)));
-    if (at_marks<T>(a.x.data, a.x.stride)) hipLaunchKernelGGL((k_checkpoint_save<T, true>), grid, dim3(kBlock), 0, s, a);
-    else                                   hipLaunchKernelGGL((k_checkpoint_save<T, false>), grid, dim3(kBlock), 0, s, a);
+    hipLaunchKernelGGL(k_checkpoint_save<T>, grid, dim3(kBlock), 0, s, a);
     return hipGetLastError();
 }
 
@@ -134,8 +131,7 @@ template <typename T>
 static hipError_t launch_load(const gns_ctx* c, const CheckpointArgs& a, hipStream_t s)
 {
     const dim3 grid(grid_of(c, ((int64_t) a.count.rows * a.groups + kBlock / 4 - 1) / (kBlock / 4)));
-    if (at_marks<T>(a.out.data, a.out.stride)) hipLaunchKernelGGL((k_checkpoint_load<T, true>), grid, dim3(kBlock), 0, s, a);
-    else                                       hipLaunchKernelGGL((k_checkpoint_load<T, false>), grid, dim3(kBlock), 0, s, a);
+    hipLaunchKernelGGL(k_checkpoint_load<T>, grid, dim3(kBlock), 0, s, a);
     return hipGetLastError();
 }
 

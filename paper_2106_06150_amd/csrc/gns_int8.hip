@@ -14,19 +14,19 @@ __device__ __forceinline__ float output_of(int sum, float w_scale, float scale, 
 template <typename T> constexpr int kPiece = 16 / (int) sizeof(T);
 template <typename T> struct alignas(16) Piece { T v[kPiece<T>]; };
 
-// kAligned: both inputs' rows begin at 16-byte marks and f1 is a multiple of the piece, so a piece inside a row is one read;
-// else its values are read singly.  Columns past the last are zero.
-template <typename T, bool kAligned>
+// A piece that lies in one input's row is one read, whatever the row's alignment; where an input ends inside, its values are read
+// singly.  Columns past the last are zero.
+template <typename T>
 __device__ __forceinline__ void load_piece(const QuantizeArgs& a, int64_t r, int32_t c, float (&x)[kPiece<T>])
 {
     constexpr int V = kPiece<T>;
     const int32_t f1 = a.x1.width, k = f1 + a.x2.width;
-    if (kAligned && c + V <= k) {
-        const T* from = c < f1 ? reinterpret_cast<const T*>(a.x1.data) + r * a.x1.stride + c
-                               : reinterpret_cast<const T*>(a.x2.data) + r * a.x2.stride + (c - f1);
-        const Piece<T> p = *reinterpret_cast<const Piece<T>*>(from);
+    if (c + V <= f1 || (c >= f1 && c + V <= k)) {
+        uint32_t words[4];
+        load_words(c < f1 ? reinterpret_cast<const T*>(a.x1.data) + r * a.x1.stride + c
+                          : reinterpret_cast<const T*>(a.x2.data) + r * a.x2.stride + (c - f1), words);
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = to_float(p.v[i]);
+        for (int i = 0; i < V; ++i) x[i] = value_of_words<T>(words, i);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -83,7 +83,7 @@ __device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
 }
 
 // Rows of up to L * P pieces: L lanes a row, P pieces a lane in registers; the row is read once.
-template <typename T, bool kAligned, int L, int P>
+template <typename T, int L, int P>
 __global__ void __launch_bounds__(kBlock) k_quantize_rows(QuantizeArgs a)
 {
     constexpr int V = kPiece<T>;
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kBlock) k_quantize_rows(QuantizeArgs a)
         float x[P][V];
         uint32_t most = 0;
 #pragma unroll
-        for (int p = 0; p < P; ++p) load_piece<T, kAligned>(a, r, (p * L + l) * V, x[p]);
+        for (int p = 0; p < P; ++p) load_piece<T>(a, r, (p * L + l) * V, x[p]);
 #pragma unroll
         for (int p = 0; p < P; ++p) most = largest_of(x[p], most);
         const RowScale s = row_scale(largest_of_lanes<L>(most));
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kBlock) k_quantize_rows(QuantizeArgs a)
 
 // Longer rows: a block per row, which reads it twice (the second time near by).
 constexpr int kLongBlock = 1024;
-template <typename T, bool kAligned>
+template <typename T>
 __global__ void __launch_bounds__(kLongBlock) k_quantize_long(QuantizeArgs a)
 {
     constexpr int V = kPiece<T>;
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kLongBlock) k_quantize_long(QuantizeArgs a)
         uint32_t most = 0;
         for (int32_t c = (int32_t) threadIdx.x * V; c < k; c += kLongBlock * V) {
             float x[V];
-            load_piece<T, kAligned>(a, r, c, x);
+            load_piece<T>(a, r, c, x);
             most = largest_of(x, most);
         }
         most = largest_of_lanes<kWave>(most);
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kLongBlock) k_quantize_long(QuantizeArgs a)
         const RowScale s = row_scale(most);
         for (int32_t c = (int32_t) threadIdx.x * V; c < (int32_t) a.stride; c += kLongBlock * V) {
             float x[V];
-            load_piece<T, kAligned>(a, r, c, x);
+            load_piece<T>(a, r, c, x);
             store_piece<T>(a.q + r * a.stride + c, x, s.inverse);
         }
         if (threadIdx.x == 0) a.scale[r] = s.scale;
@@ -304,7 +304,7 @@ constexpr size_t kFewLds = 64 * 1024;         // of quantised rows
 
 __host__ __device__ constexpr int64_t few_stride(int64_t stride) { return stride + 16; }        // of rows in LDS, off the banks' period
 
-template <typename T, typename X, bool kFused, bool kAligned, int MT>
+template <typename T, typename X, bool kFused, int MT>
 __global__ void __launch_bounds__(kFewBlock) k_int8_few(DenseInt8Args a, QuantizeArgs x)
 {
     constexpr int V = kPiece<X>;
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kFewBlock) k_int8_few(DenseInt8Args a, Quantiz
 #pragma unroll 4
             for (int32_t c = c0; c < a.k; c += team * V) {
                 float v[V];
-                load_piece<X, kAligned>(x, r, c, v);
+                load_piece<X>(x, r, c, v);
                 most = largest_of(v, most);
             }
         }
@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(kFewBlock) k_int8_few(DenseInt8Args a, Quantiz
 #pragma unroll 4
             for (int32_t c = c0; c < (int32_t) a.stride; c += team * V) {
                 float v[V];
-                load_piece<X, kAligned>(x, r, c, v);
+                load_piece<X>(x, r, c, v);
                 store_piece<X>(s_q + r * pitch + c, v, inverse);
             }
         }
@@ -444,8 +444,8 @@ __global__ void __launch_bounds__(kWaves * kWave) k_int8_rows(DenseInt8Args a, Q
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const int32_t c = (p * L + l) * V, cc = c < k ? c : 0;
-                v[t][p] = *reinterpret_cast<const Piece<T>*>(cc < f1 ? reinterpret_cast<const T*>(x.x1.data) + r * x.x1.stride + cc
-                                                                     : reinterpret_cast<const T*>(x.x2.data) + r * x.x2.stride + (cc - f1));
+                __builtin_memcpy(&v[t][p], cc < f1 ? reinterpret_cast<const T*>(x.x1.data) + r * x.x1.stride + cc
+                                                   : reinterpret_cast<const T*>(x.x2.data) + r * x.x2.stride + (cc - f1), 16);
             }
         }
     };
@@ -522,32 +522,23 @@ static unsigned grid_of(const gns_ctx* c, int64_t blocks, int per_cu)
     return (unsigned) (blocks < most ? blocks : most);
 }
 
-// Whether pieces of these rows are single reads
 template <typename T>
-static bool whole_pieces(const QuantizeArgs& a)
-{
-    auto marks = [](const ConstRows& x) { return reinterpret_cast<uintptr_t>(x.data) % 16 == 0 && (uint64_t) x.stride * sizeof(T) % 16 == 0; };
-    return marks(a.x1) && (a.x2.width == 0 || (marks(a.x2) && a.x1.width % kPiece<T> == 0));
-}
-
-template <typename T, bool kAligned>
 static hipError_t launch_quantize_typed(const gns_ctx* c, const QuantizeArgs& a, hipStream_t s)
 {
     const int64_t rows = a.count.rows, pieces = a.stride / kPiece<T>;
     const dim3 short_grid(grid_of(c, (rows + 15) / 16, 32)), wave_grid(grid_of(c, (rows + 3) / 4, 32));
-    if (pieces <= 32)        hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 16, 2>), short_grid, dim3(kBlock), 0, s, a);
-    else if (pieces <= 64)   hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 16, 4>), short_grid, dim3(kBlock), 0, s, a);
-    else if (pieces <= 256)  hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 64, 4>), wave_grid, dim3(kBlock), 0, s, a);
-    else if (pieces <= 512)  hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 64, 8>), wave_grid, dim3(kBlock), 0, s, a);
-    else if (pieces <= 1024 && sizeof(T) == 4) hipLaunchKernelGGL((k_quantize_rows<T, kAligned, 64, 16>), wave_grid, dim3(kBlock), 0, s, a);
-    else                     hipLaunchKernelGGL((k_quantize_long<T, kAligned>), dim3(grid_of(c, rows, 8)), dim3(kLongBlock), 0, s, a);
+    if (pieces <= 32)        hipLaunchKernelGGL((k_quantize_rows<T, 16, 2>), short_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 64)   hipLaunchKernelGGL((k_quantize_rows<T, 16, 4>), short_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 256)  hipLaunchKernelGGL((k_quantize_rows<T, 64, 4>), wave_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 512)  hipLaunchKernelGGL((k_quantize_rows<T, 64, 8>), wave_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 1024 && sizeof(T) == 4) hipLaunchKernelGGL((k_quantize_rows<T, 64, 16>), wave_grid, dim3(kBlock), 0, s, a);
+    else                     hipLaunchKernelGGL((k_quantize_long<T>), dim3(grid_of(c, rows, 8)), dim3(kLongBlock), 0, s, a);
     return hipGetLastError();
 }
 
 hipError_t launch_quantize(const gns_ctx* c, const QuantizeArgs& a, int32_t type, hipStream_t s)
 {
-    if (type == GNS_FP32) return whole_pieces<float>(a) ? launch_quantize_typed<float, true>(c, a, s) : launch_quantize_typed<float, false>(c, a, s);
-    return whole_pieces<Bf16>(a) ? launch_quantize_typed<Bf16, true>(c, a, s) : launch_quantize_typed<Bf16, false>(c, a, s);
+    return type == GNS_FP32 ? launch_quantize_typed<float>(c, a, s) : launch_quantize_typed<Bf16>(c, a, s);
 }
 
 template <typename T, int BM, int BN, int WM, int WN>
@@ -567,9 +558,9 @@ static hipError_t launch_typed(const gns_ctx* c, const DenseInt8Args& a, hipStre
 {
     if (a.count.rows <= kFewRows) {
         const dim3 grid((unsigned) ((a.out.width + kFewColumns - 1) / kFewColumns));
-        if (a.count.rows <= 16)      hipLaunchKernelGGL((k_int8_few<T, float, false, false, 1>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
-        else if (a.count.rows <= 32) hipLaunchKernelGGL((k_int8_few<T, float, false, false, 2>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
-        else                         hipLaunchKernelGGL((k_int8_few<T, float, false, false, 4>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
+        if (a.count.rows <= 16)      hipLaunchKernelGGL((k_int8_few<T, float, false, 1>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
+        else if (a.count.rows <= 32) hipLaunchKernelGGL((k_int8_few<T, float, false, 2>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
+        else                         hipLaunchKernelGGL((k_int8_few<T, float, false, 4>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
         return hipGetLastError();
     }
     auto tiles = [&](int64_t bm, int64_t bn) { return (a.count.rows + bm - 1) / bm * ((a.out.width + bn - 1) / bn); };
@@ -587,7 +578,7 @@ hipError_t launch_dense_int8(const gns_ctx* c, const DenseInt8Args& a, int32_t o
 template <typename T>
 static bool rows_fit(const gns_ctx* c, const QuantizeArgs& x, const DenseInt8Args& a)
 {
-    return a.count.rows >= c->num_cus * 32 && a.stride <= 512 && a.k % kPiece<T> == 0 && whole_pieces<T>(x) &&
+    return a.count.rows >= c->num_cus * 32 && a.stride <= 512 && a.k % kPiece<T> == 0 && x.x1.width % kPiece<T> == 0 &&
            rows_lds(a.stride, a.out.width, 8) <= (int64_t) c->lds_bitmap_limit;
 }
 
@@ -619,8 +610,7 @@ template <typename T, typename X>
 static void launch_few_fused(const QuantizeArgs& x, const DenseInt8Args& a, size_t lds, hipStream_t s)
 {
     const dim3 grid((unsigned) ((a.out.width + kFewColumns - 1) / kFewColumns));
-    if (whole_pieces<X>(x)) hipLaunchKernelGGL((k_int8_few<T, X, true, true, 1>), grid, dim3(kFewBlock), lds, s, a, x);
-    else                    hipLaunchKernelGGL((k_int8_few<T, X, true, false, 1>), grid, dim3(kFewBlock), lds, s, a, x);
+    hipLaunchKernelGGL((k_int8_few<T, X, true, 1>), grid, dim3(kFewBlock), lds, s, a, x);
 }
 
 hipError_t launch_sage_dense_int8(const gns_ctx* c, const QuantizeArgs& x, const DenseInt8Args& a, int32_t type, int32_t out_type,

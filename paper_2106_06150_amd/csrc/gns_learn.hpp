@@ -66,6 +66,38 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
+// 16 bytes (a struct of four words would not always stay in registers, nor leave them as one)
+typedef uint32_t Chunk __attribute__((ext_vector_type(4)));
+
+// N words from or to wherever they begin, 16 bytes a read or write: global memory asks for no marks.
+template <int N>
+__device__ __forceinline__ void load_words(const void* from, uint32_t (&to)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N / 4; ++j) {
+        Chunk v;
+        __builtin_memcpy(&v, static_cast<const char*>(from) + 16 * j, 16);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) to[4 * j + k] = v[k];
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_words(void* to, const uint32_t (&from)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N / 4; ++j) {
+        const Chunk v = {from[4 * j], from[4 * j + 1], from[4 * j + 2], from[4 * j + 3]};
+        __builtin_memcpy(static_cast<char*>(to) + 16 * j, &v, 16);
+    }
+}
+
+// Value i of packed ones, and values packed.
+template <typename T, int N>
+__device__ __forceinline__ float value_of_words(const uint32_t (&w)[N], int i)
+{
+    return sizeof(T) == 4 ? __uint_as_float(w[i]) : __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+}
+
 // Rows of a tile lie in LDS 64 bytes each, four chunks of 16: chunk c of row r at c ^ row_turn(r), so that reads of the same chunk
 // of eight or sixteen rows spread over all banks.
 __device__ __forceinline__ int row_turn(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
