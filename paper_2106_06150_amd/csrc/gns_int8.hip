@@ -278,7 +278,7 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(De
 #pragma unroll
         for (int t = 0; t < 32 * kLanes / kWave; ++t) {
             const int row = t * (kWave / kLanes) + e_lane / kLanes;
-            const Piece<T> y = *reinterpret_cast<const Piece<T>*>(strip + row * kPitch + e_lane % kLanes * 16);
+            const Chunk y = *reinterpret_cast<const Chunk*>(strip + row * kPitch + e_lane % kLanes * 16);
             const int64_t r = m0 + wm + i * 32 + row;
             if (r >= rows) continue;
             T* out = reinterpret_cast<T*>(a.out.data) + r * a.out.stride + c;
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(De
             } else {
 #pragma unroll
                 for (int k = 0; k < V; ++k)
-                    if (c + k < n) out[k] = y.v[k];
+                    if (c + k < n) out[k] = __builtin_bit_cast(Piece<T>, y).v[k];
             }
         }
         __builtin_amdgcn_wave_barrier();
