@@ -519,13 +519,14 @@ static unsigned grid_of(const gns_ctx* c, int64_t blocks, int per_cu)
 
 constexpr int32_t kShortClasses = 256;
 
-// Parts of a row: enough for eight waves on every SIMD, of at least two tiles, and no more best classes than the join reads at once.
+// Parts of a row: two waves on every SIMD, or four of at least 24 tiles, each of two tiles at least, and no more best classes
+// than the join reads at once.  A wave's first tile and the join are what best classes cost most: bf16, top 5, 3000 rows of
+// 9776 classes whole 24 us, in two parts 31; 1000 rows of 100,003 in four parts 57, in two 60, in eight 63.
 static void split_rows(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows, int32_t* parts, int32_t* tiles)
 {
     const int32_t all = (int32_t) (((int64_t) classes + kWaveTile - 1) / kWaveTile);
-    const int64_t waves = (int64_t) c->num_cus * 4 * 8;
-    int64_t p = 1;
-    if ((int64_t) rows * 2 <= waves) p = waves / rows;
+    const int64_t simds = (int64_t) c->num_cus * 4, least = simds * 2 / max(rows, 1), most = simds * 4 / max(rows, 1);
+    int64_t p = all / 24 < least ? least : all / 24 < most ? all / 24 : most;
     if (p > all / 2) p = all / 2;
     if (top && p > kJoinKeys * kWave / top) p = kJoinKeys * kWave / top;
     if (p < 1) p = 1;
