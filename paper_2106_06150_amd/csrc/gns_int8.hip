@@ -564,7 +564,10 @@ static hipError_t launch_typed(const gns_ctx* c, const DenseInt8Args& a, hipStre
         return hipGetLastError();
     }
     auto tiles = [&](int64_t bm, int64_t bn) { return (a.count.rows + bm - 1) / bm * ((a.out.width + bn - 1) / bn); };
-    if (tiles(256, 256) >= c->num_cus && a.k >= 1024) return launch_tiles<T, 256, 256, 128, 64>(a, s);
+    // Large tiles where five in eight CUs have one and a tile is long enough for a block to be alone on its CU (with the quantisation,
+    // bf16, 3000 x 4096 x 4096, 192 tiles: 67 us, 80 with the next; 4096 x 4096 x 2048, 128 tiles: 63 and 59; 10,000 x 1500 x 4096:
+    // 102 and 111; 40,000 x 768 x 1024: 94 and 88)
+    if (tiles(256, 256) * 8 >= (int64_t) c->num_cus * 5 && a.k >= 1024) return launch_tiles<T, 256, 256, 128, 64>(a, s);
     if (tiles(128, 128) >= c->num_cus) return launch_tiles<T, 128, 128, 64, 64>(a, s);
     return launch_tiles<T, 64, 64, 32, 32>(a, s);
 }

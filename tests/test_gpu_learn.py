@@ -311,6 +311,17 @@ def test_backward_of_many_rows_or_wide_layers(ctx, rows, f1, f2, hdim, dtype):
     check_backward(*run_backward(ctx, parts, f1, f2, d_out, positive, w), x, dz, w, dtype)
 
 
+# dx of few tiles (hdim split), of rows that end inside eight columns, of fewer than eight columns, of few rows
+@TYPES
+@pytest.mark.parametrize("relu", [False, True], ids=["identity", "relu"])
+@pytest.mark.parametrize("rows,f1,f2,hdim", [(300, 100, 28, 1030), (90, 70, 0, 2050), (1104, 64, 64, 2048), (200, 520, 0, 1805), (65, 64, 0, 9),
+                                             (9001, 200, 100, 301), (200, 33, 0, 7), (5000, 300, 60, 3), (4, 70, 0, 6), (30, 40, 8, 1033)])
+def test_backward_of_few_or_odd_columns(ctx, rows, f1, f2, hdim, relu, dtype):
+    for how in ("packed", "odd"):
+        parts, x, d_out, positive, dz, w = backward_case(ctx, rows, f1, f2, hdim, dtype, relu, how)
+        check_backward(*run_backward(ctx, parts, f1, f2, d_out, positive, w, how=how), x, dz, w, dtype)
+
+
 @TYPES
 def test_backward_alone_and_in_parts(ctx, dtype):
     rows, f1, f2, hdim = 500, 96, 40, 72
@@ -768,5 +779,29 @@ def test_rows_counted_on_the_device(dtype):
             assert bool((a[count:] == 42).all()), i
         for a, b in zip(sums, want_sums):
             within(f64(a), f64(b), 1e-5 * (np.abs(f64(b)) + float(b.abs().max())))
+    finally:
+        gns.close()
+
+
+@TYPES
+@pytest.mark.parametrize("hdim", [5, 1030])
+def test_backward_of_rows_counted_on_the_device(hdim, dtype):
+    indptr, indices = random_symmetric_csr(3000, 10, np.random.default_rng(5))
+    gns = GpuGns(torch.from_numpy(indptr), torch.from_numpy(indices), None, fanouts=(6, 4), policies=(0, 0), cache_size=0, max_seeds=100)
+    try:
+        c, layer = gns.ctx, 1
+        B.gns_sample_blocks(c, 3, synth.uniform_seed_batch(3000, 60, 9).cuda(), gns.blocks.array)
+        count, cap = gns.blocks.array[layer].num_dst, gns.blocks.array[layer].cap_dst
+        assert 60 < count < cap
+        g = gen("device", hdim)
+        parts, _, d_out, positive, _, w = backward_case(c, cap, 70, 30, hdim, dtype, True, "packed")
+        dx = [torch.full((cap, 100), 42.0, dtype=dtype, device="cuda") for _ in range(2)]
+        for out, rows in zip(dx, (-1 - layer, count)):
+            space = learn.alloc_workspace(learn.gns_sage_dense_backward_workspace_bytes(c, 70, 30, hdim, rows))
+            learn.gns_sage_dense_backward(c, d_out, positive, parts[0][:2], 70, parts[1][:2], 30, w.cuda(), None, None, out, rows, space)
+        torch.cuda.synchronize()
+        assert all(bool((out[count:] == 42).all()) for out in dx)
+        tol = 2.0 ** -7 if dtype == BF16 else 1e-5
+        within(f64(dx[0][:count]), f64(dx[1][:count]), tol * (f64(dx[1][:count].abs()) + f64(dx[1][:count].abs().max())))
     finally:
         gns.close()
