@@ -108,7 +108,36 @@ __global__ void __launch_bounds__(kBlock) k_quantize_rows(QuantizeArgs a)
     }
 }
 
-// Longer rows: a block per row, which reads it twice (the second time near by).
+// Longer rows: a block per row, P pieces a thread.
+template <typename T, int P>
+__global__ void __launch_bounds__(kBlock) k_quantize_block(QuantizeArgs a)
+{
+    constexpr int V = kPiece<T>, kWaves = kBlock / kWave;
+    __shared__ uint32_t s_most[2][kWaves];                    // of this row and the one before
+    const int32_t rows = a.count.get();
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x, turn ^= 1) {
+        const int32_t c0 = (int32_t) threadIdx.x * V;
+        float x[P][V];
+        uint32_t most = 0;
+#pragma unroll
+        for (int p = 0; p < P; ++p) load_piece<T>(a, r, p * kBlock * V + c0, x[p]);
+#pragma unroll
+        for (int p = 0; p < P; ++p) most = largest_of(x[p], most);
+        most = largest_of_lanes<kWave>(most);
+        if (opaque_lane_id() == 0) s_most[turn][threadIdx.x >> 6] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) most = max(most, s_most[turn][w]);
+        const RowScale s = row_scale(most);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (p * kBlock * V + c0 < (int32_t) a.stride) store_piece<T>(a.q + r * a.stride + p * kBlock * V + c0, x[p], s.inverse);
+        if (threadIdx.x == 0) a.scale[r] = s.scale;
+    }
+}
+
+// Rows of any length: a block per row, which reads it twice (the second time near by).
 constexpr int kLongBlock = 1024;
 template <typename T>
 __global__ void __launch_bounds__(kLongBlock) k_quantize_long(QuantizeArgs a)
@@ -526,12 +555,13 @@ template <typename T>
 static hipError_t launch_quantize_typed(const gns_ctx* c, const QuantizeArgs& a, hipStream_t s)
 {
     const int64_t rows = a.count.rows, pieces = a.stride / kPiece<T>;
-    const dim3 short_grid(grid_of(c, (rows + 15) / 16, 32)), wave_grid(grid_of(c, (rows + 3) / 4, 32));
+    const dim3 short_grid(grid_of(c, (rows + 15) / 16, 32)), wave_grid(grid_of(c, (rows + 3) / 4, 32)), block_grid(grid_of(c, rows, 32));
     if (pieces <= 32)        hipLaunchKernelGGL((k_quantize_rows<T, 16, 2>), short_grid, dim3(kBlock), 0, s, a);
     else if (pieces <= 64)   hipLaunchKernelGGL((k_quantize_rows<T, 16, 4>), short_grid, dim3(kBlock), 0, s, a);
     else if (pieces <= 256)  hipLaunchKernelGGL((k_quantize_rows<T, 64, 4>), wave_grid, dim3(kBlock), 0, s, a);
     else if (pieces <= 512)  hipLaunchKernelGGL((k_quantize_rows<T, 64, 8>), wave_grid, dim3(kBlock), 0, s, a);
-    else if (pieces <= 1024 && sizeof(T) == 4) hipLaunchKernelGGL((k_quantize_rows<T, 64, 16>), wave_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 1024) hipLaunchKernelGGL((k_quantize_block<T, 4>), block_grid, dim3(kBlock), 0, s, a);
+    else if (pieces <= 2048) hipLaunchKernelGGL((k_quantize_block<T, 8>), block_grid, dim3(kBlock), 0, s, a);
     else                     hipLaunchKernelGGL((k_quantize_long<T>), dim3(grid_of(c, rows, 8)), dim3(kLongBlock), 0, s, a);
     return hipGetLastError();
 }
