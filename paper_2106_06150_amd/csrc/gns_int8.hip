@@ -581,19 +581,20 @@ static hipError_t launch_tiles(const DenseInt8Args& a, hipStream_t s)
     return hipGetLastError();
 }
 
-constexpr int32_t kFewRows = 64;
-
 template <typename T>
 static hipError_t launch_typed(const gns_ctx* c, const DenseInt8Args& a, hipStream_t s)
 {
-    if (a.count.rows <= kFewRows) {
+    auto tiles = [&](int64_t bm, int64_t bn) { return (a.count.rows + bm - 1) / bm * ((a.out.width + bn - 1) / bn); };
+    // Up to 64 rows a block per 16 channels, which divides k among its waves, while tiles would fill less than half the chip (with the
+    // quantisation, bf16, 33 x 4096 x 4096: 16 us, 19 in tiles; 20 x 4096 x 4096: 13.5 and 19; 64 x 8192 x 8192: 46 and 32; 128 x 4096
+    // x 4096 and smaller ones of that many rows: 27 and 20)
+    if (a.count.rows <= 32 || (a.count.rows <= 64 && tiles(64, 64) * 2 < c->num_cus)) {
         const dim3 grid((unsigned) ((a.out.width + kFewColumns - 1) / kFewColumns));
         if (a.count.rows <= 16)      hipLaunchKernelGGL((k_int8_few<T, float, false, 1>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
         else if (a.count.rows <= 32) hipLaunchKernelGGL((k_int8_few<T, float, false, 2>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
         else                         hipLaunchKernelGGL((k_int8_few<T, float, false, 4>), grid, dim3(kFewBlock), 0, s, a, QuantizeArgs{});
         return hipGetLastError();
     }
-    auto tiles = [&](int64_t bm, int64_t bn) { return (a.count.rows + bm - 1) / bm * ((a.out.width + bn - 1) / bn); };
     // Large tiles where five in eight CUs have one and a tile is long enough for a block to be alone on its CU (with the quantisation,
     // bf16, 3000 x 4096 x 4096, 192 tiles: 67 us, 80 with the next; 4096 x 4096 x 2048, 128 tiles: 63 and 59; 10,000 x 1500 x 4096:
     // 102 and 111; 40,000 x 768 x 1024: 94 and 88)
