@@ -31,8 +31,8 @@ enum { GNS_FP32 = 0, GNS_BF16 = 1 };
 #define GNS_MAX_STRIDE (1 << 24)
 
 /* Rows of a matrix on the device: element (r, c) is data[r * stride + c], 0 <= c < width <= GNS_MAX_WIDTH.  width <= stride <=
- * GNS_MAX_STRIDE, in elements; data aligned to the element.  Any width, stride and alignment is taken; rows that begin at multiples of 16 bytes are
- * read and written faster. */
+ * GNS_MAX_STRIDE, in elements; data aligned to the element.  Any width, stride and alignment is taken; rows that begin at
+ * multiples of 16 bytes are read and written a little faster. */
 typedef struct {
     void* data;
     int64_t stride;
@@ -74,7 +74,7 @@ gns_status gns_sage_dense_int8(gns_ctx* ctx, const gns_rows* x1, const gns_rows*
  *   exponents_dev  uint8[num_rows x G]: e + 127.  0: all values are zero (magnitudes below 2^-100 are taken as zero);
  *                  255: the group held an infinity or NaN, and all its values are NaN when loaded
  * A value is q * 2^e, rounded to nearest (ties to even), at most half a step off; it is exactly a bf16 value.
- * Magnitudes of 1.99 * 2^127 and more are kept as 127 * 2^121.
+ * Magnitudes of 127.5 * 2^121 and more are kept as 127 * 2^121.
  * positive_dev (may be NULL): uint32[num_rows x G], bit j of word g set iff x[r, 32 g + j] > 0: the mask of a ReLU whose
  * output x is. */
 gns_status gns_checkpoint_save(gns_ctx* ctx, const gns_rows* x, int8_t* q_dev, uint8_t* exponents_dev,

@@ -163,7 +163,10 @@ struct Tile {
 // k of these products are the rows of the batch, so both factors are turned on their way to LDS: a thread reads columns of a few
 // rows and writes them as rows.  X: four columns (a word) of four rows; dz: of eight rows a column of fp32 or two of bf16.
 // What a wave needs of exponents and masks is one read, lane by lane, and handed round.  Columns are placed such that
-// adjacent threads write adjacent rows of LDS.
+// adjacent threads write adjacent rows of LDS.  Splits of the rows fill the chip where dw has few tiles.
+// 85,000 rows, 256 x 256, fp32: 48 us (87 MB of gradients, 22 of checkpoints, 33 of the splits' sums: 3.0 TB/s); 16,384 rows,
+// 4096 x 4096, bf16: 580 to 660 us (0.83 to 0.95 PFLOP/s), bound by the issue of matrix and vector instructions together: a value
+// of X takes three of the latter on its way to LDS.
 struct WeightsArgs {
     BackwardArgs a;
     int32_t m_tiles, n_tiles, splits;
@@ -544,12 +547,14 @@ template <> struct InputTile<float, 256> { typedef Tile<64, 64, 32, 32, 3, 3> Ty
 template <> struct InputTile<Bf16, 512> { typedef Tile<256, 128, 64, 64, 1, 2> Type; };
 template <> struct InputTile<Bf16, 256> { typedef Tile<128, 128, 64, 64, 1, 2> Type; };
 
+// 85,000 rows, 256 x 256, fp32: 78 us (six products of terms; 0.86 PFLOP/s of them); 16,384 rows, 4096 x 4096, bf16: 955 to 995 us
+// (two products; 1.1 to 1.15 PFLOP/s, the matrix cores busy in 69 % of the cycles at the 1.5 GHz that the power leaves).
 // A thread reads eight columns of a row of dz (of two rows of bf16), and as many of W's planes.  kWhole: hdim is a multiple of
 // eight.  Chunks past the last are read as the last: W's planes are zero there.  Else a row's last chunk is its last eight
 // columns, for dz as for W, and those that the chunk before has are left out of dz.  hdim is eight at least.
 // A block goes through tiles, `stride` apart, or has a split of one tile's hdim.
 // kPlain: W is read as it is and cut here, by every block that needs it, which where there is no more than a block or two per
-// CU costs less than a launch and a trip through memory in front.
+// CU costs less than a launch and a trip through memory in front (the planes of 4096 x 4096 take 25 us).
 template <typename T, int kThreads, bool kMask, bool kWhole, bool kPlain>
 struct InputSource {
     typedef typename InputTile<T, kThreads>::Type Tiles;
@@ -728,19 +733,19 @@ __global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
     });
 }
 
-// k_backward_few: dx of rows by the ten, where W's bytes are all there is to do.  A block has 16 columns of dx (rows of W) and all
-// rows, 16 a tile; its eight waves an eighth of hdim each, 16 x 16 x 32 products; their sums meet in LDS.  W is cut into terms
-// on the way, as dz is.
-constexpr int kFewBlock = 512, kFewWaves = kFewBlock / kWave, kFewColumns = 16;
+// k_backward_few: dx of up to sixteen rows, where W's bytes are all there is to do.  A block has 16 columns of dx (rows of W) and
+// all rows; its eight waves an eighth of hdim each, 16 x 16 x 32 products; their sums meet in LDS.  W is cut into terms on the
+// way, as dz is.  One row, 4096 x 4096, fp32, dw too: 44 us, 56 in tiles with hdim split; 17 rows would take 66 and take 54 in tiles.
+constexpr int kFewRows = 16, kFewBlock = 512, kFewWaves = kFewBlock / kWave, kFewColumns = 16;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-template <typename T, int MT, bool kMask>
+template <typename T, bool kMask>
 __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
 {
     constexpr bool kFloat = sizeof(T) == 4;
-    constexpr int kTermsA = kFloat ? 3 : 1, kTermsB = kFloat ? 3 : 2, kSets = MT == 1 ? 4 : 2;
+    constexpr int kTermsA = kFloat ? 3 : 1, kTermsB = kFloat ? 3 : 2, kSets = 4;
     typedef Pairs<kTermsA, kTermsB> P;
-    __shared__ float s_sum[kFewWaves][MT][4][kWave];
+    __shared__ float s_sum[kFewWaves][4][kWave];
     const int32_t rows = a.count.get(), K = a.x1.width + a.x2.width, hdim = a.hdim, steps = (hdim + 31) / 32;
     if (rows <= 0) return;
     const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
@@ -748,53 +753,38 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
     const int32_t k0 = (int32_t) blockIdx.x * kFewColumns;
     const int32_t s0 = (int32_t) ((int64_t) steps * wave / kFewWaves), s1 = (int32_t) ((int64_t) steps * (wave + 1) / kFewWaves);
     const float* w = a.w + (int64_t) min(k0 + l16, K - 1) * hdim;
-    const T* z[MT];
-    const uint32_t* m[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {                            // rows past the last are read as the last; they are not stored
-        const int64_t r = min(t * 16 + l16, rows - 1);
-        z[t] = reinterpret_cast<const T*>(a.d_out.data) + r * a.d_out.stride;
-        if constexpr (kMask) m[t] = a.positive + r * steps;
-    }
-    uint32_t wv[kSets][8], zv[kSets][MT][kFloat ? 8 : 4], words[kSets][MT];
+    const int64_t own = min(l16, rows - 1);                   // rows past the last are read as the last; they are not stored
+    const T* z = reinterpret_cast<const T*>(a.d_out.data) + own * a.d_out.stride;
+    const uint32_t* m = nullptr;
+    if constexpr (kMask) m = a.positive + own * steps;
+    uint32_t wv[kSets][8], zv[kSets][kFloat ? 8 : 4], words[kSets];
     auto fetch = [&](int set, int32_t step) {                 // steps past the wave's last read that one again
         step = min(step, s1 - 1);
         const int32_t n = min(step * 32 + kg * 8, hdim - 8);
         load_words(w + n, wv[set]);
-#pragma unroll
-        for (int t = 0; t < MT; ++t) load_words(z[t] + n, zv[set][t]);
-        if constexpr (kMask) {
-#pragma unroll
-            for (int t = 0; t < MT; ++t) words[set][t] = m[t][step];
-        }
+        load_words(z + n, zv[set]);
+        if constexpr (kMask) words[set] = m[step];
     };
-    floatx4 acc[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     auto multiply = [&](int set, int32_t step) {
-        const uint32_t keep = columns_kept(hdim - step * 32 - kg * 8);
-        Chunk wt[kTermsB];
+        const uint32_t keep = columns_kept(hdim - step * 32 - kg * 8), k8 = kMask ? columns_left(keep, words[set] >> (kg * 8)) : keep;
+        Chunk wt[kTermsB], zt[kTermsA];
 #pragma unroll
         for (int j = 0; j < 8; ++j) wv[set][j] &= spread_bit(keep, j);
 #pragma unroll
         for (int k = 0; k < kTermsB; ++k) wt[k] = take_terms(wv[set]);
+        if constexpr (kFloat) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const uint32_t k8 = kMask ? columns_left(keep, words[set][t] >> (kg * 8)) : keep;
-            Chunk zt[kTermsA];
-            if constexpr (kFloat) {
+            for (int j = 0; j < 8; ++j) zv[set][j] &= spread_bit(k8, j);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) zv[set][t][j] &= spread_bit(k8, j);
+            for (int k = 0; k < kTermsA; ++k) zt[k] = take_terms(zv[set]);
+        } else {
 #pragma unroll
-                for (int k = 0; k < kTermsA; ++k) zt[k] = take_terms(zv[set][t]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) zt[0][j] = zv[set][t][j] & ((spread_bit(k8, 2 * j) & 0xFFFFu) | (spread_bit(k8, 2 * j + 1) & 0xFFFF0000u));
-            }
-#pragma unroll
-            for (int p = 0; p < P::kCount; ++p)
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, zt[P::kA[p]]), __builtin_bit_cast(bf16x8, wt[P::kB[p]]), acc[t], 0, 0, 0);
+            for (int j = 0; j < 4; ++j) zt[0][j] = zv[set][j] & ((spread_bit(k8, 2 * j) & 0xFFFFu) | (spread_bit(k8, 2 * j + 1) & 0xFFFF0000u));
         }
+#pragma unroll
+        for (int p = 0; p < P::kCount; ++p)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, zt[P::kA[p]]), __builtin_bit_cast(bf16x8, wt[P::kB[p]]), acc, 0, 0, 0);
     };
     if (s0 < s1) {
 #pragma unroll
@@ -808,24 +798,23 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
         }
     }
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) s_sum[wave][t][v][lane] = acc[t][v];
+    for (int v = 0; v < 4; ++v) s_sum[wave][v][lane] = acc[v];
     __syncthreads();
     // element v of lane l is row 4 * (l / 16) + v, column l % 16
-    for (int i = (int) threadIdx.x; i < MT * 4 * kWave; i += kFewBlock) {
-        const int t = i / (4 * kWave), v = i / kWave % 4, l = i % kWave;
-        const int32_t r = t * 16 + 4 * (l >> 4) + v, k = k0 + (l & 15);
-        if (r >= rows || k >= K) continue;
-        float sum = 0.f;
+    const int i = (int) threadIdx.x;
+    if (i >= 4 * kWave) return;
+    const int v = i / kWave, l = i % kWave;
+    const int32_t r = 4 * (l >> 4) + v, k = k0 + (l & 15);
+    if (r >= rows || k >= K) return;
+    float sum = 0.f;
 #pragma unroll
-        for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][t][v][l];
-        store_at<T>(a.dx, r, k, sum);
-    }
+    for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][v][l];
+    store_at<T>(a.dx, r, k, sum);
 }
 
 // k_backward_narrow: dx of fewer than eight columns of dz, by as many multiplications each, in fp32.  A lane has four columns of
-// dx, whose rows of W stay in registers, and rows one after the other; 2^lanes_log2 lanes have a row.  Bound by the bytes of dx.
+// dx, whose rows of W stay in registers, and rows one after the other; 2^lanes_log2 lanes have a row.  Bound by the bytes of dx: 85,000 rows of 100 bf16 columns from two, dw
+// too, 34 us; as tiles of products 50.
 constexpr int kNarrow = 8, kNarrowRows = 16;  // rows of a lane
 template <typename T, bool kMask>
 __global__ void __launch_bounds__(kBlock) k_backward_narrow(BackwardArgs a, int32_t lanes_log2)
@@ -910,7 +899,8 @@ static WeightsPlan plan_weights(const gns_ctx* c, int32_t f1, int32_t f2, int32_
         p.db_shares = p.splits == 1 && rows <= 512 ? 1 : p.m_tiles;
         return p;
     };
-    // Wide blocks where layers fill them and they fill half the chip at least
+    // Wide blocks where layers fill them and they fill half the chip at least (dx too, 16,384 rows of 2048 x 2048 bf16: 500 us, 571 with
+    // narrow ones; 85,000 of 256 x 256 fp32: 138 and 144; 12,600 of 512 x 256: no difference)
     const WeightsPlan p = plan(true);
     if (wide && columns > 128 && hdim > n512 / 2 && (int64_t) p.m_tiles * p.n_tiles * p.splits >= c->num_cus / 2) return p;
     return plan(false);
@@ -970,14 +960,12 @@ static hipError_t launch_input(const gns_ctx* c, InputArgs g, hipStream_t s)
     return hipGetLastError();
 }
 
-constexpr int32_t kFewRows = 64;
-
-template <typename T, int MT>
+template <typename T>
 static hipError_t launch_few(const BackwardArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned) ((a.x1.width + a.x2.width + kFewColumns - 1) / kFewColumns)), block(kFewBlock);
-    if (a.positive) hipLaunchKernelGGL((k_backward_few<T, MT, true>), grid, block, 0, s, a);
-    else            hipLaunchKernelGGL((k_backward_few<T, MT, false>), grid, block, 0, s, a);
+    if (a.positive) hipLaunchKernelGGL((k_backward_few<T, true>), grid, block, 0, s, a);
+    else            hipLaunchKernelGGL((k_backward_few<T, false>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 
@@ -1086,7 +1074,7 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     if (!dx || p.splits > 1) return hipGetLastError();
     switch (p.way) {
     case Way::kNarrow: return launch_narrow<T>(c, a, s);
-    case Way::kFew:    return a.count.rows <= 16 ? launch_few<T, 1>(a, s) : launch_few<T, 4>(a, s);
+    case Way::kFew:    return launch_few<T>(a, s);
     case Way::kPlain:  return launch_input<T, 256, true>(c, g, s);
     case Way::kCut:    return launch_input<T, 256, false>(c, g, s);
     default:           return launch_input<T, 512, false>(c, g, s);

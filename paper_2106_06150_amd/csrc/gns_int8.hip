@@ -82,7 +82,10 @@ __device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
     return v;
 }
 
-// Rows of up to L * P pieces: L lanes a row, P pieces a lane in registers; the row is read once.
+// Rows of up to L * P pieces: L lanes a row, P pieces a lane in registers; the row is read once, and nothing but its bytes counts
+// where it is long enough: 85,000 rows of 256 fp32 17 us (6.4 TB/s).  Narrow ones are bound by instructions, so lanes should not
+// idle: 79,214 rows of 32 bf16, four lanes each, 7 us, sixteen 14; but 100,000 rows of 100 bf16 with eight lanes 19.5, with
+// sixteen, whose exchange costs the same, 18.
 template <typename T, int L, int P>
 __global__ void __launch_bounds__(kBlock) k_quantize_rows(QuantizeArgs a)
 {
@@ -108,7 +111,8 @@ __global__ void __launch_bounds__(kBlock) k_quantize_rows(QuantizeArgs a)
     }
 }
 
-// Longer rows: a block per row, P pieces a thread.
+// Longer rows: a block per row, P pieces a thread.  8192 rows of 8192 bf16: 70 us (2.9 TB/s, behind a product that leaves nothing in
+// the caches); read twice by 1024 threads instead 100.
 template <typename T, int P>
 __global__ void __launch_bounds__(kBlock) k_quantize_block(QuantizeArgs a)
 {
@@ -176,7 +180,10 @@ constexpr int kStepBytes = 64;                // k of a stage
 // is read two stages before it is written to LDS, and written two before it is multiplied; one barrier a stage.  So
 // nothing that the products wait for is less than a stage old: the last fragments of a stage are read while its first are
 // multiplied, the first of the next one while its last are.  Chunk c of 16 bytes of row r lies at c ^ row_turn(r) of the
-// row, so that reads of the same chunk of eight or sixteen rows spread over all banks.
+// row, so that reads of the same chunk of eight or sixteen rows spread over all banks.  The weights are the products' left factor,
+// so that a lane holds four consecutive outputs of a row.
+// 8192 x 8192 x 8192, bf16 out: 490 to 580 us, 1.9 to 2.2 POP/s (a large library product of integers: 2.15), bound by the matrix
+// cores' cycles at the clock that the power leaves; with outputs stored value by value 40 us more.
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(DenseInt8Args a, int32_t m_tiles, int32_t n_tiles)
 {
@@ -323,7 +330,8 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(De
     }
 }
 
-// k_int8_few: for rows by the ten, where the weights' bytes are all there is to do.  A block has 16 output channels and
+// k_int8_few: for rows by the ten, where the weights' bytes are all there is to do (one row of 4096 bf16, 4096 channels: 6 us, 2.8
+// TB/s of weights, half of it launch and the chain of three dependent reads).  A block has 16 output channels and
 // all rows (16 a tile, up to MT tiles), its eight waves an eighth of k each, products of 16 x 16 x 64 bytes; their sums meet in
 // LDS.  kFused: the block quantises the rows itself into LDS (every block does, which costs less than a launch in front), while
 // its first weights are on their way.
@@ -427,7 +435,7 @@ __global__ void __launch_bounds__(kFewBlock) k_int8_few(DenseInt8Args a, Quantiz
 }
 
 // k_int8_rows: many rows against weights that fit LDS: rows come in, are quantised and multiplied, and leave, without a
-// trip through memory in 8 bits (85,000 rows, 256 x 256, fp32: 17 us for the quantisation and 44 for the product otherwise).
+// trip through memory in 8 bits (85,000 rows, 256 x 256, fp32: 34 us, 5.1 TB/s in and out; in two kernels 17 and 44).
 // A block per CU holds all weights; its waves walk tiles of 16 rows: a row is read by L lanes, P pieces each, quantised, turned
 // through a piece of LDS of the wave's own and multiplied, 16 x 16 x 64 bytes, with the weights as the left factor, so that a
 // lane gets four consecutive outputs of a row.  Bound by the rows' bytes, in and out.
@@ -556,7 +564,8 @@ static hipError_t launch_quantize_typed(const gns_ctx* c, const QuantizeArgs& a,
 {
     const int64_t rows = a.count.rows, pieces = a.stride / kPiece<T>;
     const dim3 short_grid(grid_of(c, (rows + 15) / 16, 32)), wave_grid(grid_of(c, (rows + 3) / 4, 32)), block_grid(grid_of(c, rows, 32));
-    if (pieces <= 32)        hipLaunchKernelGGL((k_quantize_rows<T, 16, 2>), short_grid, dim3(kBlock), 0, s, a);
+    if (pieces <= 8)         hipLaunchKernelGGL((k_quantize_rows<T, 4, 2>), dim3(grid_of(c, (rows + 63) / 64, 32)), dim3(kBlock), 0, s, a);
+    else if (pieces <= 32)   hipLaunchKernelGGL((k_quantize_rows<T, 16, 2>), short_grid, dim3(kBlock), 0, s, a);
     else if (pieces <= 64)   hipLaunchKernelGGL((k_quantize_rows<T, 16, 4>), short_grid, dim3(kBlock), 0, s, a);
     else if (pieces <= 256)  hipLaunchKernelGGL((k_quantize_rows<T, 64, 4>), wave_grid, dim3(kBlock), 0, s, a);
     else if (pieces <= 512)  hipLaunchKernelGGL((k_quantize_rows<T, 64, 8>), wave_grid, dim3(kBlock), 0, s, a);
@@ -608,7 +617,8 @@ hipError_t launch_dense_int8(const gns_ctx* c, const DenseInt8Args& a, int32_t o
     return out_type == GNS_FP32 ? launch_typed<float>(c, a, s) : launch_typed<Bf16>(c, a, s);
 }
 
-// Rows and weights of k_int8_rows: rows of whole pieces, as many as a tile's registers hold, and weights that leave room in LDS
+// Rows and weights of k_int8_rows: rows of whole pieces, as many as a tile's registers hold, weights that leave room in LDS, and
+// two tiles for each wave of a block per CU, or reading the weights into every LDS costs more than it saves
 template <typename T>
 static bool rows_fit(const gns_ctx* c, const QuantizeArgs& x, const DenseInt8Args& a)
 {

@@ -147,7 +147,8 @@ __device__ __forceinline__ float label_logit(const LogProbsArgs& a, int64_t r, i
 
 // Rows of up to L * E classes: L lanes a row, E values a lane in registers, 64 / L rows a wave.  The best classes come one
 // after the other: each lane has its own best at hand, the lane that wins looks for its next.
-// 85,000 rows of 172 classes, fp32, five best: see launch_log_probs.
+// 85,000 rows of 172 classes, fp32: 12.8 us (4.6 TB/s), with five best 25 to 27, with twenty 66: 70 instructions for a best class of
+// four rows.  Three in order at hand for each lane, found in one pass, take as long (26.6; twenty 84).
 template <typename T, int L, int E>
 __global__ void __launch_bounds__(kBlock) k_log_probs_short(LogProbsArgs a)
 {
@@ -275,6 +276,7 @@ struct LongArgs {
     Key* best;                    // [rows x parts x top]
 };
 
+// 4096 rows of 100,003 classes, bf16, twenty best: 175 us (4.7 TB/s); one row of 131,072, fp32: 12 us and 7 for the join.
 // Rows of any length: a wave per row, or per part of a row where there are few.  Pieces of 16 bytes are read at 16-byte
 // marks whatever the row's own alignment; the few values in front of the first mark and behind the last are read singly.
 template <typename T>
@@ -356,7 +358,7 @@ __global__ void __launch_bounds__(kBlock) k_log_probs_long(LongArgs g)
     }
 }
 
-// A wave per row: its parts' sums and best classes, which are on their way first.
+// A wave per row: its parts' sums and best classes, which are on their way first.  Bound by latency, 6 to 7 us.
 constexpr int kJoinKeys = 16;                 // of a lane
 template <typename T>
 __global__ void __launch_bounds__(kWave) k_log_probs_join(LongArgs g)
@@ -438,7 +440,8 @@ __device__ __forceinline__ float gradient_of(const RowGradient& o, float z)
     return p * (kEntropy ? fmaf(o.slope, fmaxf(log_p, kFar), o.base) : o.base);
 }
 
-// L lanes a row (of short rows several a wave), a value at a time; `chunk` columns of a long row.
+// L lanes a row (of short rows several a wave), a value at a time; `chunk` columns of a long row.  1000 rows of 47 classes: 2.7 us, a
+// launch.
 template <typename T, typename O, bool kEntropy, int L>
 __global__ void __launch_bounds__(kBlock) k_log_probs_backward(LogProbsBackwardArgs a, int32_t chunk)
 {
@@ -466,7 +469,8 @@ __global__ void __launch_bounds__(kBlock) k_log_probs_backward(LogProbsBackwardA
 }
 
 // Long rows whose logits and gradients lie alike against the 16-byte marks: pieces of 16 bytes at the marks, single values
-// in front of and behind them.  A wave has `tiles` tiles of a row.
+// in front of and behind them.  A wave has `tiles` tiles of a row.  4096 rows of 100,003 classes, bf16: 316 us, 5.2 TB/s, the rate of
+// a copy.
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kBlock) k_log_probs_backward_long(LogProbsBackwardArgs a, int32_t parts, int32_t tiles)
 {
