@@ -377,14 +377,13 @@ struct WeightsSource {
 };
 
 template <typename T, int kThreads, bool kMask, bool kPairs>
-__global__ void __launch_bounds__(kThreads, 2) k_backward_weights(WeightsArgs g)
+__device__ __forceinline__ void weights_block(const WeightsArgs& g, int32_t block, Chunk* s_stage)
 {
     typedef WeightsSource<T, kThreads, kMask, kPairs> Source;
     typedef typename Source::Tiles Tiles;
-    __shared__ Chunk s_stage[3 * Tiles::kStage];
     const BackwardArgs& a = g.a;
     const int64_t rows = a.count.get();
-    const int32_t all = g.m_tiles * g.n_tiles, t = xcd_run((int32_t) blockIdx.x, all * g.splits), split = t / all;
+    const int32_t all = g.m_tiles * g.n_tiles, t = xcd_run(block, all * g.splits), split = t / all;
     int32_t tm, tn;
     tile_of(t - split * all, g.m_tiles, g.n_tiles, &tm, &tn);
     const int32_t c0 = tm * Tiles::kM, n0 = tn * Tiles::kN;
@@ -419,6 +418,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_backward_weights(WeightsArgs g)
     const int n = (int) threadIdx.x;
     if (n < Tiles::kN && n0 + n < a.hdim)
         g.db[((int64_t) split * g.db_shares + tm) * a.hdim + n0 + n] = (s_sum[n] + s_sum[Tiles::kN + n]) + (s_sum[2 * Tiles::kN + n] + s_sum[3 * Tiles::kN + n]);
+}
+
+template <typename T, int kThreads, bool kMask, bool kPairs>
+__global__ void __launch_bounds__(kThreads, 2) k_backward_weights(WeightsArgs g)
+{
+    __shared__ Chunk s_stage[3 * WeightsTile<T, kThreads>::Type::kStage];
+    weights_block<T, kThreads, kMask, kPairs>(g, (int32_t) blockIdx.x, s_stage);
 }
 
 // ---- sums and terms -------------------------------------------------------------------------------------------------
@@ -684,16 +690,15 @@ struct InputSource {
 };
 
 template <typename T, int kThreads, bool kMask, bool kWhole, bool kPlain>
-__global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
+__device__ __forceinline__ void input_block(const InputArgs& g, int32_t block, int32_t blocks, Chunk* s_stage)
 {
     typedef InputSource<T, kThreads, kMask, kWhole, kPlain> Source;
     typedef typename Source::Tiles Tiles;
-    __shared__ Chunk s_stage[3 * Tiles::kStage];
     const BackwardArgs& a = g.a;
     const int64_t rows = a.count.get();
     if (rows <= 0) return;
     // a block's tiles: of those that have rows, every `stride`-th of its XCD's; where hdim is split, a split of one
-    const int32_t blocks = (int32_t) gridDim.x, stride = kPlain ? blocks / g.splits : blocks, at = xcd_run((int32_t) blockIdx.x, blocks);
+    const int32_t stride = kPlain ? blocks / g.splits : blocks, at = xcd_run(block, blocks);
     const int32_t split = kPlain ? at / stride : 0, first = kPlain ? at - split * stride : at;
     const int32_t m_tiles = (int32_t) ((rows + Tiles::kM - 1) / Tiles::kM), all = m_tiles * g.n_tiles;
     const int32_t tiles = first < all ? (all - first + stride - 1) / stride : 0;
@@ -731,6 +736,25 @@ __global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
                     if (whole || (r0 + m0 + Tiles::row_step(i, v) < rows && k0 + n + 32 * j < K)) row[32 * j] = from_float<T>(tile.acc[i][j][v]);
             }
     });
+}
+
+template <typename T, int kThreads, bool kMask, bool kWhole, bool kPlain>
+__global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
+{
+    __shared__ Chunk s_stage[3 * InputTile<T, kThreads>::Type::kStage];
+    input_block<T, kThreads, kMask, kWhole, kPlain>(g, (int32_t) blockIdx.x, (int32_t) gridDim.x, s_stage);
+}
+
+// Both products of a small call in one launch, since neither waits for the other: the grid's first blocks are dw's.  fp32, 64 rows
+// of 256 x 256: 9 us, one after the other 17; 1772 rows of 400 x 18 bf16 15.6 and 24; 300 of 1000 x 1000 32 and 44.
+template <typename T, bool kMask, bool kWhole, bool kPairs>
+__global__ void __launch_bounds__(256, 2) k_backward_both(WeightsArgs g, InputArgs h, int32_t weights_blocks)
+{
+    constexpr int kWeights = WeightsTile<T, 256>::Type::kStage, kInput = InputTile<T, 256>::Type::kStage, kStage = kWeights > kInput ? kWeights : kInput;
+    __shared__ Chunk s_stage[3 * kStage];
+    const int32_t block = (int32_t) blockIdx.x;
+    if (block < weights_blocks) weights_block<T, 256, kMask, kPairs>(g, block, s_stage);
+    else                        input_block<T, 256, kMask, kWhole, true>(h, block - weights_blocks, (int32_t) gridDim.x - weights_blocks, s_stage);
 }
 
 // k_backward_few: dx of up to sixteen rows, where W's bytes are all there is to do.  A block has 16 columns of dx (rows of W) and
@@ -961,6 +985,28 @@ static hipError_t launch_input(const gns_ctx* c, InputArgs g, hipStream_t s)
 }
 
 template <typename T>
+static hipError_t launch_both(const WeightsArgs& g, InputArgs h, hipStream_t s)
+{
+    const int64_t tiles = input_tiles<T, 256>(h.a, &h.m_tiles, &h.n_tiles), blocks = (int64_t) g.m_tiles * g.n_tiles * g.splits;
+    if (too_many(blocks + tiles * h.splits, 256)) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned) (blocks + tiles * h.splits)), block(256);
+    const int32_t first = (int32_t) blocks;
+    const bool whole = g.a.hdim % 8 == 0;
+    if constexpr (sizeof(T) == 2) {
+        if (!reads_pairs(g.a.d_out)) {
+            if (g.a.positive) hipLaunchKernelGGL((k_backward_both<T, true, false, false>), grid, block, 0, s, g, h, first);
+            else              hipLaunchKernelGGL((k_backward_both<T, false, false, false>), grid, block, 0, s, g, h, first);
+            return hipGetLastError();
+        }
+    }
+    if (g.a.positive && whole)  hipLaunchKernelGGL((k_backward_both<T, true, true, true>), grid, block, 0, s, g, h, first);
+    else if (g.a.positive)      hipLaunchKernelGGL((k_backward_both<T, true, false, true>), grid, block, 0, s, g, h, first);
+    else if (whole)             hipLaunchKernelGGL((k_backward_both<T, false, true, true>), grid, block, 0, s, g, h, first);
+    else                        hipLaunchKernelGGL((k_backward_both<T, false, false, true>), grid, block, 0, s, g, h, first);
+    return hipGetLastError();
+}
+
+template <typename T>
 static hipError_t launch_few(const BackwardArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned) ((a.x1.width + a.x2.width + kFewColumns - 1) / kFewColumns)), block(kFewBlock);
@@ -990,17 +1036,18 @@ struct InputPlan {
 };
 // Blocks of 512 threads where they fill half the chip and layers are not too narrow for them (fp32, dw too, 2400 rows of 1000 x 1000:
 // 78 us, 99 with 256 threads; 600 rows of 4096 x 4096: 237 and 338; with less than half 1400 rows: no difference, bf16 3000: 81
-// and 73).  Else of 256, and with no more of them than CUs W is read as it is.
+// and 73).  Else of 256, and W is read as it is by no more of them than CUs, or than run at once where dw goes with them (fp32, 6000
+// rows of 256 x 256: 26 us, 36 with W cut in a launch between).
 template <typename T>
-static InputPlan plan_input(const gns_ctx* c, const BackwardArgs& a)
+static InputPlan plan_input(const gns_ctx* c, const BackwardArgs& a, bool both)
 {
     typedef typename InputTile<T, 512>::Type Wide;
     int32_t m_tiles, n_tiles;
     if (a.hdim < kNarrow) return {Way::kNarrow, 1};
-    if (a.count.rows <= kFewRows) return {Way::kFew, 1};
+    if (a.count.rows <= kFewRows && !both) return {Way::kFew, 1};
     if (input_tiles<T, 512>(a, &m_tiles, &n_tiles) * 2 >= c->num_cus && a.x1.width + a.x2.width > Wide::kN / 2) return {Way::kWide, 1};
     const int64_t tiles = input_tiles<T, 256>(a, &m_tiles, &n_tiles);
-    return tiles <= c->num_cus ? InputPlan{Way::kPlain, input_splits<T>(c, tiles, a.hdim)} : InputPlan{Way::kCut, 1};
+    return tiles <= (int64_t) c->num_cus * (both ? 2 : 1) ? InputPlan{Way::kPlain, input_splits<T>(c, tiles, a.hdim)} : InputPlan{Way::kCut, 1};
 }
 
 size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows)
@@ -1014,7 +1061,7 @@ size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim
     }
     BackwardArgs a = {};
     a.x1.width = f1; a.x2.width = f2; a.hdim = hdim; a.count.rows = rows;
-    const int32_t splits = max(plan_input<float>(c, a).splits, plan_input<Bf16>(c, a).splits);
+    const int32_t splits = max(plan_input<float>(c, a, true).splits, plan_input<Bf16>(c, a, true).splits);     // which few rows may take or not
     return parts + max(align256(3 * k * pitch * 2), splits > 1 ? align256((size_t) splits * (size_t) rows * k * 4) : 0);
 }
 
@@ -1035,24 +1082,27 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     char* at = static_cast<char*>(a.workspace);
     BetweenArgs b = {};
     b.k = K;
-    if (a.dw) {
-        const WeightsPlan p = plan_weights(c, a.x1.width, a.x2.width, a.hdim, a.count.rows, kFloat, kFloat || reads_pairs(a.d_out));
-        WeightsArgs g = {a, p.m_tiles, p.n_tiles, p.splits, p.db_shares, a.dw, a.db};
-        if (p.splits > 1) {
-            g.dw = reinterpret_cast<float*>(at);
-            at += align256((size_t) p.splits * (size_t) K * (size_t) a.hdim * 4);
-            b.dw = join_of(c, g.dw, a.dw, (int64_t) K * a.hdim, p.splits);
-        }
-        if (a.db && p.splits * p.db_shares > 1) {
-            g.db = reinterpret_cast<float*>(at);
-            at += align256((size_t) p.splits * (size_t) p.db_shares * (size_t) a.hdim * 4);
-            b.db = join_of(c, g.db, a.db, a.hdim, p.splits * p.db_shares);
-        }
-        const hipError_t e = p.wide ? launch_weights<T, 512>(g, s) : launch_weights<T, 256>(g, s);
-        if (e != hipSuccess) return e;
-    }
     const bool dx = a.dx.data && a.count.rows;
-    const InputPlan p = dx ? plan_input<T>(c, a) : InputPlan{Way::kFew, 1};
+    WeightsPlan pw = {};
+    WeightsArgs gw = {};
+    if (a.dw) {
+        pw = plan_weights(c, a.x1.width, a.x2.width, a.hdim, a.count.rows, kFloat, kFloat || reads_pairs(a.d_out));
+        gw = {a, pw.m_tiles, pw.n_tiles, pw.splits, pw.db_shares, a.dw, a.db};
+        if (pw.splits > 1) {
+            gw.dw = reinterpret_cast<float*>(at);
+            at += align256((size_t) pw.splits * (size_t) K * (size_t) a.hdim * 4);
+            b.dw = join_of(c, gw.dw, a.dw, (int64_t) K * a.hdim, pw.splits);
+        }
+        if (a.db && pw.splits * pw.db_shares > 1) {
+            gw.db = reinterpret_cast<float*>(at);
+            at += align256((size_t) pw.splits * (size_t) pw.db_shares * (size_t) a.hdim * 4);
+            b.db = join_of(c, gw.db, a.db, a.hdim, pw.splits * pw.db_shares);
+        }
+    }
+    // dw and dx in one launch where both have blocks of 256 threads and dx takes W as it is
+    const bool may_both = dx && a.dw && !pw.wide;
+    const InputPlan p = dx ? plan_input<T>(c, a, may_both) : InputPlan{Way::kFew, 1};
+    const bool both = may_both && p.way == Way::kPlain;
     if (dx && (p.way == Way::kCut || p.way == Way::kWide)) {
         b.w = a.w;
         b.terms = reinterpret_cast<uint16_t*>(at);
@@ -1066,12 +1116,15 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
         b.dx_type = kFloat ? GNS_FP32 : GNS_BF16;
         b.dx_splits = p.splits;
         b.dx_blocks = (int32_t) grid_of(c, (int64_t) a.count.rows * K);
-        const hipError_t e = launch_input<T, 256, true>(c, g, s);             // in front of the sums
-        if (e != hipSuccess) return e;
     }
+    hipError_t e = hipSuccess;
+    if (both)      e = launch_both<T>(gw, g, s);
+    else if (a.dw) e = pw.wide ? launch_weights<T, 512>(gw, s) : launch_weights<T, 256>(gw, s);
+    if (e == hipSuccess && p.splits > 1 && !both) e = launch_input<T, 256, true>(c, g, s);      // in front of the sums
+    if (e != hipSuccess) return e;
     const int32_t blocks = b.db.blocks + b.dw.blocks + b.dx_blocks + b.term_blocks;
     if (blocks) hipLaunchKernelGGL(k_backward_between, dim3((unsigned) blocks), dim3(kBlock), 0, s, b);
-    if (!dx || p.splits > 1) return hipGetLastError();
+    if (!dx || p.splits > 1 || both) return hipGetLastError();
     switch (p.way) {
     case Way::kNarrow: return launch_narrow<T>(c, a, s);
     case Way::kFew:    return launch_few<T>(a, s);
