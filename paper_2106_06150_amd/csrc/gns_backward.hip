@@ -746,7 +746,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
 }
 
 // Both products of a small call in one launch, since neither waits for the other: the grid's first blocks are dw's.  fp32, 64 rows
-// of 256 x 256: 9 us, one after the other 17; 1772 rows of 400 x 18 bf16 15.6 and 24; 300 of 1000 x 1000 32 and 44.
+// of 256 x 256: 9 us, one after the other 17; 1772 rows of 400 x 18 bf16 15.6 and 24; 300 of 1000 x 1000 21 and 44.
 template <typename T, bool kMask, bool kWhole, bool kPairs>
 __global__ void __launch_bounds__(256, 2) k_backward_both(WeightsArgs g, InputArgs h, int32_t weights_blocks)
 {
@@ -1037,7 +1037,7 @@ struct InputPlan {
 // Blocks of 512 threads where they fill half the chip and layers are not too narrow for them (fp32, dw too, 2400 rows of 1000 x 1000:
 // 78 us, 99 with 256 threads; 600 rows of 4096 x 4096: 237 and 338; with less than half 1400 rows: no difference, bf16 3000: 81
 // and 73).  Else of 256, and W is read as it is by no more of them than CUs, or than run at once where dw goes with them (fp32, 6000
-// rows of 256 x 256: 26 us, 36 with W cut in a launch between).
+// rows of 256 x 256: 24 us, 36 with W cut in a launch between).
 template <typename T>
 static InputPlan plan_input(const gns_ctx* c, const BackwardArgs& a, bool both)
 {
@@ -1048,6 +1048,35 @@ static InputPlan plan_input(const gns_ctx* c, const BackwardArgs& a, bool both)
     if (input_tiles<T, 512>(a, &m_tiles, &n_tiles) * 2 >= c->num_cus && a.x1.width + a.x2.width > Wide::kN / 2) return {Way::kWide, 1};
     const int64_t tiles = input_tiles<T, 256>(a, &m_tiles, &n_tiles);
     return tiles <= (int64_t) c->num_cus * (both ? 2 : 1) ? InputPlan{Way::kPlain, input_splits<T>(c, tiles, a.hdim)} : InputPlan{Way::kCut, 1};
+}
+
+// Splits where dw and dx go together: steps a block, four for dw and two turns for dx at least, such that all blocks run at once.
+// fp32, 1104 rows of 128 x 2048: 24 us, with dw and dx each split for a chip of its own 28; 400 of 200 x 700: 16 and 22; bf16, 189 of
+// 2141 x 1102: 22 and 30.
+template <typename T>
+static int32_t both_least() { return 2 * (sizeof(T) == 4 ? 4 : 2); }
+template <typename T>
+static void plan_both(const gns_ctx* c, const BackwardArgs& a, WeightsPlan* weights, InputPlan* input)
+{
+    int32_t m_tiles, n_tiles;
+    const int64_t dw_tiles = (int64_t) weights->m_tiles * weights->n_tiles, dx_tiles = input_tiles<T, 256>(a, &m_tiles, &n_tiles);
+    const int32_t dw_steps = (a.count.rows + kStageK - 1) / kStageK, dx_steps = (a.hdim + kStageK - 1) / kStageK;
+    for (int32_t each = 4;; each += each / 4) {
+        const int32_t dx_each = each > both_least<T>() ? each : both_least<T>();
+        weights->splits = (dw_steps + each - 1) / each;
+        input->splits = dx_steps >= 2 * dx_each ? dx_steps / dx_each : 1;
+        if (weights->splits * dw_tiles + input->splits * dx_tiles <= (int64_t) c->num_cus * 2 || (weights->splits == 1 && input->splits == 1)) break;
+    }
+    weights->db_shares = weights->splits == 1 && a.count.rows <= 512 ? 1 : weights->m_tiles;
+}
+
+// The most splits of hdim that a call may take.
+template <typename T>
+static int32_t most_input_splits(const gns_ctx* c, const BackwardArgs& a)
+{
+    int32_t m_tiles, n_tiles;
+    const int64_t tiles = input_tiles<T, 256>(a, &m_tiles, &n_tiles), s = min((int64_t) c->num_cus * 2 / max(tiles, (int64_t) 1), (int64_t) (a.hdim + kStageK - 1) / kStageK / both_least<T>());
+    return s < 2 ? 1 : (int32_t) s;
 }
 
 size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows)
@@ -1061,7 +1090,7 @@ size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim
     }
     BackwardArgs a = {};
     a.x1.width = f1; a.x2.width = f2; a.hdim = hdim; a.count.rows = rows;
-    const int32_t splits = max(plan_input<float>(c, a, true).splits, plan_input<Bf16>(c, a, true).splits);     // which few rows may take or not
+    const int32_t splits = max(most_input_splits<float>(c, a), most_input_splits<Bf16>(c, a));
     return parts + max(align256(3 * k * pitch * 2), splits > 1 ? align256((size_t) splits * (size_t) rows * k * 4) : 0);
 }
 
@@ -1084,25 +1113,23 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     b.k = K;
     const bool dx = a.dx.data && a.count.rows;
     WeightsPlan pw = {};
-    WeightsArgs gw = {};
-    if (a.dw) {
-        pw = plan_weights(c, a.x1.width, a.x2.width, a.hdim, a.count.rows, kFloat, kFloat || reads_pairs(a.d_out));
-        gw = {a, pw.m_tiles, pw.n_tiles, pw.splits, pw.db_shares, a.dw, a.db};
-        if (pw.splits > 1) {
-            gw.dw = reinterpret_cast<float*>(at);
-            at += align256((size_t) pw.splits * (size_t) K * (size_t) a.hdim * 4);
-            b.dw = join_of(c, gw.dw, a.dw, (int64_t) K * a.hdim, pw.splits);
-        }
-        if (a.db && pw.splits * pw.db_shares > 1) {
-            gw.db = reinterpret_cast<float*>(at);
-            at += align256((size_t) pw.splits * (size_t) pw.db_shares * (size_t) a.hdim * 4);
-            b.db = join_of(c, gw.db, a.db, a.hdim, pw.splits * pw.db_shares);
-        }
-    }
+    if (a.dw) pw = plan_weights(c, a.x1.width, a.x2.width, a.hdim, a.count.rows, kFloat, kFloat || reads_pairs(a.d_out));
     // dw and dx in one launch where both have blocks of 256 threads and dx takes W as it is
     const bool may_both = dx && a.dw && !pw.wide;
-    const InputPlan p = dx ? plan_input<T>(c, a, may_both) : InputPlan{Way::kFew, 1};
+    InputPlan p = dx ? plan_input<T>(c, a, may_both) : InputPlan{Way::kFew, 1};
     const bool both = may_both && p.way == Way::kPlain;
+    if (both) plan_both<T>(c, a, &pw, &p);
+    WeightsArgs gw = {a, pw.m_tiles, pw.n_tiles, pw.splits, pw.db_shares, a.dw, a.db};
+    if (a.dw && pw.splits > 1) {
+        gw.dw = reinterpret_cast<float*>(at);
+        at += align256((size_t) pw.splits * (size_t) K * (size_t) a.hdim * 4);
+        b.dw = join_of(c, gw.dw, a.dw, (int64_t) K * a.hdim, pw.splits);
+    }
+    if (a.dw && a.db && pw.splits * pw.db_shares > 1) {
+        gw.db = reinterpret_cast<float*>(at);
+        at += align256((size_t) pw.splits * (size_t) pw.db_shares * (size_t) a.hdim * 4);
+        b.db = join_of(c, gw.db, a.db, a.hdim, pw.splits * pw.db_shares);
+    }
     if (dx && (p.way == Way::kCut || p.way == Way::kWide)) {
         b.w = a.w;
         b.terms = reinterpret_cast<uint16_t*>(at);
