@@ -2,8 +2,9 @@
 //   dz = d_out where the output was positive,  dw = X^T dz,  db = sum_r dz,  dx = dz W^T.
 // Both products run on the bf16 matrix cores at fp32's precision.  A checkpoint's values q * 2^e are bf16 values as they are.
 // An fp32 value is cut into three bf16 terms of eight bits each, which hold it exactly: so dw takes three products of fp32
-// gradients and one of bf16 ones, and is exact up to the fp32 sums.  dx of fp32 gradients takes the six products of terms that
-// are not below 2^-23 of the largest; dx of bf16 gradients, itself rounded to bf16, takes W in two terms (2^-16).
+// gradients and one of bf16 ones, and is exact up to the fp32 sums.  dx of bf16 gradients takes three products with W's terms and
+// is as exact (two terms of W moved single bf16 results: 2.1e-4 of dx's 2-norm from the fp32 products' at hdim 4096, three 1.6e-5, and
+// save 14 % of a large call); dx of fp32 gradients takes the six products of terms that are not below 2^-23 of the largest.
 #include "gns_learn.hpp"
 
 namespace gns {
@@ -39,7 +40,6 @@ __device__ __forceinline__ uint32_t row_broadcast(uint32_t old, uint32_t v)
 // The products of terms: which term of the left factor meets which of the right, the smallest first.
 template <int NA, int NB> struct Pairs;
 template <> struct Pairs<1, 1> { static constexpr int kCount = 1, kA[1] = {0}, kB[1] = {0}; };
-template <> struct Pairs<1, 2> { static constexpr int kCount = 2, kA[2] = {0, 0}, kB[2] = {1, 0}; };
 template <> struct Pairs<1, 3> { static constexpr int kCount = 3, kA[3] = {0, 0, 0}, kB[3] = {2, 1, 0}; };
 template <> struct Pairs<3, 3> { static constexpr int kCount = 6, kA[6] = {2, 0, 1, 1, 0, 0}, kB[6] = {0, 2, 1, 0, 1, 0}; };
 
@@ -447,7 +447,7 @@ struct BetweenArgs {
     const float* w;
     uint16_t* terms;
     int64_t k;
-    int32_t hdim, pitch, planes, term_blocks;
+    int32_t hdim, pitch, term_blocks;
 };
 
 // Values i .. i + 3 of n; marks: they are one read.
@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(kBlock) k_backward_between(BetweenArgs a)
         const int64_t row = t / fours, c = (t - row * fours) * 4;
         const float4 four = load_four(a.w + row * a.hdim, c, a.hdim, marks);
         float v[4] = {four.x, four.y, four.z, four.w};
-        for (int p = 0; p < a.planes; ++p) {
+        for (int p = 0; p < 3; ++p) {
             uint32_t u[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -550,11 +550,11 @@ __device__ __forceinline__ uint32_t columns_left(uint32_t kept, uint32_t bits) {
 template <typename T, int kThreads> struct InputTile;
 template <> struct InputTile<float, 512> { typedef Tile<128, 128, 64, 32, 3, 3> Type; };
 template <> struct InputTile<float, 256> { typedef Tile<64, 64, 32, 32, 3, 3> Type; };
-template <> struct InputTile<Bf16, 512> { typedef Tile<256, 128, 64, 64, 1, 2> Type; };
-template <> struct InputTile<Bf16, 256> { typedef Tile<128, 128, 64, 64, 1, 2> Type; };
+template <> struct InputTile<Bf16, 512> { typedef Tile<256, 128, 64, 64, 1, 3> Type; };
+template <> struct InputTile<Bf16, 256> { typedef Tile<128, 64, 64, 32, 1, 3> Type; };
 
-// 85,000 rows, 256 x 256, fp32: 78 us (six products of terms; 0.86 PFLOP/s of them); 16,384 rows, 4096 x 4096, bf16: 955 to 995 us
-// (two products; 1.1 to 1.15 PFLOP/s, the matrix cores busy in 69 % of the cycles at the 1.5 GHz that the power leaves).
+// 85,000 rows, 256 x 256, fp32: 78 us (six products of terms; 0.86 PFLOP/s of them); 16,384 rows, 4096 x 4096, bf16, masked, and dw:
+// 2070 us (three products here, one there).
 // A thread reads eight columns of a row of dz (of two rows of bf16), and as many of W's planes.  kWhole: hdim is a multiple of
 // eight.  Chunks past the last are read as the last: W's planes are zero there.  Else a row's last chunk is its last eight
 // columns, for dz as for W, and those that the chunk before has are left out of dz.  hdim is eight at least.
@@ -565,9 +565,9 @@ template <typename T, int kThreads, bool kMask, bool kWhole, bool kPlain>
 struct InputSource {
     typedef typename InputTile<T, kThreads>::Type Tiles;
     static constexpr bool kFloat = sizeof(T) == 4;
-    static constexpr int kPlanes = kFloat ? 3 : 2, kStep = kThreads / 4;                            // rows the threads cover at once
+    static constexpr int kPlanes = 3, kStep = kThreads / 4;                                         // rows the threads cover at once
     static constexpr int kRowsA = Tiles::kM / kStep, kRowsB = Tiles::kN / kStep, kWords = kFloat ? 8 : 4;
-    static constexpr int kSets = (kFloat ? kPlain : kThreads == 512) ? 4 : 2, kReadsB = kPlain ? 1 : kPlanes;
+    static constexpr int kSets = kFloat && kPlain ? 4 : 2, kReadsB = kPlain ? 1 : kPlanes;
     static constexpr bool kKeeps = kMask || !kWhole;          // dz has columns left out
     static constexpr int kFetches = kRowsA * (1 + (kMask ? 1 : 0)) + kRowsB * kReadsB;
     static constexpr int kPutsA = (kKeeps ? 1 : 0) + (kFloat ? 3 : 1), kPuts = kRowsA * kPutsA + kRowsB * kPlanes;
@@ -767,7 +767,7 @@ template <typename T, bool kMask>
 __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
 {
     constexpr bool kFloat = sizeof(T) == 4;
-    constexpr int kTermsA = kFloat ? 3 : 1, kTermsB = kFloat ? 3 : 2, kSets = 4;
+    constexpr int kTermsA = kFloat ? 3 : 1, kTermsB = 3, kSets = 4;
     typedef Pairs<kTermsA, kTermsB> P;
     __shared__ float s_sum[kFewWaves][4][kWave];
     const int32_t rows = a.count.get(), K = a.x1.width + a.x2.width, hdim = a.hdim, steps = (hdim + 31) / 32;
@@ -1133,7 +1133,7 @@ static hipError_t launch_typed(const gns_ctx* c, const BackwardArgs& a, hipStrea
     if (dx && (p.way == Way::kCut || p.way == Way::kWide)) {
         b.w = a.w;
         b.terms = reinterpret_cast<uint16_t*>(at);
-        b.hdim = a.hdim; b.pitch = (int32_t) pitch; b.planes = kFloat ? 3 : 2;
+        b.hdim = a.hdim; b.pitch = (int32_t) pitch;
         b.term_blocks = (int32_t) grid_of(c, K * (pitch / 4));
     }
     InputArgs g = {a, 0, 0, (int32_t) pitch, p.splits, b.terms, nullptr};
