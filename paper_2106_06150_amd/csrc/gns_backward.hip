@@ -37,6 +37,43 @@ __device__ __forceinline__ uint32_t row_broadcast(uint32_t old, uint32_t v)
     return (uint32_t) __builtin_amdgcn_update_dpp((int) old, (int) v, 0x150 + kLane, 0xf, kBanks, false);
 }
 
+// ---- sums that are not finite --------------------------------------------------------------------------------------
+// The terms of an infinity do not add up to it, and what only fills a tile (zeros times repeated rows) makes NaN of one.  A sum
+// that is not finite is therefore computed once more by a thread alone, with plain fp32 products; a NaN ends it.
+__device__ __forceinline__ bool is_finite(float v) { return fabsf(v) < __builtin_inff(); }
+
+// dz[r, n]
+template <typename T, bool kMask>
+__device__ __forceinline__ float masked_at(const BackwardArgs& a, int64_t r, int32_t n)
+{
+    if (kMask && !(a.positive[r * ((a.hdim + 31) / 32) + n / 32] >> (n & 31) & 1u)) return 0.f;
+    return load_at<T>(a.d_out, r, n);
+}
+
+// dx[r, k] of columns `begin` to `end` of dz
+template <typename T, bool kMask>
+__device__ __forceinline__ float input_again(const BackwardArgs& a, int64_t r, int32_t k, int32_t begin, int32_t end)
+{
+    const float* w = a.w + (int64_t) k * a.hdim;
+    float sum = 0.f;
+    for (int32_t n = begin; n < end && sum == sum; ++n) sum = fmaf(masked_at<T, kMask>(a, r, n), w[n], sum);
+    return sum;
+}
+
+// dw[k, n] of rows `begin` to `end`
+template <typename T, bool kMask>
+__device__ __forceinline__ float weight_again(const BackwardArgs& a, int32_t k, int32_t n, int64_t begin, int64_t end)
+{
+    const PackedRows& x = k < a.x1.width ? a.x1 : a.x2;
+    const int32_t c = k < a.x1.width ? k : k - a.x1.width;
+    float sum = 0.f;
+    for (int64_t r = begin; r < end && sum == sum; ++r) {
+        const float scale = __uint_as_float((uint32_t) x.exponents[r * x.groups + c / 32] << 23);
+        sum = fmaf((float) x.q[r * x.groups * 32 + c] * scale, masked_at<T, kMask>(a, r, n), sum);
+    }
+    return sum;
+}
+
 // The products of terms: which term of the left factor meets which of the right, the smallest first.
 template <int NA, int NB> struct Pairs;
 template <> struct Pairs<1, 1> { static constexpr int kCount = 1, kA[1] = {0}, kB[1] = {0}; };
@@ -157,6 +194,10 @@ struct Tile {
         return __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)) % (BN / WN) * WN + (lane & 31);
     }
     static constexpr int row_step(int i, int v) { return i * 32 + 8 * (v >> 2) + (v & 3); }
+    // the same for outputs numbered 0 .. kOutputs - 1 in a loop that is not unrolled
+    static constexpr int kOutputs = MI * 16 * NI;
+    static __device__ __forceinline__ int row_of(int e) { return row_step(e / (16 * NI), e / NI % 16); }
+    static __device__ __forceinline__ int column_step(int e) { return e % NI; }
 };
 
 // ---- dw and db ----------------------------------------------------------------------------------------------------
@@ -395,6 +436,8 @@ __device__ __forceinline__ void weights_block(const WeightsArgs& g, int32_t bloc
     float* dw = g.dw + (int64_t) split * (a.x1.width + a.x2.width) * a.hdim;
     tile.run(source, (int32_t) ((end - first + kRound - 1) / kRound) * Source::kSets, 1, [&](int32_t) {
         const int lane = opaque_lane_id(), m0 = Tiles::first_row(lane), n = Tiles::first_column(lane);
+        auto column_of = [&](int j) { return sizeof(T) == 4 ? n + 32 * j : pair_column(n + 32 * j); };
+        float any = 0.f;                                      // NaN if a sum is not finite
 #pragma unroll
         for (int i = 0; i < Tiles::MI; ++i)
 #pragma unroll
@@ -404,10 +447,18 @@ __device__ __forceinline__ void weights_block(const WeightsArgs& g, int32_t bloc
                 float* row = dw + (int64_t) k * a.hdim + n0;
 #pragma unroll
                 for (int j = 0; j < Tiles::NI; ++j) {
-                    const int32_t c = sizeof(T) == 4 ? n + 32 * j : pair_column(n + 32 * j);
-                    if (n0 + c < a.hdim) row[c] = tile.acc[i][j][v];
+                    any = fmaf(tile.acc[i][j][v], 0.f, any);
+                    if (n0 + column_of(j) < a.hdim) row[column_of(j)] = tile.acc[i][j][v];
                 }
             }
+        if (any == 0.f) return;
+#pragma unroll 1
+        for (int e = 0; e < Tiles::kOutputs; ++e) {           // those in place that are not
+            const int32_t k = weight_row(a, c0 + quad_column(m0 + Tiles::row_of(e))), c = n0 + column_of(Tiles::column_step(e));
+            if (k < 0 || c >= a.hdim) continue;
+            float* at = dw + (int64_t) k * a.hdim + c;
+            if (!is_finite(*at)) *at = weight_again<T, kMask>(a, k, c, first, end);
+        }
     });
     if (!g.db || tm >= g.db_shares) return;
     float* s_sum = reinterpret_cast<float*>(s_stage);         // [4][Tiles::kN]: of the four threads that read a column
@@ -714,6 +765,24 @@ __device__ __forceinline__ void input_block(const InputArgs& g, int32_t block, i
         const int32_t k0 = tn * Tiles::kN;
         const int lane = opaque_lane_id(), m0 = Tiles::first_row(lane), n = Tiles::first_column(lane);
         const bool whole = r0 + Tiles::kM <= rows && k0 + Tiles::kN <= K;
+        float any = 0.f;                                      // NaN if a sum is not finite
+#pragma unroll
+        for (int i = 0; i < Tiles::MI; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+#pragma unroll
+                for (int j = 0; j < Tiles::NI; ++j) any = fmaf(tile.acc[i][j][v], 0.f, any);
+        // outputs in place that are not finite, of columns `begin` to `end`
+        auto again = [&](auto* at, int64_t stride, int32_t begin, int32_t end, auto&& value, auto&& make) {
+#pragma unroll 1
+            for (int e = 0; e < Tiles::kOutputs; ++e) {
+                const int32_t k = k0 + n + 32 * Tiles::column_step(e);
+                const int64_t r = r0 + m0 + Tiles::row_of(e);
+                if (r >= rows || k >= K) continue;
+                auto* to = at + (int64_t) Tiles::row_of(e) * stride + 32 * Tiles::column_step(e);
+                if (!is_finite(value(*to))) *to = make(input_again<T, kMask>(a, r, k, begin, end));
+            }
+        };
         if (kPlain && g.parts) {
             float* part = g.parts + ((int64_t) split * a.count.rows + r0 + m0) * K + k0 + n;
 #pragma unroll
@@ -723,6 +792,7 @@ __device__ __forceinline__ void input_block(const InputArgs& g, int32_t block, i
 #pragma unroll
                     for (int j = 0; j < Tiles::NI; ++j)
                         if (whole || (r0 + m0 + Tiles::row_step(i, v) < rows && k0 + n + 32 * j < K)) part[(int64_t) Tiles::row_step(i, v) * K + 32 * j] = tile.acc[i][j][v];
+            if (any != 0.f) again(part, K, source.begin, min(source.end, a.hdim), [](float v) { return v; }, [](float v) { return v; });
             return;
         }
         T* first = out + (r0 + m0) * a.dx.stride + k0 + n;
@@ -735,6 +805,7 @@ __device__ __forceinline__ void input_block(const InputArgs& g, int32_t block, i
                 for (int j = 0; j < Tiles::NI; ++j)
                     if (whole || (r0 + m0 + Tiles::row_step(i, v) < rows && k0 + n + 32 * j < K)) row[32 * j] = from_float<T>(tile.acc[i][j][v]);
             }
+        if (any != 0.f) again(first, a.dx.stride, 0, a.hdim, [](T v) { return to_float(v); }, [](float v) { return from_float<T>(v); });
     });
 }
 
@@ -833,6 +904,7 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
     float sum = 0.f;
 #pragma unroll
     for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][v][l];
+    if (!is_finite(sum)) sum = input_again<T, kMask>(a, r, k, 0, hdim);
     store_at<T>(a.dx, r, k, sum);
 }
 
@@ -861,13 +933,16 @@ __global__ void __launch_bounds__(kBlock) k_backward_narrow(BackwardArgs a, int3
             const uint32_t keep = kMask ? a.positive[r] : ~0u;
             float z[kNarrow - 1];
 #pragma unroll
-            for (int n = 0; n < kNarrow - 1; ++n) z[n] = load_at<T>(a.d_out, r, n < hdim ? n : 0);
+            for (int n = 0; n < kNarrow - 1; ++n) {
+                const float v = load_at<T>(a.d_out, r, n < hdim ? n : 0);
+                z[n] = __uint_as_float(__float_as_uint(v) & spread_bit(keep, n));
+            }
             struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float sum = 0.f;
 #pragma unroll
-                for (int n = 0; n < kNarrow - 1; ++n) sum = n < hdim && (keep >> n & 1u) ? fmaf(z[n], w[j][n], sum) : sum;
+                for (int n = 0; n < kNarrow - 1; ++n) sum = n < hdim ? fmaf(z[n], w[j][n], sum) : sum;
                 y.v[j] = from_float<T>(sum);
             }
             if (row >= rows || k >= K) continue;

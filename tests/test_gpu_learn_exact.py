@@ -71,3 +71,73 @@ def test_input_gradient_sees_every_bit_of_the_weights(ctx, rows, f1, f2, hdim, d
     want = (sign.cuda() @ low.cuda().t().contiguous()).double()          # small integers times 2^-23: exact
     bound = 16 * 2.0 ** -22 + (2.0 ** -8 * want.abs() if dtype == BF16 else 0.0)
     within(f64(dx), f64(want), bound if isinstance(bound, float) else f64(bound))
+
+
+def times(a, b):
+    """a @ b in 64 bits, with each product's infinities and NaN."""
+    y = a @ b
+    odd_rows, odd_cols = ~np.isfinite(a).all(1), ~np.isfinite(b).all(0)
+    with np.errstate(invalid="ignore"):
+        for r in np.flatnonzero(odd_rows):
+            y[r] = (a[r][:, None] * b).sum(0)
+        for c in np.flatnonzero(odd_cols):
+            y[:, c] = (a * b[:, c][None, :]).sum(1)
+    return y
+
+
+@TYPES
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("rows,f1,f2,hdim,dw", [s for s in WAYS if s[0] < 10000] + [(33000, 100, 0, 72, True), (17, 300, 0, 64, True)])
+def test_backward_of_infinities(ctx, rows, f1, f2, hdim, dw, masked, dtype):
+    """Infinities and NaN in d_out, the weights and the inputs go where the formulas take them, whatever kernel runs: an infinity stays
+    one unless it meets a zero or its opposite."""
+    k = f1 + f2
+    g = gen("inf", rows, k, hdim)
+    d_out, w, x = torch.randn(rows, hdim, generator=g).to(dtype), torch.randn(k, hdim, generator=g), torch.randn(rows, k, generator=g)
+    x[torch.rand(rows, k, generator=g) < 0.3] = 0.0
+    big = torch.finfo(dtype).max
+    d_out[0, 0], d_out[rows // 2, hdim - 1], d_out[rows - 1, hdim // 2] = math.inf, -math.inf, math.inf
+    if rows > 8:
+        d_out[3, 1], d_out[5, 2], d_out[6, 1], d_out[7, 0] = math.nan, math.inf, -math.inf, -math.inf
+    w[k // 2, hdim // 3], w[k - 1, 0] = math.inf, -math.inf
+    if k > 40:
+        w[3, hdim - 1], w[39, 1] = math.nan, math.inf
+        w[39, 2] = math.inf
+    if rows > 20 and dw:
+        x[9, 1] = math.nan                               # spoils a group of its row
+    mask = torch.rand(rows, hdim, generator=g) < 0.6
+    if masked:
+        mask[0, 0] = mask[rows - 1, hdim // 2] = True
+        if rows > 8:
+            mask[5, 2] = False
+    one, two = two_checkpoints(ctx, x, f1, f2) if dw else (None, None)
+    for value in (None, big):
+        if value is not None:                            # large values, whose sums do not overflow
+            d_out = torch.where(torch.isfinite(d_out), d_out, torch.zeros_like(d_out))
+            d_out[0, 0] = d_out[rows - 1, hdim // 2] = value
+            w = torch.where(torch.isfinite(w), w, torch.zeros_like(w)).clamp(-3, 3) / 64
+        got_dw, db, dx = backward(ctx, d_out.cuda(), words_of(mask).cuda() if masked else None, one, f1, two, f2, w.cuda(), dw, True)
+        dz = np.where(mask.numpy() if masked else True, f64(d_out), 0.0)
+        w64 = f64(w)
+        with np.errstate(invalid="ignore", over="ignore"):
+            want, size = times(dz, w64.T.copy()), np.abs(dz) @ np.abs(w64).T
+            size[~np.isfinite(want)] = 0.0
+            limit = float(torch.finfo(dtype).max)
+            want = np.where(np.abs(want) > limit, np.sign(want) * np.inf, want)
+            bound = (hdim + 8) * 2 * U * size + (2.0 ** -8 * np.abs(want) if dtype == BF16 else 0.0) + 2.0 ** -126
+            within(f64(dx), want, np.nan_to_num(bound, posinf=0.0))
+        if dw:
+            values = []
+            for p, f in ((one, f1), (two, f2)):
+                if f:
+                    out = torch.empty(rows, f, device="cuda")
+                    learn.gns_checkpoint_load(ctx, *p, out, rows)
+                    values.append(f64(out))
+            x64 = np.concatenate(values, 1)
+            with np.errstate(invalid="ignore", over="ignore"):
+                want, size = times(x64.T.copy(), dz), np.abs(x64).T @ np.abs(dz)
+                want = np.where(np.abs(want) > float(torch.finfo(FP32).max), np.sign(want) * np.inf, want)
+                size[~np.isfinite(want)] = 0.0
+                within(f64(got_dw), want, np.nan_to_num((rows + 8) * 2 * U * size, posinf=0.0) + 2.0 ** -126)
+                want = dz.sum(0)
+                within(f64(db), want, np.nan_to_num((rows + 8) * 2 * U * np.abs(dz).sum(0), posinf=0.0))
