@@ -1,30 +1,43 @@
 // The backward pass of the update step out = g([x1 | x2] . W + b), with the layer's inputs from their 8-bit checkpoints:
 //   dz = d_out where the output was positive,  dw = X^T dz,  db = sum_r dz,  dx = dz W^T.
 // Both products run on the bf16 matrix cores at fp32's precision.  A checkpoint's values q * 2^e are bf16 values as they are.
-// An fp32 value is cut into three bf16 terms of eight bits each, which hold it exactly: so dw takes three products of fp32
+// An fp32 value is cut into three bf16 terms, each what is left rounded to nearest, which hold it exactly: so dw takes three products of fp32
 // gradients and one of bf16 ones, and is exact up to the fp32 sums.  dx of bf16 gradients takes three products with W's terms and
 // is as exact (two terms of W moved single bf16 results: 2.1e-4 of dx's 2-norm from the fp32 products' at hdim 4096, three 1.6e-5, and
-// save 14 % of a large call); dx of fp32 gradients takes the six products of terms that are not below 2^-23 of the largest.
+// save 14 % of a large call); dx of fp32 gradients takes six products of terms: the three left out are at most
+// 2^-24 of the factors' magnitudes together, to either side (of terms that are cut, not rounded, 2^-21 and always to one).
 #include "gns_learn.hpp"
 
 namespace gns {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 // Upper halves of two words, a's in the lower half.
 __device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 __device__ __forceinline__ uint32_t lower_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 
-// The leading bf16 terms of eight values, packed, which are taken off the values.
+// The leading bf16 terms of two values (rounded to nearest), packed, which are taken off the values.
+__device__ __forceinline__ uint32_t take_term(float& a, float& b)
+{
+    const uint32_t t = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{a, b}, bf16x2));
+    a -= __uint_as_float(t << 16);
+    b -= __uint_as_float(t & 0xFFFF0000u);
+    return t;
+}
 __device__ __forceinline__ Chunk take_terms(uint32_t (&v)[8])
 {
-    uint32_t t[4];
+    Chunk t;
 #pragma unroll
-    for (int p = 0; p < 4; ++p) t[p] = upper_halves(v[2 * p], v[2 * p + 1]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) - __uint_as_float(v[i] & 0xFFFF0000u));
-    return Chunk{t[0], t[1], t[2], t[3]};
+    for (int p = 0; p < 4; ++p) {
+        float a = __uint_as_float(v[2 * p]), b = __uint_as_float(v[2 * p + 1]);
+        t[p] = take_term(a, b);
+        v[2 * p] = __float_as_uint(a);
+        v[2 * p + 1] = __float_as_uint(b);
+    }
+    return t;
 }
 
 // All bits set if bit i of w is, else none.
@@ -569,13 +582,8 @@ __global__ void __launch_bounds__(kBlock) k_backward_between(BetweenArgs a)
         const float4 four = load_four(a.w + row * a.hdim, c, a.hdim, marks);
         float v[4] = {four.x, four.y, four.z, four.w};
         for (int p = 0; p < 3; ++p) {
-            uint32_t u[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u[j] = __float_as_uint(v[j]);
-                v[j] -= __uint_as_float(u[j] & 0xFFFF0000u);
-            }
-            *reinterpret_cast<uint2*>(a.terms + (p * a.k + row) * a.pitch + c) = make_uint2(upper_halves(u[0], u[1]), upper_halves(u[2], u[3]));
+            const uint32_t lower = take_term(v[0], v[1]), upper = take_term(v[2], v[3]);
+            *reinterpret_cast<uint2*>(a.terms + (p * a.k + row) * a.pitch + c) = make_uint2(lower, upper);
         }
     }
 }

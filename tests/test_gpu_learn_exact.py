@@ -73,6 +73,21 @@ def test_input_gradient_sees_every_bit_of_the_weights(ctx, rows, f1, f2, hdim, d
     within(f64(dx), f64(want), bound if isinstance(bound, float) else f64(bound))
 
 
+@pytest.mark.parametrize("rows,f1,f2,hdim,dw", [s for s in WAYS if s[3] >= 8])
+def test_input_gradient_of_values_that_cut_badly(ctx, rows, f1, f2, hdim, dw):
+    """Eight products of one fp32 value with itself whose bits below the leading ones are all set.  The sum's magnitude is met by one
+    rounding and what products of the last terms leave out: 2^-22 of it is more than both."""
+    v = np.uint32(0x3F80FFFF).view(np.float32)
+    w = torch.full((f1 + f2, hdim), float(v), device="cuda")
+    d_out = torch.zeros(rows, hdim, device="cuda")
+    d_out[:, :8] = float(v)
+    one, two = two_checkpoints(ctx, torch.zeros(rows, f1 + f2), f1, f2) if dw else (None, None)
+    dx = backward(ctx, d_out, None, one, f1, two, f2, w, dw, True)[2]
+    want = np.full(dx.shape, 8 * float(v) ** 2)
+    within(f64(dx), want, 2.0 ** -22 * want)
+
+
+
 def times(a, b):
     """a @ b in 64 bits, with each product's infinities and NaN."""
     y = a @ b
