@@ -87,7 +87,9 @@ __device__ __forceinline__ float weight_again(const BackwardArgs& a, int32_t k, 
     return sum;
 }
 
-// The products of terms: which term of the left factor meets which of the right, the smallest first.
+// The products of terms: which term of the left factor meets which of the right, the smallest first.  Where both factors are cut,
+// the leading terms' product, the last, has an accumulator of its own: the large sum is rounded once with every k of a product and
+// not six times (dx of 85,000 rows of 256 x 256 7.0e-8 off in the 2-norm, 2.3e-7 with one, fp32 products 2.0e-7).
 template <int NA, int NB> struct Pairs;
 template <> struct Pairs<1, 1> { static constexpr int kCount = 1, kA[1] = {0}, kB[1] = {0}; };
 template <> struct Pairs<1, 3> { static constexpr int kCount = 3, kA[3] = {0, 0, 0}, kB[3] = {2, 1, 0}; };
@@ -104,12 +106,13 @@ struct Tile {
     static constexpr int kM = BM, kN = BN, kThreads = (BM / WM) * (BN / WN) * kWave, MI = WM / 32, NI = WN / 32;
     static constexpr int kStage = (BM * NA + BN * NB) * 4, kFragments = MI * NA + NI * NB;
     typedef Pairs<NA, NB> P;
+    static constexpr bool kTwo = NA > 1 && NB > 1;
 
     Chunk* lds;                               // [3 * kStage]
     const Chunk *a_at, *b_at;
     int kh, bank;
     Chunk f[2][kFragments];
-    floatx16 acc[MI][NI];
+    floatx16 acc[MI][NI], rest[kTwo ? MI : 1][kTwo ? NI : 1];
 
     __device__ __forceinline__ explicit Tile(Chunk* s) : lds(s)
     {
@@ -136,8 +139,9 @@ struct Tile {
 #pragma unroll
         for (int m = 0; m < kProducts; ++m) {
             const int p = m / (MI * NI), i = m / NI % MI, j = m % NI;
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[h][P::kA[p] * MI + i]),
-                                                                __builtin_bit_cast(bf16x8, f[h][MI * NA + P::kB[p] * NI + j]), acc[i][j], 0, 0, 0);
+            floatx16& to = kTwo && p + 1 < P::kCount ? rest[kTwo ? i : 0][kTwo ? j : 0] : acc[i][j];
+            to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[h][P::kA[p] * MI + i]),
+                                                         __builtin_bit_cast(bf16x8, f[h][MI * NA + P::kB[p] * NI + j]), to, 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int o = others * m / kProducts; o < others * (m + 1) / kProducts; ++o) other(o);
@@ -188,10 +192,19 @@ struct Tile {
 #pragma unroll
                 for (int j = 0; j < NI; ++j)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+                    for (int v = 0; v < 16; ++v) {
+                        acc[i][j][v] = 0.f;
+                        if (kTwo) rest[i][j][v] = 0.f;
+                    }
             for (int32_t step = 0; step < steps; step += kSets) {
 #pragma unroll
                 for (int i = 0; i < kSets; ++i) turn(i);
+            }
+            if constexpr (kTwo) {
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] += rest[i][j];
             }
             finish(tile);
         }
@@ -868,7 +881,7 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
         load_words(z + n, zv[set]);
         if constexpr (kMask) words[set] = m[step];
     };
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f}, rest = acc;           // as in Tile
     auto multiply = [&](int set, int32_t step) {
         const uint32_t keep = columns_kept(hdim - step * 32 - kg * 8), k8 = kMask ? columns_left(keep, words[set] >> (kg * 8)) : keep;
         Chunk wt[kTermsB], zt[kTermsA];
@@ -886,8 +899,10 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
             for (int j = 0; j < 4; ++j) zt[0][j] = zv[set][j] & ((spread_bit(k8, 2 * j) & 0xFFFFu) | (spread_bit(k8, 2 * j + 1) & 0xFFFF0000u));
         }
 #pragma unroll
-        for (int p = 0; p < P::kCount; ++p)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, zt[P::kA[p]]), __builtin_bit_cast(bf16x8, wt[P::kB[p]]), acc, 0, 0, 0);
+        for (int p = 0; p < P::kCount; ++p) {
+            floatx4& to = kFloat && p + 1 < P::kCount ? rest : acc;
+            to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, zt[P::kA[p]]), __builtin_bit_cast(bf16x8, wt[P::kB[p]]), to, 0, 0, 0);
+        }
     };
     if (s0 < s1) {
 #pragma unroll
@@ -900,6 +915,7 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
             }
         }
     }
+    if (kFloat) acc += rest;
 #pragma unroll
     for (int v = 0; v < 4; ++v) s_sum[wave][v][lane] = acc[v];
     __syncthreads();

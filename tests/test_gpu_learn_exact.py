@@ -88,6 +88,18 @@ def test_input_gradient_of_values_that_cut_badly(ctx, rows, f1, f2, hdim, dw):
 
 
 
+@pytest.mark.parametrize("rows,f1,hdim,dw", [(3000, 256, 256, True), (12, 500, 256, False), (30000, 128, 256, False), (400, 96, 256, True)])
+def test_input_gradient_rounds_its_sums_once_per_sixteen_columns(ctx, rows, f1, hdim, dw):
+    """A sum's error in the 2-norm: each rounding costs 2.5e-8 (an ulp over the root of twelve, of a value anywhere in its binade) of the
+    part summed so far, which grows like the root; 16 of them and what joins the rest come to 8e-8, and twice that is allowed."""
+    g = gen("norm", rows, f1)
+    d_out, w = torch.randn(rows, hdim, generator=g).cuda(), torch.randn(f1, hdim, generator=g).cuda()
+    one = save(ctx, torch.zeros(rows, f1))[:2] if dw else None
+    dx = backward(ctx, d_out, None, one, f1, None, 0, w, dw, True)[2].double()
+    want = d_out.double() @ w.double().t().contiguous()
+    assert float((dx - want).norm() / want.norm()) < 1.6e-7
+
+
 def times(a, b):
     """a @ b in 64 bits, with each product's infinities and NaN."""
     y = a @ b
