@@ -19,6 +19,16 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 __device__ __forceinline__ uint32_t lower_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 
+// fp32 values are multiplied by 2^24 before they are cut, so that every term of every value is a normal bf16 value or zero (the
+// matrix cores take subnormal ones as zero), and sums of products by as many 2^-24 as there are such factors.  What overflows on the
+// way (a factor of 2^104, a sum of 2^80 with both factors scaled) is a sum that is not finite.  It costs fp32 calls 1 to 3 %.
+constexpr float kTermScale = 0x1p24f;
+__device__ __forceinline__ void scale_up(uint32_t (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * kTermScale);
+}
+
 // The leading bf16 terms of two values (rounded to nearest), packed, which are taken off the values.
 __device__ __forceinline__ uint32_t take_term(float& a, float& b)
 {
@@ -405,6 +415,7 @@ struct WeightsSource {
             if (sums[set]) add_up(set);
         } else if constexpr (kFloat) {
             uint32_t (&v)[8] = d[set];
+            if (i == 8) scale_up(v);
             lds[stage * Tiles::kStage + Tiles::place_b(i - 8, column, chunk)] = take_terms(v);
         } else {
             const int k = i - 8;
@@ -474,7 +485,7 @@ __device__ __forceinline__ void weights_block(const WeightsArgs& g, int32_t bloc
 #pragma unroll
                 for (int j = 0; j < Tiles::NI; ++j) {
                     any = fmaf(tile.acc[i][j][v], 0.f, any);
-                    if (n0 + column_of(j) < a.hdim) row[column_of(j)] = tile.acc[i][j][v];
+                    if (n0 + column_of(j) < a.hdim) row[column_of(j)] = sizeof(T) == 4 ? tile.acc[i][j][v] * (1.f / kTermScale) : tile.acc[i][j][v];
                 }
             }
         if (any == 0.f) return;
@@ -593,7 +604,7 @@ __global__ void __launch_bounds__(kBlock) k_backward_between(BetweenArgs a)
     for (int64_t t = (int64_t) block * kBlock + threadIdx.x; t < terms; t += (int64_t) a.term_blocks * kBlock) {
         const int64_t row = t / fours, c = (t - row * fours) * 4;
         const float4 four = load_four(a.w + row * a.hdim, c, a.hdim, marks);
-        float v[4] = {four.x, four.y, four.z, four.w};
+        float v[4] = {four.x * kTermScale, four.y * kTermScale, four.z * kTermScale, four.w * kTermScale};
         for (int p = 0; p < 3; ++p) {
             const uint32_t lower = take_term(v[0], v[1]), upper = take_term(v[2], v[3]);
             *reinterpret_cast<uint2*>(a.terms + (p * a.k + row) * a.pitch + c) = make_uint2(lower, upper);
@@ -618,6 +629,9 @@ __device__ __forceinline__ uint32_t columns_kept(int32_t inside)
 }
 // and those that are left of them by a mask's bits from column n on
 __device__ __forceinline__ uint32_t columns_left(uint32_t kept, uint32_t bits) { return kept & bits << ((__ffs((int) kept) - 1) & 31); }
+
+// of sums of products of W's terms and dz's, which are terms in fp32 alone
+template <typename T> constexpr float kInputScale = sizeof(T) == 4 ? 1.f / (kTermScale * kTermScale) : 1.f / kTermScale;
 
 template <typename T, int kThreads> struct InputTile;
 template <> struct InputTile<float, 512> { typedef Tile<128, 128, 64, 32, 3, 3> Type; };
@@ -735,6 +749,7 @@ struct InputSource {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] &= keep[set] ? ~0u : 0u;
                 }
+                if (p == 0) scale_up(v);
                 to[Tiles::place_b(p, row + b * kStep, chunk)] = take_terms(v);
             } else {
                 Chunk v = planes[set][b][p];
@@ -754,6 +769,7 @@ struct InputSource {
                 for (int j = 0; j < 4; ++j) d[set][b][j] &= (spread_bit(k8, 2 * j) & 0xFFFFu) | (spread_bit(k8, 2 * j + 1) & 0xFFFF0000u);
             }
         } else if constexpr (kFloat) {
+            if (u == 0) scale_up(d[set][b]);
             to[Tiles::place_a(u, row + b * kStep, chunk)] = take_terms(d[set][b]);
         } else {
             to[Tiles::place_a(0, row + b * kStep, chunk)] = Chunk{d[set][b][0], d[set][b][1], d[set][b][2], d[set][b][3]};
@@ -812,7 +828,7 @@ __device__ __forceinline__ void input_block(const InputArgs& g, int32_t block, i
                 for (int v = 0; v < 16; ++v)
 #pragma unroll
                     for (int j = 0; j < Tiles::NI; ++j)
-                        if (whole || (r0 + m0 + Tiles::row_step(i, v) < rows && k0 + n + 32 * j < K)) part[(int64_t) Tiles::row_step(i, v) * K + 32 * j] = tile.acc[i][j][v];
+                        if (whole || (r0 + m0 + Tiles::row_step(i, v) < rows && k0 + n + 32 * j < K)) part[(int64_t) Tiles::row_step(i, v) * K + 32 * j] = tile.acc[i][j][v] * kInputScale<T>;
             if (any != 0.f) again(part, K, source.begin, min(source.end, a.hdim), [](float v) { return v; }, [](float v) { return v; });
             return;
         }
@@ -824,7 +840,7 @@ __device__ __forceinline__ void input_block(const InputArgs& g, int32_t block, i
                 T* row = first + Tiles::row_step(i, v) * a.dx.stride;
 #pragma unroll
                 for (int j = 0; j < Tiles::NI; ++j)
-                    if (whole || (r0 + m0 + Tiles::row_step(i, v) < rows && k0 + n + 32 * j < K)) row[32 * j] = from_float<T>(tile.acc[i][j][v]);
+                    if (whole || (r0 + m0 + Tiles::row_step(i, v) < rows && k0 + n + 32 * j < K)) row[32 * j] = from_float<T>(tile.acc[i][j][v] * kInputScale<T>);
             }
         if (any != 0.f) again(first, a.dx.stride, 0, a.hdim, [](T v) { return to_float(v); }, [](float v) { return from_float<T>(v); });
     });
@@ -887,11 +903,13 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
         Chunk wt[kTermsB], zt[kTermsA];
 #pragma unroll
         for (int j = 0; j < 8; ++j) wv[set][j] &= spread_bit(keep, j);
+        scale_up(wv[set]);
 #pragma unroll
         for (int k = 0; k < kTermsB; ++k) wt[k] = take_terms(wv[set]);
         if constexpr (kFloat) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) zv[set][j] &= spread_bit(k8, j);
+            scale_up(zv[set]);
 #pragma unroll
             for (int k = 0; k < kTermsA; ++k) zt[k] = take_terms(zv[set]);
         } else {
@@ -928,6 +946,7 @@ __global__ void __launch_bounds__(kFewBlock) k_backward_few(BackwardArgs a)
     float sum = 0.f;
 #pragma unroll
     for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][v][l];
+    sum *= kInputScale<T>;
     if (!is_finite(sum)) sum = input_again<T, kMask>(a, r, k, 0, hdim);
     store_at<T>(a.dx, r, k, sum);
 }

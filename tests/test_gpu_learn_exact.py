@@ -100,6 +100,50 @@ def test_input_gradient_rounds_its_sums_once_per_sixteen_columns(ctx, rows, f1, 
     assert float((dx - want).norm() / want.norm()) < 1.6e-7
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -118, 1.0, 2.0 ** 100])
+@pytest.mark.parametrize("rows,f1,f2,hdim,dw", WAYS)
+def test_gradients_of_single_products_are_exact(ctx, rows, f1, f2, hdim, dw, scale):
+    """One column of a row and one row of a column count, inputs are 0, 1 and -1 and weights powers of two: each result is one
+    gradient of 24 bits, small and large ones too."""
+    k = f1 + f2
+    g = gen("single", rows, k, hdim)
+    value = (torch.randint(2 ** 23, 2 ** 24, (rows,), generator=g).double() * 2.0 ** -23 * scale).float()
+    value = torch.where(torch.rand(rows, generator=g) < 0.5, value, -value)
+    w = torch.exp2(torch.randint(-3, 4, (k, hdim), generator=g).float())
+    column = torch.randint(0, hdim, (rows,), generator=g)
+    d_out = torch.zeros(rows, hdim)
+    d_out[torch.arange(rows), column] = value
+    x = torch.randint(-1, 2, (rows, k), generator=g).float()
+    one, two = two_checkpoints(ctx, x, f1, f2) if dw else (None, None)
+    dx = backward(ctx, d_out.cuda(), None, one, f1, two, f2, w.cuda(), dw, True)[2]
+    assert torch.equal(dx.cpu(), value[:, None] * w[:, column].t())
+
+
+@TYPES
+@pytest.mark.parametrize("least", [-30, -120])
+@pytest.mark.parametrize("rows,f1,f2,hdim", [(1, 5, 0, 3), (70, 40, 0, 33), (600, 300, 100, 129), (4000, 100, 28, 40), (20000, 128, 128, 256),
+                                             (3000, 1024, 0, 1024), (2500, 257, 0, 385), (9001, 512, 0, 1030), (40001, 64, 36, 41)])
+def test_weights_gradient_keeps_every_bit(ctx, rows, f1, f2, hdim, least, dtype):
+    """In each column of d_out one row counts (the rest is masked or zero) and inputs are 0, 1 and -1: a gradient of the weights is one
+    of d_out's values, of all bits its type has, or zero, and the bias's is the value."""
+    k = f1 + f2
+    g = gen("dw", rows, k, hdim)
+    x = torch.randint(-1, 2, (rows, k), generator=g).float()
+    row = torch.randint(0, rows, (hdim,), generator=g)
+    value = ((1 + torch.rand(hdim, generator=g)) * torch.exp2(torch.randint(least, least + 60, (hdim,), generator=g).float())).to(dtype)
+    n = torch.arange(hdim)
+    one, two = two_checkpoints(ctx, x, f1, f2)
+    w = torch.zeros(k, hdim, device="cuda")
+    want = (x[row].t() * value.float()[None, :])
+    for masked in (False, True):
+        d_out = torch.randn(rows, hdim, generator=g).to(dtype) if masked else torch.zeros(rows, hdim, dtype=dtype)
+        d_out[row, n] = value
+        mask = torch.zeros(rows, hdim, dtype=torch.bool)
+        mask[row, n] = True
+        dw, db, _ = backward(ctx, d_out.cuda(), words_of(mask).cuda() if masked else None, one, f1, two, f2, w, True, False)
+        assert torch.equal(dw.cpu(), want) and torch.equal(db.cpu(), value.float())
+
+
 def times(a, b):
     """a @ b in 64 bits, with each product's infinities and NaN."""
     y = a @ b
