@@ -1024,28 +1024,31 @@ struct WeightsPlan {
     int32_t m_tiles, n_tiles, splits, db_shares;
 };
 
+static WeightsPlan plan_weights_of(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int64_t rows, bool fp32, bool wide)
+{
+    const int32_t columns = ((f1 + 31) / 32 + (f2 + 31) / 32) * 32, n512 = fp32 ? 128 : 256, bm = wide ? 256 : 128, bn = wide ? n512 : n512 / 2;
+    const int64_t most = (rows + 127) / 128;                  // splits of four steps at least
+    WeightsPlan p;
+    p.wide = wide;
+    p.m_tiles = (columns + bm - 1) / bm;
+    p.n_tiles = (hdim + bn - 1) / bn;
+    int64_t s = (int64_t) c->num_cus * (wide ? 1 : 2) / ((int64_t) p.m_tiles * p.n_tiles);
+    if (s > most) s = most;
+    p.splits = s < 1 ? 1 : (int32_t) s;
+    // a few steps more of one block in m_tiles cost less than the launch that joins the shares
+    p.db_shares = p.splits == 1 && rows <= 512 ? 1 : p.m_tiles;
+    return p;
+}
+
+// Wide blocks where layers fill them and they fill half the chip at least (dx too, 16,384 rows of 2048 x 2048 bf16: 500 us, 571 with
+// narrow ones; 85,000 of 256 x 256 fp32: 138 and 144; 12,600 of 512 x 256: no difference)
+static bool may_be_wide(int32_t f1, int32_t f2, int32_t hdim, bool fp32) { return (f1 + 31) / 32 + (f2 + 31) / 32 > 4 && hdim > (fp32 ? 64 : 128); }
+
 static WeightsPlan plan_weights(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int64_t rows, bool fp32, bool wide)
 {
-    const int32_t columns = ((f1 + 31) / 32 + (f2 + 31) / 32) * 32, n512 = fp32 ? 128 : 256;
-    const int64_t most = (rows + 127) / 128;                  // splits of four steps at least
-    auto plan = [&](bool is_wide) {
-        WeightsPlan p;
-        p.wide = is_wide;
-        const int32_t bm = is_wide ? 256 : 128, bn = is_wide ? n512 : n512 / 2;
-        p.m_tiles = (columns + bm - 1) / bm;
-        p.n_tiles = (hdim + bn - 1) / bn;
-        int64_t s = (int64_t) c->num_cus * (is_wide ? 1 : 2) / ((int64_t) p.m_tiles * p.n_tiles);
-        if (s > most) s = most;
-        p.splits = s < 1 ? 1 : (int32_t) s;
-        // a few steps more of one block in m_tiles cost less than the launch that joins the shares
-        p.db_shares = p.splits == 1 && rows <= 512 ? 1 : p.m_tiles;
-        return p;
-    };
-    // Wide blocks where layers fill them and they fill half the chip at least (dx too, 16,384 rows of 2048 x 2048 bf16: 500 us, 571 with
-    // narrow ones; 85,000 of 256 x 256 fp32: 138 and 144; 12,600 of 512 x 256: no difference)
-    const WeightsPlan p = plan(true);
-    if (wide && columns > 128 && hdim > n512 / 2 && (int64_t) p.m_tiles * p.n_tiles * p.splits >= c->num_cus / 2) return p;
-    return plan(false);
+    const WeightsPlan p = plan_weights_of(c, f1, f2, hdim, rows, fp32, true);
+    if (wide && may_be_wide(f1, f2, hdim, fp32) && (int64_t) p.m_tiles * p.n_tiles * p.splits >= c->num_cus / 2) return p;
+    return plan_weights_of(c, f1, f2, hdim, rows, fp32, false);
 }
 
 // A grid's blocks times their threads stay below 2^32.
@@ -1197,19 +1200,56 @@ static int32_t most_input_splits(const gns_ctx* c, const BackwardArgs& a)
     return s < 2 ? 1 : (int32_t) s;
 }
 
-size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows)
+// Bytes of the sums of dw's and db's parts
+static size_t parts_bytes(const WeightsPlan& p, size_t k, size_t hdim)
 {
-    const size_t k = (size_t) f1 + (size_t) f2, pitch = ((size_t) hdim + kStageK - 1) / kStageK * kStageK;
+    return (p.splits > 1 ? align256((size_t) p.splits * k * hdim * 4) : 0) + align256((size_t) p.splits * (size_t) p.db_shares * hdim * 4);
+}
+static size_t terms_bytes(size_t k, size_t hdim) { return align256(3 * k * ((hdim + kStageK - 1) / kStageK * kStageK) * 2); }
+
+size_t backward_need(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows)
+{
+    const size_t k = (size_t) f1 + (size_t) f2;
     size_t parts = 0;
-    for (int i = 0; i < 3; ++i) {                              // of either type, and of bf16 columns read singly
-        const WeightsPlan p = plan_weights(c, f1, f2, hdim, rows, i == 0, i < 2);
-        const size_t need = (p.splits > 1 ? align256((size_t) p.splits * k * (size_t) hdim * 4) : 0) + align256((size_t) p.splits * (size_t) p.db_shares * (size_t) hdim * 4);
-        if (need > parts) parts = need;
-    }
+    for (int i = 0; i < 3; ++i)                                // of either type, and of bf16 columns read singly
+        parts = max(parts, parts_bytes(plan_weights(c, f1, f2, hdim, rows, i == 0, i < 2), k, (size_t) hdim));
     BackwardArgs a = {};
     a.x1.width = f1; a.x2.width = f2; a.hdim = hdim; a.count.rows = rows;
     const int32_t splits = max(most_input_splits<float>(c, a), most_input_splits<Bf16>(c, a));
-    return parts + max(align256(3 * k * pitch * 2), splits > 1 ? align256((size_t) splits * (size_t) rows * k * 4) : 0);
+    return parts + max(terms_bytes(k, (size_t) hdim), splits > 1 ? align256((size_t) splits * (size_t) rows * k * 4) : 0);
+}
+
+// The most bytes that dx's splits take in calls of so many rows or fewer: s splits of r rows where s times the tiles of r rows is no
+// more than two for each CU.
+template <typename T>
+static size_t most_input_bytes(const gns_ctx* c, size_t k, int32_t hdim, int32_t rows)
+{
+    typedef typename InputTile<T, 256>::Type Tiles;
+    const int64_t bands = (int64_t) c->num_cus * 2 / (((int64_t) k + Tiles::kN - 1) / Tiles::kN);      // of kM rows, times splits
+    const int64_t splits = min(bands, (int64_t) (hdim + kStageK - 1) / kStageK / both_least<T>());
+    return splits < 2 ? 0 : align256((size_t) min(splits * rows, bands * Tiles::kM) * k * 4);
+}
+
+size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows)
+{
+    const size_t k = (size_t) f1 + (size_t) f2;
+    size_t parts = 0;
+    for (int i = 0; i < 3; ++i) {
+        // The splits of a plan grow with the rows, but narrow blocks have more tiles, so the most of both is taken: narrow ones
+        // are used up to the last rows whose wide blocks fill less than half the chip.
+        const bool fp32 = i == 0;
+        const WeightsPlan wide = plan_weights_of(c, f1, f2, hdim, rows, fp32, true);
+        int64_t narrow_rows = rows;
+        if (i < 2 && may_be_wide(f1, f2, hdim, fp32)) {
+            const int64_t tiles = (int64_t) wide.m_tiles * wide.n_tiles, splits = (c->num_cus / 2 + tiles - 1) / tiles;
+            if (tiles * wide.splits >= c->num_cus / 2) {
+                narrow_rows = min(narrow_rows, (splits - 1) * 128);
+                parts = max(parts, parts_bytes(wide, k, (size_t) hdim));
+            }
+        }
+        parts = max(parts, parts_bytes(plan_weights_of(c, f1, f2, hdim, narrow_rows, fp32, false), k, (size_t) hdim));
+    }
+    return parts + max(terms_bytes(k, (size_t) hdim), max(most_input_bytes<float>(c, k, hdim, rows), most_input_bytes<Bf16>(c, k, hdim, rows)));
 }
 
 // Threads that share a sum: all sums' first reads should be on their way at once.

@@ -227,7 +227,7 @@ gns_status gns_sage_dense_backward(gns_ctx* ctx, const gns_rows* d_out, const ui
     }
     GNS_REQUIRE(row_count(ctx, num_rows, &a.count), "bad device-count placeholder");
     GNS_REQUIRE(workspace && !misaligned(workspace, 256), "workspace is null or not 256-byte aligned");
-    if (workspace_bytes < gns_sage_dense_backward_workspace_bytes(ctx, f1, f2, d_out->width, num_rows))
+    if (workspace_bytes < align256(backward_need(ctx, f1, f2, d_out->width, a.count.rows)))
         return ctx_fail(ctx, GNS_ECAPACITY, "workspace is too small");
     a.d_out = as_const(d_out);
     a.positive = positive_dev;
@@ -265,7 +265,7 @@ gns_status gns_log_probs(gns_ctx* ctx, const gns_rows* logits, const int32_t* la
     LogProbsArgs a = {};
     GNS_REQUIRE(row_count(ctx, num_rows, &a.count), "bad device-count placeholder");
     if (a.count.rows == 0) return GNS_OK;
-    const size_t need = gns_log_probs_workspace_bytes(ctx, logits->width, top, num_rows);
+    const size_t need = log_probs_need(ctx, logits->width, top, a.count.rows);
     if (need) {
         GNS_REQUIRE(workspace && !misaligned(workspace, 256), "workspace is null or not 256-byte aligned");
         if (workspace_bytes < need) return ctx_fail(ctx, GNS_ECAPACITY, "workspace is too small");

@@ -200,9 +200,12 @@ hipError_t launch_sage_dense_int8(const gns_ctx* c, const QuantizeArgs& x, const
 hipError_t launch_checkpoint_save(const gns_ctx* c, const CheckpointArgs& a, int32_t type, hipStream_t s);
 hipError_t launch_checkpoint_load(const gns_ctx* c, const CheckpointArgs& a, int32_t type, hipStream_t s);
 // gns_backward.hip
+// bytes that a call of so many rows takes, and the most that one of so many or fewer does
+size_t backward_need(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows);
 size_t backward_workspace(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int32_t rows);
 hipError_t launch_backward(const gns_ctx* c, const BackwardArgs& a, int32_t type, hipStream_t s);
 // gns_log_probs.hip
+size_t log_probs_need(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows);
 size_t log_probs_workspace(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows);
 hipError_t launch_log_probs(const gns_ctx* c, const LogProbsArgs& a, int32_t type, hipStream_t s);
 hipError_t launch_log_probs_backward(const gns_ctx* c, const LogProbsBackwardArgs& a, int32_t type, int32_t out_type, hipStream_t s);

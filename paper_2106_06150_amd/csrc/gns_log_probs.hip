@@ -540,12 +540,24 @@ static void split_rows(const gns_ctx* c, int32_t classes, int32_t top, int32_t r
 
 static size_t sums_bytes(int64_t rows, int32_t parts) { return ((size_t) rows * (size_t) parts * sizeof(PartSums) + 255) / 256 * 256; }
 
-size_t log_probs_workspace(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows)
+size_t log_probs_need(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows)
 {
     if (classes <= kShortClasses) return 0;
     int32_t parts, tiles;
     split_rows(c, classes, top, rows, &parts, &tiles);
     return parts == 1 ? 0 : sums_bytes(rows, parts) + (size_t) rows * (size_t) parts * (size_t) top * sizeof(Key);
+}
+
+// Few rows have many parts: those of all rows together are no more than four for each SIMD, and those of one no more than it has
+// two tiles or the join has room for.
+size_t log_probs_workspace(const gns_ctx* c, int32_t classes, int32_t top, int32_t rows)
+{
+    if (classes <= kShortClasses) return 0;
+    const int64_t pairs = ((int64_t) classes + kWaveTile - 1) / kWaveTile / 2;
+    const int64_t one = top && pairs > kJoinKeys * kWave / top ? kJoinKeys * kWave / top : pairs, simds = (int64_t) c->num_cus * 4;
+    if (one < 2) return 0;
+    const int64_t all = one * rows < simds * 4 ? one * rows : simds * 4;
+    return sums_bytes(all, 1) + (size_t) all * (size_t) top * sizeof(Key);
 }
 
 template <typename T, int L, int E>

@@ -212,3 +212,58 @@ def test_backward_of_infinities(ctx, rows, f1, f2, hdim, dw, masked, dtype):
                 within(f64(got_dw), want, np.nan_to_num((rows + 8) * 2 * U * size, posinf=0.0) + 2.0 ** -126)
                 want = dz.sum(0)
                 within(f64(db), want, np.nan_to_num((rows + 8) * 2 * U * np.abs(dz).sum(0), posinf=0.0))
+
+
+ROWS = [0, 1, 2, 15, 16, 17, 31, 33, 64, 100, 127, 129, 200, 255, 257, 300, 400, 511, 512, 513, 600, 700, 1000, 1023, 1025, 1400, 1500, 2000, 2047, 2048, 2049,
+        3000, 4000, 4096, 4097, 5000, 6982, 8192, 8193, 10000, 12000, 16384, 20000, 32746, 40000, 65536, 85000, 100000, 300000, 1000000]
+
+
+def test_workspaces_grow_with_the_rows(ctx):
+    """A workspace for some rows serves any call of fewer."""
+    def grows(bytes_of):
+        sizes = [bytes_of(r) for r in ROWS]
+        assert sizes == sorted(sizes), [(r, s) for r, s in zip(ROWS, sizes)]
+    for classes in (47, 257, 1000, 2100, 5003, 10000, 100003, 131072):
+        for top in (0, 1, 5, 20, 32):
+            grows(lambda r: learn.gns_log_probs_workspace_bytes(ctx, classes, top, r))
+    for f1, f2, hdim in ((1, 0, 1), (40, 0, 72), (100, 28, 47), (128, 128, 256), (400, 0, 256), (64, 64, 2048), (1024, 0, 1024), (4096, 0, 4096), (300, 0, 5),
+                         (2141, 0, 1102), (1000, 0, 1000), (40000, 0, 64), (64, 0, 40000)):
+        grows(lambda r: learn.gns_sage_dense_backward_workspace_bytes(ctx, f1, f2, hdim, r))
+    for k in (1, 64, 1000, 4096):
+        grows(lambda r: learn.gns_sage_dense_int8_workspace_bytes(ctx, k, r))
+
+
+@TYPES
+@pytest.mark.parametrize("most,classes,top", [(4096, 100003, 20), (4096, 10000, 5), (5000, 5003, 20), (1500, 2100, 32)])
+def test_log_probs_of_fewer_rows_in_the_same_workspace(ctx, most, classes, top, dtype):
+    z = torch.randn(512, classes, generator=gen("fewer", classes), dtype=torch.float32).to(dtype).cuda()
+    space = learn.alloc_workspace(learn.gns_log_probs_workspace_bytes(ctx, classes, top, most))
+    for rows in (512, 300, 129, 17, 2, 1):
+        results = []
+        for s in (space, learn.alloc_workspace(learn.gns_log_probs_workspace_bytes(ctx, classes, top, rows))):
+            if s is not None:
+                s.fill_(255)
+            entropy, index, value = torch.zeros(rows, device="cuda"), torch.zeros(rows, top, dtype=torch.int32, device="cuda"), torch.zeros(rows, top, device="cuda")
+            learn.gns_log_probs(ctx, z[:rows], None, None, entropy, None, index, value, rows, s)
+            results.append((entropy, index, value))
+        assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@TYPES
+@pytest.mark.parametrize("most,f1,f2,hdim", [(10000, 400, 0, 256), (8192, 1024, 0, 1024), (40000, 64, 64, 2048), (20000, 300, 0, 47), (6000, 600, 9, 1001)])
+def test_backward_of_fewer_rows_in_the_same_workspace(ctx, most, f1, f2, hdim, dtype):
+    g = gen("fewer", most, f1, hdim)
+    rows0 = min(most, 7000)
+    x = torch.randn(rows0, f1 + f2, generator=g)
+    d_out, w = torch.randn(rows0, hdim, generator=g).to(dtype).cuda(), torch.randn(f1 + f2, hdim, generator=g).cuda()
+    one, two = two_checkpoints(ctx, x, f1, f2)
+    space = learn.alloc_workspace(learn.gns_sage_dense_backward_workspace_bytes(ctx, f1, f2, hdim, most))
+    for rows in (rows0, 6982, 4096, 2000, 1104, 500, 129, 64, 9, 1):
+        if rows > rows0:
+            continue
+        results = []
+        for s in (space, None):
+            if s is not None:
+                s.fill_(255)
+            results.append(backward(ctx, d_out[:rows], None, one, f1, two, f2, w, True, True, s))
+        assert all(torch.equal(a, b) for a, b in zip(*results)), rows
