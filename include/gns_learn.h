@@ -13,7 +13,7 @@
  * gns_last_error(ctx).  From the context these calls take the device's properties, the place for errors, the stage
  * timer and, for num_rows < 0, the counts of its last mini-batch: num_rows may be GNS_DEVICE_COUNTS(i), the dst rows of
  * layer index i, read on the device (buffers must then hold that layer's cap_dst rows; what lies behind the count is
- * not written).  num_rows may be 0.  A workspace for some num_rows serves calls of fewer rows too.  Calls on one context
+ * not written).  num_rows may be 0, and buffers of rows NULL then.  A workspace for some num_rows serves calls of fewer rows too.  Calls on one context
  * may be enqueued on several streams as long as they do not share a workspace.  Inputs and outputs of a call must not
  * overlap unless the call says so.  Results do not depend on timing: a repeated call gives the same bits.
  */

@@ -26,10 +26,10 @@ int32_t worst_rows(const gns_ctx* c, int32_t num_rows)
     return -1 - num_rows < c->config.num_layers ? (int32_t) c->lay.rows[-1 - num_rows] : -1;
 }
 
-// What is wrong with rows of a call; null if nothing.
-const char* rows_fault(const gns_rows* x)
+// What is wrong with rows of a call of num_rows; null if nothing.  Without rows there need be no data.
+const char* rows_fault(const gns_rows* x, int32_t num_rows)
 {
-    if (!x || !x->data) return "null rows";
+    if (!x || (!x->data && num_rows)) return "null rows";
     if (x->type != GNS_FP32 && x->type != GNS_BF16) return "rows are of no known type";
     if (x->width < 1 || x->width > GNS_MAX_WIDTH) return "width of rows out of range";
     if (x->stride < x->width || x->stride > GNS_MAX_STRIDE) return "stride of rows out of range";
@@ -44,8 +44,10 @@ MutRows as_mut(const gns_rows* x) { return MutRows{x->data, x->stride, x->width}
 
 #define GNS_REQUIRE(cond, message) \
     do { if (!(cond)) return ctx_fail(ctx, GNS_EINVAL, message); } while (0)
+// what belongs to the rows of a call: its buffers have no address where there are none
+#define GNS_REQUIRE_OF_ROWS(cond, message) GNS_REQUIRE((cond) || num_rows == 0, message)
 #define GNS_REQUIRE_ROWS(x) \
-    do { if (const char* fault = rows_fault(x)) return ctx_fail(ctx, GNS_EINVAL, fault); } while (0)
+    do { if (const char* fault = rows_fault(x, num_rows)) return ctx_fail(ctx, GNS_EINVAL, fault); } while (0)
 
 // [x1 | x2] of a quantising call
 gns_status quantize_args(gns_ctx* ctx, const gns_rows* x1, const gns_rows* x2, int32_t num_rows, QuantizeArgs* a)
@@ -67,7 +69,7 @@ gns_status quantize_args(gns_ctx* ctx, const gns_rows* x1, const gns_rows* x2, i
 }
 
 gns_status dense_int8_args(gns_ctx* ctx, int32_t k, const int8_t* wq, const float* w_scale, const float* bias, int32_t relu,
-                           const gns_rows* out, DenseInt8Args* a)
+                           const gns_rows* out, int32_t num_rows, DenseInt8Args* a)
 {
     GNS_REQUIRE_ROWS(out);
     GNS_REQUIRE(wq && w_scale, "null weights or scales");
@@ -91,7 +93,7 @@ gns_status gns_quantize_rows(gns_ctx* ctx, const gns_rows* x1, const gns_rows* x
     QuantizeArgs a;
     const gns_status st = quantize_args(ctx, x1, x2, num_rows, &a);
     if (st != GNS_OK) return st;
-    GNS_REQUIRE(q_dev && scale_dev, "null output");
+    GNS_REQUIRE_OF_ROWS(q_dev && scale_dev, "null output");
     GNS_REQUIRE(!misaligned(q_dev, 16) && !misaligned(scale_dev, 4), "rows in 8 bits must be 16-byte aligned");
     a.q = q_dev; a.scale = scale_dev;
     if (a.count.rows == 0) return GNS_OK;
@@ -106,11 +108,11 @@ gns_status gns_dense_int8(gns_ctx* ctx, const int8_t* q_dev, const float* scale_
                           int32_t num_rows, void* hip_stream)
 {
     if (!ctx) return GNS_EINVAL;
-    GNS_REQUIRE(q_dev && scale_dev, "null rows in 8 bits");
+    GNS_REQUIRE_OF_ROWS(q_dev && scale_dev, "null rows in 8 bits");
     GNS_REQUIRE(!misaligned(q_dev, 16) && !misaligned(scale_dev, 4), "rows in 8 bits must be 16-byte aligned");
     GNS_REQUIRE(k >= 1 && k <= GNS_INT8_MAX_K, "k out of range");
     DenseInt8Args a;
-    const gns_status st = dense_int8_args(ctx, k, wq_dev, w_scale_dev, bias_dev, relu, out, &a);
+    const gns_status st = dense_int8_args(ctx, k, wq_dev, w_scale_dev, bias_dev, relu, out, num_rows, &a);
     if (st != GNS_OK) return st;
     GNS_REQUIRE(row_count(ctx, num_rows, &a.count), "bad device-count placeholder");
     a.q = q_dev; a.scale = scale_dev;
@@ -139,7 +141,7 @@ gns_status gns_sage_dense_int8(gns_ctx* ctx, const gns_rows* x1, const gns_rows*
     if (st != GNS_OK) return st;
     const int32_t k = x.x1.width + x.x2.width;
     DenseInt8Args a;
-    st = dense_int8_args(ctx, k, wq_dev, w_scale_dev, bias_dev, relu, out, &a);
+    st = dense_int8_args(ctx, k, wq_dev, w_scale_dev, bias_dev, relu, out, num_rows, &a);
     if (st != GNS_OK) return st;
     a.count = x.count;
     if (a.count.rows == 0) return GNS_OK;
@@ -160,7 +162,7 @@ gns_status gns_checkpoint_save(gns_ctx* ctx, const gns_rows* x, int8_t* q_dev, u
 {
     if (!ctx) return GNS_EINVAL;
     GNS_REQUIRE_ROWS(x);
-    GNS_REQUIRE(q_dev && exponents_dev, "null checkpoint");
+    GNS_REQUIRE_OF_ROWS(q_dev && exponents_dev, "null checkpoint");
     GNS_REQUIRE(!misaligned(q_dev, 16) && !misaligned(positive_dev, 4), "checkpoints must be 16-byte aligned");
     CheckpointArgs a = {};
     GNS_REQUIRE(row_count(ctx, num_rows, &a.count), "bad device-count placeholder");
@@ -179,7 +181,7 @@ gns_status gns_checkpoint_load(gns_ctx* ctx, const int8_t* q_dev, const uint8_t*
 {
     if (!ctx) return GNS_EINVAL;
     GNS_REQUIRE_ROWS(x);
-    GNS_REQUIRE(q_dev && exponents_dev, "null checkpoint");
+    GNS_REQUIRE_OF_ROWS(q_dev && exponents_dev, "null checkpoint");
     GNS_REQUIRE(!misaligned(q_dev, 16), "checkpoints must be 16-byte aligned");
     CheckpointArgs a = {};
     GNS_REQUIRE(row_count(ctx, num_rows, &a.count), "bad device-count placeholder");
@@ -213,7 +215,7 @@ gns_status gns_sage_dense_backward(gns_ctx* ctx, const gns_rows* d_out, const ui
     GNS_REQUIRE(dw_dev || !db_dev, "db comes with dw only");
     GNS_REQUIRE(!misaligned(positive_dev, 4) && !misaligned(db_dev, 4), "positive and db must be aligned");
     if (dw_dev) {
-        GNS_REQUIRE(q1_dev && exponents1_dev && (!f2 || (q2_dev && exponents2_dev)), "null checkpoint");
+        GNS_REQUIRE_OF_ROWS(q1_dev && exponents1_dev && (!f2 || (q2_dev && exponents2_dev)), "null checkpoint");
         GNS_REQUIRE(!misaligned(q1_dev, 16) && (!f2 || !misaligned(q2_dev, 16)), "checkpoints must be 16-byte aligned");
         GNS_REQUIRE(!misaligned(dw_dev, 4), "dw must be aligned");
     }
@@ -255,10 +257,10 @@ gns_status gns_log_probs(gns_ctx* ctx, const gns_rows* logits, const int32_t* la
 {
     if (!ctx) return GNS_EINVAL;
     GNS_REQUIRE_ROWS(logits);
-    GNS_REQUIRE(!labels_dev == !logp_dev, "labels and logp go together");
+    GNS_REQUIRE_OF_ROWS(!labels_dev == !logp_dev, "labels and logp go together");
     GNS_REQUIRE(top >= 0 && top <= GNS_MAX_TOP, "top out of range");
-    GNS_REQUIRE(top ? top_index_dev && top_logp_dev : !top_index_dev && !top_logp_dev, "top and its outputs do not agree");
-    GNS_REQUIRE(logp_dev || entropy_dev || stats_dev || top, "no output is wanted");
+    GNS_REQUIRE_OF_ROWS(top ? top_index_dev && top_logp_dev : !top_index_dev && !top_logp_dev, "top and its outputs do not agree");
+    GNS_REQUIRE_OF_ROWS(logp_dev || entropy_dev || stats_dev || top, "no output is wanted");
     GNS_REQUIRE(!misaligned(labels_dev, 4) && !misaligned(logp_dev, 4) && !misaligned(entropy_dev, 4) &&
                 !misaligned(top_index_dev, 4) && !misaligned(top_logp_dev, 4), "labels and outputs must be aligned");
     GNS_REQUIRE(!misaligned(stats_dev, 8), "stats must be 8-byte aligned");
@@ -288,12 +290,13 @@ gns_status gns_log_probs_backward(gns_ctx* ctx, const gns_rows* logits, const in
     GNS_REQUIRE_ROWS(logits);
     GNS_REQUIRE_ROWS(d_logits);
     GNS_REQUIRE(d_logits->width == logits->width, "d_logits must have the width of the logits");
-    GNS_REQUIRE(d_logits->data != logits->data || (d_logits->stride == logits->stride && d_logits->type == logits->type),
+    GNS_REQUIRE_OF_ROWS(d_logits->data != logits->data || (d_logits->stride == logits->stride && d_logits->type == logits->type),
                 "d_logits may only be the logits' own rows");
-    GNS_REQUIRE(stats_dev && !misaligned(stats_dev, 8), "stats are null or not 8-byte aligned");
-    GNS_REQUIRE(!g_logp_dev || labels_dev, "g_logp needs the labels");
-    GNS_REQUIRE(!g_entropy_dev || entropy_dev, "g_entropy needs the entropy");
-    GNS_REQUIRE(g_logp_dev || g_entropy_dev, "no gradient is given");
+    GNS_REQUIRE_OF_ROWS(stats_dev, "null stats");
+    GNS_REQUIRE(!misaligned(stats_dev, 8), "stats must be 8-byte aligned");
+    GNS_REQUIRE_OF_ROWS(!g_logp_dev || labels_dev, "g_logp needs the labels");
+    GNS_REQUIRE_OF_ROWS(!g_entropy_dev || entropy_dev, "g_entropy needs the entropy");
+    GNS_REQUIRE_OF_ROWS(g_logp_dev || g_entropy_dev, "no gradient is given");
     GNS_REQUIRE(!misaligned(labels_dev, 4) && !misaligned(g_logp_dev, 4) && !misaligned(entropy_dev, 4) && !misaligned(g_entropy_dev, 4),
                 "labels and gradients must be aligned");
     LogProbsBackwardArgs a = {};

@@ -267,3 +267,34 @@ def test_backward_of_fewer_rows_in_the_same_workspace(ctx, most, f1, f2, hdim, d
                 s.fill_(255)
             results.append(backward(ctx, d_out[:rows], None, one, f1, two, f2, w, True, True, s))
         assert all(torch.equal(a, b) for a, b in zip(*results)), rows
+
+
+@TYPES
+def test_calls_with_empty_tensors(ctx, dtype):
+    """No rows: their buffers have no address.  The gradients of the weights and the bias are zero all the same."""
+    def none(*shape, t=FP32):
+        return torch.empty((0,) + shape, dtype=t, device="cuda")
+
+    x, weights, scales = none(40, t=dtype), torch.zeros(24, 64, dtype=torch.int8, device="cuda"), torch.ones(24, device="cuda")
+    q, scale = none(64, t=torch.int8), none()
+    learn.gns_quantize_rows(ctx, x, none(3, t=dtype), q, scale, 0)
+    learn.gns_dense_int8(ctx, q, scale, 40, weights, scales, None, False, none(24, t=dtype), 0)
+    learn.gns_sage_dense_int8(ctx, x, none(3, t=dtype), weights, scales, None, True, none(24, t=dtype), 0, None)
+    one, two = (none(64, t=torch.int8), none(2, t=torch.uint8)), (none(32, t=torch.int8), none(1, t=torch.uint8))
+    learn.gns_checkpoint_save(ctx, x, *one, none(2, t=torch.int32), 0)
+    learn.gns_checkpoint_load(ctx, *one, x, 0)
+    labels, logp, stats = none(t=torch.int32), none(), none(2)
+    for top in (0, 3):
+        learn.gns_log_probs(ctx, x, labels, logp, logp, stats, none(top, t=torch.int32) if top else None, none(top) if top else None, 0)
+    learn.gns_log_probs_backward(ctx, x, labels, stats, logp, logp, logp, none(40, t=dtype), 0)
+    w, dw, db = torch.ones(43, 24, device="cuda"), torch.full((43, 24), 3.0, device="cuda"), torch.full((24,), 3.0, device="cuda")
+    space = learn.alloc_workspace(learn.gns_sage_dense_backward_workspace_bytes(ctx, 40, 3, 24, 0))
+    learn.gns_sage_dense_backward(ctx, none(24, t=dtype), none(1, t=torch.int32), one, 40, two, 3, w, dw, db, none(43, t=dtype), 0, space)
+    torch.cuda.synchronize()
+    assert not dw.any() and not db.any()
+    learn.gns_sage_dense_backward(ctx, none(24, t=dtype), None, None, 40, None, 3, w, None, None, none(43, t=dtype), 0, space)
+    # what does not belong to the rows is asked for as ever
+    with pytest.raises(B.GnsError):
+        learn.gns_dense_int8(ctx, q, scale, 40, None, scales, None, False, none(24, t=dtype), 0)
+    with pytest.raises(B.GnsError):
+        learn.gns_sage_dense_backward(ctx, none(24, t=dtype), None, one, 40, two, 3, w, None, None, None, 0, space)
