@@ -1,12 +1,18 @@
 // The update step in 8-bit integers: rows quantised with a scale each, exact integer products, scales and bias behind them.
 #include "gns_learn.hpp"
+#include <type_traits>
 
 namespace gns {
 
-// In this order only results that are too large overflow.
+// With channel scales of up to 2^96 a sum times one does not overflow, and only results that are too large do.  kFar: with any,
+// where the smaller scale comes first (a NaN counts as that), which the kernels that are bound by such instructions do for
+// tiles alone that have a larger one.
+constexpr float kFarScale = 0x1p96f;
+template <bool kFar>
 __device__ __forceinline__ float output_of(int sum, float w_scale, float scale, float bias, int32_t relu)
 {
-    const float y = (float) sum * w_scale * scale + bias;
+    const bool turn = kFar && !(w_scale < scale);
+    const float y = (float) sum * (turn ? scale : w_scale) * (turn ? w_scale : scale) + bias;
     return relu ? relu_of(y) : y;
 }
 
@@ -184,8 +190,9 @@ constexpr int kStepBytes = 64;                // k of a stage
 // so that a lane holds four consecutive outputs of a row.
 // 8192 x 8192 x 8192, bf16 out: 490 to 580 us, 1.9 to 2.2 POP/s (a large library product of integers: 2.15), bound by the matrix
 // cores' cycles at the clock that the power leaves; with outputs stored value by value 40 us more.
+// Blocks of 128 x 128 are three a CU, for which the compiler has to be told (two: 79,214 rows of 32 x 4096 bf16 164 -> 203 us).
 template <typename T, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(DenseInt8Args a, int32_t m_tiles, int32_t n_tiles)
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, BM == 128 ? 3 : 2) k_int8_tiles(DenseInt8Args a, int32_t m_tiles, int32_t n_tiles)
 {
     constexpr int kWaves = (BM / WM) * (BN / WN), kLoads = (BM + BN) / 16 / kWaves;     // of 16 rows, by a wave and stage
     constexpr int MI = WM / 32, NI = WN / 32, kStage = (BM + BN) * 4;
@@ -294,40 +301,46 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave) k_int8_tiles(De
     const int e_lane = opaque_lane_id(), e32 = e_lane & 31, four = 4 * (e_lane >> 5);
     char* const strip = reinterpret_cast<char*>(s_stage) + wave * (32 * kPitch);
     const int32_t c = n0 + wn + e_lane % kLanes * V;
+    const bool far = __ballot(fabsf(s_w_scale[wn + e_lane % WN]) > kFarScale) != 0;
+    auto finish = [&](auto is_far) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        const float scale = s_scale[wm + i * 32 + e32];
+        for (int i = 0; i < MI; ++i) {
+            const float scale = s_scale[wm + i * 32 + e32];
 #pragma unroll
-        for (int j = 0; j < NI; ++j)
+            for (int j = 0; j < NI; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {                     // elements 4 q .. 4 q + 3: four columns of row e32
-                const int at = j * 32 + 8 * q + four;
-                const float4 ws = *reinterpret_cast<const float4*>(s_w_scale + wn + at), b = *reinterpret_cast<const float4*>(s_bias + wn + at);
-                struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
-                y.v[0] = from_float<T>(output_of(acc[i][j][4 * q], ws.x, scale, b.x, a.relu));
-                y.v[1] = from_float<T>(output_of(acc[i][j][4 * q + 1], ws.y, scale, b.y, a.relu));
-                y.v[2] = from_float<T>(output_of(acc[i][j][4 * q + 2], ws.z, scale, b.z, a.relu));
-                y.v[3] = from_float<T>(output_of(acc[i][j][4 * q + 3], ws.w, scale, b.w, a.relu));
-                *reinterpret_cast<Four*>(strip + e32 * kPitch + at * (int) sizeof(T)) = y;
+                for (int q = 0; q < 4; ++q) {                 // elements 4 q .. 4 q + 3: four columns of row e32
+                    const int at = j * 32 + 8 * q + four;
+                    const float4 ws = *reinterpret_cast<const float4*>(s_w_scale + wn + at), b = *reinterpret_cast<const float4*>(s_bias + wn + at);
+                    struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
+                    constexpr bool kFar = decltype(is_far)::value;
+                    y.v[0] = from_float<T>(output_of<kFar>(acc[i][j][4 * q], ws.x, scale, b.x, a.relu));
+                    y.v[1] = from_float<T>(output_of<kFar>(acc[i][j][4 * q + 1], ws.y, scale, b.y, a.relu));
+                    y.v[2] = from_float<T>(output_of<kFar>(acc[i][j][4 * q + 2], ws.z, scale, b.z, a.relu));
+                    y.v[3] = from_float<T>(output_of<kFar>(acc[i][j][4 * q + 3], ws.w, scale, b.w, a.relu));
+                    *reinterpret_cast<Four*>(strip + e32 * kPitch + at * (int) sizeof(T)) = y;
+                }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int t = 0; t < 32 * kLanes / kWave; ++t) {
+                const int row = t * (kWave / kLanes) + e_lane / kLanes;
+                const Chunk y = *reinterpret_cast<const Chunk*>(strip + row * kPitch + e_lane % kLanes * 16);
+                const int64_t r = m0 + wm + i * 32 + row;
+                if (r >= rows) continue;
+                T* out = reinterpret_cast<T*>(a.out.data) + r * a.out.stride + c;
+                if (c + V <= n) {
+                    __builtin_memcpy(out, &y, 16);            // whatever the row's alignment
+                } else {
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        if (c + k < n) out[k] = __builtin_bit_cast(Piece<T>, y).v[k];
+                }
             }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int t = 0; t < 32 * kLanes / kWave; ++t) {
-            const int row = t * (kWave / kLanes) + e_lane / kLanes;
-            const Chunk y = *reinterpret_cast<const Chunk*>(strip + row * kPitch + e_lane % kLanes * 16);
-            const int64_t r = m0 + wm + i * 32 + row;
-            if (r >= rows) continue;
-            T* out = reinterpret_cast<T*>(a.out.data) + r * a.out.stride + c;
-            if (c + V <= n) {
-                __builtin_memcpy(out, &y, 16);                // whatever the row's alignment
-            } else {
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-                    if (c + k < n) out[k] = __builtin_bit_cast(Piece<T>, y).v[k];
-            }
+            __builtin_amdgcn_wave_barrier();
         }
-        __builtin_amdgcn_wave_barrier();
-    }
+    };
+    if (far) finish(std::true_type{});
+    else     finish(std::false_type{});
 }
 
 // k_int8_few: for rows by the ten, where the weights' bytes are all there is to do (one row of 4096 bf16, 4096 channels: 6 us, 2.8
@@ -430,7 +443,7 @@ __global__ void __launch_bounds__(kFewBlock) k_int8_few(DenseInt8Args a, Quantiz
 #pragma unroll
         for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][t][v][l];
         const float scale = kFused ? row_scale(s_most[r & 15]).scale : a.scale[r];
-        store_at<T>(a.out, r, c, output_of(sum, a.w_scale[c], scale, a.bias ? a.bias[c] : 0.f, a.relu));
+        store_at<T>(a.out, r, c, output_of<true>(sum, a.w_scale[c], scale, a.bias ? a.bias[c] : 0.f, a.relu));
     }
 }
 
@@ -468,6 +481,9 @@ __global__ void __launch_bounds__(kWaves * kWave) k_int8_rows(DenseInt8Args a, Q
         s_bias[i] = a.bias ? a.bias[i < n ? i : n - 1] : 0.f;
     }
     __syncthreads();
+    bool far = false;
+    for (int32_t i = lane_id(); i < n16; i += kWave) far |= fabsf(s_scale[i]) > kFarScale;
+    far = __ballot(far) != 0;
     const int32_t tiles = (rows + 15) / 16;
     const bool stores = n % 4 == 0 && reinterpret_cast<uintptr_t>(a.out.data) % 16 == 0 && (uint64_t) a.out.stride * sizeof(T) % 16 == 0;
     // A tile's rows are read when the one before has been quantised, and come while that one is multiplied and stored.  Rows past
@@ -530,16 +546,16 @@ __global__ void __launch_bounds__(kWaves * kWave) k_int8_rows(DenseInt8Args a, Q
                     acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const int4v*>(w[g] + s * 64), right, acc[g], 0, 0, 0);
             }
             // element i of lane l is output column 4 * (l / 16) + i of row l % 16
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
+            auto store_group = [&](auto is_far, int g) {
+                constexpr bool kFar = decltype(is_far)::value;
                 const int32_t c = c0 + g * 16 + 4 * kg;
-                if (c0 + g * 16 >= n16 || r0 + l16 >= rows) continue;
+                if (c0 + g * 16 >= n16 || r0 + l16 >= rows) return;
                 const float4 ws = *reinterpret_cast<const float4*>(s_scale + c), b = *reinterpret_cast<const float4*>(s_bias + c);
                 struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
-                y.v[0] = from_float<T>(output_of(acc[g][0], ws.x, scale, b.x, a.relu));
-                y.v[1] = from_float<T>(output_of(acc[g][1], ws.y, scale, b.y, a.relu));
-                y.v[2] = from_float<T>(output_of(acc[g][2], ws.z, scale, b.z, a.relu));
-                y.v[3] = from_float<T>(output_of(acc[g][3], ws.w, scale, b.w, a.relu));
+                y.v[0] = from_float<T>(output_of<kFar>(acc[g][0], ws.x, scale, b.x, a.relu));
+                y.v[1] = from_float<T>(output_of<kFar>(acc[g][1], ws.y, scale, b.y, a.relu));
+                y.v[2] = from_float<T>(output_of<kFar>(acc[g][2], ws.z, scale, b.z, a.relu));
+                y.v[3] = from_float<T>(output_of<kFar>(acc[g][3], ws.w, scale, b.w, a.relu));
                 if (stores) {
                     if (c < n) *reinterpret_cast<Four*>(out + c) = y;
                 } else {
@@ -547,6 +563,13 @@ __global__ void __launch_bounds__(kWaves * kWave) k_int8_rows(DenseInt8Args a, Q
                     for (int i = 0; i < 4; ++i)
                         if (c + i < n) out[c + i] = y.v[i];
                 }
+            };
+            if (far) {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) store_group(std::true_type{}, g);
+            } else {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) store_group(std::false_type{}, g);
             }
         }
         __builtin_amdgcn_wave_barrier();

@@ -298,3 +298,33 @@ def test_calls_with_empty_tensors(ctx, dtype):
         learn.gns_dense_int8(ctx, q, scale, 40, None, scales, None, False, none(24, t=dtype), 0)
     with pytest.raises(B.GnsError):
         learn.gns_sage_dense_backward(ctx, none(24, t=dtype), None, one, 40, two, 3, w, None, None, None, 0, space)
+
+
+@TYPES
+@pytest.mark.parametrize("rows,k,n", [(3, 64, 40), (20, 100, 33), (50, 64, 64), (100, 300, 47), (2100, 64, 2051), (2600, 1100, 4099)])
+def test_product_of_scales_far_apart(ctx, rows, k, n, dtype):
+    """A large scale of one side and a small one of the other: what is finite comes out finite, whichever is which."""
+    q = torch.full((rows, learn.int8_stride(k)), 0, dtype=torch.int8)
+    q[:, :k] = 127
+    wq = q[:1].repeat(n, 1)
+    for row_scale, channel_scale in ((2.0 ** -100, 2.0 ** 118), (2.0 ** 118, 2.0 ** -100)):
+        out = torch.zeros(rows, n, dtype=dtype, device="cuda")
+        learn.gns_dense_int8(ctx, q.cuda(), torch.full((rows,), row_scale, device="cuda"), k, wq.cuda(), torch.full((n,), channel_scale, device="cuda"),
+                             None, False, out, rows)
+        want = 127.0 * 127.0 * k * 2.0 ** 18
+        within(f64(out), np.full((rows, n), want), (2.0 ** -8 if dtype == BF16 else 2 * U) * want)
+
+
+@TYPES
+@pytest.mark.parametrize("rows", [5, 100, 9000])
+def test_update_step_of_scales_far_apart(ctx, rows, dtype):
+    k, n = 64, 48
+    x = torch.full((rows, k), 127 * 2.0 ** -100, dtype=dtype, device="cuda")
+    x[1] = math.nan                                          # a spoilt row stays one
+    wq = torch.full((n, k), 127, dtype=torch.int8, device="cuda")
+    out = torch.zeros(rows, n, dtype=dtype, device="cuda")
+    space = learn.alloc_workspace(learn.gns_sage_dense_int8_workspace_bytes(ctx, k, rows))
+    learn.gns_sage_dense_int8(ctx, x, None, wq, torch.full((n,), 2.0 ** 118, device="cuda"), None, False, out, rows, space)
+    want = np.full((rows, n), 127.0 * 127.0 * k * 2.0 ** 18)
+    want[1] = math.nan
+    within(f64(out), want, (2.0 ** -8 if dtype == BF16 else 2 * U) * np.nan_to_num(want))
