@@ -201,8 +201,10 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, BM == 128 ? 3 :
     __shared__ float s_scale[BM], s_w_scale[BN], s_bias[BN];
     const int32_t rows = a.count.get(), n = a.out.width;
     const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
+    const int32_t block = (int32_t) (blockIdx.y * gridDim.x + blockIdx.x);
+    if (block >= m_tiles * n_tiles) return;
     int32_t tm, tn;
-    tile_of(xcd_run((int32_t) blockIdx.x, m_tiles * n_tiles), m_tiles, n_tiles, &tm, &tn);
+    tile_of(xcd_run(block, m_tiles * n_tiles), m_tiles, n_tiles, &tm, &tn);
     const int64_t m0 = (int64_t) tm * BM;
     const int32_t n0 = tn * BN;
     if (m0 >= rows) return;
@@ -606,10 +608,11 @@ hipError_t launch_quantize(const gns_ctx* c, const QuantizeArgs& a, int32_t type
 template <typename T, int BM, int BN, int WM, int WN>
 static hipError_t launch_tiles(const DenseInt8Args& a, hipStream_t s)
 {
-    const int64_t m_tiles = ((int64_t) a.count.rows + BM - 1) / BM, n_tiles = (a.out.width + BN - 1) / BN;
-    if (m_tiles * n_tiles > (1 << 22)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_int8_tiles<T, BM, BN, WM, WN>), dim3((unsigned) (m_tiles * n_tiles)), dim3((BM / WM) * (BN / WN) * kWave), 0, s, a,
-                       (int32_t) m_tiles, (int32_t) n_tiles);
+    // a dimension of a grid has fewer than 2^32 threads; 2^31 tiles of outputs fit no memory
+    const int64_t m_tiles = ((int64_t) a.count.rows + BM - 1) / BM, n_tiles = (a.out.width + BN - 1) / BN, tiles = m_tiles * n_tiles, most = 1 << 22;
+    if (tiles > INT32_MAX - most) return hipErrorInvalidValue;
+    const dim3 grid((unsigned) (tiles < most ? tiles : most), (unsigned) ((tiles + most - 1) / most));
+    hipLaunchKernelGGL((k_int8_tiles<T, BM, BN, WM, WN>), grid, dim3((BM / WM) * (BN / WN) * kWave), 0, s, a, (int32_t) m_tiles, (int32_t) n_tiles);
     return hipGetLastError();
 }
 

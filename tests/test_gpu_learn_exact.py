@@ -328,3 +328,20 @@ def test_update_step_of_scales_far_apart(ctx, rows, dtype):
     want = np.full((rows, n), 127.0 * 127.0 * k * 2.0 ** 18)
     want[1] = math.nan
     within(f64(out), want, (2.0 ** -8 if dtype == BF16 else 2 * U) * np.nan_to_num(want))
+
+
+def test_product_of_very_many_rows(ctx):
+    """More tiles than the 2^22 that one dimension of a grid is given."""
+    rows, k, n = (1 << 29) + 12345, 16, 1
+    q = torch.zeros(rows, learn.int8_stride(k), dtype=torch.int8, device="cuda")
+    scale, out = torch.ones(rows, device="cuda"), torch.full((rows, n), 9.0, device="cuda")
+    at = torch.tensor([0, 1, 127, 128, 4097, (1 << 29) - 1, 1 << 29, (1 << 29) + 200, rows - 1], device="cuda")
+    q[at, 0] = torch.arange(1, at.numel() + 1, dtype=torch.int8, device="cuda")
+    wq = torch.zeros(n, learn.int8_stride(k), dtype=torch.int8, device="cuda")
+    wq[0, 0] = 3
+    learn.gns_dense_int8(ctx, q, scale, k, wq, torch.ones(n, device="cuda"), None, False, out, rows)
+    assert torch.equal(out[at, 0], 3.0 * torch.arange(1, at.numel() + 1, device="cuda"))
+    out[at] = 0.0
+    assert int(torch.count_nonzero(out)) == 0
+    del q, scale, out
+    torch.cuda.empty_cache()                                 # 39 GB
