@@ -120,7 +120,7 @@ gns_status gns_log_probs(gns_ctx* ctx, const gns_rows* logits, const int32_t* la
 /* The gradient of sum_r g_logp[r] * logp[r] + g_entropy[r] * entropy[r] with respect to the logits:
  *   d_logits[r, j] = g_logp[r] * ([j = labels[r]] - p_j) - g_entropy[r] * p_j * (log p_j + entropy[r])
  * from the stats and entropy that gns_log_probs wrote.  A row without a label has no first term; rows without any class
- * left get zeros; rows of NaN, or with a label >= C, get NaN.  Either term may be left out (g_logp or g_entropy NULL; what
+ * left get zeros; rows of NaN, or with a label >= C, get NaN; p_j below 2^-126 counts as zero.  Either term may be left out (g_logp or g_entropy NULL; what
  * else the term needs is then not read), not both.  d_logits has the width of the logits, either type, and may be the logits' own rows (same data, stride
  * and type). */
 gns_status gns_log_probs_backward(gns_ctx* ctx, const gns_rows* logits, const int32_t* labels_dev, const float* stats_dev,

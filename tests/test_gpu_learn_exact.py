@@ -144,6 +144,22 @@ def test_weights_gradient_keeps_every_bit(ctx, rows, f1, f2, hdim, least, dtype)
         assert torch.equal(dw.cpu(), want) and torch.equal(db.cpu(), value.float())
 
 
+@TYPES
+@pytest.mark.parametrize("classes", [11, 47, 200, 300, 4097])
+def test_probabilities_far_below_the_largest(ctx, classes, dtype):
+    """The gradient is -p with p = e^z, of logits that are log probabilities as they are: the exponential is good to a unit in the last
+    place and two roundings wherever z is, not to |z| of them."""
+    z = -torch.linspace(0.0, 80.0, 3 * classes).view(3, classes)
+    z = z.to(dtype)
+    stats = torch.zeros(3, 2, device="cuda")
+    labels = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for how in ("packed", "odd"):
+        out = layout(torch.zeros(3, classes), how)
+        learn.gns_log_probs_backward(ctx, layout(z, how), labels, stats, None, torch.ones(3, device="cuda"), None, out, 3)
+        want = -np.exp(f64(z))
+        within(f64(out)[:, 1:], want[:, 1:], 4 * U * np.abs(want[:, 1:]))
+
+
 def times(a, b):
     """a @ b in 64 bits, with each product's infinities and NaN."""
     y = a @ b
