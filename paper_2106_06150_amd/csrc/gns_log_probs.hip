@@ -369,7 +369,8 @@ __global__ void __launch_bounds__(kBlock) k_log_probs_long(LongArgs g)
     }
 }
 
-// A wave per row: its parts' sums and best classes, which are on their way first.  Bound by latency, 6 to 7 us.
+// A wave per row: its parts' sums and best classes, which are on their way first.  A row has no more best classes in its parts than
+// a wave reads at once (split_rows).  Bound by latency, 6 to 7 us.
 constexpr int kJoinKeys = 16;                 // of a lane
 template <typename T>
 __global__ void __launch_bounds__(kWave) k_log_probs_join(LongArgs g)
@@ -382,19 +383,17 @@ __global__ void __launch_bounds__(kWave) k_log_probs_join(LongArgs g)
         const Key* from = g.best + r * n;
         float z[kJoinKeys];
         int32_t index[kJoinKeys];
-        float largest;
-        auto fetch = [&](int32_t i0) {
-            largest = kNone;
+        float largest = kNone;
+        if (top) {
 #pragma unroll
             for (int j = 0; j < kJoinKeys; ++j) {
-                const int32_t i = i0 + j * kWave + lane;
+                const int32_t i = j * kWave + lane;
                 const Key k = i < n ? from[i] : kNoKey;
                 z[j] = value_of(k);
                 index[j] = index_of(k);
                 largest = fmaxf(largest, z[j]);
             }
-        };
-        if (top) fetch(0);
+        }
         int32_t label;
         const float z_label = label_logit<T>(a, r, &label);
         Softmax s = {kNone, 0.f, 0.f};
@@ -411,12 +410,7 @@ __global__ void __launch_bounds__(kWave) k_log_probs_join(LongArgs g)
         if (!top) continue;
         WaveList list = empty_list();
         bound_by_lanes(list, largest, top);
-        for (int32_t i0 = 0;;) {
-            take_up(list, z, largest, top, [&](int j) { return index[j]; });
-            i0 += kWave * kJoinKeys;
-            if (i0 >= n) break;
-            fetch(i0);
-        }
+        take_up(list, z, largest, top, [&](int j) { return index[j]; });
         if (lane < top) {
             const bool gone = o.bad || list.mine == kNoKey;
             a.top_index[r * top + lane] = gone ? -1 : index_of(list.mine);
