@@ -361,3 +361,200 @@ def test_product_of_very_many_rows(ctx):
     assert int(torch.count_nonzero(out)) == 0
     del q, scale, out
     torch.cuda.empty_cache()                                 # 39 GB
+
+
+# ---- sizes at which a kernel takes over -----------------------------------------------------------------------------
+@TYPES
+@pytest.mark.parametrize("rows,f1,f2", [(5, 4100, 0), (70, 8000, 191), (3, 8191, 0), (40, 8195, 0), (9, 16384, 0), (600, 6000, 0)])
+def test_quantize_rows_of_a_block(ctx, rows, f1, f2, dtype):
+    """Rows that a whole block has: each value half a step off at most (and the inverse's two roundings), the largest 127 steps."""
+    k = f1 + f2
+    x = (torch.randn(rows, k, generator=gen("block", rows, k)) * torch.exp(torch.randn(rows, 1, generator=gen(rows)))).to(dtype)
+    x[0, k - 1] = 100.0
+    if rows > 4:
+        x[1], x[2, k // 2], x[3, 0] = 0.0, math.inf, math.nan
+    for how in ("packed", "odd"):
+        q = torch.full((rows, learn.int8_stride(k)), 77, dtype=torch.int8, device="cuda")
+        scale = torch.full((rows,), -1.0, device="cuda")
+        learn.gns_quantize_rows(ctx, layout(x[:, :f1], how), layout(x[:, f1:], how) if f2 else None, q, scale, rows)
+        a = x.cuda().double().abs().amax(1, keepdim=True)
+        good = torch.isfinite(a[:, 0]) & (a[:, 0] > 0)
+        steps = x.cuda().double()[good] * 127.0 / a[good]
+        assert float((q[good][:, :k].double() - steps).abs().max()) <= 0.5 + 127 * 4 * U
+        assert bool((q[good][:, :k].abs().amax(1) == 127).all())
+        assert not q[:, k:].any() and not q[~good].any()
+        want = f64(a[:, 0] / 127.0)
+        want[f64(~good) > 0] = np.where(f64(a[:, 0])[f64(~good) > 0] == 0, 0.0, np.nan)
+        within(f64(scale), want, U * np.nan_to_num(np.abs(want)))
+
+
+# 128 x 128 and 256 x 256 outputs a block, the longest sums
+@TYPES
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("rows,k,n", [(2100, 300, 2051), (2049, 1000, 2048), (3001, 1100, 4099), (10000, 1500, 1030), (65, 131072, 70),
+                                      (1, 131072, 40), (20, 131071, 20), (33, 100000, 100)])
+def test_int8_product_of_large_tiles_and_long_sums(ctx, rows, k, n, relu, dtype):
+    g = torch.Generator(device="cuda").manual_seed(rows + k + n)
+    q = torch.randint(-127, 128, (rows, learn.int8_stride(k)), generator=g, dtype=torch.int8, device="cuda")
+    w = torch.randint(-127, 128, (n, learn.int8_stride(k)), generator=g, dtype=torch.int8, device="cuda")
+    q[:, k:] = 0
+    q[rows // 2, :k], w[n // 2, :k], w[0, :k] = 127, -127, 127
+    scale, w_scale = torch.rand(rows, generator=g, device="cuda") * 0.05, torch.rand(n, generator=g, device="cuda") * 0.01
+    bias = torch.randn(n, generator=g, device="cuda") if rows % 2 else None
+    y = (q[:, :k].double() @ w[:, :k].double().t().contiguous()) * scale.double()[:, None] * w_scale.double()
+    size = y.abs() + (0.0 if bias is None else bias.double().abs())
+    y = y if bias is None else y + bias.double()
+    y = y.relu() if relu else y
+    bound = 4 * U * size + (2.0 ** -8 * y.abs() if dtype == BF16 else 0.0) + 2.0 ** -133
+    for how in ("packed", "odd"):
+        out = layout(torch.full((rows, n), 9.0, dtype=dtype), how)
+        learn.gns_dense_int8(ctx, q, scale, k, w, w_scale, bias, relu, out, rows)
+        off = (out.double() - y).abs() - bound
+        assert float(off.max()) <= 0.0, int(off.argmax())
+
+
+@TYPES
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("rows,f1,f2,hdim,dw", WAYS + [(17000, 300, 0, 264, True), (16385, 300, 0, 520, False)])
+def test_backward_in_every_way(ctx, rows, f1, f2, hdim, dw, relu, dtype):
+    """Normal values.  Errors of sums of so many roundings add up as a random walk: eight of its standard deviations at most."""
+    k = f1 + f2
+    g = torch.Generator(device="cuda").manual_seed(rows + k + hdim)
+    x = torch.randn(rows, k, generator=g, device="cuda")
+    d_out = (torch.randn(rows, hdim, generator=g, device="cuda") * 1e-2).to(dtype)
+    w = torch.randn(k, hdim, generator=g, device="cuda") / math.sqrt(k)
+    mask = torch.rand(rows, hdim, generator=g, device="cuda") < 0.5
+    dz = d_out.double() * mask if relu else d_out.double()
+    one, two = two_checkpoints(ctx, x, f1, f2) if dw else (None, None)
+    if relu:
+        d_out = torch.where(mask, d_out, torch.full_like(d_out, math.nan))
+    for how in ("packed", "odd"):
+        got_dw, db, dx = backward(ctx, layout(d_out, how), words_of(mask) if relu else None, one, f1, two, f2, w, dw, True)
+        want = dz @ w.double().t().contiguous()
+        size = ((dz * dz) @ (w.double() ** 2).t().contiguous()).sqrt()
+        bound = 8 * U * size * math.sqrt(hdim + 8) + (2.0 ** -8 * want.abs() if dtype == BF16 else 0.0) + 2.0 ** -126
+        assert float(((dx.double() - want).abs() - bound).max()) <= 0.0
+        if dw:
+            values = []
+            for p, f in ((one, f1), (two, f2)):
+                if f:
+                    values.append(torch.empty(rows, f, device="cuda"))
+                    learn.gns_checkpoint_load(ctx, *p, values[-1], rows)
+            x64 = torch.cat(values, 1).double()
+            want, size = x64.t().contiguous() @ dz, ((x64 * x64).t().contiguous() @ (dz * dz)).sqrt()
+            assert float(((got_dw.double() - want).abs() - 8 * U * size * math.sqrt(rows + 8) - 2.0 ** -126).max()) <= 0.0
+            want, size = dz.sum(0), (dz * dz).sum(0).sqrt()
+            assert float(((db.double() - want).abs() - 8 * U * size * math.sqrt(rows + 8) - 2.0 ** -126).max()) <= 0.0
+
+
+@TYPES
+@pytest.mark.parametrize("rows,classes,top", [(1500, 2100, 20), (4200, 5003, 20), (9000, 1025, 3), (700, 30011, 32), (5000, 300, 0)])
+def test_log_probs_of_many_long_rows(ctx, rows, classes, top, dtype):
+    """Whole rows of several tiles a wave, against 64 bits on the device."""
+    g = torch.Generator(device="cuda").manual_seed(rows + classes)
+    z = (torch.randn(rows, classes, generator=g, device="cuda") * 3).to(dtype)
+    z[5::16] = torch.where(torch.rand(z[5::16].shape, generator=g, device="cuda") < 0.5, torch.full((), -math.inf, dtype=dtype, device="cuda"), z[5::16])
+    z[7] = -math.inf
+    z[9] = 0.25
+    labels = torch.randint(0, classes, (rows,), generator=g, dtype=torch.int32, device="cuda")
+    labels[::17] = -1
+    z64 = z.double()
+    m = z64.amax(1)
+    safe = torch.where(torch.isinf(m), torch.zeros_like(m), m)
+    d = z64 - safe[:, None]
+    p = d.exp()
+    s = p.sum(1)
+    none = torch.isinf(m)
+    log_s = torch.where(none, torch.zeros_like(s), s.log())
+    entropy = torch.where(none, torch.zeros_like(s), log_s - torch.where(p > 0, p * d, torch.zeros_like(p)).sum(1) / s.clamp(min=1e-300))
+    at = d.gather(1, labels.clamp(min=0).long()[:, None])[:, 0] - log_s
+    logp = torch.where(labels < 0, torch.zeros_like(at), at)
+    logp[none & (labels >= 0)] = -math.inf
+    order = torch.sort(z64, dim=1, descending=True, stable=True)
+    index = torch.where(torch.isinf(order.values[:, :top]), torch.full((), -1, device="cuda"), order.indices[:, :top])
+    chain = 64 + classes / 64 + 16
+    tol = 2 * U * (chain + 2 * log_s.abs())
+    for how in ("packed", "odd"):
+        out = dict(logp=torch.full((rows,), 9.0, device="cuda"), entropy=torch.full((rows,), 9.0, device="cuda"), stats=torch.full((rows, 2), 9.0, device="cuda"))
+        best, value = (torch.full((rows, top), 9, dtype=t, device="cuda") if top else None for t in (torch.int32, FP32))
+        space = learn.alloc_workspace(learn.gns_log_probs_workspace_bytes(ctx, classes, top, rows))
+        learn.gns_log_probs(ctx, layout(z, how), labels, out["logp"], out["entropy"], out["stats"], best, value, rows, space)
+        within(f64(out["logp"]), f64(logp), f64(tol + 4 * U * torch.nan_to_num(logp.abs(), posinf=0.0)))
+        within(f64(out["entropy"]), f64(entropy), f64(2 * U * chain * (1 + entropy.abs() + log_s.abs())))
+        within(f64(out["stats"][:, 0]), f64(m), 0.0)
+        within(f64(out["stats"][:, 1]), f64(log_s), f64(tol))
+        if top:
+            assert torch.equal(best.long(), index)
+            want = order.values[:, :top] - (safe + log_s)[:, None]
+            within(f64(value), f64(want), f64(tol[:, None] + 4 * U * torch.nan_to_num(want.abs(), posinf=0.0)))
+
+
+@TYPES
+@pytest.mark.parametrize("rows,f1,f2", [(40, 50, 0), (200, 7, 57), (30, 1500, 0), (9, 1025, 900), (33, 513, 0), (5, 2048, 0)])
+def test_quantize_rows_of_a_few_lanes_or_a_wave(ctx, rows, f1, f2, dtype):
+    """Half a step off at most (and the inverse's two roundings), the largest 127 steps."""
+    k = f1 + f2
+    x = (torch.randn(rows, k, generator=gen("lanes", rows, k)) * torch.exp(torch.randn(rows, 1, generator=gen(rows)))).to(dtype)
+    for how in ("packed", "odd"):
+        q = torch.full((rows, learn.int8_stride(k)), 77, dtype=torch.int8, device="cuda")
+        scale = torch.full((rows,), -1.0, device="cuda")
+        learn.gns_quantize_rows(ctx, layout(x[:, :f1], how), layout(x[:, f1:], how) if f2 else None, q, scale, rows)
+        a = x.cuda().double().abs().amax(1, keepdim=True)
+        assert float((q[:, :k].double() - x.cuda().double() * 127.0 / a).abs().max()) <= 0.5 + 127 * 4 * U
+        assert bool((q[:, :k].abs().amax(1) == 127).all()) and not q[:, k:].any()
+        want = f64(a[:, 0] / 127.0)
+        within(f64(scale), want, U * want)
+
+
+# inputs of one type and outputs of the other; weights that leave eight waves' room in LDS and not sixteen's
+@pytest.mark.parametrize("rows,f1,f2,n", [(1, 300, 0, 70), (7, 100, 29, 33), (16, 1024, 0, 40), (100, 200, 0, 65), (9001, 128, 0, 900), (8300, 256, 0, 400),
+                                          (8192, 504, 0, 100), (8250, 64, 0, 1650), (9000, 100, 28, 908)])
+@pytest.mark.parametrize("x_type,out_type", [(FP32, FP32), (FP32, BF16), (BF16, FP32), (BF16, BF16)])
+def test_update_step_of_mixed_types_and_wide_weights(ctx, rows, f1, f2, n, x_type, out_type):
+    k = f1 + f2
+    g = torch.Generator(device="cuda").manual_seed(rows + k + n)
+    x = torch.randn(rows, k, generator=g, device="cuda").to(x_type)
+    w = torch.randint(-127, 128, (n, learn.int8_stride(k)), generator=g, dtype=torch.int8, device="cuda")
+    w_scale, bias = torch.rand(n, generator=g, device="cuda") * 0.01, torch.randn(n, generator=g, device="cuda")
+    q = torch.empty(rows, learn.int8_stride(k), dtype=torch.int8, device="cuda")
+    scale = torch.empty(rows, device="cuda")
+    learn.gns_quantize_rows(ctx, x, None, q, scale, rows)
+    y = (q[:, :k].double() @ w[:, :k].double().t().contiguous()) * scale.double()[:, None] * w_scale.double()
+    size = y.abs() + bias.double().abs()
+    y = (y + bias.double()).relu()
+    bound = 4 * U * size + (2.0 ** -8 * y.abs() if out_type == BF16 else 0.0)
+    space = learn.alloc_workspace(learn.gns_sage_dense_int8_workspace_bytes(ctx, k, rows))
+    for how in ("packed", "odd"):
+        out = layout(torch.full((rows, n), 9.0, dtype=out_type), how)
+        one, two = layout(x[:, :f1], how), layout(x[:, f1:], how) if f2 else None
+        learn.gns_sage_dense_int8(ctx, one, two, w, w_scale, bias, True, out, rows, space)
+        assert float(((out.double() - y).abs() - bound).max()) <= 0.0
+
+
+@TYPES
+@pytest.mark.parametrize("entropy_term", [False, True])
+@pytest.mark.parametrize("classes", [300, 4099])
+def test_gradient_that_lies_unlike_its_logits(ctx, classes, entropy_term, dtype):
+    """Logits and gradients at different places against the 16-byte marks: the same results as at like ones, but for the order in which
+    a product is rounded."""
+    rows = 40
+    g = gen("unlike", classes)
+    z = (torch.randn(rows, classes, generator=g) * 3).to(dtype)
+    labels = torch.randint(0, classes, (rows,), generator=g, dtype=torch.int32).cuda()
+    g_logp, g_entropy = torch.randn(rows, generator=g).cuda(), torch.randn(rows, generator=g).cuda()
+    log_p = torch.log_softmax(z.double(), 1)
+    stats = torch.stack([z.double().amax(1), torch.logsumexp(z.double(), 1) - z.double().amax(1)], 1).float().cuda()
+    entropy = -(log_p.exp() * log_p).sum(1).float().cuda()
+    want_log_p = z.cuda().double() - stats[:, :1].double() - stats[:, 1:].double()
+    p = want_log_p.exp()
+    one = torch.nn.functional.one_hot(labels.long(), classes).double()
+    want = g_logp.double()[:, None] * (one - p)
+    size = g_logp.double().abs()[:, None] * (one + p * (8 + want_log_p.abs()))
+    if entropy_term:
+        want = want - g_entropy.double()[:, None] * p * (want_log_p + entropy.double()[:, None])
+        size = size + g_entropy.double().abs()[:, None] * p * (8 + want_log_p.abs()) * (1 + want_log_p.abs() + entropy.double()[:, None])
+    bound = 4 * U * size + (2.0 ** -8 * want.abs() if dtype == BF16 else 0.0) + 2.0 ** -126
+    for how, out_how in (("packed", "odd"), ("odd", "packed"), ("odd", "odd")):
+        out = layout(torch.full((rows, classes), 9.0, dtype=dtype), out_how)
+        learn.gns_log_probs_backward(ctx, layout(z, how), labels, stats, entropy if entropy_term else None, g_logp, g_entropy if entropy_term else None, out, rows)
+        assert float(((out.double() - want).abs() - bound).max()) <= 0.0
