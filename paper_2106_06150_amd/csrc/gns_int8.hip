@@ -589,8 +589,13 @@ static hipError_t launch_quantize_typed(const gns_ctx* c, const QuantizeArgs& a,
 {
     const int64_t rows = a.count.rows, pieces = a.stride / kPiece<T>;
     const dim3 short_grid(grid_of(c, (rows + 15) / 16, 32)), wave_grid(grid_of(c, (rows + 3) / 4, 32)), block_grid(grid_of(c, rows, 32));
-    if (pieces <= 8)         hipLaunchKernelGGL((k_quantize_rows<T, 4, 2>), dim3(grid_of(c, (rows + 63) / 64, 32)), dim3(kBlock), 0, s, a);
-    else if (pieces <= 32)   hipLaunchKernelGGL((k_quantize_rows<T, 16, 2>), short_grid, dim3(kBlock), 0, s, a);
+    if constexpr (kPiece<T> == 8) {               // rows in 8 bits are 64 bytes at least, sixteen pieces of fp32
+        if (pieces <= 8) {
+            hipLaunchKernelGGL((k_quantize_rows<T, 4, 2>), dim3(grid_of(c, (rows + 63) / 64, 32)), dim3(kBlock), 0, s, a);
+            return hipGetLastError();
+        }
+    }
+    if (pieces <= 32)        hipLaunchKernelGGL((k_quantize_rows<T, 16, 2>), short_grid, dim3(kBlock), 0, s, a);
     else if (pieces <= 64)   hipLaunchKernelGGL((k_quantize_rows<T, 16, 4>), short_grid, dim3(kBlock), 0, s, a);
     else if (pieces <= 256)  hipLaunchKernelGGL((k_quantize_rows<T, 64, 4>), wave_grid, dim3(kBlock), 0, s, a);
     else if (pieces <= 512)  hipLaunchKernelGGL((k_quantize_rows<T, 64, 8>), wave_grid, dim3(kBlock), 0, s, a);
