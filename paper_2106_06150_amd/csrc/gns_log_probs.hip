@@ -13,7 +13,7 @@ constexpr float kFar = -1000.f;               // e^kFar is zero in fp32
 
 // e^x but for an error of |x| roundings.  In the sums it adds up to no more than log S is rounded by, since the mean of |z - m| by
 // the probabilities is at most log S, and T / S does not notice what S and T share: with exact_exp_of the entropy of 4096 rows of
-// 100,003 classes is 8.4e-8 off in the 2-norm and not 8.6e-8, and the call takes 18 % longer.
+// 100,003 classes was 2 % nearer in the 2-norm, and the call took 18 % longer.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
 
 // e^x to two roundings, where single values are results (the gradient, bound by its bytes): 2^t times 1 + (x - t log 2).  Below
@@ -92,26 +92,30 @@ __device__ __forceinline__ void raise(Softmax& s, float most)
     }
 }
 
-// Adds N values none of which is above s.m.  Masked ones (-infinity) make T NaN, and it is summed once more with their share
-// left out: a test per value would cost all rows what only masked ones need.
+// Adds N values none of which is above s.m, summed first, so that a long row's sums are rounded once for N of them (the entropy of
+// 100,003 classes 5.2e-8 off in the 2-norm, 8.6e-8 one by one).  Masked ones (-infinity) make T NaN, and it is summed once more with
+// their share left out: a test per value would cost all rows what only masked ones need.
 template <int N>
 __device__ __forceinline__ void add_values(Softmax& s, const float (&z)[N])
 {
-    const float m = s.m == -__builtin_inff() ? 0.f : s.m, T0 = s.T;
+    const float m = s.m == -__builtin_inff() ? 0.f : s.m;
+    float S = 0.f, T = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const float d = z[i] - m, p = exp_of(d);
-        s.S += p;
-        s.T = fmaf(p, d, s.T);
+        S += p;
+        T = fmaf(p, d, T);
     }
-    if (__builtin_expect(s.T != s.T, 0)) {
-        s.T = T0;
+    if (__builtin_expect(T != T, 0)) {
+        T = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float d = z[i] - m;
-            s.T = fmaf(exp_of(d), fmaxf(d, kFar), s.T);
+            T = fmaf(exp_of(d), fmaxf(d, kFar), T);
         }
     }
+    s.S += S;
+    s.T += T;
 }
 
 // The sums of a group of L lanes; every lane gets them.
