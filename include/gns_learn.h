@@ -47,9 +47,10 @@ typedef struct {
 #define GNS_INT8_MAX_K 131072 /* 127 * 127 * k stays below 2^31 */
 
 /* Quantises rows [x1 | x2] (x2 may be NULL; both of one type) of together k <= GNS_INT8_MAX_K columns: a = max |x[r, :]|,
- * scale[r] = a / 127, q[r, c] = x[r, c] * (127 * (1 / a)) rounded to nearest, ties to even, each operation in fp32.  A row whose a is
- * below 2^-120 gets scale 0 and zeros; one with an infinity or NaN gets scale NaN and zeros.  Also the way to quantise
- * weights, given as hdim rows of k (one scale per output channel). */
+ * scale[r] = a / 127, q[r, c] = x[r, c] * (127 * (1 / a)) rounded to nearest, ties to even, each operation in fp32: half a
+ * step off and two roundings at most (halfway between two steps it may be either).  A row whose a is below 2^-120 gets
+ * scale 0 and zeros; one with an infinity or NaN gets scale NaN and zeros.  Also the way to quantise weights, given as
+ * hdim rows of k (one scale per output channel). */
 gns_status gns_quantize_rows(gns_ctx* ctx, const gns_rows* x1, const gns_rows* x2, int8_t* q_dev, float* scale_dev,
                              int32_t num_rows, void* hip_stream);
 
@@ -91,7 +92,9 @@ gns_status gns_checkpoint_load(gns_ctx* ctx, const int8_t* q_dev, const uint8_t*
  *   dx[r, k] = sum_n dz[r, n] * w[k, n]     rows of f1 + f2 columns, in d_out's type, or NULL; w fp32[(f1 + f2) x hdim]
  * hdim = d_out->width.  dw may be NULL (then neither checkpoint is read).  Products have fp32's precision (fp32 values are
  * split into three bf16 terms), sums are fp32.  Infinities and NaN go where these formulas take them: an infinity stays one
- * unless it meets a zero or its opposite.  With no rows dw and db are zero.  workspace: gns_sage_dense_backward_workspace_bytes(...) bytes, 256-byte aligned. */
+ * unless it meets a zero or its opposite (each such result is summed by a thread alone; a call with very many takes
+ * long).  With no rows dw and db are zero.  workspace: gns_sage_dense_backward_workspace_bytes(...) bytes, 256-byte
+ * aligned. */
 size_t gns_sage_dense_backward_workspace_bytes(const gns_ctx* ctx, int32_t f1, int32_t f2, int32_t hdim, int32_t num_rows);
 gns_status gns_sage_dense_backward(gns_ctx* ctx, const gns_rows* d_out, const uint32_t* positive_dev,
                                    const int8_t* q1_dev, const uint8_t* exponents1_dev, int32_t f1,
@@ -120,9 +123,9 @@ gns_status gns_log_probs(gns_ctx* ctx, const gns_rows* logits, const int32_t* la
 /* The gradient of sum_r g_logp[r] * logp[r] + g_entropy[r] * entropy[r] with respect to the logits:
  *   d_logits[r, j] = g_logp[r] * ([j = labels[r]] - p_j) - g_entropy[r] * p_j * (log p_j + entropy[r])
  * from the stats and entropy that gns_log_probs wrote.  A row without a label has no first term; rows without any class
- * left get zeros; rows of NaN, or with a label >= C, get NaN; p_j below 2^-126 counts as zero.  Either term may be left out (g_logp or g_entropy NULL; what
- * else the term needs is then not read), not both.  d_logits has the width of the logits, either type, and may be the logits' own rows (same data, stride
- * and type). */
+ * left get zeros; rows of NaN, or with a label >= C, get NaN; p_j below 2^-126 counts as zero.  Either term may be left
+ * out (g_logp or g_entropy NULL; what else the term needs is then not read), not both.  d_logits has the width of the
+ * logits, either type, and may be the logits' own rows (same data, stride and type). */
 gns_status gns_log_probs_backward(gns_ctx* ctx, const gns_rows* logits, const int32_t* labels_dev, const float* stats_dev,
                                   const float* entropy_dev, const float* g_logp_dev, const float* g_entropy_dev,
                                   const gns_rows* d_logits, int32_t num_rows, void* hip_stream);

@@ -1,11 +1,11 @@
 // The backward pass of the update step out = g([x1 | x2] . W + b), with the layer's inputs from their 8-bit checkpoints:
 //   dz = d_out where the output was positive,  dw = X^T dz,  db = sum_r dz,  dx = dz W^T.
 // Both products run on the bf16 matrix cores at fp32's precision.  A checkpoint's values q * 2^e are bf16 values as they are.
-// An fp32 value is cut into three bf16 terms, each what is left rounded to nearest, which hold it exactly: so dw takes three products of fp32
-// gradients and one of bf16 ones, and is exact up to the fp32 sums.  dx of bf16 gradients takes three products with W's terms and
-// is as exact (two terms of W moved single bf16 results: 2.1e-4 of dx's 2-norm from the fp32 products' at hdim 4096, three 1.6e-5, and
-// save 14 % of a large call); dx of fp32 gradients takes six products of terms: the three left out are at most
-// 2^-24 of the factors' magnitudes together, to either side (of terms that are cut, not rounded, 2^-21 and always to one).
+// An fp32 value is cut into three bf16 terms, each what is left rounded to nearest, which hold it exactly: so dw takes three
+// products of fp32 gradients and one of bf16 ones, and is exact up to the fp32 sums.  dx of bf16 gradients takes three products
+// with W's terms and is as exact (two terms that are cut moved single bf16 results, 2.1e-4 of dx's 2-norm from the fp32 products'
+// at hdim 4096, and saved a fifth of a large call); dx of fp32 gradients takes six products of terms: the three left out are at
+// most 2^-24 of the factors' magnitudes together, to either side (of terms that are cut, 2^-21 and always to one).
 #include "gns_learn.hpp"
 
 namespace gns {
@@ -242,7 +242,7 @@ struct Tile {
 // What a wave needs of exponents and masks is one read, lane by lane, and handed round.  Columns are placed such that
 // adjacent threads write adjacent rows of LDS.  Splits of the rows fill the chip where dw has few tiles.
 // 85,000 rows, 256 x 256, fp32: 48 us (87 MB of gradients, 22 of checkpoints, 33 of the splits' sums: 3.0 TB/s); 16,384 rows,
-// 4096 x 4096, bf16: 580 to 660 us (0.83 to 0.95 PFLOP/s), bound by the issue of matrix and vector instructions together: a value
+// 4096 x 4096, bf16: 590 to 720 us (0.76 to 0.93 PFLOP/s, by the clock that dx leaves it), bound by the issue of matrix and vector instructions together: a value
 // of X takes three of the latter on its way to LDS.
 struct WeightsArgs {
     BackwardArgs a;
@@ -639,14 +639,14 @@ template <> struct InputTile<float, 256> { typedef Tile<64, 64, 32, 32, 3, 3> Ty
 template <> struct InputTile<Bf16, 512> { typedef Tile<256, 128, 64, 64, 1, 3> Type; };
 template <> struct InputTile<Bf16, 256> { typedef Tile<128, 64, 64, 32, 1, 3> Type; };
 
-// 85,000 rows, 256 x 256, fp32: 78 us (six products of terms; 0.86 PFLOP/s of them); 16,384 rows, 4096 x 4096, bf16, masked, and dw:
-// 2070 us (three products here, one there).
+// 85,000 rows, 256 x 256, fp32: 83 us (six products of terms; 0.81 PFLOP/s of them); 16,384 rows, 4096 x 4096, bf16: 1415 to 1480 us
+// (three products; 1.1 to 1.17 PFLOP/s, the matrix cores busy in 70 % of the cycles at the 1.5 GHz that the power leaves).
 // A thread reads eight columns of a row of dz (of two rows of bf16), and as many of W's planes.  kWhole: hdim is a multiple of
 // eight.  Chunks past the last are read as the last: W's planes are zero there.  Else a row's last chunk is its last eight
 // columns, for dz as for W, and those that the chunk before has are left out of dz.  hdim is eight at least.
 // A block goes through tiles, `stride` apart, or has a split of one tile's hdim.
 // kPlain: W is read as it is and cut here, by every block that needs it, which where there is no more than a block or two per
-// CU costs less than a launch and a trip through memory in front (the planes of 4096 x 4096 take 25 us).
+// CU costs less than a launch and a trip through memory in front (the planes of 4096 x 4096 take 31 us).
 template <typename T, int kThreads, bool kMask, bool kWhole, bool kPlain>
 struct InputSource {
     typedef typename InputTile<T, kThreads>::Type Tiles;
@@ -854,7 +854,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_backward_input(InputArgs g)
 }
 
 // Both products of a small call in one launch, since neither waits for the other: the grid's first blocks are dw's.  fp32, 64 rows
-// of 256 x 256: 9 us, one after the other 17; 1772 rows of 400 x 18 bf16 15.6 and 24; 300 of 1000 x 1000 21 and 44.
+// of 256 x 256: 10 us, one after the other 17; 1772 rows of 400 x 18 bf16 16 and 24; 300 of 1000 x 1000 23 and 44.
 template <typename T, bool kMask, bool kWhole, bool kPairs>
 __global__ void __launch_bounds__(256, 2) k_backward_both(WeightsArgs g, InputArgs h, int32_t weights_blocks)
 {
@@ -867,7 +867,7 @@ __global__ void __launch_bounds__(256, 2) k_backward_both(WeightsArgs g, InputAr
 
 // k_backward_few: dx of up to sixteen rows, where W's bytes are all there is to do.  A block has 16 columns of dx (rows of W) and
 // all rows; its eight waves an eighth of hdim each, 16 x 16 x 32 products; their sums meet in LDS.  W is cut into terms on the
-// way, as dz is.  One row, 4096 x 4096, fp32, dw too: 44 us, 56 in tiles with hdim split; 17 rows would take 66 and take 54 in tiles.
+// way, as dz is.  One row, 4096 x 4096, fp32, dw too: 40 us, 56 in tiles with hdim split; 17 rows would take 66 and take 52 in tiles.
 constexpr int kFewRows = 16, kFewBlock = 512, kFewWaves = kFewBlock / kWave, kFewColumns = 16;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
@@ -1040,8 +1040,8 @@ static WeightsPlan plan_weights_of(const gns_ctx* c, int32_t f1, int32_t f2, int
     return p;
 }
 
-// Wide blocks where layers fill them and they fill half the chip at least (dx too, 16,384 rows of 2048 x 2048 bf16: 500 us, 571 with
-// narrow ones; 85,000 of 256 x 256 fp32: 138 and 144; 12,600 of 512 x 256: no difference)
+// Wide blocks where layers fill them and they fill half the chip at least (dx too, 16,384 rows of 2048 x 2048 bf16: 540 us, 604 with
+// narrow ones; 85,000 of 256 x 256 fp32: 139 and 153; 12,600 of 512 x 256: no difference)
 static bool may_be_wide(int32_t f1, int32_t f2, int32_t hdim, bool fp32) { return (f1 + 31) / 32 + (f2 + 31) / 32 > 4 && hdim > (fp32 ? 64 : 128); }
 
 static WeightsPlan plan_weights(const gns_ctx* c, int32_t f1, int32_t f2, int32_t hdim, int64_t rows, bool fp32, bool wide)
@@ -1156,9 +1156,9 @@ struct InputPlan {
     int32_t splits;
 };
 // Blocks of 512 threads where they fill half the chip and layers are not too narrow for them (fp32, dw too, 2400 rows of 1000 x 1000:
-// 78 us, 99 with 256 threads; 600 rows of 4096 x 4096: 237 and 338; with less than half 1400 rows: no difference, bf16 3000: 81
-// and 73).  Else of 256, and W is read as it is by no more of them than CUs, or than run at once where dw goes with them (fp32, 6000
-// rows of 256 x 256: 24 us, 36 with W cut in a launch between).
+// 80 us, 99 with 256 threads; 600 rows of 4096 x 4096: 245 and 338; with less than half 1400 rows of 1000 x 1000: 71 and 66, bf16
+// 3000: 79 and 73).  Else of 256, and W is read as it is by no more of them than CUs, or than run at once where dw goes with them
+// (fp32, 6000 rows of 256 x 256: 25 us, 36 with W cut in a launch between).
 template <typename T>
 static InputPlan plan_input(const gns_ctx* c, const BackwardArgs& a, bool both)
 {
@@ -1172,8 +1172,8 @@ static InputPlan plan_input(const gns_ctx* c, const BackwardArgs& a, bool both)
 }
 
 // Splits where dw and dx go together: steps a block, four for dw and two turns for dx at least, such that all blocks run at once.
-// fp32, 1104 rows of 128 x 2048: 24 us, with dw and dx each split for a chip of its own 28; 400 of 200 x 700: 16 and 22; bf16, 189 of
-// 2141 x 1102: 22 and 30.
+// fp32, 1104 rows of 128 x 2048: 24 us, with dw and dx each split for a chip of its own 28; 400 of 200 x 700: 17 and 22; bf16, 189 of
+// 2141 x 1102: 21 and 30.
 template <typename T>
 static int32_t both_least() { return 2 * (sizeof(T) == 4 ? 4 : 2); }
 template <typename T>

@@ -117,8 +117,8 @@ __global__ void __launch_bounds__(kBlock) k_quantize_rows(QuantizeArgs a)
     }
 }
 
-// Longer rows: a block per row, P pieces a thread.  8192 rows of 8192 bf16: 70 us (2.9 TB/s, behind a product that leaves nothing in
-// the caches); read twice by 1024 threads instead 100.
+// Longer rows: a block per row, P pieces a thread.  8192 rows of 8192 bf16: 62 to 71 us (2.8 to 3.2 TB/s; a copy of as many bytes 39):
+// each row's values are held as fp32, twice their bytes, across a barrier.  Read twice by 1024 threads instead 100.
 template <typename T, int P>
 __global__ void __launch_bounds__(kBlock) k_quantize_block(QuantizeArgs a)
 {
@@ -188,7 +188,7 @@ constexpr int kStepBytes = 64;                // k of a stage
 // multiplied, the first of the next one while its last are.  Chunk c of 16 bytes of row r lies at c ^ row_turn(r) of the
 // row, so that reads of the same chunk of eight or sixteen rows spread over all banks.  The weights are the products' left factor,
 // so that a lane holds four consecutive outputs of a row.
-// 8192 x 8192 x 8192, bf16 out: 490 to 580 us, 1.9 to 2.2 POP/s (a large library product of integers: 2.15), bound by the matrix
+// 8192 x 8192 x 8192, bf16 out: 490 to 610 us, 1.8 to 2.2 POP/s (a large library product of integers: 2.15), bound by the matrix
 // cores' cycles at the clock that the power leaves; with outputs stored value by value 40 us more.
 // Blocks of 128 x 128 are three a CU, for which the compiler has to be told (two: 79,214 rows of 32 x 4096 bf16 164 -> 203 us).
 template <typename T, int BM, int BN, int WM, int WN>
@@ -450,10 +450,12 @@ __global__ void __launch_bounds__(kFewBlock) k_int8_few(DenseInt8Args a, Quantiz
 }
 
 // k_int8_rows: many rows against weights that fit LDS: rows come in, are quantised and multiplied, and leave, without a
-// trip through memory in 8 bits (85,000 rows, 256 x 256, fp32: 34 us, 5.1 TB/s in and out; in two kernels 17 and 44).
+// trip through memory in 8 bits (85,000 rows, 256 x 256, fp32: 34 us, 5.1 TB/s in and out, with rows from the infinity cache, a call
+// of 49 without, where a copy takes 34; in two kernels 17 and 44).
 // A block per CU holds all weights; its waves walk tiles of 16 rows: a row is read by L lanes, P pieces each, quantised, turned
 // through a piece of LDS of the wave's own and multiplied, 16 x 16 x 64 bytes, with the weights as the left factor, so that a
-// lane gets four consecutive outputs of a row.  Bound by the rows' bytes, in and out.
+// lane gets four consecutive outputs of a row.  Bound by the rows' bytes, in and out; 85,000 rows are 1.3 tiles a wave, so
+// reading, multiplying and writing overlap little.
 constexpr int64_t rows_lds(int64_t stride, int32_t n, int waves)
 {
     return (few_stride(stride) * ((n + 15) / 16 * 16 + waves * 16)) + (int64_t) (n + 15) / 16 * 16 * 8;

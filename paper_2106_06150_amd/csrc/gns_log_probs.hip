@@ -291,7 +291,7 @@ struct LongArgs {
     Key* best;                    // [rows x parts x top]
 };
 
-// 4096 rows of 100,003 classes, bf16, twenty best: 175 us (4.7 TB/s); one row of 131,072, fp32: 12 us and 7 for the join.
+// 4096 rows of 100,003 classes, bf16, twenty best: 177 us (4.6 TB/s); one row of 131,072, fp32: 12 us and 7 for the join.
 // Rows of any length: a wave per row, or per part of a row where there are few.  Pieces of 16 bytes are read at 16-byte
 // marks whatever the row's own alignment; the few values in front of the first mark and behind the last are read singly.
 template <typename T>
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(kBlock) k_log_probs_backward(LogProbsBackwardA
 }
 
 // Long rows whose logits and gradients lie alike against the 16-byte marks: pieces of 16 bytes at the marks, single values
-// in front of and behind them.  A wave has `tiles` tiles of a row.  4096 rows of 100,003 classes, bf16: 316 us, 5.2 TB/s, the rate of
+// in front of and behind them.  A wave has `tiles` tiles of a row.  4096 rows of 100,003 classes, bf16: 317 us, 5.2 TB/s, the rate of
 // a copy.
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kBlock) k_log_probs_backward_long(LogProbsBackwardArgs a, int32_t parts, int32_t tiles)
