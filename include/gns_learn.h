@@ -91,7 +91,7 @@ gns_status gns_checkpoint_load(gns_ctx* ctx, const int8_t* q_dev, const uint8_t*
  *   db[n]    = sum_r dz[r, n]               fp32[hdim], or NULL; comes with dw only
  *   dx[r, k] = sum_n dz[r, n] * w[k, n]     rows of f1 + f2 columns, in d_out's type, or NULL; w fp32[(f1 + f2) x hdim]
  * hdim = d_out->width.  dw may be NULL (then neither checkpoint is read).  Products have fp32's precision (fp32 values are
- * split into three bf16 terms), sums are fp32.  Infinities and NaN go where these formulas take them: an infinity stays one
+ * split into three bf16 terms), sums are fp32; subnormal bf16 values of d_out may count as zero in them.  Infinities and NaN go where these formulas take them: an infinity stays one
  * unless it meets a zero or its opposite (each such result is summed by a thread alone; a call with very many takes
  * long).  With no rows dw and db are zero.  workspace: gns_sage_dense_backward_workspace_bytes(...) bytes, 256-byte
  * aligned. */
