@@ -91,10 +91,10 @@ gns_status gns_checkpoint_load(gns_ctx* ctx, const int8_t* q_dev, const uint8_t*
  *   db[n]    = sum_r dz[r, n]               fp32[hdim], or NULL; comes with dw only
  *   dx[r, k] = sum_n dz[r, n] * w[k, n]     rows of f1 + f2 columns, in d_out's type, or NULL; w fp32[(f1 + f2) x hdim]
  * hdim = d_out->width.  dw may be NULL (then neither checkpoint is read).  Products have fp32's precision (fp32 values are
- * split into three bf16 terms), sums are fp32; subnormal bf16 values of d_out may count as zero in them.  Infinities and NaN go where these formulas take them: an infinity stays one
- * unless it meets a zero or its opposite (each such result is summed by a thread alone; a call with very many takes
- * long).  With no rows dw and db are zero.  workspace: gns_sage_dense_backward_workspace_bytes(...) bytes, 256-byte
- * aligned. */
+ * split into three bf16 terms), sums are fp32; subnormal bf16 values of d_out may count as zero in them.  Infinities and
+ * NaN go where these formulas take them: an infinity stays one unless it meets a zero or its opposite (each such result
+ * is summed by a thread alone; a call with very many takes long).  With no rows dw and db are zero.  workspace:
+ * gns_sage_dense_backward_workspace_bytes(...) bytes, 256-byte aligned. */
 size_t gns_sage_dense_backward_workspace_bytes(const gns_ctx* ctx, int32_t f1, int32_t f2, int32_t hdim, int32_t num_rows);
 gns_status gns_sage_dense_backward(gns_ctx* ctx, const gns_rows* d_out, const uint32_t* positive_dev,
                                    const int8_t* q1_dev, const uint8_t* exponents1_dev, int32_t f1,
