@@ -1,0 +1,143 @@
+/*
+ * gns_layers.h -- C ABI of what deeper classifiers need next to the update step: what stands between two layers, what
+ * moves their weights, and the update step in 8-bit floats.
+ *
+ *   gns_group_norm, gns_group_norm_backward                    rows normalised over segments of rows and groups of columns,
+ *                                                              scaled, shifted, put through an activation; the gradients
+ *   gns_orthogonal_update                                      momentum, its Newton-Schulz orthogonalisation, the weights' step
+ *   gns_quantize_fp8, gns_dense_fp8, gns_sage_dense_fp8        the update step with rows and weights in 8-bit floats
+ *
+ * The general rules of gns_learn.h hold: gns_rows of either type with any width, stride and alignment, num_rows a count or
+ * GNS_DEVICE_COUNTS(i), buffers and workspaces of the caller, enqueue only, one workspace for calls of so many rows and
+ * fewer, the same bits from a repeated call.  Workspaces are 256-byte aligned and serve one call at a time.
+ */
+#ifndef GNS_LAYERS_H_
+#define GNS_LAYERS_H_
+
+#include "gns_learn.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- group norm with an activation ----------------------------------------------------------------------------------
+ * Rows are the positions of a channels-last tensor, or the nodes of mini-batches: segment s has the rows
+ *   segments_dev[s] .. segments_dev[s + 1] - 1   (num_segments + 1 ascending offsets, 0 <= s < num_segments), or
+ *   s * segment_rows .. (s + 1) * segment_rows - 1   with segments_dev NULL (the last may be shorter; num_segments is then
+ *                                                    not read; with segment_rows 1 each row is normalised by itself)
+ * and group j of a row the columns j * w .. (j + 1) * w - 1, w = width / groups (which must be whole).  For the n values of a
+ * segment and group:
+ *   mean = sum x / n,  rstd = 1 / sqrt(sum (x - mean)^2 / n + eps)
+ *   y[r, c] = (x[r, c] - mean) * rstd * gamma[c] + beta[c],  out[r, c] = activation(y[r, c])
+ *   stats[2 (s * groups + j)], stats[2 (s * groups + j) + 1] = mean, rstd;   0, 0 for a segment without rows
+ * Rows of no segment (in front of the first, behind the last) are not read, and their outputs left as they were.  Offsets that do not ascend or lie
+ * outside the rows give unspecified values in the rows' outputs and nothing else.  All arithmetic is fp32.  A group with an
+ * infinity or NaN, or whose squares leave fp32's range, has NaN in stats and outputs. */
+#define GNS_ACT_NONE 0
+#define GNS_ACT_RELU 1 /* max(0, y); a NaN stays one      */
+#define GNS_ACT_SILU 2 /* y / (1 + exp(-y))               */
+#define GNS_ACT_GELU 3 /* y (1 + erf(y / sqrt 2)) / 2     */
+
+typedef struct {
+    const int32_t* segments_dev; /* num_segments + 1 offsets, or NULL */
+    const float* gamma_dev;      /* width scales, or NULL: ones       */
+    const float* beta_dev;       /* width shifts, or NULL: zeros      */
+    int32_t num_segments;        /* 0 .. GNS_MAX_SEGMENTS             */
+    int32_t segment_rows;        /* >= 1 with segments_dev NULL       */
+    int32_t groups;
+    int32_t activation;
+    float eps;                   /* > 0, finite                       */
+} gns_norm;
+#define GNS_MAX_SEGMENTS (1 << 24)
+
+/* stats_dev fp32[num_segments x groups x 2] (segments by rows: as many as num_rows fill), 8-byte aligned, or NULL.  out has
+ * the width and type of x and may be x's own rows (same data and stride).  workspace may be NULL if
+ * gns_group_norm_workspace_bytes(...) is 0. */
+size_t gns_group_norm_workspace_bytes(const gns_ctx* ctx, int32_t width, const gns_norm* norm, int32_t num_rows);
+gns_status gns_group_norm(gns_ctx* ctx, const gns_rows* x, const gns_norm* norm, const gns_rows* out, float* stats_dev,
+                          int32_t num_rows, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The gradients, from x and the stats that gns_group_norm wrote: with h = (x - mean) * rstd, dy = d_out * activation'(y)
+ * (relu'(0) = 0),
+ *   dbeta[c] = sum_r dy[r, c],  dgamma[c] = sum_r dy[r, c] * h[r, c]     fp32[width] each, over the rows of all segments
+ *   dx[r, c] = rstd * (g - m1 - h * m2),  g = dy * gamma[c],  m1 = sum g / n,  m2 = sum g * h / n over segment and group
+ * d_out, x and dx have one width and type; dx may be NULL, d_out's own rows or x's (same data and stride).  dgamma_dev and
+ * dbeta_dev may be NULL, each for itself.  Without rows both are zero. */
+size_t gns_group_norm_backward_workspace_bytes(const gns_ctx* ctx, int32_t width, const gns_norm* norm, int32_t num_rows);
+gns_status gns_group_norm_backward(gns_ctx* ctx, const gns_rows* d_out, const gns_rows* x, const gns_norm* norm,
+                                   const float* stats_dev, const gns_rows* dx, float* dgamma_dev, float* dbeta_dev,
+                                   int32_t num_rows, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- orthogonalised update of weights ----------------------------------------------------------------------------------
+ * For the gradient g of a matrix of num_rows x width weights (no device counts here):
+ *   m' = mu * m + g                       momentum (NULL: m' = g), written to momentum_out
+ *   u  = g + mu * m' if nesterov != 0, m' otherwise
+ *   X  = u / (|u|_F + eps), turned so that its rows are the shorter side;  then, `steps` times with the coefficients a, b, c of
+ *        that step,  A = X X^T,  X <- a X + (b A + c A A) X,  which moves X's singular values s to a s + b s^3 + c s^5
+ *   out = keep * w + rate * X             w NULL: out = rate * X (turned back)
+ * (3.4445, -4.775, 2.0315) five times brings singular values between about 0.01 and 1 near 1, (1.875, -1.25, 0.375) any of up
+ * to 1 slowly and exactly.  Products are of fp32's precision: X and the matrices between are kept as two fp16 terms
+ * (22 bits down to 2^-26, an absolute 2^-37 below that), sums are fp32; the norm is summed in 64 bits.  Coefficients that
+ * take an element of X or b A + c A A to 16 or beyond give infinities or NaN.  A gradient of zeros gives X = 0, one with an
+ * infinity or NaN gives NaN throughout.  num_rows and width are up to GNS_ORTHOGONAL_MAX; all matrices have one shape, each
+ * its own type and stride; momentum_out may be momentum's own rows, out w's or the gradient's (same data, stride and type).
+ * m' is rounded to momentum_out's type once, u is made of it before that. */
+#define GNS_ORTHOGONAL_MAX 32768
+#define GNS_MAX_STEPS 16
+typedef struct {
+    float mu;
+    int32_t nesterov;
+    float eps; /* >= 0 */
+    float keep, rate;
+    int32_t steps; /* 0 .. GNS_MAX_STEPS */
+    float coefficients[GNS_MAX_STEPS][3];
+} gns_orthogonal;
+
+size_t gns_orthogonal_update_workspace_bytes(const gns_ctx* ctx, int32_t width, int32_t num_rows);
+gns_status gns_orthogonal_update(gns_ctx* ctx, const gns_rows* grad, const gns_rows* momentum, const gns_orthogonal* how,
+                                 const gns_rows* w, const gns_rows* momentum_out, const gns_rows* out, int32_t num_rows,
+                                 void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- the update step in 8-bit floats ------------------------------------------------------------------------------------
+ * Rows in 8-bit floats: 4 exponent and 3 fraction bits, largest value 448, no infinities (OCP E4M3), a power of two for each
+ * block of 128 columns of a row:
+ *   q_dev          uint8[num_rows x GNS_FP8_STRIDE(k)], 16-byte aligned; columns k and beyond are zero
+ *   exponents_dev  uint8[num_rows x GNS_FP8_EXPONENTS(k)], 4-byte aligned: e + 127 of each block, bytes behind the last block zero.
+ *                  0: all values are zero (a block of magnitudes below 2^-100 is taken as zeros); 255: the block held an infinity
+ *                  or NaN, and all its values are NaN
+ * A value is q * 2^e, e the smallest with which the block's largest magnitude is at most 464 * 2^e (which rounds to 448), rounded
+ * to nearest, ties to even; down to 2^(e - 9), so a value is at most 2^-4 of itself or 2^(e - 10) off. */
+#define GNS_FP8_BLOCK 128
+#define GNS_FP8_STRIDE(k) (((int64_t) (k) + 127) / 128 * 128)
+#define GNS_FP8_EXPONENTS(k) (((int64_t) (k) + 511) / 512 * 4)
+#define GNS_FP8_MAX_K (1 << 20)
+
+/* Quantises rows [x1 | x2] (x2 may be NULL; both of one type) of together k <= GNS_FP8_MAX_K columns.  Also the way to
+ * quantise weights, given as hdim rows of k. */
+gns_status gns_quantize_fp8(gns_ctx* ctx, const gns_rows* x1, const gns_rows* x2, uint8_t* q_dev, uint8_t* exponents_dev,
+                            int32_t num_rows, void* hip_stream);
+
+/* out[r, n] = g( sum_c x[r, c] * w[n, c] + bias[n] ), x and w the values of rows in 8-bit floats, w of out->width rows; g as in
+ * gns_dense_int8; bias may be NULL; out of either type.  fp32 outputs are sums in fp32 of exact products; bf16 outputs may be
+ * sums that lose, of each 128 columns' products, what lies below 2^-13 of the largest.  Results below 2^-120 may be zero.
+ * Columns k and beyond of q and w must be finite values, of one of them zeros, and e between -109 and 120, as
+ * gns_quantize_fp8 leaves both. */
+gns_status gns_dense_fp8(gns_ctx* ctx, const uint8_t* q_dev, const uint8_t* exponents_dev, int32_t k, const uint8_t* wq_dev,
+                         const uint8_t* w_exponents_dev, const float* bias_dev, int32_t relu, const gns_rows* out,
+                         int32_t num_rows, void* hip_stream);
+
+/* Both in one call: the update step of gns_sage_dense with rows quantised as they come (x2 may be NULL). */
+size_t gns_sage_dense_fp8_workspace_bytes(const gns_ctx* ctx, int32_t k, int32_t num_rows);
+gns_status gns_sage_dense_fp8(gns_ctx* ctx, const gns_rows* x1, const gns_rows* x2, const uint8_t* wq_dev,
+                              const uint8_t* w_exponents_dev, const float* bias_dev, int32_t relu, const gns_rows* out,
+                              int32_t num_rows, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Stages of gns_profile_begin (see gns.h) for the calls above. */
+#define GNS_STAGE_NORM 26       /* gns_group_norm, gns_group_norm_backward             */
+#define GNS_STAGE_ORTHOGONAL 27 /* gns_orthogonal_update                               */
+#define GNS_STAGE_FP8 28        /* gns_quantize_fp8, gns_dense_fp8, gns_sage_dense_fp8 */
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* GNS_LAYERS_H_ */

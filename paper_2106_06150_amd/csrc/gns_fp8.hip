@@ -1,0 +1,705 @@
+// The update step in 8-bit floats: rows quantised with a power of two per block of 128 columns.
+//
+// Two ways to multiply.  The matrix cores' product of 8-bit floats takes an exponent byte per row and 32 columns and runs at twice bf16's
+// rate, but of the products it sums it drops what lies below 2^-13 of the largest (one of 2^16 beside seven of 4 gives 2^16; with seven of
+// 8 nothing is lost; sums so far keep fp32's bits).  Against 64 bits that is 1.5e-5 of the results' 2-norm, lost in bf16's rounding of
+// 1.7e-3, so bf16 outputs take it.  fp32 outputs (and a few rows, whose time is the weights' bytes) take products of bf16, which holds
+// every value exactly, with sums of fp32's precision.
+#include "gns_layers.hpp"
+#include <type_traits>
+
+namespace gns {
+
+typedef int int4v __attribute__((ext_vector_type(4)));
+typedef int int8v __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
+typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
+
+// Values are turned into bf16 as q * 2^(e - 2): e is between -109 and 120 and q's magnitudes between 2^-9 and 448, so they lie between
+// 2^-120 and 2^127, where bf16 is exact.  Sums of products of such values are multiplied by 16.
+constexpr float kSumUp = 16.f;
+__device__ __forceinline__ float power_of(uint32_t byte)
+{
+    // the power's bits; the least is 2^-126, which only zeros have
+    return byte == 255u ? quiet_nan() : __uint_as_float((byte > 2u ? byte - 2u : 1u) << 23);
+}
+__device__ __forceinline__ bf8v values_of(uint32_t low, uint32_t high, float power)
+{
+    const bf2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, power, true);
+    const bf2v c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, power, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, power, true);
+    return bf8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ __forceinline__ float output_of(float sum, float bias, int32_t relu)
+{
+    const float y = sum + bias;
+    return relu ? relu_of(y) : y;
+}
+
+// Pieces of V consecutive columns of a row [x1 | x2]: 16 bytes of either type.  Lanes of a block of 128 columns.
+template <typename T> constexpr int kPiece = 16 / (int) sizeof(T);
+template <typename T> constexpr int kBlockLanes = GNS_FP8_BLOCK / kPiece<T>;
+
+// A piece that lies in one input's row is one read, whatever the row's alignment; where an input ends inside, its values are read
+// singly.  Columns past the last are zero.
+template <typename T>
+__device__ __forceinline__ void load_piece(const QuantizeFp8Args& a, int64_t r, int32_t c, float (&x)[kPiece<T>])
+{
+    constexpr int V = kPiece<T>;
+    const int32_t f1 = a.x1.width, k = f1 + a.x2.width;
+    if (c + V <= f1 || (c >= f1 && c + V <= k)) {
+        uint32_t words[4];
+        load_words(c < f1 ? reinterpret_cast<const T*>(a.x1.data) + r * a.x1.stride + c
+                          : reinterpret_cast<const T*>(a.x2.data) + r * a.x2.stride + (c - f1), words);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = value_of_words<T>(words, i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            x[i] = c + i < f1 ? load_at<T>(a.x1, r, c + i) : c + i < k ? load_at<T>(a.x2, r, c + i - f1) : 0.f;
+    }
+}
+
+template <int V>
+__device__ __forceinline__ uint32_t largest_of(const float (&x)[V], uint32_t most)
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) most = max(most, magnitude_bits(x[i]));
+    return most;
+}
+
+// Largest of the L lanes of a block (16 or 32)
+template <int L>
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
+{
+    v = max(v, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) v, 0xB1, 0xf, 0xf, true));       // lanes 1 0 3 2
+    v = max(v, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) v, 0x4E, 0xf, 0xf, true));       // lanes 2 3 0 1
+    v = max(v, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) v, 0x141, 0xf, 0xf, true));      // mirrored in 8
+    v = max(v, (uint32_t) __builtin_amdgcn_update_dpp(0, (int) v, 0x140, 0xf, 0xf, true));      // mirrored in 16
+    if (L > 16) v = max(v, (uint32_t) __shfl_xor((int) v, 16));
+    return v;
+}
+
+// A block's exponent byte and 2^-e, from the bits of its largest magnitude m 2^x, 1 <= m < 2: e = x - 8, one more where m > 464 / 256.
+struct BlockScale {
+    uint32_t byte;
+    float inverse;                // 0: no values; NaN: spoilt
+};
+__device__ __forceinline__ BlockScale block_scale(uint32_t most)
+{
+    if (most >= kInfBits) return BlockScale{255u, quiet_nan()};
+    if (most < 0x0D800000u) return BlockScale{0u, 0.f};       // 2^-100
+    const uint32_t byte = (most >> 23) - 8 + ((most & 0x7FFFFFu) > 0x680000u ? 1u : 0u);
+    return BlockScale{byte, __uint_as_float((254u - byte) << 23)};
+}
+
+// Four values in 8-bit floats, rounded to nearest, ties to even.  Scaled magnitudes are up to 464, and what is above 448 rounds to it.
+__device__ __forceinline__ uint32_t pack4(const float* x, float inverse)
+{
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_fmed3f(x[i] * inverse, -448.f, 448.f);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (uint32_t) __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+}
+
+// The piece at column c of a block: zeros where the block has none, NaN where it is spoilt (but zeros behind the last column).
+template <typename T>
+__device__ __forceinline__ void store_piece(uint8_t* to, const float (&x)[kPiece<T>], float inverse, int32_t c, int32_t k)
+{
+    constexpr int V = kPiece<T>;
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+        w[i] = pack4(x + 4 * i, inverse);
+        if (!(inverse > 0.f)) {
+            w[i] = 0;
+            if (inverse != 0.f)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) w[i] |= c + 4 * i + n < k ? 0x7Fu << (8 * n) : 0u;
+        }
+    }
+    if (V == 4) *reinterpret_cast<uint32_t*>(to) = w[0];
+    else        *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[V / 4 - 1]);
+}
+
+// A team of lanes per block of 128 columns, one piece each; the exponents' padding is written by teams of its own.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) k_quantize_fp8(QuantizeFp8Args a)
+{
+    constexpr int V = kPiece<T>, L = kBlockLanes<T>;
+    const int32_t rows = a.count.get(), k = a.x1.width + a.x2.width, blocks = (int32_t) a.exponent_stride, whole = (int32_t) (a.stride / GNS_FP8_BLOCK);
+    const int64_t units = (int64_t) rows * blocks, step = (int64_t) gridDim.x * (kBlock / L);
+    for (int64_t u0 = ((int64_t) blockIdx.x * kBlock + (threadIdx.x & ~(kWave - 1))) / L; u0 < units; u0 += step) {
+        const int lane = opaque_lane_id(), l = lane & (L - 1);
+        const int64_t unit = u0 + lane / L, u = unit < units ? unit : units - 1, r = u / blocks;
+        const int32_t block = (int32_t) (u - r * blocks), c = block * GNS_FP8_BLOCK + l * V;
+        float x[V];
+        load_piece<T>(a, r, c, x);
+        const BlockScale s = block_scale(largest_of_lanes<L>(largest_of(x, 0u)));
+        if (unit >= units) continue;
+        if (block < whole) store_piece<T>(a.q + r * a.stride + c, x, s.inverse, c, k);
+        if (l == 0) a.exponents[u] = (uint8_t) s.byte;
+    }
+}
+
+constexpr int kStepBytes = 64;                // k of a stage
+
+// k_fp8_tiles: BM x BN outputs a block, WM x WN a wave, products of 32 x 32 x 64.  A stage of 64 k of the rows and weights is read two
+// stages before it is written to LDS, and written two before it is multiplied; one barrier a stage.  Chunk c of 16 bytes of
+// row r lies at c ^ row_turn(r) of the row, so that reads of the same chunk of eight or sixteen rows spread over all banks.  A lane's 32
+// bytes of a product are chunks l / 32 and 2 + l / 32: any order does that both factors share, as they have one exponent.  The weights are the
+// products' left factor, so that a lane holds four consecutive outputs of a row.  Exponents are read as words of four blocks, 512 k ahead.
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, 2) k_fp8_tiles(DenseFp8Args a, int32_t m_tiles, int32_t n_tiles)
+{
+    constexpr int kWaves = (BM / WM) * (BN / WN), kLoads = (BM + BN) / 16 / kWaves;     // of 16 rows, by a wave and stage
+    constexpr int MI = WM / 32, NI = WN / 32, kStage = (BM + BN) * 4;
+    constexpr bool kPrecise = sizeof(T) == 4;
+    static_assert((BM + BN) / 16 % kWaves == 0 && BM / 16 % kLoads == 0, "a wave loads whole pieces of one side");
+    __shared__ int4v s_stage[3 * kStage];
+    __shared__ float s_bias[BN];
+    const int32_t rows = a.count.get(), n = a.out.width;
+    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
+    const int32_t block = (int32_t) (blockIdx.y * gridDim.x + blockIdx.x);
+    if (block >= m_tiles * n_tiles) return;
+    int32_t tm, tn;
+    tile_of(xcd_run(block, m_tiles * n_tiles), m_tiles, n_tiles, &tm, &tn);
+    const int64_t m0 = (int64_t) tm * BM;
+    const int32_t n0 = tn * BN;
+    if (m0 >= rows) return;
+    const int32_t steps = (int32_t) (a.stride / kStepBytes);  // even
+    for (int i = (int) threadIdx.x; i < BN; i += kWaves * kWave) s_bias[i] = a.bias ? a.bias[n0 + i < n ? n0 + i : n - 1] : 0.f;
+    // this wave's pieces: 16 rows each, of the rows' side or the weights'; those past the end repeat the last
+    const bool weights = wave * kLoads * 16 >= BM;
+    const int32_t first = wave * kLoads * 16 - (weights ? BM : 0);
+    const int64_t last = weights ? n - 1 - n0 : rows - 1 - m0;
+    const uint8_t* base = weights ? a.wq + (int64_t) n0 * a.stride : a.q + m0 * a.stride;
+    const int32_t turned = (lane & 3) ^ row_turn(lane >> 2);
+    uint32_t from[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int32_t row = first + i * 16 + (lane >> 2), at = (int32_t) (row < last ? row : last);
+        from[i] = (uint32_t) at * (uint32_t) a.stride + (uint32_t) (lane & 3) * 16;
+    }
+    int4v* put_at = s_stage + (wave * kLoads * 16 + (lane >> 2)) * 4 + turned;
+    int4v read[2][kLoads];
+    const uint8_t* next;                                      // of the step that is read
+    auto seek = [&](int32_t step) { next = base + (int64_t) (step < steps ? step : steps - 1) * kStepBytes; };   // past the last: the last again
+    auto fetch = [&](int set, int i) { read[set][i] = *reinterpret_cast<const int4v*>(next + from[i]); };
+    auto put = [&](int set, int stage, int i) { put_at[stage * kStage + i * 64] = read[set][i]; };
+    auto fetch_all = [&](int set, int32_t step) {
+        seek(step);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) fetch(set, i);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto put_all = [&](int set, int stage) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) put(set, stage, i);
+    };
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+    const int l32 = lane & 31, kh = lane >> 5, bank = row_turn(l32);
+    // exponents of this lane's rows and channels, four blocks a word
+    const uint8_t* exponents[MI + NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int64_t r = m0 + wm + i * 32 + l32;
+        exponents[i] = a.exponents + (r < rows ? r : rows - 1) * a.exponent_stride;
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const int32_t c = n0 + wn + i * 32 + l32;
+        exponents[MI + i] = a.w_exponents + (int64_t) (c < n ? c : n - 1) * a.exponent_stride;
+    }
+    const int32_t words = (int32_t) (a.exponent_stride / 4);
+    int scale[2][MI + NI];
+    auto fetch_scales = [&](int set, int32_t word) {
+        const int32_t at = word < words ? word : words - 1;
+#pragma unroll
+        for (int i = 0; i < MI + NI; ++i) scale[set][i] = *reinterpret_cast<const int*>(exponents[i] + 4 * (int64_t) at);
+    };
+    float16v acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    int8v f[2][MI + NI];                                      // fragments of the rows, then of the weights, of this stage and the next
+    const int4v* x_at = s_stage + (wm + l32) * 4;
+    const int4v* w_at = s_stage + (BM + wn + l32) * 4;
+    auto get = [&](int set, int stage, int i) {
+        const int4v* at = i < MI ? x_at + stage * kStage + i * 128 : w_at + stage * kStage + (i - MI) * 128;
+        const int4v low = at[kh ^ bank], high = at[(2 + kh) ^ bank];
+        f[set][i] = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    int s0 = 0, s1 = 1, s2 = 2;                               // stages of this step, the next and the one after
+    fetch_scales(0, 0);
+    fetch_all(0, 0);
+    fetch_all(1, 1);
+    put_all(0, 0);
+    fetch_all(0, 2);
+    put_all(1, 1);
+    fetch_all(1, 3);
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < MI + NI; ++i) get(0, 0, i);
+    // Stage `step` is multiplied; what was read for step + 2 goes to LDS, what is read now is for step + 4; the next stage's fragments are read.
+    auto turn = [&](auto at, int32_t step, int word_set) {
+        constexpr int kAt = decltype(at)::value, set = kAt & 1, kByte = kAt / 2;
+        constexpr int kProducts = MI * NI, kOthers = MI + NI + 2 * kLoads;
+        seek(step + 4);
+        auto others = [&](int m, int all) {                   // behind product m of so many
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int o = kOthers * m / all; o < kOthers * (m + 1) / all; ++o) {
+                if (o < MI + NI)               get(1 - set, s1, o);
+                else if (o < MI + NI + kLoads) put(set, s2, o - (MI + NI));
+                else                           fetch(set, o - (MI + NI) - kLoads);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if constexpr (kPrecise) {
+            float power[MI + NI];
+#pragma unroll
+            for (int i = 0; i < MI + NI; ++i) power[i] = power_of((uint32_t) scale[word_set][i] >> (8 * kByte) & 255u);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                bf8v v[MI + NI];
+#pragma unroll
+                for (int i = 0; i < MI + NI; ++i) v[i] = values_of((uint32_t) f[set][i][2 * h], (uint32_t) f[set][i][2 * h + 1], power[i]);
+#pragma unroll
+                for (int m = 0; m < kProducts; ++m) {
+                    acc[m / NI][m % NI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[MI + m % NI], v[m / NI], acc[m / NI][m % NI], 0, 0, 0);
+                    others(h * kProducts + m, 4 * kProducts);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int m = 0; m < kProducts; ++m) {
+                acc[m / NI][m % NI] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f[set][MI + m % NI], f[set][m / NI], acc[m / NI][m % NI], 0, 0,
+                                                                                     kByte, scale[word_set][MI + m % NI], kByte, scale[word_set][m / NI]);
+                others(m, kProducts);
+            }
+        }
+        const int t = s0;
+        s0 = s1; s1 = s2; s2 = t;
+        lds_barrier();
+    };
+    auto eight = [&](int32_t step, int set) {                 // the steps of a word of exponents; false: the last was among them
+        fetch_scales(1 - set, step / 8 + 1);
+        turn(std::integral_constant<int, 0>{}, step, set);
+        turn(std::integral_constant<int, 1>{}, step + 1, set);
+        if (step + 2 >= steps) return false;
+        turn(std::integral_constant<int, 2>{}, step + 2, set);
+        turn(std::integral_constant<int, 3>{}, step + 3, set);
+        if (step + 4 >= steps) return false;
+        turn(std::integral_constant<int, 4>{}, step + 4, set);
+        turn(std::integral_constant<int, 5>{}, step + 5, set);
+        if (step + 6 >= steps) return false;
+        turn(std::integral_constant<int, 6>{}, step + 6, set);
+        turn(std::integral_constant<int, 7>{}, step + 7, set);
+        return step + 8 < steps;
+    };
+    for (int32_t step = 0;; step += 16) {
+        if (!eight(step, 0)) break;
+        if (!eight(step + 8, 1)) break;
+    }
+    // Each strip of 32 rows goes through a piece of LDS of the wave's own, so that rows leave in pieces of 16 bytes.
+    // (from a lane id the compiler cannot see through: what it would work out of this in front of the loop costs registers)
+    constexpr int V = 16 / (int) sizeof(T), kLanes = WN / V, kPitch = WN * (int) sizeof(T) + 16;
+    static_assert(kWaves * 32 * kPitch <= 3 * kStage * 16, "the strips lie in the stages' place");
+    const int e_lane = opaque_lane_id(), e32 = e_lane & 31, four = 4 * (e_lane >> 5);
+    char* const strip = reinterpret_cast<char*>(s_stage) + wave * (32 * kPitch);
+    const int32_t c = n0 + wn + e_lane % kLanes * V;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {                     // elements 4 q .. 4 q + 3: four columns of row e32
+                const int at = j * 32 + 8 * q + four;
+                const float4 b = *reinterpret_cast<const float4*>(s_bias + wn + at);
+                struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
+                y.v[0] = from_float<T>(output_of(acc[i][j][4 * q] * (kPrecise ? kSumUp : 1.f), b.x, a.relu));
+                y.v[1] = from_float<T>(output_of(acc[i][j][4 * q + 1] * (kPrecise ? kSumUp : 1.f), b.y, a.relu));
+                y.v[2] = from_float<T>(output_of(acc[i][j][4 * q + 2] * (kPrecise ? kSumUp : 1.f), b.z, a.relu));
+                y.v[3] = from_float<T>(output_of(acc[i][j][4 * q + 3] * (kPrecise ? kSumUp : 1.f), b.w, a.relu));
+                *reinterpret_cast<Four*>(strip + e32 * kPitch + at * (int) sizeof(T)) = y;
+            }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int t = 0; t < 32 * kLanes / kWave; ++t) {
+            const int row = t * (kWave / kLanes) + e_lane / kLanes;
+            const Chunk y = *reinterpret_cast<const Chunk*>(strip + row * kPitch + e_lane % kLanes * 16);
+            const int64_t r = m0 + wm + i * 32 + row;
+            if (r >= rows) continue;
+            T* out = reinterpret_cast<T*>(a.out.data) + r * a.out.stride + c;
+            if (c + V <= n) {
+                __builtin_memcpy(out, &y, 16);                // whatever the row's alignment
+            } else {
+                struct Values { T v[V]; } values = __builtin_bit_cast(Values, y);
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (c + k < n) out[k] = values.v[k];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// k_fp8_few: for rows by the ten, where the weights' bytes are all there is to do.  A block has 16 output channels and all
+// rows (16 a tile, up to MT tiles), its eight waves an eighth of k each, products of bf16, 16 x 16 x 32; their sums meet in
+// LDS.  kFused: the block quantises the rows itself into LDS (every block does, which costs less than a launch
+// in front), while its first weights are on their way.
+constexpr int kFewBlock = 512, kFewWaves = kFewBlock / kWave, kFewColumns = 16;
+constexpr int kFewDepth = 4;                  // blocks of weights in flight
+constexpr size_t kFewLds = 64 * 1024;         // of quantised rows
+
+__host__ __device__ constexpr int64_t few_stride(int64_t stride) { return stride + 16; }        // of rows in LDS, off the banks' period
+__host__ __device__ constexpr int64_t few_lds(int64_t rows, int64_t stride) { return rows * (few_stride(stride) + stride / GNS_FP8_BLOCK) + 16; }
+
+template <typename T, typename X, bool kFused, int MT>
+__global__ void __launch_bounds__(kFewBlock) k_fp8_few(DenseFp8Args a, QuantizeFp8Args x)
+{
+    constexpr int V = kPiece<X>, L = kBlockLanes<X>;
+    extern __shared__ int4v s_rows[];                         // kFused: the rows in 8 bits, then their exponents
+    __shared__ float s_sum[kFewWaves][MT][4][kWave];
+    const int32_t rows = a.count.get(), n = a.out.width, steps = (int32_t) (a.stride / GNS_FP8_BLOCK);
+    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
+    const int l16 = lane & 15, kg = lane >> 4;
+    const int32_t n0 = (int32_t) blockIdx.x * kFewColumns, column = n0 + l16 < n ? n0 + l16 : n - 1;
+    const int32_t s0 = (int32_t) ((int64_t) steps * wave / kFewWaves), s1 = (int32_t) ((int64_t) steps * (wave + 1) / kFewWaves);
+    const uint8_t* w = a.wq + (int64_t) column * a.stride + kg * 16;
+    const uint8_t* w_exponents = a.w_exponents + (int64_t) column * a.exponent_stride;
+    int4v read[kFewDepth][2];
+    uint32_t w_byte[kFewDepth];
+    auto fetch = [&](int32_t from) {                          // steps past the last repeat it
+#pragma unroll
+        for (int d = 0; d < kFewDepth; ++d) {
+            const int32_t s = from + d < s1 ? from + d : s1 - 1;
+            read[d][0] = *reinterpret_cast<const int4v*>(w + (int64_t) s * GNS_FP8_BLOCK);
+            read[d][1] = *reinterpret_cast<const int4v*>(w + (int64_t) s * GNS_FP8_BLOCK + 64);
+            w_byte[d] = w_exponents[s];
+        }
+    };
+    if (s0 < s1) fetch(s0);
+    if (rows <= 0) return;
+    const int64_t pitch = few_stride(a.stride);
+    uint8_t* const s_q = reinterpret_cast<uint8_t*>(s_rows);
+    uint8_t* const s_exponents = s_q + rows * pitch;
+    if (kFused) {
+        const int32_t units = rows * steps;
+        for (int32_t u0 = wave * (kWave / L); u0 < units; u0 += kFewBlock / L) {
+            const int32_t unit = u0 + opaque_lane_id() / L, u = unit < units ? unit : units - 1, r = u / steps, block = u - r * steps;
+            const int32_t c = block * GNS_FP8_BLOCK + (opaque_lane_id() & (L - 1)) * V;
+            float v[V];
+            load_piece<X>(x, r, c, v);
+            const BlockScale s = block_scale(largest_of_lanes<L>(largest_of(v, 0u)));
+            if (unit >= units) continue;
+            store_piece<X>(s_q + r * pitch + c, v, s.inverse, c, a.k);
+            if ((lane & (L - 1)) == 0) s_exponents[u] = (uint8_t) s.byte;
+        }
+        __syncthreads();
+    }
+    const uint8_t* q[MT];
+    const uint8_t* exponents[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int32_t r = t * 16 + l16 < rows ? t * 16 + l16 : rows - 1;
+        q[t] = (kFused ? s_q + r * pitch : a.q + (int64_t) r * a.stride) + kg * 16;
+        exponents[t] = kFused ? s_exponents + r * steps : a.exponents + (int64_t) r * a.exponent_stride;
+    }
+    float4v acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
+    for (int32_t s = s0; s < s1; s += kFewDepth) {
+        int4v now[kFewDepth][2];
+        float w_power[kFewDepth];
+#pragma unroll
+        for (int d = 0; d < kFewDepth; ++d) {
+            now[d][0] = read[d][0];
+            now[d][1] = read[d][1];
+            w_power[d] = power_of(w_byte[d]);
+        }
+        if (s + kFewDepth < s1) fetch(s + kFewDepth);
+#pragma unroll
+        for (int d = 0; d < kFewDepth; ++d) {
+            if (s + d >= s1) break;                           // wave-uniform
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const bf8v right = values_of((uint32_t) now[d][h / 2][h % 2 * 2], (uint32_t) now[d][h / 2][h % 2 * 2 + 1], w_power[d]);
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(q[t] + (int64_t) (s + d) * GNS_FP8_BLOCK + h / 2 * 64 + h % 2 * 8);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values_of(v.x, v.y, power_of(exponents[t][s + d])), right, acc[t], 0, 0, 0);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s_sum[wave][t][v][lane] = acc[t][v];
+    __syncthreads();
+    // element v of lane l is row 4 * (l / 16) + v, column l % 16
+    for (int i = (int) threadIdx.x; i < MT * 4 * kWave; i += kFewBlock) {
+        const int t = i / (4 * kWave), v = i / kWave % 4, l = i % kWave;
+        const int32_t r = t * 16 + 4 * (l >> 4) + v, c = n0 + (l & 15);
+        if (r >= rows || c >= n) continue;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < kFewWaves; ++u) sum += s_sum[u][t][v][l];
+        store_at<T>(a.out, r, c, output_of(sum * kSumUp, a.bias ? a.bias[c] : 0.f, a.relu));
+    }
+}
+
+// k_fp8_rows: many rows against weights that fit LDS: rows come in, are quantised and multiplied, and leave, without a trip
+// through memory in 8 bits.  A block per CU (or two) holds all weights; its waves walk tiles of 16 rows: a row is read by L lanes, P pieces each,
+// quantised, turned through a piece of LDS of the wave's own and multiplied, 16 x 16 x 128, with the weights as the left
+// factor, so that a lane gets four consecutive outputs of a row.
+__host__ __device__ constexpr int64_t rows_lds(int64_t stride, int32_t n, int waves)
+{
+    return few_stride(stride) * ((n + 15) / 16 * 16 + waves * 16) + (int64_t) (n + 15) / 16 * 16 * 8 + waves * 64;
+}
+
+template <typename T, int L, int P, int kWaves>
+__global__ void __launch_bounds__(kWaves * kWave) k_fp8_rows(DenseFp8Args a, QuantizeFp8Args x)
+{
+    constexpr int V = kPiece<T>, kTurns = 16 * L / kWave;      // of a wave over a tile's rows
+    constexpr int kGroups = 4, kTeam = kBlockLanes<T>;         // of 16 output columns, multiplied together; lanes of a block of columns
+    constexpr bool kPrecise = sizeof(T) == 4;
+    extern __shared__ int4v s_rows[];
+    const int32_t rows = a.count.get(), n = a.out.width, n16 = (n + 15) / 16 * 16, steps = (int32_t) (a.stride / GNS_FP8_BLOCK);
+    const int32_t pitch = (int32_t) few_stride(a.stride), f1 = x.x1.width, k = a.k;
+    uint8_t* const s_w = reinterpret_cast<uint8_t*>(s_rows);
+    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6));
+    uint8_t* const s_q = s_w + n16 * pitch + wave * 16 * pitch;
+    float* const s_bias = reinterpret_cast<float*>(s_w + (n16 + kWaves * 16) * pitch);
+    int* const s_w_scale = reinterpret_cast<int*>(s_bias + n16);
+    uint8_t* const s_scale = reinterpret_cast<uint8_t*>(s_w_scale + n16) + wave * 64;          // of the tile's rows, four bytes each
+    const int32_t chunks = (int32_t) (a.stride / 16);
+    for (int32_t i = (int32_t) threadIdx.x; i < n16 * chunks; i += kWaves * kWave) {
+        const int32_t row = i / chunks, chunk = i - row * chunks;
+        *reinterpret_cast<int4v*>(s_w + row * pitch + chunk * 16) =
+            *reinterpret_cast<const int4v*>(a.wq + (int64_t) (row < n ? row : n - 1) * a.stride + chunk * 16);
+    }
+    for (int32_t i = (int32_t) threadIdx.x; i < n16; i += kWaves * kWave) {
+        s_w_scale[i] = *reinterpret_cast<const int*>(a.w_exponents + (int64_t) (i < n ? i : n - 1) * a.exponent_stride);
+        s_bias[i] = a.bias ? a.bias[i < n ? i : n - 1] : 0.f;
+    }
+    __syncthreads();
+    const int32_t tiles = (rows + 15) / 16;
+    const bool stores = n % 4 == 0 && reinterpret_cast<uintptr_t>(a.out.data) % 16 == 0 && (uint64_t) a.out.stride * sizeof(T) % 16 == 0;
+    // A tile's rows are read when the one before has been quantised, and come while that one is multiplied and stored.  Rows past
+    // the last are read as the last, lanes past the last column read the first.
+    Chunk v[kTurns][P];
+    auto fetch = [&](int32_t tile) {
+        const int lane = opaque_lane_id(), l = lane & (L - 1);
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int64_t row = (int64_t) tile * 16 + t * (kWave / L) + lane / L, r = row < rows ? row : rows - 1;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int32_t c = (p * L + l) * V, cc = c < k ? c : 0;
+                __builtin_memcpy(&v[t][p], cc < f1 ? reinterpret_cast<const T*>(x.x1.data) + r * x.x1.stride + cc
+                                                   : reinterpret_cast<const T*>(x.x2.data) + r * x.x2.stride + (cc - f1), 16);
+            }
+        }
+    };
+    // the blocks' first waves take the first tiles: a remainder spreads over all CUs
+    int32_t tile = wave * (int32_t) gridDim.x + (int32_t) blockIdx.x;
+    if (tile < tiles) fetch(tile);
+    for (; tile < tiles; tile += (int32_t) gridDim.x * kWaves) {
+        const int lane = opaque_lane_id(), l = lane & (L - 1), l16 = lane & 15, kg = lane >> 4;
+        const int64_t r0 = (int64_t) tile * 16;
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int32_t row = t * (kWave / L) + lane / L;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int32_t c = (p * L + l) * V;
+                const uint32_t words[4] = {v[t][p].x, v[t][p].y, v[t][p].z, v[t][p].w};
+                float f[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] = c < k ? value_of_words<T>(words, i) : 0.f;
+                const BlockScale s = block_scale(largest_of_lanes<kTeam>(largest_of(f, 0u)));
+                if (c < (int32_t) a.stride) {
+                    store_piece<T>(s_q + row * pitch + c, f, s.inverse, c, k);
+                    if ((l & (kTeam - 1)) == 0) s_scale[row * 4 + c / GNS_FP8_BLOCK] = (uint8_t) s.byte;
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (tile + (int32_t) gridDim.x * kWaves < tiles) fetch(tile + (int32_t) gridDim.x * kWaves);
+        const uint8_t* q = s_q + l16 * pitch + kg * 16;
+        const int scale = *reinterpret_cast<const int*>(s_scale + l16 * 4);
+        T* out = reinterpret_cast<T*>(a.out.data) + (r0 + l16) * a.out.stride;
+        for (int32_t c0 = 0; c0 < n16; c0 += 16 * kGroups) {
+            const uint8_t* w[kGroups];
+            int w_scale[kGroups];
+            float4v acc[kGroups];
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {               // groups past the last repeat it
+                const int32_t at = (c0 + g * 16 < n16 ? c0 + g * 16 : n16 - 16) + l16;
+                w[g] = s_w + at * pitch + kg * 16;
+                w_scale[g] = s_w_scale[at];
+                acc[g] = float4v{0.f, 0.f, 0.f, 0.f};
+            }
+            for (int32_t s = 0; s < steps; ++s) {
+                const int4v right[2] = {*reinterpret_cast<const int4v*>(q + s * GNS_FP8_BLOCK), *reinterpret_cast<const int4v*>(q + s * GNS_FP8_BLOCK + 64)};
+                if constexpr (kPrecise) {
+                    const float power = power_of((uint32_t) scale >> (8 * s) & 255u);
+                    bf8v values[4];
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) values[h] = values_of((uint32_t) right[h / 2][h % 2 * 2], (uint32_t) right[h / 2][h % 2 * 2 + 1], power);
+#pragma unroll
+                    for (int g = 0; g < kGroups; ++g) {
+                        const int4v left[2] = {*reinterpret_cast<const int4v*>(w[g] + s * GNS_FP8_BLOCK), *reinterpret_cast<const int4v*>(w[g] + s * GNS_FP8_BLOCK + 64)};
+                        const float w_power = power_of((uint32_t) w_scale[g] >> (8 * s) & 255u);
+#pragma unroll
+                        for (int h = 0; h < 4; ++h)
+                            acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values_of((uint32_t) left[h / 2][h % 2 * 2], (uint32_t) left[h / 2][h % 2 * 2 + 1], w_power),
+                                                                            values[h], acc[g], 0, 0, 0);
+                    }
+                } else {
+                    const int8v both = __builtin_shufflevector(right[0], right[1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                    for (int g = 0; g < kGroups; ++g) {
+                        const int8v left = __builtin_shufflevector(*reinterpret_cast<const int4v*>(w[g] + s * GNS_FP8_BLOCK),
+                                                                   *reinterpret_cast<const int4v*>(w[g] + s * GNS_FP8_BLOCK + 64), 0, 1, 2, 3, 4, 5, 6, 7);
+                        acc[g] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(left, both, acc[g], 0, 0, 0, w_scale[g] >> (8 * s), 0, scale >> (8 * s));
+                    }
+                }
+            }
+            // element i of lane l is output column 4 * (l / 16) + i of row l % 16
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int32_t c = c0 + g * 16 + 4 * kg;
+                if (c0 + g * 16 >= n16 || r0 + l16 >= rows) continue;
+                const float4 b = *reinterpret_cast<const float4*>(s_bias + c);
+                struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
+                y.v[0] = from_float<T>(output_of(acc[g][0] * (kPrecise ? kSumUp : 1.f), b.x, a.relu));
+                y.v[1] = from_float<T>(output_of(acc[g][1] * (kPrecise ? kSumUp : 1.f), b.y, a.relu));
+                y.v[2] = from_float<T>(output_of(acc[g][2] * (kPrecise ? kSumUp : 1.f), b.z, a.relu));
+                y.v[3] = from_float<T>(output_of(acc[g][3] * (kPrecise ? kSumUp : 1.f), b.w, a.relu));
+                if (stores) {
+                    if (c < n) *reinterpret_cast<Four*>(out + c) = y;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (c + i < n) out[c + i] = y.v[i];
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+static unsigned grid_of(const gns_ctx* c, int64_t blocks, int per_cu)
+{
+    const int64_t most = (int64_t) c->num_cus * per_cu;
+    return (unsigned) (blocks < most ? blocks : most);
+}
+
+hipError_t launch_quantize_fp8(const gns_ctx* c, const QuantizeFp8Args& a, int32_t type, hipStream_t s)
+{
+    const int64_t lanes = type == GNS_FP32 ? kBlockLanes<float> : kBlockLanes<Bf16>;
+    const dim3 grid(grid_of(c, ((int64_t) a.count.rows * a.exponent_stride * lanes + kBlock - 1) / kBlock, 32));
+    if (type == GNS_FP32) hipLaunchKernelGGL((k_quantize_fp8<float>), grid, dim3(kBlock), 0, s, a);
+    else                  hipLaunchKernelGGL((k_quantize_fp8<Bf16>), grid, dim3(kBlock), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T, int BM, int BN, int WM, int WN>
+static hipError_t launch_tiles(const DenseFp8Args& a, hipStream_t s)
+{
+    // a dimension of a grid has fewer than 2^32 threads; 2^31 tiles of outputs fit no memory
+    const int64_t m_tiles = ((int64_t) a.count.rows + BM - 1) / BM, n_tiles = (a.out.width + BN - 1) / BN, tiles = m_tiles * n_tiles, most = 1 << 22;
+    if (tiles > INT32_MAX - most) return hipErrorInvalidValue;
+    const dim3 grid((unsigned) (tiles < most ? tiles : most), (unsigned) ((tiles + most - 1) / most));
+    hipLaunchKernelGGL((k_fp8_tiles<T, BM, BN, WM, WN>), grid, dim3((BM / WM) * (BN / WN) * kWave), 0, s, a, (int32_t) m_tiles, (int32_t) n_tiles);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_typed(const gns_ctx* c, const DenseFp8Args& a, hipStream_t s)
+{
+    auto tiles = [&](int64_t bm, int64_t bn) { return (a.count.rows + bm - 1) / bm * ((a.out.width + bn - 1) / bn); };
+    if (a.count.rows <= 32 || (a.count.rows <= 64 && tiles(64, 64) * 2 < c->num_cus)) {
+        const dim3 grid((unsigned) ((a.out.width + kFewColumns - 1) / kFewColumns));
+        if (a.count.rows <= 16)      hipLaunchKernelGGL((k_fp8_few<T, float, false, 1>), grid, dim3(kFewBlock), 0, s, a, QuantizeFp8Args{});
+        else if (a.count.rows <= 32) hipLaunchKernelGGL((k_fp8_few<T, float, false, 2>), grid, dim3(kFewBlock), 0, s, a, QuantizeFp8Args{});
+        else                         hipLaunchKernelGGL((k_fp8_few<T, float, false, 4>), grid, dim3(kFewBlock), 0, s, a, QuantizeFp8Args{});
+        return hipGetLastError();
+    }
+    if (tiles(128, 128) >= c->num_cus) return launch_tiles<T, 128, 128, 64, 64>(a, s);
+    return launch_tiles<T, 64, 64, 32, 32>(a, s);
+}
+
+hipError_t launch_dense_fp8(const gns_ctx* c, const DenseFp8Args& a, int32_t out_type, hipStream_t s)
+{
+    return out_type == GNS_FP32 ? launch_typed<float>(c, a, s) : launch_typed<Bf16>(c, a, s);
+}
+
+// Rows and weights of k_fp8_rows: rows of whole pieces, as many as a tile's registers hold, weights that leave room in LDS, and
+// two tiles for each wave of a block per CU, or reading the weights into every LDS costs more than it saves
+template <typename T>
+static bool rows_fit(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a)
+{
+    return a.count.rows >= c->num_cus * 32 && a.stride <= 512 && a.k % kPiece<T> == 0 && x.x1.width % kPiece<T> == 0 &&
+           rows_lds(a.stride, a.out.width, 8) <= (int64_t) c->lds_bitmap_limit;
+}
+
+template <typename T, int L, int P>
+static void launch_rows_of(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a, hipStream_t s)
+{
+    constexpr bool kMany = P == 1 && (sizeof(T) == 2 || L < 64);       // registers for sixteen waves
+    const int64_t lds16 = rows_lds(a.stride, a.out.width, 16), lds8 = rows_lds(a.stride, a.out.width, 8);
+    if (kMany && lds16 <= (int64_t) c->lds_bitmap_limit) {
+        const dim3 grid((unsigned) (c->num_cus * (lds16 <= 80 * 1024 ? 2 : 1)));
+        hipLaunchKernelGGL((k_fp8_rows<T, L, P, kMany ? 16 : 8>), grid, dim3(16 * kWave), (size_t) lds16, s, a, x);
+    } else {
+        const dim3 grid((unsigned) (c->num_cus * (lds8 <= 80 * 1024 ? 2 : 1)));
+        hipLaunchKernelGGL((k_fp8_rows<T, L, P, 8>), grid, dim3(8 * kWave), (size_t) lds8, s, a, x);
+    }
+}
+
+template <typename T>
+static hipError_t launch_rows(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a, hipStream_t s)
+{
+    constexpr int V = kPiece<T>, L = kBlockLanes<T>;
+    if (a.stride <= L * V)          launch_rows_of<T, L, 1>(c, x, a, s);
+    else if (a.stride <= 2 * L * V) launch_rows_of<T, 2 * L, 1>(c, x, a, s);
+    else                            launch_rows_of<T, 64, 64 * V >= 512 ? 1 : 2>(c, x, a, s);
+    return hipGetLastError();
+}
+
+template <typename T, typename X>
+static void launch_few_fused(const QuantizeFp8Args& x, const DenseFp8Args& a, size_t lds, hipStream_t s)
+{
+    const dim3 grid((unsigned) ((a.out.width + kFewColumns - 1) / kFewColumns));
+    hipLaunchKernelGGL((k_fp8_few<T, X, true, 1>), grid, dim3(kFewBlock), lds, s, a, x);
+}
+
+hipError_t launch_sage_dense_fp8(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a, int32_t type, int32_t out_type,
+                                 hipStream_t s)
+{
+    const int64_t lds = few_lds(a.count.rows, a.stride);
+    if (a.count.rows <= 16 && lds <= (int64_t) kFewLds) {
+        if (type == GNS_FP32 && out_type == GNS_FP32) launch_few_fused<float, float>(x, a, (size_t) lds, s);
+        else if (type == GNS_FP32)                    launch_few_fused<Bf16, float>(x, a, (size_t) lds, s);
+        else if (out_type == GNS_FP32)                launch_few_fused<float, Bf16>(x, a, (size_t) lds, s);
+        else                                          launch_few_fused<Bf16, Bf16>(x, a, (size_t) lds, s);
+        return hipGetLastError();
+    }
+    if (type == GNS_FP32 && out_type == GNS_FP32 && rows_fit<float>(c, x, a)) return launch_rows<float>(c, x, a, s);
+    if (type == GNS_BF16 && out_type == GNS_BF16 && rows_fit<Bf16>(c, x, a)) return launch_rows<Bf16>(c, x, a, s);
+    const hipError_t e = launch_quantize_fp8(c, x, type, s);
+    return e != hipSuccess ? e : launch_dense_fp8(c, a, out_type, s);
+}
+
+}  // namespace gns

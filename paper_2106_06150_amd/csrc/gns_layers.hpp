@@ -1,0 +1,68 @@
+// What the kernels of group norm, of orthogonalised updates and of 8-bit floats share with the entry points (gfx950, wave64).
+#pragma once
+#include "../../include/gns_layers.h"
+#include "gns_learn.hpp"
+
+namespace gns {
+
+struct NormArgs {
+    ConstRows x, d_out;           // d_out: the backward pass
+    MutRows out;                  // of the forward pass, or dx (data null: not wanted)
+    const int32_t* segments;      // null: segment_rows rows each
+    int32_t num_segments, segment_rows;
+    int32_t groups, activation;
+    float eps;
+    const float* gamma;
+    const float* beta;
+    float* stats;                 // read by the backward pass; null: not wanted
+    float* dgamma;
+    float* dbeta;
+    RowCount count;
+    void* workspace;
+};
+
+struct OrthogonalArgs {
+    ConstRows grad, momentum, w;  // data null: none
+    MutRows momentum_out, out;
+    int32_t grad_type, momentum_type, w_type, momentum_out_type, out_type;
+    int32_t rows;
+    const gns_orthogonal* how;    // the host's
+    void* workspace;
+};
+
+struct QuantizeFp8Args {
+    ConstRows x1, x2;             // x2.width 0: one input
+    uint8_t* q;
+    uint8_t* exponents;
+    int64_t stride, exponent_stride;
+    RowCount count;
+};
+
+struct DenseFp8Args {
+    const uint8_t* q;
+    const uint8_t* exponents;
+    const uint8_t* wq;
+    const uint8_t* w_exponents;
+    const float* bias;
+    MutRows out;
+    int64_t stride, exponent_stride;
+    int32_t k, relu;
+    RowCount count;
+};
+
+// gns_norm.hip
+// bytes that a call of so many rows takes, and the most that one of so many or fewer does
+size_t norm_need(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type, int32_t rows, bool backward);
+size_t norm_workspace(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t rows, bool backward);
+hipError_t launch_norm(const gns_ctx* c, const NormArgs& a, int32_t type, hipStream_t s);
+hipError_t launch_norm_backward(const gns_ctx* c, const NormArgs& a, int32_t type, hipStream_t s);
+// gns_orthogonal.hip
+size_t orthogonal_workspace(int32_t width, int32_t rows);
+hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStream_t s);
+// gns_fp8.hip
+hipError_t launch_quantize_fp8(const gns_ctx* c, const QuantizeFp8Args& a, int32_t type, hipStream_t s);
+hipError_t launch_dense_fp8(const gns_ctx* c, const DenseFp8Args& a, int32_t out_type, hipStream_t s);
+hipError_t launch_sage_dense_fp8(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a, int32_t type, int32_t out_type,
+                                 hipStream_t s);
+
+}  // namespace gns

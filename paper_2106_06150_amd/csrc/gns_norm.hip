@@ -1,0 +1,947 @@
+// Group norm with an activation and its backward pass.  Two ways: groups of a row that lanes hold in registers (segments of one
+// row), and tiles of rows whose sums are joined (any segments).
+#include "gns_layers.hpp"
+#include <algorithm>
+
+namespace gns {
+
+template <typename T> constexpr int kPiece = 16 / (int) sizeof(T);        // values of 16 bytes
+
+__device__ __forceinline__ float sigmoid_of(float y) { return __builtin_amdgcn_rcpf(1.f + expf(-y)); }
+// The normal distribution's function, good to a few roundings of itself also far down.
+__device__ __forceinline__ float normal_below(float y) { return 0.5f * erfcf(-0.70710678f * y); }
+
+__device__ __forceinline__ float activate(float y, int32_t kind)
+{
+    if (kind == GNS_ACT_RELU) return relu_of(y);
+    if (kind == GNS_ACT_SILU) return y * sigmoid_of(y);
+    if (kind == GNS_ACT_GELU) return y * normal_below(y);
+    return y;
+}
+
+__device__ __forceinline__ float slope_at(float y, int32_t kind)
+{
+    if (kind == GNS_ACT_RELU) return y > 0.f ? 1.f : y <= 0.f ? 0.f : y;  // a NaN stays one
+    if (kind == GNS_ACT_SILU) {
+        const float s = sigmoid_of(y);
+        return s * (1.f + y * (1.f - s));
+    }
+    if (kind == GNS_ACT_GELU) return normal_below(y) + y * expf(-0.5f * y * y) * 0.39894228f;
+    return 1.f;
+}
+
+// Up to V consecutive columns of a range of `width`.  Where the range ends inside a piece the piece begins earlier, and what the one
+// before has is not its own; ranges of fewer than V columns are read singly.
+struct Columns {
+    int32_t first;                // column of value 0
+    int32_t skip, end;            // own values: skip <= i < end
+};
+template <int V>
+__device__ __forceinline__ Columns columns_from(int32_t c, int32_t width)
+{
+    if (c >= width) return Columns{0, 0, 0};
+    if (width < V) return Columns{0, 0, width};
+    const int32_t first = min(c, width - V);
+    return Columns{first, c - first, V};
+}
+
+template <typename T, bool kWhole>
+__device__ __forceinline__ void load_columns(const T* row, const Columns& c, uint32_t (&words)[4])
+{
+    constexpr int V = kPiece<T>;
+    if (kWhole || c.end == V) {
+        load_words(row + c.first, words);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) words[i] = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < c.end) {
+                if (sizeof(T) == 4) words[i] = __float_as_uint(to_float(row[c.first + i]));
+                else                words[i / 2] |= (__float_as_uint(to_float(row[c.first + i])) >> 16) << (16 * (i & 1));
+            }
+    }
+}
+
+template <typename T, bool kWhole>
+__device__ __forceinline__ void store_columns(T* row, const Columns& c, const float (&v)[kPiece<T>])
+{
+    constexpr int V = kPiece<T>;
+    struct Values { T v[V]; } out;
+#pragma unroll
+    for (int i = 0; i < V; ++i) out.v[i] = from_float<T>(v[i]);
+    if (kWhole || (c.skip == 0 && c.end == V)) {
+        __builtin_memcpy(row + c.first, &out, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i >= c.skip && i < c.end) row[c.first + i] = out.v[i];
+    }
+}
+
+// Parameters of the columns; `missing` where there are none.
+template <int V, bool kWhole>
+__device__ __forceinline__ void load_parameters(const float* p, const Columns& c, float missing, float (&v)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = missing;
+    if (!p) return;
+    if (kWhole || c.end == V) {
+        __builtin_memcpy(v, p + c.first, V * 4);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < c.end) v[i] = p[c.first + i];
+    }
+}
+
+// Sum over teams of L lanes (L = kBlock: the block, by way of LDS, which the caller's next call may use at once).
+template <int L>
+__device__ __forceinline__ float team_sum(float v, float* s_sums, int turn)
+{
+    if (L > 1) v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0xB1, 0xf, 0xf, true));        // lanes 1 0 3 2
+    if (L > 2) v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x4E, 0xf, 0xf, true));        // lanes 2 3 0 1
+    if (L > 4) v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x141, 0xf, 0xf, true));       // mirrored in 8
+    if (L > 8) v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x140, 0xf, 0xf, true));       // mirrored in 16
+    if (L > 16) v += __shfl_xor(v, 16);
+    if (L > 32) v += __shfl_xor(v, 32);
+    if (L > kWave) {
+        float* const s = s_sums + turn * (kBlock / kWave);
+        if (opaque_lane_id() == 0) s[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kBlock / kWave; ++w) v += s[w];
+    }
+    return v;
+}
+
+// A group whose variance is no finite number is spoilt.
+__device__ __forceinline__ float2 stats_of(float mean, float var, float eps)
+{
+    if (!(var < __uint_as_float(kInfBits))) return make_float2(quiet_nan(), quiet_nan());
+    return make_float2(mean, 1.f / sqrtf(var + eps));
+}
+
+// ---- segments of one row: a unit is a group of a row ---------------------------------------------------------------------
+// L lanes hold a unit in P pieces each, so rows are read once.  The launch's units number a multiple of the groups: a thread keeps
+// its columns, and with them scales and shifts.
+template <typename T, int L, int P, bool kWhole>
+__global__ void __launch_bounds__(kBlock) k_norm_units(NormArgs a, int64_t row_step)
+{
+    constexpr int V = kPiece<T>, U = kBlock / L;
+    constexpr bool kKeep = P * V <= 16;                       // parameters in registers
+    __shared__ float s_sums[2][kBlock / kWave];
+    const int32_t rows = a.count.get(), w = a.x.width / a.groups;
+    const int64_t u0 = (int64_t) blockIdx.x * U + threadIdx.x / L;
+    const int64_t r0 = u0 / a.groups;
+    const int32_t j = (int32_t) (u0 - r0 * a.groups), l = (int) threadIdx.x % L;
+    const float inverse = 1.f / (float) w;
+    Columns c[P];
+    float gamma[P][V], beta[P][V];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        c[p] = kWhole ? Columns{(p * L + l) * V, 0, V} : columns_from<V>((p * L + l) * V, w);
+        if (kKeep) {
+            load_parameters<V, kWhole>(a.gamma ? a.gamma + (int64_t) j * w : nullptr, c[p], 1.f, gamma[p]);
+            load_parameters<V, kWhole>(a.beta ? a.beta + (int64_t) j * w : nullptr, c[p], 0.f, beta[p]);
+        }
+    }
+    // a wave's lanes make as many turns as its first, which has the lowest row
+    for (int64_t row = r0; (int32_t) __builtin_amdgcn_readfirstlane((int32_t) min(row, (int64_t) INT32_MAX)) < rows; row += row_step) {
+        const int64_t r = row < rows ? row : rows - 1;
+        const T* x = reinterpret_cast<const T*>(a.x.data) + r * a.x.stride + (int64_t) j * w;
+        uint32_t words[P][4];
+#pragma unroll
+        for (int p = 0; p < P; ++p) load_columns<T, kWhole>(x, c[p], words[p]);
+        float sum = 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (kWhole || (i >= c[p].skip && i < c[p].end)) sum += value_of_words<T>(words[p], i);
+        const float mean = team_sum<L>(sum, &s_sums[0][0], 0) * inverse;
+        float squares = 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (kWhole || (i >= c[p].skip && i < c[p].end)) {
+                    const float d = value_of_words<T>(words[p], i) - mean;
+                    squares += d * d;
+                }
+        const float2 s = stats_of(mean, team_sum<L>(squares, &s_sums[0][0], 1) * inverse, a.eps);
+        if (row >= rows) continue;
+        T* out = reinterpret_cast<T*>(a.out.data) + r * a.out.stride + (int64_t) j * w;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float y[V], g[V], b[V];
+            if (!kKeep) {
+                load_parameters<V, kWhole>(a.gamma ? a.gamma + (int64_t) j * w : nullptr, c[p], 1.f, g);
+                load_parameters<V, kWhole>(a.beta ? a.beta + (int64_t) j * w : nullptr, c[p], 0.f, b);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                y[i] = activate((value_of_words<T>(words[p], i) - s.x) * (s.y * (kKeep ? gamma[p][i] : g[i])) + (kKeep ? beta[p][i] : b[i]), a.activation);
+            store_columns<T, kWhole>(out, c[p], y);
+        }
+        if (a.stats && l == 0) reinterpret_cast<float2*>(a.stats)[r * a.groups + j] = s;
+    }
+}
+
+// The backward pass of the same: rows are read once, sums for dgamma and dbeta stay in registers and leave as `parts`, rows of
+// width pairs (dbeta, dgamma), which k_norm_columns sums.  Where a block has all groups of several rows it joins those first.
+template <typename T, int L, int P, bool kWhole>
+__global__ void __launch_bounds__(kBlock) k_norm_grad_units(NormArgs a, int64_t row_step, float2* parts)
+{
+    constexpr int V = kPiece<T>, U = kBlock / L;
+    __shared__ float s_sums[2][kBlock / kWave];
+    __shared__ float2 s_part[kBlock * V];
+    const int32_t rows = a.count.get(), w = a.x.width / a.groups;
+    const int64_t u0 = (int64_t) blockIdx.x * U + threadIdx.x / L;
+    const int64_t r0 = u0 / a.groups;
+    const int32_t j = (int32_t) (u0 - r0 * a.groups), l = (int) threadIdx.x % L;
+    const float inverse = 1.f / (float) w;
+    const float* gammas = a.gamma ? a.gamma + (int64_t) j * w : nullptr;
+    const float* betas = a.beta ? a.beta + (int64_t) j * w : nullptr;
+    Columns c[P];
+    float sum1[P][V], sum2[P][V];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        c[p] = kWhole ? Columns{(p * L + l) * V, 0, V} : columns_from<V>((p * L + l) * V, w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum1[p][i] = sum2[p][i] = 0.f;
+    }
+    for (int64_t row = r0; (int32_t) __builtin_amdgcn_readfirstlane((int32_t) min(row, (int64_t) INT32_MAX)) < rows; row += row_step) {
+        const int64_t r = row < rows ? row : rows - 1;
+        const T* x = reinterpret_cast<const T*>(a.x.data) + r * a.x.stride + (int64_t) j * w;
+        const T* d = reinterpret_cast<const T*>(a.d_out.data) + r * a.d_out.stride + (int64_t) j * w;
+        const float2 s = reinterpret_cast<const float2*>(a.stats)[r * a.groups + j];
+        uint32_t xw[P][4], dw[P][4];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            load_columns<T, kWhole>(x, c[p], xw[p]);
+            load_columns<T, kWhole>(d, c[p], dw[p]);
+        }
+        float h[P][V], g[P][V], m1 = 0.f, m2 = 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float gamma[V], beta[V];
+            load_parameters<V, kWhole>(gammas, c[p], 1.f, gamma);
+            load_parameters<V, kWhole>(betas, c[p], 0.f, beta);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                h[p][i] = (value_of_words<T>(xw[p], i) - s.x) * s.y;
+                const float dy = value_of_words<T>(dw[p], i) * slope_at(h[p][i] * gamma[i] + beta[i], a.activation);
+                g[p][i] = dy * gamma[i];
+                if (kWhole || (i >= c[p].skip && i < c[p].end)) {
+                    m1 += g[p][i];
+                    m2 += g[p][i] * h[p][i];
+                    if (row < rows) {
+                        sum1[p][i] += dy;
+                        sum2[p][i] += dy * h[p][i];
+                    }
+                }
+            }
+        }
+        if (!a.out.data) continue;
+        m1 = team_sum<L>(m1, &s_sums[0][0], 0) * inverse;
+        m2 = team_sum<L>(m2, &s_sums[0][0], 1) * inverse;
+        if (L > kWave) __syncthreads();                       // the next row's sums go to the same places
+        if (row >= rows) continue;
+        T* out = reinterpret_cast<T*>(a.out.data) + r * a.out.stride + (int64_t) j * w;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float dx[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) dx[i] = s.y * (g[p][i] - m1 - h[p][i] * m2);
+            store_columns<T, kWhole>(out, c[p], dx);
+        }
+    }
+    if (!parts) return;
+    const int32_t width = a.x.width;
+    const bool joined = U % a.groups == 0;
+    const int32_t same = joined ? U / a.groups : 1;           // units of a group in this block
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        if (same > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) s_part[i * kBlock + threadIdx.x] = make_float2(sum1[p][i], sum2[p][i]);
+            __syncthreads();
+            if ((int) threadIdx.x < kBlock / same) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float2 t = make_float2(0.f, 0.f);
+                    for (int k = 0; k < same; ++k) {
+                        const float2 v = s_part[i * kBlock + k * (kBlock / same) + threadIdx.x];
+                        t.x += v.x; t.y += v.y;
+                    }
+                    sum1[p][i] = t.x; sum2[p][i] = t.y;
+                }
+            }
+        }
+        if ((int) threadIdx.x >= kBlock / same) continue;
+        float2* to = parts + (joined ? (int64_t) blockIdx.x : r0) * width + (int64_t) j * w + c[p].first;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (kWhole || (i >= c[p].skip && i < c[p].end)) to[i] = make_float2(sum1[p][i], sum2[p][i]);
+    }
+}
+
+// dbeta and dgamma from `count` rows of pairs (count_of: as many as there are tiles of so many rows): 16 columns a block, sixteen threads each.
+constexpr int kJoinColumns = 16;
+__global__ void __launch_bounds__(kBlock) k_norm_columns(const float2* parts, int64_t count, RowCount rows, int32_t tile_rows, int32_t width,
+                                                         float* dgamma, float* dbeta)
+{
+    __shared__ float2 s_sum[kBlock / kJoinColumns][kJoinColumns];
+    constexpr int kTurns = kBlock / kJoinColumns;
+    if (tile_rows) count = ((int64_t) rows.get() + tile_rows - 1) / tile_rows;
+    const int at = (int) threadIdx.x % kJoinColumns, k = (int) threadIdx.x / kJoinColumns;
+    const int32_t column = (int32_t) blockIdx.x * kJoinColumns + at, c = column < width ? column : width - 1;
+    float2 t = make_float2(0.f, 0.f);
+#pragma unroll 8
+    for (int64_t i = k; i < count; i += kTurns) {
+        const float2 v = parts[i * width + c];
+        t.x += v.x; t.y += v.y;
+    }
+    s_sum[k][at] = t;
+    __syncthreads();
+    if (k || column >= width) return;
+    for (int i = 1; i < kTurns; ++i) { t.x += s_sum[i][at].x; t.y += s_sum[i][at].y; }
+    if (dbeta) dbeta[column] = t.x;
+    if (dgamma) dgamma[column] = t.y;
+}
+
+// ---- any segments: tiles of rows -------------------------------------------------------------------------------------------
+// Where the segments lie.  Offsets are kept inside the rows, whatever they hold.
+struct Segments {
+    const int32_t* at;
+    int32_t n, per, rows;
+    __device__ __forceinline__ Segments(const NormArgs& a, int32_t rows_) : at(a.segments), per(a.segment_rows), rows(rows_)
+    {
+        n = at ? a.num_segments : (int32_t) (((int64_t) rows + per - 1) / per);
+    }
+    __device__ __forceinline__ int32_t begin(int32_t s) const
+    {
+        return at ? min(max(at[s], 0), rows) : (int32_t) min((int64_t) s * per, (int64_t) rows);
+    }
+    __device__ __forceinline__ int32_t end(int32_t s) const
+    {
+        return at ? min(max(at[s + 1], begin(s)), rows) : (int32_t) min((int64_t) (s + 1) * per, (int64_t) rows);
+    }
+    // the first segment that ends behind a row
+    __device__ __forceinline__ int32_t first(int32_t row) const
+    {
+        if (!at) return row / per;
+        int32_t low = 0, high = n;
+        while (low < high) {
+            const int32_t mid = low + (high - low) / 2;
+            if (at[mid + 1] > row) high = mid;
+            else                   low = mid + 1;
+        }
+        return low;
+    }
+};
+
+// A tile's rows meet segments in order, a slab's columns groups: pairs (tile, segment) and (slab, group) each have a place of their
+// own at the sum of the two, and there are no more places than tiles and segments, slabs and groups together.
+struct Tiling {
+    int32_t tile_rows, slabs;     // slabs of up to kBlock pieces
+    int64_t tiles;
+    int32_t threads, turns;       // threads of a row, rows at a time
+    int64_t entries;              // of a slot: slabs + groups
+};
+
+template <typename T>
+__host__ __device__ constexpr int32_t slab_columns() { return kBlock * kPiece<T>; }
+
+// What a block of the tiled kernels has to do with
+template <typename T>
+struct TileBlock {
+    int32_t rows, width, w, slab, first_row, last_row, c0, c1, turn;      // c0, c1: the slab's columns
+    bool works;
+    Columns c;
+    __device__ __forceinline__ TileBlock(const NormArgs& a, const Tiling& t)
+    {
+        rows = a.count.get();
+        width = a.x.width;
+        w = width / a.groups;
+        slab = (int32_t) blockIdx.y;
+        first_row = (int32_t) min((int64_t) blockIdx.x * t.tile_rows, (int64_t) rows);
+        last_row = (int32_t) min((int64_t) (blockIdx.x + 1) * t.tile_rows, (int64_t) rows);
+        c0 = slab * slab_columns<T>();
+        c1 = min(width, c0 + slab_columns<T>());
+        turn = (int32_t) threadIdx.x / t.threads;
+        works = turn < t.turns;
+        c = columns_from<kPiece<T>>(c0 + ((int32_t) threadIdx.x - turn * t.threads) * kPiece<T>, width);
+        if (!works) c.end = c.skip = 0;
+    }
+};
+
+// Teams of a block for `parts` things, each of up to `most` entries: lanes a team, at most a wave.
+__device__ __forceinline__ int32_t team_lanes(int32_t parts, int32_t most)
+{
+    int32_t lanes = kWave;
+    while (lanes > 1 && (parts * lanes > kBlock || lanes / 2 >= most)) lanes /= 2;
+    return lanes;
+}
+__device__ __forceinline__ float lanes_sum(float v, int32_t lanes)
+{
+    for (int32_t m = 1; m < lanes; m *= 2) v += __shfl_xor(v, m);
+    return v;
+}
+
+// Mean and sum of squared distances of each group of the slab, for each segment in the tile: by column in registers (Welford's
+// steps, every column of a thread has as many rows), then over threads and columns by way of LDS.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) k_norm_parts(NormArgs a, Tiling t, float2* parts)
+{
+    constexpr int V = kPiece<T>;
+    __shared__ float s_mean[kBlock * V], s_squares[kBlock * V];
+    const TileBlock<T> b(a, t);
+    const Segments segments(a, b.rows);
+    const int32_t pitch = t.threads * V, first_group = b.c0 / b.w, groups = (b.c1 - 1) / b.w - first_group + 1;
+    const int32_t lanes = team_lanes(groups, b.w);
+    for (int32_t s = segments.first(b.first_row); s < segments.n && b.first_row < b.last_row; ++s) {
+        const int32_t begin = segments.begin(s);
+        if (begin >= b.last_row) break;
+        const int32_t r0 = max(begin, b.first_row), r1 = min(segments.end(s), b.last_row);
+        if (r0 >= r1) continue;
+        float mean[V], squares[V], n = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) mean[i] = squares[i] = 0.f;
+        if (b.c.end) {
+            for (int32_t r = r0 + b.turn; r < r1; r += t.turns) {
+                uint32_t words[4];
+                load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + (int64_t) r * a.x.stride, b.c, words);
+                n += 1.f;
+                const float inverse = __builtin_amdgcn_rcpf(n);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float v = value_of_words<T>(words, i), d = v - mean[i];
+                    mean[i] += d * inverse;
+                    squares[i] += d * (v - mean[i]);
+                }
+            }
+        }
+        __syncthreads();                                      // the segment before may still be read
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i >= b.c.skip && i < b.c.end) {
+                s_mean[b.turn * pitch + b.c.first + i - b.c0] = mean[i];
+                s_squares[b.turn * pitch + b.c.first + i - b.c0] = squares[i];
+            }
+        __syncthreads();
+        const int32_t team = opaque((int) threadIdx.x) / lanes, lane = opaque((int) threadIdx.x) % lanes, turns = min(t.turns, r1 - r0);
+        for (int32_t g0 = 0; g0 < groups; g0 += kBlock / lanes) {
+            const int32_t g = min(g0 + team, groups - 1), j = first_group + g;
+            const int32_t from = max(j * b.w, b.c0) - b.c0, to = min((j + 1) * b.w, b.c1) - b.c0;
+            float sum = 0.f;
+            for (int32_t k = 0; k < turns; ++k) {
+                const float of = (float) ((r1 - r0 - k + t.turns - 1) / t.turns);
+                for (int32_t c = from + lane; c < to; c += lanes) sum += of * s_mean[k * pitch + c];
+            }
+            const float all = lanes_sum(sum, lanes) / ((float) (r1 - r0) * (float) (to - from));
+            sum = 0.f;
+            for (int32_t k = 0; k < turns; ++k) {
+                const float of = (float) ((r1 - r0 - k + t.turns - 1) / t.turns);
+                for (int32_t c = from + lane; c < to; c += lanes) {
+                    const float d = s_mean[k * pitch + c] - all;
+                    sum += s_squares[k * pitch + c] + of * d * d;
+                }
+            }
+            sum = lanes_sum(sum, lanes);
+            if (lane == 0 && g0 + team < groups) parts[((int64_t) blockIdx.x + s) * t.entries + j + b.slab] = make_float2(all, sum);
+        }
+    }
+}
+
+// What tiles and slabs found for a segment and group, together: L lanes each.  kGrad: sums of the backward pass, divided by the
+// number of values, to `moments`; otherwise means and squares, to the stats.
+template <typename T, int L, bool kGrad>
+__global__ void __launch_bounds__(kBlock) k_norm_join(NormArgs a, Tiling t, const float2* parts, float2* to)
+{
+    __shared__ float s_sums[2][kBlock / kWave];
+    const int32_t rows = a.count.get(), w = a.x.width / a.groups;
+    const Segments segments(a, rows);
+    const int64_t units = (int64_t) segments.n * a.groups, step = (int64_t) gridDim.x * (kBlock / L);
+    for (int64_t u0 = (int64_t) blockIdx.x * (kBlock / L); u0 < units; u0 += step) {
+        const int64_t u = min(u0 + (int64_t) opaque((int) threadIdx.x) / L, units - 1);
+        const int32_t l = opaque((int) threadIdx.x) % L, s = (int32_t) (u / a.groups), j = (int32_t) (u - (int64_t) s * a.groups);
+        const int32_t begin = segments.begin(s), end = segments.end(s);
+        const int32_t tile0 = begin / t.tile_rows, tiles = end > begin ? (end - 1) / t.tile_rows - tile0 + 1 : 0;
+        const int64_t c0 = (int64_t) j * w, c1 = c0 + w;
+        const int32_t slab0 = (int32_t) (c0 / slab_columns<T>()), slabs = (int32_t) ((c1 - 1) / slab_columns<T>()) - slab0 + 1;
+        const float n = (float) (end - begin) * (float) w;
+        auto part = [&](int64_t e, float* of) {
+            const int32_t tile = tile0 + (int32_t) (e / slabs), slab = slab0 + (int32_t) (e % slabs);
+            const int64_t row0 = max((int64_t) begin, (int64_t) tile * t.tile_rows), row1 = min((int64_t) end, (int64_t) (tile + 1) * t.tile_rows);
+            const int64_t from = max(c0, (int64_t) slab * slab_columns<T>()), upto = min(c1, (int64_t) (slab + 1) * slab_columns<T>());
+            *of = (float) (row1 - row0) * (float) (upto - from);
+            return parts[((int64_t) tile + s) * t.entries + j + slab];
+        };
+        const int64_t all = (int64_t) tiles * slabs;
+        float one = 0.f, two = 0.f, of;
+        for (int64_t e = l; e < all; e += L) {
+            const float2 p = part(e, &of);
+            one += kGrad ? p.x : of * p.x;
+            two += p.y;
+        }
+        one = team_sum<L>(one, &s_sums[0][0], 0) / n;
+        if (!kGrad) {
+            for (int64_t e = l; e < all; e += L) {
+                const float d = part(e, &of).x - one;
+                two += of * d * d;
+            }
+        }
+        two = team_sum<L>(two, &s_sums[0][0], 1) / n;
+        if (L > kWave) __syncthreads();
+        if (l == 0) {
+            if (all == 0)   to[u] = make_float2(0.f, 0.f);
+            else if (kGrad) to[u] = make_float2(one, two);
+            else            to[u] = stats_of(one, two, a.eps);
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kBlock) k_norm_apply(NormArgs a, Tiling t, const float2* stats)
+{
+    constexpr int V = kPiece<T>;
+    const TileBlock<T> b(a, t);
+    const Segments segments(a, b.rows);
+    if (!b.c.end) return;
+    float gamma[V], beta[V];
+    int32_t j[V];
+    load_parameters<V, false>(a.gamma, b.c, 1.f, gamma);
+    load_parameters<V, false>(a.beta, b.c, 0.f, beta);
+#pragma unroll
+    for (int i = 0; i < V; ++i) j[i] = min(b.c.first + i, b.width - 1) / b.w;
+    for (int32_t s = segments.first(b.first_row); s < segments.n && b.first_row < b.last_row; ++s) {
+        const int32_t begin = segments.begin(s);
+        if (begin >= b.last_row) break;
+        const int32_t r0 = max(begin, b.first_row), r1 = min(segments.end(s), b.last_row);
+        float mean[V], scale[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float2 v = stats[(int64_t) s * a.groups + j[i]];
+            mean[i] = v.x;
+            scale[i] = v.y * gamma[i];
+        }
+        for (int32_t r = r0 + b.turn; r < r1; r += t.turns) {
+            uint32_t words[4];
+            float y[V];
+            load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + (int64_t) r * a.x.stride, b.c, words);
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = activate((value_of_words<T>(words, i) - mean[i]) * scale[i] + beta[i], a.activation);
+            store_columns<T, false>(reinterpret_cast<T*>(a.out.data) + (int64_t) r * a.out.stride, b.c, y);
+        }
+    }
+}
+
+// Sums of gamma dy and gamma dy h of each group of the slab, for each segment in the tile, and of dy and dy h of each column over
+// the tile's segments.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) k_norm_grad_parts(NormArgs a, Tiling t, float2* parts, float2* columns)
+{
+    constexpr int V = kPiece<T>;
+    __shared__ float s_one[kBlock * V], s_two[kBlock * V];
+    const TileBlock<T> b(a, t);
+    const Segments segments(a, b.rows);
+    const int32_t pitch = t.threads * V, first_group = b.c0 / b.w, groups = (b.c1 - 1) / b.w - first_group + 1;
+    const int32_t lanes = team_lanes(groups, b.w);
+    float gamma[V], beta[V], sum1[V], sum2[V];
+    int32_t j[V];
+    load_parameters<V, false>(a.gamma, b.c, 1.f, gamma);
+    load_parameters<V, false>(a.beta, b.c, 0.f, beta);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        j[i] = min(b.c.first + i, b.width - 1) / b.w;
+        sum1[i] = sum2[i] = 0.f;
+    }
+    auto put = [&](const float (&one)[V], const float (&two)[V]) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i >= b.c.skip && i < b.c.end) {
+                s_one[b.turn * pitch + b.c.first + i - b.c0] = one[i];
+                s_two[b.turn * pitch + b.c.first + i - b.c0] = two[i];
+            }
+    };
+    for (int32_t s = segments.first(b.first_row); s < segments.n && b.first_row < b.last_row; ++s) {
+        const int32_t begin = segments.begin(s);
+        if (begin >= b.last_row) break;
+        const int32_t r0 = max(begin, b.first_row), r1 = min(segments.end(s), b.last_row);
+        if (r0 >= r1) continue;
+        float one[V], two[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) one[i] = two[i] = 0.f;
+        if (b.c.end) {
+            float mean[V], rstd[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float2 v = reinterpret_cast<const float2*>(a.stats)[(int64_t) s * a.groups + j[i]];
+                mean[i] = v.x;
+                rstd[i] = v.y;
+            }
+            for (int32_t r = r0 + b.turn; r < r1; r += t.turns) {
+                uint32_t xw[4], dw[4];
+                load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + (int64_t) r * a.x.stride, b.c, xw);
+                load_columns<T, false>(reinterpret_cast<const T*>(a.d_out.data) + (int64_t) r * a.d_out.stride, b.c, dw);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float h = (value_of_words<T>(xw, i) - mean[i]) * rstd[i];
+                    const float dy = value_of_words<T>(dw, i) * slope_at(h * gamma[i] + beta[i], a.activation);
+                    one[i] += dy;
+                    two[i] += dy * h;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                sum1[i] += one[i];
+                sum2[i] += two[i];
+                one[i] *= gamma[i];
+                two[i] *= gamma[i];
+            }
+        }
+        __syncthreads();
+        put(one, two);
+        __syncthreads();
+        if (!parts) continue;
+        const int32_t team = opaque((int) threadIdx.x) / lanes, lane = opaque((int) threadIdx.x) % lanes;
+        for (int32_t g0 = 0; g0 < groups; g0 += kBlock / lanes) {
+            const int32_t g = min(g0 + team, groups - 1), group = first_group + g;
+            const int32_t from = max(group * b.w, b.c0) - b.c0, to = min((group + 1) * b.w, b.c1) - b.c0;
+            float m1 = 0.f, m2 = 0.f;
+            for (int32_t k = 0; k < t.turns; ++k)
+                for (int32_t c = from + lane; c < to; c += lanes) {
+                    m1 += s_one[k * pitch + c];
+                    m2 += s_two[k * pitch + c];
+                }
+            m1 = lanes_sum(m1, lanes);
+            m2 = lanes_sum(m2, lanes);
+            if (lane == 0 && g0 + team < groups) parts[((int64_t) blockIdx.x + s) * t.entries + group + b.slab] = make_float2(m1, m2);
+        }
+    }
+    if (!columns || b.first_row >= b.last_row) return;
+    __syncthreads();
+    put(sum1, sum2);
+    __syncthreads();
+    for (int32_t c = (int32_t) threadIdx.x; c < b.c1 - b.c0; c += kBlock) {
+        float m1 = 0.f, m2 = 0.f;
+        for (int32_t k = 0; k < t.turns; ++k) {
+            m1 += s_one[k * pitch + c];
+            m2 += s_two[k * pitch + c];
+        }
+        columns[(int64_t) blockIdx.x * b.width + b.c0 + c] = make_float2(m1, m2);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kBlock) k_norm_grad_apply(NormArgs a, Tiling t, const float2* moments)
+{
+    constexpr int V = kPiece<T>;
+    const TileBlock<T> b(a, t);
+    const Segments segments(a, b.rows);
+    if (!b.c.end) return;
+    float gamma[V], beta[V];
+    int32_t j[V];
+    load_parameters<V, false>(a.gamma, b.c, 1.f, gamma);
+    load_parameters<V, false>(a.beta, b.c, 0.f, beta);
+#pragma unroll
+    for (int i = 0; i < V; ++i) j[i] = min(b.c.first + i, b.width - 1) / b.w;
+    for (int32_t s = segments.first(b.first_row); s < segments.n && b.first_row < b.last_row; ++s) {
+        const int32_t begin = segments.begin(s);
+        if (begin >= b.last_row) break;
+        const int32_t r0 = max(begin, b.first_row), r1 = min(segments.end(s), b.last_row);
+        float mean[V], rstd[V], m1[V], m2[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float2 v = reinterpret_cast<const float2*>(a.stats)[(int64_t) s * a.groups + j[i]], m = moments[(int64_t) s * a.groups + j[i]];
+            mean[i] = v.x; rstd[i] = v.y;
+            m1[i] = m.x; m2[i] = m.y;
+        }
+        for (int32_t r = r0 + b.turn; r < r1; r += t.turns) {
+            uint32_t xw[4], dw[4];
+            float dx[V];
+            load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + (int64_t) r * a.x.stride, b.c, xw);
+            load_columns<T, false>(reinterpret_cast<const T*>(a.d_out.data) + (int64_t) r * a.d_out.stride, b.c, dw);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float h = (value_of_words<T>(xw, i) - mean[i]) * rstd[i];
+                const float dy = value_of_words<T>(dw, i) * slope_at(h * gamma[i] + beta[i], a.activation);
+                dx[i] = rstd[i] * (dy * gamma[i] - m1[i] - h * m2[i]);
+            }
+            store_columns<T, false>(reinterpret_cast<T*>(a.out.data) + (int64_t) r * a.out.stride, b.c, dx);
+        }
+    }
+}
+
+// ---- which way, and what it takes ------------------------------------------------------------------------------------------
+namespace {
+
+constexpr size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+int64_t gcd(int64_t a, int64_t b)
+{
+    while (b) { const int64_t t = a % b; a = b; b = t; }
+    return a;
+}
+
+int32_t piece_of(int32_t type) { return type == GNS_FP32 ? 4 : 8; }
+
+int64_t segment_count(const gns_norm* n, int32_t rows)
+{
+    return n->segments_dev ? n->num_segments : ((int64_t) rows + n->segment_rows - 1) / n->segment_rows;
+}
+
+// Lanes and pieces of a unit of w columns; lanes 0: it is too long for registers.
+struct UnitShape {
+    int32_t lanes, pieces;
+};
+UnitShape unit_shape(int32_t w, int32_t type)
+{
+    const int64_t pieces = ((int64_t) w + piece_of(type) - 1) / piece_of(type);
+    for (int32_t lanes = 1; lanes <= kWave; lanes *= 2)
+        if (pieces <= lanes) return {lanes, 1};
+    if (pieces <= 2 * kWave) return {kWave, 2};
+    if (pieces <= 2 * kBlock) return {kBlock, 2};
+    if (pieces <= 4 * kBlock) return {kBlock, 4};
+    if (pieces <= 8 * kBlock) return {kBlock, 8};
+    return {0, 0};
+}
+
+bool by_units(const gns_norm* n, int32_t width, int32_t type)
+{
+    return !n->segments_dev && n->segment_rows == 1 && unit_shape(width / n->groups, type).lanes > 0;
+}
+
+// Blocks of a launch over units, and the rows between a thread's units.  Their units are whole rows, or turns of rows.
+struct UnitGrid {
+    int64_t blocks, row_step;
+};
+UnitGrid unit_grid(int64_t rows, int32_t groups, int32_t lanes, int64_t most)
+{
+    const int64_t each = kBlock / lanes, all = (rows * groups + each - 1) / each, whole = groups / gcd(groups, each);
+    const int64_t blocks = std::max<int64_t>(std::min(all, most) / whole, 1) * whole;
+    return {blocks, blocks * each / groups};
+}
+
+// Rows of parts for dgamma and dbeta that a launch over units leaves
+int64_t unit_parts(const UnitGrid& g, int32_t groups, int32_t lanes) { return (kBlock / lanes) % groups == 0 ? g.blocks : g.row_step; }
+
+// The backward pass's blocks: few enough that their parts are a tenth of the rows at most, one a CU at least
+int64_t unit_grad_blocks(const gns_ctx* c, int64_t rows, int32_t groups, int32_t lanes)
+{
+    const int64_t per = std::max<int64_t>(1, groups / std::max<int64_t>(kBlock / lanes, 1));     // blocks to a row of parts
+    return std::max<int64_t>(c->num_cus, std::min<int64_t>((int64_t) c->num_cus * 8, rows / 16 * per));
+}
+
+Tiling tiling_of(const gns_ctx* c, int32_t width, int32_t groups, int32_t type, int32_t rows)
+{
+    Tiling t;
+    const int32_t pieces = (width + piece_of(type) - 1) / piece_of(type);
+    t.slabs = (pieces + kBlock - 1) / kBlock;
+    t.threads = std::min(pieces, kBlock);
+    t.turns = kBlock / t.threads;
+    t.tile_rows = 16;
+    while (t.tile_rows < 256 && (int64_t) t.tile_rows * 4 * c->num_cus < (int64_t) rows * t.slabs) t.tile_rows *= 2;
+    t.tiles = ((int64_t) rows + t.tile_rows - 1) / t.tile_rows;
+    t.entries = (int64_t) t.slabs + groups;
+    return t;
+}
+
+struct TiledSpace {
+    size_t parts, moments, columns, all;      // where each begins
+};
+TiledSpace tiled_space(const Tiling& t, int64_t tiles, int64_t segments, int32_t width, int32_t groups, bool backward)
+{
+    TiledSpace s;
+    s.parts = 0;
+    s.moments = up((size_t) (tiles + segments) * (size_t) t.entries * 8);
+    s.columns = s.moments + up((size_t) segments * (size_t) groups * 8);
+    s.all = s.columns + (backward ? up((size_t) tiles * (size_t) width * 8) : 0);
+    return s;
+}
+
+size_t need_of(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type, int32_t rows, bool backward)
+{
+    if (by_units(n, width, type)) {
+        if (!backward) return 0;
+        const int32_t lanes = unit_shape(width / n->groups, type).lanes;
+        const UnitGrid g = unit_grid(rows, n->groups, lanes, unit_grad_blocks(c, rows, n->groups, lanes));
+        return (size_t) unit_parts(g, n->groups, lanes) * (size_t) width * 8;
+    }
+    const Tiling t = tiling_of(c, width, n->groups, type, rows);
+    return tiled_space(t, t.tiles, segment_count(n, rows), width, n->groups, backward).all;
+}
+
+// The most of any number of rows up to this.  Units: parts grow with the rows.  Tiles: those of a height are most just before the next
+// height begins.
+size_t most_of(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type, int32_t rows, bool backward)
+{
+    if (by_units(n, width, type)) {
+        if (!backward) return 0;
+        const int32_t lanes = unit_shape(width / n->groups, type).lanes;
+        // a launch has no more blocks than this, or those of one row
+        const int64_t each = kBlock / lanes, whole = n->groups / gcd(n->groups, each);
+        const UnitGrid g = {std::max(unit_grad_blocks(c, rows, n->groups, lanes), whole), 0};
+        return (size_t) unit_parts({g.blocks, (g.blocks * each + n->groups - 1) / n->groups}, n->groups, lanes) * (size_t) width * 8;
+    }
+    const Tiling t = tiling_of(c, width, n->groups, type, rows);
+    int64_t tiles = t.tiles;
+    for (int32_t height = 16; height < t.tile_rows; height *= 2)
+        tiles = std::max<int64_t>(tiles, (int64_t) 4 * c->num_cus / t.slabs + 1);
+    return tiled_space(t, tiles, segment_count(n, rows), width, n->groups, backward).all;
+}
+
+template <typename T, int L, int P>
+void launch_units(const NormArgs& a, const UnitGrid& g, bool whole, hipStream_t s)
+{
+    const dim3 grid((unsigned) g.blocks);
+    if (whole) hipLaunchKernelGGL((k_norm_units<T, L, P, true>), grid, dim3(kBlock), 0, s, a, g.row_step);
+    else       hipLaunchKernelGGL((k_norm_units<T, L, P, false>), grid, dim3(kBlock), 0, s, a, g.row_step);
+}
+
+template <typename T, int L, int P>
+void launch_grad_units(const NormArgs& a, const UnitGrid& g, bool whole, float2* parts, hipStream_t s)
+{
+    const dim3 grid((unsigned) g.blocks);
+    if (whole) hipLaunchKernelGGL((k_norm_grad_units<T, L, P, true>), grid, dim3(kBlock), 0, s, a, g.row_step, parts);
+    else       hipLaunchKernelGGL((k_norm_grad_units<T, L, P, false>), grid, dim3(kBlock), 0, s, a, g.row_step, parts);
+}
+
+template <typename T>
+hipError_t launch_norm_typed(const gns_ctx* c, const NormArgs& a, const gns_norm* n, int32_t type, hipStream_t s)
+{
+    const int32_t width = a.x.width, w = width / a.groups, rows = a.count.rows;
+    if (by_units(n, width, type)) {
+        const UnitShape u = unit_shape(w, type);
+        const UnitGrid g = unit_grid(rows, a.groups, u.lanes, (int64_t) c->num_cus * 8);
+        const bool whole = w == u.lanes * u.pieces * kPiece<T>;
+        switch (u.lanes) {
+        case 1: launch_units<T, 1, 1>(a, g, whole, s); break;
+        case 2: launch_units<T, 2, 1>(a, g, whole, s); break;
+        case 4: launch_units<T, 4, 1>(a, g, whole, s); break;
+        case 8: launch_units<T, 8, 1>(a, g, whole, s); break;
+        case 16: launch_units<T, 16, 1>(a, g, whole, s); break;
+        case 32: launch_units<T, 32, 1>(a, g, whole, s); break;
+        case 64:
+            if (u.pieces == 1) launch_units<T, 64, 1>(a, g, whole, s);
+            else               launch_units<T, 64, 2>(a, g, whole, s);
+            break;
+        default:
+            if (u.pieces == 2)      launch_units<T, kBlock, 2>(a, g, whole, s);
+            else if (u.pieces == 4) launch_units<T, kBlock, 4>(a, g, whole, s);
+            else                    launch_units<T, kBlock, 8>(a, g, whole, s);
+        }
+        return hipGetLastError();
+    }
+    const Tiling t = tiling_of(c, width, a.groups, type, rows);
+    const int64_t segments = segment_count(n, rows);
+    const TiledSpace space = tiled_space(t, t.tiles, segments, width, a.groups, false);
+    float2* const parts = static_cast<float2*>(a.workspace);
+    float2* const stats = a.stats ? reinterpret_cast<float2*>(a.stats) : reinterpret_cast<float2*>(static_cast<char*>(a.workspace) + space.moments);
+    const dim3 grid((unsigned) t.tiles, (unsigned) t.slabs);
+    if (!segments) return hipSuccess;
+    hipLaunchKernelGGL((k_norm_parts<T>), grid, dim3(kBlock), 0, s, a, t, parts);
+    const int64_t units = segments * a.groups, most = (int64_t) c->num_cus * 32;
+    if (t.tiles * t.slabs > segments * 128)
+        hipLaunchKernelGGL((k_norm_join<T, kBlock, false>), dim3((unsigned) std::min(units, most)), dim3(kBlock), 0, s, a, t, parts, stats);
+    else
+        hipLaunchKernelGGL((k_norm_join<T, kWave, false>), dim3((unsigned) std::min((units + 3) / 4, most)), dim3(kBlock), 0, s, a, t, parts, stats);
+    hipLaunchKernelGGL((k_norm_apply<T>), grid, dim3(kBlock), 0, s, a, t, stats);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_grad_typed(const gns_ctx* c, const NormArgs& a, const gns_norm* n, int32_t type, hipStream_t s)
+{
+    const int32_t width = a.x.width, w = width / a.groups, rows = a.count.rows;
+    const bool columns_wanted = a.dgamma || a.dbeta;
+    const dim3 join((unsigned) ((width + kJoinColumns - 1) / kJoinColumns));
+    if (by_units(n, width, type)) {
+        const UnitShape u = unit_shape(w, type);
+        const UnitGrid g = unit_grid(rows, a.groups, u.lanes, unit_grad_blocks(c, rows, a.groups, u.lanes));
+        const bool whole = w == u.lanes * u.pieces * kPiece<T>;
+        float2* const parts = columns_wanted ? static_cast<float2*>(a.workspace) : nullptr;
+        switch (u.lanes) {
+        case 1: launch_grad_units<T, 1, 1>(a, g, whole, parts, s); break;
+        case 2: launch_grad_units<T, 2, 1>(a, g, whole, parts, s); break;
+        case 4: launch_grad_units<T, 4, 1>(a, g, whole, parts, s); break;
+        case 8: launch_grad_units<T, 8, 1>(a, g, whole, parts, s); break;
+        case 16: launch_grad_units<T, 16, 1>(a, g, whole, parts, s); break;
+        case 32: launch_grad_units<T, 32, 1>(a, g, whole, parts, s); break;
+        case 64:
+            if (u.pieces == 1) launch_grad_units<T, 64, 1>(a, g, whole, parts, s);
+            else               launch_grad_units<T, 64, 2>(a, g, whole, parts, s);
+            break;
+        default:
+            if (u.pieces == 2)      launch_grad_units<T, kBlock, 2>(a, g, whole, parts, s);
+            else if (u.pieces == 4) launch_grad_units<T, kBlock, 4>(a, g, whole, parts, s);
+            else                    launch_grad_units<T, kBlock, 8>(a, g, whole, parts, s);
+        }
+        if (columns_wanted)
+            hipLaunchKernelGGL(k_norm_columns, join, dim3(kBlock), 0, s, parts, unit_parts(g, a.groups, u.lanes), a.count, 0, width, a.dgamma, a.dbeta);
+        return hipGetLastError();
+    }
+    const Tiling t = tiling_of(c, width, a.groups, type, rows);
+    const int64_t segments = segment_count(n, rows);
+    const TiledSpace space = tiled_space(t, t.tiles, segments, width, a.groups, true);
+    char* const at = static_cast<char*>(a.workspace);
+    float2* const parts = reinterpret_cast<float2*>(at + space.parts);
+    float2* const moments = reinterpret_cast<float2*>(at + space.moments);
+    float2* const columns = reinterpret_cast<float2*>(at + space.columns);
+    const dim3 grid((unsigned) t.tiles, (unsigned) t.slabs);
+    hipLaunchKernelGGL((k_norm_grad_parts<T>), grid, dim3(kBlock), 0, s, a, t, a.out.data ? parts : nullptr, columns_wanted ? columns : nullptr);
+    if (columns_wanted)
+        hipLaunchKernelGGL(k_norm_columns, join, dim3(kBlock), 0, s, columns, (int64_t) 0, a.count, t.tile_rows, width, a.dgamma, a.dbeta);
+    if (a.out.data && segments) {
+        const int64_t units = segments * a.groups, most = (int64_t) c->num_cus * 32;
+        if (t.tiles * t.slabs > segments * 128)
+            hipLaunchKernelGGL((k_norm_join<T, kBlock, true>), dim3((unsigned) std::min(units, most)), dim3(kBlock), 0, s, a, t, parts, moments);
+        else
+            hipLaunchKernelGGL((k_norm_join<T, kWave, true>), dim3((unsigned) std::min((units + 3) / 4, most)), dim3(kBlock), 0, s, a, t, parts, moments);
+        hipLaunchKernelGGL((k_norm_grad_apply<T>), grid, dim3(kBlock), 0, s, a, t, moments);
+    }
+    return hipGetLastError();
+}
+
+gns_norm norm_of(const NormArgs& a)
+{
+    return gns_norm{a.segments, a.gamma, a.beta, a.num_segments, a.segment_rows, a.groups, a.activation, a.eps};
+}
+
+hipError_t fill_zero(float* p, size_t n, hipStream_t s) { return p && n ? launch_fill_u32(reinterpret_cast<uint32_t*>(p), n, 0, s) : hipSuccess; }
+
+}  // namespace
+
+size_t norm_need(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type, int32_t rows, bool backward)
+{
+    return need_of(c, width, n, type, rows, backward);
+}
+
+size_t norm_workspace(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t rows, bool backward)
+{
+    return std::max(most_of(c, width, n, GNS_FP32, rows, backward), most_of(c, width, n, GNS_BF16, rows, backward));
+}
+
+hipError_t launch_norm(const gns_ctx* c, const NormArgs& a, int32_t type, hipStream_t s)
+{
+    const gns_norm n = norm_of(a);
+    if (a.count.rows == 0)        // segments without rows
+        return a.segments ? fill_zero(a.stats, (size_t) 2 * a.num_segments * a.groups, s) : hipSuccess;
+    return type == GNS_FP32 ? launch_norm_typed<float>(c, a, &n, type, s) : launch_norm_typed<Bf16>(c, a, &n, type, s);
+}
+
+hipError_t launch_norm_backward(const gns_ctx* c, const NormArgs& a, int32_t type, hipStream_t s)
+{
+    const gns_norm n = norm_of(a);
+    if (a.count.rows == 0) {
+        const hipError_t e = fill_zero(a.dgamma, (size_t) a.x.width, s);
+        return e != hipSuccess ? e : fill_zero(a.dbeta, (size_t) a.x.width, s);
+    }
+    return type == GNS_FP32 ? launch_grad_typed<float>(c, a, &n, type, s) : launch_grad_typed<Bf16>(c, a, &n, type, s);
+}
+
+}  // namespace gns

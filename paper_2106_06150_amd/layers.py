@@ -1,0 +1,163 @@
+"""ctypes binding of include/gns_layers.h (argument marshalling only): group norm with an activation and its backward pass,
+orthogonalised updates of weights, the update step in 8-bit floats.
+
+Matrices of floats, row counts, workspaces and errors are as in learn.py.
+"""
+import ctypes
+
+import torch
+
+from .binding import _check, _stream_ptr, lib
+from .learn import _flat, _rows, _space, alloc_workspace, gns_rows  # noqa: F401
+
+GNS_ACT_NONE, GNS_ACT_RELU, GNS_ACT_SILU, GNS_ACT_GELU = 0, 1, 2, 3
+GNS_MAX_SEGMENTS = 1 << 24
+GNS_ORTHOGONAL_MAX = 32768
+GNS_MAX_STEPS = 16
+GNS_FP8_BLOCK = 128
+GNS_FP8_MAX_K = 1 << 20
+GNS_STAGE_NORM, GNS_STAGE_ORTHOGONAL, GNS_STAGE_FP8 = 26, 27, 28
+
+EXPORTED = ["gns_group_norm", "gns_group_norm_workspace_bytes", "gns_group_norm_backward",
+            "gns_group_norm_backward_workspace_bytes", "gns_orthogonal_update", "gns_orthogonal_update_workspace_bytes",
+            "gns_quantize_fp8", "gns_dense_fp8", "gns_sage_dense_fp8", "gns_sage_dense_fp8_workspace_bytes"]
+
+
+class gns_norm(ctypes.Structure):
+    _fields_ = [("segments_dev", ctypes.c_void_p), ("gamma_dev", ctypes.c_void_p), ("beta_dev", ctypes.c_void_p),
+                ("num_segments", ctypes.c_int32), ("segment_rows", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class gns_orthogonal(ctypes.Structure):
+    _fields_ = [("mu", ctypes.c_float), ("nesterov", ctypes.c_int32), ("eps", ctypes.c_float), ("keep", ctypes.c_float),
+                ("rate", ctypes.c_float), ("steps", ctypes.c_int32), ("coefficients", ctypes.c_float * 3 * GNS_MAX_STEPS)]
+
+
+def _declare():
+    vp, i32, size = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    R, N, O = ctypes.POINTER(gns_rows), ctypes.POINTER(gns_norm), ctypes.POINTER(gns_orthogonal)
+    for name, args in dict(
+            gns_group_norm=[vp, R, N, R, vp, i32, vp, size, vp],
+            gns_group_norm_backward=[vp, R, R, N, vp, R, vp, vp, i32, vp, size, vp],
+            gns_orthogonal_update=[vp, R, R, O, R, R, R, i32, vp, size, vp],
+            gns_quantize_fp8=[vp, R, R, vp, vp, i32, vp],
+            gns_dense_fp8=[vp, vp, vp, i32, vp, vp, vp, i32, R, i32, vp],
+            gns_sage_dense_fp8=[vp, R, R, vp, vp, vp, i32, R, i32, vp, size, vp]).items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = ctypes.c_int
+    for name, args in dict(gns_group_norm_workspace_bytes=[vp, i32, N, i32],
+                           gns_group_norm_backward_workspace_bytes=[vp, i32, N, i32],
+                           gns_orthogonal_update_workspace_bytes=[vp, i32, i32],
+                           gns_sage_dense_fp8_workspace_bytes=[vp, i32, i32]).items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = size
+
+
+_declare()
+
+
+class Norm:
+    """A gns_norm and the tensors it points to: segments int32 [num_segments + 1] or None (then of segment_rows rows each),
+    gamma and beta fp32 [width] or None."""
+
+    def __init__(self, groups, segments=None, segment_rows=1, activation=GNS_ACT_NONE, eps=1e-5, gamma=None, beta=None):
+        self.segments, self.gamma, self.beta = segments, gamma, beta
+        self.struct = gns_norm(_flat(segments, torch.int32, 1), _flat(gamma, torch.float32, 0), _flat(beta, torch.float32, 0),
+                               0 if segments is None else segments.numel() - 1, segment_rows, groups, activation, eps)
+
+    def segment_count(self, num_rows):
+        if self.segments is not None:
+            return self.segments.numel() - 1
+        return (max(num_rows, 0) + self.struct.segment_rows - 1) // max(self.struct.segment_rows, 1)
+
+    def _checked(self, width):
+        assert all(t is None or t.numel() == width for t in (self.gamma, self.beta))
+        return self.struct
+
+
+class Orthogonal:
+    """A gns_orthogonal: coefficients are `steps` triples (a, b, c)."""
+
+    def __init__(self, coefficients, mu=0.0, nesterov=False, eps=1e-7, keep=1.0, rate=1.0):
+        coefficients = [tuple(c) for c in coefficients]
+        assert len(coefficients) <= GNS_MAX_STEPS and all(len(c) == 3 for c in coefficients)
+        self.struct = gns_orthogonal(mu, 1 if nesterov else 0, eps, keep, rate, len(coefficients))
+        for i, c in enumerate(coefficients):
+            self.struct.coefficients[i][:] = c
+
+
+def fp8_stride(k):
+    """Bytes between rows in 8-bit floats of k columns."""
+    return (k + 127) // 128 * 128
+
+
+def fp8_exponents(k):
+    """Exponent bytes of a row of k columns."""
+    return (k + 511) // 512 * 4
+
+
+def gns_group_norm_workspace_bytes(ctx, width, norm, num_rows):
+    return lib.gns_group_norm_workspace_bytes(ctx, width, norm._checked(width), num_rows)
+
+
+def gns_group_norm(ctx, x, norm, out, stats, num_rows, workspace=None, stream=None):
+    """stats fp32 [segments, groups, 2] or None; out may be x itself."""
+    space, nbytes = _space(workspace)
+    cells = 2 * norm.segment_count(num_rows) * norm.struct.groups
+    _check(lib.gns_group_norm(ctx, _rows(x, num_rows), norm._checked(x.shape[1]), _rows(out, num_rows), _flat(stats, torch.float32, cells),
+                              num_rows, space, nbytes, _stream_ptr(stream)), ctx)
+
+
+def gns_group_norm_backward_workspace_bytes(ctx, width, norm, num_rows):
+    return lib.gns_group_norm_backward_workspace_bytes(ctx, width, norm._checked(width), num_rows)
+
+
+def gns_group_norm_backward(ctx, d_out, x, norm, stats, dx, dgamma, dbeta, num_rows, workspace=None, stream=None):
+    """stats as gns_group_norm wrote them; dx, dgamma and dbeta (fp32 [width]) may be None; dx may be d_out or x itself."""
+    space, nbytes = _space(workspace)
+    width = x.shape[1]
+    cells = 2 * norm.segment_count(num_rows) * norm.struct.groups
+    _check(lib.gns_group_norm_backward(ctx, _rows(d_out, num_rows), _rows(x, num_rows), norm._checked(width), _flat(stats, torch.float32, cells),
+                                       _rows(dx, num_rows), _flat(dgamma, torch.float32, width), _flat(dbeta, torch.float32, width),
+                                       num_rows, space, nbytes, _stream_ptr(stream)), ctx)
+
+
+def gns_orthogonal_update_workspace_bytes(ctx, width, num_rows):
+    return lib.gns_orthogonal_update_workspace_bytes(ctx, width, num_rows)
+
+
+def gns_orthogonal_update(ctx, grad, momentum, how, w, momentum_out, out, num_rows, workspace, stream=None):
+    """grad, w, out [rows, width]; momentum with momentum_out, or both None; w may be None.  momentum_out may be momentum, out
+    may be w or grad."""
+    space, nbytes = _space(workspace)
+    _check(lib.gns_orthogonal_update(ctx, _rows(grad, num_rows), _rows(momentum, num_rows), how.struct, _rows(w, num_rows),
+                                     _rows(momentum_out, num_rows), _rows(out, num_rows), num_rows, space, nbytes, _stream_ptr(stream)), ctx)
+
+
+def gns_quantize_fp8(ctx, x1, x2, q, exponents, num_rows, stream=None):
+    """q uint8 [rows, fp8_stride(k)], exponents uint8 [rows, fp8_exponents(k)]; x2 may be None."""
+    k = x1.shape[1] + (0 if x2 is None else x2.shape[1])
+    rows = max(num_rows, 0)
+    _check(lib.gns_quantize_fp8(ctx, _rows(x1, num_rows), _rows(x2, num_rows), _flat(q, torch.uint8, rows * fp8_stride(k)),
+                                _flat(exponents, torch.uint8, rows * fp8_exponents(k)), num_rows, _stream_ptr(stream)), ctx)
+
+
+def gns_dense_fp8(ctx, q, exponents, k, wq, w_exponents, bias, relu, out, num_rows, stream=None):
+    """wq uint8 [out.shape[1], fp8_stride(k)], w_exponents uint8 [out.shape[1], fp8_exponents(k)], bias fp32 or None."""
+    n, rows = out.shape[1], max(num_rows, 0)
+    _check(lib.gns_dense_fp8(ctx, _flat(q, torch.uint8, rows * fp8_stride(k)), _flat(exponents, torch.uint8, rows * fp8_exponents(k)), k,
+                             _flat(wq, torch.uint8, n * fp8_stride(k)), _flat(w_exponents, torch.uint8, n * fp8_exponents(k)),
+                             _flat(bias, torch.float32, n), 1 if relu else 0, _rows(out, num_rows), num_rows, _stream_ptr(stream)), ctx)
+
+
+def gns_sage_dense_fp8_workspace_bytes(ctx, k, num_rows):
+    return lib.gns_sage_dense_fp8_workspace_bytes(ctx, k, num_rows)
+
+
+def gns_sage_dense_fp8(ctx, x1, x2, wq, w_exponents, bias, relu, out, num_rows, workspace, stream=None):
+    n, k = out.shape[1], x1.shape[1] + (0 if x2 is None else x2.shape[1])
+    space, nbytes = _space(workspace)
+    _check(lib.gns_sage_dense_fp8(ctx, _rows(x1, num_rows), _rows(x2, num_rows), _flat(wq, torch.uint8, n * fp8_stride(k)),
+                                  _flat(w_exponents, torch.uint8, n * fp8_exponents(k)), _flat(bias, torch.float32, n), 1 if relu else 0,
+                                  _rows(out, num_rows), num_rows, space, nbytes, _stream_ptr(stream)), ctx)
