@@ -159,7 +159,7 @@ gns_status gns_group_norm_backward(gns_ctx* ctx, const gns_rows* d_out, const gn
 size_t gns_orthogonal_update_workspace_bytes(const gns_ctx* ctx, int32_t width, int32_t num_rows)
 {
     if (!ctx || width < 1 || width > GNS_ORTHOGONAL_MAX || num_rows < 1 || num_rows > GNS_ORTHOGONAL_MAX) return 0;
-    return align256(orthogonal_workspace(width, num_rows));
+    return align256(orthogonal_workspace(ctx, width, num_rows));
 }
 
 gns_status gns_orthogonal_update(gns_ctx* ctx, const gns_rows* grad, const gns_rows* momentum, const gns_orthogonal* how,
@@ -198,7 +198,7 @@ gns_status gns_orthogonal_update(gns_ctx* ctx, const gns_rows* grad, const gns_r
     GNS_REQUIRE_OF_ROWS(out->data != grad->data || same_rows(out, grad), "out may only be the gradient's own rows");
     if (num_rows == 0) return GNS_OK;
     GNS_REQUIRE(workspace && !misaligned(workspace, 256), "workspace is null or not 256-byte aligned");
-    if (workspace_bytes < orthogonal_workspace(grad->width, num_rows)) return ctx_fail(ctx, GNS_ECAPACITY, "workspace is too small");
+    if (workspace_bytes < orthogonal_workspace(ctx, grad->width, num_rows)) return ctx_fail(ctx, GNS_ECAPACITY, "workspace is too small");
     a.grad = as_const(grad); a.grad_type = grad->type;
     a.out = as_mut(out); a.out_type = out->type;
     a.rows = num_rows;

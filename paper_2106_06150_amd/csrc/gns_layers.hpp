@@ -57,7 +57,7 @@ size_t norm_workspace(const gns_ctx* c, int32_t width, const gns_norm* n, int32_
 hipError_t launch_norm(const gns_ctx* c, const NormArgs& a, int32_t type, hipStream_t s);
 hipError_t launch_norm_backward(const gns_ctx* c, const NormArgs& a, int32_t type, hipStream_t s);
 // gns_orthogonal.hip
-size_t orthogonal_workspace(int32_t width, int32_t rows);
+size_t orthogonal_workspace(const gns_ctx* c, int32_t width, int32_t rows);
 hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStream_t s);
 // gns_fp8.hip
 hipError_t launch_quantize_fp8(const gns_ctx* c, const QuantizeFp8Args& a, int32_t type, hipStream_t s);

@@ -5,6 +5,7 @@
 // kept as it is and turned, the others are symmetric.
 #include "gns_layers.hpp"
 #include <algorithm>
+#include <type_traits>
 
 namespace gns {
 
@@ -12,7 +13,7 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr float kUp = 4096.f, kDown = 1.f / 4096.f;
-constexpr int kPad = 128;                     // rows and columns of the matrices in terms are multiples of it, zeros behind the values
+constexpr int kPad = 64;                      // rows and columns of the matrices in terms are multiples of it, zeros behind the values
 constexpr int kTermBlock = 32;                // values of a row whose first terms, then second terms lie together: 128 bytes
 
 // Where the terms of 8 values of a row begin: c a multiple of 8; the second terms lie 64 bytes behind the first.
@@ -144,8 +145,18 @@ constexpr int kSpread = 64;
 // X in terms, as it is and turned, a tile of 64 x 64 a block.
 __global__ void __launch_bounds__(kBlock) k_spread(SpreadArgs a)
 {
+    constexpr int kTurns = kSpread * kSpread / kBlock;
     __shared__ float s_tile[kSpread][kSpread + 1];
     __shared__ double s_sum[kBlock / kWave];
+    // the tile as u has it, on its way while the norm is worked out
+    const int32_t x0 = (int32_t) blockIdx.y * kSpread, y0 = (int32_t) blockIdx.x * kSpread;      // in X: rows, columns
+    const int32_t u_row = a.tall ? y0 : x0, u_column = a.tall ? x0 : y0;
+    float u[kTurns];
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+        const int32_t r = u_row + (t * kBlock + (int) threadIdx.x) / kSpread, c = u_column + (int) threadIdx.x % kSpread;
+        u[t] = r < a.rows && c < a.width ? a.u[(int64_t) r * a.pitch + c] : 0.f;
+    }
     double sum = 0.0;
     for (int32_t i = (int32_t) threadIdx.x; i < a.sum_count; i += kBlock) sum += a.sums[i];
     for (int m = 1; m < kWave; m *= 2) sum += __shfl_xor(sum, m);
@@ -153,13 +164,10 @@ __global__ void __launch_bounds__(kBlock) k_spread(SpreadArgs a)
     __syncthreads();
     const double norm = sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
     const double inverse = !(norm < (double) __builtin_inff()) ? (double) quiet_nan() : norm > 0.0 ? (double) kUp / (norm + a.eps) : 0.0;
-    // the tile as u has it
-    const int32_t x0 = (int32_t) blockIdx.y * kSpread, y0 = (int32_t) blockIdx.x * kSpread;      // in X: rows, columns
-    const int32_t u_row = a.tall ? y0 : x0, u_column = a.tall ? x0 : y0;
-    for (int i = (int) threadIdx.x; i < kSpread * kSpread; i += kBlock) {
-        const int32_t r = i / kSpread, c = i % kSpread;
-        float v = 0.f;
-        if (u_row + r < a.rows && u_column + c < a.width) v = (float) ((double) a.u[(int64_t) (u_row + r) * a.pitch + u_column + c] * inverse);
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+        const int r = (t * kBlock + (int) threadIdx.x) / kSpread, c = (int) threadIdx.x % kSpread;
+        const float v = (float) ((double) u[t] * inverse);
         if (a.tall) s_tile[c][r] = v;
         else        s_tile[r][c] = v;
     }
@@ -185,6 +193,8 @@ struct ProductArgs {
     const char* same;             // kPoly: A; kStep, kLast: X, of the shape of P
     char* to;                     // kGram: P; kPoly: b A + c P; kStep: a X + P
     char* turned;                 // kStep: the same turned
+    int32_t whole_tiles, parts;   // tiles behind so many are summed in so many parts
+    float* sums;                  // of parts
     float a, b, c;
     // kLast: out = keep * w + rate * (a X + P), turned back if tall
     ConstRows w;
@@ -193,130 +203,259 @@ struct ProductArgs {
     float keep, rate;
 };
 
-// k_product: 128 x 128 of P a block, 64 x 64 a wave, products of 32 x 32 x 16.  A stage is 32 of k: 128 bytes of a row, both terms, from
-// memory straight to LDS, where chunk c of 16 bytes of row r lies at c ^ (r & 7).  Symmetric products are made for the tiles
-// on and below the diagonal and written to both places.
-constexpr int kSide = 128, kStageBytes = 2 * kSide * 128, kOutPitch = kSide + 4;
-
-template <int kWhat>
-__global__ void __launch_bounds__(kBlock, 2) k_product(ProductArgs a)
+// 32 rows of P from row0 on, WN columns from column0 on, in a wave's accumulators, become what the launch makes of them: by way of a
+// strip of LDS of the wave's own, by rows, then by columns.  once: P's element is not wanted in the mirrored place too.
+template <int WN> constexpr int kStripPitch = WN + 4;
+template <int kWhat, int WN>
+__device__ __forceinline__ void finish_strip(const ProductArgs& a, float* strip, const float16v (&acc)[WN / 32], int32_t row0, int32_t column0, bool once)
 {
-    constexpr bool kSymmetric = kWhat == kGram || kWhat == kPoly;
-    __shared__ __attribute__((aligned(128))) char s_stage[kSide * kOutPitch * 4 > 2 * kStageBytes ? kSide * kOutPitch * 4 : 2 * kStageBytes];
-    int32_t tm, tn;
-    if (kSymmetric) {
-        // block b is the pair (tm, tn), tn <= tm, in the order of rows
-        const int32_t b = (int32_t) blockIdx.x;
-        tm = (int32_t) ((sqrtf(8.f * (float) b + 1.f) - 1.f) * 0.5f);
-        while (tm * (tm + 1) / 2 > b) --tm;
-        while ((tm + 1) * (tm + 2) / 2 <= b) ++tm;
-        tn = b - tm * (tm + 1) / 2;
-    } else {
-        tile_of(xcd_run((int32_t) blockIdx.x, (int32_t) gridDim.x), a.m / kSide, a.n / kSide, &tm, &tn);
-    }
-    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
-    const int64_t row_bytes = (int64_t) a.k * 4;
-    // this wave's pieces of a stage: 8 rows each, 8 of either side; a lane's 16 bytes come from where its place in LDS has them
-    const int32_t piece_row = lane >> 3, chunk = (lane & 7) ^ piece_row;
-    const char* from = (wave < 2 ? a.left + ((int64_t) tm * kSide + wave * 64) * row_bytes : a.right + ((int64_t) tn * kSide + (wave - 2) * 64) * row_bytes) +
-                       piece_row * row_bytes + chunk * 16;
-    auto fetch = [&](int buffer, int32_t step) {
+    constexpr int kPitch = kStripPitch<WN>, kChunks = WN / 8;
+    const int lane = opaque_lane_id(), l32 = lane & 31, kh = lane >> 5;
+    const bool columns_too = kWhat == kLast ? a.tall : kWhat == kStep || !once;
+    // element v of lane l is row 8 * (v / 4) + 4 * (l / 32) + v % 4, column l % 32; 2^12 P
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void*) (from + (int64_t) step * 128 + (int64_t) i * 8 * row_bytes),
-                (__attribute__((address_space(3))) void*) (s_stage + buffer * kStageBytes + (wave * 64 + i * 8) * 128), 16, 0, 0);
-    };
-    const int wm = wave / 2 * 64, wn = wave % 2 * 64, l32 = lane & 31, kh = lane >> 5;
-    float16v acc[2][2];
+    for (int j = 0; j < WN / 32; ++j)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+        for (int v = 0; v < 16; ++v) strip[(8 * (v / 4) + 4 * kh + v % 4) * kPitch + j * 32 + l32] = acc[j][v] * kDown;
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-    const int32_t steps = a.k / kTermBlock;
-    fetch(0, 0);
-    for (int32_t step = 0; step < steps; ++step) {
-        __syncthreads();          // this stage has come, and the one before has been read
-        if (step + 1 < steps) fetch((step + 1) & 1, step + 1);
-        const char* at = s_stage + (step & 1) * kStageBytes;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            half8 x[2][2], y[2][2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int32_t place = ((t * 4 + s * 2 + kh) ^ (l32 & 7)) * 16;
-                    x[i][t] = *reinterpret_cast<const half8*>(at + (wm + i * 32 + l32) * 128 + place);
-                    y[i][t] = *reinterpret_cast<const half8*>(at + (kSide + wn + i * 32 + l32) * 128 + place);
-                }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], y[j][0], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[j][1], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[j][0], acc[i][j], 0, 0, 0);
-                }
-        }
-    }
-    __syncthreads();
-    float (*s_out)[kOutPitch] = reinterpret_cast<float (*)[kOutPitch]>(s_stage);
-    // element v of lane l is row 8 * (v / 4) + 4 * (l / 32) + v % 4, column l % 32
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s_out[wm + i * 32 + 8 * (v / 4) + 4 * kh + v % 4][wn + j * 32 + l32] = acc[i][j][v] * kDown;
-    __syncthreads();
-    // s_out holds 2^12 P; by rows
-    const int32_t m0 = tm * kSide, n0 = tn * kSide;
-    for (int i = (int) threadIdx.x; i < kSide * kSide / 8; i += kBlock) {
-        const int32_t r = i / (kSide / 8), c = i % (kSide / 8) * 8;
+    for (int p = 0; p < WN / 16; ++p) {
+        const int r = p * (kWave / kChunks) + lane / kChunks, c = lane % kChunks * 8;
         float v[8], x[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = s_out[r][c + k];
-        const int64_t place = terms_at(m0 + r, n0 + c, a.n);
+        for (int k = 0; k < 8; ++k) v[k] = strip[r * kPitch + c + k];
+        const int64_t place = terms_at(row0 + r, column0 + c, a.n);
         if (kWhat != kGram) {
             load_terms(a.same + place, x);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = kWhat == kPoly ? a.b * x[k] + a.c * v[k] : a.a * x[k] + v[k];
+            if (columns_too)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s_out[r][c + k] = v[k];
+                for (int k = 0; k < 8; ++k) strip[r * kPitch + c + k] = v[k];
         }
         if (kWhat != kLast) {
             store_terms(a.to + place, v);
-        } else if (!a.tall && m0 + r < a.rows && n0 + c < a.out.width) {
+        } else if (!a.tall && row0 + r < a.rows && column0 + c < a.out.width) {
             float w[8];
-            if (a.w.data) load_eight(a.w, a.w_type, m0 + r, n0 + c, w);
+            if (a.w.data) load_eight(a.w, a.w_type, row0 + r, column0 + c, w);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = (a.w.data ? a.keep * w[k] : 0.f) + a.rate * (v[k] * kDown);
-            store_eight(a.out, a.out_type, m0 + r, n0 + c, v);
+            store_eight(a.out, a.out_type, row0 + r, column0 + c, v);
         }
     }
-    if (kWhat == kLast ? !a.tall : kSymmetric && tm == tn) return;
-    __syncthreads();
-    // and by columns
-    for (int i = (int) threadIdx.x; i < kSide * kSide / 8; i += kBlock) {
-        const int32_t r = i % kSide, c = i / kSide * 8;        // row of the turned tile
+    __builtin_amdgcn_wave_barrier();
+    if (!columns_too) return;
+#pragma unroll
+    for (int p = 0; p < WN / 16; ++p) {
+        const int r = p * 16 + lane / 4, c = lane % 4 * 8;    // of the turned strip
         float v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = s_out[c + k][r];
+        for (int k = 0; k < 8; ++k) v[k] = strip[(c + k) * kPitch + r];
         if (kWhat == kLast) {
-            if (n0 + r < a.rows && m0 + c < a.out.width) {
+            if (column0 + r < a.rows && row0 + c < a.out.width) {
                 float w[8];
-                if (a.w.data) load_eight(a.w, a.w_type, n0 + r, m0 + c, w);
+                if (a.w.data) load_eight(a.w, a.w_type, column0 + r, row0 + c, w);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] = (a.w.data ? a.keep * w[k] : 0.f) + a.rate * (v[k] * kDown);
-                store_eight(a.out, a.out_type, n0 + r, m0 + c, v);
+                store_eight(a.out, a.out_type, column0 + r, row0 + c, v);
             }
         } else {
-            store_terms((kSymmetric ? a.to : a.turned) + terms_at(n0 + r, m0 + c, a.m), v);
+            store_terms((kWhat == kStep ? a.turned : a.to) + terms_at(column0 + r, row0 + c, a.m), v);
         }
     }
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Tile t of P.  Of a symmetric one, the pairs (tm, tn), tn <= tm: bands of eight rows of tiles, column after column, so that what runs
+// together on an XCD shares rows.
+template <int kWhat, int BM, int BN>
+__device__ __forceinline__ void tile_at(const ProductArgs& a, int32_t t, int32_t* tm, int32_t* tn)
+{
+    if (kWhat == kGram || kWhat == kPoly) {
+        // before band b there are 32 b b + 4 b tiles
+        int32_t b = (int32_t) ((sqrtf(16.f + 128.f * (float) t) - 4.f) * (1.f / 64.f));
+        while (32 * b * b + 4 * b > t) --b;
+        while (32 * (b + 1) * (b + 1) + 4 * (b + 1) <= t) ++b;
+        int32_t in = t - (32 * b * b + 4 * b), height = min(8, (a.m + BM - 1) / BM - 8 * b);
+        if (in < 8 * b * height) {
+            *tm = 8 * b + in % height;
+            *tn = in / height;
+            return;
+        }
+        in -= 8 * b * height;
+        int32_t c = 0;
+        for (; in >= height - c; ++c) in -= height - c;
+        *tm = 8 * b + c + in;
+        *tn = 8 * b + c;
+    } else {
+        tile_of(t, (a.m + BM - 1) / BM, (a.n + BN - 1) / BN, tm, tn);
+    }
+}
+
+__device__ __forceinline__ int turn_of(int row) { return row >> 1 & 7; }
+
+// k_product: BM x BN of P a block, WM x WN a wave, products of 32 x 32 x 16.  A stage is 32 of k (for each of KS groups of waves, whose sums
+// are joined at the end): 128 bytes of a row, both terms, which go from memory straight to LDS, chunk c of 16 bytes of row r to
+// c ^ turn_of(r), so that reads of the same chunk of sixteen rows spread over all 64 banks.  Fragments are read from LDS half a stage before they are multiplied, so a stage has been read when its first half
+// is multiplied: there the block's one barrier stands, and behind it the stage S later is fetched to the same place.
+// Symmetric products are made for the tiles on and below the diagonal and written to both places.
+template <int kWhat, int BM, int BN, int WM, int WN, int KS, int S>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, (BM / WM) * (BN / WN) * KS / 4) k_product(ProductArgs a)
+{
+    constexpr bool kSymmetric = kWhat == kGram || kWhat == kPoly;
+    constexpr int kGroup = (BM / WM) * (BN / WN), kWaves = kGroup * KS, kRows = BM + BN, kStage = kRows * 128 * KS;
+    constexpr int kLoads = kRows * KS / 8 / kWaves, MI = WM / 32, NI = WN / 32;
+    constexpr int kSums = MI * NI == 1 ? 3 : 1;               // a wave of one product at a time keeps a sum for each kind of terms
+    constexpr int kStrip = 32 * kStripPitch<WN> * 4;
+    static_assert(BM / 8 % kLoads == 0, "a wave fetches one side");
+    static_assert(kGroup * kStrip + (KS > 1 ? kGroup * kWave * 64 * MI * NI : 0) <= S * kStage, "what follows the products has their place");
+    __shared__ __attribute__((aligned(128))) char s_stage[S * kStage];
+    // blocks of whole tiles, then those of parts of the others
+    int32_t tile, part = -1, tm, tn;
+    if ((int32_t) blockIdx.x < a.whole_tiles) {
+        tile = xcd_run((int32_t) blockIdx.x, a.whole_tiles);
+    } else {
+        part = (int32_t) blockIdx.x - a.whole_tiles;
+        tile = a.whole_tiles + part / a.parts;
+    }
+    tile_at<kWhat, BM, BN>(a, tile, &tm, &tn);
+    const int32_t m0 = tm * BM, n0 = tn * BN;
+    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
+    const int group = wave / kGroup, w = wave % kGroup;
+    const int64_t row_bytes = (int64_t) a.k * 4;
+    const int32_t all = a.k / (32 * KS), step0 = part < 0 ? 0 : all * (part % a.parts) / a.parts;
+    const int32_t steps = part < 0 ? all : all * (part % a.parts + 1) / a.parts - step0;
+    // This wave's pieces of a stage: 8 rows each; a lane's 16 bytes come from where its place in LDS has them.  Rows past the last repeat it.
+    const int piece = wave * kLoads % (kRows / 8);
+    const bool right = piece * 8 >= BM;
+    const int32_t first = piece * 8 - (right ? BM : 0), last = (right ? a.n - n0 : a.m - m0) - 1;
+    const char* const base = (right ? a.right + (int64_t) n0 * row_bytes : a.left + (int64_t) m0 * row_bytes) + wave * kLoads / (kRows / 8) * 128 +
+                             (int64_t) step0 * (128 * KS);
+    uint32_t from[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+        from[i] = (uint32_t) min(first + i * 8 + (lane >> 3), last) * (uint32_t) row_bytes + (uint32_t) ((lane & 7) ^ turn_of((piece + i) * 8 + (lane >> 3))) * 16;
+    const char* next = base;
+    char* next_to = s_stage;
+    auto seek = [&](int32_t step, int buffer) {               // past the last: the last again
+        next = base + (int64_t) min(step, steps - 1) * (128 * KS);
+        next_to = s_stage + buffer * kStage + wave * kLoads * 1024;
+    };
+    auto fetch = [&](int i) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*) (next + from[i]),
+                                         (__attribute__((address_space(3))) void*) (next_to + i * 1024), 16, 0, 0);
+    };
+    const int wm = w / (BN / WN) * WM, wn = w % (BN / WN) * WN, l32 = lane & 31, kh = lane >> 5;
+    const char* const x_at = s_stage + (group * kRows + wm + l32) * 128;
+    const char* const y_at = s_stage + (group * kRows + BM + wn + l32) * 128;
+    half8 f[2][2 * (MI + NI)];                                // fragments of a half stage: first terms of the left and the right, then second terms
+    constexpr int kGets = 2 * (MI + NI);
+    auto get = [&](int set, int buffer, int i) {
+        const int t = i / (MI + NI), at = i % (MI + NI), place = ((t * 4 + set * 2 + kh) ^ turn_of(l32)) * 16 + buffer * kStage;
+        f[set][i] = *reinterpret_cast<const half8*>(at < MI ? x_at + at * 4096 + place : y_at + (at - MI) * 4096 + place);
+    };
+    float16v acc[kSums][MI][NI];
+#pragma unroll
+    for (int t = 0; t < kSums; ++t)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[t][i][j][v] = 0.f;
+    // the products of half a stage, and between them, one after the other, what else there is to do
+    auto multiply = [&](int set, auto&& other, int others) {
+        constexpr int kProducts = 3 * MI * NI;
+        constexpr int kEarly = kProducts > 8 ? kProducts * 3 / 4 : kProducts;      // the last products cover the last reads
+#pragma unroll
+        for (int m = 0; m < kProducts; ++m) {
+            const int t = m / (MI * NI), i = m / NI % MI, j = m % NI;
+            // small ones first
+            acc[t % kSums][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[set][(t == 0 ? MI + NI : 0) + i], f[set][(t == 1 ? MI + NI : 0) + MI + j],
+                                                                         acc[t % kSums][i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (m < kEarly) {
+#pragma unroll
+                for (int o = others * m / kEarly; o < others * (m + 1) / kEarly; ++o) other(o);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+#pragma unroll
+    for (int p = 0; p < S; ++p) {
+        seek(p, p);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) fetch(i);
+    }
+    auto come = [&](auto ahead) {                             // all stages but the last `ahead` have come, and the block's waves are here
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(decltype(ahead)::value * kLoads) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    come(std::integral_constant<int, S - 1>{});
+#pragma unroll
+    for (int i = 0; i < kGets; ++i) get(0, 0, i);
+    int buffer = 0;
+    for (int32_t step = 0; step < steps; ++step) {
+        const int after = buffer + 1 < S ? buffer + 1 : 0;
+        multiply(0, [&](int o) { get(1, buffer, o); }, kGets);
+        come(std::integral_constant<int, S - 2>{});
+        seek(step + S, buffer);
+        multiply(1, [&](int o) { if (o < kLoads) fetch(o); else get(0, after, o - kLoads); }, kGets + kLoads);
+        buffer = after;
+    }
+    come(std::integral_constant<int, 0>{});                   // what was fetched past the last has come too
+    float* const strip = reinterpret_cast<float*>(s_stage + w * kStrip);
+    if (KS > 1) {
+        float16v* const others = reinterpret_cast<float16v*>(s_stage + kGroup * kStrip) + (w * kWave + lane) * MI * NI;
+        if (group)
+#pragma unroll
+            for (int i = 0; i < MI * NI; ++i) others[i] = kSums == 3 ? acc[0][0][0] + acc[1][0][0] + acc[2][0][0] : acc[0][i / NI][i % NI];
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int i = 0; i < MI * NI; ++i) acc[0][i / NI][i % NI] += others[i];
+    }
+    if (kSums == 3) acc[0][0][0] += acc[1][0][0] + acc[2][0][0];
+    if (part >= 0) {                                          // as the accumulators lie; k_join goes on
+        float4* to = reinterpret_cast<float4*>(a.sums) + ((int64_t) part * kGroup + w) * (MI * NI * 4 * kWave) + lane;
+#pragma unroll
+        for (int i = 0; i < MI * NI * 4; ++i) {
+            const float16v& v = acc[0][i / 4 / NI][i / 4 % NI];
+            to[i * kWave] = make_float4(v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]);
+        }
+        return;
+    }
+    if (n0 + wn >= a.n) return;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+        if (m0 + wm + i * 32 < a.m) finish_strip<kWhat, WN>(a, strip, acc[0][i], m0 + wm + i * 32, n0 + wn, kSymmetric && tm == tn);
+}
+
+// The parts of tiles of 128 x 128, in their order, and what the launch makes of them: a wave for each 32 x 64.
+template <int kWhat>
+__global__ void __launch_bounds__(kWave) k_join(ProductArgs a)
+{
+    __shared__ __attribute__((aligned(16))) float s_strip[32 * kStripPitch<64>];
+    const int lane = (int) threadIdx.x;
+    const int32_t tile = (int32_t) blockIdx.x / 8, at = (int32_t) blockIdx.x % 8, w = at / 2, i = at % 2;
+    int32_t tm, tn;
+    tile_at<kWhat, 128, 128>(a, a.whole_tiles + tile, &tm, &tn);
+    const int32_t row0 = tm * 128 + w / 2 * 64 + i * 32, column0 = tn * 128 + w % 2 * 64;
+    if (row0 >= a.m || column0 >= a.n) return;
+    float16v acc[2];
+#pragma unroll 4
+    for (int32_t p = 0; p < a.parts; ++p) {
+        const float4* from = reinterpret_cast<const float4*>(a.sums) + (((int64_t) tile * a.parts + p) * 8 + at) * (8 * kWave) + lane;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float4 v = from[q * kWave];
+            const float of[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[q / 4][q % 4 * 4 + k] = p ? acc[q / 4][q % 4 * 4 + k] + of[k] : of[k];
+        }
+    }
+    finish_strip<kWhat, 64>(a, s_strip, acc, row0, column0, (kWhat == kGram || kWhat == kPoly) && tm == tn);
 }
 
 // No steps: out = keep * w + rate * X from X in terms.
@@ -337,11 +476,14 @@ __global__ void __launch_bounds__(kBlock) k_no_step(ProductArgs a, int32_t piece
 
 namespace {
 
+constexpr int32_t kMostParts = 16;
+constexpr size_t kPartBytes = 128 * 128 * 4;
+
 struct Space {
     int32_t short_side, long_side;
-    size_t sums, x, turned[2], gram, poly, all;       // where each begins; u lies where the second turned X will
+    size_t sums, x, turned[2], gram, poly, parts, all;        // where each begins; u lies where the second turned X will
 };
-Space space_of(int32_t width, int32_t rows)
+Space space_of(const gns_ctx* c, int32_t width, int32_t rows)
 {
     auto padded = [](int32_t n) { return (n + kPad - 1) / kPad * kPad; };
     Space s;
@@ -354,19 +496,69 @@ Space space_of(int32_t width, int32_t rows)
     s.turned[1] = s.turned[0] + large;
     s.gram = s.turned[1] + large;
     s.poly = s.gram + small;
-    s.all = s.poly + small;
+    s.parts = s.poly + small;
+    const int64_t tiles = ((int64_t) s.short_side + 127) / 128 * ((s.long_side + 127) / 128);
+    s.all = s.parts + (size_t) std::min<int64_t>(tiles * kMostParts, 2 * (int64_t) c->num_cus) * kPartBytes;
     return s;
 }
 
 }  // namespace
 
+// Tiles of a product of this side
+int64_t tiles_of(bool symmetric, int64_t m, int64_t n, int64_t side)
+{
+    m = (m + side - 1) / side;
+    n = (n + side - 1) / side;
+    return symmetric ? m * (m + 1) / 2 : m * n;
+}
+
+template <int kWhat, int BM, int BN, int WM, int WN, int KS, int S>
+void launch_tiles(const ProductArgs& a, int64_t blocks, hipStream_t s)
+{
+    hipLaunchKernelGGL((k_product<kWhat, BM, BN, WM, WN, KS, S>), dim3((unsigned) blocks), dim3((BM / WM) * (BN / WN) * KS * kWave), 0, s, a);
+}
+
+// Which tiles, and how the last of them are divided.  What a block takes is counted in stages of tiles of 128 (0.48 us): tiles of 64 take as
+// long for 64 of k, those of 256 three and a half times as long; a block's beginning and end take eight, of 256 forty; the sums of parts and
+// their join fourteen.
+template <int kWhat>
+void launch_product(const gns_ctx* c, ProductArgs a, hipStream_t s)
+{
+    constexpr bool kSymmetric = kWhat == kGram || kWhat == kPoly;
+    const int64_t cus = c->num_cus;
+    auto tiles = [&](int64_t side) { return tiles_of(kSymmetric, a.m, a.n, side); };
+    auto rounds = [&](int64_t t) { return (double) ((t + cus - 1) / cus); };
+    const double steps = a.k / 32;
+    const double small = rounds(tiles(64)) * (steps / 2 + 8), large = rounds(tiles(256)) * (3.5 * steps + 40);
+    const int64_t all = tiles(128), rest = all % cus;
+    double medium = rounds(all) * (steps + 8);
+    int32_t parts = 1;
+    for (int32_t p = 2; p <= kMostParts && p * 4 <= steps && rest * p <= 2 * cus; ++p) {
+        const double t = (double) (all / cus) * (steps + 8) + rounds(rest * p) * (steps / p + 8) + 14;
+        if (t < medium) { medium = t; parts = p; }
+    }
+    a.parts = 1;
+    if (small <= medium && small <= large) {
+        a.whole_tiles = (int32_t) tiles(64);
+        launch_tiles<kWhat, 64, 64, 32, 32, 2, 4>(a, a.whole_tiles, s);
+    } else if (large <= medium) {
+        a.whole_tiles = (int32_t) tiles(256);
+        launch_tiles<kWhat, 256, 256, 128, 64, 1, 2>(a, a.whole_tiles, s);
+    } else {
+        a.parts = parts;
+        a.whole_tiles = (int32_t) (parts > 1 ? all - rest : all);
+        launch_tiles<kWhat, 128, 128, 64, 64, 1, 4>(a, a.whole_tiles + (all - a.whole_tiles) * parts, s);
+        if (parts > 1) hipLaunchKernelGGL((k_join<kWhat>), dim3((unsigned) rest * 8), dim3(kWave), 0, s, a);
+    }
+}
+
 // A workspace for a matrix of so many rows serves those of fewer: a shorter side's padding is no longer.
-size_t orthogonal_workspace(int32_t width, int32_t rows) { return space_of(width, rows).all; }
+size_t orthogonal_workspace(const gns_ctx* c, int32_t width, int32_t rows) { return space_of(c, width, rows).all; }
 
 hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStream_t s)
 {
     const int32_t width = a.grad.width, rows = a.rows, pieces = (width + 7) / 8;
-    const Space space = space_of(width, rows);
+    const Space space = space_of(c, width, rows);
     char* const at = static_cast<char*>(a.workspace);
     const bool tall = rows > width;
     double* const sums = reinterpret_cast<double*>(at + space.sums);
@@ -379,7 +571,7 @@ hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStrea
     ProductArgs q = {};
     q.w = a.w; q.out = a.out; q.w_type = a.w_type; q.out_type = a.out_type; q.rows = rows; q.tall = tall;
     q.keep = a.how->keep; q.rate = a.how->rate;
-    const unsigned side = (unsigned) (space.short_side / kSide), whole = side * (unsigned) (space.long_side / kSide);
+    q.sums = reinterpret_cast<float*>(at + space.parts);
     int32_t turn = 0;
     for (int32_t i = 0; i < a.how->steps; ++i) {
         const float* f = a.how->coefficients[i];
@@ -388,16 +580,16 @@ hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStrea
         g.left = g.right = at + space.x;
         g.m = g.n = space.short_side; g.k = space.long_side;
         g.to = at + space.gram;
-        hipLaunchKernelGGL((k_product<kGram>), dim3(side * (side + 1) / 2), dim3(kBlock), 0, s, g);
+        launch_product<kGram>(c, g, s);
         g.left = g.right = g.same = at + space.gram;
         g.k = space.short_side;
         g.to = at + space.poly;
-        hipLaunchKernelGGL((k_product<kPoly>), dim3(side * (side + 1) / 2), dim3(kBlock), 0, s, g);
+        launch_product<kPoly>(c, g, s);
         g.left = at + space.poly; g.right = at + space.turned[turn]; g.same = at + space.x;
         g.n = space.long_side;
         g.to = at + space.x; g.turned = at + space.turned[1 - turn];
-        if (i + 1 < a.how->steps) hipLaunchKernelGGL((k_product<kStep>), dim3(whole), dim3(kBlock), 0, s, g);
-        else                      hipLaunchKernelGGL((k_product<kLast>), dim3(whole), dim3(kBlock), 0, s, g);
+        if (i + 1 < a.how->steps) launch_product<kStep>(c, g, s);
+        else                      launch_product<kLast>(c, g, s);
         turn = 1 - turn;
     }
     if (!a.how->steps) {
