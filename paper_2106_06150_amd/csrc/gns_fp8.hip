@@ -145,21 +145,23 @@ __global__ void __launch_bounds__(kBlock) k_quantize_fp8(QuantizeFp8Args a)
     }
 }
 
-constexpr int kStepBytes = 64;                // k of a stage
+// k_fp8_tiles: BM x BN outputs a block, WM x WN a wave.  A stage is 128 of k, a block of columns: 128 bytes of a row go from memory straight
+// to LDS, chunk c of 16 bytes of row r to c ^ turn_of(r), so that reads of the same chunk of sixteen rows spread over all 64 banks.  Half a stage
+// is multiplied (products of 32 x 32 x 64, or four of bf16 of 32 x 32 x 16) while the next half's fragments are read; a stage has been
+// read when its first half is multiplied: there the block's one barrier stands, and behind it the stage S later is fetched to the same
+// place.  A lane's 32 bytes are any chunks that both factors share, as they have one exponent.  The weights are the products' left factor, so that a
+// lane holds four consecutive outputs of a row.  Exponents come as words of four stages, as many ahead.
+__device__ __forceinline__ int turn_of(int row) { return row >> 1 & 7; }
 
-// k_fp8_tiles: BM x BN outputs a block, WM x WN a wave, products of 32 x 32 x 64.  A stage of 64 k of the rows and weights is read two
-// stages before it is written to LDS, and written two before it is multiplied; one barrier a stage.  Chunk c of 16 bytes of
-// row r lies at c ^ row_turn(r) of the row, so that reads of the same chunk of eight or sixteen rows spread over all banks.  A lane's 32
-// bytes of a product are chunks l / 32 and 2 + l / 32: any order does that both factors share, as they have one exponent.  The weights are the
-// products' left factor, so that a lane holds four consecutive outputs of a row.  Exponents are read as words of four blocks, 512 k ahead.
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, int S>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, 2) k_fp8_tiles(DenseFp8Args a, int32_t m_tiles, int32_t n_tiles)
 {
-    constexpr int kWaves = (BM / WM) * (BN / WN), kLoads = (BM + BN) / 16 / kWaves;     // of 16 rows, by a wave and stage
-    constexpr int MI = WM / 32, NI = WN / 32, kStage = (BM + BN) * 4;
+    constexpr int kWaves = (BM / WM) * (BN / WN), kLoads = (BM + BN) / 8 / kWaves;      // of 8 rows, by a wave and stage
+    constexpr int MI = WM / 32, NI = WN / 32, kStage = (BM + BN) * 128;
     constexpr bool kPrecise = sizeof(T) == 4;
-    static_assert((BM + BN) / 16 % kWaves == 0 && BM / 16 % kLoads == 0, "a wave loads whole pieces of one side");
-    __shared__ int4v s_stage[3 * kStage];
+    static_assert((BM + BN) / 8 % kWaves == 0 && BM / 8 % kLoads == 0, "a wave loads whole pieces of one side");
+    __shared__ __attribute__((aligned(128))) char s_stage[S * kStage];
+    __shared__ int s_scale[2][BM + BN];
     __shared__ float s_bias[BN];
     const int32_t rows = a.count.get(), n = a.out.width;
     const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
@@ -170,56 +172,45 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, 2) k_fp8_tiles(
     const int64_t m0 = (int64_t) tm * BM;
     const int32_t n0 = tn * BN;
     if (m0 >= rows) return;
-    const int32_t steps = (int32_t) (a.stride / kStepBytes);  // even
+    const int32_t steps = (int32_t) (a.stride / GNS_FP8_BLOCK);
     for (int i = (int) threadIdx.x; i < BN; i += kWaves * kWave) s_bias[i] = a.bias ? a.bias[n0 + i < n ? n0 + i : n - 1] : 0.f;
-    // this wave's pieces: 16 rows each, of the rows' side or the weights'; those past the end repeat the last
-    const bool weights = wave * kLoads * 16 >= BM;
-    const int32_t first = wave * kLoads * 16 - (weights ? BM : 0);
-    const int64_t last = weights ? n - 1 - n0 : rows - 1 - m0;
-    const uint8_t* base = weights ? a.wq + (int64_t) n0 * a.stride : a.q + m0 * a.stride;
-    const int32_t turned = (lane & 3) ^ row_turn(lane >> 2);
+    // this wave's pieces: 8 rows each, of the rows' side or the weights'; a lane's 16 bytes come from where its place in LDS has them.  Rows past
+    // the last repeat it.
+    const bool weights = wave * kLoads * 8 >= BM;
+    const int32_t first = wave * kLoads * 8 - (weights ? BM : 0);
+    const int32_t last = weights ? n - 1 - n0 : (int32_t) min(rows - 1 - m0, (int64_t) BM);
+    const uint8_t* const base = weights ? a.wq + (int64_t) n0 * a.stride : a.q + m0 * a.stride;
     uint32_t from[kLoads];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int32_t row = first + i * 16 + (lane >> 2), at = (int32_t) (row < last ? row : last);
-        from[i] = (uint32_t) at * (uint32_t) a.stride + (uint32_t) (lane & 3) * 16;
-    }
-    int4v* put_at = s_stage + (wave * kLoads * 16 + (lane >> 2)) * 4 + turned;
-    int4v read[2][kLoads];
-    const uint8_t* next;                                      // of the step that is read
-    auto seek = [&](int32_t step) { next = base + (int64_t) (step < steps ? step : steps - 1) * kStepBytes; };   // past the last: the last again
-    auto fetch = [&](int set, int i) { read[set][i] = *reinterpret_cast<const int4v*>(next + from[i]); };
-    auto put = [&](int set, int stage, int i) { put_at[stage * kStage + i * 64] = read[set][i]; };
-    auto fetch_all = [&](int set, int32_t step) {
-        seek(step);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) fetch(set, i);
-        __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < kLoads; ++i)
+        from[i] = (uint32_t) min(first + i * 8 + (lane >> 3), last) * (uint32_t) a.stride + (uint32_t) ((lane & 7) ^ turn_of((wave * kLoads + i) * 8 + (lane >> 3))) * 16;
+    const uint8_t* next;                                      // of the stage that is fetched, and its place
+    char* next_to;
+    auto seek = [&](int32_t step, int buffer) {               // past the last: the last again
+        next = base + (int64_t) min(step, steps - 1) * GNS_FP8_BLOCK;
+        next_to = s_stage + buffer * kStage + wave * kLoads * 1024;
     };
-    auto put_all = [&](int set, int stage) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) put(set, stage, i);
+    auto fetch = [&](int i) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*) (next + from[i]),
+                                         (__attribute__((address_space(3))) void*) (next_to + i * 1024), 16, 0, 0);
     };
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
-    const int l32 = lane & 31, kh = lane >> 5, bank = row_turn(l32);
-    // exponents of this lane's rows and channels, four blocks a word
-    const uint8_t* exponents[MI + NI];
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        const int64_t r = m0 + wm + i * 32 + l32;
-        exponents[i] = a.exponents + (r < rows ? r : rows - 1) * a.exponent_stride;
-    }
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        const int32_t c = n0 + wn + i * 32 + l32;
-        exponents[MI + i] = a.w_exponents + (int64_t) (c < n ? c : n - 1) * a.exponent_stride;
-    }
+    const int l32 = lane & 31, kh = lane >> 5;
+    // exponents, four blocks a word, of 64 rows or channels a wave, go to LDS too
+    const bool scales_too = wave * kWave < BM + BN, scale_of_weights = wave * kWave >= BM;
+    const int32_t scale_row = wave * kWave + lane - (scale_of_weights ? BM : 0);
+    const uint8_t* const exponents = scale_of_weights ? a.w_exponents + (int64_t) n0 * a.exponent_stride : a.exponents + m0 * a.exponent_stride;
+    const uint32_t exponent_at = (uint32_t) min(scale_row, scale_of_weights ? n - 1 - n0 : (int32_t) min(rows - 1 - m0, (int64_t) BM)) * (uint32_t) a.exponent_stride;
     const int32_t words = (int32_t) (a.exponent_stride / 4);
-    int scale[2][MI + NI];
     auto fetch_scales = [&](int set, int32_t word) {
-        const int32_t at = word < words ? word : words - 1;
+        if (scales_too)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*) (exponents + 4 * min(word, words - 1) + exponent_at),
+                                             (__attribute__((address_space(3))) void*) (s_scale[set] + wave * kWave), 4, 0, 0);
+    };
+    int scale[MI + NI];                                       // of this lane's rows and channels
+    auto get_scales = [&](int set) {
 #pragma unroll
-        for (int i = 0; i < MI + NI; ++i) scale[set][i] = *reinterpret_cast<const int*>(exponents[i] + 4 * (int64_t) at);
+        for (int i = 0; i < MI + NI; ++i) scale[i] = s_scale[set][i < MI ? wm + i * 32 + l32 : BM + wn + (i - MI) * 32 + l32];
     };
     float16v acc[MI][NI];
 #pragma unroll
@@ -228,92 +219,90 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, 2) k_fp8_tiles(
         for (int j = 0; j < NI; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-    int8v f[2][MI + NI];                                      // fragments of the rows, then of the weights, of this stage and the next
-    const int4v* x_at = s_stage + (wm + l32) * 4;
-    const int4v* w_at = s_stage + (BM + wn + l32) * 4;
-    auto get = [&](int set, int stage, int i) {
-        const int4v* at = i < MI ? x_at + stage * kStage + i * 128 : w_at + stage * kStage + (i - MI) * 128;
-        const int4v low = at[kh ^ bank], high = at[(2 + kh) ^ bank];
-        f[set][i] = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
+    int8v f[2][MI + NI];                                      // fragments of the rows, then of the weights, of this half stage and the next
+    const char* const x_at = s_stage + (wm + l32) * 128;
+    const char* const w_at = s_stage + (BM + wn + l32) * 128;
+    auto get = [&](int half, int buffer, int i) {
+        const char* at = (i < MI ? x_at + i * 4096 : w_at + (i - MI) * 4096) + buffer * kStage;
+        const int4v low = *reinterpret_cast<const int4v*>(at + ((half * 4 + kh) ^ turn_of(l32)) * 16);
+        const int4v high = *reinterpret_cast<const int4v*>(at + ((half * 4 + 2 + kh) ^ turn_of(l32)) * 16);
+        f[half][i] = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    int s0 = 0, s1 = 1, s2 = 2;                               // stages of this step, the next and the one after
-    fetch_scales(0, 0);
-    fetch_all(0, 0);
-    fetch_all(1, 1);
-    put_all(0, 0);
-    fetch_all(0, 2);
-    put_all(1, 1);
-    fetch_all(1, 3);
-    lds_barrier();
-#pragma unroll
-    for (int i = 0; i < MI + NI; ++i) get(0, 0, i);
-    // Stage `step` is multiplied; what was read for step + 2 goes to LDS, what is read now is for step + 4; the next stage's fragments are read.
-    auto turn = [&](auto at, int32_t step, int word_set) {
-        constexpr int kAt = decltype(at)::value, set = kAt & 1, kByte = kAt / 2;
-        constexpr int kProducts = MI * NI, kOthers = MI + NI + 2 * kLoads;
-        seek(step + 4);
-        auto others = [&](int m, int all) {                   // behind product m of so many
+    // the products of half a stage, and between them, one after the other, what else there is to do
+    auto multiply = [&](auto byte, int half, auto&& other, int others) __attribute__((always_inline)) {
+        constexpr int kByte = decltype(byte)::value, kProducts = MI * NI * (kPrecise ? 4 : 1);
+        constexpr int kEarly = kProducts > 4 ? kProducts * 3 / 4 : kProducts;      // the last products cover the last reads
+        auto between = [&](int m) __attribute__((always_inline)) {
             __builtin_amdgcn_sched_barrier(0);
+            if (m < kEarly) {
 #pragma unroll
-            for (int o = kOthers * m / all; o < kOthers * (m + 1) / all; ++o) {
-                if (o < MI + NI)               get(1 - set, s1, o);
-                else if (o < MI + NI + kLoads) put(set, s2, o - (MI + NI));
-                else                           fetch(set, o - (MI + NI) - kLoads);
+                for (int o = others * m / kEarly; o < others * (m + 1) / kEarly; ++o) other(o);
             }
             __builtin_amdgcn_sched_barrier(0);
         };
         if constexpr (kPrecise) {
             float power[MI + NI];
 #pragma unroll
-            for (int i = 0; i < MI + NI; ++i) power[i] = power_of((uint32_t) scale[word_set][i] >> (8 * kByte) & 255u);
+            for (int i = 0; i < MI + NI; ++i) power[i] = power_of((uint32_t) scale[i] >> (8 * kByte) & 255u);
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 bf8v v[MI + NI];
 #pragma unroll
-                for (int i = 0; i < MI + NI; ++i) v[i] = values_of((uint32_t) f[set][i][2 * h], (uint32_t) f[set][i][2 * h + 1], power[i]);
+                for (int i = 0; i < MI + NI; ++i) v[i] = values_of((uint32_t) f[half][i][2 * h], (uint32_t) f[half][i][2 * h + 1], power[i]);
 #pragma unroll
-                for (int m = 0; m < kProducts; ++m) {
+                for (int m = 0; m < MI * NI; ++m) {
                     acc[m / NI][m % NI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[MI + m % NI], v[m / NI], acc[m / NI][m % NI], 0, 0, 0);
-                    others(h * kProducts + m, 4 * kProducts);
+                    between(h * MI * NI + m);
                 }
             }
         } else {
 #pragma unroll
             for (int m = 0; m < kProducts; ++m) {
-                acc[m / NI][m % NI] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f[set][MI + m % NI], f[set][m / NI], acc[m / NI][m % NI], 0, 0,
-                                                                                     kByte, scale[word_set][MI + m % NI], kByte, scale[word_set][m / NI]);
-                others(m, kProducts);
+                acc[m / NI][m % NI] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f[half][MI + m % NI], f[half][m / NI], acc[m / NI][m % NI], 0, 0,
+                                                                                     kByte, scale[MI + m % NI], kByte, scale[m / NI]);
+                between(m);
             }
         }
-        const int t = s0;
-        s0 = s1; s1 = s2; s2 = t;
-        lds_barrier();
     };
-    auto eight = [&](int32_t step, int set) {                 // the steps of a word of exponents; false: the last was among them
-        fetch_scales(1 - set, step / 8 + 1);
-        turn(std::integral_constant<int, 0>{}, step, set);
-        turn(std::integral_constant<int, 1>{}, step + 1, set);
-        if (step + 2 >= steps) return false;
-        turn(std::integral_constant<int, 2>{}, step + 2, set);
-        turn(std::integral_constant<int, 3>{}, step + 3, set);
-        if (step + 4 >= steps) return false;
-        turn(std::integral_constant<int, 4>{}, step + 4, set);
-        turn(std::integral_constant<int, 5>{}, step + 5, set);
-        if (step + 6 >= steps) return false;
-        turn(std::integral_constant<int, 6>{}, step + 6, set);
-        turn(std::integral_constant<int, 7>{}, step + 7, set);
-        return step + 8 < steps;
-    };
-    for (int32_t step = 0;; step += 16) {
-        if (!eight(step, 0)) break;
-        if (!eight(step + 8, 1)) break;
+    fetch_scales(0, 0);
+#pragma unroll
+    for (int p = 0; p < S; ++p) {
+        seek(p, p);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) fetch(i);
     }
+    auto come = [&](auto ahead) {                             // all stages but the last `ahead` have come, and the block's waves are here
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(decltype(ahead)::value * kLoads) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    come(std::integral_constant<int, S - 1>{});
+#pragma unroll
+    for (int i = 0; i < MI + NI; ++i) get(0, 0, i);
+    int buffer = 0;
+    auto stage = [&](auto at, int32_t step) __attribute__((always_inline)) {        // false: it is the last
+        const int after = buffer + 1 < S ? buffer + 1 : 0;
+        multiply(at, 0, [&](int o) { get(1, buffer, o); }, MI + NI);
+        come(std::integral_constant<int, S - 2>{});
+        seek(step + S, buffer);
+        multiply(at, 1, [&](int o) { if (o < kLoads) fetch(o); else get(0, after, o - kLoads); }, MI + NI + kLoads);
+        buffer = after;
+        return step + 1 < steps;
+    };
+    auto four_stages = [&](int32_t step, int set) __attribute__((always_inline)) {                  // the stages of a word of exponents; false: the last was among them
+        get_scales(set);
+        fetch_scales(1 - set, step / 4 + 1);
+        return stage(std::integral_constant<int, 0>{}, step) && stage(std::integral_constant<int, 1>{}, step + 1) &&
+               stage(std::integral_constant<int, 2>{}, step + 2) && stage(std::integral_constant<int, 3>{}, step + 3);
+    };
+    for (int32_t step = 0; four_stages(step, step / 4 & 1); step += 4) {}
+    come(std::integral_constant<int, 0>{});                   // what was fetched past the last has come too
     // Each strip of 32 rows goes through a piece of LDS of the wave's own, so that rows leave in pieces of 16 bytes.
     // (from a lane id the compiler cannot see through: what it would work out of this in front of the loop costs registers)
     constexpr int V = 16 / (int) sizeof(T), kLanes = WN / V, kPitch = WN * (int) sizeof(T) + 16;
-    static_assert(kWaves * 32 * kPitch <= 3 * kStage * 16, "the strips lie in the stages' place");
+    static_assert(kWaves * 32 * kPitch <= S * kStage, "the strips lie in the stages' place");
     const int e_lane = opaque_lane_id(), e32 = e_lane & 31, four = 4 * (e_lane >> 5);
-    char* const strip = reinterpret_cast<char*>(s_stage) + wave * (32 * kPitch);
+    char* const strip = s_stage + wave * (32 * kPitch);
     const int32_t c = n0 + wn + e_lane % kLanes * V;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
@@ -614,14 +603,14 @@ hipError_t launch_quantize_fp8(const gns_ctx* c, const QuantizeFp8Args& a, int32
     return hipGetLastError();
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, int S>
 static hipError_t launch_tiles(const DenseFp8Args& a, hipStream_t s)
 {
     // a dimension of a grid has fewer than 2^32 threads; 2^31 tiles of outputs fit no memory
     const int64_t m_tiles = ((int64_t) a.count.rows + BM - 1) / BM, n_tiles = (a.out.width + BN - 1) / BN, tiles = m_tiles * n_tiles, most = 1 << 22;
     if (tiles > INT32_MAX - most) return hipErrorInvalidValue;
     const dim3 grid((unsigned) (tiles < most ? tiles : most), (unsigned) ((tiles + most - 1) / most));
-    hipLaunchKernelGGL((k_fp8_tiles<T, BM, BN, WM, WN>), grid, dim3((BM / WM) * (BN / WN) * kWave), 0, s, a, (int32_t) m_tiles, (int32_t) n_tiles);
+    hipLaunchKernelGGL((k_fp8_tiles<T, BM, BN, WM, WN, S>), grid, dim3((BM / WM) * (BN / WN) * kWave), 0, s, a, (int32_t) m_tiles, (int32_t) n_tiles);
     return hipGetLastError();
 }
 
@@ -636,8 +625,10 @@ static hipError_t launch_typed(const gns_ctx* c, const DenseFp8Args& a, hipStrea
         else                         hipLaunchKernelGGL((k_fp8_few<T, float, false, 4>), grid, dim3(kFewBlock), 0, s, a, QuantizeFp8Args{});
         return hipGetLastError();
     }
-    if (tiles(128, 128) >= c->num_cus) return launch_tiles<T, 128, 128, 64, 64>(a, s);
-    return launch_tiles<T, 64, 64, 32, 32>(a, s);
+    if constexpr (sizeof(T) == 2)
+        if (tiles(256, 256) * 8 >= (int64_t) c->num_cus * 5 && a.k >= 1024) return launch_tiles<T, 256, 256, 128, 64, 2>(a, s);
+    if (tiles(128, 128) >= c->num_cus) return launch_tiles<T, 128, 128, 64, 64, 2>(a, s);
+    return launch_tiles<T, 64, 64, 32, 32, 4>(a, s);
 }
 
 hipError_t launch_dense_fp8(const gns_ctx* c, const DenseFp8Args& a, int32_t out_type, hipStream_t s)
