@@ -185,15 +185,12 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, 2) k_fp8_tiles(
     for (int i = 0; i < kLoads; ++i)
         from[i] = (uint32_t) min(first + i * 8 + (lane >> 3), last) * (uint32_t) a.stride + (uint32_t) ((lane & 7) ^ turn_of((wave * kLoads + i) * 8 + (lane >> 3))) * 16;
     const uint8_t* next;                                      // of the stage that is fetched, and its place
-    char* next_to;
+    uint32_t next_to;
     auto seek = [&](int32_t step, int buffer) {               // past the last: the last again
         next = base + (int64_t) min(step, steps - 1) * GNS_FP8_BLOCK;
-        next_to = s_stage + buffer * kStage + wave * kLoads * 1024;
+        next_to = lds_address(s_stage) + buffer * kStage + wave * kLoads * 1024;
     };
-    auto fetch = [&](int i) {
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*) (next + from[i]),
-                                         (__attribute__((address_space(3))) void*) (next_to + i * 1024), 16, 0, 0);
-    };
+    auto fetch = [&](int i) { fetch_to_lds(next, from[i], next_to + i * 1024); };
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
     const int l32 = lane & 31, kh = lane >> 5;
     // exponents, four blocks a word, of 64 rows or channels a wave, go to LDS too
@@ -203,9 +200,7 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, 2) k_fp8_tiles(
     const uint32_t exponent_at = (uint32_t) min(scale_row, scale_of_weights ? n - 1 - n0 : (int32_t) min(rows - 1 - m0, (int64_t) BM)) * (uint32_t) a.exponent_stride;
     const int32_t words = (int32_t) (a.exponent_stride / 4);
     auto fetch_scales = [&](int set, int32_t word) {
-        if (scales_too)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*) (exponents + 4 * min(word, words - 1) + exponent_at),
-                                             (__attribute__((address_space(3))) void*) (s_scale[set] + wave * kWave), 4, 0, 0);
+        if (scales_too) fetch_word_to_lds(exponents + 4 * min(word, words - 1), exponent_at, lds_address(s_scale[set]) + wave * kWave * 4);
     };
     int scale[MI + NI];                                       // of this lane's rows and channels
     auto get_scales = [&](int set) {
@@ -222,21 +217,27 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, 2) k_fp8_tiles(
     int8v f[2][MI + NI];                                      // fragments of the rows, then of the weights, of this half stage and the next
     const char* const x_at = s_stage + (wm + l32) * 128;
     const char* const w_at = s_stage + (BM + wn + l32) * 128;
-    auto get = [&](int half, int buffer, int i) {
+    auto get = [&](int half, int buffer, int o) {             // in the order in which products ask for them
+        const int i = o == 0 ? 0 : o <= NI ? MI + o - 1 : o - NI;
         const char* at = (i < MI ? x_at + i * 4096 : w_at + (i - MI) * 4096) + buffer * kStage;
         const int4v low = *reinterpret_cast<const int4v*>(at + ((half * 4 + kh) ^ turn_of(l32)) * 16);
         const int4v high = *reinterpret_cast<const int4v*>(at + ((half * 4 + 2 + kh) ^ turn_of(l32)) * 16);
         f[half][i] = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
     };
     // the products of half a stage, and between them, one after the other, what else there is to do
-    auto multiply = [&](auto byte, int half, auto&& other, int others) __attribute__((always_inline)) {
+    auto multiply = [&](auto byte, int half, auto&& soon, int most_soon, auto&& late, int most_late) __attribute__((always_inline)) {
         constexpr int kByte = decltype(byte)::value, kProducts = MI * NI * (kPrecise ? 4 : 1);
-        constexpr int kEarly = kProducts > 4 ? kProducts * 3 / 4 : kProducts;      // the last products cover the last reads
+        constexpr int kSoon = (kProducts + 1) / 2, kLate = kProducts - kSoon > 0 ? kProducts - kSoon : 1;
         auto between = [&](int m) __attribute__((always_inline)) {
             __builtin_amdgcn_sched_barrier(0);
-            if (m < kEarly) {
+            if (m < kSoon) {
 #pragma unroll
-                for (int o = others * m / kEarly; o < others * (m + 1) / kEarly; ++o) other(o);
+                for (int o = most_soon * m / kSoon; o < most_soon * (m + 1) / kSoon; ++o) soon(o);
+            }
+            if (m >= kProducts - kLate) {
+                const int l = m - (kProducts - kLate);
+#pragma unroll
+                for (int o = most_late * l / kLate; o < most_late * (l + 1) / kLate; ++o) late(o);
             }
             __builtin_amdgcn_sched_barrier(0);
         };
@@ -282,10 +283,10 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * kWave, 2) k_fp8_tiles(
     int buffer = 0;
     auto stage = [&](auto at, int32_t step) __attribute__((always_inline)) {        // false: it is the last
         const int after = buffer + 1 < S ? buffer + 1 : 0;
-        multiply(at, 0, [&](int o) { get(1, buffer, o); }, MI + NI);
+        multiply(at, 0, [&](int o) { get(1, buffer, o); }, MI + NI, [&](int) {}, 0);
         come(std::integral_constant<int, S - 2>{});
         seek(step + S, buffer);
-        multiply(at, 1, [&](int o) { if (o < kLoads) fetch(o); else get(0, after, o - kLoads); }, MI + NI + kLoads);
+        multiply(at, 1, [&](int o) { get(0, after, o); }, MI + NI, [&](int o) { fetch(o); }, kLoads);
         buffer = after;
         return step + 1 < steps;
     };

@@ -336,15 +336,12 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, (BM / WM) 
     for (int i = 0; i < kLoads; ++i)
         from[i] = (uint32_t) min(first + i * 8 + (lane >> 3), last) * (uint32_t) row_bytes + (uint32_t) ((lane & 7) ^ turn_of((piece + i) * 8 + (lane >> 3))) * 16;
     const char* next = base;
-    char* next_to = s_stage;
+    uint32_t next_to = 0;
     auto seek = [&](int32_t step, int buffer) {               // past the last: the last again
         next = base + (int64_t) min(step, steps - 1) * (128 * KS);
-        next_to = s_stage + buffer * kStage + wave * kLoads * 1024;
+        next_to = lds_address(s_stage) + buffer * kStage + wave * kLoads * 1024;
     };
-    auto fetch = [&](int i) {
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*) (next + from[i]),
-                                         (__attribute__((address_space(3))) void*) (next_to + i * 1024), 16, 0, 0);
-    };
+    auto fetch = [&](int i) { fetch_to_lds(next, from[i], next_to + i * 1024); };
     const int wm = w / (BN / WN) * WM, wn = w % (BN / WN) * WN, l32 = lane & 31, kh = lane >> 5;
     const char* const x_at = s_stage + (group * kRows + wm + l32) * 128;
     const char* const y_at = s_stage + (group * kRows + BM + wn + l32) * 128;
