@@ -7,27 +7,72 @@ namespace gns {
 
 template <typename T> constexpr int kPiece = 16 / (int) sizeof(T);        // values of 16 bytes
 
-__device__ __forceinline__ float sigmoid_of(float y) { return __builtin_amdgcn_rcpf(1.f + expf(-y)); }
-// The normal distribution's function, good to a few roundings of itself also far down.
-__device__ __forceinline__ float normal_below(float y) { return 0.5f * erfcf(-0.70710678f * y); }
+// exp(y) as 2 to the rounded product: off by |y| roundings at most, which is little of a sum with 1 and of a tail.
+__device__ __forceinline__ float exp_of(float y) { return __builtin_amdgcn_exp2f(y * 1.44269504f); }
+__device__ __forceinline__ float sigmoid_of(float y) { return __builtin_amdgcn_rcpf(1.f + exp_of(-y)); }
 
-__device__ __forceinline__ float activate(float y, int32_t kind)
+// The normal distribution's function and density (without its factor 1 / sqrt(2 pi)): for y < 0, exp(-y^2 / 2) times half of the scaled complementary
+// error function of -y / sqrt 2, which falls slowly from 1/2 and is a polynomial of 1 / (1 + 0.3 |y|): one of least
+// relative error over 0 .. 14.5 (6e-8, fitted to the function's values in 64 bits), 1.6 roundings in the mean as computed.
+__device__ __forceinline__ float normal_below(float y, float* density)
 {
-    if (kind == GNS_ACT_RELU) return relu_of(y);
-    if (kind == GNS_ACT_SILU) return y * sigmoid_of(y);
-    if (kind == GNS_ACT_GELU) return y * normal_below(y);
-    return y;
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.3f * fabsf(y));
+    float r = 0.038407475f;
+    r = r * t - 0.16930783f;
+    r = r * t + 0.22895248f;
+    r = r * t - 0.076840408f;
+    r = r * t + 0.14276575f;
+    r = r * t + 0.094585687f;
+    r = r * t + 0.1219453f;
+    r = r * t + 0.1194842f;
+    r = r * t + 7.3726083e-6f;
+    *density = exp_of(-0.5f * y * y);
+    const float tail = r * *density;
+    return y < 0.f ? tail : 1.f - tail;
 }
 
-__device__ __forceinline__ float slope_at(float y, int32_t kind)
+// Values of the activation, and its slopes, in the place of y: one branch for all of them.
+template <int V>
+__device__ __forceinline__ void activate(float (&y)[V], int32_t kind)
 {
-    if (kind == GNS_ACT_RELU) return y > 0.f ? 1.f : y <= 0.f ? 0.f : y;  // a NaN stays one
-    if (kind == GNS_ACT_SILU) {
-        const float s = sigmoid_of(y);
-        return s * (1.f + y * (1.f - s));
+    if (kind == GNS_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = relu_of(y[i]);
+    } else if (kind == GNS_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] *= sigmoid_of(y[i]);
+    } else if (kind == GNS_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float density;
+            y[i] *= normal_below(y[i], &density);
+        }
     }
-    if (kind == GNS_ACT_GELU) return normal_below(y) + y * expf(-0.5f * y * y) * 0.39894228f;
-    return 1.f;
+}
+
+template <int V>
+__device__ __forceinline__ void slopes_at(float (&y)[V], int32_t kind)
+{
+    if (kind == GNS_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = y[i] > 0.f ? 1.f : y[i] <= 0.f ? 0.f : y[i];       // a NaN stays one
+    } else if (kind == GNS_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float s = sigmoid_of(y[i]);
+            y[i] = s * (1.f + y[i] * (1.f - s));
+        }
+    } else if (kind == GNS_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float density;
+            const float below = normal_below(y[i], &density);
+            y[i] = below + y[i] * density * 0.39894228f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = 1.f;
+    }
 }
 
 // Up to V consecutive columns of a range of `width`.  Where the range ends inside a piece the piece begins earlier, and what the one
@@ -181,8 +226,8 @@ __global__ void __launch_bounds__(kBlock) k_norm_units(NormArgs a, int64_t row_s
                 load_parameters<V, kWhole>(a.beta ? a.beta + (int64_t) j * w : nullptr, c[p], 0.f, b);
             }
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                y[i] = activate((value_of_words<T>(words[p], i) - s.x) * (s.y * (kKeep ? gamma[p][i] : g[i])) + (kKeep ? beta[p][i] : b[i]), a.activation);
+            for (int i = 0; i < V; ++i) y[i] = (value_of_words<T>(words[p], i) - s.x) * (s.y * (kKeep ? gamma[p][i] : g[i])) + (kKeep ? beta[p][i] : b[i]);
+            activate(y, a.activation);
             store_columns<T, kWhole>(out, c[p], y);
         }
         if (a.stats && l == 0) reinterpret_cast<float2*>(a.stats)[r * a.groups + j] = s;
@@ -229,10 +274,16 @@ __global__ void __launch_bounds__(kBlock) k_norm_grad_units(NormArgs a, int64_t 
             float gamma[V], beta[V];
             load_parameters<V, kWhole>(gammas, c[p], 1.f, gamma);
             load_parameters<V, kWhole>(betas, c[p], 0.f, beta);
+            float slope[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 h[p][i] = (value_of_words<T>(xw[p], i) - s.x) * s.y;
-                const float dy = value_of_words<T>(dw[p], i) * slope_at(h[p][i] * gamma[i] + beta[i], a.activation);
+                slope[i] = h[p][i] * gamma[i] + beta[i];
+            }
+            slopes_at(slope, a.activation);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float dy = value_of_words<T>(dw[p], i) * slope[i];
                 g[p][i] = dy * gamma[i];
                 if (kWhole || (i >= c[p].skip && i < c[p].end)) {
                     m1 += g[p][i];
@@ -289,28 +340,36 @@ __global__ void __launch_bounds__(kBlock) k_norm_grad_units(NormArgs a, int64_t 
     }
 }
 
-// dbeta and dgamma from `count` rows of pairs (count_of: as many as there are tiles of so many rows): 16 columns a block, sixteen threads each.
-constexpr int kJoinColumns = 16;
-__global__ void __launch_bounds__(kBlock) k_norm_columns(const float2* parts, int64_t count, RowCount rows, int32_t tile_rows, int32_t width,
-                                                         float* dgamma, float* dbeta)
+// dbeta and dgamma of one of the runs of eight columns, from `count` rows of pairs: 32 threads a column.
+constexpr int kJoinColumns = 8;
+__device__ __forceinline__ void sum_columns(int32_t run, const float2* parts, int64_t count, int32_t width, float* dgamma, float* dbeta, float2* s_sum)
 {
-    __shared__ float2 s_sum[kBlock / kJoinColumns][kJoinColumns];
     constexpr int kTurns = kBlock / kJoinColumns;
-    if (tile_rows) count = ((int64_t) rows.get() + tile_rows - 1) / tile_rows;
     const int at = (int) threadIdx.x % kJoinColumns, k = (int) threadIdx.x / kJoinColumns;
-    const int32_t column = (int32_t) blockIdx.x * kJoinColumns + at, c = column < width ? column : width - 1;
+    const int32_t column = run * kJoinColumns + at, c = column < width ? column : width - 1;
     float2 t = make_float2(0.f, 0.f);
 #pragma unroll 8
     for (int64_t i = k; i < count; i += kTurns) {
         const float2 v = parts[i * width + c];
         t.x += v.x; t.y += v.y;
     }
-    s_sum[k][at] = t;
+    s_sum[threadIdx.x] = t;
     __syncthreads();
     if (k || column >= width) return;
-    for (int i = 1; i < kTurns; ++i) { t.x += s_sum[i][at].x; t.y += s_sum[i][at].y; }
+    for (int i = 1; i < kTurns; ++i) {
+        t.x += s_sum[i * kJoinColumns + at].x;
+        t.y += s_sum[i * kJoinColumns + at].y;
+    }
     if (dbeta) dbeta[column] = t.x;
     if (dgamma) dgamma[column] = t.y;
+}
+// tile_rows: the rows of pairs are those of as many tiles of rows as there are
+__global__ void __launch_bounds__(kBlock) k_norm_columns(const float2* parts, int64_t count, RowCount rows, int32_t tile_rows, int32_t width,
+                                                         float* dgamma, float* dbeta)
+{
+    __shared__ float2 s_sum[kBlock];
+    if (tile_rows) count = ((int64_t) rows.get() + tile_rows - 1) / tile_rows;
+    sum_columns((int32_t) blockIdx.x, parts, count, width, dgamma, dbeta, s_sum);
 }
 
 // ---- any segments: tiles of rows -------------------------------------------------------------------------------------------
@@ -330,15 +389,17 @@ struct Segments {
     {
         return at ? min(max(at[s + 1], begin(s)), rows) : (int32_t) min((int64_t) (s + 1) * per, (int64_t) rows);
     }
-    // the first segment that ends behind a row
+    // the first segment that ends behind a row; all lanes of a wave ask, each looks at one of 64 places at a time
     __device__ __forceinline__ int32_t first(int32_t row) const
     {
         if (!at) return row / per;
         int32_t low = 0, high = n;
         while (low < high) {
-            const int32_t mid = low + (high - low) / 2;
-            if (at[mid + 1] > row) high = mid;
-            else                   low = mid + 1;
+            const int32_t step = (high - low + kWave - 1) / kWave, place = low + opaque_lane_id() * step;
+            const int32_t before = (int32_t) __popcll(__ballot(place < high && at[min(place, n - 1) + 1] <= row));
+            if (before == 0) break;
+            high = min(high, low + before * step);
+            low += (before - 1) * step + 1;
         }
         return low;
     }
@@ -379,6 +440,30 @@ struct TileBlock {
     }
 };
 
+// Rows r, r + step, .. below end: kRows at a time are read before the first of them is worked on.
+template <int N> struct Batch { uint32_t words[N][4]; };
+template <int N, int kRows, typename Load, typename Work>
+__device__ __forceinline__ void by_batches_of(int32_t r, int32_t end, int32_t step, Load&& load, Work&& work)
+{
+    for (; r + (kRows - 1) * step < end; r += kRows * step) {
+        Batch<N> of[kRows];
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) load(r + k * step, of[k]);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) work(r + k * step, of[k]);
+    }
+    for (; r < end; r += step) {
+        Batch<N> of;
+        load(r, of);
+        work(r, of);
+    }
+}
+template <typename T, bool kWhole>
+__device__ __forceinline__ void load_row(const ConstRows& x, int32_t r, const Columns& c, uint32_t (&words)[4])
+{
+    load_columns<T, kWhole>(reinterpret_cast<const T*>(x.data) + (int64_t) r * x.stride, c, words);
+}
+
 // Teams of a block for `parts` things, each of up to `most` entries: lanes a team, at most a wave.
 __device__ __forceinline__ int32_t team_lanes(int32_t parts, int32_t most)
 {
@@ -392,9 +477,11 @@ __device__ __forceinline__ float lanes_sum(float v, int32_t lanes)
     return v;
 }
 
+// kOne in these kernels: groups are whole pieces, so a thread's columns are of one group and all its own.
+//
 // Mean and sum of squared distances of each group of the slab, for each segment in the tile: by column in registers (Welford's
 // steps, every column of a thread has as many rows), then over threads and columns by way of LDS.
-template <typename T>
+template <typename T, bool kOne>
 __global__ void __launch_bounds__(kBlock) k_norm_parts(NormArgs a, Tiling t, float2* parts)
 {
     constexpr int V = kPiece<T>;
@@ -412,23 +499,21 @@ __global__ void __launch_bounds__(kBlock) k_norm_parts(NormArgs a, Tiling t, flo
 #pragma unroll
         for (int i = 0; i < V; ++i) mean[i] = squares[i] = 0.f;
         if (b.c.end) {
-            for (int32_t r = r0 + b.turn; r < r1; r += t.turns) {
-                uint32_t words[4];
-                load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + (int64_t) r * a.x.stride, b.c, words);
+            by_batches_of<1, 4>(r0 + b.turn, r1, t.turns, [&](int32_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); }, [&](int32_t, const Batch<1>& of) {
                 n += 1.f;
                 const float inverse = __builtin_amdgcn_rcpf(n);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float v = value_of_words<T>(words, i), d = v - mean[i];
+                    const float v = value_of_words<T>(of.words[0], i), d = v - mean[i];
                     mean[i] += d * inverse;
                     squares[i] += d * (v - mean[i]);
                 }
-            }
+            });
         }
         __syncthreads();                                      // the segment before may still be read
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (i >= b.c.skip && i < b.c.end) {
+            if (kOne ? b.c.end != 0 : i >= b.c.skip && i < b.c.end) {
                 s_mean[b.turn * pitch + b.c.first + i - b.c0] = mean[i];
                 s_squares[b.turn * pitch + b.c.first + i - b.c0] = squares[i];
             }
@@ -457,113 +542,150 @@ __global__ void __launch_bounds__(kBlock) k_norm_parts(NormArgs a, Tiling t, flo
     }
 }
 
-// What tiles and slabs found for a segment and group, together: L lanes each.  kGrad: sums of the backward pass, divided by the
-// number of values, to `moments`; otherwise means and squares, to the stats.
+// What tiles and slabs found for segment s and group j, together, by `lanes` lanes of which this is number l (all call it): kGrad, the sums of the backward
+// pass, divided by the number of values; otherwise mean and variance.  sum(v) is the sum of the lanes' v.
+template <typename T, bool kGrad, typename Sum>
+__device__ __forceinline__ float2 join_parts(const NormArgs& a, const Tiling& t, const float2* parts, int32_t s, int32_t begin, int32_t end, int32_t j, int32_t l,
+                                             int32_t lanes, Sum&& sum)
+{
+    const int32_t w = a.x.width / a.groups;
+    const int32_t tile0 = begin / t.tile_rows, tiles = end > begin ? (end - 1) / t.tile_rows - tile0 + 1 : 0;
+    const int64_t c0 = (int64_t) j * w, c1 = c0 + w;
+    const int32_t slab0 = (int32_t) (c0 / slab_columns<T>()), slabs = (int32_t) ((c1 - 1) / slab_columns<T>()) - slab0 + 1;
+    const float n = (float) (end - begin) * (float) w;
+    auto part = [&](int32_t e, float* of) {
+        const int32_t in = slabs == 1 ? e : e / slabs, tile = tile0 + in, slab = slab0 + (e - in * slabs);
+        const int64_t row0 = max((int64_t) begin, (int64_t) tile * t.tile_rows), row1 = min((int64_t) end, (int64_t) (tile + 1) * t.tile_rows);
+        const int64_t from = max(c0, (int64_t) slab * slab_columns<T>()), upto = min(c1, (int64_t) (slab + 1) * slab_columns<T>());
+        *of = (float) (row1 - row0) * (float) (upto - from);
+        return parts[((int64_t) tile + s) * t.entries + j + slab];
+    };
+    const int32_t all = tiles * slabs;                        // both at most 2^23, as there are workspaces for them
+    float one = 0.f, two = 0.f, of;
+#pragma unroll 4
+    for (int32_t e = l; e < all; e += lanes) {
+        const float2 p = part(e, &of);
+        one += kGrad ? p.x : of * p.x;
+        two += p.y;
+    }
+    one = sum(one, 0) / n;
+    if (!kGrad) {
+#pragma unroll 4
+        for (int32_t e = l; e < all; e += lanes) {
+            const float d = part(e, &of).x - one;
+            two += of * d * d;
+        }
+    }
+    two = sum(two, 1) / n;
+    if (all == 0) return make_float2(0.f, 0.f);
+    return kGrad ? make_float2(one, two) : stats_of(one, two, a.eps);
+}
+
+// In a launch of its own, L lanes for each segment and group.
 template <typename T, int L, bool kGrad>
 __global__ void __launch_bounds__(kBlock) k_norm_join(NormArgs a, Tiling t, const float2* parts, float2* to)
 {
     __shared__ float s_sums[2][kBlock / kWave];
-    const int32_t rows = a.count.get(), w = a.x.width / a.groups;
-    const Segments segments(a, rows);
+    const Segments segments(a, a.count.get());
     const int64_t units = (int64_t) segments.n * a.groups, step = (int64_t) gridDim.x * (kBlock / L);
     for (int64_t u0 = (int64_t) blockIdx.x * (kBlock / L); u0 < units; u0 += step) {
         const int64_t u = min(u0 + (int64_t) opaque((int) threadIdx.x) / L, units - 1);
         const int32_t l = opaque((int) threadIdx.x) % L, s = (int32_t) (u / a.groups), j = (int32_t) (u - (int64_t) s * a.groups);
-        const int32_t begin = segments.begin(s), end = segments.end(s);
-        const int32_t tile0 = begin / t.tile_rows, tiles = end > begin ? (end - 1) / t.tile_rows - tile0 + 1 : 0;
-        const int64_t c0 = (int64_t) j * w, c1 = c0 + w;
-        const int32_t slab0 = (int32_t) (c0 / slab_columns<T>()), slabs = (int32_t) ((c1 - 1) / slab_columns<T>()) - slab0 + 1;
-        const float n = (float) (end - begin) * (float) w;
-        auto part = [&](int64_t e, float* of) {
-            const int32_t tile = tile0 + (int32_t) (e / slabs), slab = slab0 + (int32_t) (e % slabs);
-            const int64_t row0 = max((int64_t) begin, (int64_t) tile * t.tile_rows), row1 = min((int64_t) end, (int64_t) (tile + 1) * t.tile_rows);
-            const int64_t from = max(c0, (int64_t) slab * slab_columns<T>()), upto = min(c1, (int64_t) (slab + 1) * slab_columns<T>());
-            *of = (float) (row1 - row0) * (float) (upto - from);
-            return parts[((int64_t) tile + s) * t.entries + j + slab];
-        };
-        const int64_t all = (int64_t) tiles * slabs;
-        float one = 0.f, two = 0.f, of;
-        for (int64_t e = l; e < all; e += L) {
-            const float2 p = part(e, &of);
-            one += kGrad ? p.x : of * p.x;
-            two += p.y;
-        }
-        one = team_sum<L>(one, &s_sums[0][0], 0) / n;
-        if (!kGrad) {
-            for (int64_t e = l; e < all; e += L) {
-                const float d = part(e, &of).x - one;
-                two += of * d * d;
-            }
-        }
-        two = team_sum<L>(two, &s_sums[0][0], 1) / n;
-        if (L > kWave) __syncthreads();
-        if (l == 0) {
-            if (all == 0)   to[u] = make_float2(0.f, 0.f);
-            else if (kGrad) to[u] = make_float2(one, two);
-            else            to[u] = stats_of(one, two, a.eps);
-        }
+        const float2 v = join_parts<T, kGrad>(a, t, parts, s, segments.begin(s), segments.end(s), j, l, L,
+                                              [&](float x, int turn) { return team_sum<L>(x, &s_sums[0][0], turn); });
+        if (l == 0) to[u] = v;
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kBlock) k_norm_apply(NormArgs a, Tiling t, const float2* stats)
+// Or in the blocks that need it: of segment s all groups of this block's slab, to s_of.
+template <typename T, bool kGrad>
+__device__ __forceinline__ void join_here(const NormArgs& a, const Tiling& t, const TileBlock<T>& b, const float2* parts, int32_t s, int32_t begin, int32_t end,
+                                          float2* s_of)
 {
-    constexpr int V = kPiece<T>;
+    const int32_t first_group = b.c0 / b.w, groups = (b.c1 - 1) / b.w - first_group + 1;
+    const int32_t lanes = team_lanes(groups, kWave), team = opaque((int) threadIdx.x) / lanes, lane = opaque((int) threadIdx.x) % lanes;
+    __syncthreads();                                          // the segment before may still be read
+    for (int32_t g0 = 0; g0 < groups; g0 += kBlock / lanes) {
+        const int32_t g = min(g0 + team, groups - 1);
+        const float2 v = join_parts<T, kGrad>(a, t, parts, s, begin, end, first_group + g, lane, lanes, [&](float x, int) { return lanes_sum(x, lanes); });
+        if (lane == 0 && g0 + team < groups) {
+            s_of[g] = v;
+            // written once: by the segment's first tile, the slab where the group begins
+            if (!kGrad && a.stats && begin >= b.first_row && (first_group + g) * b.w >= b.c0)
+                reinterpret_cast<float2*>(a.stats)[(int64_t) s * a.groups + first_group + g] = v;
+        }
+    }
+    __syncthreads();
+}
+
+// kJoin: from the tiles' parts, otherwise from the joined statistics.
+template <typename T, bool kJoin, bool kOne>
+__global__ void __launch_bounds__(kBlock, kOne ? 5 : 4) k_norm_apply(NormArgs a, Tiling t, const float2* from)
+{
+    constexpr int V = kPiece<T>, G = kOne ? 1 : V;
+    __shared__ float2 s_of[kJoin ? kBlock * V : 1];
     const TileBlock<T> b(a, t);
     const Segments segments(a, b.rows);
-    if (!b.c.end) return;
+    if (kJoin && a.stats && a.segments && b.slab == 0) {      // segments without rows are in no tile
+        for (int64_t s = (int64_t) blockIdx.x * kBlock + threadIdx.x; s < segments.n; s += (int64_t) gridDim.x * kBlock)
+            if (segments.begin((int32_t) s) >= segments.end((int32_t) s))
+                for (int32_t g = 0; g < a.groups; ++g) reinterpret_cast<float2*>(a.stats)[s * a.groups + g] = make_float2(0.f, 0.f);
+    }
     float gamma[V], beta[V];
-    int32_t j[V];
-    load_parameters<V, false>(a.gamma, b.c, 1.f, gamma);
-    load_parameters<V, false>(a.beta, b.c, 0.f, beta);
+    int32_t j[G];
+    load_parameters<V, kOne>(a.gamma, b.c, 1.f, gamma);
+    load_parameters<V, kOne>(a.beta, b.c, 0.f, beta);
 #pragma unroll
-    for (int i = 0; i < V; ++i) j[i] = min(b.c.first + i, b.width - 1) / b.w;
+    for (int i = 0; i < G; ++i) j[i] = min(b.c.first + i, b.width - 1) / b.w;
     for (int32_t s = segments.first(b.first_row); s < segments.n && b.first_row < b.last_row; ++s) {
-        const int32_t begin = segments.begin(s);
+        const int32_t begin = segments.begin(s), end = segments.end(s);
         if (begin >= b.last_row) break;
-        const int32_t r0 = max(begin, b.first_row), r1 = min(segments.end(s), b.last_row);
-        float mean[V], scale[V];
+        const int32_t r0 = max(begin, b.first_row), r1 = min(end, b.last_row);
+        if (r0 >= r1) continue;
+        if (kJoin) join_here<T, false>(a, t, b, from, s, begin, end, s_of);
+        if (!b.c.end) continue;
+        float mean[G], scale[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float2 v = stats[(int64_t) s * a.groups + j[i]];
+        for (int i = 0; i < G; ++i) {
+            const float2 v = kJoin ? s_of[max(j[i] - b.c0 / b.w, 0)] : from[(int64_t) s * a.groups + j[i]];
             mean[i] = v.x;
-            scale[i] = v.y * gamma[i];
+            scale[i] = v.y;
         }
-        for (int32_t r = r0 + b.turn; r < r1; r += t.turns) {
-            uint32_t words[4];
-            float y[V];
-            load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + (int64_t) r * a.x.stride, b.c, words);
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = activate((value_of_words<T>(words, i) - mean[i]) * scale[i] + beta[i], a.activation);
-            store_columns<T, false>(reinterpret_cast<T*>(a.out.data) + (int64_t) r * a.out.stride, b.c, y);
-        }
+        for (int i = V - 1; i >= 0; --i) scale[i] = scale[kOne ? 0 : i] * gamma[i];
+        by_batches_of<1, 4>(r0 + b.turn, r1, t.turns, [&](int32_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); }, [&](int32_t r, const Batch<1>& of) {
+            float y[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = (value_of_words<T>(of.words[0], i) - mean[kOne ? 0 : i]) * scale[i] + beta[i];
+            activate(y, a.activation);
+            store_columns<T, kOne>(reinterpret_cast<T*>(a.out.data) + (int64_t) r * a.out.stride, b.c, y);
+        });
     }
 }
 
 // Sums of gamma dy and gamma dy h of each group of the slab, for each segment in the tile, and of dy and dy h of each column over
 // the tile's segments.
-template <typename T>
-__global__ void __launch_bounds__(kBlock) k_norm_grad_parts(NormArgs a, Tiling t, float2* parts, float2* columns)
+template <typename T, bool kOne>
+__global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_parts(NormArgs a, Tiling t, float2* parts, float2* columns)
 {
-    constexpr int V = kPiece<T>;
+    constexpr int V = kPiece<T>, G = kOne ? 1 : V;
     __shared__ float s_one[kBlock * V], s_two[kBlock * V];
     const TileBlock<T> b(a, t);
     const Segments segments(a, b.rows);
     const int32_t pitch = t.threads * V, first_group = b.c0 / b.w, groups = (b.c1 - 1) / b.w - first_group + 1;
     const int32_t lanes = team_lanes(groups, b.w);
     float gamma[V], beta[V], sum1[V], sum2[V];
-    int32_t j[V];
-    load_parameters<V, false>(a.gamma, b.c, 1.f, gamma);
-    load_parameters<V, false>(a.beta, b.c, 0.f, beta);
+    int32_t j[G];
+    load_parameters<V, kOne>(a.gamma, b.c, 1.f, gamma);
+    load_parameters<V, kOne>(a.beta, b.c, 0.f, beta);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        j[i] = min(b.c.first + i, b.width - 1) / b.w;
-        sum1[i] = sum2[i] = 0.f;
-    }
+    for (int i = 0; i < G; ++i) j[i] = min(b.c.first + i, b.width - 1) / b.w;
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum1[i] = sum2[i] = 0.f;
     auto put = [&](const float (&one)[V], const float (&two)[V]) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (i >= b.c.skip && i < b.c.end) {
+            if (kOne ? b.c.end != 0 : i >= b.c.skip && i < b.c.end) {
                 s_one[b.turn * pitch + b.c.first + i - b.c0] = one[i];
                 s_two[b.turn * pitch + b.c.first + i - b.c0] = two[i];
             }
@@ -577,25 +699,30 @@ __global__ void __launch_bounds__(kBlock) k_norm_grad_parts(NormArgs a, Tiling t
 #pragma unroll
         for (int i = 0; i < V; ++i) one[i] = two[i] = 0.f;
         if (b.c.end) {
-            float mean[V], rstd[V];
+            float mean[G], rstd[G];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
+            for (int i = 0; i < G; ++i) {
                 const float2 v = reinterpret_cast<const float2*>(a.stats)[(int64_t) s * a.groups + j[i]];
                 mean[i] = v.x;
                 rstd[i] = v.y;
             }
-            for (int32_t r = r0 + b.turn; r < r1; r += t.turns) {
-                uint32_t xw[4], dw[4];
-                load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + (int64_t) r * a.x.stride, b.c, xw);
-                load_columns<T, false>(reinterpret_cast<const T*>(a.d_out.data) + (int64_t) r * a.d_out.stride, b.c, dw);
+            by_batches_of<2, 2>(r0 + b.turn, r1, t.turns,
+                [&](int32_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); },
+                [&](int32_t, const Batch<2>& of) {
+                    float h[V], slope[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float h = (value_of_words<T>(xw, i) - mean[i]) * rstd[i];
-                    const float dy = value_of_words<T>(dw, i) * slope_at(h * gamma[i] + beta[i], a.activation);
-                    one[i] += dy;
-                    two[i] += dy * h;
-                }
-            }
+                    for (int i = 0; i < V; ++i) {
+                        h[i] = (value_of_words<T>(of.words[0], i) - mean[kOne ? 0 : i]) * rstd[kOne ? 0 : i];
+                        slope[i] = h[i] * gamma[i] + beta[i];
+                    }
+                    slopes_at(slope, a.activation);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float dy = value_of_words<T>(of.words[1], i) * slope[i];
+                        one[i] += dy;
+                        two[i] += dy * h[i];
+                    }
+                });
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 sum1[i] += one[i];
@@ -637,43 +764,54 @@ __global__ void __launch_bounds__(kBlock) k_norm_grad_parts(NormArgs a, Tiling t
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kBlock) k_norm_grad_apply(NormArgs a, Tiling t, const float2* moments)
+// kJoin: as above, and blocks behind the tiles' sum the columns for dgamma and dbeta.
+template <typename T, bool kJoin, bool kOne>
+__global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_apply(NormArgs a, Tiling t, const float2* from, const float2* columns)
 {
-    constexpr int V = kPiece<T>;
+    constexpr int V = kPiece<T>, G = kOne ? 1 : V;
+    __shared__ float2 s_of[kJoin ? kBlock * V : 1];
+    if (kJoin && (int64_t) blockIdx.x >= t.tiles) {
+        if (blockIdx.y == 0)
+            sum_columns((int32_t) ((int64_t) blockIdx.x - t.tiles), columns, ((int64_t) a.count.get() + t.tile_rows - 1) / t.tile_rows, a.x.width, a.dgamma, a.dbeta, s_of);
+        return;
+    }
     const TileBlock<T> b(a, t);
     const Segments segments(a, b.rows);
-    if (!b.c.end) return;
     float gamma[V], beta[V];
-    int32_t j[V];
-    load_parameters<V, false>(a.gamma, b.c, 1.f, gamma);
-    load_parameters<V, false>(a.beta, b.c, 0.f, beta);
+    int32_t j[G];
+    load_parameters<V, kOne>(a.gamma, b.c, 1.f, gamma);
+    load_parameters<V, kOne>(a.beta, b.c, 0.f, beta);
 #pragma unroll
-    for (int i = 0; i < V; ++i) j[i] = min(b.c.first + i, b.width - 1) / b.w;
+    for (int i = 0; i < G; ++i) j[i] = min(b.c.first + i, b.width - 1) / b.w;
     for (int32_t s = segments.first(b.first_row); s < segments.n && b.first_row < b.last_row; ++s) {
-        const int32_t begin = segments.begin(s);
+        const int32_t begin = segments.begin(s), end = segments.end(s);
         if (begin >= b.last_row) break;
-        const int32_t r0 = max(begin, b.first_row), r1 = min(segments.end(s), b.last_row);
-        float mean[V], rstd[V], m1[V], m2[V];
+        const int32_t r0 = max(begin, b.first_row), r1 = min(end, b.last_row);
+        if (r0 >= r1) continue;
+        if (kJoin) join_here<T, true>(a, t, b, from, s, begin, end, s_of);
+        if (!b.c.end) continue;
+        float mean[G], rstd[G], m1[G], m2[G];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float2 v = reinterpret_cast<const float2*>(a.stats)[(int64_t) s * a.groups + j[i]], m = moments[(int64_t) s * a.groups + j[i]];
+        for (int i = 0; i < G; ++i) {
+            const float2 v = reinterpret_cast<const float2*>(a.stats)[(int64_t) s * a.groups + j[i]];
+            const float2 m = kJoin ? s_of[max(j[i] - b.c0 / b.w, 0)] : from[(int64_t) s * a.groups + j[i]];
             mean[i] = v.x; rstd[i] = v.y;
             m1[i] = m.x; m2[i] = m.y;
         }
-        for (int32_t r = r0 + b.turn; r < r1; r += t.turns) {
-            uint32_t xw[4], dw[4];
-            float dx[V];
-            load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + (int64_t) r * a.x.stride, b.c, xw);
-            load_columns<T, false>(reinterpret_cast<const T*>(a.d_out.data) + (int64_t) r * a.d_out.stride, b.c, dw);
+        by_batches_of<2, 2>(r0 + b.turn, r1, t.turns,
+            [&](int32_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); },
+            [&](int32_t r, const Batch<2>& of) {
+                float h[V], dx[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float h = (value_of_words<T>(xw, i) - mean[i]) * rstd[i];
-                const float dy = value_of_words<T>(dw, i) * slope_at(h * gamma[i] + beta[i], a.activation);
-                dx[i] = rstd[i] * (dy * gamma[i] - m1[i] - h * m2[i]);
-            }
-            store_columns<T, false>(reinterpret_cast<T*>(a.out.data) + (int64_t) r * a.out.stride, b.c, dx);
-        }
+                for (int i = 0; i < V; ++i) {
+                    h[i] = (value_of_words<T>(of.words[0], i) - mean[kOne ? 0 : i]) * rstd[kOne ? 0 : i];
+                    dx[i] = h[i] * gamma[i] + beta[i];
+                }
+                slopes_at(dx, a.activation);
+#pragma unroll
+                for (int i = 0; i < V; ++i) dx[i] = rstd[kOne ? 0 : i] * (value_of_words<T>(of.words[1], i) * dx[i] * gamma[i] - m1[kOne ? 0 : i] - h[i] * m2[kOne ? 0 : i]);
+                store_columns<T, kOne>(reinterpret_cast<T*>(a.out.data) + (int64_t) r * a.out.stride, b.c, dx);
+            });
     }
 }
 
@@ -745,10 +883,19 @@ Tiling tiling_of(const gns_ctx* c, int32_t width, int32_t groups, int32_t type, 
     t.threads = std::min(pieces, kBlock);
     t.turns = kBlock / t.threads;
     t.tile_rows = 16;
-    while (t.tile_rows < 256 && (int64_t) t.tile_rows * 4 * c->num_cus < (int64_t) rows * t.slabs) t.tile_rows *= 2;
+    while (t.tile_rows < 256 && (int64_t) t.tile_rows * 4 * c->num_cus <= (int64_t) rows * t.slabs) t.tile_rows *= 2;
     t.tiles = ((int64_t) rows + t.tile_rows - 1) / t.tile_rows;
     t.entries = (int64_t) t.slabs + groups;
     return t;
+}
+
+// Whether the blocks that write the rows join the parts themselves: where that is less than a launch, a few thousand pairs a block and a
+// few million together.  The worst case: of ragged segments one has all tiles.
+bool join_by_tile(const gns_norm* n, const Tiling& t, int32_t groups)
+{
+    const int64_t each = n->segments_dev ? t.tiles : std::min<int64_t>(t.tiles, n->segment_rows / t.tile_rows + 2);
+    return each * (groups + t.slabs) <= 8192 && t.tiles * t.slabs * each * (groups / t.slabs + 1) <= (16 << 20) &&
+           (n->segments_dev ? n->num_segments <= t.tiles : n->segment_rows >= t.tile_rows);
 }
 
 struct TiledSpace {
@@ -837,6 +984,7 @@ hipError_t launch_norm_typed(const gns_ctx* c, const NormArgs& a, const gns_norm
         }
         return hipGetLastError();
     }
+    const bool one = w % kPiece<T> == 0;
     const Tiling t = tiling_of(c, width, a.groups, type, rows);
     const int64_t segments = segment_count(n, rows);
     const TiledSpace space = tiled_space(t, t.tiles, segments, width, a.groups, false);
@@ -844,13 +992,20 @@ hipError_t launch_norm_typed(const gns_ctx* c, const NormArgs& a, const gns_norm
     float2* const stats = a.stats ? reinterpret_cast<float2*>(a.stats) : reinterpret_cast<float2*>(static_cast<char*>(a.workspace) + space.moments);
     const dim3 grid((unsigned) t.tiles, (unsigned) t.slabs);
     if (!segments) return hipSuccess;
-    hipLaunchKernelGGL((k_norm_parts<T>), grid, dim3(kBlock), 0, s, a, t, parts);
+    if (one) hipLaunchKernelGGL((k_norm_parts<T, true>), grid, dim3(kBlock), 0, s, a, t, parts);
+    else     hipLaunchKernelGGL((k_norm_parts<T, false>), grid, dim3(kBlock), 0, s, a, t, parts);
+    if (join_by_tile(n, t, a.groups)) {
+        if (one) hipLaunchKernelGGL((k_norm_apply<T, true, true>), grid, dim3(kBlock), 0, s, a, t, parts);
+        else     hipLaunchKernelGGL((k_norm_apply<T, true, false>), grid, dim3(kBlock), 0, s, a, t, parts);
+        return hipGetLastError();
+    }
     const int64_t units = segments * a.groups, most = (int64_t) c->num_cus * 32;
     if (t.tiles * t.slabs > segments * 128)
         hipLaunchKernelGGL((k_norm_join<T, kBlock, false>), dim3((unsigned) std::min(units, most)), dim3(kBlock), 0, s, a, t, parts, stats);
     else
         hipLaunchKernelGGL((k_norm_join<T, kWave, false>), dim3((unsigned) std::min((units + 3) / 4, most)), dim3(kBlock), 0, s, a, t, parts, stats);
-    hipLaunchKernelGGL((k_norm_apply<T>), grid, dim3(kBlock), 0, s, a, t, stats);
+    if (one) hipLaunchKernelGGL((k_norm_apply<T, false, true>), grid, dim3(kBlock), 0, s, a, t, stats);
+    else     hipLaunchKernelGGL((k_norm_apply<T, false, false>), grid, dim3(kBlock), 0, s, a, t, stats);
     return hipGetLastError();
 }
 
@@ -885,6 +1040,7 @@ hipError_t launch_grad_typed(const gns_ctx* c, const NormArgs& a, const gns_norm
             hipLaunchKernelGGL(k_norm_columns, join, dim3(kBlock), 0, s, parts, unit_parts(g, a.groups, u.lanes), a.count, 0, width, a.dgamma, a.dbeta);
         return hipGetLastError();
     }
+    const bool one = w % kPiece<T> == 0;
     const Tiling t = tiling_of(c, width, a.groups, type, rows);
     const int64_t segments = segment_count(n, rows);
     const TiledSpace space = tiled_space(t, t.tiles, segments, width, a.groups, true);
@@ -893,7 +1049,16 @@ hipError_t launch_grad_typed(const gns_ctx* c, const NormArgs& a, const gns_norm
     float2* const moments = reinterpret_cast<float2*>(at + space.moments);
     float2* const columns = reinterpret_cast<float2*>(at + space.columns);
     const dim3 grid((unsigned) t.tiles, (unsigned) t.slabs);
-    hipLaunchKernelGGL((k_norm_grad_parts<T>), grid, dim3(kBlock), 0, s, a, t, a.out.data ? parts : nullptr, columns_wanted ? columns : nullptr);
+    float2* const parts_to = a.out.data ? parts : nullptr;
+    float2* const columns_to = columns_wanted ? columns : nullptr;
+    if (one) hipLaunchKernelGGL((k_norm_grad_parts<T, true>), grid, dim3(kBlock), 0, s, a, t, parts_to, columns_to);
+    else     hipLaunchKernelGGL((k_norm_grad_parts<T, false>), grid, dim3(kBlock), 0, s, a, t, parts_to, columns_to);
+    if (a.out.data && segments && join_by_tile(n, t, a.groups)) {
+        const dim3 both((unsigned) (t.tiles + (columns_wanted ? join.x : 0)), (unsigned) t.slabs);
+        if (one) hipLaunchKernelGGL((k_norm_grad_apply<T, true, true>), both, dim3(kBlock), 0, s, a, t, parts, columns);
+        else     hipLaunchKernelGGL((k_norm_grad_apply<T, true, false>), both, dim3(kBlock), 0, s, a, t, parts, columns);
+        return hipGetLastError();
+    }
     if (columns_wanted)
         hipLaunchKernelGGL(k_norm_columns, join, dim3(kBlock), 0, s, columns, (int64_t) 0, a.count, t.tile_rows, width, a.dgamma, a.dbeta);
     if (a.out.data && segments) {
@@ -902,7 +1067,8 @@ hipError_t launch_grad_typed(const gns_ctx* c, const NormArgs& a, const gns_norm
             hipLaunchKernelGGL((k_norm_join<T, kBlock, true>), dim3((unsigned) std::min(units, most)), dim3(kBlock), 0, s, a, t, parts, moments);
         else
             hipLaunchKernelGGL((k_norm_join<T, kWave, true>), dim3((unsigned) std::min((units + 3) / 4, most)), dim3(kBlock), 0, s, a, t, parts, moments);
-        hipLaunchKernelGGL((k_norm_grad_apply<T>), grid, dim3(kBlock), 0, s, a, t, moments);
+        if (one) hipLaunchKernelGGL((k_norm_grad_apply<T, false, true>), grid, dim3(kBlock), 0, s, a, t, moments, columns);
+        else     hipLaunchKernelGGL((k_norm_grad_apply<T, false, false>), grid, dim3(kBlock), 0, s, a, t, moments, columns);
     }
     return hipGetLastError();
 }
