@@ -447,145 +447,165 @@ __global__ void __launch_bounds__(kFewBlock) k_fp8_few(DenseFp8Args a, QuantizeF
     }
 }
 
-// k_fp8_rows: many rows against weights that fit LDS: rows come in, are quantised and multiplied, and leave, without a trip
-// through memory in 8 bits.  A block per CU (or two) holds all weights; its waves walk tiles of 16 rows: a row is read by L lanes, P pieces each,
-// quantised, turned through a piece of LDS of the wave's own and multiplied, 16 x 16 x 128, with the weights as the left
-// factor, so that a lane gets four consecutive outputs of a row.
-__host__ __device__ constexpr int64_t rows_lds(int64_t stride, int32_t n, int waves)
+// k_fp8_rows: many rows against weights that fit LDS: rows come in, are quantised and multiplied, and leave, without a trip through memory or
+// LDS in 8 bits.  A block holds all its weights (as bf16 values for fp32 outputs) and its waves walk tiles of 16 rows.  A lane
+// reads of one row, in every 32 columns, the eight that it multiplies, so a block of 128 columns is in four lanes: two exchanges find
+// its largest value, and the rounded values are the products' right factor as they are.  The weights are the left factor, so that a lane
+// gets four consecutive outputs of a row.
+__host__ __device__ constexpr int64_t rows_pitch(int64_t stride, bool precise) { return stride * (precise ? 2 : 1) + 16; }      // of a channel in LDS
+__host__ __device__ constexpr int64_t rows_lds(int64_t stride, int32_t channels, bool precise)
 {
-    return few_stride(stride) * ((n + 15) / 16 * 16 + waves * 16) + (int64_t) (n + 15) / 16 * 16 * 8 + waves * 64;
+    return (rows_pitch(stride, precise) + 8) * ((channels + 31) / 32 * 32);
 }
 
-template <typename T, int L, int P, int kWaves>
-__global__ void __launch_bounds__(kWaves * kWave) k_fp8_rows(DenseFp8Args a, QuantizeFp8Args x)
+template <typename T, int B, int kWaves>
+__global__ void __launch_bounds__(kWaves * kWave) k_fp8_rows(DenseFp8Args a, QuantizeFp8Args x, int32_t channels)
 {
-    constexpr int V = kPiece<T>, kTurns = 16 * L / kWave;      // of a wave over a tile's rows
-    constexpr int kGroups = 4, kTeam = kBlockLanes<T>;         // of 16 output columns, multiplied together; lanes of a block of columns
+    constexpr int V = kPiece<T>, kEach = 8 / V;                // pieces of eight columns
     constexpr bool kPrecise = sizeof(T) == 4;
-    extern __shared__ int4v s_rows[];
-    const int32_t rows = a.count.get(), n = a.out.width, n16 = (n + 15) / 16 * 16, steps = (int32_t) (a.stride / GNS_FP8_BLOCK);
-    const int32_t pitch = (int32_t) few_stride(a.stride), f1 = x.x1.width, k = a.k;
-    uint8_t* const s_w = reinterpret_cast<uint8_t*>(s_rows);
+    constexpr int kGroups = 4;                                 // of 16 output channels, multiplied together
+    extern __shared__ int4v s_weights[];
+    const int32_t first = (int32_t) blockIdx.y * channels, n = min(a.out.width - first, channels), n16 = (n + 31) / 32 * 32;
+    const int32_t rows = a.count.get(), pitch = (int32_t) rows_pitch(a.stride, kPrecise), f1 = x.x1.width, k = a.k;
+    // the channel (of this block's) whose weights lie in a row: element 4 kg + i of product g of a pair is 8 kg + 4 g + i, or as they come
+    auto channel_of = [](int32_t row) { return kPrecise ? row : (row & ~31) | (row >> 2 & 3) << 3 | (row >> 4 & 1) << 2 | (row & 3); };
+    char* const s_w = reinterpret_cast<char*>(s_weights);
+    float* const s_bias = reinterpret_cast<float*>(s_w + n16 * pitch);
+    int* const s_scale = reinterpret_cast<int*>(s_bias + n16);
     const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6));
-    uint8_t* const s_q = s_w + n16 * pitch + wave * 16 * pitch;
-    float* const s_bias = reinterpret_cast<float*>(s_w + (n16 + kWaves * 16) * pitch);
-    int* const s_w_scale = reinterpret_cast<int*>(s_bias + n16);
-    uint8_t* const s_scale = reinterpret_cast<uint8_t*>(s_w_scale + n16) + wave * 64;          // of the tile's rows, four bytes each
-    const int32_t chunks = (int32_t) (a.stride / 16);
-    for (int32_t i = (int32_t) threadIdx.x; i < n16 * chunks; i += kWaves * kWave) {
-        const int32_t row = i / chunks, chunk = i - row * chunks;
-        *reinterpret_cast<int4v*>(s_w + row * pitch + chunk * 16) =
-            *reinterpret_cast<const int4v*>(a.wq + (int64_t) (row < n ? row : n - 1) * a.stride + chunk * 16);
-    }
-    for (int32_t i = (int32_t) threadIdx.x; i < n16; i += kWaves * kWave) {
-        s_w_scale[i] = *reinterpret_cast<const int*>(a.w_exponents + (int64_t) (i < n ? i : n - 1) * a.exponent_stride);
-        s_bias[i] = a.bias ? a.bias[i < n ? i : n - 1] : 0.f;
-    }
-    __syncthreads();
     const int32_t tiles = (rows + 15) / 16;
-    const bool stores = n % 4 == 0 && reinterpret_cast<uintptr_t>(a.out.data) % 16 == 0 && (uint64_t) a.out.stride * sizeof(T) % 16 == 0;
+    const bool stores = reinterpret_cast<uintptr_t>(a.out.data) % 16 == 0 && (uint64_t) a.out.stride * sizeof(T) % 16 == 0;      // channels begin at multiples of 16
     // A tile's rows are read when the one before has been quantised, and come while that one is multiplied and stored.  Rows past
-    // the last are read as the last, lanes past the last column read the first.
-    Chunk v[kTurns][P];
-    auto fetch = [&](int32_t tile) {
-        const int lane = opaque_lane_id(), l = lane & (L - 1);
+    // the last are read as the last, columns past the last as the first.
+    Chunk raw[B * 4 * kEach];
+    auto fetch = [&](int32_t tile) __attribute__((always_inline)) {
+        const int lane = opaque_lane_id();
+        const int64_t r = min((int64_t) tile * 16 + (lane & 15), (int64_t) rows - 1);
+        const T* const x1 = reinterpret_cast<const T*>(x.x1.data) + r * x.x1.stride;
+        const T* const x2 = reinterpret_cast<const T*>(x.x2.data) + r * x.x2.stride - f1;
 #pragma unroll
-        for (int t = 0; t < kTurns; ++t) {
-            const int64_t row = (int64_t) tile * 16 + t * (kWave / L) + lane / L, r = row < rows ? row : rows - 1;
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int32_t c = (p * L + l) * V, cc = c < k ? c : 0;
-                __builtin_memcpy(&v[t][p], cc < f1 ? reinterpret_cast<const T*>(x.x1.data) + r * x.x1.stride + cc
-                                                   : reinterpret_cast<const T*>(x.x2.data) + r * x.x2.stride + (cc - f1), 16);
-            }
+        for (int p = 0; p < B * 4 * kEach; ++p) {
+            const int32_t c = p / kEach * 32 + (lane >> 4) * 8 + p % kEach * V, cc = c < k ? c : 0;
+            __builtin_memcpy(&raw[p], (cc < f1 ? x1 : x2) + cc, 16);
         }
     };
     // the blocks' first waves take the first tiles: a remainder spreads over all CUs
     int32_t tile = wave * (int32_t) gridDim.x + (int32_t) blockIdx.x;
     if (tile < tiles) fetch(tile);
+    const int32_t chunks = (int32_t) (a.stride / 16);
+    for (int32_t i = (int32_t) threadIdx.x; i < n16 * chunks; i += kWaves * kWave) {
+        const int32_t row = i / chunks, chunk = i - row * chunks, channel = first + min(channel_of(row), n - 1);
+        const int4v v = *reinterpret_cast<const int4v*>(a.wq + (int64_t) channel * a.stride + chunk * 16);
+        if constexpr (kPrecise) {
+            const float power = power_of(a.w_exponents[(int64_t) channel * a.exponent_stride + chunk / 8]);
+            bf8v* to = reinterpret_cast<bf8v*>(s_w + row * pitch + chunk * 32);
+            to[0] = values_of((uint32_t) v[0], (uint32_t) v[1], power);
+            to[1] = values_of((uint32_t) v[2], (uint32_t) v[3], power);
+        } else {
+            // a lane's eight columns of every 32 of a block of 128 lie together
+            int2* to = reinterpret_cast<int2*>(s_w + row * pitch + chunk / 8 * GNS_FP8_BLOCK + chunk % 2 * 64 + chunk % 8 / 2 * 8);
+            to[0] = make_int2(v[0], v[1]);
+            to[4] = make_int2(v[2], v[3]);
+        }
+    }
+    for (int32_t i = (int32_t) threadIdx.x; i < n16; i += kWaves * kWave) {
+        const int32_t channel = first + min(i, n - 1);
+        s_bias[i] = a.bias ? a.bias[channel] : 0.f;
+    }
+    for (int32_t i = (int32_t) threadIdx.x; i < n16; i += kWaves * kWave) {
+        const int32_t channel = first + min(channel_of(i), n - 1);
+        s_scale[i] = *reinterpret_cast<const int*>(a.w_exponents + (int64_t) channel * a.exponent_stride);
+    }
+    __syncthreads();
     for (; tile < tiles; tile += (int32_t) gridDim.x * kWaves) {
-        const int lane = opaque_lane_id(), l = lane & (L - 1), l16 = lane & 15, kg = lane >> 4;
+        const int lane = opaque_lane_id(), l16 = lane & 15, kg = lane >> 4;
         const int64_t r0 = (int64_t) tile * 16;
+        uint2 q[kPrecise ? 1 : B * 4];                        // eight columns each
+        bf8v values[kPrecise ? B * 4 : 1];                    // or their values
+        uint32_t bytes[B];
 #pragma unroll
-        for (int t = 0; t < kTurns; ++t) {
-            const int32_t row = t * (kWave / L) + lane / L;
+        for (int p = 0; p < B; ++p) {
+            uint32_t most = 0;
+            float f[4][8];
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int32_t c = (p * L + l) * V;
-                const uint32_t words[4] = {v[t][p].x, v[t][p].y, v[t][p].z, v[t][p].w};
-                float f[V];
+            for (int h = 0; h < 4; ++h) {
+                const int32_t c = (p * 4 + h) * 32 + kg * 8;
 #pragma unroll
-                for (int i = 0; i < V; ++i) f[i] = c < k ? value_of_words<T>(words, i) : 0.f;
-                const BlockScale s = block_scale(largest_of_lanes<kTeam>(largest_of(f, 0u)));
-                if (c < (int32_t) a.stride) {
-                    store_piece<T>(s_q + row * pitch + c, f, s.inverse, c, k);
-                    if ((l & (kTeam - 1)) == 0) s_scale[row * 4 + c / GNS_FP8_BLOCK] = (uint8_t) s.byte;
+                for (int i = 0; i < 8; ++i) {
+                    const Chunk& v = raw[(p * 4 + h) * kEach + i / V];
+                    const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+                    f[h][i] = c + i / V * V < k ? value_of_words<T>(words, i % V) : 0.f;
                 }
+                most = largest_of(f[h], most);
+            }
+            most = max(most, (uint32_t) __shfl_xor((int) most, 16));
+            most = max(most, (uint32_t) __shfl_xor((int) most, 32));
+            const BlockScale s = block_scale(most);
+            bytes[p] = s.byte;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                uint2 v = make_uint2(pack4(f[h], s.inverse), pack4(f[h] + 4, s.inverse));
+                if (!(s.inverse > 0.f)) v = s.inverse == 0.f ? make_uint2(0, 0) : make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                if constexpr (kPrecise) values[p * 4 + h] = values_of(v.x, v.y, power_of(s.byte));
+                else                    q[p * 4 + h] = v;
             }
         }
-        __builtin_amdgcn_wave_barrier();
         if (tile + (int32_t) gridDim.x * kWaves < tiles) fetch(tile + (int32_t) gridDim.x * kWaves);
-        const uint8_t* q = s_q + l16 * pitch + kg * 16;
-        const int scale = *reinterpret_cast<const int*>(s_scale + l16 * 4);
-        T* out = reinterpret_cast<T*>(a.out.data) + (r0 + l16) * a.out.stride;
+        T* out = reinterpret_cast<T*>(a.out.data) + (r0 + l16) * a.out.stride + first;
         for (int32_t c0 = 0; c0 < n16; c0 += 16 * kGroups) {
-            const uint8_t* w[kGroups];
-            int w_scale[kGroups];
+            const char* w[kGroups];
             float4v acc[kGroups];
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {               // groups past the last repeat it
-                const int32_t at = (c0 + g * 16 < n16 ? c0 + g * 16 : n16 - 16) + l16;
-                w[g] = s_w + at * pitch + kg * 16;
-                w_scale[g] = s_w_scale[at];
+                w[g] = s_w + ((c0 + g * 16 < n16 ? c0 + g * 16 : n16 - 16) + l16) * pitch + kg * (kPrecise ? 16 : 32);
                 acc[g] = float4v{0.f, 0.f, 0.f, 0.f};
             }
-            for (int32_t s = 0; s < steps; ++s) {
-                const int4v right[2] = {*reinterpret_cast<const int4v*>(q + s * GNS_FP8_BLOCK), *reinterpret_cast<const int4v*>(q + s * GNS_FP8_BLOCK + 64)};
-                if constexpr (kPrecise) {
-                    const float power = power_of((uint32_t) scale >> (8 * s) & 255u);
-                    bf8v values[4];
+            if constexpr (kPrecise) {
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) values[h] = values_of((uint32_t) right[h / 2][h % 2 * 2], (uint32_t) right[h / 2][h % 2 * 2 + 1], power);
+                for (int p = 0; p < B * 4; ++p)
 #pragma unroll
-                    for (int g = 0; g < kGroups; ++g) {
-                        const int4v left[2] = {*reinterpret_cast<const int4v*>(w[g] + s * GNS_FP8_BLOCK), *reinterpret_cast<const int4v*>(w[g] + s * GNS_FP8_BLOCK + 64)};
-                        const float w_power = power_of((uint32_t) w_scale[g] >> (8 * s) & 255u);
+                    for (int g = 0; g < kGroups; ++g)
+                        acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf8v*>(w[g] + p * 64), values[p], acc[g], 0, 0, 0);
+            } else {
 #pragma unroll
-                        for (int h = 0; h < 4; ++h)
-                            acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values_of((uint32_t) left[h / 2][h % 2 * 2], (uint32_t) left[h / 2][h % 2 * 2 + 1], w_power),
-                                                                            values[h], acc[g], 0, 0, 0);
-                    }
-                } else {
-                    const int8v both = __builtin_shufflevector(right[0], right[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                for (int p = 0; p < B; ++p) {
+                    const int8v right = {(int) q[p * 4].x, (int) q[p * 4].y, (int) q[p * 4 + 1].x, (int) q[p * 4 + 1].y,
+                                         (int) q[p * 4 + 2].x, (int) q[p * 4 + 2].y, (int) q[p * 4 + 3].x, (int) q[p * 4 + 3].y};
 #pragma unroll
                     for (int g = 0; g < kGroups; ++g) {
-                        const int8v left = __builtin_shufflevector(*reinterpret_cast<const int4v*>(w[g] + s * GNS_FP8_BLOCK),
-                                                                   *reinterpret_cast<const int4v*>(w[g] + s * GNS_FP8_BLOCK + 64), 0, 1, 2, 3, 4, 5, 6, 7);
-                        acc[g] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(left, both, acc[g], 0, 0, 0, w_scale[g] >> (8 * s), 0, scale >> (8 * s));
+                        const int8v left = __builtin_shufflevector(*reinterpret_cast<const int4v*>(w[g] + p * GNS_FP8_BLOCK),
+                                                                   *reinterpret_cast<const int4v*>(w[g] + p * GNS_FP8_BLOCK + 16), 0, 1, 2, 3, 4, 5, 6, 7);
+                        const int32_t channel = (c0 + g * 16 < n16 ? c0 + g * 16 : n16 - 16) + l16;
+                        acc[g] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(left, right, acc[g], 0, 0, 0, s_scale[channel] >> (8 * p), 0, (int) bytes[p]);
                     }
                 }
             }
-            // element i of lane l is output column 4 * (l / 16) + i of row l % 16
+            // The products have all lanes, also those of rows past the last: the compiler takes the scaled ones for a lane's own affair
+            // and would move them, with the reads of their factors, behind the branch.
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                const int32_t c = c0 + g * 16 + 4 * kg;
+            for (int g = 0; g < kGroups; ++g) asm volatile("" : "+v"(acc[g]));
+            // element i of lane l is row l % 16, and in its product's order output 4 * (l / 16) + i
+            constexpr int N = kPrecise ? 4 : 8;               // outputs that follow each other: 16 bytes
+#pragma unroll
+            for (int g = 0; g < kGroups; g += N / 4) {
+                const int32_t c = c0 + g * 16 + N * kg;
                 if (c0 + g * 16 >= n16 || r0 + l16 >= rows) continue;
-                const float4 b = *reinterpret_cast<const float4*>(s_bias + c);
-                struct alignas(4 * sizeof(T)) Four { T v[4]; } y;
-                y.v[0] = from_float<T>(output_of(acc[g][0] * (kPrecise ? kSumUp : 1.f), b.x, a.relu));
-                y.v[1] = from_float<T>(output_of(acc[g][1] * (kPrecise ? kSumUp : 1.f), b.y, a.relu));
-                y.v[2] = from_float<T>(output_of(acc[g][2] * (kPrecise ? kSumUp : 1.f), b.z, a.relu));
-                y.v[3] = from_float<T>(output_of(acc[g][3] * (kPrecise ? kSumUp : 1.f), b.w, a.relu));
-                if (stores) {
-                    if (c < n) *reinterpret_cast<Four*>(out + c) = y;
+                struct alignas(16) Outputs { T v[N]; } y;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    y.v[i] = from_float<T>(output_of(acc[g + i / 4][i % 4] * (kPrecise ? kSumUp : 1.f), s_bias[c + i], a.relu));
+                if (stores && c + N <= n) {
+                    const Chunk out16 = __builtin_bit_cast(Chunk, y);
+                    // past the caches where rows are this long (85,000 rows, 256 channels, fp32: of 256 columns 49 -> 45 us, of 128 33 -> 35)
+                    if (kPrecise && B == 2) __builtin_nontemporal_store(out16, reinterpret_cast<Chunk*>(out + c));
+                    else                    *reinterpret_cast<Chunk*>(out + c) = out16;
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < N; ++i)
                         if (c + i < n) out[c + i] = y.v[i];
                 }
             }
         }
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -637,37 +657,38 @@ hipError_t launch_dense_fp8(const gns_ctx* c, const DenseFp8Args& a, int32_t out
     return out_type == GNS_FP32 ? launch_typed<float>(c, a, s) : launch_typed<Bf16>(c, a, s);
 }
 
-// Rows and weights of k_fp8_rows: rows of whole pieces, as many as a tile's registers hold, weights that leave room in LDS, and
-// two tiles for each wave of a block per CU, or reading the weights into every LDS costs more than it saves
+// Output channels of a block of k_fp8_rows, 0 if the call is not for it: rows of whole pieces, as many as a tile's registers hold, weights that
+// fit LDS in two blocks' parts at most (of rows read twice), and two tiles for each wave of a block per CU, or reading the
+// weights into every LDS costs more than it saves.  Elsewhere the rows are quantised and multiplied in two launches (85,000 rows, 256 channels, us:
+// fp32 of 128 columns 33, in two launches 66, of 256 45 and 68; bf16 of 128 21 and 46, of 256 29 and 53, of 512 52 and 56).
 template <typename T>
-static bool rows_fit(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a)
+static int32_t rows_channels(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a)
 {
-    return a.count.rows >= c->num_cus * 32 && a.stride <= 512 && a.k % kPiece<T> == 0 && x.x1.width % kPiece<T> == 0 &&
-           rows_lds(a.stride, a.out.width, 8) <= (int64_t) c->lds_bitmap_limit;
-}
-
-template <typename T, int L, int P>
-static void launch_rows_of(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a, hipStream_t s)
-{
-    constexpr bool kMany = P == 1 && (sizeof(T) == 2 || L < 64);       // registers for sixteen waves
-    const int64_t lds16 = rows_lds(a.stride, a.out.width, 16), lds8 = rows_lds(a.stride, a.out.width, 8);
-    if (kMany && lds16 <= (int64_t) c->lds_bitmap_limit) {
-        const dim3 grid((unsigned) (c->num_cus * (lds16 <= 80 * 1024 ? 2 : 1)));
-        hipLaunchKernelGGL((k_fp8_rows<T, L, P, kMany ? 16 : 8>), grid, dim3(16 * kWave), (size_t) lds16, s, a, x);
-    } else {
-        const dim3 grid((unsigned) (c->num_cus * (lds8 <= 80 * 1024 ? 2 : 1)));
-        hipLaunchKernelGGL((k_fp8_rows<T, L, P, 8>), grid, dim3(8 * kWave), (size_t) lds8, s, a, x);
+    if (a.count.rows < c->num_cus * 32 || a.stride > (sizeof(T) == 4 ? 256 : 512) || a.k % kPiece<T> || x.x1.width % kPiece<T>) return 0;
+    for (int32_t parts = 1; parts <= 2; ++parts) {
+        const int32_t channels = (int32_t) ((a.out.width + parts - 1) / parts + 31) / 32 * 32;
+        if (rows_lds(a.stride, channels, sizeof(T) == 4) <= (int64_t) c->lds_bitmap_limit) return channels;
     }
+    return 0;
+}
+
+template <typename T, int B>
+static hipError_t launch_rows_of(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a, int32_t channels, hipStream_t s)
+{
+    constexpr int kWaves = B == 1 ? 16 : 8;                    // as registers allow
+    const int64_t lds = rows_lds(a.stride, channels, sizeof(T) == 4);
+    const unsigned parts = (unsigned) ((a.out.width + channels - 1) / channels), blocks = (unsigned) c->num_cus * (lds <= 80 * 1024 ? 2 : 1);
+    hipLaunchKernelGGL((k_fp8_rows<T, B, kWaves>), dim3(blocks / parts, parts), dim3(kWaves * kWave), (size_t) lds, s, a, x, channels);
+    return hipGetLastError();
 }
 
 template <typename T>
-static hipError_t launch_rows(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a, hipStream_t s)
+static hipError_t launch_rows(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a, int32_t channels, hipStream_t s)
 {
-    constexpr int V = kPiece<T>, L = kBlockLanes<T>;
-    if (a.stride <= L * V)          launch_rows_of<T, L, 1>(c, x, a, s);
-    else if (a.stride <= 2 * L * V) launch_rows_of<T, 2 * L, 1>(c, x, a, s);
-    else                            launch_rows_of<T, 64, 64 * V >= 512 ? 1 : 2>(c, x, a, s);
-    return hipGetLastError();
+    if (a.stride <= 128) return launch_rows_of<T, 1>(c, x, a, channels, s);
+    if (a.stride <= 256) return launch_rows_of<T, 2>(c, x, a, channels, s);
+    if constexpr (sizeof(T) == 2) return launch_rows_of<T, 4>(c, x, a, channels, s);
+    return hipErrorInvalidValue;                              // no rows so long
 }
 
 template <typename T, typename X>
@@ -688,8 +709,9 @@ hipError_t launch_sage_dense_fp8(const gns_ctx* c, const QuantizeFp8Args& x, con
         else                                          launch_few_fused<Bf16, Bf16>(x, a, (size_t) lds, s);
         return hipGetLastError();
     }
-    if (type == GNS_FP32 && out_type == GNS_FP32 && rows_fit<float>(c, x, a)) return launch_rows<float>(c, x, a, s);
-    if (type == GNS_BF16 && out_type == GNS_BF16 && rows_fit<Bf16>(c, x, a)) return launch_rows<Bf16>(c, x, a, s);
+    if (type == out_type)
+        if (const int32_t channels = type == GNS_FP32 ? rows_channels<float>(c, x, a) : rows_channels<Bf16>(c, x, a))
+            return type == GNS_FP32 ? launch_rows<float>(c, x, a, channels, s) : launch_rows<Bf16>(c, x, a, channels, s);
     const hipError_t e = launch_quantize_fp8(c, x, type, s);
     return e != hipSuccess ? e : launch_dense_fp8(c, a, out_type, s);
 }

@@ -673,7 +673,7 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_parts(NormAr
     const TileBlock<T> b(a, t);
     const Segments segments(a, b.rows);
     const int32_t pitch = t.threads * V, first_group = b.c0 / b.w, groups = (b.c1 - 1) / b.w - first_group + 1;
-    const int32_t lanes = team_lanes(groups, b.w);
+    const int32_t lanes = team_lanes(groups, kOne ? b.w / V : b.w);
     float gamma[V], beta[V], sum1[V], sum2[V];
     int32_t j[G];
     load_parameters<V, kOne>(a.gamma, b.c, 1.f, gamma);
@@ -695,9 +695,9 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_parts(NormAr
         if (begin >= b.last_row) break;
         const int32_t r0 = max(begin, b.first_row), r1 = min(segments.end(s), b.last_row);
         if (r0 >= r1) continue;
-        float one[V], two[V];
+        float one[G], two[G];                                 // of g = gamma dy and g h
 #pragma unroll
-        for (int i = 0; i < V; ++i) one[i] = two[i] = 0.f;
+        for (int i = 0; i < G; ++i) one[i] = two[i] = 0.f;
         if (b.c.end) {
             float mean[G], rstd[G];
 #pragma unroll
@@ -719,31 +719,33 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_parts(NormAr
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const float dy = value_of_words<T>(of.words[1], i) * slope[i];
-                        one[i] += dy;
-                        two[i] += dy * h[i];
+                        const float g = dy * gamma[i];
+                        sum1[i] += dy;
+                        sum2[i] += dy * h[i];
+                        one[kOne ? 0 : i] += g;
+                        two[kOne ? 0 : i] += g * h[i];
                     }
                 });
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                sum1[i] += one[i];
-                sum2[i] += two[i];
-                one[i] *= gamma[i];
-                two[i] *= gamma[i];
-            }
+        }
+        if (!parts) continue;
+        __syncthreads();
+        if constexpr (!kOne) {
+            put(one, two);
+        } else if (b.c.end) {
+            s_one[threadIdx.x] = one[0];
+            s_two[threadIdx.x] = two[0];
         }
         __syncthreads();
-        put(one, two);
-        __syncthreads();
-        if (!parts) continue;
         const int32_t team = opaque((int) threadIdx.x) / lanes, lane = opaque((int) threadIdx.x) % lanes;
         for (int32_t g0 = 0; g0 < groups; g0 += kBlock / lanes) {
             const int32_t g = min(g0 + team, groups - 1), group = first_group + g;
-            const int32_t from = max(group * b.w, b.c0) - b.c0, to = min((group + 1) * b.w, b.c1) - b.c0;
+            constexpr int kEach = kOne ? V : 1;               // columns of an entry
+            const int32_t from = (max(group * b.w, b.c0) - b.c0) / kEach, to = (min((group + 1) * b.w, b.c1) - b.c0) / kEach;
             float m1 = 0.f, m2 = 0.f;
             for (int32_t k = 0; k < t.turns; ++k)
                 for (int32_t c = from + lane; c < to; c += lanes) {
-                    m1 += s_one[k * pitch + c];
-                    m2 += s_two[k * pitch + c];
+                    m1 += s_one[k * (pitch / kEach) + c];
+                    m2 += s_two[k * (pitch / kEach) + c];
                 }
             m1 = lanes_sum(m1, lanes);
             m2 = lanes_sum(m2, lanes);
