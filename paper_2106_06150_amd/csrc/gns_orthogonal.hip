@@ -1,8 +1,8 @@
 // Orthogonalised updates: momentum, Newton-Schulz products on the matrix cores, the weights' step.
 //
 // Values v of X and of the matrices between are kept as two fp16 terms of 2^12 v: the value rounded, and what is left rounded.  A product
-// of two values is three products of terms (what is left out is 2^-22 of it), summed in fp32.  All products are of rows with rows: X is
-// kept as it is and turned, the others are symmetric.
+// of two values is three products of terms (what is left out is 2^-22 of it), summed in fp32.  Products are of rows with rows, as all
+// matrices but X are symmetric; where X is the right factor its rows are turned as they are read from LDS.
 #include "gns_layers.hpp"
 #include <algorithm>
 #include <type_traits>
@@ -137,12 +137,11 @@ struct SpreadArgs {
     int32_t short_side, long_side, tall;      // padded; tall: X is u turned
     double eps;
     char* x;                      // [short][long]
-    char* turned;                 // [long][short]
 };
 
 constexpr int kSpread = 64;
 
-// X in terms, as it is and turned, a tile of 64 x 64 a block.
+// X in terms, a tile of 64 x 64 a block.
 __global__ void __launch_bounds__(kBlock) k_spread(SpreadArgs a)
 {
     constexpr int kTurns = kSpread * kSpread / kBlock;
@@ -178,9 +177,6 @@ __global__ void __launch_bounds__(kBlock) k_spread(SpreadArgs a)
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = s_tile[r][c + k];
         store_terms(a.x + terms_at(x0 + r, y0 + c, a.long_side), v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = s_tile[c + k][r];
-        store_terms(a.turned + terms_at(y0 + r, x0 + c, a.short_side), v);
     }
 }
 
@@ -188,11 +184,10 @@ __global__ void __launch_bounds__(kBlock) k_spread(SpreadArgs a)
 enum { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };
 struct ProductArgs {
     const char* left;             // [m][k] in terms
-    const char* right;            // [n][k]
+    const char* right;            // [n][k]; kStep, kLast: [k][n]
     int32_t m, n, k;              // multiples of kPad
     const char* same;             // kPoly: A; kStep, kLast: X, of the shape of P
     char* to;                     // kGram: P; kPoly: b A + c P; kStep: a X + P
-    char* turned;                 // kStep: the same turned
     int32_t whole_tiles, parts;   // tiles behind so many are summed in so many parts
     float* sums;                  // of parts
     float a, b, c;
@@ -204,14 +199,32 @@ struct ProductArgs {
 };
 
 // 32 rows of P from row0 on, WN columns from column0 on, in a wave's accumulators, become what the launch makes of them: by way of a
-// strip of LDS of the wave's own, by rows, then by columns.  once: P's element is not wanted in the mirrored place too.
+// strip of LDS of the wave's own, by rows, and where P or the result is wanted by columns too, so.  The terms of `same` are read
+// while the strip before is worked on.  once: P's element is not wanted in the mirrored place.
 template <int WN> constexpr int kStripPitch = WN + 4;
+template <int WN> struct Same { half8 one[WN / 16], two[WN / 16]; };
+
 template <int kWhat, int WN>
-__device__ __forceinline__ void finish_strip(const ProductArgs& a, float* strip, const float16v (&acc)[WN / 32], int32_t row0, int32_t column0, bool once)
+__device__ __forceinline__ void load_same(const ProductArgs& a, int32_t row0, int32_t column0, Same<WN>& same)
+{
+    if (kWhat == kGram) return;
+    constexpr int kChunks = WN / 8;
+    const int lane = opaque_lane_id();
+#pragma unroll
+    for (int p = 0; p < WN / 16; ++p) {
+        const char* at = a.same + terms_at(row0 + p * (kWave / kChunks) + lane / kChunks, column0 + lane % kChunks * 8, a.n);
+        same.one[p] = *reinterpret_cast<const half8*>(at);
+        same.two[p] = *reinterpret_cast<const half8*>(at + 64);
+    }
+}
+
+template <int kWhat, int WN>
+__device__ __forceinline__ void finish_strip(const ProductArgs& a, float* strip, const float16v (&acc)[WN / 32], const Same<WN>& same, int32_t row0, int32_t column0,
+                                             bool once)
 {
     constexpr int kPitch = kStripPitch<WN>, kChunks = WN / 8;
     const int lane = opaque_lane_id(), l32 = lane & 31, kh = lane >> 5;
-    const bool columns_too = kWhat == kLast ? a.tall : kWhat == kStep || !once;
+    const bool columns_too = kWhat == kLast ? a.tall : kWhat != kStep && !once;
     // element v of lane l is row 8 * (v / 4) + 4 * (l / 32) + v % 4, column l % 32; 2^12 P
 #pragma unroll
     for (int j = 0; j < WN / 32; ++j)
@@ -221,20 +234,21 @@ __device__ __forceinline__ void finish_strip(const ProductArgs& a, float* strip,
 #pragma unroll
     for (int p = 0; p < WN / 16; ++p) {
         const int r = p * (kWave / kChunks) + lane / kChunks, c = lane % kChunks * 8;
-        float v[8], x[8];
+        float v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = strip[r * kPitch + c + k];
-        const int64_t place = terms_at(row0 + r, column0 + c, a.n);
         if (kWhat != kGram) {
-            load_terms(a.same + place, x);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = kWhat == kPoly ? a.b * x[k] + a.c * v[k] : a.a * x[k] + v[k];
+            for (int k = 0; k < 8; ++k) {
+                const float x = (float) same.one[p][k] + (float) same.two[p][k];
+                v[k] = kWhat == kPoly ? a.b * x + a.c * v[k] : a.a * x + v[k];
+            }
             if (columns_too)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) strip[r * kPitch + c + k] = v[k];
         }
         if (kWhat != kLast) {
-            store_terms(a.to + place, v);
+            store_terms(a.to + terms_at(row0 + r, column0 + c, a.n), v);
         } else if (!a.tall && row0 + r < a.rows && column0 + c < a.out.width) {
             float w[8];
             if (a.w.data) load_eight(a.w, a.w_type, row0 + r, column0 + c, w);
@@ -260,7 +274,7 @@ __device__ __forceinline__ void finish_strip(const ProductArgs& a, float* strip,
                 store_eight(a.out, a.out_type, column0 + r, row0 + c, v);
             }
         } else {
-            store_terms((kWhat == kStep ? a.turned : a.to) + terms_at(column0 + r, row0 + c, a.m), v);
+            store_terms(a.to + terms_at(column0 + r, row0 + c, a.m), v);
         }
     }
     __builtin_amdgcn_wave_barrier();
@@ -293,6 +307,7 @@ __device__ __forceinline__ void tile_at(const ProductArgs& a, int32_t t, int32_t
 }
 
 __device__ __forceinline__ int turn_of(int row) { return row >> 1 & 7; }
+__device__ __forceinline__ int turn_of_turned(int row) { return (row >> 1 & 1) * 4; }
 
 // k_product: BM x BN of P a block, WM x WN a wave, products of 32 x 32 x 16.  A stage is 32 of k (for each of KS groups of waves, whose sums
 // are joined at the end): 128 bytes of a row, both terms, which go from memory straight to LDS, chunk c of 16 bytes of row r to
@@ -302,7 +317,7 @@ __device__ __forceinline__ int turn_of(int row) { return row >> 1 & 7; }
 template <int kWhat, int BM, int BN, int WM, int WN, int KS, int S>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, (BM / WM) * (BN / WN) * KS / 4) k_product(ProductArgs a)
 {
-    constexpr bool kSymmetric = kWhat == kGram || kWhat == kPoly;
+    constexpr bool kSymmetric = kWhat == kGram || kWhat == kPoly, kTurns = !kSymmetric;
     constexpr int kGroup = (BM / WM) * (BN / WN), kWaves = kGroup * KS, kRows = BM + BN, kStage = kRows * 128 * KS;
     constexpr int kLoads = kRows * KS / 8 / kWaves, MI = WM / 32, NI = WN / 32;
     constexpr int kSums = MI * NI == 1 ? 3 : 1;               // a wave of one product at a time keeps a sum for each kind of terms
@@ -310,46 +325,70 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, (BM / WM) 
     static_assert(BM / 8 % kLoads == 0, "a wave fetches one side");
     static_assert(kGroup * kStrip + (KS > 1 ? kGroup * kWave * 64 * MI * NI : 0) <= S * kStage, "what follows the products has their place");
     __shared__ __attribute__((aligned(128))) char s_stage[S * kStage];
-    // blocks of whole tiles, then those of parts of the others
-    int32_t tile, part = -1, tm, tn;
+    // blocks of whole tiles, then those of parts of the others: all tiles' first parts, then all second ones, so that what runs together on an
+    // XCD shares rows and their place in k
+    int32_t tile, part = -1, at_part = 0, tm, tn;
     if ((int32_t) blockIdx.x < a.whole_tiles) {
         tile = xcd_run((int32_t) blockIdx.x, a.whole_tiles);
     } else {
-        part = (int32_t) blockIdx.x - a.whole_tiles;
-        tile = a.whole_tiles + part / a.parts;
+        const int32_t count = (int32_t) gridDim.x - a.whole_tiles, rest = count / a.parts, i = xcd_run((int32_t) blockIdx.x - a.whole_tiles, count);
+        at_part = i / rest;
+        tile = a.whole_tiles + i % rest;
+        part = i % rest * a.parts + at_part;
     }
     tile_at<kWhat, BM, BN>(a, tile, &tm, &tn);
     const int32_t m0 = tm * BM, n0 = tn * BN;
     const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63;
     const int group = wave / kGroup, w = wave % kGroup;
     const int64_t row_bytes = (int64_t) a.k * 4;
-    const int32_t all = a.k / (32 * KS), step0 = part < 0 ? 0 : all * (part % a.parts) / a.parts;
-    const int32_t steps = part < 0 ? all : all * (part % a.parts + 1) / a.parts - step0;
+    const int32_t all = a.k / (32 * KS), step0 = part < 0 ? 0 : all * at_part / a.parts;
+    const int32_t steps = part < 0 ? all : all * (at_part + 1) / a.parts - step0;
     // This wave's pieces of a stage: 8 rows each; a lane's 16 bytes come from where its place in LDS has them.  Rows past the last repeat it.
     const int piece = wave * kLoads % (kRows / 8);
     const bool right = piece * 8 >= BM;
     const int32_t first = piece * 8 - (right ? BM : 0), last = (right ? a.n - n0 : a.m - m0) - 1;
-    const char* const base = (right ? a.right + (int64_t) n0 * row_bytes : a.left + (int64_t) m0 * row_bytes) + wave * kLoads / (kRows / 8) * 128 +
-                             (int64_t) step0 * (128 * KS);
+    // X as the right factor: of every 32 columns 32 rows, one behind the other
+    const bool turned = kTurns && right;
+    const int64_t right_bytes = (int64_t) a.n * 4, advance = turned ? right_bytes * 32 : 128;      // of the right factor's rows; from one 32 of k to the next
+    const char* const base = (turned ? a.right + (int64_t) n0 * 4 : right ? a.right + (int64_t) n0 * row_bytes : a.left + (int64_t) m0 * row_bytes) +
+                             (wave * kLoads / (kRows / 8) + (int64_t) step0 * KS) * advance;
     uint32_t from[kLoads];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-        from[i] = (uint32_t) min(first + i * 8 + (lane >> 3), last) * (uint32_t) row_bytes + (uint32_t) ((lane & 7) ^ turn_of((piece + i) * 8 + (lane >> 3))) * 16;
+    for (int i = 0; i < kLoads; ++i) {
+        const int32_t row = first + i * 8 + (lane >> 3);
+        if (turned) from[i] = (uint32_t) (row % 32) * (uint32_t) right_bytes + (uint32_t) min(row / 32, (last + 1) / 32 - 1) * 128 + (uint32_t) ((lane & 7) ^ turn_of_turned(row)) * 16;
+        else        from[i] = (uint32_t) min(row, last) * (uint32_t) row_bytes + (uint32_t) ((lane & 7) ^ turn_of((piece + i) * 8 + (lane >> 3))) * 16;
+    }
     const char* next = base;
     uint32_t next_to = 0;
     auto seek = [&](int32_t step, int buffer) {               // past the last: the last again
-        next = base + (int64_t) min(step, steps - 1) * (128 * KS);
+        next = base + (int64_t) min(step, steps - 1) * KS * advance;
         next_to = lds_address(s_stage) + buffer * kStage + wave * kLoads * 1024;
     };
     auto fetch = [&](int i) { fetch_to_lds(next, from[i], next_to + i * 1024); };
     const int wm = w / (BN / WN) * WM, wn = w % (BN / WN) * WN, l32 = lane & 31, kh = lane >> 5;
     const char* const x_at = s_stage + (group * kRows + wm + l32) * 128;
-    const char* const y_at = s_stage + (group * kRows + BM + wn + l32) * 128;
+    const char* const y_at = s_stage + (group * kRows + BM + wn + (kTurns ? kh * 8 + (lane & 15) / 4 : l32)) * 128;
     half8 f[2][2 * (MI + NI)];                                // fragments of a half stage: first terms of the left and the right, then second terms
     constexpr int kGets = 2 * (MI + NI);
-    auto get = [&](int set, int buffer, int i) {
+    auto get = [&](int set, int buffer, int i) __attribute__((always_inline)) {
         const int t = i / (MI + NI), at = i % (MI + NI), place = ((t * 4 + set * 2 + kh) ^ turn_of(l32)) * 16 + buffer * kStage;
-        f[set][i] = *reinterpret_cast<const half8*>(at < MI ? x_at + at * 4096 + place : y_at + (at - MI) * 4096 + place);
+        if (at < MI) {
+            f[set][i] = *reinterpret_cast<const half8*>(x_at + at * 4096 + place);
+        } else if constexpr (kTurns) {
+            // Lane 4 j + q of sixteen gives four columns of row j of four, lane n gets column n of the four rows; the eight rows that a lane
+            // multiplies are two such fours.
+            const char* const from = y_at + (at - MI) * 4096 + buffer * kStage + set * 2048 + (lane & 1) * 8;
+            const int chunk = t * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+            typedef short short4v __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) short4v* At;
+            // rows 4 apart have the same turn
+            const char* const here = from + (chunk ^ turn_of_turned((lane & 15) / 4)) * 16;
+            const short4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At) (here)), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At) (here + 512));
+            f[set][i] = __builtin_bit_cast(half8, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            f[set][i] = *reinterpret_cast<const half8*>(y_at + (at - MI) * 4096 + place);
+        }
     };
     float16v acc[kSums][MI][NI];
 #pragma unroll
@@ -401,6 +440,9 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, (BM / WM) 
         multiply(1, [&](int o) { if (o < kLoads) fetch(o); else get(0, after, o - kLoads); }, kGets + kLoads);
         buffer = after;
     }
+    Same<WN> same[2];
+    const bool strips = part < 0 && group == 0 && n0 + wn < a.n;
+    if (strips && m0 + wm < a.m) load_same<kWhat, WN>(a, m0 + wm, n0 + wn, same[0]);
     come(std::integral_constant<int, 0>{});                   // what was fetched past the last has come too
     float* const strip = reinterpret_cast<float*>(s_stage + w * kStrip);
     if (KS > 1) {
@@ -423,10 +465,13 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, (BM / WM) 
         }
         return;
     }
-    if (n0 + wn >= a.n) return;
+    if (!strips) return;
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
-        if (m0 + wm + i * 32 < a.m) finish_strip<kWhat, WN>(a, strip, acc[0][i], m0 + wm + i * 32, n0 + wn, kSymmetric && tm == tn);
+    for (int i = 0; i < MI; ++i) {
+        if (m0 + wm + i * 32 >= a.m) return;
+        if (i + 1 < MI && m0 + wm + (i + 1) * 32 < a.m) load_same<kWhat, WN>(a, m0 + wm + (i + 1) * 32, n0 + wn, same[(i + 1) % 2]);
+        finish_strip<kWhat, WN>(a, strip, acc[0][i], same[i % 2], m0 + wm + i * 32, n0 + wn, kSymmetric && tm == tn);
+    }
 }
 
 // The parts of tiles of 128 x 128, in their order, and what the launch makes of them: a wave for each 32 x 64.
@@ -440,6 +485,8 @@ __global__ void __launch_bounds__(kWave) k_join(ProductArgs a)
     tile_at<kWhat, 128, 128>(a, a.whole_tiles + tile, &tm, &tn);
     const int32_t row0 = tm * 128 + w / 2 * 64 + i * 32, column0 = tn * 128 + w % 2 * 64;
     if (row0 >= a.m || column0 >= a.n) return;
+    Same<64> same;
+    load_same<kWhat, 64>(a, row0, column0, same);
     float16v acc[2];
 #pragma unroll 4
     for (int32_t p = 0; p < a.parts; ++p) {
@@ -452,7 +499,7 @@ __global__ void __launch_bounds__(kWave) k_join(ProductArgs a)
             for (int k = 0; k < 4; ++k) acc[q / 4][q % 4 * 4 + k] = p ? acc[q / 4][q % 4 * 4 + k] + of[k] : of[k];
         }
     }
-    finish_strip<kWhat, 64>(a, s_strip, acc, row0, column0, (kWhat == kGram || kWhat == kPoly) && tm == tn);
+    finish_strip<kWhat, 64>(a, s_strip, acc, same, row0, column0, (kWhat == kGram || kWhat == kPoly) && tm == tn);
 }
 
 // No steps: out = keep * w + rate * X from X in terms.
@@ -463,7 +510,15 @@ __global__ void __launch_bounds__(kBlock) k_no_step(ProductArgs a, int32_t piece
         const uint32_t r = i / (uint32_t) pieces;
         const int32_t c = (int32_t) (i - r * (uint32_t) pieces) * 8;
         float v[8], w[8];
-        load_terms(a.same + terms_at(r, c, a.k), v);
+        if (a.tall) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {                     // padded columns are rows of zeros
+                const char* at = a.same + terms_at(c + k, (int32_t) r & ~7, a.n) + (r & 7) * 2;
+                v[k] = (float) *reinterpret_cast<const _Float16*>(at) + (float) *reinterpret_cast<const _Float16*>(at + 64);
+            }
+        } else {
+            load_terms(a.same + terms_at(r, c, a.n), v);
+        }
         if (a.w.data) load_eight(a.w, a.w_type, r, c, w);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = (a.w.data ? a.keep * w[k] : 0.f) + a.rate * (v[k] * kDown);
@@ -478,7 +533,7 @@ constexpr size_t kPartBytes = 128 * 128 * 4;
 
 struct Space {
     int32_t short_side, long_side;
-    size_t sums, x, turned[2], gram, poly, parts, all;        // where each begins; u lies where the second turned X will
+    size_t sums, x[2], gram, poly, parts, all;        // where each begins; u lies where the second X will
 };
 Space space_of(const gns_ctx* c, int32_t width, int32_t rows)
 {
@@ -488,10 +543,9 @@ Space space_of(const gns_ctx* c, int32_t width, int32_t rows)
     s.long_side = padded(std::max(width, rows));
     const size_t large = (size_t) s.short_side * s.long_side * 4, small = (size_t) s.short_side * s.short_side * 4;
     s.sums = 0;
-    s.x = kSumBlocks * sizeof(double);
-    s.turned[0] = s.x + large;
-    s.turned[1] = s.turned[0] + large;
-    s.gram = s.turned[1] + large;
+    s.x[0] = kSumBlocks * sizeof(double);
+    s.x[1] = s.x[0] + large;
+    s.gram = s.x[1] + large;
     s.poly = s.gram + small;
     s.parts = s.poly + small;
     const int64_t tiles = ((int64_t) s.short_side + 127) / 128 * ((s.long_side + 127) / 128);
@@ -559,11 +613,11 @@ hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStrea
     char* const at = static_cast<char*>(a.workspace);
     const bool tall = rows > width;
     double* const sums = reinterpret_cast<double*>(at + space.sums);
-    float* const u = reinterpret_cast<float*>(at + space.turned[1]);
+    float* const u = reinterpret_cast<float*>(at + space.x[1]);
     const int32_t blocks = (int32_t) std::min<int64_t>(((int64_t) rows * pieces + kBlock - 1) / kBlock, kSumBlocks);
     MomentumArgs m = {a.grad, a.momentum, a.momentum_out, a.grad_type, a.momentum_type, a.momentum_out_type, rows, a.how->nesterov, a.how->mu, u, pieces, sums};
     hipLaunchKernelGGL(k_momentum, dim3((unsigned) blocks), dim3(kBlock), 0, s, m);
-    SpreadArgs p = {u, sums, blocks, rows, width, pieces * 8, space.short_side, space.long_side, tall, (double) a.how->eps, at + space.x, at + space.turned[0]};
+    SpreadArgs p = {u, sums, blocks, rows, width, pieces * 8, space.short_side, space.long_side, tall, (double) a.how->eps, at + space.x[0]};
     hipLaunchKernelGGL(k_spread, dim3((unsigned) (space.long_side / kSpread), (unsigned) (space.short_side / kSpread)), dim3(kBlock), 0, s, p);
     ProductArgs q = {};
     q.w = a.w; q.out = a.out; q.w_type = a.w_type; q.out_type = a.out_type; q.rows = rows; q.tall = tall;
@@ -574,7 +628,7 @@ hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStrea
         const float* f = a.how->coefficients[i];
         ProductArgs g = q;
         g.a = f[0]; g.b = f[1]; g.c = f[2];
-        g.left = g.right = at + space.x;
+        g.left = g.right = at + space.x[turn];
         g.m = g.n = space.short_side; g.k = space.long_side;
         g.to = at + space.gram;
         launch_product<kGram>(c, g, s);
@@ -582,16 +636,16 @@ hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStrea
         g.k = space.short_side;
         g.to = at + space.poly;
         launch_product<kPoly>(c, g, s);
-        g.left = at + space.poly; g.right = at + space.turned[turn]; g.same = at + space.x;
+        g.left = at + space.poly; g.right = g.same = at + space.x[turn];
         g.n = space.long_side;
-        g.to = at + space.x; g.turned = at + space.turned[1 - turn];
+        g.to = at + space.x[1 - turn];
         if (i + 1 < a.how->steps) launch_product<kStep>(c, g, s);
         else                      launch_product<kLast>(c, g, s);
         turn = 1 - turn;
     }
     if (!a.how->steps) {
-        q.same = tall ? at + space.turned[0] : at + space.x;
-        q.k = tall ? space.short_side : space.long_side;
+        q.same = at + space.x[0];
+        q.n = space.long_side;
         hipLaunchKernelGGL(k_no_step, dim3((unsigned) blocks), dim3(kBlock), 0, s, q, pieces);
     }
     return hipGetLastError();
