@@ -488,7 +488,7 @@ __global__ void __launch_bounds__(kWave) k_join(ProductArgs a)
     Same<64> same;
     load_same<kWhat, 64>(a, row0, column0, same);
     float16v acc[2];
-#pragma unroll 4
+#pragma unroll 1
     for (int32_t p = 0; p < a.parts; ++p) {
         const float4* from = reinterpret_cast<const float4*>(a.sums) + (((int64_t) tile * a.parts + p) * 8 + at) * (8 * kWave) + lane;
 #pragma unroll
