@@ -1,0 +1,129 @@
+"""The node classifier of node_classifier.py with a normalised hidden layer, weights moved by orthogonalised updates and answers in 8-bit floats:
+
+  z = [x | neighbors' mean] W1 + b1               gns_sage_dense; x, the mean and h kept in 8 bits
+  h = silu(norm(z) gamma + beta)                  gns_group_norm, groups of columns of each node
+  logits = [h | x] W2 + b2                        gns_sage_dense
+  gradients back to W1                            gns_sage_dense_backward, gns_group_norm_backward
+  W1, W2 along their momenta's nearest            gns_orthogonal_update (five steps); vectors by Adam
+    orthogonal matrices
+  answers: both layers in 8-bit floats            gns_sage_dense_fp8, gns_group_norm between them
+
+    python examples/deep_classifier.py --steps 200
+"""
+import argparse
+import os
+import sys
+
+import torch
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+for path in (HERE, os.path.dirname(HERE)):
+    if path not in sys.path:
+        sys.path.insert(0, path)
+
+from node_classifier import BETA, NodeClassifier  # noqa: E402
+from paper_2106_06150_amd import binding as B  # noqa: E402
+from paper_2106_06150_amd import layers, learn  # noqa: E402
+
+GROUPS = 8
+COEFFICIENTS = [(3.4445, -4.7750, 2.0315)] * 5
+MU, DECAY = 0.95, 1e-3
+
+
+class Fp8Layer:
+    """Weights [k, n] as n rows in 8-bit floats."""
+
+    def __init__(self, ctx, w, bias):
+        k, n = w.shape
+        self.q = torch.empty((n, layers.fp8_stride(k)), dtype=torch.uint8, device=w.device)
+        self.exponents = torch.empty((n, layers.fp8_exponents(k)), dtype=torch.uint8, device=w.device)
+        self.bias = bias
+        layers.gns_quantize_fp8(ctx, w.t().contiguous(), None, self.q, self.exponents, n)
+
+
+class DeepClassifier(NodeClassifier):
+    def __init__(self, rate=0.02, **kwargs):
+        super().__init__(**kwargs)
+        dev, batch, hidden = self.dev, self.batch, self.hidden
+        self.gamma, self.beta = torch.ones(hidden, device=dev, requires_grad=True), torch.zeros(hidden, device=dev, requires_grad=True)
+        self.vectors = [self.b1, self.b2, self.gamma, self.beta]
+        self.adam = torch.optim.Adam(self.vectors, lr=0.003)
+        self.norm = layers.Norm(GROUPS, activation=layers.GNS_ACT_SILU, gamma=self.gamma.detach(), beta=self.beta.detach())
+        self.z = torch.empty((batch, hidden), device=dev)
+        self.norm_stats = torch.empty((batch, GROUPS, 2), device=dev)
+        self.momenta = [torch.zeros_like(w.detach()) for w in (self.w1, self.w2)]
+        # a step as long in each layer as its matrix is wide: elements of an orthogonal matrix are about one over its longer side's root
+        self.how = [layers.Orthogonal(COEFFICIENTS, mu=MU, nesterov=True, keep=1.0 - rate * DECAY, rate=-rate * max(1.0, w.shape[0] / w.shape[1]) ** 0.5)
+                    for w in (self.w1, self.w2)]
+        sizes = [layers.gns_orthogonal_update_workspace_bytes(self.ctx, w.shape[1], w.shape[0]) for w in (self.w1, self.w2)]
+        sizes += [layers.gns_group_norm_backward_workspace_bytes(self.ctx, hidden, self.norm, batch), layers.gns_group_norm_workspace_bytes(self.ctx, hidden, self.norm, batch)]
+        sizes += [layers.gns_sage_dense_fp8_workspace_bytes(self.ctx, k, batch) for k in (2 * self.feat, hidden + self.feat)]
+        self.layer_space = layers.alloc_workspace(max(sizes), dev)
+
+    def gradients(self, seeds, batch_seed):
+        """Gradients of the mean loss to every parameter's .grad; the loss, on the device."""
+        ctx, n, classes, k = self.ctx, seeds.numel(), self.classes, self.kept
+        labels = self.labels[seeds.long()]
+        x, mean = self.inputs(seeds, batch_seed)
+        B.gns_sage_dense(ctx, x, mean, self.w1.detach(), self.b1.detach(), False, self.z, n)
+        layers.gns_group_norm(ctx, self.z, self.norm, self.h, self.norm_stats, n, self.layer_space)
+        B.gns_sage_dense(ctx, self.h, x, self.w2.detach(), self.b2.detach(), False, self.logits, n)
+        for name, rows in (("x", x), ("mean", mean), ("h", self.h)):
+            k[name].save(ctx, rows, n)
+        learn.gns_log_probs(ctx, self.logits[:, :classes], labels, self.logp, self.entropy, self.stats, None, None, n, self.space)
+        loss = -(self.logp[:n].mean() + BETA * self.entropy[:n].mean())
+        g_logp, g_entropy = torch.full((n,), -1.0 / n, device=self.dev), torch.full((n,), -BETA / n, device=self.dev)
+        learn.gns_log_probs_backward(ctx, self.logits[:, :classes], labels, self.stats, self.entropy, g_logp, g_entropy, self.d_logits[:, :classes], n)
+        for p in (self.w1, self.w2, *self.vectors):
+            p.grad = torch.empty_like(p)
+        learn.gns_sage_dense_backward(ctx, self.d_logits, None, k["h"].packed, self.hidden, k["x"].packed, self.feat, self.w2.detach(),
+                                      self.w2.grad, self.b2.grad, self.d_in, n, self.space)
+        d_h = self.d_in[:, :self.hidden]
+        layers.gns_group_norm_backward(ctx, d_h, self.z, self.norm, self.norm_stats, d_h, self.gamma.grad, self.beta.grad, n, self.layer_space)
+        learn.gns_sage_dense_backward(ctx, d_h, None, k["x"].packed, self.feat, k["mean"].packed, self.feat, self.w1.detach(),
+                                      self.w1.grad, self.b1.grad, None, n, self.space)
+        return loss
+
+    def step(self, seeds, batch_seed):
+        loss = self.gradients(seeds, batch_seed)
+        for w, momentum, how in zip((self.w1, self.w2), self.momenta, self.how):
+            layers.gns_orthogonal_update(self.ctx, w.grad, momentum, how, w.detach(), momentum, w.detach(), w.shape[0], self.layer_space)
+        self.adam.step()
+        return loss
+
+    def answer(self, seeds, batch_seed, fp8=True, top=5):
+        ctx, n = self.ctx, seeds.numel()
+        x, mean = self.inputs(seeds, batch_seed)
+        if fp8:
+            one, two = Fp8Layer(ctx, self.w1.detach(), self.b1.detach()), Fp8Layer(ctx, self.w2.detach(), self.b2.detach())
+            layers.gns_sage_dense_fp8(ctx, x, mean, one.q, one.exponents, one.bias, False, self.z, n, self.layer_space)
+            layers.gns_group_norm(ctx, self.z, self.norm, self.h, None, n, self.layer_space)
+            layers.gns_sage_dense_fp8(ctx, self.h, x, two.q, two.exponents, two.bias, False, self.logits, n, self.layer_space)
+        else:
+            B.gns_sage_dense(ctx, x, mean, self.w1.detach(), self.b1.detach(), False, self.z, n)
+            layers.gns_group_norm(ctx, self.z, self.norm, self.h, None, n, self.layer_space)
+            B.gns_sage_dense(ctx, self.h, x, self.w2.detach(), self.b2.detach(), False, self.logits, n)
+        index = torch.empty((n, top), dtype=torch.int32, device=self.dev)
+        value = torch.empty((n, top), device=self.dev)
+        learn.gns_log_probs(ctx, self.logits[:, :self.classes], None, None, None, None, index, value, n, self.space)
+        return index, value
+
+
+def main():
+    ap = argparse.ArgumentParser()
+    ap.add_argument("--steps", type=int, default=200)
+    args = ap.parse_args()
+    model = DeepClassifier()
+    losses = model.train(args.steps)
+    seeds = torch.arange(model.batch, dtype=torch.int32, device=model.dev)
+    labels = model.labels[seeds.long()]
+    exact, _ = model.answer(seeds, 7, fp8=False)
+    index, _ = model.answer(seeds, 7)
+    print("loss %.3f -> %.3f; right answers: fp32 %.1f %%, 8-bit floats %.1f %%, among the five best %.1f %%; same answer %.1f %%" % (
+        losses[0], losses[-1], 100 * (exact[:, 0] == labels).float().mean(), 100 * (index[:, 0] == labels).float().mean(),
+        100 * (index == labels[:, None]).any(1).float().mean(), 100 * (index[:, 0] == exact[:, 0]).float().mean()))
+    model.close()
+
+
+if __name__ == "__main__":
+    main()
