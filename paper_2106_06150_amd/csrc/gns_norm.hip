@@ -440,23 +440,31 @@ struct TileBlock {
     }
 };
 
-// Rows r, r + step, .. below end: kRows at a time are read before the first of them is worked on.
+// Rows r, r + step, .. below end: kRows at a time are read before the first of them is worked on.  have: the first ones have been read.
 template <int N> struct Batch { uint32_t words[N][4]; };
 template <int N, int kRows, typename Load, typename Work>
-__device__ __forceinline__ void by_batches_of(int32_t r, int32_t end, int32_t step, Load&& load, Work&& work)
+__device__ __forceinline__ void by_batches_of(int32_t r, int32_t end, int32_t step, Batch<N> (&of)[kRows], bool have, Load&& load, Work&& work)
 {
-    for (; r + (kRows - 1) * step < end; r += kRows * step) {
-        Batch<N> of[kRows];
+    for (int32_t left = end - r; left > 0; left -= kRows * step, r += kRows * step) {
+        if (!have) {
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) load(r + k * step, of[k]);
+            for (int k = 0; k < kRows; ++k) load(r + min(k * step, left - 1), of[k]);
+        }
+        have = false;
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) work(r + k * step, of[k]);
+        for (int k = 0; k < kRows; ++k)
+            if (k * step < left) work(r + k * step, of[k]);
     }
-    for (; r < end; r += step) {
-        Batch<N> of;
-        load(r, of);
-        work(r, of);
-    }
+}
+// A tile's first rows, on their way while its segment is looked for: whether there are any for this thread.
+template <int N, int kRows, typename Block, typename Load>
+__device__ __forceinline__ bool read_ahead(const Block& b, int32_t step, Batch<N> (&of)[kRows], Load&& load)
+{
+    const int32_t r = b.first_row + b.turn;
+    if (!b.c.end || r >= b.last_row) return false;
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) load(r + min(k * step, b.last_row - 1 - r), of[k]);
+    return true;
 }
 template <typename T, bool kWhole>
 __device__ __forceinline__ void load_row(const ConstRows& x, int32_t r, const Columns& c, uint32_t (&words)[4])
@@ -487,6 +495,9 @@ __global__ void __launch_bounds__(kBlock) k_norm_parts(NormArgs a, Tiling t, flo
     constexpr int V = kPiece<T>;
     __shared__ float s_mean[kBlock * V], s_squares[kBlock * V];
     const TileBlock<T> b(a, t);
+    const auto load = [&](int32_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); };
+    Batch<1> ahead[4];
+    const bool have = read_ahead(b, t.turns, ahead, load);
     const Segments segments(a, b.rows);
     const int32_t pitch = t.threads * V, first_group = b.c0 / b.w, groups = (b.c1 - 1) / b.w - first_group + 1;
     const int32_t lanes = team_lanes(groups, b.w);
@@ -499,7 +510,7 @@ __global__ void __launch_bounds__(kBlock) k_norm_parts(NormArgs a, Tiling t, flo
 #pragma unroll
         for (int i = 0; i < V; ++i) mean[i] = squares[i] = 0.f;
         if (b.c.end) {
-            by_batches_of<1, 4>(r0 + b.turn, r1, t.turns, [&](int32_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); }, [&](int32_t, const Batch<1>& of) {
+            by_batches_of(r0 + b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load, [&](int32_t, const Batch<1>& of) {
                 n += 1.f;
                 const float inverse = __builtin_amdgcn_rcpf(n);
 #pragma unroll
@@ -522,19 +533,27 @@ __global__ void __launch_bounds__(kBlock) k_norm_parts(NormArgs a, Tiling t, flo
         for (int32_t g0 = 0; g0 < groups; g0 += kBlock / lanes) {
             const int32_t g = min(g0 + team, groups - 1), j = first_group + g;
             const int32_t from = max(j * b.w, b.c0) - b.c0, to = min((j + 1) * b.w, b.c1) - b.c0;
-            float sum = 0.f;
-            for (int32_t k = 0; k < turns; ++k) {
-                const float of = (float) ((r1 - r0 - k + t.turns - 1) / t.turns);
-                for (int32_t c = from + lane; c < to; c += lanes) sum += of * s_mean[k * pitch + c];
+            // entry i of the group: of turn k, which has as many rows as this or one more
+            const int32_t all_entries = turns * (to - from), least = (r1 - r0) / t.turns, more = r1 - r0 - least * t.turns;
+            const float per = 1.f / (float) (to - from);
+            auto entry = [&](int32_t i, float* of) {
+                const int32_t k = (int32_t) (((float) i + 0.5f) * per);       // exact: i is below 2^11
+                *of = (float) (least + (k < more));
+                return k * (pitch - (to - from)) + from + i;
+            };
+            float sum = 0.f, of;
+#pragma unroll 4
+            for (int32_t i = lane; i < all_entries; i += lanes) {
+                const int32_t at = entry(i, &of);
+                sum += of * s_mean[at];
             }
             const float all = lanes_sum(sum, lanes) / ((float) (r1 - r0) * (float) (to - from));
             sum = 0.f;
-            for (int32_t k = 0; k < turns; ++k) {
-                const float of = (float) ((r1 - r0 - k + t.turns - 1) / t.turns);
-                for (int32_t c = from + lane; c < to; c += lanes) {
-                    const float d = s_mean[k * pitch + c] - all;
-                    sum += s_squares[k * pitch + c] + of * d * d;
-                }
+#pragma unroll 4
+            for (int32_t i = lane; i < all_entries; i += lanes) {
+                const int32_t at = entry(i, &of);
+                const float d = s_mean[at] - all;
+                sum += s_squares[at] + of * d * d;
             }
             sum = lanes_sum(sum, lanes);
             if (lane == 0 && g0 + team < groups) parts[((int64_t) blockIdx.x + s) * t.entries + j + b.slab] = make_float2(all, sum);
@@ -561,17 +580,26 @@ __device__ __forceinline__ float2 join_parts(const NormArgs& a, const Tiling& t,
         return parts[((int64_t) tile + s) * t.entries + j + slab];
     };
     const int32_t all = tiles * slabs;                        // both at most 2^23, as there are workspaces for them
-    float one = 0.f, two = 0.f, of;
+    // a lane's first entry, which is often its only one, stays in registers for the second turn
+    float one = 0.f, two = 0.f, of, first_of = 0.f;
+    float2 first = make_float2(0.f, 0.f);
+    if (l < all) {
+        first = part(l, &first_of);
+        one = kGrad ? first.x : first_of * first.x;
+        two = first.y;
+    }
 #pragma unroll 4
-    for (int32_t e = l; e < all; e += lanes) {
+    for (int32_t e = l + lanes; e < all; e += lanes) {
         const float2 p = part(e, &of);
         one += kGrad ? p.x : of * p.x;
         two += p.y;
     }
     one = sum(one, 0) / n;
     if (!kGrad) {
+        const float d = first.x - one;
+        two += first_of > 0.f ? first_of * d * d : 0.f;
 #pragma unroll 4
-        for (int32_t e = l; e < all; e += lanes) {
+        for (int32_t e = l + lanes; e < all; e += lanes) {
             const float d = part(e, &of).x - one;
             two += of * d * d;
         }
@@ -620,11 +648,14 @@ __device__ __forceinline__ void join_here(const NormArgs& a, const Tiling& t, co
 
 // kJoin: from the tiles' parts, otherwise from the joined statistics.
 template <typename T, bool kJoin, bool kOne>
-__global__ void __launch_bounds__(kBlock, kOne ? 5 : 4) k_norm_apply(NormArgs a, Tiling t, const float2* from)
+__global__ void __launch_bounds__(kBlock, 4) k_norm_apply(NormArgs a, Tiling t, const float2* from)
 {
     constexpr int V = kPiece<T>, G = kOne ? 1 : V;
     __shared__ float2 s_of[kJoin ? kBlock * V : 1];
     const TileBlock<T> b(a, t);
+    const auto load = [&](int32_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); };
+    Batch<1> ahead[4];
+    const bool have = read_ahead(b, t.turns, ahead, load);
     const Segments segments(a, b.rows);
     if (kJoin && a.stats && a.segments && b.slab == 0) {      // segments without rows are in no tile
         for (int64_t s = (int64_t) blockIdx.x * kBlock + threadIdx.x; s < segments.n; s += (int64_t) gridDim.x * kBlock)
@@ -653,7 +684,7 @@ __global__ void __launch_bounds__(kBlock, kOne ? 5 : 4) k_norm_apply(NormArgs a,
         }
 #pragma unroll
         for (int i = V - 1; i >= 0; --i) scale[i] = scale[kOne ? 0 : i] * gamma[i];
-        by_batches_of<1, 4>(r0 + b.turn, r1, t.turns, [&](int32_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); }, [&](int32_t r, const Batch<1>& of) {
+        by_batches_of(r0 + b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load, [&](int32_t r, const Batch<1>& of) {
             float y[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = (value_of_words<T>(of.words[0], i) - mean[kOne ? 0 : i]) * scale[i] + beta[i];
@@ -671,6 +702,9 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_parts(NormAr
     constexpr int V = kPiece<T>, G = kOne ? 1 : V;
     __shared__ float s_one[kBlock * V], s_two[kBlock * V];
     const TileBlock<T> b(a, t);
+    const auto load = [&](int32_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); };
+    Batch<2> ahead[2];
+    const bool have = read_ahead(b, t.turns, ahead, load);
     const Segments segments(a, b.rows);
     const int32_t pitch = t.threads * V, first_group = b.c0 / b.w, groups = (b.c1 - 1) / b.w - first_group + 1;
     const int32_t lanes = team_lanes(groups, kOne ? b.w / V : b.w);
@@ -706,8 +740,7 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_parts(NormAr
                 mean[i] = v.x;
                 rstd[i] = v.y;
             }
-            by_batches_of<2, 2>(r0 + b.turn, r1, t.turns,
-                [&](int32_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); },
+            by_batches_of(r0 + b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load,
                 [&](int32_t, const Batch<2>& of) {
                     float h[V], slope[V];
 #pragma unroll
@@ -778,6 +811,9 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_apply(NormAr
         return;
     }
     const TileBlock<T> b(a, t);
+    const auto load = [&](int32_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); };
+    Batch<2> ahead[2];
+    const bool have = read_ahead(b, t.turns, ahead, load);
     const Segments segments(a, b.rows);
     float gamma[V], beta[V];
     int32_t j[G];
@@ -800,8 +836,7 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_apply(NormAr
             mean[i] = v.x; rstd[i] = v.y;
             m1[i] = m.x; m2[i] = m.y;
         }
-        by_batches_of<2, 2>(r0 + b.turn, r1, t.turns,
-            [&](int32_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); },
+        by_batches_of(r0 + b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load,
             [&](int32_t r, const Batch<2>& of) {
                 float h[V], dx[V];
 #pragma unroll
@@ -827,6 +862,8 @@ int64_t gcd(int64_t a, int64_t b)
     while (b) { const int64_t t = a % b; a = b; b = t; }
     return a;
 }
+
+constexpr int32_t kTileRows = 256;
 
 int32_t piece_of(int32_t type) { return type == GNS_FP32 ? 4 : 8; }
 
@@ -877,6 +914,9 @@ int64_t unit_grad_blocks(const gns_ctx* c, int64_t rows, int32_t groups, int32_t
     return std::max<int64_t>(c->num_cus, std::min<int64_t>((int64_t) c->num_cus * 8, rows / 16 * per));
 }
 
+// Tiles a CU gets: as few as have at most so many rows each, all CUs as many.
+int64_t tile_rounds(const gns_ctx* c, int32_t slabs, int32_t rows) { return std::max<int64_t>(2, ((int64_t) rows * slabs - 1) / ((int64_t) kTileRows * c->num_cus) + 1); }
+
 Tiling tiling_of(const gns_ctx* c, int32_t width, int32_t groups, int32_t type, int32_t rows)
 {
     Tiling t;
@@ -884,8 +924,7 @@ Tiling tiling_of(const gns_ctx* c, int32_t width, int32_t groups, int32_t type, 
     t.slabs = (pieces + kBlock - 1) / kBlock;
     t.threads = std::min(pieces, kBlock);
     t.turns = kBlock / t.threads;
-    t.tile_rows = 16;
-    while (t.tile_rows < 256 && (int64_t) t.tile_rows * 4 * c->num_cus <= (int64_t) rows * t.slabs) t.tile_rows *= 2;
+    t.tile_rows = (int32_t) std::max<int64_t>(16, ((int64_t) rows * t.slabs - 1) / (tile_rounds(c, t.slabs, rows) * c->num_cus) + 1);
     t.tiles = ((int64_t) rows + t.tile_rows - 1) / t.tile_rows;
     t.entries = (int64_t) t.slabs + groups;
     return t;
@@ -925,8 +964,8 @@ size_t need_of(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type,
     return tiled_space(t, t.tiles, segment_count(n, rows), width, n->groups, backward).all;
 }
 
-// The most of any number of rows up to this.  Units: parts grow with the rows.  Tiles: those of a height are most just before the next
-// height begins.
+// The most of any number of rows up to this.  Units: parts grow with the rows.  Tiles: so many
+// rounds of them or fewer.
 size_t most_of(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type, int32_t rows, bool backward)
 {
     if (by_units(n, width, type)) {
@@ -938,9 +977,7 @@ size_t most_of(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type,
         return (size_t) unit_parts({g.blocks, (g.blocks * each + n->groups - 1) / n->groups}, n->groups, lanes) * (size_t) width * 8;
     }
     const Tiling t = tiling_of(c, width, n->groups, type, rows);
-    int64_t tiles = t.tiles;
-    for (int32_t height = 16; height < t.tile_rows; height *= 2)
-        tiles = std::max<int64_t>(tiles, (int64_t) 4 * c->num_cus / t.slabs + 1);
+    const int64_t tiles = std::max(t.tiles, std::min(((int64_t) rows + 15) / 16, tile_rounds(c, t.slabs, rows) * c->num_cus / t.slabs + 1));
     return tiled_space(t, tiles, segment_count(n, rows), width, n->groups, backward).all;
 }
 
