@@ -139,39 +139,42 @@ struct SpreadArgs {
     char* x;                      // [short][long]
 };
 
-constexpr int kSpread = 64;
+constexpr int kSpread = 64, kSpreadBlock = 512;
 
 // X in terms, a tile of 64 x 64 a block.
-__global__ void __launch_bounds__(kBlock) k_spread(SpreadArgs a)
+__global__ void __launch_bounds__(kSpreadBlock) k_spread(SpreadArgs a)
 {
-    constexpr int kTurns = kSpread * kSpread / kBlock;
+    constexpr int kTurns = kSpread * kSpread / kSpreadBlock;
     __shared__ float s_tile[kSpread][kSpread + 1];
-    __shared__ double s_sum[kBlock / kWave];
+    __shared__ double s_sum[kSpreadBlock / kWave];
     // the tile as u has it, on its way while the norm is worked out
     const int32_t x0 = (int32_t) blockIdx.y * kSpread, y0 = (int32_t) blockIdx.x * kSpread;      // in X: rows, columns
     const int32_t u_row = a.tall ? y0 : x0, u_column = a.tall ? x0 : y0;
     float u[kTurns];
 #pragma unroll
     for (int t = 0; t < kTurns; ++t) {
-        const int32_t r = u_row + (t * kBlock + (int) threadIdx.x) / kSpread, c = u_column + (int) threadIdx.x % kSpread;
+        const int32_t r = u_row + (t * kSpreadBlock + (int) threadIdx.x) / kSpread, c = u_column + (int) threadIdx.x % kSpread;
         u[t] = r < a.rows && c < a.width ? a.u[(int64_t) r * a.pitch + c] : 0.f;
     }
     double sum = 0.0;
-    for (int32_t i = (int32_t) threadIdx.x; i < a.sum_count; i += kBlock) sum += a.sums[i];
+    for (int32_t i = (int32_t) threadIdx.x; i < a.sum_count; i += kSpreadBlock) sum += a.sums[i];
     for (int m = 1; m < kWave; m *= 2) sum += __shfl_xor(sum, m);
     if (opaque_lane_id() == 0) s_sum[threadIdx.x >> 6] = sum;
     __syncthreads();
-    const double norm = sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kSpreadBlock / kWave; ++w) sum += s_sum[w];
+    const double norm = sqrt(sum);
     const double inverse = !(norm < (double) __builtin_inff()) ? (double) quiet_nan() : norm > 0.0 ? (double) kUp / (norm + a.eps) : 0.0;
 #pragma unroll
     for (int t = 0; t < kTurns; ++t) {
-        const int r = (t * kBlock + (int) threadIdx.x) / kSpread, c = (int) threadIdx.x % kSpread;
+        const int r = (t * kSpreadBlock + (int) threadIdx.x) / kSpread, c = (int) threadIdx.x % kSpread;
         const float v = (float) ((double) u[t] * inverse);
         if (a.tall) s_tile[c][r] = v;
         else        s_tile[r][c] = v;
     }
     __syncthreads();
-    for (int i = (int) threadIdx.x; i < kSpread * kSpread / 8; i += kBlock) {
+    for (int i = (int) threadIdx.x; i < kSpread * kSpread / 8; i += kSpreadBlock) {
         const int32_t r = i / (kSpread / 8), c = i % (kSpread / 8) * 8;
         float v[8];
 #pragma unroll
@@ -571,7 +574,7 @@ void launch_tiles(const ProductArgs& a, int64_t blocks, hipStream_t s)
 
 // Which tiles, and how the last of them are divided.  What a block takes is counted in stages of tiles of 128 (0.48 us): tiles of 64 take as
 // long for 64 of k, those of 256 three and a half times as long; a block's beginning and end take eight, of 256 forty; the sums of parts and
-// their join fourteen.
+// their join twenty-eight.
 template <int kWhat>
 void launch_product(const gns_ctx* c, ProductArgs a, hipStream_t s)
 {
@@ -585,7 +588,7 @@ void launch_product(const gns_ctx* c, ProductArgs a, hipStream_t s)
     double medium = rounds(all) * (steps + 8);
     int32_t parts = 1;
     for (int32_t p = 2; p <= kMostParts && p * 4 <= steps && rest * p <= 2 * cus; ++p) {
-        const double t = (double) (all / cus) * (steps + 8) + rounds(rest * p) * (steps / p + 8) + 14;
+        const double t = (double) (all / cus) * (steps + 8) + rounds(rest * p) * (steps / p + 8) + 28;
         if (t < medium) { medium = t; parts = p; }
     }
     a.parts = 1;
@@ -618,7 +621,7 @@ hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStrea
     MomentumArgs m = {a.grad, a.momentum, a.momentum_out, a.grad_type, a.momentum_type, a.momentum_out_type, rows, a.how->nesterov, a.how->mu, u, pieces, sums};
     hipLaunchKernelGGL(k_momentum, dim3((unsigned) blocks), dim3(kBlock), 0, s, m);
     SpreadArgs p = {u, sums, blocks, rows, width, pieces * 8, space.short_side, space.long_side, tall, (double) a.how->eps, at + space.x[0]};
-    hipLaunchKernelGGL(k_spread, dim3((unsigned) (space.long_side / kSpread), (unsigned) (space.short_side / kSpread)), dim3(kBlock), 0, s, p);
+    hipLaunchKernelGGL(k_spread, dim3((unsigned) (space.long_side / kSpread), (unsigned) (space.short_side / kSpread)), dim3(kSpreadBlock), 0, s, p);
     ProductArgs q = {};
     q.w = a.w; q.out = a.out; q.w_type = a.w_type; q.out_type = a.out_type; q.rows = rows; q.tall = tall;
     q.keep = a.how->keep; q.rate = a.how->rate;
