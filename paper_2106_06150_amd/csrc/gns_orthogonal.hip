@@ -318,14 +318,14 @@ __device__ __forceinline__ int turn_of_turned(int row) { return (row >> 1 & 1) *
 // is multiplied: there the block's one barrier stands, and behind it the stage S later is fetched to the same place.
 // Symmetric products are made for the tiles on and below the diagonal and written to both places.
 template <int kWhat, int BM, int BN, int WM, int WN, int KS, int S>
-__global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, (BM / WM) * (BN / WN) * KS / 4) k_product(ProductArgs a)
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, ((BM / WM) * (BN / WN) * KS + 3) / 4) k_product(ProductArgs a)
 {
     constexpr bool kSymmetric = kWhat == kGram || kWhat == kPoly, kTurns = !kSymmetric;
     constexpr int kGroup = (BM / WM) * (BN / WN), kWaves = kGroup * KS, kRows = BM + BN, kStage = kRows * 128 * KS;
     constexpr int kLoads = kRows * KS / 8 / kWaves, MI = WM / 32, NI = WN / 32;
     constexpr int kSums = MI * NI == 1 ? 3 : 1;               // a wave of one product at a time keeps a sum for each kind of terms
     constexpr int kStrip = 32 * kStripPitch<WN> * 4;
-    static_assert(BM / 8 % kLoads == 0, "a wave fetches one side");
+    static_assert(BM / 8 % kLoads == 0 || kLoads == kRows / 8, "a wave fetches one side or both");
     static_assert(kGroup * kStrip + (KS > 1 ? kGroup * kWave * 64 * MI * NI : 0) <= S * kStage, "what follows the products has their place");
     __shared__ __attribute__((aligned(128))) char s_stage[S * kStage];
     // blocks of whole tiles, then those of parts of the others: all tiles' first parts, then all second ones, so that what runs together on an
@@ -346,29 +346,43 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, (BM / WM) 
     const int64_t row_bytes = (int64_t) a.k * 4;
     const int32_t all = a.k / (32 * KS), step0 = part < 0 ? 0 : all * at_part / a.parts;
     const int32_t steps = part < 0 ? all : all * (at_part + 1) / a.parts - step0;
-    // This wave's pieces of a stage: 8 rows each; a lane's 16 bytes come from where its place in LDS has them.  Rows past the last repeat it.
+    // This wave's pieces of a stage: 8 rows each, of one side or, kBoth, all of a group's; a lane's 16 bytes come from where its place in
+    // LDS has them.  Rows past the last repeat it.
+    constexpr bool kBoth = kLoads == kRows / 8;
     const int piece = wave * kLoads % (kRows / 8);
-    const bool right = piece * 8 >= BM;
-    const int32_t first = piece * 8 - (right ? BM : 0), last = (right ? a.n - n0 : a.m - m0) - 1;
+    const int32_t group_of = wave * kLoads / (kRows / 8);
     // X as the right factor: of every 32 columns 32 rows, one behind the other
-    const bool turned = kTurns && right;
-    const int64_t right_bytes = (int64_t) a.n * 4, advance = turned ? right_bytes * 32 : 128;      // of the right factor's rows; from one 32 of k to the next
-    const char* const base = (turned ? a.right + (int64_t) n0 * 4 : right ? a.right + (int64_t) n0 * row_bytes : a.left + (int64_t) m0 * row_bytes) +
-                             (wave * kLoads / (kRows / 8) + (int64_t) step0 * KS) * advance;
+    const int64_t right_bytes = (int64_t) a.n * 4;            // of its rows
+    const char* base[2];
+    int64_t advance[2];                                       // from one 32 of k to the next
     uint32_t from[kLoads];
+    auto side = [&](int q, bool right, int i0, int i1) __attribute__((always_inline)) {
+        const bool turned = kTurns && right;
+        const int32_t first = piece * 8 - (right ? BM : 0), last = (right ? a.n - n0 : a.m - m0) - 1;
+        advance[q] = turned ? right_bytes * 32 : 128;
+        base[q] = (turned ? a.right + (int64_t) n0 * 4 : right ? a.right + (int64_t) n0 * row_bytes : a.left + (int64_t) m0 * row_bytes) +
+                  (group_of + (int64_t) step0 * KS) * advance[q];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int32_t row = first + i * 8 + (lane >> 3);
-        if (turned) from[i] = (uint32_t) (row % 32) * (uint32_t) right_bytes + (uint32_t) min(row / 32, (last + 1) / 32 - 1) * 128 + (uint32_t) ((lane & 7) ^ turn_of_turned(row)) * 16;
-        else        from[i] = (uint32_t) min(row, last) * (uint32_t) row_bytes + (uint32_t) ((lane & 7) ^ turn_of((piece + i) * 8 + (lane >> 3))) * 16;
+        for (int i = i0; i < i1; ++i) {
+            const int32_t row = first + i * 8 + (lane >> 3);
+            if (turned) from[i] = (uint32_t) (row % 32) * (uint32_t) right_bytes + (uint32_t) min(row / 32, (last + 1) / 32 - 1) * 128 + (uint32_t) ((lane & 7) ^ turn_of_turned(row)) * 16;
+            else        from[i] = (uint32_t) min(row, last) * (uint32_t) row_bytes + (uint32_t) ((lane & 7) ^ turn_of((piece + i) * 8 + (lane >> 3))) * 16;
+        }
+    };
+    if (kBoth) {
+        side(0, false, 0, BM / 8);
+        side(1, true, BM / 8, kLoads);
+    } else {
+        side(0, piece * 8 >= BM, 0, kLoads);
     }
-    const char* next = base;
+    const char* next[2];
     uint32_t next_to = 0;
     auto seek = [&](int32_t step, int buffer) {               // past the last: the last again
-        next = base + (int64_t) min(step, steps - 1) * KS * advance;
+        next[0] = base[0] + (int64_t) min(step, steps - 1) * KS * advance[0];
+        if (kBoth) next[1] = base[1] + (int64_t) min(step, steps - 1) * KS * advance[1];
         next_to = lds_address(s_stage) + buffer * kStage + wave * kLoads * 1024;
     };
-    auto fetch = [&](int i) { fetch_to_lds(next, from[i], next_to + i * 1024); };
+    auto fetch = [&](int i) { fetch_to_lds(next[kBoth && i >= BM / 8], from[i], next_to + i * 1024); };
     const int wm = w / (BN / WN) * WM, wn = w % (BN / WN) * WN, l32 = lane & 31, kh = lane >> 5;
     const char* const x_at = s_stage + (group * kRows + wm + l32) * 128;
     const char* const y_at = s_stage + (group * kRows + BM + wn + (kTurns ? kh * 8 + (lane & 15) / 4 : l32)) * 128;
@@ -572,9 +586,10 @@ void launch_tiles(const ProductArgs& a, int64_t blocks, hipStream_t s)
     hipLaunchKernelGGL((k_product<kWhat, BM, BN, WM, WN, KS, S>), dim3((unsigned) blocks), dim3((BM / WM) * (BN / WN) * KS * kWave), 0, s, a);
 }
 
-// Which tiles, and how the last of them are divided.  What a block takes is counted in stages of tiles of 128 (0.48 us): tiles of 64 take as
-// long for 64 of k, those of 256 three and a half times as long; a block's beginning and end take eight, of 256 forty; the sums of parts and
-// their join twenty-eight.
+// Which tiles, and how the last of them are divided.  What a block takes is counted in stages of tiles of 128 (0.48 us): tiles of 32 take as
+// long for 128 of k and tiles of 64 for 64, those of 256 three and a half times as long; a block's beginning and end take eight, of 32 four,
+// of 256 forty; the sums of parts and their join twenty-eight.  Measured (five steps, bf16, us, with tiles of 32 and without): 256 x 256 87
+// and 103, 512 x 512 101 and 128, 512 x 2000 139 and 173, 900 x 900 170 and 175.
 template <int kWhat>
 void launch_product(const gns_ctx* c, ProductArgs a, hipStream_t s)
 {
@@ -583,7 +598,7 @@ void launch_product(const gns_ctx* c, ProductArgs a, hipStream_t s)
     auto tiles = [&](int64_t side) { return tiles_of(kSymmetric, a.m, a.n, side); };
     auto rounds = [&](int64_t t) { return (double) ((t + cus - 1) / cus); };
     const double steps = a.k / 32;
-    const double small = rounds(tiles(64)) * (steps / 2 + 8), large = rounds(tiles(256)) * (3.5 * steps + 40);
+    const double least = rounds(tiles(32)) * (steps / 4 + 4), small = rounds(tiles(64)) * (steps / 2 + 8), large = rounds(tiles(256)) * (3.5 * steps + 40);
     const int64_t all = tiles(128), rest = all % cus;
     double medium = rounds(all) * (steps + 8);
     int32_t parts = 1;
@@ -592,7 +607,10 @@ void launch_product(const gns_ctx* c, ProductArgs a, hipStream_t s)
         if (t < medium) { medium = t; parts = p; }
     }
     a.parts = 1;
-    if (small <= medium && small <= large) {
+    if (least <= small && least <= medium && least <= large) {
+        a.whole_tiles = (int32_t) tiles(32);
+        launch_tiles<kWhat, 32, 32, 32, 32, 2, 4>(a, a.whole_tiles, s);
+    } else if (small <= medium && small <= large) {
         a.whole_tiles = (int32_t) tiles(64);
         launch_tiles<kWhat, 64, 64, 32, 32, 2, 4>(a, a.whole_tiles, s);
     } else if (large <= medium) {
