@@ -170,7 +170,8 @@ __device__ __forceinline__ float2 stats_of(float mean, float var, float eps)
 
 // ---- segments of one row: a unit is a group of a row ---------------------------------------------------------------------
 // L lanes hold a unit in P pieces each, so rows are read once.  The launch's units number a multiple of the groups: a thread keeps
-// its columns, and with them scales and shifts.
+// its columns, and with them scales and shifts.  Bound by memory: 85,000 x 256 fp32 in groups of 32 with ReLU 33 us, 179 MB at 5.4 TB/s
+// (a large copy has 5.0); one row of 4096 bf16 3.1 us, most of it a launch.
 template <typename T, int L, int P, bool kWhole>
 __global__ void __launch_bounds__(kBlock) k_norm_units(NormArgs a, int64_t row_step)
 {
@@ -235,7 +236,8 @@ __global__ void __launch_bounds__(kBlock) k_norm_units(NormArgs a, int64_t row_s
 }
 
 // The backward pass of the same: rows are read once, sums for dgamma and dbeta stay in registers and leave as `parts`, rows of
-// width pairs (dbeta, dgamma), which k_norm_columns sums.  Where a block has all groups of several rows it joins those first.
+// width pairs (dbeta, dgamma), which k_norm_columns sums.  Where a block has all groups of several rows it joins those first.  85,000 x 256
+// fp32 with ReLU: 52 us, 267 MB at 5.1 TB/s, and 6.6 us for the columns.
 template <typename T, int L, int P, bool kWhole>
 __global__ void __launch_bounds__(kBlock) k_norm_grad_units(NormArgs a, int64_t row_step, float2* parts)
 {
@@ -440,12 +442,14 @@ struct TileBlock {
     }
 };
 
-// Rows r, r + step, .. below end: kRows at a time are read before the first of them is worked on.  have: the first ones have been read.
+// Rows r0 + turn, and every step-th from there, below end: kRows at a time are read before the first of them is worked on.  have: the first ones
+// have been read.  (65,536 x 512 bf16: four rows 26 us, eight 29; the backward pass's two 36, one 39, four 43, as registers cost waves.)
 template <int N> struct Batch { uint32_t words[N][4]; };
 template <int N, int kRows, typename Load, typename Work>
-__device__ __forceinline__ void by_batches_of(int32_t r, int32_t end, int32_t step, Batch<N> (&of)[kRows], bool have, Load&& load, Work&& work)
+__device__ __forceinline__ void by_batches_of(int32_t r0, int32_t turn, int32_t end, int32_t step, Batch<N> (&of)[kRows], bool have, Load&& load, Work&& work)
 {
-    for (int32_t left = end - r; left > 0; left -= kRows * step, r += kRows * step) {
+    int64_t r = (int64_t) r0 + turn;
+    for (int32_t left = end - r0 - turn; left > 0; left -= kRows * step, r += kRows * step) {
         if (!have) {
 #pragma unroll
             for (int k = 0; k < kRows; ++k) load(r + min(k * step, left - 1), of[k]);
@@ -460,16 +464,16 @@ __device__ __forceinline__ void by_batches_of(int32_t r, int32_t end, int32_t st
 template <int N, int kRows, typename Block, typename Load>
 __device__ __forceinline__ bool read_ahead(const Block& b, int32_t step, Batch<N> (&of)[kRows], Load&& load)
 {
-    const int32_t r = b.first_row + b.turn;
-    if (!b.c.end || r >= b.last_row) return false;
+    const int32_t left = b.last_row - b.first_row - b.turn;
+    if (!b.c.end || left <= 0) return false;
 #pragma unroll
-    for (int k = 0; k < kRows; ++k) load(r + min(k * step, b.last_row - 1 - r), of[k]);
+    for (int k = 0; k < kRows; ++k) load((int64_t) b.first_row + b.turn + min(k * step, left - 1), of[k]);
     return true;
 }
 template <typename T, bool kWhole>
-__device__ __forceinline__ void load_row(const ConstRows& x, int32_t r, const Columns& c, uint32_t (&words)[4])
+__device__ __forceinline__ void load_row(const ConstRows& x, int64_t r, const Columns& c, uint32_t (&words)[4])
 {
-    load_columns<T, kWhole>(reinterpret_cast<const T*>(x.data) + (int64_t) r * x.stride, c, words);
+    load_columns<T, kWhole>(reinterpret_cast<const T*>(x.data) + r * x.stride, c, words);
 }
 
 // Teams of a block for `parts` things, each of up to `most` entries: lanes a team, at most a wave.
@@ -485,6 +489,10 @@ __device__ __forceinline__ float lanes_sum(float v, int32_t lanes)
     return v;
 }
 
+// A segment is more than a CU holds, and blocks meet only where a launch ends: the forward pass reads rows twice, the backward pass rows
+// and their gradients.  65,536 x 512 bf16 in segments of 4096 rows with SiLU: parts 15 us (67 MB, 4.5 TB/s) and rows 26 (134 MB, 5.1 TB/s), backward
+// 36 (134 MB) and 36 (201 MB, 5.6 TB/s); 168,003 x 100 fp32 in sixteen ragged segments with GELU 21 and 32 (67 and 134 MB).
+//
 // kOne in these kernels: groups are whole pieces, so a thread's columns are of one group and all its own.
 //
 // Mean and sum of squared distances of each group of the slab, for each segment in the tile: by column in registers (Welford's
@@ -495,7 +503,7 @@ __global__ void __launch_bounds__(kBlock) k_norm_parts(NormArgs a, Tiling t, flo
     constexpr int V = kPiece<T>;
     __shared__ float s_mean[kBlock * V], s_squares[kBlock * V];
     const TileBlock<T> b(a, t);
-    const auto load = [&](int32_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); };
+    const auto load = [&](int64_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); };
     Batch<1> ahead[4];
     const bool have = read_ahead(b, t.turns, ahead, load);
     const Segments segments(a, b.rows);
@@ -510,7 +518,7 @@ __global__ void __launch_bounds__(kBlock) k_norm_parts(NormArgs a, Tiling t, flo
 #pragma unroll
         for (int i = 0; i < V; ++i) mean[i] = squares[i] = 0.f;
         if (b.c.end) {
-            by_batches_of(r0 + b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load, [&](int32_t, const Batch<1>& of) {
+            by_batches_of(r0, b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load, [&](int64_t, const Batch<1>& of) {
                 n += 1.f;
                 const float inverse = __builtin_amdgcn_rcpf(n);
 #pragma unroll
@@ -653,7 +661,7 @@ __global__ void __launch_bounds__(kBlock, 4) k_norm_apply(NormArgs a, Tiling t, 
     constexpr int V = kPiece<T>, G = kOne ? 1 : V;
     __shared__ float2 s_of[kJoin ? kBlock * V : 1];
     const TileBlock<T> b(a, t);
-    const auto load = [&](int32_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); };
+    const auto load = [&](int64_t r, Batch<1>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); };
     Batch<1> ahead[4];
     const bool have = read_ahead(b, t.turns, ahead, load);
     const Segments segments(a, b.rows);
@@ -684,12 +692,12 @@ __global__ void __launch_bounds__(kBlock, 4) k_norm_apply(NormArgs a, Tiling t, 
         }
 #pragma unroll
         for (int i = V - 1; i >= 0; --i) scale[i] = scale[kOne ? 0 : i] * gamma[i];
-        by_batches_of(r0 + b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load, [&](int32_t r, const Batch<1>& of) {
+        by_batches_of(r0, b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load, [&](int64_t r, const Batch<1>& of) {
             float y[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = (value_of_words<T>(of.words[0], i) - mean[kOne ? 0 : i]) * scale[i] + beta[i];
             activate(y, a.activation);
-            store_columns<T, kOne>(reinterpret_cast<T*>(a.out.data) + (int64_t) r * a.out.stride, b.c, y);
+            store_columns<T, kOne>(reinterpret_cast<T*>(a.out.data) + r * a.out.stride, b.c, y);
         });
     }
 }
@@ -702,7 +710,7 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_parts(NormAr
     constexpr int V = kPiece<T>, G = kOne ? 1 : V;
     __shared__ float s_one[kBlock * V], s_two[kBlock * V];
     const TileBlock<T> b(a, t);
-    const auto load = [&](int32_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); };
+    const auto load = [&](int64_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); };
     Batch<2> ahead[2];
     const bool have = read_ahead(b, t.turns, ahead, load);
     const Segments segments(a, b.rows);
@@ -740,8 +748,8 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_parts(NormAr
                 mean[i] = v.x;
                 rstd[i] = v.y;
             }
-            by_batches_of(r0 + b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load,
-                [&](int32_t, const Batch<2>& of) {
+            by_batches_of(r0, b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load,
+                [&](int64_t, const Batch<2>& of) {
                     float h[V], slope[V];
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
@@ -811,7 +819,7 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_apply(NormAr
         return;
     }
     const TileBlock<T> b(a, t);
-    const auto load = [&](int32_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); };
+    const auto load = [&](int64_t r, Batch<2>& of) { load_row<T, kOne>(a.x, r, b.c, of.words[0]); load_row<T, kOne>(a.d_out, r, b.c, of.words[1]); };
     Batch<2> ahead[2];
     const bool have = read_ahead(b, t.turns, ahead, load);
     const Segments segments(a, b.rows);
@@ -836,8 +844,8 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_apply(NormAr
             mean[i] = v.x; rstd[i] = v.y;
             m1[i] = m.x; m2[i] = m.y;
         }
-        by_batches_of(r0 + b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load,
-            [&](int32_t r, const Batch<2>& of) {
+        by_batches_of(r0, b.turn, r1, t.turns, ahead, have && r0 == b.first_row, load,
+            [&](int64_t r, const Batch<2>& of) {
                 float h[V], dx[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
@@ -847,7 +855,7 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_apply(NormAr
                 slopes_at(dx, a.activation);
 #pragma unroll
                 for (int i = 0; i < V; ++i) dx[i] = rstd[kOne ? 0 : i] * (value_of_words<T>(of.words[1], i) * dx[i] * gamma[i] - m1[kOne ? 0 : i] - h[i] * m2[kOne ? 0 : i]);
-                store_columns<T, kOne>(reinterpret_cast<T*>(a.out.data) + (int64_t) r * a.out.stride, b.c, dx);
+                store_columns<T, kOne>(reinterpret_cast<T*>(a.out.data) + r * a.out.stride, b.c, dx);
             });
     }
 }
@@ -914,7 +922,9 @@ int64_t unit_grad_blocks(const gns_ctx* c, int64_t rows, int32_t groups, int32_t
     return std::max<int64_t>(c->num_cus, std::min<int64_t>((int64_t) c->num_cus * 8, rows / 16 * per));
 }
 
-// Tiles a CU gets: as few as have at most so many rows each, all CUs as many.
+// Tiles a CU gets, all CUs as many: as few as have at most kTileRows rows each, but two, as one does not fill a CU's memory queues (65,536 x 512
+// bf16: parts 15 us with two tiles a CU, 17 with one, rows 26 and 29, with four 28).  168,003 x 100 ragged: rows 31.7 us with three a CU, 33.6
+// with 2.6.
 int64_t tile_rounds(const gns_ctx* c, int32_t slabs, int32_t rows) { return std::max<int64_t>(2, ((int64_t) rows * slabs - 1) / ((int64_t) kTileRows * c->num_cus) + 1); }
 
 Tiling tiling_of(const gns_ctx* c, int32_t width, int32_t groups, int32_t type, int32_t rows)
