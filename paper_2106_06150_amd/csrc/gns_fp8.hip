@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(kWaves * kWave) k_fp8_rows(DenseFp8Args a, Qua
             }
         }
         if (tile + (int32_t) gridDim.x * kWaves < tiles) fetch(tile + (int32_t) gridDim.x * kWaves);
-        T* out = reinterpret_cast<T*>(a.out.data) + (r0 + l16) * a.out.stride + first;
+        T* const out = reinterpret_cast<T*>(a.out.data) + r0 * a.out.stride + first;
         for (int32_t c0 = 0; c0 < n16; c0 += 16 * kGroups) {
             const char* w[kGroups];
             float4v acc[kGroups];
@@ -587,25 +587,42 @@ __global__ void __launch_bounds__(kWaves * kWave) k_fp8_rows(DenseFp8Args a, Qua
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) asm volatile("" : "+v"(acc[g]));
             // element i of lane l is row l % 16, and in its product's order output 4 * (l / 16) + i
-            constexpr int N = kPrecise ? 4 : 8;               // outputs that follow each other: 16 bytes
-#pragma unroll
-            for (int g = 0; g < kGroups; g += N / 4) {
-                const int32_t c = c0 + g * 16 + N * kg;
-                if (c0 + g * 16 >= n16 || r0 + l16 >= rows) continue;
-                struct alignas(16) Outputs { T v[N]; } y;
+            constexpr int N = kPrecise ? 4 : 8, kSpan = 4 * N; // outputs that follow each other: 16 bytes; of a row's four lanes
+            struct alignas(16) Outputs { T v[N]; };
+            auto outputs = [&](int span) __attribute__((always_inline)) {
+                const int32_t c = min(c0 + span * kSpan, n16 - kSpan) + N * kg;
+                Outputs y;
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    y.v[i] = from_float<T>(output_of(acc[g + i / 4][i % 4] * (kPrecise ? kSumUp : 1.f), s_bias[c + i], a.relu));
+                    y.v[i] = from_float<T>(output_of(acc[span * (N / 4) + i / 4][i % 4] * (kPrecise ? kSumUp : 1.f), s_bias[c + i], a.relu));
+                return __builtin_bit_cast(Chunk, y);
+            };
+            // Rows r and r + 8 exchange a span each, so that a store writes 128 bytes of each of eight rows: whole lines, past the caches (85,000 rows,
+            // 256 channels, us, so, with 64 bytes of each of sixteen rows, and through the caches: fp32 of 256 columns 39, 45, 48, of 128 28, 35, 34;
+            // bf16 of 512 columns 36, -, 42, of 256 24, -, 26, of 128 18, -, 18)
+            const bool high = (l16 & 8) != 0;
+            auto store = [&](int32_t r, int32_t c, const Chunk& y) __attribute__((always_inline)) {
+                if (r0 + r >= rows) return;
+                T* const to = out + (int64_t) r * a.out.stride + c;
                 if (stores && c + N <= n) {
-                    const Chunk out16 = __builtin_bit_cast(Chunk, y);
-                    // past the caches where rows are this long (85,000 rows, 256 channels, fp32: of 256 columns 49 -> 45 us, of 128 33 -> 35)
-                    if (kPrecise && B == 2) __builtin_nontemporal_store(out16, reinterpret_cast<Chunk*>(out + c));
-                    else                    *reinterpret_cast<Chunk*>(out + c) = out16;
+                    __builtin_nontemporal_store(y, reinterpret_cast<Chunk*>(to));
                 } else {
+                    const Outputs of = __builtin_bit_cast(Outputs, y);
 #pragma unroll
                     for (int i = 0; i < N; ++i)
-                        if (c + i < n) out[c + i] = y.v[i];
+                        if (c + i < n) to[i] = of.v[i];
                 }
+            };
+#pragma unroll
+            for (int p = 0; p < kGroups * 16 / kSpan; p += 2) {
+                if (c0 + p * kSpan >= n16) break;             // all lanes are here, which the exchange needs
+                const Chunk y0 = outputs(p), y1 = outputs(p + 1);
+                Chunk other;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) other[i] = (uint32_t) __builtin_amdgcn_update_dpp(0, (int) (high ? y0[i] : y1[i]), 0x128, 0xf, 0xf, true);       // from lane l ^ 8
+                const int32_t c = c0 + (p + high) * kSpan + N * kg;
+                store(l16 & 7, c, high ? other : y0);
+                store((l16 & 7) + 8, c, high ? y1 : other);
             }
         }
     }
@@ -662,7 +679,7 @@ hipError_t launch_dense_fp8(const gns_ctx* c, const DenseFp8Args& a, int32_t out
 // Output channels of a block of k_fp8_rows, 0 if the call is not for it: rows of whole pieces, as many as a tile's registers hold, weights that
 // fit LDS in two blocks' parts at most (of rows read twice), and two tiles for each wave of a block per CU, or reading the
 // weights into every LDS costs more than it saves.  Elsewhere the rows are quantised and multiplied in two launches (85,000 rows, 256 channels, us:
-// fp32 of 128 columns 33, in two launches 66, of 256 45 and 68; bf16 of 128 21 and 46, of 256 29 and 53, of 512 52 and 56).
+// fp32 of 128 columns 28, in two launches 66, of 256 39 and 68; bf16 of 128 18 and 46, of 256 24 and 53, of 512 36 and 56).
 template <typename T>
 static int32_t rows_channels(const gns_ctx* c, const QuantizeFp8Args& x, const DenseFp8Args& a)
 {
