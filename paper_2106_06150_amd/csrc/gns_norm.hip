@@ -915,11 +915,12 @@ UnitGrid unit_grid(int64_t rows, int32_t groups, int32_t lanes, int64_t most)
 // Rows of parts for dgamma and dbeta that a launch over units leaves
 int64_t unit_parts(const UnitGrid& g, int32_t groups, int32_t lanes) { return (kBlock / lanes) % groups == 0 ? g.blocks : g.row_step; }
 
-// The backward pass's blocks: few enough that their parts are a tenth of the rows at most, one a CU at least
+// The backward pass's blocks: few enough that their parts are a tenth of the rows at most, one a CU at least (85,000 x 256 fp32: four a CU 54.5 us with the
+// columns, eight 59, two 61)
 int64_t unit_grad_blocks(const gns_ctx* c, int64_t rows, int32_t groups, int32_t lanes)
 {
     const int64_t per = std::max<int64_t>(1, groups / std::max<int64_t>(kBlock / lanes, 1));     // blocks to a row of parts
-    return std::max<int64_t>(c->num_cus, std::min<int64_t>((int64_t) c->num_cus * 8, rows / 16 * per));
+    return std::max<int64_t>(c->num_cus, std::min<int64_t>((int64_t) c->num_cus * 4, rows / 16 * per));
 }
 
 // Tiles a CU gets, all CUs as many: as few as have at most kTileRows rows each, but two, as one does not fill a CU's memory queues (65,536 x 512
