@@ -96,6 +96,28 @@ struct MomentumArgs {
 
 constexpr int kSumBlocks = 1024;
 
+// Eight columns of the gradient and of the momentum, and what becomes of them: the momentum written, and u in the gradient's place.
+__device__ __forceinline__ void load_gradient(const MomentumArgs& a, int64_t r, int32_t c, float (&g)[8], float (&m)[8])
+{
+    load_eight(a.grad, a.grad_type, r, c, g);
+    if (a.momentum.data) load_eight(a.momentum, a.momentum_type, r, c, m);
+}
+__device__ __forceinline__ void u_of(const MomentumArgs& a, int64_t r, int32_t c, float (&g)[8], float (&m)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] = a.momentum.data ? a.mu * m[k] + g[k] : g[k];
+    if (a.momentum.data) store_eight(a.momentum_out, a.momentum_out_type, r, c, m);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) g[k] = a.nesterov ? g[k] + a.mu * m[k] : m[k];
+}
+
+// 2^12 over the norm, by which u becomes X
+__device__ __forceinline__ double scale_of(double squares, double eps)
+{
+    const double norm = sqrt(squares);
+    return !(norm < (double) __builtin_inff()) ? (double) quiet_nan() : norm > 0.0 ? (double) kUp / (norm + eps) : 0.0;
+}
+
 // The momentum and u, and u's squares by block, in 64 bits: neither large nor small gradients leave their range.  4096 x 4096 fp32: 48 us,
 // 268 MB at 5.6 TB/s.
 __global__ void __launch_bounds__(kBlock) k_momentum(MomentumArgs a)
@@ -106,19 +128,9 @@ __global__ void __launch_bounds__(kBlock) k_momentum(MomentumArgs a)
     for (uint32_t i = blockIdx.x * kBlock + threadIdx.x; i < all; i += gridDim.x * kBlock) {
         const uint32_t r = i / (uint32_t) a.pieces;
         const int32_t c = (int32_t) (i - r * (uint32_t) a.pieces) * 8;
-        float g[8], u[8];
-        load_eight(a.grad, a.grad_type, r, c, g);
-        if (a.momentum.data) {
-            load_eight(a.momentum, a.momentum_type, r, c, u);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) u[k] = a.mu * u[k] + g[k];
-            store_eight(a.momentum_out, a.momentum_out_type, r, c, u);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) u[k] = a.nesterov ? g[k] + a.mu * u[k] : u[k];
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) u[k] = a.nesterov ? g[k] + a.mu * g[k] : g[k];
-        }
+        float u[8], m[8];
+        load_gradient(a, r, c, u, m);
+        u_of(a, r, c, u, m);
         float4* to = reinterpret_cast<float4*>(a.u + (int64_t) i * 8);
         to[0] = make_float4(u[0], u[1], u[2], u[3]);
         to[1] = make_float4(u[4], u[5], u[6], u[7]);
@@ -166,8 +178,7 @@ __global__ void __launch_bounds__(kSpreadBlock) k_spread(SpreadArgs a)
     sum = 0.0;
 #pragma unroll
     for (int w = 0; w < kSpreadBlock / kWave; ++w) sum += s_sum[w];
-    const double norm = sqrt(sum);
-    const double inverse = !(norm < (double) __builtin_inff()) ? (double) quiet_nan() : norm > 0.0 ? (double) kUp / (norm + a.eps) : 0.0;
+    const double inverse = scale_of(sum, a.eps);
 #pragma unroll
     for (int t = 0; t < kTurns; ++t) {
         const int r = (t * kSpreadBlock + (int) threadIdx.x) / kSpread, c = (int) threadIdx.x % kSpread;
@@ -525,6 +536,221 @@ __global__ void __launch_bounds__(kWave) k_join(ProductArgs a)
     finish_strip<kWhat, 64>(a, s_strip, acc, same, row0, column0, (kWhat == kGram || kWhat == kPoly) && tm == tn);
 }
 
+// Matrices whose shorter side is up to 64 and whose longer one up to 512, in one block: X in terms stays in LDS from the gradient to the weights, A
+// and b A + c A A take turns behind it. Rows are 16 bytes longer than their terms, so that reads of the same chunk of sixteen rows spread over
+// all banks.  A wave makes a quarter of A over half of k, then the columns of its own 32 of X, which nobody else reads: as X' (b A + c A A),
+// so that a lane has four consecutive columns of a row.  One launch for seventeen: 32 x 64 fp32 20 us (with a launch for each product 65), 64 x 256
+// 33 (70), 47 x 512 48 (75).  Bound by its barriers (3 us a step at 64 columns) and by what one CU reads, writes and multiplies (7 at 512).
+constexpr int kSmallBlock = 512, kSmallShort = 64, kSmallLong = 512, kSmallPieces = kSmallShort * kSmallLong / 8 / kSmallBlock;
+constexpr int kSmallPitch = kSmallShort * 4 + 16;             // of A
+__host__ __device__ constexpr int32_t small_lds(int32_t long_side) { return kSmallShort * (long_side * 4 + 16 + kSmallPitch); }
+
+struct SmallArgs {
+    MomentumArgs m;
+    ConstRows w;
+    MutRows out;
+    int32_t w_type, out_type, tall, long_side;                // padded
+    float keep, rate;
+    double eps;
+    int32_t steps;                // at least one
+    float coefficients[GNS_MAX_STEPS][3];
+};
+
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void store_four(char* to, const float (&v)[4])
+{
+    half4 one, two;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        one[i] = (_Float16) v[i];
+        two[i] = (_Float16) (v[i] - (float) one[i]);
+    }
+    *reinterpret_cast<half4*>(to) = one;
+    *reinterpret_cast<half4*>(to + 64) = two;
+}
+
+// Adds to acc[0], acc[1], acc[2] the products of terms of 32 columns of two rows of terms
+__device__ __forceinline__ void multiply_rows(float16v (&acc)[3], const char* left, const char* right)
+{
+#pragma unroll
+    for (int set = 0; set < 2; ++set) {
+        const half8 x = *reinterpret_cast<const half8*>(left + set * 32), x2 = *reinterpret_cast<const half8*>(left + set * 32 + 64);
+        const half8 y = *reinterpret_cast<const half8*>(right + set * 32), y2 = *reinterpret_cast<const half8*>(right + set * 32 + 64);
+        acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x2, y, acc[0], 0, 0, 0);
+        acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y2, acc[1], 0, 0, 0);
+        acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, acc[2], 0, 0, 0);
+    }
+}
+
+__global__ void __launch_bounds__(kSmallBlock) k_small(SmallArgs a)
+{
+    extern __shared__ int4 s_small[];
+    __shared__ double s_sum[kSmallBlock / kWave];
+    const int32_t pitch = a.long_side * 4 + 16, blocks = a.long_side / kTermBlock, all = a.m.rows * a.m.pieces;
+    char* const s_x = reinterpret_cast<char*>(s_small);
+    char* const s_a = s_x + kSmallShort * pitch;
+    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63, l32 = lane & 31, kh = lane >> 5;
+    float u[kSmallPieces][8], momentum[kSmallPieces][8];
+    double sum = 0.0;
+#pragma unroll
+    for (int t = 0; t < kSmallPieces; ++t) {
+        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces;
+        if (i < all) load_gradient(a.m, r, (i - r * a.m.pieces) * 8, u[t], momentum[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < kSmallPieces; ++t) {
+        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces;
+        if (i >= all) continue;
+        u_of(a.m, r, (i - r * a.m.pieces) * 8, u[t], momentum[t]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += (double) u[t][k] * (double) u[t][k];
+    }
+    for (int32_t i = (int32_t) threadIdx.x; i < kSmallShort * pitch / 16; i += kSmallBlock) s_small[i] = make_int4(0, 0, 0, 0);
+    for (int m = 1; m < kWave; m *= 2) sum += __shfl_xor(sum, m);
+    if (lane == 0) s_sum[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kSmallBlock / kWave; ++w) sum += s_sum[w];
+    const double inverse = scale_of(sum, a.eps);
+#pragma unroll
+    for (int t = 0; t < kSmallPieces; ++t) {
+        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces, c = (i - r * a.m.pieces) * 8;
+        if (i >= all) continue;
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = (float) ((double) u[t][k] * inverse);
+        if (!a.tall) {
+            store_terms(s_x + r * pitch + c / kTermBlock * 128 + c % kTermBlock * 2, v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                _Float16* const to = reinterpret_cast<_Float16*>(s_x + (c + k) * pitch + r / kTermBlock * 128 + r % kTermBlock * 2);
+                to[0] = (_Float16) v[k];
+                to[32] = (_Float16) (v[k] - (float) (_Float16) v[k]);
+            }
+        }
+    }
+    __syncthreads();
+    const int tm = wave & 1, tn = wave >> 1 & 1, half = wave >> 2;
+    auto zero = [](float16v& v) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = 0.f;
+    };
+    // a tile of a symmetric matrix, in the mirrored place: element v of lane l is row 8 * (v / 4) + 4 * (l / 32) + v % 4, column l % 32
+    auto store_symmetric = [&](const float16v& v) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            store_four(s_a + (tn * 32 + l32) * kSmallPitch + tm * 128 + (8 * q + 4 * kh) * 2, {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
+    };
+    for (int32_t step = 0; step < a.steps; ++step) {
+        const float ca = a.coefficients[step][0], cb = a.coefficients[step][1], cc = a.coefficients[step][2];
+        float16v sums[3];
+#pragma unroll
+        for (int t = 0; t < 3; ++t) zero(sums[t]);
+        for (int32_t b = half; b < blocks; b += 2)
+            multiply_rows(sums, s_x + (tm * 32 + l32) * pitch + kh * 16 + b * 128, s_x + (tn * 32 + l32) * pitch + kh * 16 + b * 128);
+        float16v gram = sums[0] + sums[1] + sums[2];
+        float4* const others = reinterpret_cast<float4*>(s_a) + (wave & 3) * 4 * kWave + lane;        // A's place is free: 16 KB of 17
+        if (half)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) others[q * kWave] = make_float4(gram[4 * q], gram[4 * q + 1], gram[4 * q + 2], gram[4 * q + 3]);
+        __syncthreads();
+        if (!half)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 v = others[q * kWave];
+                gram[4 * q] = (gram[4 * q] + v.x) * kDown; gram[4 * q + 1] = (gram[4 * q + 1] + v.y) * kDown;
+                gram[4 * q + 2] = (gram[4 * q + 2] + v.z) * kDown; gram[4 * q + 3] = (gram[4 * q + 3] + v.w) * kDown;
+            }
+        __syncthreads();
+        if (!half) store_symmetric(gram);
+        __syncthreads();
+        if (!half) {
+#pragma unroll
+            for (int t = 0; t < 3; ++t) zero(sums[t]);
+#pragma unroll
+            for (int b = 0; b < kSmallShort / kTermBlock; ++b)
+                multiply_rows(sums, s_a + (tm * 32 + l32) * kSmallPitch + kh * 16 + b * 128, s_a + (tn * 32 + l32) * kSmallPitch + kh * 16 + b * 128);
+            const float16v square = sums[0] + sums[1] + sums[2];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) gram[v] = cb * gram[v] + cc * (square[v] * kDown);
+        }
+        __syncthreads();
+        if (!half) store_symmetric(gram);
+        __syncthreads();
+        half8 poly[2][4][2];                                  // rows of 32, sixteen columns, term
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    poly[i][k][t] = *reinterpret_cast<const half8*>(s_a + (i * 32 + l32) * kSmallPitch + k / 2 * 128 + k % 2 * 32 + kh * 16 + t * 64);
+        for (int32_t b = wave; b < blocks; b += kSmallBlock / kWave) {
+            float16v acc[2];
+            zero(acc[0]);
+            zero(acc[1]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                // X turned: lane 4 j + q of sixteen gives four columns of row j of four, lane n gets column n of the four rows
+                typedef short short4v __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) short4v* At;
+                half8 x[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    char* const from = s_x + (k * 16 + kh * 8 + (lane & 15) / 4) * pitch + b * 128 + t * 64 + (lane >> 4 & 1) * 32 + (lane >> 1 & 1) * 16 + (lane & 1) * 8;
+                    const short4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At) (from)), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At) (from + 4 * pitch));
+                    x[t] = __builtin_bit_cast(half8, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[1], poly[i][k][0], acc[i], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[0], poly[i][k][1], acc[i], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[0], poly[i][k][0], acc[i], 0, 0, 0);
+            }
+            // the last X in place of its terms, in fp32
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                char* const at = s_x + (i * 32 + l32) * pitch + b * 128;
+                float v[4][4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const half4 one = *reinterpret_cast<const half4*>(at + (8 * q + 4 * kh) * 2), two = *reinterpret_cast<const half4*>(at + (8 * q + 4 * kh) * 2 + 64);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[q][k] = ca * ((float) one[k] + (float) two[k]) + acc[i][4 * q + k] * kDown;
+                }
+                __builtin_amdgcn_wave_barrier();              // both halves of the wave have read the row
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (step + 1 < a.steps) store_four(at + (8 * q + 4 * kh) * 2, v[q]);
+                    else                    *reinterpret_cast<float4*>(at + (8 * q + 4 * kh) * 4) = make_float4(v[q][0], v[q][1], v[q][2], v[q][3]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    // out, as u came in
+#pragma unroll
+    for (int t = 0; t < kSmallPieces; ++t) {
+        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces;
+        if (i < all && a.w.data) load_eight(a.w, a.w_type, r, (i - r * a.m.pieces) * 8, u[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < kSmallPieces; ++t) {
+        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces, c = (i - r * a.m.pieces) * 8;
+        if (i >= all) continue;
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            v[k] = *reinterpret_cast<const float*>(a.tall ? s_x + (c + k) * pitch + r * 4 : s_x + r * pitch + (c + k) * 4);
+            v[k] = (a.w.data ? a.keep * u[t][k] : 0.f) + a.rate * (v[k] * kDown);
+        }
+        store_eight(a.out, a.out_type, r, c, v);
+    }
+}
+
 // No steps: out = keep * w + rate * X from X in terms.
 __global__ void __launch_bounds__(kBlock) k_no_step(ProductArgs a, int32_t pieces)
 {
@@ -643,6 +869,12 @@ hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStrea
     float* const u = reinterpret_cast<float*>(at + space.x[1]);
     const int32_t blocks = (int32_t) std::min<int64_t>(((int64_t) rows * pieces + kBlock - 1) / kBlock, kSumBlocks);
     MomentumArgs m = {a.grad, a.momentum, a.momentum_out, a.grad_type, a.momentum_type, a.momentum_out_type, rows, a.how->nesterov, a.how->mu, u, pieces, sums};
+    if (a.how->steps && space.short_side == kSmallShort && space.long_side <= kSmallLong) {
+        SmallArgs q = {m, a.w, a.out, a.w_type, a.out_type, tall, space.long_side, a.how->keep, a.how->rate, (double) a.how->eps, a.how->steps, {}};
+        std::copy_n(&a.how->coefficients[0][0], 3 * GNS_MAX_STEPS, &q.coefficients[0][0]);
+        hipLaunchKernelGGL(k_small, dim3(1), dim3(kSmallBlock), (size_t) small_lds(space.long_side), s, q);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(k_momentum, dim3((unsigned) blocks), dim3(kBlock), 0, s, m);
     SpreadArgs p = {u, sums, blocks, rows, width, pieces * 8, space.short_side, space.long_side, tall, (double) a.how->eps, at + space.x[0]};
     hipLaunchKernelGGL(k_spread, dim3((unsigned) (space.long_side / kSpread), (unsigned) (space.short_side / kSpread)), dim3(kSpreadBlock), 0, s, p);
