@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(kFewBlock) k_fp8_few(DenseFp8Args a, QuantizeF
 // LDS in 8 bits.  A block holds all its weights (as bf16 values for fp32 outputs) and its waves walk tiles of 16 rows.  A lane
 // reads of one row, in every 32 columns, the eight that it multiplies, so a block of 128 columns is in four lanes: two exchanges find
 // its largest value, and the rounded values are the products' right factor as they are.  The weights are the left factor, so that a lane
-// gets four consecutive outputs of a row.
+// gets four consecutive outputs of a row.  Bound by memory: 85,000 rows, 128 + 128 fp32 to 256, 39 us, 174 MB at 4.5 TB/s (a large copy has 5.0).
 __host__ __device__ constexpr int64_t rows_pitch(int64_t stride, bool precise) { return stride * (precise ? 2 : 1) + 16; }      // of a channel in LDS
 __host__ __device__ constexpr int64_t rows_lds(int64_t stride, int32_t channels, bool precise)
 {

@@ -330,8 +330,8 @@ __device__ __forceinline__ int turn_of_turned(int row) { return (row >> 1 & 1) *
 // c ^ turn_of(r), so that reads of the same chunk of sixteen rows spread over all 64 banks.  Fragments are read from LDS half a stage before they are multiplied, so a stage has been read when its first half
 // is multiplied: there the block's one barrier stands, and behind it the stage S later is fetched to the same place.
 // Symmetric products are made for the tiles on and below the diagonal and written to both places.
-// Bound by the matrix cores, whose clock falls with their power: 4096 x 4096, three products of terms each, the step 313 us (412 GFLOP,
-// 1.32 PFLOP/s; the library's fp16 product of 8192 has 1.24), A and b A + c A A 195 us each (212 GFLOP, 1.09 PFLOP/s: 528 tiles of 128 for 256 CUs).
+// Bound by the matrix cores, whose clock falls with their power: 4096 x 4096, three products of terms each, the step 313 to 320 us (412 GFLOP,
+// 1.3 PFLOP/s; the library's fp16 product of 8192 has 1.24), A and b A + c A A 195 to 205 us each (212 GFLOP, 1.06 PFLOP/s: 528 tiles of 128 for 256 CUs).
 // 256 x 256: 5 us a product, of which the matrix cores work a tenth; the rest is a launch and the way to memory and back.
 template <int kWhat, int BM, int BN, int WM, int WN, int KS, int S>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * KS * kWave, ((BM / WM) * (BN / WN) * KS + 3) / 4) k_product(ProductArgs a)
