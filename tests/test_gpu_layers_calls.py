@@ -15,7 +15,7 @@ if torch.cuda.is_available():
     from paper_2106_06150_amd import layers, learn, synth
     from gpu_harness import GpuGns
 
-from test_gpu_layers import (BF16, FP32, QUINTIC, TABLE, TYPES, U, check_norm, check_norm_grad, f64, fp8_values, gen, parameters, random_fp8,  # noqa: E402
+from test_gpu_layers import (BF16, FP32, QUINTIC, TABLE, TYPES, U, check_norm, check_norm_grad, check_update, f64, fp8_values, gen, parameters, random_fp8,  # noqa: E402
                              stored, within)
 from test_gpu_layers import ctx  # noqa: E402,F401  (the module's context)
 
@@ -418,3 +418,41 @@ def test_orthogonal_updates_of_every_size(ctx, rows, width, steps):  # noqa: F81
     assert off <= bound, (off, bound)
     # element by element: an element in a wrong place is off by as much as elements are large, an error by a few times the mean one
     assert float((out.double() - want).abs().max()) <= 64 * (bound / math.sqrt(rows * width) + U * float(want.abs().max()))
+
+
+@pytest.mark.parametrize("rows,width", [(40, 60), (512, 33), (64, 512), (130, 150)])
+def test_orthogonal_updates_of_nothing_of_any_size_and_of_what_is_not_finite(ctx, rows, width):  # noqa: F811
+    """In one block and in many."""
+    conf = layers.Orthogonal([QUINTIC] * 3, keep=0.5, rate=1.0, eps=0.0)
+    space = layers.alloc_workspace(layers.gns_orthogonal_update_workspace_bytes(ctx, width, rows))
+    w = torch.randn(rows, width, generator=gen("w", rows)).cuda()
+    out = torch.empty_like(w)
+    layers.gns_orthogonal_update(ctx, torch.zeros(rows, width, device="cuda"), None, conf, w, None, out, rows, space)
+    assert torch.equal(out, 0.5 * w)
+    for bad in (math.inf, math.nan):
+        grad = torch.randn(rows, width, generator=gen("g", rows)).cuda()
+        grad[13, 7] = bad
+        layers.gns_orthogonal_update(ctx, grad, None, conf, w, None, out, rows, space)
+        assert out.isnan().all()
+    for scale in (1e-30, 1e30):
+        check_update(ctx, rows, width, (FP32, FP32, FP32), [QUINTIC] * 3, momentum=False, scale=scale, eps=0.0)
+    # over the gradient, and the same bits from a graph that is replayed
+    grad = torch.randn(rows, width, generator=gen("in place", rows)).cuda()
+    alone = torch.empty_like(grad)
+    layers.gns_orthogonal_update(ctx, grad, None, conf, None, None, alone, rows, space)
+    moved, m = grad.clone(), torch.zeros_like(grad)
+    layers.gns_orthogonal_update(ctx, moved, None, conf, None, None, moved, rows, space)
+    assert torch.equal(moved, alone)
+    first = torch.empty_like(grad)
+    layers.gns_orthogonal_update(ctx, grad, m, conf, w, m, first, rows, space)
+    again, kept = torch.empty_like(grad), torch.zeros_like(grad)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        layers.gns_orthogonal_update(ctx, grad, kept, conf, w, kept, again, rows, space)
+    for _ in range(3):
+        kept.zero_()
+        again.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(again, first) and torch.equal(kept, m)
