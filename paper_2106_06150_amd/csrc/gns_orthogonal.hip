@@ -536,12 +536,12 @@ __global__ void __launch_bounds__(kWave) k_join(ProductArgs a)
     finish_strip<kWhat, 64>(a, s_strip, acc, same, row0, column0, (kWhat == kGram || kWhat == kPoly) && tm == tn);
 }
 
-// Matrices whose shorter side is up to 64 and whose longer one up to 512, in one block: X in terms stays in LDS from the gradient to the weights, A
-// and b A + c A A take turns behind it. Rows are 16 bytes longer than their terms, so that reads of the same chunk of sixteen rows spread over
+// Matrices whose shorter side is up to 64 and whose longer one up to 256, in one block: X in terms stays in LDS from the gradient to the weights, A
+// and b A + c A A take turns behind it.  Rows are 16 bytes longer than their terms, so that reads of the same chunk of sixteen rows spread over
 // all banks.  A wave makes a quarter of A over half of k, then the columns of its own 32 of X, which nobody else reads: as X' (b A + c A A),
 // so that a lane has four consecutive columns of a row.  One launch for seventeen: 32 x 64 fp32 20 us (with a launch for each product 65), 64 x 256
-// 33 (70), 47 x 512 48 (75).  Bound by its barriers (3 us a step at 64 columns) and by what one CU reads, writes and multiplies (7 at 512).
-constexpr int kSmallBlock = 512, kSmallShort = 64, kSmallLong = 512, kSmallPieces = kSmallShort * kSmallLong / 8 / kSmallBlock;
+// 33 (70).  Bound by its barriers (3 us a step at 64 columns) and by what one CU reads, writes and multiplies.
+constexpr int kSmallBlock = 512, kSmallShort = 64, kSmallLong = 256, kSmallPieces = kSmallShort * kSmallLong / 8 / kSmallBlock;
 constexpr int kSmallPitch = kSmallShort * 4 + 16;             // of A
 __host__ __device__ constexpr int32_t small_lds(int32_t long_side) { return kSmallShort * (long_side * 4 + 16 + kSmallPitch); }
 
@@ -582,45 +582,38 @@ __device__ __forceinline__ void multiply_rows(float16v (&acc)[3], const char* le
     }
 }
 
-__global__ void __launch_bounds__(kSmallBlock) k_small(SmallArgs a)
-{
-    extern __shared__ int4 s_small[];
-    __shared__ double s_sum[kSmallBlock / kWave];
-    const int32_t pitch = a.long_side * 4 + 16, blocks = a.long_side / kTermBlock, all = a.m.rows * a.m.pieces;
-    char* const s_x = reinterpret_cast<char*>(s_small);
-    char* const s_a = s_x + kSmallShort * pitch;
-    const int wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6)), lane = (int) threadIdx.x & 63, l32 = lane & 31, kh = lane >> 5;
-    float u[kSmallPieces][8], momentum[kSmallPieces][8];
-    double sum = 0.0;
-#pragma unroll
-    for (int t = 0; t < kSmallPieces; ++t) {
-        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces;
-        if (i < all) load_gradient(a.m, r, (i - r * a.m.pieces) * 8, u[t], momentum[t]);
+// A block's X, or its columns of it, and the products of a step.  All waves call all of these.
+struct SmallBlock {
+    char* s_x;
+    char* s_a;
+    int32_t pitch, blocks;                                    // of X: bytes of a row, 32 columns each
+    int wave, lane, l32, kh, tm, tn, half;                    // tm, tn: a quarter of A; half: of k
+    __device__ __forceinline__ SmallBlock(char* lds, int32_t columns)
+    {
+        pitch = columns * 4 + 16;
+        blocks = columns / kTermBlock;
+        s_x = lds;
+        s_a = lds + kSmallShort * pitch;
+        wave = __builtin_amdgcn_readfirstlane((int) (threadIdx.x >> 6));
+        lane = (int) threadIdx.x & 63; l32 = lane & 31; kh = lane >> 5;
+        tm = wave & 1; tn = wave >> 1 & 1; half = wave >> 2;
     }
+    static __device__ __forceinline__ void zero(float16v& v)
+    {
 #pragma unroll
-    for (int t = 0; t < kSmallPieces; ++t) {
-        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces;
-        if (i >= all) continue;
-        u_of(a.m, r, (i - r * a.m.pieces) * 8, u[t], momentum[t]);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum += (double) u[t][k] * (double) u[t][k];
+        for (int i = 0; i < 16; ++i) v[i] = 0.f;
     }
-    for (int32_t i = (int32_t) threadIdx.x; i < kSmallShort * pitch / 16; i += kSmallBlock) s_small[i] = make_int4(0, 0, 0, 0);
-    for (int m = 1; m < kWave; m *= 2) sum += __shfl_xor(sum, m);
-    if (lane == 0) s_sum[wave] = sum;
-    __syncthreads();
-    sum = 0.0;
-#pragma unroll
-    for (int w = 0; w < kSmallBlock / kWave; ++w) sum += s_sum[w];
-    const double inverse = scale_of(sum, a.eps);
-#pragma unroll
-    for (int t = 0; t < kSmallPieces; ++t) {
-        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces, c = (i - r * a.m.pieces) * 8;
-        if (i >= all) continue;
+    __device__ __forceinline__ void clear() const             // rows and columns behind the values
+    {
+        for (int32_t i = (int32_t) threadIdx.x; i < kSmallShort * pitch / 16; i += kSmallBlock) reinterpret_cast<int4*>(s_x)[i] = make_int4(0, 0, 0, 0);
+    }
+    // Columns c .. c + 7 of row r of u (c a multiple of 8) times `inverse`, in terms
+    __device__ __forceinline__ void put(const float (&u)[8], double inverse, int32_t r, int32_t c, bool tall) const
+    {
         float v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = (float) ((double) u[t][k] * inverse);
-        if (!a.tall) {
+        for (int k = 0; k < 8; ++k) v[k] = (float) ((double) u[k] * inverse);
+        if (!tall) {
             store_terms(s_x + r * pitch + c / kTermBlock * 128 + c % kTermBlock * 2, v);
         } else {
 #pragma unroll
@@ -631,26 +624,19 @@ __global__ void __launch_bounds__(kSmallBlock) k_small(SmallArgs a)
             }
         }
     }
-    __syncthreads();
-    const int tm = wave & 1, tn = wave >> 1 & 1, half = wave >> 2;
-    auto zero = [](float16v& v) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = 0.f;
-    };
-    // a tile of a symmetric matrix, in the mirrored place: element v of lane l is row 8 * (v / 4) + 4 * (l / 32) + v % 4, column l % 32
-    auto store_symmetric = [&](const float16v& v) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            store_four(s_a + (tn * 32 + l32) * kSmallPitch + tm * 128 + (8 * q + 4 * kh) * 2, {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
-    };
-    for (int32_t step = 0; step < a.steps; ++step) {
-        const float ca = a.coefficients[step][0], cb = a.coefficients[step][1], cc = a.coefficients[step][2];
+    // 2^24 A, this wave's quarter over its half of these columns
+    __device__ __forceinline__ float16v gram() const
+    {
         float16v sums[3];
 #pragma unroll
         for (int t = 0; t < 3; ++t) zero(sums[t]);
         for (int32_t b = half; b < blocks; b += 2)
             multiply_rows(sums, s_x + (tm * 32 + l32) * pitch + kh * 16 + b * 128, s_x + (tn * 32 + l32) * pitch + kh * 16 + b * 128);
-        float16v gram = sums[0] + sums[1] + sums[2];
+        return sums[0] + sums[1] + sums[2];
+    }
+    // The halves' sums, in the first half's waves
+    __device__ __forceinline__ void join(float16v& gram) const
+    {
         float4* const others = reinterpret_cast<float4*>(s_a) + (wave & 3) * 4 * kWave + lane;        // A's place is free: 16 KB of 17
         if (half)
 #pragma unroll
@@ -660,13 +646,28 @@ __global__ void __launch_bounds__(kSmallBlock) k_small(SmallArgs a)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float4 v = others[q * kWave];
-                gram[4 * q] = (gram[4 * q] + v.x) * kDown; gram[4 * q + 1] = (gram[4 * q + 1] + v.y) * kDown;
-                gram[4 * q + 2] = (gram[4 * q + 2] + v.z) * kDown; gram[4 * q + 3] = (gram[4 * q + 3] + v.w) * kDown;
+                gram[4 * q] += v.x; gram[4 * q + 1] += v.y; gram[4 * q + 2] += v.z; gram[4 * q + 3] += v.w;
             }
         __syncthreads();
-        if (!half) store_symmetric(gram);
+    }
+    // a tile of a symmetric matrix, in the mirrored place: element v of lane l is row 8 * (v / 4) + 4 * (l / 32) + v % 4, column l % 32
+    __device__ __forceinline__ void store_symmetric(const float16v& v) const
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            store_four(s_a + (tn * 32 + l32) * kSmallPitch + tm * 128 + (8 * q + 4 * kh) * 2, {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
+    }
+    // b A + c A A in A's place
+    __device__ __forceinline__ void polynomial(float16v& gram, float cb, float cc) const
+    {
+        if (!half) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) gram[v] *= kDown;
+            store_symmetric(gram);
+        }
         __syncthreads();
         if (!half) {
+            float16v sums[3];
 #pragma unroll
             for (int t = 0; t < 3; ++t) zero(sums[t]);
 #pragma unroll
@@ -679,6 +680,10 @@ __global__ void __launch_bounds__(kSmallBlock) k_small(SmallArgs a)
         __syncthreads();
         if (!half) store_symmetric(gram);
         __syncthreads();
+    }
+    // X becomes a X + (b A + c A A) X; the last one is left in place of its terms, in fp32
+    __device__ __forceinline__ void advance(float ca, bool last) const
+    {
         half8 poly[2][4][2];                                  // rows of 32, sixteen columns, term
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -710,7 +715,6 @@ __global__ void __launch_bounds__(kSmallBlock) k_small(SmallArgs a)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[0], poly[i][k][0], acc[i], 0, 0, 0);
             }
-            // the last X in place of its terms, in fp32
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 char* const at = s_x + (i * 32 + l32) * pitch + b * 128;
@@ -724,12 +728,61 @@ __global__ void __launch_bounds__(kSmallBlock) k_small(SmallArgs a)
                 __builtin_amdgcn_wave_barrier();              // both halves of the wave have read the row
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    if (step + 1 < a.steps) store_four(at + (8 * q + 4 * kh) * 2, v[q]);
-                    else                    *reinterpret_cast<float4*>(at + (8 * q + 4 * kh) * 4) = make_float4(v[q][0], v[q][1], v[q][2], v[q][3]);
+                    if (!last) store_four(at + (8 * q + 4 * kh) * 2, v[q]);
+                    else       *reinterpret_cast<float4*>(at + (8 * q + 4 * kh) * 4) = make_float4(v[q][0], v[q][1], v[q][2], v[q][3]);
                 }
             }
         }
         __syncthreads();
+    }
+    // Columns c .. c + 7 of row r of the gradient's shape, of the last X
+    __device__ __forceinline__ void get(float (&v)[8], int32_t r, int32_t c, bool tall) const
+    {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const float*>(tall ? s_x + (c + k) * pitch + r * 4 : s_x + r * pitch + (c + k) * 4);
+    }
+};
+
+__global__ void __launch_bounds__(kSmallBlock) k_small(SmallArgs a)
+{
+    extern __shared__ int4 s_small[];
+    __shared__ double s_sum[kSmallBlock / kWave];
+    const SmallBlock x(reinterpret_cast<char*>(s_small), a.long_side);
+    const int32_t all = a.m.rows * a.m.pieces;
+    float u[kSmallPieces][8], momentum[kSmallPieces][8];
+    double sum = 0.0;
+#pragma unroll
+    for (int t = 0; t < kSmallPieces; ++t) {
+        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces;
+        if (i < all) load_gradient(a.m, r, (i - r * a.m.pieces) * 8, u[t], momentum[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < kSmallPieces; ++t) {
+        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces;
+        if (i >= all) continue;
+        u_of(a.m, r, (i - r * a.m.pieces) * 8, u[t], momentum[t]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += (double) u[t][k] * (double) u[t][k];
+    }
+    x.clear();
+    for (int m = 1; m < kWave; m *= 2) sum += __shfl_xor(sum, m);
+    if (x.lane == 0) s_sum[x.wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kSmallBlock / kWave; ++w) sum += s_sum[w];
+    const double inverse = scale_of(sum, a.eps);
+#pragma unroll
+    for (int t = 0; t < kSmallPieces; ++t) {
+        const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces;
+        if (i < all) x.put(u[t], inverse, r, (i - r * a.m.pieces) * 8, a.tall);
+    }
+    __syncthreads();
+    for (int32_t step = 0; step < a.steps; ++step) {
+        float16v gram = x.gram();
+        x.join(gram);
+        x.polynomial(gram, a.coefficients[step][1], a.coefficients[step][2]);
+        x.advance(a.coefficients[step][0], step + 1 == a.steps);
     }
     // out, as u came in
 #pragma unroll
@@ -742,13 +795,112 @@ __global__ void __launch_bounds__(kSmallBlock) k_small(SmallArgs a)
         const int32_t i = t * kSmallBlock + (int32_t) threadIdx.x, r = i / a.m.pieces, c = (i - r * a.m.pieces) * 8;
         if (i >= all) continue;
         float v[8];
+        x.get(v, r, c, a.tall);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            v[k] = *reinterpret_cast<const float*>(a.tall ? s_x + (c + k) * pitch + r * 4 : s_x + r * pitch + (c + k) * 4);
-            v[k] = (a.w.data ? a.keep * u[t][k] : 0.f) + a.rate * (v[k] * kDown);
-        }
+        for (int k = 0; k < 8; ++k) v[k] = (a.w.data ? a.keep * u[t][k] : 0.f) + a.rate * (v[k] * kDown);
         store_eight(a.out, a.out_type, r, c, v);
     }
+}
+
+// Longer ones: a block has some columns of X, and a launch is a step.  It adds up what the blocks found of A in the launch before, makes
+// b A + c A A (each block its own, which is less than a launch), its columns of X' and what they have of the next A.  The first launch makes X
+// of u.  Seven launches for seventeen: 64 x 1024 fp32 48 us (with a launch for each product 89), 50 x 4096 66 (129).
+struct ChunkArgs {
+    const float* u;
+    const double* sums;
+    int32_t sum_count, rows, width, pitch;                    // of u
+    int32_t tall, long_side, columns;                         // of a block
+    double eps;
+    char* x;                      // a block's rows, one behind the other
+    const float4* parts;          // of A, by block, of the launch before
+    float4* next_parts;
+    float a, b, c;
+    int32_t last;
+    ConstRows w;
+    MutRows out;
+    int32_t w_type, out_type;
+    float keep, rate;
+};
+
+// Few blocks have few parts to add up, many have few columns: of 128, 256 and 512 columns (us) 64 x 1024 takes 48, 57 and 79, 64 x 8192 89, 78 and
+// 92, 64 x 32,768 225, 149 and 132.  (64 x 512: 45, in one block 52; 64 x 256: 42 and 33.)
+constexpr int32_t chunk_columns(int32_t long_side) { return long_side <= 4096 ? 128 : long_side <= 16384 ? 256 : 512; }
+
+template <bool kFirst>
+__global__ void __launch_bounds__(kSmallBlock) k_chunk(ChunkArgs a)
+{
+    extern __shared__ int4 s_small[];
+    __shared__ double s_sum[kSmallBlock / kWave];
+    const int32_t first = (int32_t) blockIdx.x * a.columns, columns = min(a.columns, a.long_side - first), units = columns / 4;
+    const SmallBlock x(reinterpret_cast<char*>(s_small), columns);
+    int4* const image = reinterpret_cast<int4*>(a.x + (int64_t) kSmallShort * first * 4);
+    // pieces of eight of this block's part of the gradient's shape: rows, or columns, `first` and on
+    const int32_t r0 = a.tall ? first : 0, c0 = a.tall ? 0 : first, rows = a.tall ? min(columns, a.rows - first) : a.rows;
+    const int32_t width = a.tall ? a.width : min(columns, a.width - first), pieces = (width + 7) / 8, all = rows * pieces;
+    if constexpr (kFirst) {
+        double sum = 0.0;
+        for (int32_t i = (int32_t) threadIdx.x; i < a.sum_count; i += kSmallBlock) sum += a.sums[i];
+        x.clear();
+        for (int m = 1; m < kWave; m *= 2) sum += __shfl_xor(sum, m);
+        if (x.lane == 0) s_sum[x.wave] = sum;
+        __syncthreads();
+        sum = 0.0;
+#pragma unroll
+        for (int w = 0; w < kSmallBlock / kWave; ++w) sum += s_sum[w];
+        const double inverse = scale_of(sum, a.eps);
+#pragma unroll 4
+        for (int32_t i = (int32_t) threadIdx.x; i < all; i += kSmallBlock) {
+            const int32_t r = i / pieces, c = (i - r * pieces) * 8;
+            const float4* from = reinterpret_cast<const float4*>(a.u + (int64_t) (r0 + r) * a.pitch + c0 + c);
+            const float4 one = from[0], two = from[1];
+            x.put({one.x, one.y, one.z, one.w, two.x, two.y, two.z, two.w}, inverse, r, c, a.tall);
+        }
+        __syncthreads();
+    } else {
+#pragma unroll 4
+        for (int32_t i = (int32_t) threadIdx.x; i < kSmallShort * units; i += kSmallBlock) {
+            const int32_t r = i / units;
+            *reinterpret_cast<int4*>(x.s_x + r * x.pitch + (i - r * units) * 16) = image[i];
+        }
+        float16v gram;
+        SmallBlock::zero(gram);
+        const int32_t count = (int32_t) gridDim.x;
+#pragma unroll 4
+        for (int32_t p = x.half; p < count; p += 2) {
+            const float4* from = a.parts + (int64_t) p * (16 * kWave) + (x.wave & 3) * 4 * kWave + x.lane;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 v = from[q * kWave];
+                gram[4 * q] += v.x; gram[4 * q + 1] += v.y; gram[4 * q + 2] += v.z; gram[4 * q + 3] += v.w;
+            }
+        }
+        x.join(gram);
+        x.polynomial(gram, a.b, a.c);
+        x.advance(a.a, a.last);
+        if (a.last) {
+            for (int32_t i = (int32_t) threadIdx.x; i < all; i += kSmallBlock) {
+                const int32_t r = i / pieces, c = (i - r * pieces) * 8;
+                float v[8], w[8];
+                if (a.w.data) load_eight(a.w, a.w_type, r0 + r, c0 + c, w);
+                x.get(v, r, c, a.tall);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = (a.w.data ? a.keep * w[k] : 0.f) + a.rate * (v[k] * kDown);
+                store_eight(a.out, a.out_type, r0 + r, c0 + c, v);
+            }
+            return;
+        }
+    }
+#pragma unroll 4
+    for (int32_t i = (int32_t) threadIdx.x; i < kSmallShort * units; i += kSmallBlock) {
+        const int32_t r = i / units;
+        image[i] = *reinterpret_cast<const int4*>(x.s_x + r * x.pitch + (i - r * units) * 16);
+    }
+    float16v gram = x.gram();
+    x.join(gram);
+    if (!x.half)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            a.next_parts[(int64_t) blockIdx.x * (16 * kWave) + (x.wave * 4 + q) * kWave + x.lane] = make_float4(gram[4 * q], gram[4 * q + 1], gram[4 * q + 2], gram[4 * q + 3]);
 }
 
 // No steps: out = keep * w + rate * X from X in terms.
@@ -876,6 +1028,26 @@ hipError_t launch_orthogonal(const gns_ctx* c, const OrthogonalArgs& a, hipStrea
         return hipGetLastError();
     }
     hipLaunchKernelGGL(k_momentum, dim3((unsigned) blocks), dim3(kBlock), 0, s, m);
+    if (a.how->steps && space.short_side == kSmallShort) {
+        ChunkArgs q = {};
+        q.u = u; q.sums = sums; q.sum_count = blocks; q.rows = rows; q.width = width; q.pitch = pieces * 8;
+        q.tall = tall; q.long_side = space.long_side; q.columns = chunk_columns(space.long_side);
+        q.eps = (double) a.how->eps;
+        q.x = at + space.x[0];
+        q.w = a.w; q.out = a.out; q.w_type = a.w_type; q.out_type = a.out_type;
+        q.keep = a.how->keep; q.rate = a.how->rate;
+        const unsigned count = (unsigned) ((space.long_side + q.columns - 1) / q.columns);
+        float4* const parts[2] = {reinterpret_cast<float4*>(at + space.parts), reinterpret_cast<float4*>(at + space.parts + (size_t) count * 16 * kWave * sizeof(float4))};
+        q.next_parts = parts[0];
+        hipLaunchKernelGGL(k_chunk<true>, dim3(count), dim3(kSmallBlock), (size_t) small_lds(q.columns), s, q);
+        for (int32_t i = 0; i < a.how->steps; ++i) {
+            q.a = a.how->coefficients[i][0]; q.b = a.how->coefficients[i][1]; q.c = a.how->coefficients[i][2];
+            q.parts = parts[i % 2]; q.next_parts = parts[1 - i % 2];
+            q.last = i + 1 == a.how->steps;
+            hipLaunchKernelGGL(k_chunk<false>, dim3(count), dim3(kSmallBlock), (size_t) small_lds(q.columns), s, q);
+        }
+        return hipGetLastError();
+    }
     SpreadArgs p = {u, sums, blocks, rows, width, pieces * 8, space.short_side, space.long_side, tall, (double) a.how->eps, at + space.x[0]};
     hipLaunchKernelGGL(k_spread, dim3((unsigned) (space.long_side / kSpread), (unsigned) (space.short_side / kSpread)), dim3(kSpreadBlock), 0, s, p);
     ProductArgs q = {};

@@ -391,9 +391,9 @@ def test_fp8_rows_in_registers_are_exact(ctx, rows, f1, f2, n, dtype):  # noqa: 
 
 @pytest.mark.parametrize("rows,width,steps", [(900, 900, 2), (1000, 2500, 2), (2500, 1000, 2), (1500, 1500, 1), (4100, 4096, 2), (4096, 4160, 2), (5632, 5632, 1), (2304, 9000, 1), (600, 32000, 1),
                                               (3000, 70, 2), (70, 3000, 2), (1024, 1024, 2), (64, 512, 2), (512, 64, 2), (64, 513, 2), (513, 64, 2),
-                                              (65, 512, 2), (1, 512, 3), (47, 300, 5), (33, 31, 5), (2, 1, 1)])
+                                              (65, 512, 2), (1, 512, 3), (64, 256, 2), (257, 20, 3), (64, 5000, 2), (20000, 33, 1), (1, 4097, 2), (47, 300, 5), (33, 31, 5), (2, 1, 1)])
 def test_orthogonal_updates_of_every_size(ctx, rows, width, steps):  # noqa: F811
-    """One block for all, tiles of 32, 64, 128 and 256, whole and in parts, wide and tall, against 64 bits on the GPU.  In the 2-norm: 22 bits of each factor and
+    """One block for all, blocks of 128, 256 and 512 columns, tiles of 32, 64, 128 and 256, whole and in parts, wide and tall, against 64 bits on the GPU.  In the 2-norm: 22 bits of each factor and
     sums' roundings, which are as good as random, and every step lets the errors before it grow by its slope, at most 5 below norm 1."""
     g = torch.Generator(device="cuda").manual_seed(rows * 7 + width)
     grad = torch.randn(rows, width, device="cuda", generator=g)
