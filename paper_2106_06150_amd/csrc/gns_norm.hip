@@ -654,6 +654,173 @@ __device__ __forceinline__ void join_here(const NormArgs& a, const Tiling& t, co
     __syncthreads();
 }
 
+// ---- short segments of equal length: several to a block ---------------------------------------------------------------------
+// A block's values lie in LDS in fp32, teams of lanes sum a segment and group each, and rows are read once.
+constexpr int32_t kShortValues = 4096;
+
+struct ShortBlock {
+    int32_t width, w, groups, per, rows, first_row, segments, pieces;      // rows, segments: of the block
+    float each;                   // 1 / w
+    __device__ __forceinline__ ShortBlock(const NormArgs& a, int32_t per_, int32_t most, int32_t piece)
+    {
+        width = a.x.width; groups = a.groups; w = width / groups; per = per_;
+        const int32_t all = a.count.get();
+        first_row = (int32_t) min((int64_t) blockIdx.x * most * per, (int64_t) max(all, 0));
+        rows = min(most * per, all - first_row);
+        segments = rows > 0 ? (rows - 1) / per + 1 : 0;
+        pieces = (width - 1) / piece + 1;
+        each = 1.f / (float) w;
+    }
+    // exact: columns and values of a segment are fewer than 2^12
+    __device__ __forceinline__ int32_t group_of(int32_t c) const { return (int32_t) (((float) c + 0.5f) * each); }
+    // Work on the pieces of 16 bytes, rows of the block one behind the other.
+    template <int V, typename Work>
+    __device__ __forceinline__ void by_pieces(Work&& work) const
+    {
+        for (int32_t q = (int32_t) threadIdx.x; q < rows * pieces; q += kBlock) {
+            const int32_t r = q / pieces;
+            work(r, columns_from<V>((q - r * pieces) * V, width));
+        }
+    }
+    // Work on (segment, group) by teams of `lanes`: value i of n lies at place(i) of the block's values
+    template <typename Work>
+    __device__ __forceinline__ void by_units(Work&& work) const
+    {
+        const int32_t units = segments * groups, lanes = team_lanes(units, per * w);
+        const int32_t team = opaque((int) threadIdx.x) / lanes, lane = opaque((int) threadIdx.x) % lanes;
+        for (int32_t u0 = 0; u0 < units; u0 += kBlock / lanes) {
+            const int32_t u = min(u0 + team, units - 1), s = u / groups, j = u - s * groups, n = min(per, rows - s * per) * w, from = s * per * width + j * w;
+            work(u, n, lane, lanes, u0 + team < units, [&](int32_t i) {
+                const int32_t r = group_of(i);
+                return from + r * (width - w) + i;
+            });
+        }
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kBlock) k_norm_short(NormArgs a, int32_t per, int32_t most)
+{
+    constexpr int V = kPiece<T>;
+    __shared__ float s_x[kShortValues];
+    __shared__ float2 s_of[kShortValues / 2];                 // a segment has two rows at least, or is a row of so few columns
+    const ShortBlock b(a, per, most, V);
+    b.template by_pieces<V>([&](int32_t r, const Columns& c) {
+        uint32_t words[4];
+        load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + ((int64_t) b.first_row + r) * a.x.stride, c, words);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i >= c.skip && i < c.end) s_x[r * b.width + c.first + i] = value_of_words<T>(words, i);
+    });
+    __syncthreads();
+    b.by_units([&](int32_t u, int32_t n, int32_t lane, int32_t lanes, bool own, auto&& place) {
+        const float inverse = 1.f / (float) n;
+        float sum = 0.f;
+#pragma unroll 4
+        for (int32_t i = lane; i < n; i += lanes) sum += s_x[place(i)];
+        const float mean = lanes_sum(sum, lanes) * inverse;
+        sum = 0.f;
+#pragma unroll 4
+        for (int32_t i = lane; i < n; i += lanes) {
+            const float d = s_x[place(i)] - mean;
+            sum += d * d;
+        }
+        const float2 v = stats_of(mean, lanes_sum(sum, lanes) * inverse, a.eps);
+        if (lane == 0 && own) {
+            s_of[u] = v;
+            if (a.stats) reinterpret_cast<float2*>(a.stats)[(int64_t) b.first_row / per * b.groups + u] = v;
+        }
+    });
+    __syncthreads();
+    b.template by_pieces<V>([&](int32_t r, const Columns& c) {
+        float y[V], gamma[V], beta[V];
+        load_parameters<V, false>(a.gamma, c, 1.f, gamma);
+        load_parameters<V, false>(a.beta, c, 0.f, beta);
+        const int32_t unit = r / per * b.groups;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int32_t column = min(c.first + i, b.width - 1);
+            const float2 v = s_of[unit + b.group_of(column)];
+            y[i] = (s_x[r * b.width + column] - v.x) * (v.y * gamma[i]) + beta[i];
+        }
+        activate(y, a.activation);
+        store_columns<T, false>(reinterpret_cast<T*>(a.out.data) + ((int64_t) b.first_row + r) * a.out.stride, c, y);
+    });
+}
+
+// The same backward: dy and h in LDS; the block's sums of columns go to row blockIdx.x of `columns`.
+template <typename T>
+__global__ void __launch_bounds__(kBlock) k_norm_grad_short(NormArgs a, int32_t per, int32_t most, float2* columns)
+{
+    constexpr int V = kPiece<T>;
+    __shared__ float s_dy[kShortValues], s_h[kShortValues];
+    __shared__ float2 s_of[kShortValues / 2];
+    const ShortBlock b(a, per, most, V);
+    const float2* const stats = reinterpret_cast<const float2*>(a.stats) + (int64_t) b.first_row / per * b.groups;
+    b.template by_pieces<V>([&](int32_t r, const Columns& c) {
+        uint32_t x[4], d[4];
+        load_columns<T, false>(reinterpret_cast<const T*>(a.x.data) + ((int64_t) b.first_row + r) * a.x.stride, c, x);
+        load_columns<T, false>(reinterpret_cast<const T*>(a.d_out.data) + ((int64_t) b.first_row + r) * a.d_out.stride, c, d);
+        float gamma[V], beta[V], h[V], slope[V];
+        load_parameters<V, false>(a.gamma, c, 1.f, gamma);
+        load_parameters<V, false>(a.beta, c, 0.f, beta);
+        const int32_t unit = r / per * b.groups;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float2 v = stats[unit + b.group_of(min(c.first + i, b.width - 1))];
+            h[i] = (value_of_words<T>(x, i) - v.x) * v.y;
+            slope[i] = h[i] * gamma[i] + beta[i];
+        }
+        slopes_at(slope, a.activation);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i >= c.skip && i < c.end) {
+                s_dy[r * b.width + c.first + i] = value_of_words<T>(d, i) * slope[i];
+                s_h[r * b.width + c.first + i] = h[i];
+            }
+    });
+    __syncthreads();
+    if (columns)
+        for (int32_t c = (int32_t) threadIdx.x; c < b.width; c += kBlock) {
+            float2 t = make_float2(0.f, 0.f);
+#pragma unroll 4
+            for (int32_t r = 0; r < b.rows; ++r) {
+                const float dy = s_dy[r * b.width + c];
+                t.x += dy;
+                t.y += dy * s_h[r * b.width + c];
+            }
+            columns[(int64_t) blockIdx.x * b.width + c] = t;
+        }
+    if (!a.out.data) return;
+    b.by_units([&](int32_t u, int32_t n, int32_t lane, int32_t lanes, bool own, auto&& place) {
+        const float* gamma = a.gamma ? a.gamma + u % b.groups * b.w : nullptr;
+        const float inverse = 1.f / (float) n;
+        float m1 = 0.f, m2 = 0.f;
+#pragma unroll 4
+        for (int32_t i = lane; i < n; i += lanes) {
+            const int32_t at = place(i);
+            const float g = s_dy[at] * (gamma ? gamma[i - b.group_of(i) * b.w] : 1.f);
+            m1 += g;
+            m2 += g * s_h[at];
+        }
+        m1 = lanes_sum(m1, lanes) * inverse;
+        m2 = lanes_sum(m2, lanes) * inverse;
+        if (lane == 0 && own) s_of[u] = make_float2(m1, m2);
+    });
+    __syncthreads();
+    b.template by_pieces<V>([&](int32_t r, const Columns& c) {
+        float gamma[V], dx[V];
+        load_parameters<V, false>(a.gamma, c, 1.f, gamma);
+        const int32_t unit = r / per * b.groups;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int32_t column = min(c.first + i, b.width - 1), j = unit + b.group_of(column), at = r * b.width + column;
+            dx[i] = stats[j].y * (s_dy[at] * gamma[i] - s_of[j].x - s_h[at] * s_of[j].y);
+        }
+        store_columns<T, false>(reinterpret_cast<T*>(a.out.data) + ((int64_t) b.first_row + r) * a.out.stride, c, dx);
+    });
+}
+
 // kJoin: from the tiles' parts, otherwise from the joined statistics.
 template <typename T, bool kJoin, bool kOne>
 __global__ void __launch_bounds__(kBlock, 4) k_norm_apply(NormArgs a, Tiling t, const float2* from)
@@ -901,6 +1068,19 @@ bool by_units(const gns_norm* n, int32_t width, int32_t type)
     return !n->segments_dev && n->segment_rows == 1 && unit_shape(width / n->groups, type).lanes > 0;
 }
 
+// Segments of equal length that lie in a block's LDS together: as many rows as that, and as many segments; 0: they do not.
+struct ShortShape {
+    int32_t per, most;
+    int64_t blocks;
+};
+ShortShape short_shape(const gns_norm* n, int32_t width, int32_t rows)
+{
+    const int64_t per = std::min(n->segment_rows, rows);
+    if (n->segments_dev || n->segment_rows == 1 || per * width > kShortValues || width > kShortValues / 2) return {0, 0, 0};
+    const int64_t most = kShortValues / (per * width);
+    return {(int32_t) per, (int32_t) most, (((int64_t) rows + per - 1) / per + most - 1) / most};
+}
+
 // Blocks of a launch over units, and the rows between a thread's units.  Their units are whole rows, or turns of rows.
 struct UnitGrid {
     int64_t blocks, row_step;
@@ -928,7 +1108,7 @@ int64_t unit_grad_blocks(const gns_ctx* c, int64_t rows, int32_t groups, int32_t
 // with 2.6.
 int64_t tile_rounds(const gns_ctx* c, int32_t slabs, int32_t rows) { return std::max<int64_t>(2, ((int64_t) rows * slabs - 1) / ((int64_t) kTileRows * c->num_cus) + 1); }
 
-Tiling tiling_of(const gns_ctx* c, int32_t width, int32_t groups, int32_t type, int32_t rows)
+Tiling tiling_of(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type, int32_t rows)
 {
     Tiling t;
     const int32_t pieces = (width + piece_of(type) - 1) / piece_of(type);
@@ -936,8 +1116,10 @@ Tiling tiling_of(const gns_ctx* c, int32_t width, int32_t groups, int32_t type, 
     t.threads = std::min(pieces, kBlock);
     t.turns = kBlock / t.threads;
     t.tile_rows = (int32_t) std::max<int64_t>(16, ((int64_t) rows * t.slabs - 1) / (tile_rounds(c, t.slabs, rows) * c->num_cus) + 1);
+    // segments of equal length that are shorter are tiles
+    if (!n->segments_dev && n->segment_rows < t.tile_rows) t.tile_rows = (15 / n->segment_rows + 1) * n->segment_rows;
     t.tiles = ((int64_t) rows + t.tile_rows - 1) / t.tile_rows;
-    t.entries = (int64_t) t.slabs + groups;
+    t.entries = (int64_t) t.slabs + n->groups;
     return t;
 }
 
@@ -971,7 +1153,8 @@ size_t need_of(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type,
         const UnitGrid g = unit_grid(rows, n->groups, lanes, unit_grad_blocks(c, rows, n->groups, lanes));
         return (size_t) unit_parts(g, n->groups, lanes) * (size_t) width * 8;
     }
-    const Tiling t = tiling_of(c, width, n->groups, type, rows);
+    if (const ShortShape b = short_shape(n, width, rows); b.per) return backward ? (size_t) b.blocks * (size_t) width * 8 : 0;
+    const Tiling t = tiling_of(c, width, n, type, rows);
     return tiled_space(t, t.tiles, segment_count(n, rows), width, n->groups, backward).all;
 }
 
@@ -987,8 +1170,11 @@ size_t most_of(const gns_ctx* c, int32_t width, const gns_norm* n, int32_t type,
         const UnitGrid g = {std::max(unit_grad_blocks(c, rows, n->groups, lanes), whole), 0};
         return (size_t) unit_parts({g.blocks, (g.blocks * each + n->groups - 1) / n->groups}, n->groups, lanes) * (size_t) width * 8;
     }
-    const Tiling t = tiling_of(c, width, n->groups, type, rows);
-    const int64_t tiles = std::max(t.tiles, std::min(((int64_t) rows + 15) / 16, tile_rounds(c, t.slabs, rows) * c->num_cus / t.slabs + 1));
+    if (const ShortShape b = short_shape(n, width, rows); b.per) return backward ? (size_t) b.blocks * (size_t) width * 8 : 0;
+    const Tiling t = tiling_of(c, width, n, type, rows);
+    const int64_t whole = n->segments_dev ? 0 : ((int64_t) rows - 1) / std::max(n->segment_rows, 16) + 1;      // tiles that are segments
+    const int64_t tiles = std::max(t.tiles, std::min(((int64_t) rows + 15) / 16, std::max(whole, tile_rounds(c, t.slabs, rows) * c->num_cus / t.slabs + 1)));
+    // (fewer rows may be one short segment: a row of columns, fewer than tiles')
     return tiled_space(t, tiles, segment_count(n, rows), width, n->groups, backward).all;
 }
 
@@ -1034,8 +1220,12 @@ hipError_t launch_norm_typed(const gns_ctx* c, const NormArgs& a, const gns_norm
         }
         return hipGetLastError();
     }
+    if (const ShortShape b = short_shape(n, width, rows); b.per) {
+        hipLaunchKernelGGL(k_norm_short<T>, dim3((unsigned) b.blocks), dim3(kBlock), 0, s, a, b.per, b.most);
+        return hipGetLastError();
+    }
     const bool one = w % kPiece<T> == 0;
-    const Tiling t = tiling_of(c, width, a.groups, type, rows);
+    const Tiling t = tiling_of(c, width, n, type, rows);
     const int64_t segments = segment_count(n, rows);
     const TiledSpace space = tiled_space(t, t.tiles, segments, width, a.groups, false);
     float2* const parts = static_cast<float2*>(a.workspace);
@@ -1090,8 +1280,15 @@ hipError_t launch_grad_typed(const gns_ctx* c, const NormArgs& a, const gns_norm
             hipLaunchKernelGGL(k_norm_columns, join, dim3(kBlock), 0, s, parts, unit_parts(g, a.groups, u.lanes), a.count, 0, width, a.dgamma, a.dbeta);
         return hipGetLastError();
     }
+    if (const ShortShape b = short_shape(n, width, rows); b.per) {
+        float2* const parts = columns_wanted ? static_cast<float2*>(a.workspace) : nullptr;
+        hipLaunchKernelGGL(k_norm_grad_short<T>, dim3((unsigned) b.blocks), dim3(kBlock), 0, s, a, b.per, b.most, parts);
+        if (columns_wanted)
+            hipLaunchKernelGGL(k_norm_columns, join, dim3(kBlock), 0, s, parts, b.blocks, a.count, 0, width, a.dgamma, a.dbeta);
+        return hipGetLastError();
+    }
     const bool one = w % kPiece<T> == 0;
-    const Tiling t = tiling_of(c, width, a.groups, type, rows);
+    const Tiling t = tiling_of(c, width, n, type, rows);
     const int64_t segments = segment_count(n, rows);
     const TiledSpace space = tiled_space(t, t.tiles, segments, width, a.groups, true);
     char* const at = static_cast<char*>(a.workspace);

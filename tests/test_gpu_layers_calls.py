@@ -83,7 +83,7 @@ def test_refusals(ctx):  # noqa: F811
         refused(einval, "gns_dense_fp8", bp, ep, 64, bp, ep, None, 0, rows(), n, s)
         refused(einval, "gns_sage_dense_fp8", rows(), None, bp, ep, None, 0, rows(), n, wp, size, s)
     # norm: shapes that do not agree, rows that overlap otherwise than as the same, workspaces
-    tiled = norm(per=2)
+    tiled = norm(offsets.data_ptr(), count=1)
     refused(einval, "gns_group_norm", rows(), norm(), rows(p2, width=32), None, 4, wp, size, s)
     refused(einval, "gns_group_norm", rows(), norm(), rows(p2, type=1), None, 4, wp, size, s)
     refused(einval, "gns_group_norm", rows(width=32), norm(), rows(width=32, stride=32), None, 4, wp, size, s)
@@ -456,3 +456,17 @@ def test_orthogonal_updates_of_nothing_of_any_size_and_of_what_is_not_finite(ctx
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(again, first) and torch.equal(kept, m)
+
+
+@TYPES
+@pytest.mark.parametrize("rows,width,groups,per", [(999, 11, 11, 18), (998, 2048, 2048, 2), (1, 2048, 2048, 7), (1, 2049, 3, 7), (71, 2049, 3, 2), (5, 37, 1, 1000), (8193, 1, 1, 4096),
+                                                   (8193, 1, 1, 4097), (300, 64, 8, 64), (300, 65, 5, 63), (300, 65, 5, 64), (203, 512, 32, 20), (503, 1024, 32, 5), (2000, 3, 3, 2), (777, 100, 4, 40)])
+def test_norm_of_short_segments(ctx, rows, width, groups, per, dtype):  # noqa: F811
+    """Several segments to a block, a segment that just fits one and that just does not, tiles that are segments, the last one shorter."""
+    g = gen(rows, width, per)
+    x = (torch.randn(rows, width, generator=g) * 2 + torch.randn(1, width, generator=g)).to(dtype)
+    d_out = torch.randn(rows, width, generator=g).to(dtype)
+    gamma, beta = parameters(width, g)
+    for act in (1, 3):
+        check_norm(ctx, x, groups, act, segment_rows=per, gamma=gamma, beta=beta, inplace=act == 3)
+        check_norm_grad(ctx, x, d_out, groups, act, segment_rows=per, gamma=gamma, beta=beta)
