@@ -75,6 +75,13 @@ __device__ __forceinline__ void slopes_at(float (&y)[V], int32_t kind)
     }
 }
 
+// A product rounded by itself, not with the sum that it goes to: of a group of one value g - m1 is zero only if both are the same product.
+__device__ __forceinline__ float product_of(float a, float b)
+{
+#pragma clang fp contract(off)
+    return a * b;
+}
+
 // Up to V consecutive columns of a range of `width`.  Where the range ends inside a piece the piece begins earlier, and what the one
 // before has is not its own; ranges of fewer than V columns are read singly.
 struct Columns {
@@ -285,8 +292,8 @@ __global__ void __launch_bounds__(kBlock) k_norm_grad_units(NormArgs a, int64_t 
             slopes_at(slope, a.activation);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float dy = value_of_words<T>(dw[p], i) * slope[i];
-                g[p][i] = dy * gamma[i];
+                const float dy = product_of(value_of_words<T>(dw[p], i), slope[i]);
+                g[p][i] = product_of(dy, gamma[i]);
                 if (kWhole || (i >= c[p].skip && i < c[p].end)) {
                     m1 += g[p][i];
                     m2 += g[p][i] * h[p][i];
@@ -778,7 +785,7 @@ __global__ void __launch_bounds__(kBlock) k_norm_grad_short(NormArgs a, int32_t 
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (i >= c.skip && i < c.end) {
-                s_dy[r * b.width + c.first + i] = value_of_words<T>(d, i) * slope[i];
+                s_dy[r * b.width + c.first + i] = product_of(value_of_words<T>(d, i), slope[i]);
                 s_h[r * b.width + c.first + i] = h[i];
             }
     });
@@ -817,7 +824,7 @@ __global__ void __launch_bounds__(kBlock) k_norm_grad_short(NormArgs a, int32_t 
 #pragma unroll 4
         for (int32_t i = lane; i < n; i += lanes) {
             const int32_t at = place(i);
-            const float g = s_dy[at] * (gamma ? gamma[i - b.group_of(i) * b.w] : 1.f);
+            const float g = product_of(s_dy[at], gamma ? gamma[i - b.group_of(i) * b.w] : 1.f);
             m1 += g;
             m2 += g * s_h[at];
         }
@@ -833,7 +840,7 @@ __global__ void __launch_bounds__(kBlock) k_norm_grad_short(NormArgs a, int32_t 
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int32_t column = min(c.first + i, b.width - 1), j = unit + b.group_of(column), at = r * b.width + column;
-            dx[i] = stats[j].y * (s_dy[at] * gamma[i] - s_of[j].x - s_h[at] * s_of[j].y);
+            dx[i] = stats[j].y * (product_of(s_dy[at], gamma[i]) - s_of[j].x - s_h[at] * s_of[j].y);
         }
         store_columns<T, false>(reinterpret_cast<T*>(a.out.data) + ((int64_t) b.first_row + r) * a.out.stride, c, dx);
     });
@@ -944,8 +951,8 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_parts(NormAr
                     slopes_at(slope, a.activation);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const float dy = value_of_words<T>(of.words[1], i) * slope[i];
-                        const float g = dy * gamma[i];
+                        const float dy = product_of(value_of_words<T>(of.words[1], i), slope[i]);
+                        const float g = product_of(dy, gamma[i]);
                         sum1[i] += dy;
                         sum2[i] += dy * h[i];
                         one[kOne ? 0 : i] += g;
@@ -1039,7 +1046,7 @@ __global__ void __launch_bounds__(kBlock, kOne ? 4 : 2) k_norm_grad_apply(NormAr
                 }
                 slopes_at(dx, a.activation);
 #pragma unroll
-                for (int i = 0; i < V; ++i) dx[i] = rstd[kOne ? 0 : i] * (value_of_words<T>(of.words[1], i) * dx[i] * gamma[i] - m1[kOne ? 0 : i] - h[i] * m2[kOne ? 0 : i]);
+                for (int i = 0; i < V; ++i) dx[i] = rstd[kOne ? 0 : i] * (product_of(product_of(value_of_words<T>(of.words[1], i), dx[i]), gamma[i]) - m1[kOne ? 0 : i] - h[i] * m2[kOne ? 0 : i]);
                 store_columns<T, kOne>(reinterpret_cast<T*>(a.out.data) + r * a.out.stride, b.c, dx);
             });
     }

@@ -470,3 +470,23 @@ def test_norm_of_short_segments(ctx, rows, width, groups, per, dtype):  # noqa: 
     for act in (1, 3):
         check_norm(ctx, x, groups, act, segment_rows=per, gamma=gamma, beta=beta, inplace=act == 3)
         check_norm_grad(ctx, x, d_out, groups, act, segment_rows=per, gamma=gamma, beta=beta)
+
+
+@TYPES
+@pytest.mark.parametrize("rows,width,how", [(53, 19, dict()), (53, 64, dict()), (53, 19, dict(segments=True)), (53, 64, dict(segments=True)), (40, 2600, dict(segments=True)), (1, 19, dict(segment_rows=7)),
+                                            (1, 2600, dict(segment_rows=7))])
+def test_the_gradient_of_a_group_of_one_value_is_zero(ctx, rows, width, how, dtype):  # noqa: F811
+    """x is its mean whatever it is; what rounding leaves would be multiplied by 1 / sqrt(eps)."""
+    g = gen(rows, width, len(how))
+    x, d_out = torch.randn(rows, width, generator=g).to(dtype).cuda(), torch.randn(rows, width, generator=g).to(dtype).cuda()
+    gamma, beta = (t.cuda() for t in parameters(width, g))
+    if "segments" in how:
+        how = dict(segments=torch.arange(rows + 1, dtype=torch.int32, device="cuda"))
+    for act in range(4):
+        norm = layers.Norm(width, activation=act, gamma=gamma, beta=beta, **how)
+        sizes = [layers.gns_group_norm_workspace_bytes(ctx, width, norm, rows), layers.gns_group_norm_backward_workspace_bytes(ctx, width, norm, rows)]
+        space = layers.alloc_workspace(max(sizes))
+        stats, out, dx = torch.empty(rows, width, 2, device="cuda"), torch.empty_like(x), torch.full_like(x, 7.0)
+        layers.gns_group_norm(ctx, x, norm, out, stats, rows, space)
+        layers.gns_group_norm_backward(ctx, d_out, x, norm, stats, dx, None, None, rows, space)
+        assert torch.equal(stats[..., 0], x.float()) and bool((dx == 0).all())
